@@ -287,6 +287,94 @@ int mc_expert_significance_host(const int32_t *idx, const float *w, const uint8_
 int mc_pmq_allocate(const double *phi, const double *wact, const double *eps, int E, int bits_total, double alpha,
                     double beta, double gamma, int8_t *bits_out, double *objective_out);
 
+/* ------------------------------------------------------------------------ *
+ * The attention half of a decoder layer, in serving form: a paged key-value cache,
+ * the append of new tokens to it, and their attention over it.  The MoE block above is
+ * the other half (Sec. 3.1: the Mixtral models' layers); the paper leaves attention as
+ * it is, so these calls have no passage of their own.
+ *
+ * Cache: keys and values in pages, element (page, head, row, d) at
+ *   page * page_stride + (head * page_size + row) * head_dim + d.
+ * Row r of a sequence lies in row r % page_size of its page table[r / page_size].
+ * Rows that no token was written to may hold anything, NaN included.
+ * ------------------------------------------------------------------------ */
+enum { MC_BF16 = 0, MC_FP16 = 1 };
+
+typedef struct {
+    void *k, *v;          /* device, 16-byte aligned */
+    int64_t page_stride;  /* elements from page to page, >= kv_heads * page_size * head_dim, a multiple of 8 */
+    int32_t num_pages, page_size; /* page_size: a multiple of 16, at most 32768 */
+    int32_t kv_heads, head_dim;   /* head_dim 64 or 128 */
+    int32_t dtype;                /* MC_BF16 or MC_FP16: the cache's, the queries' and the outputs' */
+} mc_kv_cache;
+
+/* The tokens of one call.  Sequence b has n_b new tokens, rows cu_q[b] .. cu_q[b+1]-1 of
+ * the call's token arrays (cu_q ascending from 0); with cu_q NULL one each, row b.
+ * lens[b] is its length WITH them: new token i has position p = lens[b] - n_b + i.
+ * A token with p < 0 (an idle slot has lens[b] = 0) has no position: it is not
+ * appended and sees no key.  Rows from cu_q[seqs] on are padding: nothing of theirs is
+ * read or written.  table[b * table_width + i], i < ceil(lens[b] / page_size), are b's
+ * pages; other entries are not read.  A page outside [0, num_pages) (its rows are not
+ * written, and read as zeros), a length beyond table_width pages (cut to them), a cu_q that
+ * descends or passes tokens (that sequence has no tokens) and a position outside the rope
+ * table (as none) are recorded as MC_ERR_RANGE in the workspace's status word
+ * (mc_check_status). */
+typedef struct {
+    const int32_t *lens, *table, *cu_q; /* device; cu_q may be NULL */
+    int32_t seqs, tokens, table_width;  /* tokens: rows of the token arrays (= seqs when cu_q is NULL) */
+} mc_kv_batch;
+
+/* Workspace bytes of the three calls below for a cache and a head count, whatever the
+ * batch.  Zeroed once by the caller; the status word comes first.  Calls that share one
+ * must not overlap in time. */
+size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads);
+
+/* New tokens into the cache, in one pass over their queries, keys and values:
+ *   norm    (q_norm / k_norm, [head_dim] in the cache's dtype, NULL: none)
+ *           x / sqrt(mean(x^2) + eps) * norm, per head
+ *   rotate  (rope fp32 [rope_rows][rot_dim]: rot_dim/2 cosines, then as many sines, of each
+ *           position; rot_dim a multiple of 16 up to head_dim, 0: none): pair i of the
+ *           first rot_dim elements turns as (a c - b s, b c + a s); the pair is elements
+ *           (i, i + rot_dim/2), or (2i, 2i + 1) with `interleaved`
+ *   write   queries to q_out [tokens][q_heads][head_dim] (contiguous), keys and values
+ *           (these neither normed nor rotated) to the cache
+ * q, k, v: the cache's dtype, heads of a token contiguous, token strides in elements
+ * (multiples of 8), 16-byte aligned: slices of one projection's output do.  Arithmetic in
+ * fp32, rounded once.  A token without a position gets a zero q_out row.  q_out may be q itself
+ * where q is contiguous.  Two tokens of a call must not name the same row of a page.
+ * workspace (may be NULL): for the status word alone. */
+int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
+                 int64_t k_stride, const void *v, int64_t v_stride, int q_heads, const void *q_norm,
+                 const void *k_norm, float eps, const float *rope, int rope_rows, int rot_dim, int interleaved,
+                 void *q_out, void *workspace, void *stream);
+
+/* What a query's scores go through.  With x = scale * (q . k_j):
+ *   softcap > 0   x <- softcap * tanh(x / softcap)
+ *   slopes        (fp32 [q_heads], NULL: none) x <- x + slopes[head] * (j - p)
+ * and the query at position p sees key j of its sequence iff
+ *   (j <= p or j < prefix[b]) and (window == 0 or j > p - window) and j < lens[b]
+ * prefix (int32 [seqs], NULL: none; mc_attn_prefill only): keys that every query sees. */
+typedef struct {
+    float scale, softcap;
+    int32_t window;
+    const float *slopes;
+    const int32_t *prefix;
+} mc_attn_opts;
+
+/* Attention of the batch's new tokens over the cache (which already holds them): query
+ * head h reads key head h / (q_heads / kv_heads).
+ *   out [token][q_heads][head_dim] (token stride out_stride) = softmax over the visible keys . v
+ *   lse fp32 [tokens][q_heads] (may be NULL): log of the sum of exponentials
+ * A query that sees no key gets a zero row and lse = -inf.  Scores, statistics and sums
+ * are fp32; the probabilities are rounded to the cache's dtype for their product with v.
+ * mc_attn_decode takes one new token per sequence (cu_q NULL), mc_attn_prefill any number. */
+int mc_attn_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                   const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                   size_t ws_bytes, void *stream);
+int mc_attn_prefill(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                    const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                    size_t ws_bytes, void *stream);
+
 /* Test hook: choose the expert path of mc_moe_forward: 0 = automatic (the GEMV
  * below 240 kept-or-not pairs, 2T < 240, else the GEMM), 1 = the mma.sync
  * grouped GEMV with work chunks of 16 pairs (decode), 2 = the tcgen05 grouped
@@ -331,7 +419,7 @@ int mc_check_status(void *workspace, void *stream);
  * synchronises on the recorded events, writes the summed milliseconds and launch
  * counts of kernel ids 0 .. n-1 (names from mc_profile_name: route, permute,
  * gemv_w13, gemv_w2, combine, frag_x, gemm_w13, gemm_w2, rmsnorm, importance,
- * x_img) and
+ * x_img, kv_append, attn_decode, attn_prefill, attn_join) and
  * clears the records.  Inside stream capture the events become event nodes of
  * the graph: every replay records them again, and each mc_profile_read reports
  * the latest replay and keeps those records until mc_profile_clear. */

@@ -48,6 +48,7 @@ def load():
                           "or `python paper_2410_06270_gb300/build.py`")
     lib = ctypes.CDLL(LIB_PATH)
     P, I, Z, F32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
+    L = ctypes.c_int64
     S = ctypes.POINTER(Shape)
     sig = {
         "mc_last_error": (ctypes.c_char_p, []),
@@ -77,6 +78,10 @@ def load():
         "mc_odp_threshold_host": (I, [P, P, I, ctypes.c_double, P]),
         "mc_expert_significance_host": (I, [P, P, P, I, I, P, P]),
         "mc_pmq_allocate": (I, [P, P, P, I, I, ctypes.c_double, ctypes.c_double, ctypes.c_double, P, P]),
+        "mc_attn_workspace_size": (Z, [P, I]),
+        "mc_kv_append": (I, [P, P, P, L, P, L, P, L, I, P, P, F32, P, I, I, I, P, P, P]),
+        "mc_attn_decode": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
+        "mc_attn_prefill": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
         "mc_profile_enable": (I, [I]),
         "mc_profile_select": (ctypes.c_uint, [ctypes.c_uint]),
         "mc_profile_read": (I, [P, P, I]),
@@ -375,9 +380,177 @@ def add(a, b, out=None):
     return out
 
 
+# ---------------------------------------------------------------- attention --
+
+class _KvCacheC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class _KvBatchC(ctypes.Structure):
+    _fields_ = [("lens", ctypes.c_void_p), ("table", ctypes.c_void_p), ("cu_q", ctypes.c_void_p),
+                ("seqs", ctypes.c_int32), ("tokens", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class _AttnOptsC(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p), ("prefix", ctypes.c_void_p)]
+
+
+def _bad(msg):
+    raise MCError(ERR_INVALID_ARG, msg)
+
+
+class KVCache:
+    """A paged key-value cache over the caller's tensors k and v, both [pages, kv_heads,
+    page_size, head_dim] in bf16 or fp16.  Pages may be strided (one layer of a larger
+    allocation, or keys and values of a page side by side); the rest is contiguous."""
+
+    def __init__(self, k, v):
+        import torch
+        codes = {torch.bfloat16: 0, torch.float16: 1}
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+            _bad("k and v must be alike: [pages, kv_heads, page_size, head_dim]")
+        if k.dtype not in codes:
+            raise MCError(ERR_UNSUPPORTED, "cache of %s" % k.dtype)
+        pages, heads, size, dim = k.shape
+        if k.stride()[1:] != (size * dim, dim, 1):
+            _bad("the heads of a page must be contiguous")
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        self.kv_heads, self.page_size, self.head_dim = heads, size, dim
+        stride = k.stride(0) if pages > 1 else max(k.stride(0), heads * size * dim)
+        self._c = _KvCacheC(k.data_ptr(), v.data_ptr(), stride, pages, size, heads, dim, codes[k.dtype])
+        self._ref = ctypes.addressof(self._c)
+
+
+class KVBatch:
+    """The tokens of one call: lens int32 [seqs] (lengths WITH the new tokens), table int32
+    [seqs, width] (pages), cu_q int32 [seqs + 1] (rows of each sequence's new tokens; None:
+    one each).  tokens: rows of the token arrays, padding included, where cu_q is given.
+    Device tensors, read when the calls run."""
+
+    def __init__(self, lens, table, cu_q=None, tokens=None):
+        import torch
+        if lens.dim() != 1 or table.dim() != 2 or table.shape[0] != lens.shape[0]:
+            _bad("lens [seqs] and table [seqs, width]")
+        if cu_q is not None and (cu_q.dim() != 1 or cu_q.shape[0] != lens.shape[0] + 1 or tokens is None):
+            _bad("cu_q [seqs + 1] and tokens")
+        for t in (lens, table, cu_q):
+            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != lens.device):
+                _bad("lens, table and cu_q must be contiguous int32 on one device")
+        self._keep = (lens, table, cu_q)
+        self.device = lens.device
+        self.seqs = lens.shape[0]
+        self.tokens = self.seqs if tokens is None else int(tokens)
+        self._c = _KvBatchC(lens.data_ptr(), table.data_ptr(), _ptr(cu_q), self.seqs, self.tokens, table.shape[1])
+        self._ref = ctypes.addressof(self._c)
+
+
+def _rows(name, t, cache, batch, heads=None):
+    """Token stride of t [tokens, heads, head_dim] (heads contiguous)."""
+    sh, st = t.shape, t.stride()
+    if len(sh) != 3 or sh[0] != batch.tokens or sh[2] != cache.head_dim or (heads is not None and sh[1] != heads):
+        _bad("%s must be [tokens, heads, head_dim], got %s" % (name, tuple(sh)))
+    if t.dtype != cache.dtype or t.device != cache.device or batch.device != cache.device:
+        _bad("%s, the batch and the cache must share a device, %s and the cache a dtype" % (name, name))
+    if st[2] != 1 or (sh[1] > 1 and st[1] != sh[2]):
+        _bad("%s: the heads of a token must be contiguous" % name)
+    return st[0] if sh[0] > 1 else max(st[0], sh[1] * sh[2])
+
+
+def _side(name, t, cache, dtype, shape):
+    """Pointer of a contiguous side input, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != cache.device:
+        _bad("%s must be a contiguous %s tensor %s on the cache's device" % (name, dtype, shape))
+    return t.data_ptr()
+
+
+def attn_workspace(cache: KVCache, q_heads: int):
+    """Zeroed workspace of attn_decode / attn_prefill (and the status word of kv_append)
+    for a cache and a number of query heads, whatever the batch."""
+    import torch
+    n = load().mc_attn_workspace_size(cache._ref, int(q_heads))
+    if n == 0:
+        raise MCError(ERR_INVALID_ARG, last_error())
+    return torch.zeros(n, dtype=torch.uint8, device=cache.device)
+
+
+def kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope=None, interleaved: bool = False, q_norm=None, k_norm=None,
+              eps: float = 1e-6, q_out=None, workspace=None):
+    """New tokens into the cache, in one pass: q and k [tokens, heads, head_dim] normed per
+    head (q_norm / k_norm [head_dim], None: not) and rotated (rope fp32 [positions,
+    rot_dim]: rot_dim/2 cosines, then sines; None: not), k and v written to their pages.
+    Returns the queries [tokens, q_heads, head_dim].  q, k, v may be slices of one
+    projection's output."""
+    import torch
+    heads = q.shape[1] if q.dim() == 3 else -1
+    qs = _rows("q", q, cache, batch)
+    ks = _rows("k", k, cache, batch, cache.kv_heads)
+    vs = _rows("v", v, cache, batch, cache.kv_heads)
+    if q_out is None:
+        q_out = torch.empty((batch.tokens, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+    elif not q_out.is_contiguous():
+        _bad("q_out must be contiguous")
+    else:
+        _rows("q_out", q_out, cache, batch, heads)
+    rows = rot = 0
+    if rope is not None:
+        if rope.dim() != 2 or rope.dtype != torch.float32 or not rope.is_contiguous() or rope.device != cache.device:
+            _bad("rope must be a contiguous fp32 [positions, rot_dim] on the cache's device")
+        rows, rot = rope.shape
+    dim = (cache.head_dim,)
+    _check(load().mc_kv_append(cache._ref, batch._ref, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, heads,
+                               _side("q_norm", q_norm, cache, cache.dtype, dim),
+                               _side("k_norm", k_norm, cache, cache.dtype, dim), eps, _ptr(rope), rows, rot,
+                               1 if interleaved else 0, q_out.data_ptr(), _ptr(workspace), _stream()))
+    return q_out
+
+
+def _attention(fn, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace):
+    import torch
+    qs = _rows("q", q, cache, batch)
+    heads = q.shape[1]
+    if out is None:
+        out = torch.empty((batch.tokens, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+    os_ = _rows("out", out, cache, batch, heads)
+    if workspace is None:
+        workspace = attn_workspace(cache, heads)
+    elif workspace.device != cache.device:
+        _bad("the workspace must be on the cache's device")
+    lse = torch.empty((batch.tokens, heads), dtype=torch.float32, device=cache.device) if with_lse else None
+    opts = _AttnOptsC(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
+                      _side("slopes", slopes, cache, torch.float32, (heads,)),
+                      _side("prefix", prefix, cache, torch.int32, (batch.seqs,)))
+    _check(fn(cache._ref, batch._ref, q.data_ptr(), qs, heads, ctypes.addressof(opts), out.data_ptr(), os_, _ptr(lse),
+              workspace.data_ptr(), workspace.numel(), _stream()))
+    return (out, lse) if with_lse else out
+
+
+def attn_decode(cache: KVCache, batch: KVBatch, q, scale=None, softcap: float = 0.0, window: int = 0, slopes=None,
+                out=None, with_lse: bool = False, workspace=None):
+    """Attention of one new token per sequence, q [seqs, heads, head_dim], over the cache
+    that already holds it.  scale: head_dim ** -0.5 by default; softcap > 0: scores
+    softcap * tanh(x / softcap); window > 0: the last `window` keys only; slopes fp32
+    [heads]: bias slope * (j - p).  Returns out (and lse fp32 [seqs, heads])."""
+    return _attention(load().mc_attn_decode, cache, batch, q, scale, softcap, window, slopes, None, out, with_lse,
+                      workspace)
+
+
+def attn_prefill(cache: KVCache, batch: KVBatch, q, scale=None, softcap: float = 0.0, window: int = 0, slopes=None,
+                 prefix=None, out=None, with_lse: bool = False, workspace=None):
+    """Causal attention of the batch's new tokens, q [tokens, heads, head_dim], over the
+    cache that already holds them; options as attn_decode's, and prefix int32 [seqs]:
+    leading keys that every query of the sequence sees.  Returns out (and lse)."""
+    return _attention(load().mc_attn_prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse,
+                      workspace)
+
+
 # -------------------------------------------------------------- profiling --
 
-N_KERNELS = 11
+N_KERNELS = 15
 
 
 def token_importance(t, attn, protect_frac: float = 0.02, importance=None, mask=None, with_mask: bool = True,

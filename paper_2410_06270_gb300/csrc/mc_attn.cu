@@ -1,0 +1,250 @@
+// mc_attn.cu -- the entry points of the paged cache and its attention: argument checks,
+// workspace and dispatch; and the plain attention kernel.
+#include <math.h>
+
+#include "mc_attn.h"
+#include "mc_host.h"
+#include "mc_profile.h"
+
+namespace mc {
+
+// One warp per (token, head), key by key with a running maximum and sum.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(128) attn_kernel(const AttnParams p)
+{
+    constexpr int kPer = D / 64;  // 32-bit words a lane holds of a row
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (w >= (int64_t)p.b.tokens * p.q_heads) return;
+    const int t = (int)(w / p.q_heads), h = (int)(w % p.q_heads), kh = h / p.group;
+    const int s = token_seq(p.b, t, lane);
+    if (s < 0) return;
+    int first;
+    const int n = seq_rows(p.b, s, first, p.status);
+    if (t < first || t - first >= n) return;
+    const int len = seq_len(p.b, p.c, s, p.status), pos = len - n + (t - first);
+    float2 q[kPer], o[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        q[e] = unpack2<BF16>(*reinterpret_cast<const uint32_t *>(p.q + t * p.q_stride + h * D + 2 * (lane * kPer + e)));
+        o[e] = make_float2(0.f, 0.f);
+    }
+    float m = -INFINITY, l = 0.f;
+    int end = pos + 1, j = 0;
+    if (p.prefix) end = max(end, __ldg(p.prefix + s));
+    end = min(end, len);
+    if (p.window) j = max(0, pos - p.window + 1);
+    const float slope = p.slopes ? __ldg(p.slopes + h) : 0.f;
+    if (pos < 0) end = 0;
+    for (; j < end; ++j) {
+        const int page = seq_page(p.b, p.c, s, j / p.c.page_size, p.status);
+        const int64_t at = page * p.c.page_stride + ((int64_t)kh * p.c.page_size + j % p.c.page_size) * D;
+        float x = 0.f;
+        float2 v[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int64_t i = at + 2 * (lane * kPer + e);
+            const float2 k = unpack2<BF16>(page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(p.c.k + i));
+            v[e] = unpack2<BF16>(page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(p.c.v + i));
+            x = fmaf(q[e].x, k.x, fmaf(q[e].y, k.y, x));
+        }
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        x *= p.scale;
+        if (p.softcap > 0.f) x = capped(x, p.softcap);
+        x = (x + slope * (float)(j - pos)) * kLog2e;
+        const float top = fmaxf(m, x), keep = top == m ? 1.f : ex2(m - top), pr = ex2(x - top);
+        m = top;
+        l = fmaf(l, keep, pr);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = make_float2(fmaf(o[e].x, keep, pr * v[e].x), fmaf(o[e].y, keep, pr * v[e].y));
+    }
+    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        *reinterpret_cast<uint32_t *>(p.out + t * p.out_stride + h * D + 2 * (lane * kPer + e)) =
+            pack2<BF16>(o[e].x * inv, o[e].y * inv);
+    if (p.lse && lane == 0) p.lse[w] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+int launch_attn(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st)
+{
+    const int64_t ctas = ((int64_t)p.b.tokens * p.q_heads + 3) / 4;
+    if (ctas > 0x7fffffff) return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d heads in one call", p.b.tokens, p.q_heads);
+    auto k = head_dim == 64 ? (bf16 ? attn_kernel<64, true> : attn_kernel<64, false>)
+                            : (bf16 ? attn_kernel<128, true> : attn_kernel<128, false>);
+    cudaError_t e = launch_k(k, dim3((unsigned)ctas), dim3(128), 0, st, p);
+    if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "attention launch: %s", cudaGetErrorString(e));
+    return MC_OK;
+}
+
+static int check_cache(const mc_kv_cache *c, int q_heads)
+{
+    if (!c) return set_error(MC_ERR_INVALID_ARG, "NULL cache");
+    if (c->dtype != MC_BF16 && c->dtype != MC_FP16) return set_error(MC_ERR_UNSUPPORTED, "cache dtype %d", c->dtype);
+    if (c->head_dim != 64 && c->head_dim != 128)
+        return set_error(MC_ERR_UNSUPPORTED, "head_dim %d (64 or 128)", c->head_dim);
+    if (c->kv_heads < 1 || c->kv_heads > 1024 || q_heads < c->kv_heads || q_heads > 4096 || q_heads % c->kv_heads)
+        return set_error(MC_ERR_INVALID_ARG, "%d query heads on %d key heads", q_heads, c->kv_heads);
+    if (c->page_size < 16 || c->page_size > 32768 || c->page_size % 16)
+        return set_error(MC_ERR_INVALID_ARG, "page_size %d (a multiple of 16, at most 32768)", c->page_size);
+    if (c->num_pages < 1) return set_error(MC_ERR_INVALID_ARG, "num_pages %d", c->num_pages);
+    if (c->page_stride % 8 || c->page_stride < (int64_t)c->kv_heads * c->page_size * c->head_dim)
+        return set_error(MC_ERR_INVALID_ARG, "page_stride %lld", (long long)c->page_stride);
+    return MC_OK;
+}
+
+static int check_batch(const mc_kv_cache *c, const mc_kv_batch *b)
+{
+    if (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16))
+        return set_error(MC_ERR_INVALID_ARG, "cache pointers must be 16-byte aligned");
+    if (!b->lens || !b->table) return set_error(MC_ERR_INVALID_ARG, "NULL pointer argument");
+    if (!aligned(b->lens, 4) || !aligned(b->table, 4) || !aligned(b->cu_q, 4))
+        return set_error(MC_ERR_INVALID_ARG, "misaligned batch pointer");
+    if (b->table_width < 1) return set_error(MC_ERR_INVALID_ARG, "table_width %d", b->table_width);
+    if (!b->cu_q && b->tokens != b->seqs)
+        return set_error(MC_ERR_INVALID_ARG, "%d tokens of %d sequences need cu_q", b->tokens, b->seqs);
+    return MC_OK;
+}
+
+// A batch's token count: 0 and no error for an empty one.
+static int check_counts(const mc_kv_batch *b)
+{
+    if (!b) return set_error(MC_ERR_INVALID_ARG, "NULL batch");
+    if (b->seqs < 0 || b->tokens < 0) return set_error(MC_ERR_INVALID_ARG, "seqs %d, tokens %d", b->seqs, b->tokens);
+    return MC_OK;
+}
+
+static int check_rows(const char *what, const void *p, int64_t stride, int heads, int D)
+{
+    if (!p || !aligned(p, 16)) return set_error(MC_ERR_INVALID_ARG, "%s must be 16-byte aligned", what);
+    if (stride % 8 || stride < (int64_t)heads * D)
+        return set_error(MC_ERR_INVALID_ARG, "%s: token stride %lld", what, (long long)stride);
+    return MC_OK;
+}
+
+static KvView view(const mc_kv_cache *c)
+{
+    return {(uint16_t *)c->k, (uint16_t *)c->v, c->page_stride, c->num_pages, c->page_size, c->kv_heads};
+}
+
+static BatchView view(const mc_kv_batch *b)
+{
+    return {b->lens, b->table, b->cu_q, b->seqs, b->tokens, b->table_width};
+}
+
+static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                     const mc_attn_opts *o, void *out, int64_t out_stride, float *lse, void *workspace, size_t ws_bytes,
+                     bool decode, void *stream)
+{
+    clear_error();
+    int rc = check_cache(cache, q_heads);
+    if (rc || (rc = check_counts(batch))) return rc;
+    if (!o) return set_error(MC_ERR_INVALID_ARG, "NULL options");
+    if (!isfinite(o->scale) || !(o->softcap >= 0.f) || !isfinite(o->softcap) || o->window < 0)
+        return set_error(MC_ERR_INVALID_ARG, "scale %g, softcap %g, window %d", o->scale, o->softcap, o->window);
+    if (decode && batch->cu_q) return set_error(MC_ERR_INVALID_ARG, "one token per sequence: cu_q must be NULL");
+    if (decode && o->prefix) return set_error(MC_ERR_INVALID_ARG, "a prefix is mc_attn_prefill's");
+    if (batch->tokens == 0 || batch->seqs == 0) return MC_OK;
+    if ((rc = check_batch(cache, batch))) return rc;
+    if ((rc = check_rows("q", q, q_stride, q_heads, cache->head_dim))) return rc;
+    if ((rc = check_rows("out", out, out_stride, q_heads, cache->head_dim))) return rc;
+    if (!aligned(lse, 4) || !aligned(o->slopes, 4) || !aligned(o->prefix, 4))
+        return set_error(MC_ERR_INVALID_ARG, "misaligned lse, slopes or prefix");
+    if (!workspace || !aligned(workspace, 256)) return set_error(MC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    const size_t need = mc_attn_workspace_size(cache, q_heads);
+    if (ws_bytes < need) return set_error(MC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", ws_bytes, need);
+    AttnParams p = {};
+    p.c = view(cache);
+    p.b = view(batch);
+    p.q = (const uint16_t *)q;
+    p.q_stride = q_stride;
+    p.q_heads = q_heads;
+    p.group = q_heads / cache->kv_heads;
+    p.softcap = o->softcap;
+    p.scale = o->softcap > 0.f ? o->scale / o->softcap : o->scale;
+    p.window = o->window;
+    p.slopes = o->slopes;
+    p.prefix = o->prefix;
+    p.out = (uint16_t *)out;
+    p.out_stride = out_stride;
+    p.lse = lse;
+    p.status = (int32_t *)workspace;
+    p.part = (uint8_t *)workspace + 256;
+    return launch_attn(p, cache->head_dim, cache->dtype == MC_BF16, (cudaStream_t)stream);
+}
+
+}  // namespace mc
+
+using namespace mc;
+
+extern "C" {
+
+size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads)
+{
+    clear_error();
+    if (check_cache(cache, q_heads)) return 0;
+    return 256;
+}
+
+int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
+                 int64_t k_stride, const void *v, int64_t v_stride, int q_heads, const void *q_norm,
+                 const void *k_norm, float eps, const float *rope, int rope_rows, int rot_dim, int interleaved,
+                 void *q_out, void *workspace, void *stream)
+{
+    clear_error();
+    int rc = check_cache(cache, q_heads);
+    if (rc || (rc = check_counts(batch))) return rc;
+    const int D = cache->head_dim;
+    if (rot_dim < 0 || rot_dim > D || rot_dim % 16)
+        return set_error(MC_ERR_INVALID_ARG, "rot_dim %d (a multiple of 16 up to head_dim %d)", rot_dim, D);
+    if (rot_dim && (!rope || !aligned(rope, 16) || rope_rows < 1))
+        return set_error(MC_ERR_INVALID_ARG, "rope must be 16-byte aligned and have rows");
+    if (!(eps >= 0.f) || !isfinite(eps)) return set_error(MC_ERR_INVALID_ARG, "eps %g", eps);
+    if (batch->tokens == 0 || batch->seqs == 0) return MC_OK;
+    if ((rc = check_batch(cache, batch))) return rc;
+    if ((rc = check_rows("q", q, q_stride, q_heads, D)) || (rc = check_rows("k", k, k_stride, cache->kv_heads, D)) ||
+        (rc = check_rows("v", v, v_stride, cache->kv_heads, D)) ||
+        (rc = check_rows("q_out", q_out, (int64_t)q_heads * D, q_heads, D)))
+        return rc;
+    if (!aligned(q_norm, 8) || !aligned(k_norm, 8) || !aligned(workspace, 4))
+        return set_error(MC_ERR_INVALID_ARG, "misaligned norm or workspace");
+    AppendParams p = {};
+    p.c = view(cache);
+    p.b = view(batch);
+    p.q = (const uint16_t *)q;
+    p.k = (const uint16_t *)k;
+    p.v = (const uint16_t *)v;
+    p.q_stride = q_stride;
+    p.k_stride = k_stride;
+    p.v_stride = v_stride;
+    p.q_heads = q_heads;
+    p.q_norm = (const uint16_t *)q_norm;
+    p.k_norm = (const uint16_t *)k_norm;
+    p.eps = eps;
+    p.rope = rope;
+    p.rope_rows = rope_rows;
+    p.rot = rot_dim;
+    p.interleaved = interleaved != 0;
+    p.q_out = (uint16_t *)q_out;
+    p.status = (int32_t *)workspace;
+    return launch_append(p, D, cache->dtype == MC_BF16, (cudaStream_t)stream);
+}
+
+int mc_attn_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                   const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                   size_t ws_bytes, void *stream)
+{
+    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, true, stream);
+}
+
+int mc_attn_prefill(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                    const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                    size_t ws_bytes, void *stream)
+{
+    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, false, stream);
+}
+
+}  // extern "C"

@@ -20,7 +20,8 @@ std::vector<Rec> g_recs;
 std::vector<cudaEvent_t> g_pool;
 cudaEvent_t g_pending[kKCount];
 const char *g_names[kKCount] = {"route", "permute", "gemv_w13", "gemv_w2", "combine",
-                                "frag_x", "gemm_w13", "gemm_w2", "rmsnorm", "importance", "x_img"};
+                                "frag_x", "gemm_w13", "gemm_w2", "rmsnorm", "importance", "x_img", "kv_append", "attn_decode",
+                                "attn_prefill", "attn_join"};
 
 // An event record on st; inside stream capture it becomes an event node of the
 // graph, so every replay of the graph records it again.

@@ -17,6 +17,10 @@ enum KernelId {
     kKRmsnorm,
     kKImportance,
     kKXImg,       // prefill path: activations -> SW128 images
+    kKAppend,     // new tokens into the key-value cache
+    kKAttnDecode,
+    kKAttnPrefill,
+    kKAttnJoin,   // partial results of items split over the cache's length
     kKCount
 };
 

@@ -1,0 +1,278 @@
+"""The paged cache's append and the two attentions over it against their definitions in
+64 bits: head layouts, types, page sizes, lengths around every tile's edges, empty rows,
+masks, strides, NaN where nothing was written, streams, graphs and repeated calls."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import attn_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mc():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2410_06270_gb300 import build
+    build.build()
+    import paper_2410_06270_gb300 as m
+    m.load()
+    m.set_debug(0, 1_000_000_000)
+    return m
+
+
+EDGES = [0, 1, 2, 15, 16, 17, 31, 63, 64, 65, 100, 127, 128, 129, 255, 257, 700]
+
+
+# ---------------------------------------------------------------- append --
+
+@pytest.mark.parametrize("heads,kv,dim,dtype,page,rot,interleaved,norm,ragged", [
+    (32, 8, 128, "bf16", 16, 128, False, False, False),
+    (12, 4, 64, "fp16", 48, 32, True, True, True),
+    (5, 1, 128, "bf16", 64, 64, False, True, True),
+    (3, 3, 64, "bf16", 16, 64, False, False, True),
+    (7, 7, 128, "fp16", 32, 16, True, False, False),
+    (16, 2, 128, "fp16", 128, 0, False, True, True),
+    (1, 1, 64, "bf16", 16, 16, False, True, False),
+])
+def test_append_matches_its_definition(mc, heads, kv, dim, dtype, page, rot, interleaved, norm, ragged):
+    lens = [0, 1, page, page + 1, 100, 5 * page - 1, 3]
+    new = [0, 1, page, 2, 100, 33, 5] if ragged else [1] * len(lens)  # the last: more new tokens than its length
+    B = ref.Batch(lens, new, kv, page, dim, dtype, 11, pad_tokens=3 if ragged else 0)
+    qkv = B.randn(B.tokens, (heads + 2 * kv) * dim + 8)  # a row's tail is not the call's
+    cut = lambda x, a, n: x[:, a * dim:(a + n) * dim].unflatten(1, (n, dim))  # noqa: E731
+    qn, kn = ((1 + 0.1 * B.randn(dim)).to(ref.DT[dtype]) for _ in range(2)) if norm else (None, None)
+    rope = ref.rope_table(600, rot) if rot else None
+    parts = [cut(qkv, 0, heads), cut(qkv, heads, kv), cut(qkv, heads + kv, kv)]
+    want = ref.append(B, *parts, rope, interleaved, qn, kn)
+    cache, batch = B.device(mc, cu=ragged)
+    ws = mc.attn_workspace(cache, heads)
+    dev = qkv.cuda()
+    up = lambda t: None if t is None else t.cuda()  # noqa: E731
+    q_out = torch.full((B.tokens, heads, dim), 7.0, dtype=ref.DT[dtype], device="cuda")
+    q = mc.kv_append(cache, batch, cut(dev, 0, heads), cut(dev, heads, kv), cut(dev, heads + kv, kv), rope=up(rope),
+                     interleaved=interleaved, q_norm=up(qn), k_norm=up(kn), q_out=q_out, workspace=ws)
+    mc.check_status(ws)
+    assert q.data_ptr() == q_out.data_ptr()
+    n = B.cu[-1]
+    assert (q[n:] == 7).all()  # padding is left alone
+    # one rounding of a value formed in fp32 (a few units of 2^-24 of the pair's larger member)
+    for got, ex in ((q[:n], want[0][:n]), (cache.k, want[1]), (cache.v, want[2])):
+        got = got.double().cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(ex))
+        ok = ~torch.isnan(ex)
+        assert ((got - ex)[ok].abs() <= ref.HALF_ULP[dtype] * ex[ok].abs() + 2.0 ** -20 * 8 + (2.0 ** -24 if dtype == "fp16" else 0)).all()
+    assert torch.equal(torch.nan_to_num(cache.v.cpu()), torch.nan_to_num(want[2].to(ref.DT[dtype])))  # copied bits
+
+
+def test_append_in_place_and_long_offsets(mc):
+    """q_out may be q; a page far into a strided pool lies past 2^31 elements."""
+    B = ref.Batch([70], [70], 2, 64, 64, "bf16", 3, spare=0)
+    big = torch.zeros((1 << 31) // 4 * 5 // 4 + (1 << 20), dtype=torch.int64, device="cuda").view(torch.bfloat16)
+    stride = (1 << 31) + 1024
+    k = big.as_strided((2, 2, 64, 64), (stride, 64 * 64, 64, 1))
+    v = big.as_strided((2, 2, 64, 64), (stride, 64 * 64, 64, 1), 64 * 64 * 2)
+    cache = mc.KVCache(k, v)
+    batch = mc.KVBatch(torch.tensor([70], dtype=torch.int32).cuda(), B.table.cuda(),
+                       torch.tensor([0, 70], dtype=torch.int32).cuda(), 70)
+    x = B.randn(3, 70, 2, 64)
+    rope = ref.rope_table(70, 64)
+    want = ref.append(B, x[0], x[1], x[2], rope)
+    q = x[0].cuda()
+    got = mc.kv_append(cache, batch, q, x[1].cuda(), x[2].cuda(), rope=rope.cuda(), q_out=q)
+    assert got.data_ptr() == q.data_ptr()
+    assert (got.double().cpu() - want[0]).abs().max() <= 2.0 ** -8 * want[0].abs().max() + 1e-5
+    for c, w in ((k, want[1]), (v, want[2])):
+        ok = ~torch.isnan(w)
+        assert ((c.double().cpu() - w)[ok].abs() <= 2.0 ** -8 * w[ok].abs() + 1e-5).all()
+    q2 = x[0].cuda()
+    out = mc.attn_prefill(cache, batch, q2)
+    att = ref.Batch([70], [70], 2, 64, 64, "bf16", 3, spare=0)
+    att.k, att.v = k.cpu(), v.cpu()
+    w = ref.attention(att, x[0], 64 ** -0.5)
+    ref.assert_attention(out, None, w, "bf16", 70, 5.0)
+
+
+# ---------------------------------------------------------------- decode --
+
+DECODE = [
+    # heads, kv, dim, dtype, page, softcap, window, bias
+    (32, 8, 128, "bf16", 16, 0.0, 0, False),
+    (8, 8, 64, "fp16", 48, 0.0, 0, False),
+    (6, 2, 128, "fp16", 64, 30.0, 0, True),
+    (48, 4, 64, "bf16", 32, 0.0, 50, False),
+    (16, 1, 128, "bf16", 128, 50.0, 129, True),
+    (40, 2, 128, "bf16", 16, 0.0, 1, False),
+    (33, 1, 64, "fp16", 16, 0.0, 0, True),
+    (1, 1, 128, "bf16", 256, 0.0, 0, False),
+]
+
+
+def _slopes(heads):
+    return torch.tensor([2.0 ** (-8.0 * (h + 1) / heads) for h in range(heads)])
+
+
+@pytest.mark.parametrize("heads,kv,dim,dtype,page,softcap,window,bias", DECODE)
+def test_decode_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap, window, bias):
+    B = ref.Batch(EDGES, [1] * len(EDGES), kv, page, dim, dtype, 5, interleave=True)
+    q = 1.5 * B.randn(len(EDGES), heads, dim)
+    sl = _slopes(heads) if bias else None
+    want = ref.attention(B, q, dim ** -0.5, softcap, window, sl)
+    cache, batch = B.device(mc, cu=False, interleave=True)
+    ws = mc.attn_workspace(cache, heads)
+    out, lse = mc.attn_decode(cache, batch, q.cuda(), softcap=softcap, window=window,
+                              slopes=None if sl is None else sl.cuda(), with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    ref.assert_attention(out, lse, want, dtype, max(EDGES), 5.0)
+
+
+@pytest.mark.parametrize("seqs,length,kv,heads", [(1, 5000, 1, 8), (1, 20011, 2, 8), (3, 2049, 8, 32), (300, 40, 1, 2), (1, 1, 1, 1)])
+def test_decode_splits_and_joins(mc, seqs, length, kv, heads):
+    lens = [max(1, length - 37 * b) if seqs < 100 else (b * 7) % length for b in range(seqs)]
+    B = ref.Batch(lens, [1] * seqs, kv, 32, 128, "bf16", 8)
+    q = B.randn(seqs, heads, 128)
+    want = ref.attention(B, q, 0.1)
+    cache, batch = B.device(mc, cu=False)
+    out, lse = mc.attn_decode(cache, batch, q.cuda(), scale=0.1, with_lse=True)
+    ref.assert_attention(out, lse, want, "bf16", length, 5.0)
+    again, _ = mc.attn_decode(cache, batch, q.cuda(), scale=0.1, with_lse=True)
+    assert torch.equal(out, again)  # the same sums in the same order
+
+
+def test_decode_large_scores(mc):
+    """One key far above the others, early or late: running maxima have to move."""
+    for at in (0, 300, 999):
+        B = ref.Batch([1000], [1], 1, 16, 64, "bf16", 9)
+        q = B.randn(1, 4, 64)
+        B.k[B.table[0, at // 16], 0, at % 16] = (q[0, 1] * 20).to(torch.bfloat16)
+        want = ref.attention(B, q, 1.0)
+        cache, batch = B.device(mc, cu=False)
+        out, lse = mc.attn_decode(cache, batch, q.cuda(), scale=1.0, with_lse=True)
+        assert (out.double().cpu() - want[0]).abs().max() <= 2.0 ** -8 * 5 + 2e-2  # scores of hundreds: 1e-5 of them in fp32
+        assert ((lse.double().cpu() - want[1]).abs() <= 1e-5 * want[1].abs() + 1e-4).all()
+
+
+# --------------------------------------------------------------- prefill --
+
+PREFILL = [
+    # heads, kv, dim, dtype, page, softcap, window, bias, prefix
+    (8, 2, 128, "bf16", 16, 0.0, 0, False, False),
+    (4, 4, 64, "fp16", 48, 0.0, 0, False, True),
+    (6, 2, 128, "fp16", 64, 30.0, 0, True, False),
+    (12, 1, 64, "bf16", 32, 0.0, 50, False, False),
+    (5, 1, 128, "bf16", 128, 50.0, 129, True, True),
+    (8, 8, 64, "bf16", 16, 0.0, 1, False, False),
+    (2, 1, 128, "fp16", 256, 0.0, 300, False, True),
+]
+
+
+@pytest.mark.parametrize("heads,kv,dim,dtype,page,softcap,window,bias,prefix", PREFILL)
+def test_prefill_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap, window, bias, prefix):
+    lens = [0, 1, 17, 64, 130, 300, 511, 9, 257]
+    new = [2, 1, 17, 3, 130, 1, 129, 12, 64]  # sequences 0 and 7: more new tokens than their length
+    B = ref.Batch(lens, new, kv, page, dim, dtype, 6, pad_tokens=2)
+    q = 1.5 * B.randn(B.tokens, heads, dim)
+    sl = _slopes(heads) if bias else None
+    pre = [0, 1, 9, 64, 70, 299, 1000, 4, 250] if prefix else None
+    want = ref.attention(B, q, dim ** -0.5, softcap, window, sl, pre)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, heads)
+    out = torch.full((B.tokens, heads + 1, dim), 3.0, dtype=ref.DT[dtype], device="cuda")
+    got, lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=softcap, window=window,
+                               slopes=None if sl is None else sl.cuda(),
+                               prefix=None if pre is None else torch.tensor(pre, dtype=torch.int32).cuda(),
+                               out=out[:, :heads], with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    n = B.cu[-1]
+    assert (out[:, heads] == 3).all() and (out[n:] == 3).all()  # other heads' columns and padding rows
+    ref.assert_attention(got, lse, want, dtype, 512, 5.0, rows=slice(0, n))
+
+
+@pytest.mark.parametrize("new,length,kv,heads,dim", [(1, 4000, 1, 4, 128), (40, 6000, 2, 4, 64), (700, 700, 1, 1, 128),
+                                                     (515, 2100, 2, 6, 128), (1, 1, 1, 1, 64)])
+def test_prefill_splits_and_joins(mc, new, length, kv, heads, dim):
+    B = ref.Batch([length], [new], kv, 64, dim, "bf16", 8)
+    q = B.randn(new, heads, dim)
+    want = ref.attention(B, q, dim ** -0.5)
+    cache, batch = B.device(mc)
+    out, lse = mc.attn_prefill(cache, batch, q.cuda(), with_lse=True)
+    ref.assert_attention(out, lse, want, "bf16", length, 5.0)
+    again, _ = mc.attn_prefill(cache, batch, q.cuda(), with_lse=True)
+    assert torch.equal(out, again)
+
+
+def test_prefill_of_one_token_each_is_decode(mc):
+    """The same rows through both entry points, each within its bound of the other's sums."""
+    B = ref.Batch(EDGES, [1] * len(EDGES), 2, 16, 128, "bf16", 15)
+    q = B.randn(len(EDGES), 8, 128)
+    cache, batch = B.device(mc, cu=False)
+    d, dl = mc.attn_decode(cache, batch, q.cuda(), with_lse=True)
+    p, pl = mc.attn_prefill(cache, batch, q.cuda(), with_lse=True)
+    assert (d.float() - p.float()).abs().max() <= 4 * 2.0 ** -9 * 5
+    assert torch.allclose(dl, pl, rtol=1e-4, atol=1e-4)
+
+
+# ----------------------------------------------------------- streams, status --
+
+def test_on_another_stream_and_in_a_graph(mc):
+    B = ref.Batch([40, 130, 7], [1] * 3, 2, 16, 64, "bf16", 21)
+    cache, batch = B.device(mc, cu=False)
+    q, k, v = (B.randn(3, n, 64).cuda() for n in (8, 2, 2))
+    rope = ref.rope_table(200, 64).cuda()
+    ws = mc.attn_workspace(cache, 8)
+
+    def step():
+        return mc.attn_decode(cache, batch, mc.kv_append(cache, batch, q, k, v, rope=rope, workspace=ws), workspace=ws)
+
+    want = step().clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = step()
+    s.synchronize()
+    assert torch.equal(got, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        res = step()
+    res.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(res, want)
+
+
+def test_bad_pages_lengths_and_positions_are_reported(mc):
+    """What only the device can see is bounded there and reported, and the next call works."""
+    B = ref.Batch([40, 64], [1, 1], 2, 16, 64, "bf16", 22)
+    cache, batch = B.device(mc, cu=False)
+    q, k, v = (B.randn(2, n, 64).cuda() for n in (4, 2, 2))
+    ws = mc.attn_workspace(cache, 4)
+    good = mc.attn_decode(cache, batch, q, workspace=ws)
+    mc.check_status(ws)
+    bad = B.table.clone()
+    bad[0, 1] = cache.k.shape[0]
+    cases = [mc.KVBatch(batch._keep[0], bad.cuda()), mc.KVBatch(torch.tensor([40, 1 << 20], dtype=torch.int32).cuda(), B.table.cuda())]
+    for other in cases:
+        for call in (mc.attn_decode, mc.attn_prefill):
+            out = call(cache, other, q, workspace=ws)
+            with pytest.raises(mc.MCError) as e:
+                mc.check_status(ws)
+            assert e.value.code == mc.ERR_RANGE
+            assert torch.equal(out[1], good[1]) or other is cases[1] or call is mc.attn_prefill
+    before = cache.k.clone()
+    bad[0, 2] = -1  # the page of the new token of sequence 0
+    mc.kv_append(cache, mc.KVBatch(batch._keep[0], bad.cuda()), q, k, v, workspace=ws)
+    with pytest.raises(mc.MCError):
+        mc.check_status(ws)
+    changed = (torch.nan_to_num(cache.k.float()) != torch.nan_to_num(before.float())).flatten(1).any(1).nonzero().flatten()
+    assert changed.tolist() == [int(B.table[1, 3])]
+    mc.kv_append(cache, batch, q, k, v, rope=ref.rope_table(10, 64).cuda(), workspace=ws)  # positions past the table
+    with pytest.raises(mc.MCError):
+        mc.check_status(ws)
+    cu = torch.tensor([0, 3, 2], dtype=torch.int32).cuda()
+    mc.attn_prefill(cache, mc.KVBatch(batch._keep[0], batch._keep[1], cu, 2), q, workspace=ws)
+    with pytest.raises(mc.MCError):
+        mc.check_status(ws)
+    mc.attn_decode(cache, batch, q, workspace=ws)
+    mc.check_status(ws)
