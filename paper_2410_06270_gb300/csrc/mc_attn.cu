@@ -2,6 +2,8 @@
 // workspace and dispatch; and the plain attention kernel.
 #include <math.h>
 
+#include <atomic>
+
 #include "mc_attn.h"
 #include "mc_host.h"
 #include "mc_profile.h"
@@ -78,6 +80,22 @@ int launch_attn(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st)
     cudaError_t e = launch_k(k, dim3((unsigned)ctas), dim3(128), 0, st, p);
     if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "attention launch: %s", cudaGetErrorString(e));
     return MC_OK;
+}
+
+cudaError_t sm_count(int *out)
+{
+    static std::atomic<int> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    int n = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (!n) {
+        e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+    }
+    *out = n;
+    return cudaSuccess;
 }
 
 static int check_cache(const mc_kv_cache *c, int q_heads)
@@ -173,7 +191,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.lse = lse;
     p.status = (int32_t *)workspace;
     p.part = (uint8_t *)workspace + 256;
-    return launch_attn(p, cache->head_dim, cache->dtype == MC_BF16, (cudaStream_t)stream);
+    return (decode ? launch_decode : launch_attn)(p, cache->head_dim, cache->dtype == MC_BF16, (cudaStream_t)stream);
 }
 
 }  // namespace mc
@@ -186,7 +204,7 @@ size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads)
 {
     clear_error();
     if (check_cache(cache, q_heads)) return 0;
-    return 256;
+    return 256 + decode_part_bytes(cache->head_dim, q_heads / cache->kv_heads);
 }
 
 int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,

@@ -141,6 +141,11 @@ __device__ __forceinline__ float capped(float x, float cap)
 }
 
 int launch_append(const AppendParams &p, int head_dim, bool bf16, cudaStream_t st);
+constexpr int kAttnMaxSms = 160;  // SMs that the workspace has room for (the GB300's 152)
+// SMs of the current device, asked for once per device.
+cudaError_t sm_count(int *out);
+size_t decode_part_bytes(int head_dim, int group);
+int launch_decode(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
 int launch_attn(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
 
 }  // namespace mc

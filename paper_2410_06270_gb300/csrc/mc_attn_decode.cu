@@ -1,0 +1,504 @@
+// mc_attn_decode.cu -- attention of one new token per sequence over the paged cache.
+//
+// o = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m), one pass over the keys with a running
+// maximum m and sum l (scores carried in units of log 2).  Every key and value is read once
+// for a group of query heads, 4 head_dim bytes for 4 head_dim group flops: bound by HBM, so
+// the design is about keeping loads in flight on every SM whatever the lengths are.
+//
+// Work is cut into units of 64 keys of one (sequence, key head); the units of the whole
+// batch, in order, are dealt to the CTAs as equal contiguous runs, which each CTA finds from
+// the lengths by itself (no host knowledge of them, so a captured graph serves any).  A run
+// that ends inside an item leaves a partial result (m, l, o in fp32); join_kernel adds the
+// pieces of an item in their order.  At most two partials per CTA, whatever the batch.
+#include <math.h>
+
+#include "mc_attn.h"
+#include "mc_host.h"
+#include "mc_profile.h"
+
+namespace mc {
+
+constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
+constexpr int kDecKeys = 16;                   // keys of a unit that one warp takes
+constexpr int kDecUnit = kDecKeys * kDecWarps;
+constexpr int kDecCtasPerSm = 2;
+constexpr float kLazy = 8.f;  // the maximum moves only when a score passes it by 2^8: the
+                              // weights stay below 2^8, far inside fp16 and bf16
+
+template <bool BF16>
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+                     "{%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        mma16816(d, a[0], a[1], a[2], a[3], b0, b1);
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+__device__ __forceinline__ uint32_t transposed8x8(uint32_t a)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
+    return r;
+}
+
+// 16 bytes to shared memory, or 16 zeros where !real (the address is then not read).
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+
+// Keys [start, len) of a sequence, as units of kDecUnit keys from `base` on (base: start
+// rounded down to 16, so that a warp's 16 keys lie in one page).
+struct Keys {
+    int start, len, base, units;
+};
+
+__device__ __forceinline__ Keys keys_of(const AttnParams &p, int len)
+{
+    Keys k;
+    k.len = len;
+    k.start = p.window && len > p.window ? len - p.window : 0;
+    k.base = k.start & ~15;
+    k.units = (len - k.base + kDecUnit - 1) / kDecUnit;
+    return k;
+}
+
+// A place in the run of units: sequence, head slice, unit of its keys.
+struct Place {
+    int b, hv, u;
+    Keys k;
+};
+
+__device__ __forceinline__ void step(const AttnParams &p, int slices, Place &at)
+{
+    if (++at.u < at.k.units) return;
+    at.u = 0;
+    if (++at.hv < slices) return;
+    at.hv = 0;
+    while (++at.b < p.b.seqs) {
+        at.k = keys_of(p, seq_len(p.b, p.c, at.b, nullptr));
+        if (at.k.units) return;
+    }
+}
+
+// Header of a CTA's open item, for the join: the pieces of (sequence b, head slice hv) are
+// this CTA's tail partial and the head partials of the next pieces - 1 CTAs; 0: none.
+struct OpenItem {
+    int32_t pieces, b, hv, pad;
+};
+
+__host__ __device__ constexpr size_t dec_part_floats(int D, int nt) { return (size_t)8 * nt * (D + 2); }
+
+template <int D, int NT>
+struct DecShape {
+    static constexpr int kRow = D * 2;                       // bytes of a key
+    static constexpr int kSlot = 2 * kDecKeys * kRow;        // a warp's keys and values of a unit
+    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kRing = kSlot * kStages * kDecWarps;
+    static constexpr int kJoin = kDecWarps * 8 * (D + 4) * 4;
+    static constexpr int kSmem = kRing + kJoin + kDecWarps * 8 * NT * 8;
+};
+
+// NT: n-tiles of 8 query heads that a slice holds (1: up to 8 heads of a group, 2: 16).
+// The products are formed transposed, S^T = K Q^T and O^T += V^T P^T: the 16 keys of a
+// warp fill the rows of the m16n8k16 instruction and the heads its 8 columns, half the
+// instructions and accumulators of heads as rows.
+template <int D, bool BF16, int NT>
+__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(const AttnParams p, OpenItem *open, float *part)
+{
+    using Sh = DecShape<D, NT>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    const int slices_per = (p.group + 8 * NT - 1) / (8 * NT), slices = p.c.kv_heads * slices_per;
+    float *jo = reinterpret_cast<float *>(smem + Sh::kRing);
+    float2 *jml = reinterpret_cast<float2 *>(smem + Sh::kRing + Sh::kJoin);  // [warp][8 NT]
+    const uint32_t ring = smem_u32(smem) + warp * Sh::kSlot * Sh::kStages;
+    pdl_trigger();
+    pdl_wait();
+
+    // idle sequences
+    for (int b = blockIdx.x; b < p.b.seqs; b += gridDim.x)
+        if (seq_len(p.b, p.c, b, p.status) == 0) {
+            for (int i = tid; i < p.q_heads * D / 8; i += kDecThreads)
+                *reinterpret_cast<uint4 *>(p.out + b * p.out_stride + 8 * i) = make_uint4(0, 0, 0, 0);
+            if (p.lse)
+                for (int i = tid; i < p.q_heads; i += kDecThreads) p.lse[(int64_t)b * p.q_heads + i] = -INFINITY;
+        }
+
+    // all units, and the place of this CTA's first: 128 lengths a round
+    int64_t total = 0;
+    for (int b0 = 0; b0 < p.b.seqs; b0 += 128) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = b0 + 4 * lane + i;
+            if (b < p.b.seqs) n += keys_of(p, seq_len(p.b, p.c, b, nullptr)).units;
+        }
+        total += __reduce_add_sync(0xffffffffu, n);
+    }
+    total *= slices;
+    const int64_t ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
+    if ((int64_t)blockIdx.x >= ctas) {
+        if (tid == 0) open[blockIdx.x].pieces = 0;
+        return;
+    }
+    const int64_t u0 = total * blockIdx.x / ctas, u1 = total * (blockIdx.x + 1) / ctas;
+    Place at;  // compute side
+    {
+        int64_t before = 0;
+        at.b = -1;
+        for (int b0 = 0; at.b < 0 && b0 < p.b.seqs; b0 += 32) {
+            const int b = b0 + lane;
+            const int n = b < p.b.seqs ? keys_of(p, seq_len(p.b, p.c, b, nullptr)).units : 0;
+            int64_t sum = n;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int64_t o = __shfl_up_sync(0xffffffffu, sum, d);
+                if (lane >= d) sum += o;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * slices > u0);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                at.b = b0 + l;
+                before += __shfl_sync(0xffffffffu, sum - n, l);
+            } else {
+                before += __shfl_sync(0xffffffffu, sum, 31);
+            }
+        }
+        if (at.b < 0) {  // lengths that changed between the two readings
+            if (tid == 0) open[blockIdx.x].pieces = 0;
+            return;
+        }
+        at.k = keys_of(p, seq_len(p.b, p.c, at.b, nullptr));
+        const int64_t r = u0 - before * slices;
+        at.hv = (int)(r / at.k.units);
+        at.u = (int)(r % at.k.units);
+    }
+    int left = (int)(u1 - u0);
+
+    // ---- loads: this warp's 16 keys and values of a unit into ring slot i % kStages
+    constexpr int kChunks = D / 8, kPer = 32 / kChunks;  // 16-byte chunks of a row; rows per warp copy
+    const int lc = lane % kChunks, lr = lane / kChunks;
+    Place ld = at;
+    int ld_left = left, page = -1;
+    auto fetch_page = [&]() {
+        const int j = ld.k.base + ld.u * kDecUnit + warp * kDecKeys;
+        page = ld_left > 0 && j < ld.k.len ? seq_page(p.b, p.c, ld.b, j / p.c.page_size, p.status) : -1;
+    };
+    auto issue = [&](int slot) {
+        if (ld_left > 0) {
+            const int j = ld.k.base + ld.u * kDecUnit + warp * kDecKeys;
+            const int kvh = ld.hv / slices_per;
+            const int64_t off = (page < 0 ? 0 : page * p.c.page_stride) +
+                                ((int64_t)kvh * p.c.page_size + j % p.c.page_size + lr) * D + lc * 8;
+            const uint32_t dst = ring + slot * Sh::kSlot;
+#pragma unroll
+            for (int i = 0; i < kDecKeys / kPer; ++i) {
+                const int r = lr + i * kPer;
+                const bool real = page >= 0 && j + r >= ld.k.start && j + r < ld.k.len;
+                const uint32_t d = dst + r * Sh::kRow + ((lc ^ (r & 7)) << 4);
+                copy16(d, p.c.k + (real ? off + i * kPer * D : 0), real);
+                copy16(d + kDecKeys * Sh::kRow, p.c.v + (real ? off + i * kPer * D : 0), real);
+            }
+            --ld_left;
+            step(p, slices, ld);
+            fetch_page();
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    fetch_page();
+#pragma unroll
+    for (int s = 0; s < Sh::kStages - 1; ++s) issue(s);
+
+    int slot = 0;
+    bool open_tail = false;
+    while (left > 0) {
+        // ---- one piece: units [at.u, at.u + n) of one item
+        const int n = min(left, at.k.units - at.u);
+        const bool from_first = at.u == 0, to_last = at.u + n == at.k.units;
+        const int kvh = at.hv / slices_per, hs = (at.hv % slices_per) * 8 * NT;  // first head of the slice in its group
+        const int h0 = kvh * p.group + hs;
+        const int heads = min(8 * NT, p.group - hs);
+        uint32_t qf[NT][D / 16][2];
+        float slope[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const bool has = 8 * nt + g < heads;
+            const uint16_t *q = p.q + at.b * p.q_stride + (h0 + 8 * nt + g) * D + 2 * t4;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                qf[nt][ks][0] = has ? *reinterpret_cast<const uint32_t *>(q + 16 * ks) : 0u;
+                qf[nt][ks][1] = has ? *reinterpret_cast<const uint32_t *>(q + 16 * ks + 8) : 0u;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                slope[nt][c] = p.slopes && 8 * nt + 2 * t4 + c < heads ? __ldg(p.slopes + h0 + 8 * nt + 2 * t4 + c) * kLog2e : 0.f;
+        }
+        float o[NT][D / 16][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[nt][mt][c] = 0.f;
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.f;
+        }
+        const Keys keys = at.k;
+        for (int u = at.u; u < at.u + n; ++u) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kStages - 2) : "memory");
+            __syncwarp();  // every lane is done with the slot of the round before, which is filled next
+            issue(slot == 0 ? Sh::kStages - 1 : slot - 1);
+            const uint32_t kk = ring + slot * Sh::kSlot, vv = kk + kDecKeys * Sh::kRow;
+            const int j0 = keys.base + u * kDecUnit + warp * kDecKeys;
+            if (j0 < keys.len) {
+                // S^T: rows are keys g, g + 8; columns heads 2 t4, 2 t4 + 1; two chains
+                float s[NT][2][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) s[nt][0][c] = s[nt][1][c] = 0.f;
+                const int kr = lane & 15;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    uint32_t a[4];
+                    ldsm4(a, kk + kr * Sh::kRow + (((2 * ks + (lane >> 4)) ^ (kr & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16<BF16>(s[nt][ks & 1], a, qf[nt][ks][0], qf[nt][ks][1]);
+                }
+                bool over = false;
+                float x[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int j = j0 + g + (c >> 1) * 8;
+                        float v = (s[nt][0][c] + s[nt][1][c]) * p.scale;
+                        v = (p.softcap > 0.f ? capped(v, p.softcap) : v) * kLog2e;
+                        if (p.slopes) v = fmaf(slope[nt][c & 1], (float)(j - keys.len + 1), v);
+                        x[nt][c] = j >= keys.start && j < keys.len ? v : -INFINITY;
+                        over |= x[nt][c] > m[nt][c & 1] + kLazy;
+                    }
+                if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            float top = fmaxf(x[nt][c], x[nt][c + 2]);
+#pragma unroll
+                            for (int d = 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                            top = fmaxf(top, m[nt][c]);
+                            const float keep = top == m[nt][c] ? 1.f : ex2(m[nt][c] - top);
+                            m[nt][c] = top;
+                            l[nt][c] *= keep;
+#pragma unroll
+                            for (int mt = 0; mt < D / 16; ++mt) {
+                                o[nt][mt][c] *= keep;
+                                o[nt][mt][c + 2] *= keep;
+                            }
+                        }
+                }
+                uint32_t pf[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float pr[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float ref = m[nt][c & 1];
+                        pr[c] = ex2(x[nt][c] - (ref == -INFINITY ? 0.f : ref));
+                        l[nt][c & 1] += pr[c];
+                    }
+                    // rounded to the cache's type for the second product; l keeps fp32
+                    pf[nt][0] = transposed8x8(pack2<BF16>(pr[0], pr[1]));
+                    pf[nt][1] = transposed8x8(pack2<BF16>(pr[2], pr[3]));
+                }
+                const int vr = (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                for (int mt = 0; mt < D / 16; ++mt) {
+                    uint32_t a[4];
+                    ldsm4t(a, vv + vr * Sh::kRow + (((2 * mt + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16<BF16>(o[nt][mt], a, pf[nt][0], pf[nt][1]);
+                }
+            }
+            if (++slot == Sh::kStages) slot = 0;
+        }
+
+        // ---- the four warps' parts
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int d = 4; d <= 16; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
+                if (g == 0) jml[warp * 8 * NT + 8 * nt + 2 * t4 + c] = make_float2(m[nt][c], l[nt][c]);
+            }
+        const bool whole = from_first && to_last;
+        float *mine = part + (2 * blockIdx.x + (from_first ? 1 : 0)) * dec_part_floats(D, NT);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt) __syncthreads();
+#pragma unroll
+            for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    jo[(warp * 8 + 2 * t4 + (c & 1)) * (D + 4) + 16 * mt + g + (c >> 1) * 8] = o[nt][mt][c];
+            __syncthreads();
+            for (int i = tid; i < 8 * (D / 4); i += kDecThreads) {
+                const int h = i / (D / 4), d = (i % (D / 4)) * 4, hh = 8 * nt + h;
+                if (hh >= heads) continue;
+                float top = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < kDecWarps; ++w) top = fmaxf(top, jml[w * 8 * NT + hh].x);
+                float sum = 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < kDecWarps; ++w) {
+                    const float2 ml = jml[w * 8 * NT + hh];
+                    const float k = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+                    const float4 v = *reinterpret_cast<const float4 *>(jo + (w * 8 + h) * (D + 4) + d);
+                    sum = fmaf(k, ml.y, sum);
+                    acc = make_float4(fmaf(k, v.x, acc.x), fmaf(k, v.y, acc.y), fmaf(k, v.z, acc.z), fmaf(k, v.w, acc.w));
+                }
+                if (whole) {
+                    const float inv = 1.f / sum;
+                    *reinterpret_cast<uint2 *>(p.out + at.b * p.out_stride + (h0 + hh) * D + d) =
+                        make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
+                    if (p.lse && d == 0) p.lse[(int64_t)at.b * p.q_heads + h0 + hh] = (top + log2f(sum)) * kLn2;
+                } else {
+                    *reinterpret_cast<float4 *>(mine + hh * D + d) = acc;
+                    if (d == 0) *reinterpret_cast<float2 *>(mine + 8 * NT * D + 2 * hh) = make_float2(top, sum);
+                }
+            }
+        }
+        __syncthreads();  // the join buffers are free again
+        if (from_first && !to_last) {
+            open_tail = true;
+            if (tid == 0) {
+                const int64_t end = u1 - left + at.k.units;  // one past the item's last unit
+                const int64_t last = (end * ctas + total - 1) / total;  // one past the CTA that holds it
+                open[blockIdx.x] = {(int32_t)(last - blockIdx.x), at.b, at.hv, 0};
+            }
+        }
+        left -= n;
+        at.u += n - 1;
+        step(p, slices, at);
+    }
+    if (!open_tail && tid == 0) open[blockIdx.x].pieces = 0;
+}
+
+// One CTA per (CTA of the pass before, head of a slice): adds the pieces of that CTA's open
+// item in their order.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const OpenItem *open, const float *part, int nt)
+{
+    constexpr int kCols = D / 4, kGroups = 128 / kCols;
+    __shared__ float red[4], sums[kGroups];
+    __shared__ float4 acc_s[128];
+    pdl_trigger();
+    pdl_wait();
+    const OpenItem it = open[blockIdx.x];
+    if (it.pieces == 0) return;
+    const int per = (p.group + 8 * nt - 1) / (8 * nt);
+    const int hs = (it.hv % per) * 8 * nt, hh = blockIdx.y;
+    if (hs + hh >= p.group) return;
+    const int head = (it.hv / per) * p.group + hs + hh, tid = threadIdx.x;
+    const size_t stride = dec_part_floats(D, nt);
+    auto piece = [&](int i) { return part + (2 * ((size_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * stride; };
+    float top = -INFINITY;
+    for (int i = tid; i < it.pieces; i += 128) top = fmaxf(top, piece(i)[8 * nt * D + 2 * hh]);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    if ((tid & 31) == 0) red[tid >> 5] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int col = tid % kCols, grp = tid / kCols;
+    for (int i = grp; i < it.pieces; i += kGroups) {
+        const float *q = piece(i);
+        const float2 ml = *reinterpret_cast<const float2 *>(q + 8 * nt * D + 2 * hh);
+        const float4 v = *reinterpret_cast<const float4 *>(q + hh * D + 4 * col);
+        const float k = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+        sum = fmaf(k, ml.y, sum);
+        acc = make_float4(fmaf(k, v.x, acc.x), fmaf(k, v.y, acc.y), fmaf(k, v.z, acc.z), fmaf(k, v.w, acc.w));
+    }
+    acc_s[tid] = acc;
+    if (col == 0) sums[grp] = sum;
+    __syncthreads();
+    if (grp) return;
+    sum = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+        const float4 v = acc_s[i * kCols + col];
+        sum += sums[i];
+        acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
+    }
+    const float inv = 1.f / sum;
+    *reinterpret_cast<uint2 *>(p.out + it.b * p.out_stride + head * D + 4 * col) =
+        make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
+    if (p.lse && col == 0) p.lse[(int64_t)it.b * p.q_heads + head] = (top + log2f(sum)) * kLn2;
+}
+
+constexpr int kDecMaxCtas = kDecCtasPerSm * kAttnMaxSms;
+
+size_t decode_part_bytes(int head_dim, int group)
+{
+    return kDecMaxCtas * (sizeof(OpenItem) + 2 * 4 * dec_part_floats(head_dim, group > 8 ? 2 : 1));
+}
+
+template <int D, bool BF16, int NT>
+static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t st)
+{
+    using Sh = DecShape<D, NT>;
+    OpenItem *open = reinterpret_cast<OpenItem *>(p.part);
+    float *part = reinterpret_cast<float *>(p.part + kDecMaxCtas * sizeof(OpenItem));
+    auto k = decode_kernel<D, BF16, NT>;
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
+    if (e != cudaSuccess) return e;
+    profile_begin(kKAttnDecode, st);
+    e = launch_k(k, dim3(ctas), dim3(kDecThreads), Sh::kSmem, st, p, open, part);
+    profile_end(kKAttnDecode, st);
+    if (e != cudaSuccess) return e;
+    profile_begin(kKAttnJoin, st);
+    e = launch_k(join_kernel<D, BF16>, dim3(ctas, p.group < 8 * NT ? p.group : 8 * NT), dim3(128), 0, st, p,
+                 (const OpenItem *)open, (const float *)part, NT);
+    profile_end(kKAttnJoin, st);
+    return e;
+}
+
+int launch_decode(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st)
+{
+    int nsm = 0;
+    cudaError_t e = sm_count(&nsm);
+    if (e == cudaSuccess) {
+        const int ctas = kDecCtasPerSm * (nsm < kAttnMaxSms ? nsm : kAttnMaxSms);
+        const bool two = p.group > 8;
+        auto f = head_dim == 64
+                     ? (bf16 ? (two ? launch_decode_t<64, true, 2> : launch_decode_t<64, true, 1>)
+                             : (two ? launch_decode_t<64, false, 2> : launch_decode_t<64, false, 1>))
+                     : (bf16 ? (two ? launch_decode_t<128, true, 2> : launch_decode_t<128, true, 1>)
+                             : (two ? launch_decode_t<128, false, 2> : launch_decode_t<128, false, 1>));
+        e = f(p, ctas, st);
+    }
+    if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "decode launch: %s", cudaGetErrorString(e));
+    return MC_OK;
+}
+
+}  // namespace mc
