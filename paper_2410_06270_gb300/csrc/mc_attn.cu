@@ -1,7 +1,8 @@
 // mc_attn.cu -- the entry points of the paged cache and its attention: argument checks,
-// workspace and dispatch; and the plain attention kernel.
+// workspace and dispatch.
 #include <math.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "mc_attn.h"
@@ -9,78 +10,6 @@
 #include "mc_profile.h"
 
 namespace mc {
-
-// One warp per (token, head), key by key with a running maximum and sum.
-template <int D, bool BF16>
-__global__ void __launch_bounds__(128) attn_kernel(const AttnParams p)
-{
-    constexpr int kPer = D / 64;  // 32-bit words a lane holds of a row
-    pdl_trigger();
-    pdl_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (w >= (int64_t)p.b.tokens * p.q_heads) return;
-    const int t = (int)(w / p.q_heads), h = (int)(w % p.q_heads), kh = h / p.group;
-    const int s = token_seq(p.b, t, lane);
-    if (s < 0) return;
-    int first;
-    const int n = seq_rows(p.b, s, first, p.status);
-    if (t < first || t - first >= n) return;
-    const int len = seq_len(p.b, p.c, s, p.status), pos = len - n + (t - first);
-    float2 q[kPer], o[kPer];
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        q[e] = unpack2<BF16>(*reinterpret_cast<const uint32_t *>(p.q + t * p.q_stride + h * D + 2 * (lane * kPer + e)));
-        o[e] = make_float2(0.f, 0.f);
-    }
-    float m = -INFINITY, l = 0.f;
-    int end = pos + 1, j = 0;
-    if (p.prefix) end = max(end, __ldg(p.prefix + s));
-    end = min(end, len);
-    if (p.window) j = max(0, pos - p.window + 1);
-    const float slope = p.slopes ? __ldg(p.slopes + h) : 0.f;
-    if (pos < 0) end = 0;
-    for (; j < end; ++j) {
-        const int page = seq_page(p.b, p.c, s, j / p.c.page_size, p.status);
-        const int64_t at = page * p.c.page_stride + ((int64_t)kh * p.c.page_size + j % p.c.page_size) * D;
-        float x = 0.f;
-        float2 v[kPer];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            const int64_t i = at + 2 * (lane * kPer + e);
-            const float2 k = unpack2<BF16>(page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(p.c.k + i));
-            v[e] = unpack2<BF16>(page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(p.c.v + i));
-            x = fmaf(q[e].x, k.x, fmaf(q[e].y, k.y, x));
-        }
-#pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        x *= p.scale;
-        if (p.softcap > 0.f) x = capped(x, p.softcap);
-        x = (x + slope * (float)(j - pos)) * kLog2e;
-        const float top = fmaxf(m, x), keep = top == m ? 1.f : ex2(m - top), pr = ex2(x - top);
-        m = top;
-        l = fmaf(l, keep, pr);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] = make_float2(fmaf(o[e].x, keep, pr * v[e].x), fmaf(o[e].y, keep, pr * v[e].y));
-    }
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-#pragma unroll
-    for (int e = 0; e < kPer; ++e)
-        *reinterpret_cast<uint32_t *>(p.out + t * p.out_stride + h * D + 2 * (lane * kPer + e)) =
-            pack2<BF16>(o[e].x * inv, o[e].y * inv);
-    if (p.lse && lane == 0) p.lse[w] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-}
-
-int launch_attn(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st)
-{
-    const int64_t ctas = ((int64_t)p.b.tokens * p.q_heads + 3) / 4;
-    if (ctas > 0x7fffffff) return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d heads in one call", p.b.tokens, p.q_heads);
-    auto k = head_dim == 64 ? (bf16 ? attn_kernel<64, true> : attn_kernel<64, false>)
-                            : (bf16 ? attn_kernel<128, true> : attn_kernel<128, false>);
-    cudaError_t e = launch_k(k, dim3((unsigned)ctas), dim3(128), 0, st, p);
-    if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "attention launch: %s", cudaGetErrorString(e));
-    return MC_OK;
-}
 
 cudaError_t sm_count(int *out)
 {
@@ -132,6 +61,7 @@ static int check_counts(const mc_kv_batch *b)
 {
     if (!b) return set_error(MC_ERR_INVALID_ARG, "NULL batch");
     if (b->seqs < 0 || b->tokens < 0) return set_error(MC_ERR_INVALID_ARG, "seqs %d, tokens %d", b->seqs, b->tokens);
+    if (b->tokens > kMaxLen) return set_error(MC_ERR_UNSUPPORTED, "%d tokens in one call", b->tokens);
     return MC_OK;
 }
 
@@ -161,7 +91,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     int rc = check_cache(cache, q_heads);
     if (rc || (rc = check_counts(batch))) return rc;
     if (!o) return set_error(MC_ERR_INVALID_ARG, "NULL options");
-    if (!isfinite(o->scale) || !(o->softcap >= 0.f) || !isfinite(o->softcap) || o->window < 0)
+    if (!(o->scale > 0.f) || !isfinite(o->scale) || !(o->softcap >= 0.f) || !isfinite(o->softcap) || o->window < 0)
         return set_error(MC_ERR_INVALID_ARG, "scale %g, softcap %g, window %d", o->scale, o->softcap, o->window);
     if (decode && batch->cu_q) return set_error(MC_ERR_INVALID_ARG, "one token per sequence: cu_q must be NULL");
     if (decode && o->prefix) return set_error(MC_ERR_INVALID_ARG, "a prefix is mc_attn_prefill's");
@@ -183,7 +113,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.group = q_heads / cache->kv_heads;
     p.softcap = o->softcap;
     p.scale = o->softcap > 0.f ? o->scale / o->softcap : o->scale;
-    p.window = o->window;
+    p.window = o->window >= kMaxLen ? 0 : o->window;  // no length passes kMaxLen
     p.slopes = o->slopes;
     p.prefix = o->prefix;
     p.out = (uint16_t *)out;
@@ -191,7 +121,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.lse = lse;
     p.status = (int32_t *)workspace;
     p.part = (uint8_t *)workspace + 256;
-    return (decode ? launch_decode : launch_attn)(p, cache->head_dim, cache->dtype == MC_BF16, (cudaStream_t)stream);
+    return (decode ? launch_decode : launch_prefill)(p, cache->head_dim, cache->dtype == MC_BF16, (cudaStream_t)stream);
 }
 
 }  // namespace mc
@@ -204,7 +134,7 @@ size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads)
 {
     clear_error();
     if (check_cache(cache, q_heads)) return 0;
-    return 256 + decode_part_bytes(cache->head_dim, q_heads / cache->kv_heads);
+    return 256 + std::max(decode_part_bytes(cache->head_dim, q_heads / cache->kv_heads), prefill_part_bytes(cache->head_dim));
 }
 
 int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,

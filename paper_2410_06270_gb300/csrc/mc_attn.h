@@ -7,6 +7,7 @@ namespace mc {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kMaxLen = 1 << 30;  // keys of a sequence, so that positions and windows stay in 32 bits
 
 struct KvView {
     uint16_t *k, *v;
@@ -55,7 +56,7 @@ struct AppendParams {
 __device__ __forceinline__ int seq_len(const BatchView &bv, const KvView &c, int b, int32_t *status)
 {
     const int len = __ldg(bv.lens + b);
-    const int64_t cap = (int64_t)bv.table_width * c.page_size;
+    const int64_t room = (int64_t)bv.table_width * c.page_size, cap = room < kMaxLen ? room : kMaxLen;
     if (len > cap) {
         set_status(status, MC_ERR_RANGE);
         return (int)cap;
@@ -146,6 +147,7 @@ constexpr int kAttnMaxSms = 160;  // SMs that the workspace has room for (the GB
 cudaError_t sm_count(int *out);
 size_t decode_part_bytes(int head_dim, int group);
 int launch_decode(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
-int launch_attn(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
+size_t prefill_part_bytes(int head_dim);
+int launch_prefill(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
 
 }  // namespace mc

@@ -1,0 +1,838 @@
+// mc_attn_prefill.cu -- attention of many new tokens per sequence over the paged cache, on
+// the 5th-generation tensor cores.
+//
+// An item is 256 consecutive (token, head of the group) rows of one sequence and key head,
+// as two tiles of 128 rows, and the keys that any of them sees, in units of 128.  Packing a
+// group's heads into the rows lets them share a unit's keys and values, and keeps the
+// diagonal short (256 rows are 256 / group tokens).  For each unit and tile
+//   S = Q K^T            tcgen05.mma, both operands in shared memory, S in tensor memory
+//   P = 2^(c S - m)      one row per thread: maximum, exponentials, sum, no exchange
+//   O (+)= P V           tcgen05.mma with P (rounded to the cache's type) in tensor memory
+//                        over S's columns, V as stored, key-major
+// The two tiles alternate: the tensor pipe works for one while the other's softmax runs.
+// The maximum moves only when a row's scores pass it by 2^8 (the weights then stay below
+// 2^8), so O is rescaled in the first few units of a row and hardly after.
+//
+// Units of the whole batch, in order, are dealt to the CTAs (one per SM) as equal
+// contiguous runs, found on the device from the lengths; a run that ends inside an item
+// leaves (m, l, O) in fp32 and prefill_join_kernel adds an item's pieces in their order.
+// This splits a long cache over the SMs when there are few rows, and balances the causal
+// triangle, by the same rule.
+//
+// Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 issues the MMAs,
+// 9-11 copy (cp.async: any page size and alignment of 16 rows, zeros past the last key).
+// Tensor memory: S (and P) of tile t at column 128 t, O at 256 + 128 t.
+#include <math.h>
+
+#include <atomic>
+
+#include "mc_attn.h"
+#include "mc_host.h"
+#include "mc_profile.h"
+#include "mc_umma.cuh"
+
+namespace mc {
+
+constexpr int kPfRows = 256, kPfTile = 128, kPfKeys = 128;
+constexpr int kPfThreads = 384, kPfMma = 8, kPfLoad0 = 9, kPfLoaders = 3;
+constexpr int kPfMaxStages = 8;
+constexpr float kPfLazy = 8.f;
+
+struct PfShared {
+    uint64_t kfull[kPfMaxStages], kempty[kPfMaxStages];  // ring of keys / values
+    uint64_t qfull, qempty;
+    uint64_t sfull[2], pfull[2], ofull[2];               // per tile
+    uint64_t drain;
+    uint32_t tmem_base;
+    volatile int abort;
+    int b, h, mt, u;                                     // this CTA's first unit
+    int64_t total;
+    int sums[32];
+};
+
+template <int D>
+struct PfShape {
+    static constexpr int kHalf = kPfKeys * 128;               // 64 columns of a tile: SW128 atoms
+    static constexpr int kTileBytes = kHalf * (D / 64);
+    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kHdr = 1024;
+    static constexpr int kRing = kHdr + 2 * kTileBytes;       // after the two query tiles
+    static constexpr int kSmem = kRing + kStages * kTileBytes;
+};
+static_assert(sizeof(PfShared) <= PfShape<128>::kHdr, "prefill header");
+static_assert(PfShape<128>::kSmem <= 232448, "prefill shared memory");
+
+struct PfOpen;
+
+struct PfParams {
+    AttnParams a;
+    PfOpen *open;
+    float *part;
+    uint64_t timeout_ns;
+    int debug;
+};
+
+// Header of a CTA's open item: its pieces are this CTA's tail partial and the head
+// partials of the next pieces - 1 CTAs; 0: none.
+struct PfOpen {
+    int32_t pieces, b, h, mt;
+};
+
+// A partial: O [D / 4][256 rows] float4 (a warp's rows are consecutive), then (m, l).
+__host__ __device__ constexpr size_t pf_part_floats(int D) { return (size_t)kPfRows * (D + 2); }
+
+__device__ __forceinline__ bool g_wait(uint64_t *bar, uint32_t parity, const PfParams &p, PfShared *sh)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    while (true) {
+        if (mbar_try_wait_sleep(bar, parity, kWaitHintNs)) return true;
+        if (sh->abort) return false;
+        if (globaltimer_ns() - t0 > p.timeout_ns) {
+            set_status(p.a.status, MC_ERR_TIMEOUT);
+            sh->abort = 1;
+            return false;
+        }
+    }
+}
+
+// One answer for the warp (what follows is executed by all of its lanes together).
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, const PfParams &p, PfShared *sh)
+{
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, g_wait(bar, parity, p, sh));
+}
+
+// ------------------------------------------------------------------ items --
+
+struct PfSeq {
+    int first, n, len, prefix;  // first token row, new tokens, length, prefix
+};
+
+__device__ __forceinline__ PfSeq pf_seq(const AttnParams &p, int b, int32_t *status)
+{
+    PfSeq s;
+    s.n = seq_rows(p.b, b, s.first, status);
+    s.len = seq_len(p.b, p.c, b, status);
+    s.prefix = p.prefix ? __ldg(p.prefix + b) : 0;
+    return s;
+}
+
+// Keys [base, end) that rows of item mt see, base rounded down to a page's 16; at least
+// one unit (of zeros, all masked), so that rows without keys take the same way.
+struct PfKeys {
+    int base, end, units, p_lo;
+};
+
+__device__ __forceinline__ PfKeys pf_keys(const AttnParams &p, const PfSeq &s, int mt)
+{
+    PfKeys k;
+    const int last = min((mt + 1) * kPfRows, s.n * p.group) - 1;
+    k.p_lo = s.len - s.n + mt * kPfRows / p.group;
+    const int p_hi = s.len - s.n + last / p.group;
+    k.end = p_hi < 0 ? 0 : min(s.len, max(p_hi + 1, s.prefix));
+    k.base = p.window ? max(0, k.p_lo - p.window + 1) & ~15 : 0;
+    k.units = max(1, (k.end - k.base + kPfKeys - 1) / kPfKeys);
+    return k;
+}
+
+__device__ __forceinline__ int pf_tiles(const AttnParams &p, const PfSeq &s)
+{
+    return (s.n * p.group + kPfRows - 1) / kPfRows;
+}
+
+struct PfPlace {
+    int b, h, mt, u;
+    PfSeq s;
+    PfKeys k;
+};
+
+__device__ __forceinline__ void pf_next_item(const AttnParams &p, PfPlace &at)
+{
+    at.u = 0;
+    if (++at.mt >= pf_tiles(p, at.s)) {
+        at.mt = 0;
+        if (++at.h >= p.c.kv_heads) {
+            at.h = 0;
+            do {
+                if (++at.b >= p.b.seqs) return;
+                at.s = pf_seq(p, at.b, nullptr);
+            } while (at.s.n == 0);
+        }
+    }
+    at.k = pf_keys(p, at.s, at.mt);
+}
+
+// Sums of units of 32 sequences from b0 on (per key head) into sh->sums, by one warp: the
+// sequences' items are laid end to end and taken 32 at a time.  Returns their total.
+__device__ __forceinline__ int64_t pf_sums(const AttnParams &p, PfShared *sh, int b0, int lane, int32_t *status)
+{
+    PfSeq s = {0, 0, 0, 0};
+    if (b0 + lane < p.b.seqs) s = pf_seq(p, b0 + lane, status);
+    const int tiles = pf_tiles(p, s);
+    int upto = tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += o;
+    }
+    const int all = __shfl_sync(0xffffffffu, upto, 31);
+    __syncwarp();
+    sh->sums[lane] = 0;
+    __syncwarp();
+    for (int i0 = 0; i0 < all; i0 += 32) {
+        const int i = i0 + lane;
+        int own = 0;  // the sequence that holds item i: the lanes whose upto <= i come before it
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1)
+            if (__shfl_sync(0xffffffffu, upto, own + d - 1) <= i) own += d;
+        own = min(own, 31);
+        PfSeq t;
+        t.first = 0;
+        t.n = __shfl_sync(0xffffffffu, s.n, own);
+        t.len = __shfl_sync(0xffffffffu, s.len, own);
+        t.prefix = __shfl_sync(0xffffffffu, s.prefix, own);
+        const int before = __shfl_sync(0xffffffffu, upto - tiles, own);
+        if (i < all) atomicAdd(&sh->sums[own], pf_keys(p, t, i - before).units);
+    }
+    __syncwarp();
+    int64_t sum = sh->sums[lane];
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return sum;
+}
+
+// ------------------------------------------------------------ device pieces --
+
+#define PF_R8(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3]), "=r"(a[i + 4]), "=r"(a[i + 5]), "=r"(a[i + 6]), "=r"(a[i + 7])
+#define PF_P8(a, i) "+r"(a[i]), "+r"(a[i + 1]), "+r"(a[i + 2]), "+r"(a[i + 3]), "+r"(a[i + 4]), "+r"(a[i + 5]), "+r"(a[i + 6]), "+r"(a[i + 7])
+#define PF_I8(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3]), "r"(a[i + 4]), "r"(a[i + 5]), "r"(a[i + 6]), "r"(a[i + 7])
+
+// 32 columns of the warp's 32 lanes; the values may be used after pf_ld_wait of them.
+__device__ __forceinline__ void pf_ld32(uint32_t taddr, uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : PF_R8(r, 0), PF_R8(r, 8), PF_R8(r, 16), PF_R8(r, 24)
+        : "r"(taddr)
+        : "memory");
+}
+
+// Waits for every load of the warp; the operands tie the registers' uses to it.
+__device__ __forceinline__ void pf_ld_wait(uint32_t *r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : PF_P8(r, 0), PF_P8(r, 8), PF_P8(r, 16), PF_P8(r, 24) : : "memory");
+}
+
+__device__ __forceinline__ void pf_tie(uint32_t *r)
+{
+    asm volatile("" : PF_P8(r, 0), PF_P8(r, 8), PF_P8(r, 16), PF_P8(r, 24) : : "memory");
+}
+
+__device__ __forceinline__ void pf_st16(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+                 PF_I8(r, 0), PF_I8(r, 8)
+                 : "memory");
+}
+
+__device__ __forceinline__ void pf_st32(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        PF_I8(r, 0), PF_I8(r, 8), PF_I8(r, 16), PF_I8(r, 24)
+        : "memory");
+}
+
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+
+__device__ __forceinline__ void unpair2(uint64_t v, float &lo, float &hi)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// Instruction descriptor: fp16 or bf16 operands, fp32 accumulator, M = 128; b_mn: the B
+// operand's N dimension is the contiguous one (values: [key][d]).
+__host__ __device__ constexpr uint32_t pf_idesc(bool bf16, int N, bool b_mn)
+{
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+// Descriptor of a value tile as B operand, N (d) contiguous, 128-byte swizzle: atoms of 64
+// d x 8 keys, 1024 bytes from one group of 8 keys to the next (stride), a half-tile from one
+// 64-column block to the next (leading).
+__device__ __forceinline__ uint64_t pf_desc_mn(uint32_t addr, uint32_t half)
+{
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(half >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
+           ((uint64_t)1u << 46) | ((uint64_t)2u << 61);
+}
+
+__device__ __forceinline__ void pf_copy16(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+
+// Registers: the softmax threads hold a row of 128 scores, the others little.  The shares
+// (2 warpgroups of kPfSoftRegs and one of kPfRestRegs) are within what the block has at
+// launch, kPfRegs a thread (checked before the launch: a larger share would wait for ever).
+constexpr int kPfRegs = 168, kPfSoftRegs = 208, kPfRestRegs = 80;
+static_assert(2 * kPfSoftRegs + kPfRestRegs <= 3 * kPfRegs, "register shares");
+__device__ __forceinline__ void pf_take_regs() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfSoftRegs)); }
+__device__ __forceinline__ void pf_give_regs() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfRestRegs)); }
+
+// ---------------------------------------------------------------- softmax --
+
+// One row's 128 scores of a unit.  EXTRA: with a cap or a bias.
+template <bool BF16, bool EXTRA>
+__device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, uint32_t o_tmem, int D, bool masked, int lo,
+                                           int hi, float c, float cap, float slope, float at0, bool fresh, float &m, float &l)
+{
+    if (EXTRA) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i) {
+            float x = __uint_as_float(s[i]);
+            if (cap > 0.f) x = capped(x * c, cap) * kLog2e;
+            else x *= c;
+            s[i] = __float_as_uint(fmaf(slope, at0 + (float)i, x));
+        }
+    }
+    if (masked) {
+        const unsigned span = hi > lo ? hi - lo : 0;
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+            if ((unsigned)(i - lo) >= span) s[i] = 0xff800000u;
+    }
+    float t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = __uint_as_float(s[i]);
+#pragma unroll
+    for (int i = 4; i < 128; i += 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = i + k + 4 < 128 ? fmaxf(t[k], fmaxf(__uint_as_float(s[i + k]), __uint_as_float(s[i + k + 4])))
+                                                           : fmaxf(t[k], __uint_as_float(s[i + k]));
+    }
+    float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+    if (!EXTRA) top *= c;
+    if (__any_sync(0xffffffffu, top > m + kPfLazy)) {
+        const float next = top > m + kPfLazy ? top : m;
+        const float keep = next == m ? 1.f : ex2(m - next);
+        m = next;
+        l *= keep;
+        if (!fresh) {
+            for (int d = 0; d < D; d += 32) {
+                uint32_t o[32];
+                pf_ld32(o_tmem + d, o);
+                pf_ld_wait(o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+                pf_st32(o_tmem + d, o);
+            }
+        }
+    }
+    const float ref = m == -INFINITY ? 0.f : -m;
+    const uint64_t c2 = pair2(c, c), r2 = pair2(ref, ref);
+    uint64_t sum[2] = {pair2(0.f, 0.f), pair2(0.f, 0.f)};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t x = pair2(__uint_as_float(s[32 * q + 2 * i]), __uint_as_float(s[32 * q + 2 * i + 1]));
+            const uint64_t y = EXTRA ? add2(x, r2) : fma2(x, c2, r2);
+            float a, b;
+            unpair2(y, a, b);
+            a = ex2(a);
+            b = ex2(b);
+            sum[i & 1] = add2(sum[i & 1], pair2(a, b));
+            w[i] = pack2<BF16>(a, b);  // rounded to the cache's type for the product with V; l keeps fp32
+        }
+        pf_st16(s_tmem + 16 * q, w);
+    }
+    float a, b;
+    unpair2(add2(sum[0], sum[1]), a, b);
+    l += a + b;
+}
+
+// ------------------------------------------------------------------ kernel --
+
+template <int D, bool BF16, bool EXTRA>
+__global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams pp)
+{
+    using Sh = PfShape<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    PfShared *sh = reinterpret_cast<PfShared *>(smem);
+    const AttnParams &p = pp.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < Sh::kStages; ++i) {
+            mbar_init(&sh->kfull[i], 32 * kPfLoaders);
+            mbar_init(&sh->kempty[i], 1);
+        }
+        mbar_init(&sh->qfull, 32 * kPfLoaders);
+        mbar_init(&sh->qempty, 1);
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&sh->sfull[t], 1);
+            mbar_init(&sh->pfull[t], 4);
+            mbar_init(&sh->ofull[t], 1);
+        }
+        mbar_init(&sh->drain, 1);
+        sh->abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == kPfMma) tmem_alloc(&sh->tmem_base, 512);
+    pdl_wait();
+    if (warp == 0) {
+        int64_t total = 0;
+        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) total += pf_sums(p, sh, b0, lane, p.status);
+        total *= p.c.kv_heads;
+        const int64_t ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
+        int fb = -1, fh = 0, fmt = 0, fu = 0;
+        if ((int64_t)blockIdx.x < ctas) {
+            int64_t r = total * blockIdx.x / ctas;  // units before this CTA's first
+            for (int b0 = 0; b0 < p.b.seqs && fb < 0; b0 += 32) {
+                if (p.b.seqs > 32) pf_sums(p, sh, b0, lane, nullptr);
+                const int64_t own = (int64_t)sh->sums[lane] * p.c.kv_heads;
+                int64_t upto = own;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int64_t o = __shfl_up_sync(0xffffffffu, upto, d);
+                    if (lane >= d) upto += o;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, upto > r);
+                if (hit) {
+                    const int who = __ffs(hit) - 1;
+                    r -= __shfl_sync(0xffffffffu, upto - own, who);
+                    const int per = __shfl_sync(0xffffffffu, sh->sums[lane], who);
+                    fb = b0 + who;
+                    fh = (int)(r / per);
+                    int left = (int)(r % per);
+                    const PfSeq s = pf_seq(p, fb, nullptr);
+                    const int tiles = pf_tiles(p, s);
+                    for (int t0 = 0; t0 < tiles; t0 += 32) {
+                        const int n = t0 + lane < tiles ? pf_keys(p, s, t0 + lane).units : 0;
+                        int sum = n;
+#pragma unroll
+                        for (int d = 1; d < 32; d <<= 1) {
+                            const int o = __shfl_up_sync(0xffffffffu, sum, d);
+                            if (lane >= d) sum += o;
+                        }
+                        const unsigned in = __ballot_sync(0xffffffffu, sum > left);
+                        if (in) {
+                            const int w = __ffs(in) - 1;
+                            fmt = t0 + w;
+                            fu = left - __shfl_sync(0xffffffffu, sum - n, w);
+                            break;
+                        }
+                        left -= __shfl_sync(0xffffffffu, sum, 31);
+                    }
+                } else {
+                    r -= __shfl_sync(0xffffffffu, upto, 31);
+                }
+            }
+        }
+        if (lane == 0) {
+            sh->total = total;
+            sh->b = fb;
+            sh->h = fh;
+            sh->mt = fmt;
+            sh->u = fu;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = sh->tmem_base;
+    const int64_t total = sh->total, ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
+    const bool any = sh->b >= 0;
+    const int64_t u0 = any ? total * blockIdx.x / ctas : 0, u1 = any ? total * (blockIdx.x + 1) / ctas : 0;
+    PfPlace at;
+    at.b = sh->b;
+    at.h = sh->h;
+    at.mt = sh->mt;
+    at.u = sh->u;
+    if (any) {
+        at.s = pf_seq(p, at.b, nullptr);
+        at.k = pf_keys(p, at.s, at.mt);
+    }
+    int left = (int)(u1 - u0);
+
+    if (warp >= kPfMma) {
+      pf_give_regs();  // one instruction for the warpgroup
+      if (warp >= kPfLoad0) {
+        // -------------------------------------------------------------- copies --
+        constexpr int kChunks = D / 8, kPer = 32 / kChunks;
+        const int w = warp - kPfLoad0, lc = lane % kChunks, lr = lane / kChunks;
+        const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
+        const uint32_t smem0 = smem_u32(smem);
+        int it = 0;
+        bool ok = !(pp.debug & kDebugNoProducer);
+        // full barriers of the last two copy groups, arrived on once they have landed
+        uint64_t *wait0 = nullptr, *wait1 = nullptr;
+        auto commit = [&](uint64_t *bar) {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (wait1) {
+                asm volatile("cp.async.wait_group 2;" ::: "memory");
+                fence_proxy_async_smem();
+                mbar_arrive(wait1);
+            }
+            wait1 = wait0;
+            wait0 = bar;
+        };
+        auto pages = [&](const PfPlace &a, int u) {  // lane i < 8: page of the unit's i-th 16 keys
+            const int j = a.k.base + u * kPfKeys + 16 * lane;
+            return lane < 8 && j < a.k.end ? seq_page(p.b, p.c, a.b, j / p.c.page_size, p.status) : -1;
+        };
+        auto tile = [&](const uint16_t *cache, const PfPlace &a, int u, int page) {
+            const int slot = it % Sh::kStages;
+            if (it >= Sh::kStages && !warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh)) return false;
+            const uint32_t dst = smem0 + Sh::kRing + slot * Sh::kTileBytes + col;
+            for (int i = w; i < 8; i += kPfLoaders) {
+                const int pg = __shfl_sync(0xffffffffu, page, i);
+                const int j = a.k.base + u * kPfKeys + 16 * i;
+                const uint16_t *src = cache;
+                if (pg >= 0) src += pg * p.c.page_stride + ((int64_t)a.h * p.c.page_size + j % p.c.page_size + lr) * D + lc * 8;
+#pragma unroll
+                for (int r0 = 0; r0 < 16; r0 += kPer) {
+                    const int r = 16 * i + r0 + lr;
+                    const bool real = pg >= 0 && j + r0 + lr < a.k.end;
+                    pf_copy16((dst + r * 128) ^ ((r & 7) << 4), real ? src + r0 * D : cache, real);
+                }
+            }
+            ++it;
+            commit(&sh->kfull[slot]);
+            return true;
+        };
+        int items = 0;
+        while (ok && left > 0) {
+            const int n = min(left, at.k.units - at.u);
+            int page = pages(at, at.u);
+            for (int u = at.u; ok && u < at.u + n; ++u) {
+                const int next = u + 1 < at.u + n ? pages(at, u + 1) : -1;
+                ok = tile(p.c.k, at, u, page) && tile(p.c.v, at, u, page);
+                if (ok && u == at.u) {
+                    // the item's queries, once the last item's have been read
+                    if (items && !(ok = warp_wait(&sh->qempty, (items + 1) & 1, pp, sh))) break;
+                    const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
+                    const int fill = rows > kPfTile ? kPfRows : kPfTile;
+                    for (int r = w * kPer + lr; r < fill; r += kPfLoaders * kPer) {
+                        const int f = rows0 + r, tok = f / p.group, hg = f % p.group;
+                        const bool real = r < rows;
+                        const uint16_t *src = p.q + (at.s.first + tok) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
+                        const uint32_t d = smem0 + Sh::kHdr + (r >> 7) * Sh::kTileBytes + col + (r & 127) * 128;
+                        pf_copy16(d ^ ((r & 7) << 4), real ? src : p.q, real);
+                    }
+                    ++items;
+                    commit(&sh->qfull);
+                }
+                page = next;
+            }
+            left -= n;
+            if (left > 0) pf_next_item(p, at);
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        fence_proxy_async_smem();
+        if (wait1) mbar_arrive(wait1);
+        if (wait0) mbar_arrive(wait0);
+        pdl_trigger();
+      } else {
+        // ---------------------------------------------------------------- MMAs --
+        constexpr uint32_t kIdS = pf_idesc(BF16, kPfKeys, false), kIdO = pf_idesc(BF16, D, true);
+        uint64_t qd[2];
+        for (int t = 0; t < 2; ++t) qd[t] = umma_desc_sw128(smem + Sh::kHdr + t * Sh::kTileBytes);
+        const uint64_t kd0 = umma_desc_sw128(smem + Sh::kRing);
+        const uint64_t vd0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
+        constexpr uint64_t kStep = Sh::kTileBytes >> 4;
+        int kt = 0, items = 0, uses[2] = {0, 0};
+        bool ok = true;
+        auto qk = [&](int t, int slot) {  // S_t = Q_t K^T
+            const uint64_t b = kd0 + slot * kStep;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                const uint64_t o = (s >> 2) * (Sh::kHalf >> 4) + (s & 3) * 2;
+                umma_f16(tbase + 128 * t, qd[t] + o, b + o, kIdS, s > 0);
+            }
+        };
+        auto pv = [&](int t, int slot, bool first) {  // O_t (+)= P_t V
+            const uint64_t b = vd0 + slot * kStep;
+#pragma unroll
+            for (int s = 0; s < kPfKeys / 16; ++s)
+                umma_f16_ts(tbase + 256 + 128 * t, tbase + 128 * t + 8 * s, b + s * (2048 >> 4), kIdO, !first || s > 0);
+        };
+        auto full = [&](int i) { return warp_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1, pp, sh); };
+        while (ok && left > 0) {
+            const int n = min(left, at.k.units - at.u);
+            const int tiles = at.s.n * p.group - at.mt * kPfRows > kPfTile ? 2 : 1;
+            // kt: ring index of unit j's keys, kt + 1 its values
+            if (!(ok = warp_wait(&sh->qfull, items & 1, pp, sh) && full(kt))) break;
+            tc_fence_after();
+            if (elect_one()) {
+                for (int t = 0; t < tiles; ++t) {
+                    qk(t, kt % Sh::kStages);
+                    umma_commit(&sh->sfull[t]);
+                }
+                umma_commit(&sh->kempty[kt % Sh::kStages]);
+                if (n == 1) umma_commit(&sh->qempty);
+            }
+            __syncwarp();
+            for (int j = 0; ok && j < n; ++j, kt += 2) {
+                const bool more = j + 1 < n;
+                if (!(ok = full(kt + 1))) break;
+                for (int t = 0; t < tiles; ++t) {
+                    if (!(ok = warp_wait(&sh->pfull[t], uses[t] & 1, pp, sh))) break;
+                    ++uses[t];
+                    if (t == 0 && more && !(ok = full(kt + 2))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        pv(t, (kt + 1) % Sh::kStages, j == 0);
+                        if (t == tiles - 1) umma_commit(&sh->kempty[(kt + 1) % Sh::kStages]);
+                        if (more) {
+                            qk(t, (kt + 2) % Sh::kStages);
+                            umma_commit(&sh->sfull[t]);
+                            if (t == tiles - 1) {
+                                umma_commit(&sh->kempty[(kt + 2) % Sh::kStages]);
+                                if (j + 2 == n) umma_commit(&sh->qempty);
+                            }
+                        } else {
+                            umma_commit(&sh->ofull[t]);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            ++items;
+            left -= n;
+            if (left > 0) pf_next_item(p, at);
+        }
+        // the tensor pipe is idle before shared and tensor memory are given back
+        if (elect_one()) umma_commit(&sh->drain);
+        __syncwarp();
+        const uint64_t t0 = globaltimer_ns();
+        while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->drain, 0)))
+            if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
+      }
+    } else {
+        // -------------------------------------------------- softmax and epilogue --
+        pf_take_regs();
+        const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
+        const uint32_t lanes = (uint32_t)(wt * 32) << 16;
+        const uint32_t s_tmem = tbase + lanes + 128 * t, o_tmem = tbase + lanes + 256 + 128 * t;
+        const float c = p.softcap > 0.f ? p.scale : p.scale * kLog2e;
+        int su = 0, ou = 0;
+        bool ok = true, tail = false;
+        while (ok && left > 0) {
+            const int n = min(left, at.k.units - at.u);
+            const int rows0 = at.mt * kPfRows + t * kPfTile, rows = min(kPfTile, at.s.n * p.group - rows0);
+            const bool from_first = at.u == 0, to_last = at.u + n == at.k.units;
+            if (rows > 0) {
+                const bool live = row < rows;
+                const int f = rows0 + min(row, rows - 1), tok = f / p.group, head = at.h * p.group + f % p.group;
+                const int off = at.s.len - at.s.n, pos = off + tok;
+                const int lo = p.window ? max(0, pos - p.window + 1) : 0;
+                const int hi = pos < 0 ? 0 : min(at.s.len, max(pos + 1, at.s.prefix));
+                // what the tile's first and last rows see decides whether a unit needs the mask
+                const int p_first = off + rows0 / p.group, p_last = off + (rows0 + rows - 1) / p.group;
+                const int all_hi = p_first < 0 ? 0 : min(at.s.len, max(p_first + 1, at.s.prefix));
+                const int all_lo = p.window ? p_last - p.window + 1 : 0;
+                const float slope = EXTRA && p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
+                float m = -INFINITY, l = 0.f;
+                for (int u = at.u; u < at.u + n; ++u) {
+                    if (!(ok = warp_wait(&sh->sfull[t], su & 1, pp, sh))) break;
+                    ++su;
+                    tc_fence_after();
+                    if (wt * 32 < rows) {
+                        const int j0 = at.k.base + u * kPfKeys;
+                        uint32_t s[128];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) pf_ld32(s_tmem + 32 * q, s + 32 * q);
+                        pf_ld_wait(s);
+#pragma unroll
+                        for (int q = 1; q < 4; ++q) pf_tie(s + 32 * q);
+                        pf_softmax<BF16, EXTRA>(s, s_tmem, o_tmem, D, j0 < all_lo || j0 + kPfKeys > all_hi, lo - j0, hi - j0, c,
+                                                p.softcap, slope, (float)(j0 - pos), u == at.u, m, l);
+                        tmem_st_wait();
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh->pfull[t]);
+                }
+                if (!ok || !(ok = warp_wait(&sh->ofull[t], ou & 1, pp, sh))) break;
+                ++ou;
+                tc_fence_after();
+                const float inv = 1.f / l;
+                uint16_t *out = p.out + (at.s.first + tok) * p.out_stride + head * D;
+                float *mine = pp.part + (2 * blockIdx.x + (from_first ? 1 : 0)) * pf_part_floats(D);
+                const bool whole = from_first && to_last;
+                if (wt * 32 < rows) {
+#pragma unroll
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+                        pf_ld32(o_tmem + d, o);
+                        pf_ld_wait(o);
+                        if (live && whole) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    v[k] = l == 0.f ? 0u : pack2<BF16>(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
+                                *reinterpret_cast<uint4 *>(out + d + i) = make_uint4(v[0], v[1], v[2], v[3]);
+                            }
+                        } else if (live) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                reinterpret_cast<uint4 *>(mine)[(size_t)((d + i) / 4) * kPfRows + t * kPfTile + row] =
+                                    make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        }
+                        __syncwarp();
+                    }
+                    if (live && whole && p.lse)
+                        p.lse[(int64_t)(at.s.first + tok) * p.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+                    if (live && !whole)
+                        reinterpret_cast<float2 *>(mine + kPfRows * D)[t * kPfTile + row] = make_float2(m, l);
+                }
+                tc_fence_before();
+            }
+            if (from_first && !to_last) {
+                tail = true;
+                if (tid == 0) {
+                    const int64_t end = u1 - left + at.k.units;
+                    pp.open[blockIdx.x] = {(int32_t)((end * ctas + total - 1) / total - blockIdx.x), at.b, at.h, at.mt};
+                }
+            }
+            left -= n;
+            if (left > 0) pf_next_item(p, at);
+        }
+        if (!tail && tid == 0) pp.open[blockIdx.x].pieces = 0;
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kPfMma) {
+        tc_fence_after();
+        tmem_dealloc(tbase, 512);
+    }
+}
+
+// 32 rows of a CTA's open item: adds its pieces in their order.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
+{
+    const AttnParams &p = pp.a;
+    pdl_trigger();
+    pdl_wait();
+    const PfOpen it = pp.open[blockIdx.x];
+    if (it.pieces == 0) return;
+    const PfSeq s = pf_seq(p, it.b, nullptr);
+    const int lane = threadIdx.x & 31, row = blockIdx.y * 32 + lane, f = it.mt * kPfRows + row;
+    if (f >= s.n * p.group) return;
+    const int tok = f / p.group, head = it.h * p.group + f % p.group;
+    auto piece = [&](int i) { return pp.part + (2 * ((size_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * pf_part_floats(D); };
+    float top = -INFINITY;
+    for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, piece(i)[kPfRows * D + 2 * row]);
+    float4 acc[D / 32];
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+    const int c0 = threadIdx.x >> 5;  // this warp's column quads: c0, c0 + 8, ...
+    for (int i = 0; i < it.pieces; ++i) {
+        const float *q = piece(i);
+        const float2 ml = reinterpret_cast<const float2 *>(q + kPfRows * D)[row];
+        const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+        sum = fmaf(w, ml.y, sum);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const float4 v = reinterpret_cast<const float4 *>(q)[(size_t)(c0 + 8 * k) * kPfRows + row];
+            acc[k] = make_float4(fmaf(w, v.x, acc[k].x), fmaf(w, v.y, acc[k].y), fmaf(w, v.z, acc[k].z), fmaf(w, v.w, acc[k].w));
+        }
+    }
+    const float inv = 1.f / sum;
+    uint16_t *out = p.out + (s.first + tok) * p.out_stride + head * D;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k)
+        *reinterpret_cast<uint2 *>(out + 4 * (c0 + 8 * k)) =
+            sum == 0.f ? make_uint2(0, 0)
+                       : make_uint2(pack2<BF16>(acc[k].x * inv, acc[k].y * inv), pack2<BF16>(acc[k].z * inv, acc[k].w * inv));
+    if (p.lse && c0 == 0) p.lse[(int64_t)(s.first + tok) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+size_t prefill_part_bytes(int head_dim)
+{
+    return kAttnMaxSms * (sizeof(PfOpen) + 2 * 4 * pf_part_floats(head_dim));
+}
+
+template <int D, bool BF16, bool EXTRA>
+static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st)
+{
+    using Sh = PfShape<D>;
+    auto k = prefill_kernel<D, BF16, EXTRA>;
+    static std::atomic<bool> known{false};  // (the same build on every device)
+    cudaError_t e = cudaSuccess;
+    if (!known.load(std::memory_order_relaxed)) {
+        cudaFuncAttributes at;
+        e = cudaFuncGetAttributes(&at, k);
+        if (e != cudaSuccess) return e;
+        if (at.numRegs < kPfRegs) return cudaErrorInvalidConfiguration;
+        known.store(true, std::memory_order_relaxed);
+    }
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
+    if (e != cudaSuccess) return e;
+    profile_begin(kKAttnPrefill, st);
+    e = launch_k(k, dim3(ctas), dim3(kPfThreads), Sh::kSmem, st, p);
+    profile_end(kKAttnPrefill, st);
+    if (e != cudaSuccess) return e;
+    profile_begin(kKAttnJoin, st);
+    e = launch_k(prefill_join_kernel<D, BF16>, dim3(ctas, kPfRows / 32), dim3(256), 0, st, p);
+    profile_end(kKAttnJoin, st);
+    return e;
+}
+
+int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st)
+{
+    if ((int64_t)a.b.tokens * a.group > 0x7fffffff - kPfRows)
+        return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d heads a group in one call", a.b.tokens, a.group);
+    PfParams p;
+    p.a = a;
+    p.open = reinterpret_cast<PfOpen *>(a.part);
+    p.part = reinterpret_cast<float *>(a.part + kAttnMaxSms * sizeof(PfOpen));
+    p.timeout_ns = wait_bound_ns();
+    p.debug = debug_flags();
+    const bool extra = a.softcap > 0.f || a.slopes;
+    int nsm = 0;
+    cudaError_t e = sm_count(&nsm);
+    if (e == cudaSuccess) {
+        const int ctas = nsm < kAttnMaxSms ? nsm : kAttnMaxSms;
+        auto f = head_dim == 64
+                     ? (bf16 ? (extra ? launch_prefill_t<64, true, true> : launch_prefill_t<64, true, false>)
+                             : (extra ? launch_prefill_t<64, false, true> : launch_prefill_t<64, false, false>))
+                     : (bf16 ? (extra ? launch_prefill_t<128, true, true> : launch_prefill_t<128, true, false>)
+                             : (extra ? launch_prefill_t<128, false, true> : launch_prefill_t<128, false, false>));
+        e = f(p, ctas, st);
+    }
+    if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "prefill launch: %s", cudaGetErrorString(e));
+    return MC_OK;
+}
+
+}  // namespace mc

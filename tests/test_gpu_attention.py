@@ -276,3 +276,23 @@ def test_bad_pages_lengths_and_positions_are_reported(mc):
         mc.check_status(ws)
     mc.attn_decode(cache, batch, q, workspace=ws)
     mc.check_status(ws)
+
+
+def test_prefill_waits_expire_and_the_context_lives(mc):
+    """With the copies switched off every wait of the kernel reaches its bound."""
+    B = ref.Batch([300], [300], 1, 16, 64, "bf16", 23)
+    cache, batch = B.device(mc)
+    q = B.randn(300, 4, 64).cuda()
+    ws = mc.attn_workspace(cache, 4)
+    want = mc.attn_prefill(cache, batch, q, workspace=ws)
+    mc.check_status(ws)
+    mc.set_debug(1, 20_000_000)
+    try:
+        mc.attn_prefill(cache, batch, q, workspace=ws)
+        with pytest.raises(mc.MCError) as e:
+            mc.check_status(ws)
+        assert e.value.code == mc.ERR_TIMEOUT
+    finally:
+        mc.set_debug(0, 1_000_000_000)
+    assert torch.equal(mc.attn_prefill(cache, batch, q, workspace=ws), want)
+    mc.check_status(ws)
