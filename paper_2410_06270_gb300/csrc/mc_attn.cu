@@ -38,7 +38,8 @@ static int check_cache(const mc_kv_cache *c, int q_heads)
     if (c->page_size < 16 || c->page_size > 32768 || c->page_size % 16)
         return set_error(MC_ERR_INVALID_ARG, "page_size %d (a multiple of 16, at most 32768)", c->page_size);
     if (c->num_pages < 1) return set_error(MC_ERR_INVALID_ARG, "num_pages %d", c->num_pages);
-    if (c->page_stride % 8 || c->page_stride < (int64_t)c->kv_heads * c->page_size * c->head_dim)
+    if (c->page_stride % 8 || c->page_stride < (int64_t)c->kv_heads * c->page_size * c->head_dim ||
+        c->page_stride >= (int64_t)1 << 38)
         return set_error(MC_ERR_INVALID_ARG, "page_stride %lld", (long long)c->page_stride);
     return MC_OK;
 }

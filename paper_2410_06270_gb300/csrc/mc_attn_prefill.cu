@@ -20,11 +20,15 @@
 // triangle, by the same rule.
 //
 // Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 issues the MMAs,
-// 9-11 copy (cp.async: any page size and alignment of 16 rows, zeros past the last key).
+// 9 copies keys and values (TMA, a box per page and 64 columns), 10-11 the queries (cp.async:
+// their rows are heads of tokens at any stride).
 // Tensor memory: S (and P) of tile t at column 128 t, O at 256 + 128 t.
 #include <math.h>
 
+#include <algorithm>
 #include <atomic>
+
+#include <cuda.h>
 
 #include "mc_attn.h"
 #include "mc_host.h"
@@ -34,7 +38,7 @@
 namespace mc {
 
 constexpr int kPfRows = 256, kPfTile = 128, kPfKeys = 128;
-constexpr int kPfThreads = 384, kPfMma = 8, kPfLoad0 = 9, kPfLoaders = 3;
+constexpr int kPfThreads = 384, kPfMma = 8, kPfKv = 9, kPfQ0 = 10, kPfQWarps = 2;
 constexpr int kPfMaxStages = 8;
 constexpr float kPfLazy = 8.f;
 
@@ -42,7 +46,7 @@ struct PfShared {
     uint64_t kfull[kPfMaxStages], kempty[kPfMaxStages];  // ring of keys / values
     uint64_t qfull, qempty;
     uint64_t sfull[2], pfull[2], ofull[2];               // per tile
-    uint64_t drain;
+    uint64_t drain, vpatch;
     uint32_t tmem_base;
     volatile int abort;
     int b, h, mt, u;                                     // this CTA's first unit
@@ -70,6 +74,7 @@ struct PfParams {
     float *part;
     uint64_t timeout_ns;
     int debug;
+    int box_rows;  // rows of a copied box: the largest power of two that divides a page, at most a unit
 };
 
 // Header of a CTA's open item: its pieces are this CTA's tail partial and the head
@@ -118,7 +123,7 @@ __device__ __forceinline__ PfSeq pf_seq(const AttnParams &p, int b, int32_t *sta
     return s;
 }
 
-// Keys [base, end) that rows of item mt see, base rounded down to a page's 16; at least
+// Keys [base, end) that rows of item mt see, base rounded down to a unit; at least
 // one unit (of zeros, all masked), so that rows without keys take the same way.
 struct PfKeys {
     int base, end, units, p_lo;
@@ -131,7 +136,7 @@ __device__ __forceinline__ PfKeys pf_keys(const AttnParams &p, const PfSeq &s, i
     k.p_lo = s.len - s.n + mt * kPfRows / p.group;
     const int p_hi = s.len - s.n + last / p.group;
     k.end = p_hi < 0 ? 0 : min(s.len, max(p_hi + 1, s.prefix));
-    k.base = p.window ? max(0, k.p_lo - p.window + 1) & ~15 : 0;
+    k.base = p.window ? max(0, k.p_lo - p.window + 1) & ~(kPfKeys - 1) : 0;
     k.units = max(1, (k.end - k.base + kPfKeys - 1) / kPfKeys);
     return k;
 }
@@ -161,6 +166,33 @@ __device__ __forceinline__ void pf_next_item(const AttnParams &p, PfPlace &at)
         }
     }
     at.k = pf_keys(p, at.s, at.mt);
+}
+
+// This CTA's run of units, read by each role for itself (held from before the roles part,
+// it would be spilled by the softmax's need of registers for all of them).
+struct PfRun {
+    int64_t total, ctas, u1;
+    int left;
+};
+
+__device__ __forceinline__ PfRun pf_run(const AttnParams &p, const volatile PfShared *sh, PfPlace &at)
+{
+    PfRun r;
+    r.total = sh->total;
+    r.ctas = r.total < (int64_t)gridDim.x ? r.total : gridDim.x;
+    at.b = sh->b;
+    at.h = sh->h;
+    at.mt = sh->mt;
+    at.u = sh->u;
+    r.u1 = 0;
+    r.left = 0;
+    if (at.b >= 0) {
+        r.u1 = r.total * (blockIdx.x + 1) / r.ctas;
+        r.left = (int)(r.u1 - r.total * blockIdx.x / r.ctas);
+        at.s = pf_seq(p, at.b, nullptr);
+        at.k = pf_keys(p, at.s, at.mt);
+    }
+    return r;
 }
 
 // Sums of units of 32 sequences from b0 on (per key head) into sh->sums, by one warp: the
@@ -237,12 +269,14 @@ __device__ __forceinline__ void pf_st16(uint32_t taddr, const uint32_t *r)
                  : "memory");
 }
 
-__device__ __forceinline__ void pf_st32(uint32_t taddr, const uint32_t *r)
+// 16 columns, waited for.
+__device__ __forceinline__ void pf_ld16(uint32_t taddr, uint32_t *r)
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-        PF_I8(r, 0), PF_I8(r, 8), PF_I8(r, 16), PF_I8(r, 24)
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : PF_R8(r, 0), PF_R8(r, 8)
+        : "r"(taddr)
         : "memory");
 }
 
@@ -258,6 +292,9 @@ __device__ __forceinline__ void unpair2(uint64_t v, float &lo, float &hi)
     asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
 }
 
+// Two fp32 operations for one issue slot (the pipe takes as long as for two: what is saved
+// is issue, which the softmax warps run short of; one by one a unit's softmax takes 1610
+// cycles instead of 1340).
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
 {
     uint64_t r;
@@ -289,7 +326,16 @@ __device__ __forceinline__ uint64_t pf_desc_mn(uint32_t addr, uint32_t half)
            ((uint64_t)1u << 46) | ((uint64_t)2u << 61);
 }
 
-__device__ __forceinline__ void pf_copy16(uint32_t dst, const void *src, bool real)
+// One box of a page: 64 columns from c on, rows from r on, of a head.
+__device__ __forceinline__ void pf_tma(uint32_t dst, const CUtensorMap *map, int c, int r, int head, int page, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(smem_u32(bar)), "r"(c), "r"(r), "r"(head), "r"(page)
+                 : "memory");
+}
+
+// 16 bytes, or 16 zeros where !real (the address is then not read).
+__device__ __forceinline__ void pf_copy16z(uint32_t dst, const void *src, bool real)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
@@ -341,13 +387,12 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
         m = next;
         l *= keep;
         if (!fresh) {
-            for (int d = 0; d < D; d += 32) {
-                uint32_t o[32];
-                pf_ld32(o_tmem + d, o);
-                pf_ld_wait(o);
+            for (int d = 0; d < D; d += 16) {
+                uint32_t o[16];
+                pf_ld16(o_tmem + d, o);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
-                pf_st32(o_tmem + d, o);
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+                pf_st16(o_tmem + d, o);
             }
         }
     }
@@ -378,7 +423,8 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 // ------------------------------------------------------------------ kernel --
 
 template <int D, bool BF16, bool EXTRA>
-__global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams pp)
+__global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams pp, const __grid_constant__ CUtensorMap kmap,
+                                                                   const __grid_constant__ CUtensorMap vmap)
 {
     using Sh = PfShape<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -388,10 +434,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 
     if (tid == 0) {
         for (int i = 0; i < Sh::kStages; ++i) {
-            mbar_init(&sh->kfull[i], 32 * kPfLoaders);
+            mbar_init(&sh->kfull[i], 1);
             mbar_init(&sh->kempty[i], 1);
         }
-        mbar_init(&sh->qfull, 32 * kPfLoaders);
+        mbar_init(&sh->vpatch, 1);
+        mbar_init(&sh->qfull, 32 * kPfQWarps);
         mbar_init(&sh->qempty, 1);
         for (int t = 0; t < 2; ++t) {
             mbar_init(&sh->sfull[t], 1);
@@ -465,100 +512,110 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     __syncthreads();
     tc_fence_after();
     const uint32_t tbase = sh->tmem_base;
-    const int64_t total = sh->total, ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
-    const bool any = sh->b >= 0;
-    const int64_t u0 = any ? total * blockIdx.x / ctas : 0, u1 = any ? total * (blockIdx.x + 1) / ctas : 0;
-    PfPlace at;
-    at.b = sh->b;
-    at.h = sh->h;
-    at.mt = sh->mt;
-    at.u = sh->u;
-    if (any) {
-        at.s = pf_seq(p, at.b, nullptr);
-        at.k = pf_keys(p, at.s, at.mt);
-    }
-    int left = (int)(u1 - u0);
-
     if (warp >= kPfMma) {
       pf_give_regs();  // one instruction for the warpgroup
-      if (warp >= kPfLoad0) {
+      if (warp >= kPfKv) {
         // -------------------------------------------------------------- copies --
-        constexpr int kChunks = D / 8, kPer = 32 / kChunks;
-        const int w = warp - kPfLoad0, lc = lane % kChunks, lr = lane / kChunks;
-        const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
+        PfPlace at;
+        int left = pp.debug & kDebugNoProducer ? 0 : pf_run(p, sh, at).left;
         const uint32_t smem0 = smem_u32(smem);
-        int it = 0;
-        bool ok = !(pp.debug & kDebugNoProducer);
-        // full barriers of the last two copy groups, arrived on once they have landed
-        uint64_t *wait0 = nullptr, *wait1 = nullptr;
-        auto commit = [&](uint64_t *bar) {
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (wait1) {
-                asm volatile("cp.async.wait_group 2;" ::: "memory");
-                fence_proxy_async_smem();
-                mbar_arrive(wait1);
-            }
-            wait1 = wait0;
-            wait0 = bar;
-        };
-        auto pages = [&](const PfPlace &a, int u) {  // lane i < 8: page of the unit's i-th 16 keys
-            const int j = a.k.base + u * kPfKeys + 16 * lane;
-            return lane < 8 && j < a.k.end ? seq_page(p.b, p.c, a.b, j / p.c.page_size, p.status) : -1;
-        };
-        auto tile = [&](const uint16_t *cache, const PfPlace &a, int u, int page) {
-            const int slot = it % Sh::kStages;
-            if (it >= Sh::kStages && !warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh)) return false;
-            const uint32_t dst = smem0 + Sh::kRing + slot * Sh::kTileBytes + col;
-            for (int i = w; i < 8; i += kPfLoaders) {
-                const int pg = __shfl_sync(0xffffffffu, page, i);
-                const int j = a.k.base + u * kPfKeys + 16 * i;
-                const uint16_t *src = cache;
-                if (pg >= 0) src += pg * p.c.page_stride + ((int64_t)a.h * p.c.page_size + j % p.c.page_size + lr) * D + lc * 8;
-#pragma unroll
-                for (int r0 = 0; r0 < 16; r0 += kPer) {
-                    const int r = 16 * i + r0 + lr;
-                    const bool real = pg >= 0 && j + r0 + lr < a.k.end;
-                    pf_copy16((dst + r * 128) ^ ((r & 7) << 4), real ? src + r0 * D : cache, real);
-                }
-            }
-            ++it;
-            commit(&sh->kfull[slot]);
-            return true;
-        };
-        int items = 0;
-        while (ok && left > 0) {
-            const int n = min(left, at.k.units - at.u);
-            int page = pages(at, at.u);
-            for (int u = at.u; ok && u < at.u + n; ++u) {
-                const int next = u + 1 < at.u + n ? pages(at, u + 1) : -1;
-                ok = tile(p.c.k, at, u, page) && tile(p.c.v, at, u, page);
-                if (ok && u == at.u) {
-                    // the item's queries, once the last item's have been read
-                    if (items && !(ok = warp_wait(&sh->qempty, (items + 1) & 1, pp, sh))) break;
-                    const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
-                    const int fill = rows > kPfTile ? kPfRows : kPfTile;
-                    for (int r = w * kPer + lr; r < fill; r += kPfLoaders * kPer) {
-                        const int f = rows0 + r, tok = f / p.group, hg = f % p.group;
-                        const bool real = r < rows;
-                        const uint16_t *src = p.q + (at.s.first + tok) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
-                        const uint32_t d = smem0 + Sh::kHdr + (r >> 7) * Sh::kTileBytes + col + (r & 127) * 128;
-                        pf_copy16(d ^ ((r & 7) << 4), real ? src : p.q, real);
+        if (warp == kPfKv) {
+            // keys and values: lane i copies the i-th box (of a page) of a tile.  A page that is
+            // not there, and rows past the last key's page, are read beyond the map: zeros.
+            const int boxes = kPfKeys / pp.box_rows;
+            int it = 0, patches = 0;
+            bool ok = true;
+            auto pages = [&](int u) {
+                const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
+                return lane < boxes && j < at.k.end ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + j / p.c.page_size) : -1;
+            };
+            while (ok && left > 0) {
+                const int n = min(left, at.k.units - at.u);
+                int page = pages(at.u);
+                for (int u = at.u; ok && u < at.u + n; ++u) {
+                    const int next = u + 1 < at.u + n ? pages(u + 1) : -1;  // used a unit later
+                    const int j0 = at.k.base + u * kPfKeys, j = j0 + lane * pp.box_rows;
+                    const int row = j % p.c.page_size;
+                    if ((unsigned)page >= (unsigned)p.c.num_pages) {
+                        if (lane < boxes && j < at.k.end) set_status(p.status, MC_ERR_RANGE);
+                        page = p.c.num_pages;
                     }
-                    ++items;
-                    commit(&sh->qfull);
+                    for (int kv = 0; kv < 2; ++kv, ++it) {
+                        const int slot = it % Sh::kStages;
+                        if (it >= Sh::kStages && !(ok = warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh))) break;
+                        // values past the sequence's end may be NaN, and a weight of 0 would not
+                        // hide that: their rows are zeroed before the tile is given on
+                        const bool patch = kv && j0 + kPfKeys > at.s.len;
+                        uint64_t *bar = patch ? &sh->vpatch : &sh->kfull[slot];
+                        if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
+                        __syncwarp();
+                        if (lane < boxes) {
+                            const uint32_t dst = smem0 + Sh::kRing + slot * Sh::kTileBytes + lane * pp.box_rows * 128;
+#pragma unroll
+                            for (int h = 0; h < D / 64; ++h)
+                                pf_tma(dst + h * Sh::kHalf, kv ? &vmap : &kmap, 64 * h, row, at.h, page, bar);
+                        }
+                        if (patch) {
+                            if (!(ok = warp_wait(&sh->vpatch, patches++ & 1, pp, sh))) break;
+                            const int from = max(0, at.s.len - j0);
+                            for (int i = from * 8 + lane; i < kPfKeys * 8; i += 32)
+#pragma unroll
+                                for (int h = 0; h < D / 64; ++h)
+                                    *reinterpret_cast<uint4 *>(smem + Sh::kRing + slot * Sh::kTileBytes + h * Sh::kHalf + i * 16) =
+                                        make_uint4(0, 0, 0, 0);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sh->kfull[slot]);
+                        }
+                    }
+                    page = next;
                 }
-                page = next;
+                left -= n;
+                if (left > 0) pf_next_item(p, at);
             }
-            left -= n;
-            if (left > 0) pf_next_item(p, at);
+            // the last copies land before the block's shared memory is given back, on an abort too
+            const uint64_t t0 = globaltimer_ns();
+            for (int i = max(0, it - Sh::kStages); i < it; ++i)
+                while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1)))
+                    if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
+            pdl_trigger();
+        } else {
+            // queries, one row per 16-byte lane group, zeros past the last
+            constexpr int kChunks = D / 8, kPer = 32 / kChunks, kQStep = kPfQWarps * kPer;
+            const int lc = lane % kChunks, lr = lane / kChunks;
+            const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
+            const int step_hg = kQStep % p.group;
+            const int64_t q_step = kQStep / p.group * p.q_stride + step_hg * D, q_wrap = p.q_stride - p.group * D;
+            int items = 0;
+            while (left > 0) {
+                const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
+                const int fill = rows > kPfTile ? kPfRows : kPfTile;
+                int r = (warp - kPfQ0) * kPer + lr;
+                int hg = (rows0 + r) % p.group;
+                const uint16_t *src = p.q + (at.s.first + (rows0 + r) / p.group) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
+                if (items && !warp_wait(&sh->qempty, (items + 1) & 1, pp, sh)) break;
+                for (; r < fill; r += kQStep) {
+                    const uint32_t d = smem0 + Sh::kHdr + (r >> 7) * Sh::kTileBytes + col + (r & 127) * 128;
+                    const bool real = r < rows;
+                    pf_copy16z(d ^ ((r & 7) << 4), real ? src : p.q, real);
+                    src += q_step;
+                    if ((hg += step_hg) >= p.group) {
+                        hg -= p.group;
+                        src += q_wrap;
+                    }
+                }
+                asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+                fence_proxy_async_smem();
+                mbar_arrive(&sh->qfull);
+                ++items;
+                left -= min(left, at.k.units - at.u);
+                if (left > 0) pf_next_item(p, at);
+            }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        fence_proxy_async_smem();
-        if (wait1) mbar_arrive(wait1);
-        if (wait0) mbar_arrive(wait0);
-        pdl_trigger();
       } else {
         // ---------------------------------------------------------------- MMAs --
+        PfPlace at;
+        int left = pf_run(p, sh, at).left;
         constexpr uint32_t kIdS = pf_idesc(BF16, kPfKeys, false), kIdO = pf_idesc(BF16, D, true);
         uint64_t qd[2];
         for (int t = 0; t < 2; ++t) qd[t] = umma_desc_sw128(smem + Sh::kHdr + t * Sh::kTileBytes);
@@ -636,6 +693,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     } else {
         // -------------------------------------------------- softmax and epilogue --
         pf_take_regs();
+        PfPlace at;
+        const PfRun run = pf_run(p, sh, at);
+        int left = run.left;
         const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
         const uint32_t lanes = (uint32_t)(wt * 32) << 16;
         const uint32_t s_tmem = tbase + lanes + 128 * t, o_tmem = tbase + lanes + 256 + 128 * t;
@@ -718,8 +778,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             if (from_first && !to_last) {
                 tail = true;
                 if (tid == 0) {
-                    const int64_t end = u1 - left + at.k.units;
-                    pp.open[blockIdx.x] = {(int32_t)((end * ctas + total - 1) / total - blockIdx.x), at.b, at.h, at.mt};
+                    const int64_t end = run.u1 - left + at.k.units;
+                    pp.open[blockIdx.x] = {(int32_t)((end * run.ctas + run.total - 1) / run.total - blockIdx.x), at.b, at.h, at.mt};
                 }
             }
             left -= n;
@@ -783,9 +843,34 @@ size_t prefill_part_bytes(int head_dim)
     return kAttnMaxSms * (sizeof(PfOpen) + 2 * 4 * pf_part_floats(head_dim));
 }
 
+// Tensor map of keys or values: [page][head][row][d], boxes of 64 columns x box_rows rows
+// with the 128-byte swizzle.
+static bool pf_map(CUtensorMap *m, const void *base, const KvView &c, int D, bool bf16, int box_rows)
+{
+    using Encode = decltype(&cuTensorMapEncodeTiled);
+    static std::atomic<Encode> known{nullptr};
+    Encode encode = known.load(std::memory_order_relaxed);
+    if (!encode) {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r) != cudaSuccess || !f) return false;
+        encode = (Encode)f;
+        known.store(encode, std::memory_order_relaxed);
+    }
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)c.page_size, (cuuint64_t)c.kv_heads, (cuuint64_t)c.num_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)c.page_size * D * 2, (cuuint64_t)c.page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
+    return encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(base), dims,
+                  strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, bool BF16, bool EXTRA>
 static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st)
 {
+    CUtensorMap kmap, vmap;
+    if (!pf_map(&kmap, p.a.c.k, p.a.c, D, BF16, p.box_rows) || !pf_map(&vmap, p.a.c.v, p.a.c, D, BF16, p.box_rows))
+        return cudaErrorInvalidValue;
     using Sh = PfShape<D>;
     auto k = prefill_kernel<D, BF16, EXTRA>;
     static std::atomic<bool> known{false};  // (the same build on every device)
@@ -800,7 +885,7 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
     e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnPrefill, st);
-    e = launch_k(k, dim3(ctas), dim3(kPfThreads), Sh::kSmem, st, p);
+    e = launch_k(k, dim3(ctas), dim3(kPfThreads), Sh::kSmem, st, p, kmap, vmap);
     profile_end(kKAttnPrefill, st);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnJoin, st);
@@ -819,6 +904,7 @@ int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st
     p.part = reinterpret_cast<float *>(a.part + kAttnMaxSms * sizeof(PfOpen));
     p.timeout_ns = wait_bound_ns();
     p.debug = debug_flags();
+    p.box_rows = std::min(a.c.page_size & -a.c.page_size, kPfKeys);
     const bool extra = a.softcap > 0.f || a.slopes;
     int nsm = 0;
     cudaError_t e = sm_count(&nsm);
