@@ -112,8 +112,8 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.q_stride = q_stride;
     p.q_heads = q_heads;
     p.group = q_heads / cache->kv_heads;
-    p.softcap = o->softcap;
-    p.scale = o->softcap > 0.f ? o->scale / o->softcap : o->scale;
+    p.cap = o->softcap * kLog2e;
+    p.scale = o->softcap > 0.f ? o->scale / o->softcap * (2.f * kLog2e) : o->scale * kLog2e;
     p.window = o->window >= kMaxLen ? 0 : o->window;  // no length passes kMaxLen
     p.slopes = o->slopes;
     p.prefix = o->prefix;

@@ -26,8 +26,8 @@ struct AttnParams {
     const uint16_t *q;
     int64_t q_stride;
     int q_heads, group;  // group = q_heads / kv_heads
-    float scale;         // of q . k; with a cap: of tanh's argument (scale / softcap)
-    float softcap;       // 0: none
+    float scale;         // q . k in units of log 2; with a cap: in the units of capped()
+    float cap;           // the cap in units of log 2; 0: none
     int window;          // 0: none
     const float *slopes;
     const int32_t *prefix;
@@ -92,6 +92,11 @@ __device__ __forceinline__ int seq_page(const BatchView &bv, const KvView &c, in
     return page;
 }
 
+// A token's sequence, position and length, found by the whole warp.
+struct TokenPlace {
+    int seq, pos;  // seq < 0: padding; pos < 0: no position
+};
+
 // Sequence of token row t: the largest b with cu_q[b] <= t, found by the whole warp (32
 // probes a round); -1 for a padding row.  Ends for any contents of cu_q.
 __device__ __forceinline__ int token_seq(const BatchView &bv, int t, int lane)
@@ -108,6 +113,30 @@ __device__ __forceinline__ int token_seq(const BatchView &bv, int t, int lane)
         hi = top < hi ? top : hi;
     }
     return lo;
+}
+
+// Where token row t is.  Up to 31 sequences every lane reads one boundary and one length, so
+// that all comes with one memory round trip; more are searched.
+__device__ __forceinline__ TokenPlace token_place(const BatchView &bv, const KvView &c, int t, int lane, int32_t *status)
+{
+    if (bv.cu_q && bv.seqs < 32) {
+        const int cu = lane <= bv.seqs ? __ldg(bv.cu_q + lane) : 0x7fffffff;
+        const int mine = lane < bv.seqs ? seq_len(bv, c, lane, status) : 0;
+        const int s = __popc(__ballot_sync(0xffffffffu, lane > 0 && lane <= bv.seqs && cu <= t));
+        const int first = __shfl_sync(0xffffffffu, cu, s), end = __shfl_sync(0xffffffffu, cu, s + 1 < 32 ? s + 1 : 31);
+        const int len = __shfl_sync(0xffffffffu, mine, s);
+        if (s >= bv.seqs) return {-1, -1};
+        if (first < 0 || first > t || end > bv.tokens) {
+            set_status(status, MC_ERR_RANGE);
+            return {s, -1};
+        }
+        return {s, len - (end - first) + (t - first)};
+    }
+    const int s = token_seq(bv, t, lane);
+    if (s < 0) return {-1, -1};
+    int first;
+    const int n = seq_rows(bv, s, first, status), len = seq_len(bv, c, s, status);
+    return {s, t >= first && t - first < n ? len - n + (t - first) : -1};
 }
 
 template <bool BF16>
@@ -133,15 +162,20 @@ __device__ __forceinline__ float ex2(float x)
     return r;
 }
 
-// cap * tanh(x) with x already divided by the cap, as cap - 2 cap / (1 + e^2x): exact to
-// a few units of fp32 relative to the cap (tanh.approx, at 2^-11, would move a score of 20
-// by 0.01, a probability by 1 %).  e^2x may overflow to infinity: the quotient is then 0.
-__device__ __forceinline__ float capped(float x, float cap)
+__device__ __forceinline__ float rcp(float x)
 {
-    return fmaf(__fdividef(1.f, 1.f + ex2(x * (2.f * kLog2e))), -2.f * cap, cap);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
 
+// top * tanh(x / 2 log2 e), as top - 2 top / (1 + 2^x): off by a few units of fp32 of the
+// cap (tanh.approx, at 2^-11, would move a score of 20 by 0.01, a probability by 1 %).  2^x
+// may overflow to infinity: the quotient is then 0.
+__device__ __forceinline__ float capped(float x, float top) { return fmaf(rcp(1.f + ex2(x)), -2.f * top, top); }
+
 int launch_append(const AppendParams &p, int head_dim, bool bf16, cudaStream_t st);
+
 constexpr int kAttnMaxSms = 160;  // SMs that the workspace has room for (the GB300's 152)
 // SMs of the current device, asked for once per device.
 cudaError_t sm_count(int *out);

@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                     for (int c = 0; c < 4; ++c) {
                         const int j = j0 + g + (c >> 1) * 8;
                         float v = (s[nt][0][c] + s[nt][1][c]) * p.scale;
-                        v = (p.softcap > 0.f ? capped(v, p.softcap) : v) * kLog2e;
+                        if (p.cap > 0.f) v = capped(v, p.cap);
                         if (p.slopes) v = fmaf(slope[nt][c & 1], (float)(j - keys.len + 1), v);
                         x[nt][c] = j >= keys.start && j < keys.len ? v : -INFINITY;
                         over |= x[nt][c] > m[nt][c & 1] + kLazy;

@@ -302,6 +302,13 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
     return r;
 }
 
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
 {
     uint64_t r;
@@ -350,25 +357,53 @@ __device__ __forceinline__ void pf_give_regs() { asm volatile("setmaxnreg.dec.sy
 
 // ---------------------------------------------------------------- softmax --
 
-// One row's 128 scores of a unit.  EXTRA: with a cap or a bias.
-template <bool BF16, bool EXTRA>
+// What the scores go through before the softmax.
+enum { kPfPlain = 0, kPfBias = 1, kPfCap = 2 };  // kPfCap: and the bias, if there is one
+
+// The low n bits, n any number.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+// One row's 128 scores of a unit.  c: the factor to units of log 2; at0: the first key's
+// distance (key - query); slope in units of log 2; [lo, hi): the keys of the unit that the
+// row sees, where `masked`.
+template <bool BF16, int MODE>
 __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, uint32_t o_tmem, int D, bool masked, int lo,
                                            int hi, float c, float cap, float slope, float at0, bool fresh, float &m, float &l)
 {
-    if (EXTRA) {
+    if (MODE != kPfPlain) {
+        // the bias is slope * (at0 + i): the distance counts up exactly, two keys at a time;
+        // without a cap it is brought to the scores' units, so that c applies to both
+        uint64_t at = pair2(at0, at0 + 1.f);
+        const uint64_t two = pair2(2.f, 2.f);
+        const float sl = MODE == kPfBias ? slope / c : slope;
+        const uint64_t sl2 = pair2(sl, sl), c2 = pair2(c, c), top2 = pair2(cap, cap), down2 = pair2(-2.f * cap, -2.f * cap);
 #pragma unroll
-        for (int i = 0; i < 128; ++i) {
-            float x = __uint_as_float(s[i]);
-            if (cap > 0.f) x = capped(x * c, cap) * kLog2e;
-            else x *= c;
-            s[i] = __float_as_uint(fmaf(slope, at0 + (float)i, x));
+        for (int i = 0; i < 128; i += 2) {
+            uint64_t x = pair2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+            float a, b;
+            if (MODE == kPfCap) {
+                unpair2(mul2(x, c2), a, b);
+                const uint64_t y = add2(pair2(ex2(a), ex2(b)), pair2(1.f, 1.f));  // capped()
+                unpair2(y, a, b);
+                x = fma2(pair2(rcp(a), rcp(b)), down2, fma2(sl2, at, top2));
+            } else {
+                x = fma2(sl2, at, x);
+            }
+            at = add2(at, two);
+            unpair2(x, a, b);
+            s[i] = __float_as_uint(a);
+            s[i + 1] = __float_as_uint(b);
         }
+        if (MODE == kPfCap) c = 1.f;
     }
     if (masked) {
-        const unsigned span = hi > lo ? hi - lo : 0;
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
-            if ((unsigned)(i - lo) >= span) s[i] = 0xff800000u;
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t see = low_bits(hi - 32 * q) & ~low_bits(lo - 32 * q);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (!((see >> i) & 1u)) s[32 * q + i] = 0xff800000u;
+        }
     }
     float t[4];
 #pragma unroll
@@ -380,7 +415,7 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
                                                            : fmaxf(t[k], __uint_as_float(s[i + k]));
     }
     float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-    if (!EXTRA) top *= c;
+    top *= c;
     if (__any_sync(0xffffffffu, top > m + kPfLazy)) {
         const float next = top > m + kPfLazy ? top : m;
         const float keep = next == m ? 1.f : ex2(m - next);
@@ -405,7 +440,7 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const uint64_t x = pair2(__uint_as_float(s[32 * q + 2 * i]), __uint_as_float(s[32 * q + 2 * i + 1]));
-            const uint64_t y = EXTRA ? add2(x, r2) : fma2(x, c2, r2);
+            const uint64_t y = fma2(x, c2, r2);
             float a, b;
             unpair2(y, a, b);
             a = ex2(a);
@@ -422,7 +457,7 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 
 // ------------------------------------------------------------------ kernel --
 
-template <int D, bool BF16, bool EXTRA>
+template <int D, bool BF16, int MODE>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams pp, const __grid_constant__ CUtensorMap kmap,
                                                                    const __grid_constant__ CUtensorMap vmap)
 {
@@ -699,7 +734,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
         const uint32_t lanes = (uint32_t)(wt * 32) << 16;
         const uint32_t s_tmem = tbase + lanes + 128 * t, o_tmem = tbase + lanes + 256 + 128 * t;
-        const float c = p.softcap > 0.f ? p.scale : p.scale * kLog2e;
         int su = 0, ou = 0;
         bool ok = true, tail = false;
         while (ok && left > 0) {
@@ -716,7 +750,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 const int p_first = off + rows0 / p.group, p_last = off + (rows0 + rows - 1) / p.group;
                 const int all_hi = p_first < 0 ? 0 : min(at.s.len, max(p_first + 1, at.s.prefix));
                 const int all_lo = p.window ? p_last - p.window + 1 : 0;
-                const float slope = EXTRA && p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
+                const float slope = MODE != kPfPlain && p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
                 float m = -INFINITY, l = 0.f;
                 for (int u = at.u; u < at.u + n; ++u) {
                     if (!(ok = warp_wait(&sh->sfull[t], su & 1, pp, sh))) break;
@@ -730,8 +764,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         pf_ld_wait(s);
 #pragma unroll
                         for (int q = 1; q < 4; ++q) pf_tie(s + 32 * q);
-                        pf_softmax<BF16, EXTRA>(s, s_tmem, o_tmem, D, j0 < all_lo || j0 + kPfKeys > all_hi, lo - j0, hi - j0, c,
-                                                p.softcap, slope, (float)(j0 - pos), u == at.u, m, l);
+                        pf_softmax<BF16, MODE>(s, s_tmem, o_tmem, D, j0 < all_lo || j0 + kPfKeys > all_hi, lo - j0, hi - j0, p.scale,
+                                                p.cap, slope, (float)(j0 - pos), u == at.u, m, l);
                         tmem_st_wait();
                     }
                     tc_fence_before();
@@ -865,14 +899,14 @@ static bool pf_map(CUtensorMap *m, const void *base, const KvView &c, int D, boo
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool BF16, bool EXTRA>
+template <int D, bool BF16, int MODE>
 static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st)
 {
     CUtensorMap kmap, vmap;
     if (!pf_map(&kmap, p.a.c.k, p.a.c, D, BF16, p.box_rows) || !pf_map(&vmap, p.a.c.v, p.a.c, D, BF16, p.box_rows))
         return cudaErrorInvalidValue;
     using Sh = PfShape<D>;
-    auto k = prefill_kernel<D, BF16, EXTRA>;
+    auto k = prefill_kernel<D, BF16, MODE>;
     static std::atomic<bool> known{false};  // (the same build on every device)
     cudaError_t e = cudaSuccess;
     if (!known.load(std::memory_order_relaxed)) {
@@ -894,6 +928,14 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
     return e;
 }
 
+template <int D, bool BF16>
+static cudaError_t launch_prefill_m(const PfParams &p, int mode, int ctas, cudaStream_t st)
+{
+    return mode == kPfCap    ? launch_prefill_t<D, BF16, kPfCap>(p, ctas, st)
+           : mode == kPfBias ? launch_prefill_t<D, BF16, kPfBias>(p, ctas, st)
+                             : launch_prefill_t<D, BF16, kPfPlain>(p, ctas, st);
+}
+
 int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st)
 {
     if ((int64_t)a.b.tokens * a.group > 0x7fffffff - kPfRows)
@@ -905,17 +947,13 @@ int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st
     p.timeout_ns = wait_bound_ns();
     p.debug = debug_flags();
     p.box_rows = std::min(a.c.page_size & -a.c.page_size, kPfKeys);
-    const bool extra = a.softcap > 0.f || a.slopes;
+    const int mode = a.cap > 0.f ? kPfCap : a.slopes ? kPfBias : kPfPlain;
     int nsm = 0;
     cudaError_t e = sm_count(&nsm);
     if (e == cudaSuccess) {
         const int ctas = nsm < kAttnMaxSms ? nsm : kAttnMaxSms;
-        auto f = head_dim == 64
-                     ? (bf16 ? (extra ? launch_prefill_t<64, true, true> : launch_prefill_t<64, true, false>)
-                             : (extra ? launch_prefill_t<64, false, true> : launch_prefill_t<64, false, false>))
-                     : (bf16 ? (extra ? launch_prefill_t<128, true, true> : launch_prefill_t<128, true, false>)
-                             : (extra ? launch_prefill_t<128, false, true> : launch_prefill_t<128, false, false>));
-        e = f(p, ctas, st);
+        e = head_dim == 64 ? (bf16 ? launch_prefill_m<64, true>(p, mode, ctas, st) : launch_prefill_m<64, false>(p, mode, ctas, st))
+                           : (bf16 ? launch_prefill_m<128, true>(p, mode, ctas, st) : launch_prefill_m<128, false>(p, mode, ctas, st));
     }
     if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "prefill launch: %s", cudaGetErrorString(e));
     return MC_OK;

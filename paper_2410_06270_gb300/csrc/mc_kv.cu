@@ -11,6 +11,13 @@ namespace mc {
 constexpr int kAppendPasses = 4;  // rows a half or quarter warp takes, loads first
 constexpr int kAppendThreads = 128;
 
+__device__ __forceinline__ void turned(float &a, float &b, float c, float s)
+{
+    const float t = a;
+    a = t * c - b * s;
+    b = b * c + t * s;
+}
+
 // A head's row of D elements is shared by D / 8 lanes; a warp's 256 / D rows times
 // kAppendPasses are heads of one token (its queries, keys, then values), so the token's
 // position, page and rotation are found once for them.  A lane holds two runs of four
@@ -53,12 +60,10 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
         }
     }
 
-    const int s = token_seq(p.b, t, lane);
+    const TokenPlace place = token_place(p.b, p.c, t, lane, p.status);
+    const int s = place.seq;
     if (s < 0) return;  // padding
-    int first, pos = -1, row = 0;
-    const int n = seq_rows(p.b, s, first, p.status);
-    const int len = seq_len(p.b, p.c, s, p.status);
-    if (t >= first && t - first < n) pos = len - n + (t - first);
+    int pos = place.pos, row = 0;
     int64_t at = -1;  // the row's element offset in the cache
     float4 cs = make_float4(1.f, 1.f, 1.f, 1.f), sn = make_float4(0.f, 0.f, 0.f, 0.f);
     if (pos >= 0) {
@@ -107,12 +112,13 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
         }
         if (turn && (is_q || is_k)) {
             const float c4[4] = {cs.x, cs.y, cs.z, cs.w}, s4[4] = {sn.x, sn.y, sn.z, sn.w};
+            // (two static forms: indices chosen at run time put x into local memory)
+            if (p.interleaved) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int u = p.interleaved ? 2 * e : e, w = p.interleaved ? 2 * e + 1 : e + 4;
-                const float xu = x[u], xw = x[w];
-                x[u] = xu * c4[e] - xw * s4[e];
-                x[w] = xw * c4[e] + xu * s4[e];
+                for (int e = 0; e < 4; ++e) turned(x[2 * e], x[2 * e + 1], c4[e], s4[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) turned(x[e], x[e + 4], c4[e], s4[e]);
             }
         }
         if (pos < 0) {
