@@ -49,9 +49,10 @@ struct PfShared {
     uint64_t drain, vpatch;
     uint32_t tmem_base;
     volatile int abort;
-    int b, h, mt, u;                                     // this CTA's first unit
-    int64_t total;
-    int sums[32];
+    int b[2], h[2], mt[2], u[2];                         // where this CTA's run starts and ends
+    int off;                                             // the end's cost offset in its item
+    int64_t total;                                       // cost of the batch
+    int sums[2][32];
 };
 
 template <int D>
@@ -168,36 +169,40 @@ __device__ __forceinline__ void pf_next_item(const AttnParams &p, PfPlace &at)
     at.k = pf_keys(p, at.s, at.mt);
 }
 
-// This CTA's run of units, read by each role for itself (held from before the roles part,
-// it would be spilled by the softmax's need of registers for all of them).
+// What an item costs on top of its units, in units: the change of queries, the first
+// unit's softmax with no other work beside it, the epilogue.  Runs are equal in cost
+// (equal in units alone, a CTA with the 29 short items at a causal prompt's start took a
+// third longer than the mean: 8192 tokens 489 us against 364).
+constexpr int kPfItemCost = 2;
+
+// The end of this CTA's run, read by each role for itself (state held from before the
+// roles part would be spilled for all of them by the softmax's need of registers).
 struct PfRun {
-    int64_t total, ctas, u1;
-    int left;
+    int b, h, mt, u;
 };
 
 __device__ __forceinline__ PfRun pf_run(const AttnParams &p, const volatile PfShared *sh, PfPlace &at)
 {
-    PfRun r;
-    r.total = sh->total;
-    r.ctas = r.total < (int64_t)gridDim.x ? r.total : gridDim.x;
-    at.b = sh->b;
-    at.h = sh->h;
-    at.mt = sh->mt;
-    at.u = sh->u;
-    r.u1 = 0;
-    r.left = 0;
+    at.b = sh->b[0];
+    at.h = sh->h[0];
+    at.mt = sh->mt[0];
+    at.u = sh->u[0];
     if (at.b >= 0) {
-        r.u1 = r.total * (blockIdx.x + 1) / r.ctas;
-        r.left = (int)(r.u1 - r.total * blockIdx.x / r.ctas);
         at.s = pf_seq(p, at.b, nullptr);
         at.k = pf_keys(p, at.s, at.mt);
     }
-    return r;
+    return {sh->b[1], sh->h[1], sh->mt[1], sh->u[1]};
 }
 
-// Sums of units of 32 sequences from b0 on (per key head) into sh->sums, by one warp: the
+// Units of the item at hand that belong to the run; 0: the run is over.
+__device__ __forceinline__ int pf_units(const PfRun &r, const PfPlace &at)
+{
+    return (at.b == r.b && at.h == r.h && at.mt == r.mt ? r.u : at.k.units) - at.u;
+}
+
+// Costs of 32 sequences from b0 on (per key head) into sums, by one warp: the
 // sequences' items are laid end to end and taken 32 at a time.  Returns their total.
-__device__ __forceinline__ int64_t pf_sums(const AttnParams &p, PfShared *sh, int b0, int lane, int32_t *status)
+__device__ __forceinline__ int64_t pf_sums(const AttnParams &p, int *sums, int b0, int lane, int32_t *status)
 {
     PfSeq s = {0, 0, 0, 0};
     if (b0 + lane < p.b.seqs) s = pf_seq(p, b0 + lane, status);
@@ -210,7 +215,7 @@ __device__ __forceinline__ int64_t pf_sums(const AttnParams &p, PfShared *sh, in
     }
     const int all = __shfl_sync(0xffffffffu, upto, 31);
     __syncwarp();
-    sh->sums[lane] = 0;
+    sums[lane] = 0;
     __syncwarp();
     for (int i0 = 0; i0 < all; i0 += 32) {
         const int i = i0 + lane;
@@ -225,10 +230,10 @@ __device__ __forceinline__ int64_t pf_sums(const AttnParams &p, PfShared *sh, in
         t.len = __shfl_sync(0xffffffffu, s.len, own);
         t.prefix = __shfl_sync(0xffffffffu, s.prefix, own);
         const int before = __shfl_sync(0xffffffffu, upto - tiles, own);
-        if (i < all) atomicAdd(&sh->sums[own], pf_keys(p, t, i - before).units);
+        if (i < all) atomicAdd(&sums[own], pf_keys(p, t, i - before).units + kPfItemCost);
     }
     __syncwarp();
-    int64_t sum = sh->sums[lane];
+    int64_t sum = sums[lane];
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum;
@@ -486,17 +491,20 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     }
     if (warp == kPfMma) tmem_alloc(&sh->tmem_base, 512);
     pdl_wait();
-    if (warp == 0) {
+    if (warp < 2) {
+        // where the run starts (warp 0) and ends (warp 1)
+        int *sums = sh->sums[warp];
         int64_t total = 0;
-        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) total += pf_sums(p, sh, b0, lane, p.status);
+        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) total += pf_sums(p, sums, b0, lane, p.status);
         total *= p.c.kv_heads;
         const int64_t ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
-        int fb = -1, fh = 0, fmt = 0, fu = 0;
+        int fb = -1, fh = 0, fmt = 0, fu = 0, off = 0;
         if ((int64_t)blockIdx.x < ctas) {
-            int64_t r = total * blockIdx.x / ctas;  // units before this CTA's first
+            int64_t r = total * (blockIdx.x + warp) / ctas;  // cost before the place
+            if (r == total) fb = p.b.seqs;
             for (int b0 = 0; b0 < p.b.seqs && fb < 0; b0 += 32) {
-                if (p.b.seqs > 32) pf_sums(p, sh, b0, lane, nullptr);
-                const int64_t own = (int64_t)sh->sums[lane] * p.c.kv_heads;
+                if (p.b.seqs > 32) pf_sums(p, sums, b0, lane, nullptr);
+                const int64_t own = (int64_t)sums[lane] * p.c.kv_heads;
                 int64_t upto = own;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
@@ -504,43 +512,47 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                     if (lane >= d) upto += o;
                 }
                 const unsigned hit = __ballot_sync(0xffffffffu, upto > r);
-                if (hit) {
-                    const int who = __ffs(hit) - 1;
-                    r -= __shfl_sync(0xffffffffu, upto - own, who);
-                    const int per = __shfl_sync(0xffffffffu, sh->sums[lane], who);
-                    fb = b0 + who;
-                    fh = (int)(r / per);
-                    int left = (int)(r % per);
-                    const PfSeq s = pf_seq(p, fb, nullptr);
-                    const int tiles = pf_tiles(p, s);
-                    for (int t0 = 0; t0 < tiles; t0 += 32) {
-                        const int n = t0 + lane < tiles ? pf_keys(p, s, t0 + lane).units : 0;
-                        int sum = n;
-#pragma unroll
-                        for (int d = 1; d < 32; d <<= 1) {
-                            const int o = __shfl_up_sync(0xffffffffu, sum, d);
-                            if (lane >= d) sum += o;
-                        }
-                        const unsigned in = __ballot_sync(0xffffffffu, sum > left);
-                        if (in) {
-                            const int w = __ffs(in) - 1;
-                            fmt = t0 + w;
-                            fu = left - __shfl_sync(0xffffffffu, sum - n, w);
-                            break;
-                        }
-                        left -= __shfl_sync(0xffffffffu, sum, 31);
-                    }
-                } else {
+                if (!hit) {
                     r -= __shfl_sync(0xffffffffu, upto, 31);
+                    continue;
+                }
+                const int who = __ffs(hit) - 1;
+                r -= __shfl_sync(0xffffffffu, upto - own, who);
+                const int per = __shfl_sync(0xffffffffu, sums[lane], who);
+                fb = b0 + who;
+                fh = (int)(r / per);
+                off = (int)(r % per);
+                const PfSeq s = pf_seq(p, fb, nullptr);
+                const int tiles = pf_tiles(p, s);
+                for (int t0 = 0; t0 < tiles; t0 += 32) {
+                    const int n = t0 + lane < tiles ? pf_keys(p, s, t0 + lane).units + kPfItemCost : 0;
+                    int sum = n;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const int o = __shfl_up_sync(0xffffffffu, sum, d);
+                        if (lane >= d) sum += o;
+                    }
+                    const unsigned in = __ballot_sync(0xffffffffu, sum > off);
+                    if (in) {
+                        const int w = __ffs(in) - 1;
+                        fmt = t0 + w;
+                        off -= __shfl_sync(0xffffffffu, sum - n, w);
+                        fu = max(0, off - kPfItemCost);
+                        break;
+                    }
+                    off -= __shfl_sync(0xffffffffu, sum, 31);
                 }
             }
         }
         if (lane == 0) {
-            sh->total = total;
-            sh->b = fb;
-            sh->h = fh;
-            sh->mt = fmt;
-            sh->u = fu;
+            sh->b[warp] = fb;
+            sh->h[warp] = fh;
+            sh->mt[warp] = fmt;
+            sh->u[warp] = fu;
+            if (warp) {
+                sh->total = total;
+                sh->off = off;
+            }
         }
     }
     tc_fence_before();
@@ -552,20 +564,19 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
       if (warp >= kPfKv) {
         // -------------------------------------------------------------- copies --
         PfPlace at;
-        int left = pp.debug & kDebugNoProducer ? 0 : pf_run(p, sh, at).left;
+        const PfRun run = pf_run(p, sh, at);
         const uint32_t smem0 = smem_u32(smem);
         if (warp == kPfKv) {
             // keys and values: lane i copies the i-th box (of a page) of a tile.  A page that is
             // not there, and rows past the last key's page, are read beyond the map: zeros.
             const int boxes = kPfKeys / pp.box_rows;
-            int it = 0, patches = 0;
-            bool ok = true;
+            int it = 0, patches = 0, n;
+            bool ok = !(pp.debug & kDebugNoProducer);
             auto pages = [&](int u) {
                 const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
                 return lane < boxes && j < at.k.end ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + j / p.c.page_size) : -1;
             };
-            while (ok && left > 0) {
-                const int n = min(left, at.k.units - at.u);
+            while (ok && (n = pf_units(run, at)) > 0) {
                 int page = pages(at.u);
                 for (int u = at.u; ok && u < at.u + n; ++u) {
                     const int next = u + 1 < at.u + n ? pages(u + 1) : -1;  // used a unit later
@@ -605,8 +616,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                     }
                     page = next;
                 }
-                left -= n;
-                if (left > 0) pf_next_item(p, at);
+                if (at.u + n < at.k.units) break;
+                pf_next_item(p, at);
             }
             // the last copies land before the block's shared memory is given back, on an abort too
             const uint64_t t0 = globaltimer_ns();
@@ -621,8 +632,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
             const int step_hg = kQStep % p.group;
             const int64_t q_step = kQStep / p.group * p.q_stride + step_hg * D, q_wrap = p.q_stride - p.group * D;
-            int items = 0;
-            while (left > 0) {
+            int items = 0, n;
+            while ((n = pf_units(run, at)) > 0) {
                 const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
                 const int fill = rows > kPfTile ? kPfRows : kPfTile;
                 int r = (warp - kPfQ0) * kPer + lr;
@@ -643,21 +654,21 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 fence_proxy_async_smem();
                 mbar_arrive(&sh->qfull);
                 ++items;
-                left -= min(left, at.k.units - at.u);
-                if (left > 0) pf_next_item(p, at);
+                if (at.u + n < at.k.units) break;
+                pf_next_item(p, at);
             }
         }
       } else {
         // ---------------------------------------------------------------- MMAs --
         PfPlace at;
-        int left = pf_run(p, sh, at).left;
+        const PfRun run = pf_run(p, sh, at);
         constexpr uint32_t kIdS = pf_idesc(BF16, kPfKeys, false), kIdO = pf_idesc(BF16, D, true);
         uint64_t qd[2];
         for (int t = 0; t < 2; ++t) qd[t] = umma_desc_sw128(smem + Sh::kHdr + t * Sh::kTileBytes);
         const uint64_t kd0 = umma_desc_sw128(smem + Sh::kRing);
         const uint64_t vd0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
         constexpr uint64_t kStep = Sh::kTileBytes >> 4;
-        int kt = 0, items = 0, uses[2] = {0, 0};
+        int kt = 0, items = 0, uses[2] = {0, 0}, n;
         bool ok = true;
         auto qk = [&](int t, int slot) {  // S_t = Q_t K^T
             const uint64_t b = kd0 + slot * kStep;
@@ -674,8 +685,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 umma_f16_ts(tbase + 256 + 128 * t, tbase + 128 * t + 8 * s, b + s * (2048 >> 4), kIdO, !first || s > 0);
         };
         auto full = [&](int i) { return warp_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1, pp, sh); };
-        while (ok && left > 0) {
-            const int n = min(left, at.k.units - at.u);
+        while (ok && (n = pf_units(run, at)) > 0) {
             const int tiles = at.s.n * p.group - at.mt * kPfRows > kPfTile ? 2 : 1;
             // kt: ring index of unit j's keys, kt + 1 its values
             if (!(ok = warp_wait(&sh->qfull, items & 1, pp, sh) && full(kt))) break;
@@ -715,8 +725,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 }
             }
             ++items;
-            left -= n;
-            if (left > 0) pf_next_item(p, at);
+            if (at.u + n < at.k.units) break;
+            pf_next_item(p, at);
         }
         // the tensor pipe is idle before shared and tensor memory are given back
         if (elect_one()) umma_commit(&sh->drain);
@@ -730,14 +740,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         pf_take_regs();
         PfPlace at;
         const PfRun run = pf_run(p, sh, at);
-        int left = run.left;
         const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
         const uint32_t lanes = (uint32_t)(wt * 32) << 16;
         const uint32_t s_tmem = tbase + lanes + 128 * t, o_tmem = tbase + lanes + 256 + 128 * t;
-        int su = 0, ou = 0;
+        int su = 0, ou = 0, n;
         bool ok = true, tail = false;
-        while (ok && left > 0) {
-            const int n = min(left, at.k.units - at.u);
+        while (ok && (n = pf_units(run, at)) > 0) {
             const int rows0 = at.mt * kPfRows + t * kPfTile, rows = min(kPfTile, at.s.n * p.group - rows0);
             const bool from_first = at.u == 0, to_last = at.u + n == at.k.units;
             if (rows > 0) {
@@ -812,12 +820,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             if (from_first && !to_last) {
                 tail = true;
                 if (tid == 0) {
-                    const int64_t end = run.u1 - left + at.k.units;
-                    pp.open[blockIdx.x] = {(int32_t)((end * run.ctas + run.total - 1) / run.total - blockIdx.x), at.b, at.h, at.mt};
+                    // the pieces lie in the CTAs whose runs start before the item's end
+                    const int64_t total = sh->total, ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
+                    const int64_t end = total * (blockIdx.x + 1) / ctas - sh->off + kPfItemCost + at.k.units;
+                    pp.open[blockIdx.x] = {(int32_t)((end * ctas + total - 1) / total - blockIdx.x), at.b, at.h, at.mt};
                 }
             }
-            left -= n;
-            if (left > 0) pf_next_item(p, at);
+            if (at.u + n < at.k.units) break;
+            pf_next_item(p, at);
         }
         if (!tail && tid == 0) pp.open[blockIdx.x].pieces = 0;
     }
@@ -830,43 +840,49 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     }
 }
 
-// 32 rows of a CTA's open item: adds its pieces in their order.
+// 16 rows of a CTA's open item: adds its pieces in their order, the loads of four pieces
+// in flight at once.
+constexpr int kPfJoinRows = 16;
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
 {
+    constexpr int kQuads = D / 4 / 16;  // column quads of a thread: threadIdx.x / 16, + 16, ...
+    __shared__ float2 ml[kAttnMaxSms][kPfJoinRows];
     const AttnParams &p = pp.a;
     pdl_trigger();
     pdl_wait();
     const PfOpen it = pp.open[blockIdx.x];
     if (it.pieces == 0) return;
+    const int r = threadIdx.x % kPfJoinRows, c0 = threadIdx.x / kPfJoinRows, row = blockIdx.y * kPfJoinRows + r;
+    auto piece = [&](int i) { return pp.part + (2 * ((size_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * pf_part_floats(D); };
+    for (int i = c0; i < it.pieces; i += 16) ml[i][r] = reinterpret_cast<const float2 *>(piece(i) + kPfRows * D)[row];
     const PfSeq s = pf_seq(p, it.b, nullptr);
-    const int lane = threadIdx.x & 31, row = blockIdx.y * 32 + lane, f = it.mt * kPfRows + row;
+    const int f = it.mt * kPfRows + row;
+    __syncthreads();
     if (f >= s.n * p.group) return;
     const int tok = f / p.group, head = it.h * p.group + f % p.group;
-    auto piece = [&](int i) { return pp.part + (2 * ((size_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * pf_part_floats(D); };
     float top = -INFINITY;
-    for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, piece(i)[kPfRows * D + 2 * row]);
-    float4 acc[D / 32];
+    for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, ml[i][r].x);
+    float4 acc[kQuads];
 #pragma unroll
-    for (int k = 0; k < D / 32; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < kQuads; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
-    const int c0 = threadIdx.x >> 5;  // this warp's column quads: c0, c0 + 8, ...
+#pragma unroll 4
     for (int i = 0; i < it.pieces; ++i) {
         const float *q = piece(i);
-        const float2 ml = reinterpret_cast<const float2 *>(q + kPfRows * D)[row];
-        const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
-        sum = fmaf(w, ml.y, sum);
+        const float w = ml[i][r].x == -INFINITY ? 0.f : ex2(ml[i][r].x - top);
+        sum = fmaf(w, ml[i][r].y, sum);
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            const float4 v = reinterpret_cast<const float4 *>(q)[(size_t)(c0 + 8 * k) * kPfRows + row];
+        for (int k = 0; k < kQuads; ++k) {
+            const float4 v = reinterpret_cast<const float4 *>(q)[(size_t)(c0 + 16 * k) * kPfRows + row];
             acc[k] = make_float4(fmaf(w, v.x, acc[k].x), fmaf(w, v.y, acc[k].y), fmaf(w, v.z, acc[k].z), fmaf(w, v.w, acc[k].w));
         }
     }
     const float inv = 1.f / sum;
     uint16_t *out = p.out + (s.first + tok) * p.out_stride + head * D;
 #pragma unroll
-    for (int k = 0; k < D / 32; ++k)
-        *reinterpret_cast<uint2 *>(out + 4 * (c0 + 8 * k)) =
+    for (int k = 0; k < kQuads; ++k)
+        *reinterpret_cast<uint2 *>(out + 4 * (c0 + 16 * k)) =
             sum == 0.f ? make_uint2(0, 0)
                        : make_uint2(pack2<BF16>(acc[k].x * inv, acc[k].y * inv), pack2<BF16>(acc[k].z * inv, acc[k].w * inv));
     if (p.lse && c0 == 0) p.lse[(int64_t)(s.first + tok) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
@@ -923,7 +939,7 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
     profile_end(kKAttnPrefill, st);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnJoin, st);
-    e = launch_k(prefill_join_kernel<D, BF16>, dim3(ctas, kPfRows / 32), dim3(256), 0, st, p);
+    e = launch_k(prefill_join_kernel<D, BF16>, dim3(ctas, kPfRows / kPfJoinRows), dim3(256), 0, st, p);
     profile_end(kKAttnJoin, st);
     return e;
 }
