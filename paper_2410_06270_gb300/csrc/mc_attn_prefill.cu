@@ -20,8 +20,8 @@
 // triangle, by the same rule.
 //
 // Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 issues the MMAs,
-// 9 copies keys and values (TMA, a box per page and 64 columns), 10-11 the queries (cp.async:
-// their rows are heads of tokens at any stride).
+// 9 copies keys and values (TMA, a box per page and 64 columns), 10 the queries (TMA where a
+// tile is whole tokens of the group's heads, else with 11 by cp.async).
 // Tensor memory: S (and P) of tile t at column 128 t, O at 256 + 128 t.
 #include <math.h>
 
@@ -44,8 +44,7 @@ constexpr float kPfLazy = 8.f;
 
 struct PfShared {
     uint64_t kfull[kPfMaxStages], kempty[kPfMaxStages];  // ring of keys / values
-    uint64_t qfull, qempty;
-    uint64_t sfull[2], pfull[2], ofull[2];               // per tile
+    uint64_t qfull[2], qempty[2], sfull[2], pfull[2], ofull[2];  // per tile
     uint64_t drain, vpatch;
     uint32_t tmem_base;
     volatile int abort;
@@ -75,6 +74,8 @@ struct PfParams {
     float *part;
     uint64_t timeout_ns;
     int debug;
+    int q_boxes;   // a tile's queries are boxes of whole groups of heads (the group divides 128)
+    int out32;     // rows of the output start at multiples of 32 bytes
     int box_rows;  // rows of a copied box: the largest power of two that divides a page, at most a unit
 };
 
@@ -329,13 +330,32 @@ __host__ __device__ constexpr uint32_t pf_idesc(bool bf16, int N, bool b_mn)
            ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-// Descriptor of a value tile as B operand, N (d) contiguous, 128-byte swizzle: atoms of 64
-// d x 8 keys, 1024 bytes from one group of 8 keys to the next (stride), a half-tile from one
-// 64-column block to the next (leading).
-__device__ __forceinline__ uint64_t pf_desc_mn(uint32_t addr, uint32_t half)
+// Shared-memory descriptors, 128-byte swizzle: the upper word is the same for all operands
+// here (1024 bytes from one group of 8 rows, or keys, to the next), so a descriptor is its
+// lower word, and the steps along a tile are additions to it.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+// Rows of 64 columns, K contiguous.
+__device__ __forceinline__ uint32_t pf_desc_k(uint32_t addr) { return ((addr >> 4) & 0x3FFFu) | (1u << 16); }
+// A value tile as B operand, N (d) contiguous: atoms of 64 d x 8 keys, a half-tile from one
+// 64-column block to the next.
+__device__ __forceinline__ uint32_t pf_desc_mn(uint32_t addr, uint32_t half) { return ((addr >> 4) & 0x3FFFu) | ((half >> 4) << 16); }
+
+__device__ __forceinline__ void pf_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate)
 {
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(half >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
-           ((uint64_t)1u << 46) | ((uint64_t)2u << 61);
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHi)
+        : "memory");
+}
+
+__device__ __forceinline__ void pf_mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
+        "r"(a_tmem), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHi)
+        : "memory");
 }
 
 // One box of a page: 64 columns from c on, rows from r on, of a head.
@@ -343,6 +363,13 @@ __device__ __forceinline__ void pf_tma(uint32_t dst, const CUtensorMap *map, int
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
                  "l"(map), "r"(smem_u32(bar)), "r"(c), "r"(r), "r"(head), "r"(page)
+                 : "memory");
+}
+
+__device__ __forceinline__ void pf_tma3(uint32_t dst, const CUtensorMap *map, int c, int head, int token, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(smem_u32(bar)), "r"(c), "r"(head), "r"(token)
                  : "memory");
 }
 
@@ -464,7 +491,8 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 
 template <int D, bool BF16, int MODE>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams pp, const __grid_constant__ CUtensorMap kmap,
-                                                                   const __grid_constant__ CUtensorMap vmap)
+                                                                   const __grid_constant__ CUtensorMap vmap,
+                                                                   const __grid_constant__ CUtensorMap qmap)
 {
     using Sh = PfShape<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -478,9 +506,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             mbar_init(&sh->kempty[i], 1);
         }
         mbar_init(&sh->vpatch, 1);
-        mbar_init(&sh->qfull, 32 * kPfQWarps);
-        mbar_init(&sh->qempty, 1);
         for (int t = 0; t < 2; ++t) {
+            mbar_init(&sh->qfull[t], pp.q_boxes ? 1 : 32 * kPfQWarps);
+            mbar_init(&sh->qempty[t], 1);
             mbar_init(&sh->sfull[t], 1);
             mbar_init(&sh->pfull[t], 4);
             mbar_init(&sh->ofull[t], 1);
@@ -558,7 +586,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tbase = sh->tmem_base;
+    // All 512 columns are this block's, so they start at column 0: constant addresses below
+    if (sh->tmem_base != 0) {
+        if (tid == 0) set_status(p.status, MC_ERR_CUDA);
+        sh->abort = 1;
+    }
     if (warp >= kPfMma) {
       pf_give_regs();  // one instruction for the warpgroup
       if (warp >= kPfKv) {
@@ -625,37 +657,57 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1)))
                     if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
             pdl_trigger();
-        } else {
-            // queries, one row per 16-byte lane group, zeros past the last
+        } else if (warp == kPfQ0 || !pp.q_boxes) {
+            // queries, a tile as soon as the last item's has been read
             constexpr int kChunks = D / 8, kPer = 32 / kChunks, kQStep = kPfQWarps * kPer;
             const int lc = lane % kChunks, lr = lane / kChunks;
             const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
             const int step_hg = kQStep % p.group;
             const int64_t q_step = kQStep / p.group * p.q_stride + step_hg * D, q_wrap = p.q_stride - p.group * D;
-            int items = 0, n;
-            while ((n = pf_units(run, at)) > 0) {
+            int uses[2] = {0, 0}, n;
+            bool ok = !(pp.debug & kDebugNoProducer);
+            while (ok && (n = pf_units(run, at)) > 0) {
                 const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
-                const int fill = rows > kPfTile ? kPfRows : kPfTile;
-                int r = (warp - kPfQ0) * kPer + lr;
-                int hg = (rows0 + r) % p.group;
-                const uint16_t *src = p.q + (at.s.first + (rows0 + r) / p.group) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
-                if (items && !warp_wait(&sh->qempty, (items + 1) & 1, pp, sh)) break;
-                for (; r < fill; r += kQStep) {
-                    const uint32_t d = smem0 + Sh::kHdr + (r >> 7) * Sh::kTileBytes + col + (r & 127) * 128;
-                    const bool real = r < rows;
-                    pf_copy16z(d ^ ((r & 7) << 4), real ? src : p.q, real);
-                    src += q_step;
-                    if ((hg += step_hg) >= p.group) {
-                        hg -= p.group;
-                        src += q_wrap;
+                for (int t = 0; t < 2 && t * kPfTile < rows; ++t) {
+                    if (uses[t] && !(ok = warp_wait(&sh->qempty[t], (uses[t] + 1) & 1, pp, sh))) break;
+                    ++uses[t];
+                    const uint32_t tile = smem0 + Sh::kHdr + t * Sh::kTileBytes;
+                    if (pp.q_boxes) {
+                        // rows past the sequence's last are other tokens', or zeros: not stored
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(&sh->qfull[t], Sh::kTileBytes);
+#pragma unroll
+                            for (int h = 0; h < D / 64; ++h)
+                                pf_tma3(tile + h * Sh::kHalf, &qmap, 64 * h, at.h * p.group,
+                                        at.s.first + (rows0 + t * kPfTile) / p.group, &sh->qfull[t]);
+                        }
+                        continue;
                     }
+                    // one row per kChunks lanes, zeros past the last
+                    int r = t * kPfTile + (warp - kPfQ0) * kPer + lr;
+                    int hg = (rows0 + r) % p.group;
+                    const uint16_t *src = p.q + (at.s.first + (rows0 + r) / p.group) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
+                    for (; r < (t + 1) * kPfTile; r += kQStep) {
+                        const bool real = r < rows;
+                        pf_copy16z((tile + col + (r & 127) * 128) ^ ((r & 7) << 4), real ? src : p.q, real);
+                        src += q_step;
+                        if ((hg += step_hg) >= p.group) {
+                            hg -= p.group;
+                            src += q_wrap;
+                        }
+                    }
+                    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+                    fence_proxy_async_smem();
+                    mbar_arrive(&sh->qfull[t]);
                 }
-                asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-                fence_proxy_async_smem();
-                mbar_arrive(&sh->qfull);
-                ++items;
-                if (at.u + n < at.k.units) break;
+                if (!ok || at.u + n < at.k.units) break;
                 pf_next_item(p, at);
+            }
+            if (pp.q_boxes) {  // the last copies land before the block's shared memory is given back
+                const uint64_t t0 = globaltimer_ns();
+                for (int t = 0; t < 2; ++t)
+                    while (uses[t] && !__all_sync(0xffffffffu, mbar_try_wait(&sh->qfull[t], (uses[t] + 1) & 1)))
+                        if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
             }
         }
       } else {
@@ -663,70 +715,102 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         PfPlace at;
         const PfRun run = pf_run(p, sh, at);
         constexpr uint32_t kIdS = pf_idesc(BF16, kPfKeys, false), kIdO = pf_idesc(BF16, D, true);
-        uint64_t qd[2];
-        for (int t = 0; t < 2; ++t) qd[t] = umma_desc_sw128(smem + Sh::kHdr + t * Sh::kTileBytes);
-        const uint64_t kd0 = umma_desc_sw128(smem + Sh::kRing);
-        const uint64_t vd0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
-        constexpr uint64_t kStep = Sh::kTileBytes >> 4;
-        int kt = 0, items = 0, uses[2] = {0, 0}, n;
+        const uint32_t q0 = pf_desc_k(smem_u32(smem + Sh::kHdr)), k0 = pf_desc_k(smem_u32(smem + Sh::kRing));
+        const uint32_t v0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
+        constexpr uint32_t kStep = Sh::kTileBytes >> 4;
+        int uses[2] = {0, 0}, quses[2] = {0, 0};
         bool ok = true;
         auto qk = [&](int t, int slot) {  // S_t = Q_t K^T
-            const uint64_t b = kd0 + slot * kStep;
+            const uint32_t a = q0 + t * kStep, b = k0 + slot * kStep;
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
-                const uint64_t o = (s >> 2) * (Sh::kHalf >> 4) + (s & 3) * 2;
-                umma_f16(tbase + 128 * t, qd[t] + o, b + o, kIdS, s > 0);
+                const uint32_t o = (s >> 2) * (Sh::kHalf >> 4) + (s & 3) * 2;
+                pf_mma_ss(128 * t, a + o, b + o, kIdS, s > 0);
             }
         };
         auto pv = [&](int t, int slot, bool first) {  // O_t (+)= P_t V
-            const uint64_t b = vd0 + slot * kStep;
+            const uint32_t b = v0 + slot * kStep;
 #pragma unroll
-            for (int s = 0; s < kPfKeys / 16; ++s)
-                umma_f16_ts(tbase + 256 + 128 * t, tbase + 128 * t + 8 * s, b + s * (2048 >> 4), kIdO, !first || s > 0);
+            for (int s = 0; s < kPfKeys / 16; ++s) pf_mma_ts(256 + 128 * t, 128 * t + 8 * s, b + s * (2048 >> 4), kIdO, !first || s > 0);
         };
-        auto full = [&](int i) { return warp_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1, pp, sh); };
-        while (ok && (n = pf_units(run, at)) > 0) {
-            const int tiles = at.s.n * p.group - at.mt * kPfRows > kPfTile ? 2 : 1;
-            // kt: ring index of unit j's keys, kt + 1 its values
-            if (!(ok = warp_wait(&sh->qfull, items & 1, pp, sh) && full(kt))) break;
+        struct Slot {
+            int i;
+            uint32_t phase;
+            __device__ Slot next() const { return i + 1 == Sh::kStages ? Slot{0, phase ^ 1u} : Slot{i + 1, phase}; }
+        };
+        auto full = [&](const Slot &x) { return warp_wait(&sh->kfull[x.i], x.phase, pp, sh); };
+        auto tiles_of = [&](const PfPlace &a) { return a.s.n * p.group - a.mt * kPfRows > kPfTile ? 2 : 1; };
+        // Unit j's PV of a tile is followed by unit j + 1's QK of it, the next item's first one
+        // after the last: the next queries and the other tile's softmax hide the change of item.
+        Slot k = {0, 0};  // of the last keys that QK was issued for
+        int n = pf_units(run, at), tiles = n > 0 ? tiles_of(at) : 0;
+        auto issue_qk = [&](int t, const Slot &x, bool last_tile, bool last_unit) {
             tc_fence_after();
             if (elect_one()) {
-                for (int t = 0; t < tiles; ++t) {
-                    qk(t, kt % Sh::kStages);
-                    umma_commit(&sh->sfull[t]);
-                }
-                umma_commit(&sh->kempty[kt % Sh::kStages]);
-                if (n == 1) umma_commit(&sh->qempty);
+                qk(t, x.i);
+                umma_commit(&sh->sfull[t]);
+                if (last_tile) umma_commit(&sh->kempty[x.i]);
+                if (last_unit) umma_commit(&sh->qempty[t]);
             }
             __syncwarp();
-            for (int j = 0; ok && j < n; ++j, kt += 2) {
-                const bool more = j + 1 < n;
-                if (!(ok = full(kt + 1))) break;
+        };
+        if (n > 0) ok = full(k);
+        for (int t = 0; ok && t < tiles; ++t)
+            if ((ok = warp_wait(&sh->qfull[t], quses[t]++ & 1, pp, sh))) issue_qk(t, k, t == tiles - 1, n == 1);
+        while (ok && n > 0) {
+            PfPlace nx = at;
+            int next_n = 0, next_tiles = 0;
+            if (at.u + n == at.k.units) {
+                pf_next_item(p, nx);
+                next_n = pf_units(run, nx);
+                if (next_n > 0) next_tiles = tiles_of(nx);
+            }
+            // inside the item: unit j's PV and unit j + 1's QK of a tile are issued together
+            for (int j = 0; ok && j + 1 < n; ++j) {
+                const Slot v = k.next(), k2 = v.next();
+                if (!(ok = full(v) && full(k2))) break;
                 for (int t = 0; t < tiles; ++t) {
-                    if (!(ok = warp_wait(&sh->pfull[t], uses[t] & 1, pp, sh))) break;
-                    ++uses[t];
-                    if (t == 0 && more && !(ok = full(kt + 2))) break;
+                    if (!(ok = warp_wait(&sh->pfull[t], uses[t]++ & 1, pp, sh))) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        pv(t, (kt + 1) % Sh::kStages, j == 0);
-                        if (t == tiles - 1) umma_commit(&sh->kempty[(kt + 1) % Sh::kStages]);
-                        if (more) {
-                            qk(t, (kt + 2) % Sh::kStages);
-                            umma_commit(&sh->sfull[t]);
-                            if (t == tiles - 1) {
-                                umma_commit(&sh->kempty[(kt + 2) % Sh::kStages]);
-                                if (j + 2 == n) umma_commit(&sh->qempty);
-                            }
-                        } else {
-                            umma_commit(&sh->ofull[t]);
+                        pv(t, v.i, j == 0);
+                        qk(t, k2.i);
+                        umma_commit(&sh->sfull[t]);
+                        if (t == tiles - 1) {
+                            umma_commit(&sh->kempty[v.i]);
+                            umma_commit(&sh->kempty[k2.i]);
                         }
+                        if (j + 2 == n) umma_commit(&sh->qempty[t]);
                     }
                     __syncwarp();
                 }
+                k = k2;
             }
-            ++items;
-            if (at.u + n < at.k.units) break;
-            pf_next_item(p, at);
+            if (!ok) break;
+            // its last unit's PV, and the next item's first QK
+            const Slot v = k.next();
+            if (!(ok = full(v))) break;
+            k = v.next();
+            for (int t = 0; t < max(tiles, next_tiles); ++t) {
+                if (t < tiles) {
+                    if (!(ok = warp_wait(&sh->pfull[t], uses[t]++ & 1, pp, sh))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        pv(t, v.i, n == 1);
+                        if (t == tiles - 1) umma_commit(&sh->kempty[v.i]);
+                        umma_commit(&sh->ofull[t]);
+                    }
+                    __syncwarp();
+                }
+                if (t < next_tiles) {
+                    if (t == 0 && !(ok = full(k))) break;
+                    if (!(ok = warp_wait(&sh->qfull[t], quses[t]++ & 1, pp, sh))) break;
+                    issue_qk(t, k, t == next_tiles - 1, next_n == 1);
+                }
+            }
+            at = nx;
+            n = next_n;
+            tiles = next_tiles;
         }
         // the tensor pipe is idle before shared and tensor memory are given back
         if (elect_one()) umma_commit(&sh->drain);
@@ -742,7 +826,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         const PfRun run = pf_run(p, sh, at);
         const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
         const uint32_t lanes = (uint32_t)(wt * 32) << 16;
-        const uint32_t s_tmem = tbase + lanes + 128 * t, o_tmem = tbase + lanes + 256 + 128 * t;
+        const uint32_t s_tmem = lanes + 128 * t, o_tmem = lanes + 256 + 128 * t;
         int su = 0, ou = 0, n;
         bool ok = true, tail = false;
         while (ok && (n = pf_units(run, at)) > 0) {
@@ -794,13 +878,20 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         pf_ld32(o_tmem + d, o);
                         pf_ld_wait(o);
                         if (live && whole) {
+                            uint32_t v[16];
 #pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                uint32_t v[4];
+                            for (int i = 0; i < 16; ++i)
+                                v[i] = l == 0.f ? 0u : pack2<BF16>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+                            // a lane's row is 2 D bytes from its neighbour's: whole 32-byte sectors
 #pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    v[k] = l == 0.f ? 0u : pack2<BF16>(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
-                                *reinterpret_cast<uint4 *>(out + d + i) = make_uint4(v[0], v[1], v[2], v[3]);
+                            for (int i = 0; i < 16; i += 8) {
+                                if (pp.out32) {
+                                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + d + 2 * i),
+                                                 PF_I8(v, i) : "memory");
+                                } else {
+                                    *reinterpret_cast<uint4 *>(out + d + 2 * i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                                    *reinterpret_cast<uint4 *>(out + d + 2 * i + 8) = make_uint4(v[i + 4], v[i + 5], v[i + 6], v[i + 7]);
+                                }
                             }
                         } else if (live) {
 #pragma unroll
@@ -836,7 +927,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     __syncthreads();
     if (warp == kPfMma) {
         tc_fence_after();
-        tmem_dealloc(tbase, 512);
+        tmem_dealloc(sh->tmem_base, 512);
     }
 }
 
@@ -893,9 +984,9 @@ size_t prefill_part_bytes(int head_dim)
     return kAttnMaxSms * (sizeof(PfOpen) + 2 * 4 * pf_part_floats(head_dim));
 }
 
-// Tensor map of keys or values: [page][head][row][d], boxes of 64 columns x box_rows rows
-// with the 128-byte swizzle.
-static bool pf_map(CUtensorMap *m, const void *base, const KvView &c, int D, bool bf16, int box_rows)
+// A tensor map of 16-bit elements in boxes of 64 columns, with the 128-byte swizzle.
+static bool pf_map(CUtensorMap *m, const void *base, bool bf16, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
+                   const cuuint32_t *box)
 {
     using Encode = decltype(&cuTensorMapEncodeTiled);
     static std::atomic<Encode> known{nullptr};
@@ -907,10 +998,8 @@ static bool pf_map(CUtensorMap *m, const void *base, const KvView &c, int D, boo
         encode = (Encode)f;
         known.store(encode, std::memory_order_relaxed);
     }
-    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)c.page_size, (cuuint64_t)c.kv_heads, (cuuint64_t)c.num_pages};
-    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)c.page_size * D * 2, (cuuint64_t)c.page_stride * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
-    return encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(base), dims,
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    return encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void *>(base), dims,
                   strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -918,9 +1007,20 @@ static bool pf_map(CUtensorMap *m, const void *base, const KvView &c, int D, boo
 template <int D, bool BF16, int MODE>
 static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st)
 {
-    CUtensorMap kmap, vmap;
-    if (!pf_map(&kmap, p.a.c.k, p.a.c, D, BF16, p.box_rows) || !pf_map(&vmap, p.a.c.v, p.a.c, D, BF16, p.box_rows))
-        return cudaErrorInvalidValue;
+    const KvView &c = p.a.c;
+    CUtensorMap kmap, vmap, qmap;
+    const cuuint64_t dims[4] = {D, (cuuint64_t)c.page_size, (cuuint64_t)c.kv_heads, (cuuint64_t)c.num_pages};
+    const cuuint64_t strides[3] = {D * 2, (cuuint64_t)c.page_size * D * 2, (cuuint64_t)c.page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)p.box_rows, 1, 1};
+    if (!pf_map(&kmap, c.k, BF16, 4, dims, strides, box) || !pf_map(&vmap, c.v, BF16, 4, dims, strides, box)) return cudaErrorInvalidValue;
+    if (p.q_boxes) {
+        const cuuint64_t qdims[3] = {D, (cuuint64_t)p.a.q_heads, (cuuint64_t)p.a.b.tokens};
+        const cuuint64_t qstrides[2] = {D * 2, (cuuint64_t)p.a.q_stride * 2};
+        const cuuint32_t qbox[3] = {64, (cuuint32_t)p.a.group, (cuuint32_t)(kPfTile / p.a.group)};
+        if (!pf_map(&qmap, p.a.q, BF16, 3, qdims, qstrides, qbox)) return cudaErrorInvalidValue;
+    } else {
+        qmap = kmap;  // not used
+    }
     using Sh = PfShape<D>;
     auto k = prefill_kernel<D, BF16, MODE>;
     static std::atomic<bool> known{false};  // (the same build on every device)
@@ -935,7 +1035,7 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
     e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnPrefill, st);
-    e = launch_k(k, dim3(ctas), dim3(kPfThreads), Sh::kSmem, st, p, kmap, vmap);
+    e = launch_k(k, dim3(ctas), dim3(kPfThreads), Sh::kSmem, st, p, kmap, vmap, qmap);
     profile_end(kKAttnPrefill, st);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnJoin, st);
@@ -962,6 +1062,8 @@ int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st
     p.part = reinterpret_cast<float *>(a.part + kAttnMaxSms * sizeof(PfOpen));
     p.timeout_ns = wait_bound_ns();
     p.debug = debug_flags();
+    p.q_boxes = kPfTile % a.group == 0 && a.q_stride < (int64_t)1 << 38;
+    p.out32 = (uintptr_t)a.out % 32 == 0 && a.out_stride % 16 == 0;
     p.box_rows = std::min(a.c.page_size & -a.c.page_size, kPfKeys);
     const int mode = a.cap > 0.f ? kPfCap : a.slopes ? kPfBias : kPfPlain;
     int nsm = 0;
