@@ -76,13 +76,16 @@ static int check_rows(const char *what, const void *p, int64_t stride, int heads
 
 static KvView view(const mc_kv_cache *c)
 {
-    return {(uint16_t *)c->k, (uint16_t *)c->v, c->page_stride, c->num_pages, c->page_size, c->kv_heads};
+    return {(uint16_t *)c->k, (uint16_t *)c->v, c->page_stride, c->num_pages, c->page_size, c->kv_heads,
+            FastDiv(c->page_size)};
 }
 
 static BatchView view(const mc_kv_batch *b)
 {
     return {b->lens, b->table, b->cu_q, b->seqs, b->tokens, b->table_width};
 }
+
+constexpr int kFewRows = 32;
 
 static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
                      const mc_attn_opts *o, void *out, int64_t out_stride, float *lse, void *workspace, size_t ws_bytes,
@@ -112,6 +115,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.q_stride = q_stride;
     p.q_heads = q_heads;
     p.group = q_heads / cache->kv_heads;
+    p.by_group = FastDiv(p.group);
     p.cap = o->softcap * kLog2e;
     p.scale = o->softcap > 0.f ? o->scale / o->softcap * (2.f * kLog2e) : o->scale * kLog2e;
     p.window = o->window >= kMaxLen ? 0 : o->window;  // no length passes kMaxLen
@@ -122,7 +126,12 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.lse = lse;
     p.status = (int32_t *)workspace;
     p.part = (uint8_t *)workspace + 256;
-    return (decode ? launch_decode : launch_prefill)(p, cache->head_dim, cache->dtype == MC_BF16, (cudaStream_t)stream);
+    // Few rows per sequence are bound by the reading of the cache, which the decode kernel does
+    // (kFewRows); lengths and counts are the device's, so the mean decides.
+    const int64_t rows = (int64_t)((batch->tokens + batch->seqs - 1) / batch->seqs) * p.group;
+    const bool bf16 = cache->dtype == MC_BF16;
+    if (decode || rows <= kFewRows) return launch_decode(p, cache->head_dim, bf16, (int)std::min<int64_t>(rows, 1 << 20), (cudaStream_t)stream);
+    return launch_prefill(p, cache->head_dim, bf16, (cudaStream_t)stream);
 }
 
 }  // namespace mc
@@ -135,7 +144,7 @@ size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads)
 {
     clear_error();
     if (check_cache(cache, q_heads)) return 0;
-    return 256 + std::max(decode_part_bytes(cache->head_dim, q_heads / cache->kv_heads), prefill_part_bytes(cache->head_dim));
+    return 256 + std::max(decode_part_bytes(cache->head_dim), prefill_part_bytes(cache->head_dim));
 }
 
 int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,

@@ -9,10 +9,36 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaxLen = 1 << 30;  // keys of a sequence, so that positions and windows stay in 32 bits
 
+// Division of 0 .. 2^31 - 1 by a number fixed for the call: the high product is the quotient
+// or one less.
+struct FastDiv {
+    uint32_t d, m;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t by) : d(by), m(by == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / by)) {}
+#ifdef __CUDACC__
+    __device__ __forceinline__ int div(int n, int &rest) const
+    {
+        uint32_t q = __umulhi((uint32_t)n, m), r = (uint32_t)n - q * d;
+        if (r >= d) {
+            ++q;
+            r -= d;
+        }
+        rest = (int)r;
+        return (int)q;
+    }
+    __device__ __forceinline__ int div(int n) const
+    {
+        int r;
+        return div(n, r);
+    }
+#endif
+};
+
 struct KvView {
     uint16_t *k, *v;
     int64_t page_stride;
     int num_pages, page_size, kv_heads;
+    FastDiv page;  // by page_size
 };
 
 struct BatchView {
@@ -26,6 +52,7 @@ struct AttnParams {
     const uint16_t *q;
     int64_t q_stride;
     int q_heads, group;  // group = q_heads / kv_heads
+    FastDiv by_group;
     float scale;         // q . k in units of log 2; with a cap: in the units of capped()
     float cap;           // the cap in units of log 2; 0: none
     int window;          // 0: none
@@ -62,6 +89,18 @@ __device__ __forceinline__ int seq_len(const BatchView &bv, const KvView &c, int
         return (int)cap;
     }
     return len < 0 ? 0 : len;
+}
+
+// a / b and a * c / d (rounded down) for b, c, d > 0, in 32 bits where they fit: a 64-bit
+// division is a few hundred cycles at the start of every CTA.
+__device__ __forceinline__ int64_t div64(int64_t a, int64_t b)
+{
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+__device__ __forceinline__ int64_t muldiv64(int64_t a, int c, int d)  // c <= d < 2^15
+{
+    const int64_t q = div64(a, d);
+    return q * c + (uint32_t)((uint32_t)(a - q * d) * (uint32_t)c) / (uint32_t)d;
 }
 
 // New tokens of sequence b: their first row and count (0 where cu_q is not sound).
@@ -179,8 +218,8 @@ int launch_append(const AppendParams &p, int head_dim, bool bf16, cudaStream_t s
 constexpr int kAttnMaxSms = 160;  // SMs that the workspace has room for (the GB300's 152)
 // SMs of the current device, asked for once per device.
 cudaError_t sm_count(int *out);
-size_t decode_part_bytes(int head_dim, int group);
-int launch_decode(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
+size_t decode_part_bytes(int head_dim);
+int launch_decode(const AttnParams &p, int head_dim, bool bf16, int rows, cudaStream_t st);
 size_t prefill_part_bytes(int head_dim);
 int launch_prefill(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
 

@@ -22,6 +22,7 @@ constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 constexpr int kDecKeys = 16;                   // keys of a unit that one warp takes
 constexpr int kDecUnit = kDecKeys * kDecWarps;
 constexpr int kDecCtasPerSm = 2;
+constexpr int kDecMaxTiles = 4;                // n-tiles of the largest slice
 constexpr float kLazy = 8.f;  // the maximum moves only when a score passes it by 2^8: the
                               // weights stay below 2^8, far inside fp16 and bf16
 
@@ -62,47 +63,85 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 
-// Keys [start, len) of a sequence, as units of kDecUnit keys from `base` on (base: start
-// rounded down to 16, so that a warp's 16 keys lie in one page).
+// A sequence's new tokens and the keys [start, len) that any of them sees, as units of
+// kDecUnit keys from `base` on (start rounded down to 16, so that a warp's 16 keys lie in
+// one page).  Its rows are (token, head of the group), token-major, in slices.
 struct Keys {
+    int first, n;  // token rows
     int start, len, base, units;
 };
 
-__device__ __forceinline__ Keys keys_of(const AttnParams &p, int len)
+__device__ __forceinline__ Keys keys_of(const AttnParams &p, int b, int32_t *status)
 {
     Keys k;
-    k.len = len;
-    k.start = p.window && len > p.window ? len - p.window : 0;
+    k.n = seq_rows(p.b, b, k.first, status);
+    k.len = seq_len(p.b, p.c, b, status);
+    const int p0 = k.len - k.n;
+    k.start = p.window ? max(0, p0 - p.window + 1) : 0;
     k.base = k.start & ~15;
-    k.units = (len - k.base + kDecUnit - 1) / kDecUnit;
+    k.units = k.n > 0 ? (k.len - k.base + kDecUnit - 1) / kDecUnit : 0;
     return k;
 }
 
-// A place in the run of units: sequence, head slice, unit of its keys.
+// Slices of 8 NT rows of a key head, and a sequence's units of all.
+template <int NT>
+__device__ __forceinline__ int slices_of(const AttnParams &p, const Keys &k)
+{
+    return (k.n * p.group + 8 * NT - 1) / (8 * NT);
+}
+template <int NT>
+__device__ __forceinline__ int64_t units_of(const AttnParams &p, const Keys &k)
+{
+    return k.units ? (int64_t)k.units * (slices_of<NT>(p, k) * p.c.kv_heads) : 0;
+}
+
+// A place in the run of units: sequence, key head, slice of its rows, unit of its keys.
 struct Place {
-    int b, hv, u;
+    int b, h, sl, slices, u;  // slices: of a key head
     Keys k;
 };
 
-__device__ __forceinline__ void step(const AttnParams &p, int slices, Place &at)
+template <int NT>
+__device__ __forceinline__ void step(const AttnParams &p, Place &at)
 {
     if (++at.u < at.k.units) return;
     at.u = 0;
-    if (++at.hv < slices) return;
-    at.hv = 0;
+    if (++at.sl < at.slices) return;
+    at.sl = 0;
+    if (++at.h < p.c.kv_heads) return;
+    at.h = 0;
     while (++at.b < p.b.seqs) {
-        at.k = keys_of(p, seq_len(p.b, p.c, at.b, nullptr));
-        if (at.k.units) return;
+        at.k = keys_of(p, at.b, nullptr);
+        if (at.k.units) {
+            at.slices = slices_of<NT>(p, at.k);
+            return;
+        }
     }
 }
 
-// Header of a CTA's open item, for the join: the pieces of (sequence b, head slice hv) are
-// this CTA's tail partial and the head partials of the next pieces - 1 CTAs; 0: none.
+// Header of a CTA's open item, for the join: the pieces of (sequence b, head h, slice sl) are this
+// CTA's tail partial and the head partials of the next pieces - 1 CTAs; 0: none.
 struct OpenItem {
-    int32_t pieces, b, hv, pad;
+    int32_t pieces, b, h, sl;
+};
+
+// What a row of a slice sees: keys [lo, hi); its bias is slope * (key - pos).
+struct Row {
+    int lo, hi, pos;
+    float slope;
 };
 
 __host__ __device__ constexpr size_t dec_part_floats(int D, int nt) { return (size_t)8 * nt * (D + 2); }
+
+// Four elements of a finished row, and its lse with the first; a row without keys is zero.
+template <bool BF16>
+__device__ __forceinline__ void store_row(const AttnParams &p, int token, int head, int D, int d, float4 acc, float top, float sum)
+{
+    const float inv = 1.f / sum;
+    *reinterpret_cast<uint2 *>(p.out + token * p.out_stride + head * D + d) =
+        sum == 0.f ? make_uint2(0, 0) : make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
+    if (p.lse && d == 0) p.lse[(int64_t)token * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
 
 template <int D, int NT>
 struct DecShape {
@@ -110,86 +149,69 @@ struct DecShape {
     static constexpr int kSlot = 2 * kDecKeys * kRow;        // a warp's keys and values of a unit
     static constexpr int kStages = D == 128 ? 3 : 6;
     static constexpr int kRing = kSlot * kStages * kDecWarps;
-    static constexpr int kJoin = kDecWarps * 8 * (D + 4) * 4;
-    static constexpr int kSmem = kRing + kJoin + kDecWarps * 8 * NT * 8;
+    static constexpr int kPitch = D + 4;                     // floats of a row in the join: O, m, l
+    static constexpr int kJoin = kDecWarps * 8 * kPitch * 4; // a piece's rows and queries lie over it
+    static constexpr bool kQShared = NT > 2;                 // the queries' fragments: shared memory or registers
+    static constexpr int kRows0 = kQShared ? NT * (D / 16) * 256 : 0;
+    static constexpr int kSmem = kRing + kJoin;
+    static_assert(kRows0 + 8 * NT * (int)sizeof(Row) <= kJoin, "rows of a slice");
 };
 
-// NT: n-tiles of 8 query heads that a slice holds (1: up to 8 heads of a group, 2: 16).
-// The products are formed transposed, S^T = K Q^T and O^T += V^T P^T: the 16 keys of a
-// warp fill the rows of the m16n8k16 instruction and the heads its 8 columns, half the
-// instructions and accumulators of heads as rows.
+// NT: n-tiles of 8 rows of a slice.  The products are formed transposed, S^T = K Q^T and
+// O^T += V^T P^T: the 16 keys of a warp fill the rows of the m16n8k16 instruction and the
+// slice's rows its 8 columns, half the instructions and accumulators of the other way.
 template <int D, bool BF16, int NT>
 __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(const AttnParams p, OpenItem *open, float *part)
 {
     using Sh = DecShape<D, NT>;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
-    const int slices_per = (p.group + 8 * NT - 1) / (8 * NT), slices = p.c.kv_heads * slices_per;
     float *jo = reinterpret_cast<float *>(smem + Sh::kRing);
-    float2 *jml = reinterpret_cast<float2 *>(smem + Sh::kRing + Sh::kJoin);  // [warp][8 NT]
+    uint2 *qs = reinterpret_cast<uint2 *>(smem + Sh::kRing);  // [n-tile][k-step][lane]
+    Row *rows = reinterpret_cast<Row *>(smem + Sh::kRing + Sh::kRows0);
     const uint32_t ring = smem_u32(smem) + warp * Sh::kSlot * Sh::kStages;
     pdl_trigger();
     pdl_wait();
 
-    // idle sequences
-    for (int b = blockIdx.x; b < p.b.seqs; b += gridDim.x)
-        if (seq_len(p.b, p.c, b, p.status) == 0) {
-            for (int i = tid; i < p.q_heads * D / 8; i += kDecThreads)
-                *reinterpret_cast<uint4 *>(p.out + b * p.out_stride + 8 * i) = make_uint4(0, 0, 0, 0);
-            if (p.lse)
-                for (int i = tid; i < p.q_heads; i += kDecThreads) p.lse[(int64_t)b * p.q_heads + i] = -INFINITY;
-        }
-
-    // all units, and the place of this CTA's first: 128 lengths a round
-    int64_t total = 0;
-    for (int b0 = 0; b0 < p.b.seqs; b0 += 128) {
-        int n = 0;
+    // all units, and the place of this CTA's first: a sequence per lane
+    int64_t total = 0, own = 0;
+    for (int b0 = 0; b0 < p.b.seqs; b0 += 32) {
+        own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, p.status)) : 0;
+        int64_t n = own;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int b = b0 + 4 * lane + i;
-            if (b < p.b.seqs) n += keys_of(p, seq_len(p.b, p.c, b, nullptr)).units;
-        }
-        total += __reduce_add_sync(0xffffffffu, n);
+        for (int d = 16; d >= 1; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+        total += n;
     }
-    total *= slices;
-    const int64_t ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
-    if ((int64_t)blockIdx.x >= ctas) {
-        if (tid == 0) open[blockIdx.x].pieces = 0;
-        return;
-    }
-    const int64_t u0 = total * blockIdx.x / ctas, u1 = total * (blockIdx.x + 1) / ctas;
+    const int ctas = total < (int64_t)gridDim.x ? (int)total : gridDim.x;
+    const bool any = (int)blockIdx.x < ctas;
+    const int64_t u0 = any ? muldiv64(total, blockIdx.x, ctas) : 0, u1 = any ? muldiv64(total, blockIdx.x + 1, ctas) : 0;
     Place at;  // compute side
-    {
-        int64_t before = 0;
-        at.b = -1;
-        for (int b0 = 0; at.b < 0 && b0 < p.b.seqs; b0 += 32) {
-            const int b = b0 + lane;
-            const int n = b < p.b.seqs ? keys_of(p, seq_len(p.b, p.c, b, nullptr)).units : 0;
-            int64_t sum = n;
+    at.b = -1;
+    int64_t skipped = 0;
+    for (int b0 = 0; any && at.b < 0 && b0 < p.b.seqs; b0 += 32) {
+        if (p.b.seqs > 32) own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, nullptr)) : 0;
+        int64_t sum = own;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int64_t o = __shfl_up_sync(0xffffffffu, sum, d);
-                if (lane >= d) sum += o;
-            }
-            const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * slices > u0);
-            if (hit) {
-                const int l = __ffs(hit) - 1;
-                at.b = b0 + l;
-                before += __shfl_sync(0xffffffffu, sum - n, l);
-            } else {
-                before += __shfl_sync(0xffffffffu, sum, 31);
-            }
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t o = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += o;
         }
-        if (at.b < 0) {  // lengths that changed between the two readings
-            if (tid == 0) open[blockIdx.x].pieces = 0;
-            return;
+        sum += skipped;
+        const unsigned hit = __ballot_sync(0xffffffffu, sum > u0);
+        if (!hit) {
+            skipped = __shfl_sync(0xffffffffu, sum, 31);
+            continue;
         }
-        at.k = keys_of(p, seq_len(p.b, p.c, at.b, nullptr));
-        const int64_t r = u0 - before * slices;
-        at.hv = (int)(r / at.k.units);
-        at.u = (int)(r % at.k.units);
+        const int l = __ffs(hit) - 1;
+        at.b = b0 + l;
+        at.k = keys_of(p, at.b, nullptr);
+        at.slices = slices_of<NT>(p, at.k);
+        const int64_t r = u0 - __shfl_sync(0xffffffffu, sum - own, l), item = div64(r, at.k.units);
+        at.u = (int)(r - item * at.k.units);
+        at.h = (int)div64(item, at.slices);
+        at.sl = (int)(item - (int64_t)at.h * at.slices);
     }
-    int left = (int)(u1 - u0);
+    int left = at.b < 0 ? 0 : (int)(u1 - u0);
 
     // ---- loads: this warp's 16 keys and values of a unit into ring slot i % kStages
     constexpr int kChunks = D / 8, kPer = 32 / kChunks;  // 16-byte chunks of a row; rows per warp copy
@@ -198,14 +220,15 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
     int ld_left = left, page = -1;
     auto fetch_page = [&]() {
         const int j = ld.k.base + ld.u * kDecUnit + warp * kDecKeys;
-        page = ld_left > 0 && j < ld.k.len ? seq_page(p.b, p.c, ld.b, j / p.c.page_size, p.status) : -1;
+        page = ld_left > 0 && j < ld.k.len ? seq_page(p.b, p.c, ld.b, p.c.page.div(j), p.status) : -1;
     };
     auto issue = [&](int slot) {
         if (ld_left > 0) {
             const int j = ld.k.base + ld.u * kDecUnit + warp * kDecKeys;
-            const int kvh = ld.hv / slices_per;
+            int row;
+            p.c.page.div(j, row);
             const int64_t off = (page < 0 ? 0 : page * p.c.page_stride) +
-                                ((int64_t)kvh * p.c.page_size + j % p.c.page_size + lr) * D + lc * 8;
+                                ((int64_t)ld.h * p.c.page_size + row + lr) * D + lc * 8;
             const uint32_t dst = ring + slot * Sh::kSlot;
 #pragma unroll
             for (int i = 0; i < kDecKeys / kPer; ++i) {
@@ -216,7 +239,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                 copy16(d + kDecKeys * Sh::kRow, p.c.v + (real ? off + i * kPer * D : 0), real);
             }
             --ld_left;
-            step(p, slices, ld);
+            step<NT>(p, ld);
             fetch_page();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -231,24 +254,47 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         // ---- one piece: units [at.u, at.u + n) of one item
         const int n = min(left, at.k.units - at.u);
         const bool from_first = at.u == 0, to_last = at.u + n == at.k.units;
-        const int kvh = at.hv / slices_per, hs = (at.hv % slices_per) * 8 * NT;  // first head of the slice in its group
-        const int h0 = kvh * p.group + hs;
-        const int heads = min(8 * NT, p.group - hs);
-        uint32_t qf[NT][D / 16][2];
-        float slope[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const bool has = 8 * nt + g < heads;
-            const uint16_t *q = p.q + at.b * p.q_stride + (h0 + 8 * nt + g) * D + 2 * t4;
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                qf[nt][ks][0] = has ? *reinterpret_cast<const uint32_t *>(q + 16 * ks) : 0u;
-                qf[nt][ks][1] = has ? *reinterpret_cast<const uint32_t *>(q + 16 * ks + 8) : 0u;
+        const int h0 = at.h * p.group, r0 = at.sl * 8 * NT, nrows = min(8 * NT, at.k.n * p.group - r0);  // rows of the slice
+        const Keys keys = at.k;
+        const int p0 = keys.len - keys.n, prefix = p.prefix ? __ldg(p.prefix + at.b) : 0;
+        auto row_of = [&](int r) {  // r < nrows
+            Row w;
+            int hg;
+            w.pos = p0 + p.by_group.div(r0 + r, hg);
+            w.lo = p.window ? max(0, w.pos - p.window + 1) : 0;
+            w.hi = w.pos < 0 ? 0 : min(keys.len, max(w.pos + 1, prefix));
+            w.slope = p.slopes ? __ldg(p.slopes + h0 + hg) * kLog2e : 0.f;
+            return w;
+        };
+        auto query = [&](int r) {
+            int hg;
+            const int tok = p.by_group.div(r0 + min(r, nrows - 1), hg);
+            return p.q + (keys.first + tok) * p.q_stride + (h0 + hg) * D;
+        };
+        auto pair = [&](const uint16_t *q, int d, int r) { return r < nrows ? *reinterpret_cast<const uint32_t *>(q + d) : 0u; };
+        uint32_t qf[Sh::kQShared ? 1 : NT][D / 16][2];
+        if (Sh::kQShared) {
+            for (int i = tid; i < NT * (D / 16) * 32; i += kDecThreads) {
+                const int l = i & 31, ks = (i >> 5) % (D / 16), nt = (i >> 5) / (D / 16);
+                const int r = 8 * nt + (l >> 2), d = 16 * ks + 2 * (l & 3);
+                const uint16_t *q = query(r);
+                qs[i] = make_uint2(pair(q, d, r), pair(q, d + 8, r));
             }
+        } else {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-                slope[nt][c] = p.slopes && 8 * nt + 2 * t4 + c < heads ? __ldg(p.slopes + h0 + 8 * nt + 2 * t4 + c) * kLog2e : 0.f;
+            for (int nt = 0; nt < (Sh::kQShared ? 1 : NT); ++nt) {
+                const uint16_t *q = query(8 * nt + g) + 2 * t4;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    qf[nt][ks][0] = pair(q, 16 * ks, 8 * nt + g);
+                    qf[nt][ks][1] = pair(q, 16 * ks + 8, 8 * nt + g);
+                }
+            }
         }
+        if (tid < 8 * NT) rows[tid] = row_of(min(tid, nrows - 1));
+        // keys that every row of the slice sees: below the first row's end, from the last's start on
+        const int all_hi = row_of(0).hi, all_lo = row_of(nrows - 1).lo;
+        __syncthreads();
         float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -259,7 +305,6 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             m[nt][0] = m[nt][1] = -INFINITY;
             l[nt][0] = l[nt][1] = 0.f;
         }
-        const Keys keys = at.k;
         for (int u = at.u; u < at.u + n; ++u) {
             asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kStages - 2) : "memory");
             __syncwarp();  // every lane is done with the slot of the round before, which is filled next
@@ -267,33 +312,52 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             const uint32_t kk = ring + slot * Sh::kSlot, vv = kk + kDecKeys * Sh::kRow;
             const int j0 = keys.base + u * kDecUnit + warp * kDecKeys;
             if (j0 < keys.len) {
-                // S^T: rows are keys g, g + 8; columns heads 2 t4, 2 t4 + 1; two chains
-                float s[NT][2][4];
+                // S^T: rows are keys g, g + 8; columns the slice's rows 2 t4, 2 t4 + 1; few
+                // n-tiles take two accumulators each, so that the chain is half as long
+                constexpr int kChains = NT > 2 ? 1 : 2;
+                float s[NT][kChains][4];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) s[nt][0][c] = s[nt][1][c] = 0.f;
+                    for (int c = 0; c < 4; ++c) s[nt][0][c] = s[nt][kChains - 1][c] = 0.f;
                 const int kr = lane & 15;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
                     uint32_t a[4];
                     ldsm4(a, kk + kr * Sh::kRow + (((2 * ks + (lane >> 4)) ^ (kr & 7)) << 4));
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma16<BF16>(s[nt][ks & 1], a, qf[nt][ks][0], qf[nt][ks][1]);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (Sh::kQShared) {
+                            const uint2 q = qs[(nt * (D / 16) + ks) * 32 + lane];
+                            mma16<BF16>(s[nt][0], a, q.x, q.y);
+                        } else {
+                            mma16<BF16>(s[nt][ks % kChains], a, qf[nt][ks][0], qf[nt][ks][1]);
+                        }
+                    }
                 }
+                const bool masked = j0 < all_lo || j0 + kDecKeys > all_hi;
                 bool over = false;
                 float x[NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const int j = j0 + g + (c >> 1) * 8;
-                        float v = (s[nt][0][c] + s[nt][1][c]) * p.scale;
+                        float v = (kChains == 2 ? s[nt][0][c] + s[nt][kChains - 1][c] : s[nt][0][c]) * p.scale;
                         if (p.cap > 0.f) v = capped(v, p.cap);
-                        if (p.slopes) v = fmaf(slope[nt][c & 1], (float)(j - keys.len + 1), v);
-                        x[nt][c] = j >= keys.start && j < keys.len ? v : -INFINITY;
-                        over |= x[nt][c] > m[nt][c & 1] + kLazy;
+                        x[nt][c] = v;
                     }
+                    if (masked || p.slopes) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const Row w = rows[8 * nt + 2 * t4 + (c & 1)];
+                            const int j = j0 + g + (c >> 1) * 8;
+                            x[nt][c] = fmaf(w.slope, (float)(j - w.pos), x[nt][c]);
+                            if (j < w.lo || j >= w.hi) x[nt][c] = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) over |= x[nt][c] > m[nt][c & 1] + kLazy;
+                }
                 if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -339,50 +403,52 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             if (++slot == Sh::kStages) slot = 0;
         }
 
-        // ---- the four warps' parts
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                for (int d = 4; d <= 16; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
-                if (g == 0) jml[warp * 8 * NT + 8 * nt + 2 * t4 + c] = make_float2(m[nt][c], l[nt][c]);
-            }
+        // ---- the four warps' parts, an n-tile at a time
         const bool whole = from_first && to_last;
         float *mine = part + (2 * blockIdx.x + (from_first ? 1 : 0)) * dec_part_floats(D, NT);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            if (nt) __syncthreads();
+            if (8 * nt >= nrows) break;
+            __syncthreads();  // the queries, the n-tile before
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int d = 4; d <= 16; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
+                if (g == 0)
+                    *reinterpret_cast<float2 *>(jo + (warp * 8 + 2 * t4 + c) * Sh::kPitch + D) = make_float2(m[nt][c], l[nt][c]);
+            }
 #pragma unroll
             for (int mt = 0; mt < D / 16; ++mt)
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    jo[(warp * 8 + 2 * t4 + (c & 1)) * (D + 4) + 16 * mt + g + (c >> 1) * 8] = o[nt][mt][c];
+                    jo[(warp * 8 + 2 * t4 + (c & 1)) * Sh::kPitch + 16 * mt + g + (c >> 1) * 8] = o[nt][mt][c];
             __syncthreads();
             for (int i = tid; i < 8 * (D / 4); i += kDecThreads) {
-                const int h = i / (D / 4), d = (i % (D / 4)) * 4, hh = 8 * nt + h;
-                if (hh >= heads) continue;
+                const int h = i / (D / 4), d = (i % (D / 4)) * 4, r = 8 * nt + h;
+                if (r >= nrows) continue;
+                float2 ml[kDecWarps];
                 float top = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < kDecWarps; ++w) top = fmaxf(top, jml[w * 8 * NT + hh].x);
+                for (int w = 0; w < kDecWarps; ++w) {
+                    ml[w] = *reinterpret_cast<const float2 *>(jo + (w * 8 + h) * Sh::kPitch + D);
+                    top = fmaxf(top, ml[w].x);
+                }
                 float sum = 0.f;
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < kDecWarps; ++w) {
-                    const float2 ml = jml[w * 8 * NT + hh];
-                    const float k = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
-                    const float4 v = *reinterpret_cast<const float4 *>(jo + (w * 8 + h) * (D + 4) + d);
-                    sum = fmaf(k, ml.y, sum);
+                    const float k = ml[w].x == -INFINITY ? 0.f : ex2(ml[w].x - top);
+                    const float4 v = *reinterpret_cast<const float4 *>(jo + (w * 8 + h) * Sh::kPitch + d);
+                    sum = fmaf(k, ml[w].y, sum);
                     acc = make_float4(fmaf(k, v.x, acc.x), fmaf(k, v.y, acc.y), fmaf(k, v.z, acc.z), fmaf(k, v.w, acc.w));
                 }
                 if (whole) {
-                    const float inv = 1.f / sum;
-                    *reinterpret_cast<uint2 *>(p.out + at.b * p.out_stride + (h0 + hh) * D + d) =
-                        make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-                    if (p.lse && d == 0) p.lse[(int64_t)at.b * p.q_heads + h0 + hh] = (top + log2f(sum)) * kLn2;
+                    int hg;
+                    const int tok = p.by_group.div(r0 + r, hg);
+                    store_row<BF16>(p, keys.first + tok, h0 + hg, D, d, acc, top, sum);
                 } else {
-                    *reinterpret_cast<float4 *>(mine + hh * D + d) = acc;
-                    if (d == 0) *reinterpret_cast<float2 *>(mine + 8 * NT * D + 2 * hh) = make_float2(top, sum);
+                    *reinterpret_cast<float4 *>(mine + r * D + d) = acc;
+                    if (d == 0) *reinterpret_cast<float2 *>(mine + 8 * NT * D + 2 * r) = make_float2(top, sum);
                 }
             }
         }
@@ -391,18 +457,30 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             open_tail = true;
             if (tid == 0) {
                 const int64_t end = u1 - left + at.k.units;  // one past the item's last unit
-                const int64_t last = (end * ctas + total - 1) / total;  // one past the CTA that holds it
-                open[blockIdx.x] = {(int32_t)(last - blockIdx.x), at.b, at.hv, 0};
+                const int64_t last = div64(end * ctas + total - 1, total);  // one past the CTA that holds it
+                open[blockIdx.x] = {(int32_t)(last - blockIdx.x), at.b, at.h, at.sl};
             }
         }
         left -= n;
         at.u += n - 1;
-        step(p, slices, at);
+        step<NT>(p, at);
     }
     if (!open_tail && tid == 0) open[blockIdx.x].pieces = 0;
+
+    // sequences without keys
+    for (int b = blockIdx.x; b < p.b.seqs; b += gridDim.x) {
+        const Keys k = keys_of(p, b, nullptr);
+        if (k.len > 0) continue;
+        for (int t = k.first; t < k.first + k.n; ++t) {
+            for (int i = tid; i < p.q_heads * D / 8; i += kDecThreads)
+                *reinterpret_cast<uint4 *>(p.out + t * p.out_stride + 8 * i) = make_uint4(0, 0, 0, 0);
+            if (p.lse)
+                for (int i = tid; i < p.q_heads; i += kDecThreads) p.lse[(int64_t)t * p.q_heads + i] = -INFINITY;
+        }
+    }
 }
 
-// One CTA per (CTA of the pass before, head of a slice): adds the pieces of that CTA's open
+// One CTA per (CTA of the pass before, row of a slice): adds the pieces of that CTA's open
 // item in their order.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const OpenItem *open, const float *part, int nt)
@@ -414,14 +492,15 @@ __global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const Ope
     pdl_wait();
     const OpenItem it = open[blockIdx.x];
     if (it.pieces == 0) return;
-    const int per = (p.group + 8 * nt - 1) / (8 * nt);
-    const int hs = (it.hv % per) * 8 * nt, hh = blockIdx.y;
-    if (hs + hh >= p.group) return;
-    const int head = (it.hv / per) * p.group + hs + hh, tid = threadIdx.x;
+    const int r = blockIdx.y, tid = threadIdx.x;
+    int first, hg;
+    const int rows = seq_rows(p.b, it.b, first, nullptr) * p.group, f = it.sl * 8 * nt + r;
+    if (f >= rows) return;
+    const int tok = p.by_group.div(f, hg);
     const size_t stride = dec_part_floats(D, nt);
     auto piece = [&](int i) { return part + (2 * ((size_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * stride; };
     float top = -INFINITY;
-    for (int i = tid; i < it.pieces; i += 128) top = fmaxf(top, piece(i)[8 * nt * D + 2 * hh]);
+    for (int i = tid; i < it.pieces; i += 128) top = fmaxf(top, piece(i)[8 * nt * D + 2 * r]);
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     if ((tid & 31) == 0) red[tid >> 5] = top;
@@ -430,10 +509,11 @@ __global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const Ope
     float sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const int col = tid % kCols, grp = tid / kCols;
+#pragma unroll 4
     for (int i = grp; i < it.pieces; i += kGroups) {
         const float *q = piece(i);
-        const float2 ml = *reinterpret_cast<const float2 *>(q + 8 * nt * D + 2 * hh);
-        const float4 v = *reinterpret_cast<const float4 *>(q + hh * D + 4 * col);
+        const float2 ml = *reinterpret_cast<const float2 *>(q + 8 * nt * D + 2 * r);
+        const float4 v = *reinterpret_cast<const float4 *>(q + r * D + 4 * col);
         const float k = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
         sum = fmaf(k, ml.y, sum);
         acc = make_float4(fmaf(k, v.x, acc.x), fmaf(k, v.y, acc.y), fmaf(k, v.z, acc.z), fmaf(k, v.w, acc.w));
@@ -450,17 +530,14 @@ __global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const Ope
         sum += sums[i];
         acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
     }
-    const float inv = 1.f / sum;
-    *reinterpret_cast<uint2 *>(p.out + it.b * p.out_stride + head * D + 4 * col) =
-        make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-    if (p.lse && col == 0) p.lse[(int64_t)it.b * p.q_heads + head] = (top + log2f(sum)) * kLn2;
+    store_row<BF16>(p, first + tok, it.h * p.group + hg, D, 4 * col, acc, top, sum);
 }
 
 constexpr int kDecMaxCtas = kDecCtasPerSm * kAttnMaxSms;
 
-size_t decode_part_bytes(int head_dim, int group)
+size_t decode_part_bytes(int head_dim)
 {
-    return kDecMaxCtas * (sizeof(OpenItem) + 2 * 4 * dec_part_floats(head_dim, group > 8 ? 2 : 1));
+    return kDecMaxCtas * (sizeof(OpenItem) + 2 * 4 * dec_part_floats(head_dim, kDecMaxTiles));
 }
 
 template <int D, bool BF16, int NT>
@@ -477,25 +554,28 @@ static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t s
     profile_end(kKAttnDecode, st);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnJoin, st);
-    e = launch_k(join_kernel<D, BF16>, dim3(ctas, p.group < 8 * NT ? p.group : 8 * NT), dim3(128), 0, st, p,
-                 (const OpenItem *)open, (const float *)part, NT);
+    e = launch_k(join_kernel<D, BF16>, dim3(ctas, 8 * NT), dim3(128), 0, st, p, (const OpenItem *)open, (const float *)part, NT);
     profile_end(kKAttnJoin, st);
     return e;
 }
 
-int launch_decode(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st)
+template <int D, bool BF16>
+static cudaError_t launch_decode_n(const AttnParams &p, int rows, int ctas, cudaStream_t st)
+{
+    return rows <= 8 ? launch_decode_t<D, BF16, 1>(p, ctas, st) : rows <= 16 ? launch_decode_t<D, BF16, 2>(p, ctas, st)
+                                                                            : launch_decode_t<D, BF16, kDecMaxTiles>(p, ctas, st);
+}
+
+// rows: what most sequences have, (token, head of the group) each; the smallest slice that
+// holds them is taken, and sequences with more take several.
+int launch_decode(const AttnParams &p, int head_dim, bool bf16, int rows, cudaStream_t st)
 {
     int nsm = 0;
     cudaError_t e = sm_count(&nsm);
     if (e == cudaSuccess) {
         const int ctas = kDecCtasPerSm * (nsm < kAttnMaxSms ? nsm : kAttnMaxSms);
-        const bool two = p.group > 8;
-        auto f = head_dim == 64
-                     ? (bf16 ? (two ? launch_decode_t<64, true, 2> : launch_decode_t<64, true, 1>)
-                             : (two ? launch_decode_t<64, false, 2> : launch_decode_t<64, false, 1>))
-                     : (bf16 ? (two ? launch_decode_t<128, true, 2> : launch_decode_t<128, true, 1>)
-                             : (two ? launch_decode_t<128, false, 2> : launch_decode_t<128, false, 1>));
-        e = f(p, ctas, st);
+        e = head_dim == 64 ? (bf16 ? launch_decode_n<64, true>(p, rows, ctas, st) : launch_decode_n<64, false>(p, rows, ctas, st))
+                           : (bf16 ? launch_decode_n<128, true>(p, rows, ctas, st) : launch_decode_n<128, false>(p, rows, ctas, st));
     }
     if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "decode launch: %s", cudaGetErrorString(e));
     return MC_OK;

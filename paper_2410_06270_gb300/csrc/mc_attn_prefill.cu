@@ -135,8 +135,8 @@ __device__ __forceinline__ PfKeys pf_keys(const AttnParams &p, const PfSeq &s, i
 {
     PfKeys k;
     const int last = min((mt + 1) * kPfRows, s.n * p.group) - 1;
-    k.p_lo = s.len - s.n + mt * kPfRows / p.group;
-    const int p_hi = s.len - s.n + last / p.group;
+    k.p_lo = s.len - s.n + p.by_group.div(mt * kPfRows);
+    const int p_hi = s.len - s.n + p.by_group.div(last);
     k.end = p_hi < 0 ? 0 : min(s.len, max(p_hi + 1, s.prefix));
     k.base = p.window ? max(0, k.p_lo - p.window + 1) & ~(kPfKeys - 1) : 0;
     k.units = max(1, (k.end - k.base + kPfKeys - 1) / kPfKeys);
@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         const int64_t ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
         int fb = -1, fh = 0, fmt = 0, fu = 0, off = 0;
         if ((int64_t)blockIdx.x < ctas) {
-            int64_t r = total * (blockIdx.x + warp) / ctas;  // cost before the place
+            int64_t r = muldiv64(total, blockIdx.x + warp, (int)ctas);  // cost before the place
             if (r == total) fb = p.b.seqs;
             for (int b0 = 0; b0 < p.b.seqs && fb < 0; b0 += 32) {
                 if (p.b.seqs > 32) pf_sums(p, sums, b0, lane, nullptr);
@@ -548,8 +548,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 r -= __shfl_sync(0xffffffffu, upto - own, who);
                 const int per = __shfl_sync(0xffffffffu, sums[lane], who);
                 fb = b0 + who;
-                fh = (int)(r / per);
-                off = (int)(r % per);
+                fh = (int)div64(r, per);
+                off = (int)(r - (int64_t)fh * per);
                 const PfSeq s = pf_seq(p, fb, nullptr);
                 const int tiles = pf_tiles(p, s);
                 for (int t0 = 0; t0 < tiles; t0 += 32) {
@@ -606,14 +606,15 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             bool ok = !(pp.debug & kDebugNoProducer);
             auto pages = [&](int u) {
                 const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
-                return lane < boxes && j < at.k.end ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + j / p.c.page_size) : -1;
+                return lane < boxes && j < at.k.end ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j)) : -1;
             };
             while (ok && (n = pf_units(run, at)) > 0) {
                 int page = pages(at.u);
                 for (int u = at.u; ok && u < at.u + n; ++u) {
                     const int next = u + 1 < at.u + n ? pages(u + 1) : -1;  // used a unit later
                     const int j0 = at.k.base + u * kPfKeys, j = j0 + lane * pp.box_rows;
-                    const int row = j % p.c.page_size;
+                    int row;
+                    p.c.page.div(j, row);
                     if ((unsigned)page >= (unsigned)p.c.num_pages) {
                         if (lane < boxes && j < at.k.end) set_status(p.status, MC_ERR_RANGE);
                         page = p.c.num_pages;
@@ -679,14 +680,15 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 #pragma unroll
                             for (int h = 0; h < D / 64; ++h)
                                 pf_tma3(tile + h * Sh::kHalf, &qmap, 64 * h, at.h * p.group,
-                                        at.s.first + (rows0 + t * kPfTile) / p.group, &sh->qfull[t]);
+                                        at.s.first + p.by_group.div(rows0 + t * kPfTile), &sh->qfull[t]);
                         }
                         continue;
                     }
                     // one row per kChunks lanes, zeros past the last
                     int r = t * kPfTile + (warp - kPfQ0) * kPer + lr;
-                    int hg = (rows0 + r) % p.group;
-                    const uint16_t *src = p.q + (at.s.first + (rows0 + r) / p.group) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
+                    int hg;
+                    const int tok = p.by_group.div(rows0 + r, hg);
+                    const uint16_t *src = p.q + (at.s.first + tok) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
                     for (; r < (t + 1) * kPfTile; r += kQStep) {
                         const bool real = r < rows;
                         pf_copy16z((tile + col + (r & 127) * 128) ^ ((r & 7) << 4), real ? src : p.q, real);
@@ -834,12 +836,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             const bool from_first = at.u == 0, to_last = at.u + n == at.k.units;
             if (rows > 0) {
                 const bool live = row < rows;
-                const int f = rows0 + min(row, rows - 1), tok = f / p.group, head = at.h * p.group + f % p.group;
+                int hg;
+                const int tok = p.by_group.div(rows0 + min(row, rows - 1), hg), head = at.h * p.group + hg;
                 const int off = at.s.len - at.s.n, pos = off + tok;
                 const int lo = p.window ? max(0, pos - p.window + 1) : 0;
                 const int hi = pos < 0 ? 0 : min(at.s.len, max(pos + 1, at.s.prefix));
                 // what the tile's first and last rows see decides whether a unit needs the mask
-                const int p_first = off + rows0 / p.group, p_last = off + (rows0 + rows - 1) / p.group;
+                const int p_first = off + p.by_group.div(rows0), p_last = off + p.by_group.div(rows0 + rows - 1);
                 const int all_hi = p_first < 0 ? 0 : min(at.s.len, max(p_first + 1, at.s.prefix));
                 const int all_lo = p.window ? p_last - p.window + 1 : 0;
                 const float slope = MODE != kPfPlain && p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
@@ -913,8 +916,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 if (tid == 0) {
                     // the pieces lie in the CTAs whose runs start before the item's end
                     const int64_t total = sh->total, ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
-                    const int64_t end = total * (blockIdx.x + 1) / ctas - sh->off + kPfItemCost + at.k.units;
-                    pp.open[blockIdx.x] = {(int32_t)((end * ctas + total - 1) / total - blockIdx.x), at.b, at.h, at.mt};
+                    const int64_t end = muldiv64(total, blockIdx.x + 1, (int)ctas) - sh->off + kPfItemCost + at.k.units;
+                    pp.open[blockIdx.x] = {(int32_t)(div64(end * ctas + total - 1, total) - blockIdx.x), at.b, at.h, at.mt};
                 }
             }
             if (at.u + n < at.k.units) break;
@@ -951,7 +954,8 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
     const int f = it.mt * kPfRows + row;
     __syncthreads();
     if (f >= s.n * p.group) return;
-    const int tok = f / p.group, head = it.h * p.group + f % p.group;
+    int hg;
+    const int tok = p.by_group.div(f, hg), head = it.h * p.group + hg;
     float top = -INFINITY;
     for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, ml[i][r].x);
     float4 acc[kQuads];

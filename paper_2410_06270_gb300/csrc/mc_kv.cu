@@ -67,8 +67,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
     int64_t at = -1;  // the row's element offset in the cache
     float4 cs = make_float4(1.f, 1.f, 1.f, 1.f), sn = make_float4(0.f, 0.f, 0.f, 0.f);
     if (pos >= 0) {
-        row = pos % p.c.page_size;
-        const int page = seq_page(p.b, p.c, s, pos / p.c.page_size, p.status);
+        const int i = p.c.page.div(pos, row);
+        const int page = seq_page(p.b, p.c, s, i, p.status);
         if (page >= 0) at = page * p.c.page_stride + (int64_t)row * D;
         if (p.rot) {
             if (pos >= p.rope_rows) {

@@ -190,7 +190,36 @@ def test_prefill_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap
     ref.assert_attention(got, lse, want, dtype, 512, 5.0, rows=slice(0, n))
 
 
-@pytest.mark.parametrize("new,length,kv,heads,dim", [(1, 4000, 1, 4, 128), (40, 6000, 2, 4, 64), (700, 700, 1, 1, 128),
+@pytest.mark.parametrize("heads,kv,dim,dtype,page,softcap,window,bias,prefix", [
+    # few rows a sequence: slices of 8, 16 and 32 rows, some sequences with more than one
+    (4, 4, 128, "bf16", 16, 0.0, 0, False, False),
+    (3, 1, 64, "fp16", 48, 0.0, 20, True, False),
+    (8, 2, 128, "bf16", 32, 30.0, 0, False, True),
+    (12, 2, 64, "bf16", 16, 50.0, 3, True, True),
+    (6, 1, 128, "fp16", 128, 0.0, 100, False, False),
+    (4, 1, 64, "fp16", 16, 0.0, 0, True, True),
+])
+def test_prefill_of_few_tokens_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap, window, bias, prefix):
+    lens, new = [0, 5, 17, 64, 130, 300, 511, 3, 1025], [2, 5, 3, 1, 8, 4, 6, 7, 5]
+    B = ref.Batch(lens, new, kv, page, dim, dtype, 16, pad_tokens=2)
+    q = 1.5 * B.randn(B.tokens, heads, dim)
+    sl = _slopes(heads) if bias else None
+    pre = [1, 3, 17, 60, 125, 0, 600, 2, 1022] if prefix else None
+    want = ref.attention(B, q, dim ** -0.5, softcap, window, sl, pre)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, heads)
+    out = torch.full((B.tokens, heads, dim), 3.0, dtype=ref.DT[dtype], device="cuda")
+    got, lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=softcap, window=window,
+                               slopes=None if sl is None else sl.cuda(),
+                               prefix=None if pre is None else torch.tensor(pre, dtype=torch.int32).cuda(),
+                               out=out, with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    n = B.cu[-1]
+    assert (out[n:] == 3).all()
+    ref.assert_attention(got, lse, want, dtype, 1025, 5.0, rows=slice(0, n))
+
+
+@pytest.mark.parametrize("new,length,kv,heads,dim", [(1, 4000, 1, 4, 128), (5, 9000, 1, 5, 128), (40, 6000, 2, 4, 64), (700, 700, 1, 1, 128),
                                                      (515, 2100, 2, 6, 128), (1, 1, 1, 1, 64)])
 def test_prefill_splits_and_joins(mc, new, length, kv, heads, dim):
     B = ref.Batch([length], [new], kv, 64, dim, "bf16", 8)
