@@ -1,6 +1,8 @@
 // mc_attn.h -- what the paged-attention kernels share: their parameter blocks and the
 // device reading of a batch (lengths, positions, pages), checked against its bounds.
 #pragma once
+#include <atomic>
+
 #include "mc_kernels.h"
 
 namespace mc {
@@ -218,6 +220,21 @@ int launch_append(const AppendParams &p, int head_dim, bool bf16, cudaStream_t s
 constexpr int kAttnMaxSms = 160;  // SMs that the workspace has room for (the GB300's 152)
 // SMs of the current device, asked for once per device.
 cudaError_t sm_count(int *out);
+// A kernel's shared-memory size, set once on each device.
+struct SmemAttr {
+    std::atomic<uint64_t> done{0};
+    cudaError_t set(const void *kernel, int bytes)
+    {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+        if (bit & done.load(std::memory_order_relaxed)) return cudaSuccess;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+        return e;
+    }
+};
 size_t decode_part_bytes(int head_dim);
 int launch_decode(const AttnParams &p, int head_dim, bool bf16, int rows, cudaStream_t st);
 size_t prefill_part_bytes(int head_dim);

@@ -547,12 +547,18 @@ static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t s
     OpenItem *open = reinterpret_cast<OpenItem *>(p.part);
     float *part = reinterpret_cast<float *>(p.part + kDecMaxCtas * sizeof(OpenItem));
     auto k = decode_kernel<D, BF16, NT>;
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
+    static SmemAttr attr;
+    cudaError_t e = attr.set((const void *)k, Sh::kSmem);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnDecode, st);
     e = launch_k(k, dim3(ctas), dim3(kDecThreads), Sh::kSmem, st, p, open, part);
     profile_end(kKAttnDecode, st);
-    if (e != cudaSuccess) return e;
+    // A sequence that the table holds in one unit is never split.  (Adding the pieces of the
+    // others within the launch, by the CTA that finishes an item's last one, saves its launch but
+    // not time: an atomic and two dependent reads by one CTA against a CTA per row: 777 keys 7.8 us
+    // with the second launch, 9.9 without, 16 ragged sequences 26.9 and 29.5, 8000 keys of one key
+    // head 12.5 and 32.1.)
+    if (e != cudaSuccess || (int64_t)p.b.table_width * p.c.page_size <= kDecUnit) return e;
     profile_begin(kKAttnJoin, st);
     e = launch_k(join_kernel<D, BF16>, dim3(ctas, 8 * NT), dim3(128), 0, st, p, (const OpenItem *)open, (const float *)part, NT);
     profile_end(kKAttnJoin, st);

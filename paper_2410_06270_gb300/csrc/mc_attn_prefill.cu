@@ -1036,7 +1036,8 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
         if (at.numRegs < kPfRegs) return cudaErrorInvalidConfiguration;
         known.store(true, std::memory_order_relaxed);
     }
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
+    static SmemAttr attr;
+    e = attr.set((const void *)k, Sh::kSmem);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnPrefill, st);
     e = launch_k(k, dim3(ctas), dim3(kPfThreads), Sh::kSmem, st, p, kmap, vmap, qmap);
