@@ -57,10 +57,14 @@ __device__ __forceinline__ uint32_t transposed8x8(uint32_t a)
     return r;
 }
 
-// 16 bytes to shared memory, or 16 zeros where !real (the address is then not read).
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real)
+// 16 bytes to shared memory, or 16 zeros where !real (the address is then not read).  The
+// cache is read once a step and leaves L2 first: lengths, tables and what other kernels keep
+// there stay.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real, uint64_t policy)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0),
+                 "l"(policy)
+                 : "memory");
 }
 
 // A sequence's new tokens and the keys [start, len) that any of them sees, as units of
@@ -161,7 +165,7 @@ struct DecShape {
 // O^T += V^T P^T: the 16 keys of a warp fill the rows of the m16n8k16 instruction and the
 // slice's rows its 8 columns, half the instructions and accumulators of the other way.
 template <int D, bool BF16, int NT>
-__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(const AttnParams p, OpenItem *open, float *part)
+__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(const AttnParams p, FastDiv by_grid, OpenItem *open, float *part)
 {
     using Sh = DecShape<D, NT>;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -175,47 +179,81 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 
     // all units, and the place of this CTA's first: a sequence per lane
     int64_t total = 0, own = 0;
-    for (int b0 = 0; b0 < p.b.seqs; b0 += 32) {
-        own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, p.status)) : 0;
-        int64_t n = own;
-#pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
-        total += n;
-    }
-    const int ctas = total < (int64_t)gridDim.x ? (int)total : gridDim.x;
-    const bool any = (int)blockIdx.x < ctas;
-    const int64_t u0 = any ? muldiv64(total, blockIdx.x, ctas) : 0, u1 = any ? muldiv64(total, blockIdx.x + 1, ctas) : 0;
+    int ctas;
+    int64_t u0 = 0, u1 = 0;
     Place at;  // compute side
     at.b = -1;
-    int64_t skipped = 0;
-    for (int b0 = 0; any && at.b < 0 && b0 < p.b.seqs; b0 += 32) {
-        if (p.b.seqs > 32) own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, nullptr)) : 0;
-        int64_t sum = own;
+    if (p.b.seqs <= 32) {
+        own = lane < p.b.seqs ? units_of<NT>(p, keys_of(p, lane, p.status)) : 0;
+    }
+    if (p.b.seqs <= 32 && __all_sync(0xffffffffu, own < 1 << 26)) {
+        // 32 bits hold it all, and the divisions are by fixed numbers but one
+        int sum = (int)own;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int64_t o = __shfl_up_sync(0xffffffffu, sum, d);
+            const int o = __shfl_up_sync(0xffffffffu, sum, d);
             if (lane >= d) sum += o;
         }
-        sum += skipped;
-        const unsigned hit = __ballot_sync(0xffffffffu, sum > u0);
-        if (!hit) {
-            skipped = __shfl_sync(0xffffffffu, sum, 31);
-            continue;
+        const int all = __shfl_sync(0xffffffffu, sum, 31);
+        total = all;
+        ctas = min(all, (int)gridDim.x);
+        if ((int)blockIdx.x < ctas) {
+            int rest = 0, q = 1;
+            if (ctas == (int)gridDim.x) q = by_grid.div(all, rest);
+            const int c = blockIdx.x, first = q * c + by_grid.div(rest * c), end = q * (c + 1) + by_grid.div(rest * (c + 1));
+            u0 = first;
+            u1 = end;
+            at.b = __ffs(__ballot_sync(0xffffffffu, sum > first)) - 1;
+            at.k = keys_of(p, at.b, nullptr);
+            at.slices = slices_of<NT>(p, at.k);
+            const int r = first - __shfl_sync(0xffffffffu, sum - (int)own, at.b), item = (int)((unsigned)r / (unsigned)at.k.units);
+            at.u = r - item * at.k.units;
+            at.h = at.slices == 1 ? item : (int)((unsigned)item / (unsigned)at.slices);
+            at.sl = item - at.h * at.slices;
         }
-        const int l = __ffs(hit) - 1;
-        at.b = b0 + l;
-        at.k = keys_of(p, at.b, nullptr);
-        at.slices = slices_of<NT>(p, at.k);
-        const int64_t r = u0 - __shfl_sync(0xffffffffu, sum - own, l), item = div64(r, at.k.units);
-        at.u = (int)(r - item * at.k.units);
-        at.h = (int)div64(item, at.slices);
-        at.sl = (int)(item - (int64_t)at.h * at.slices);
+    } else {
+        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) {
+            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, p.status)) : 0;
+            int64_t n = own;
+#pragma unroll
+            for (int d = 16; d >= 1; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+            total += n;
+        }
+        ctas = total < (int64_t)gridDim.x ? (int)total : gridDim.x;
+        const bool any = (int)blockIdx.x < ctas;
+        u0 = any ? muldiv64(total, blockIdx.x, ctas) : 0;
+        u1 = any ? muldiv64(total, blockIdx.x + 1, ctas) : 0;
+        int64_t skipped = 0;
+        for (int b0 = 0; any && at.b < 0 && b0 < p.b.seqs; b0 += 32) {
+            if (p.b.seqs > 32) own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, nullptr)) : 0;
+            int64_t sum = own;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int64_t o = __shfl_up_sync(0xffffffffu, sum, d);
+                if (lane >= d) sum += o;
+            }
+            sum += skipped;
+            const unsigned hit = __ballot_sync(0xffffffffu, sum > u0);
+            if (!hit) {
+                skipped = __shfl_sync(0xffffffffu, sum, 31);
+                continue;
+            }
+            const int l = __ffs(hit) - 1;
+            at.b = b0 + l;
+            at.k = keys_of(p, at.b, nullptr);
+            at.slices = slices_of<NT>(p, at.k);
+            const int64_t r = u0 - __shfl_sync(0xffffffffu, sum - own, l), item = div64(r, at.k.units);
+            at.u = (int)(r - item * at.k.units);
+            at.h = (int)div64(item, at.slices);
+            at.sl = (int)(item - (int64_t)at.h * at.slices);
+        }
     }
     int left = at.b < 0 ? 0 : (int)(u1 - u0);
 
     // ---- loads: this warp's 16 keys and values of a unit into ring slot i % kStages
     constexpr int kChunks = D / 8, kPer = 32 / kChunks;  // 16-byte chunks of a row; rows per warp copy
     const int lc = lane % kChunks, lr = lane / kChunks;
+    const uint64_t policy = policy_evict_first();
     Place ld = at;
     int ld_left = left, page = -1;
     auto fetch_page = [&]() {
@@ -235,8 +273,8 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                 const int r = lr + i * kPer;
                 const bool real = page >= 0 && j + r >= ld.k.start && j + r < ld.k.len;
                 const uint32_t d = dst + r * Sh::kRow + ((lc ^ (r & 7)) << 4);
-                copy16(d, p.c.k + (real ? off + i * kPer * D : 0), real);
-                copy16(d + kDecKeys * Sh::kRow, p.c.v + (real ? off + i * kPer * D : 0), real);
+                copy16(d, p.c.k + (real ? off + i * kPer * D : 0), real, policy);
+                copy16(d + kDecKeys * Sh::kRow, p.c.v + (real ? off + i * kPer * D : 0), real, policy);
             }
             --ld_left;
             step<NT>(p, ld);
@@ -551,7 +589,7 @@ static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t s
     cudaError_t e = attr.set((const void *)k, Sh::kSmem);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnDecode, st);
-    e = launch_k(k, dim3(ctas), dim3(kDecThreads), Sh::kSmem, st, p, open, part);
+    e = launch_k(k, dim3(ctas), dim3(kDecThreads), Sh::kSmem, st, p, FastDiv(ctas), open, part);
     profile_end(kKAttnDecode, st);
     // A sequence that the table holds in one unit is never split.  (Adding the pieces of the
     // others within the launch, by the CTA that finishes an item's last one, saves its launch but
