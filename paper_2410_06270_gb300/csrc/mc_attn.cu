@@ -85,7 +85,7 @@ static BatchView view(const mc_kv_batch *b)
     return {b->lens, b->table, b->cu_q, b->seqs, b->tokens, b->table_width};
 }
 
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 16, kFewRowsCap = 32;
 
 static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
                      const mc_attn_opts *o, void *out, int64_t out_stride, float *lse, void *workspace, size_t ws_bytes,
@@ -126,11 +126,14 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.lse = lse;
     p.status = (int32_t *)workspace;
     p.part = (uint8_t *)workspace + 256;
-    // Few rows per sequence are bound by the reading of the cache, which the decode kernel does
-    // (kFewRows); lengths and counts are the device's, so the mean decides.
+    // Few rows (tokens x heads of a group) a sequence take the decode kernel, whose time grows
+    // with them, more the tensor-memory one, whose rows come 128 at a time; the counts are the
+    // device's, so the mean decides.  8 sequences of 4000 keys, decode / tensor-memory kernel:
+    // 20 rows 38 / 34 us, 32 rows 44 / 34; with a cap, whose cost follows the rows, 38 / 49 and
+    // 45 / 49; one sequence of 2000 keys, 16 rows, 12 / 17.
     const int64_t rows = (int64_t)((batch->tokens + batch->seqs - 1) / batch->seqs) * p.group;
     const bool bf16 = cache->dtype == MC_BF16;
-    if (decode || rows <= kFewRows) return launch_decode(p, cache->head_dim, bf16, (int)std::min<int64_t>(rows, 1 << 20), (cudaStream_t)stream);
+    if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, (int)rows, (cudaStream_t)stream);
     return launch_prefill(p, cache->head_dim, bf16, (cudaStream_t)stream);
 }
 

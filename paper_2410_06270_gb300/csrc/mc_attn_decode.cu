@@ -5,7 +5,7 @@
 // for a group of query heads, 4 head_dim bytes for 4 head_dim group flops: bound by HBM, so
 // the design is about keeping loads in flight on every SM whatever the lengths are.
 //
-// Work is cut into units of 64 keys of one (sequence, key head); the units of the whole
+// Work is cut into units of 64 (heads of 64: 128) keys of one (sequence, key head); the units of the whole
 // batch, in order, are dealt to the CTAs as equal contiguous runs, which each CTA finds from
 // the lengths by itself (no host knowledge of them, so a captured graph serves any).  A run
 // that ends inside an item leaves a partial result (m, l, o in fp32); join_kernel adds the
@@ -19,8 +19,11 @@
 namespace mc {
 
 constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
-constexpr int kDecKeys = 16;                   // keys of a unit that one warp takes
-constexpr int kDecUnit = kDecKeys * kDecWarps;
+// Keys of a unit that one warp takes, in tiles of 16: heads of 64 take two tiles in one step,
+// whose chains of products and exponentials overlap (a step of 16 keys takes about as long
+// whatever the head, and 16 keys of 64 are half the bytes).
+constexpr int dec_tiles(int D) { return D == 64 ? 2 : 1; }
+constexpr int dec_unit(int D) { return 16 * dec_tiles(D) * kDecWarps; }
 constexpr int kDecCtasPerSm = 2;
 constexpr int kDecMaxTiles = 4;                // n-tiles of the largest slice
 constexpr float kLazy = 8.f;  // the maximum moves only when a score passes it by 2^8: the
@@ -68,13 +71,13 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real,
 }
 
 // A sequence's new tokens and the keys [start, len) that any of them sees, as units of
-// kDecUnit keys from `base` on (start rounded down to 16, so that a warp's 16 keys lie in
-// one page).  Its rows are (token, head of the group), token-major, in slices.
+// keys from `base` on (start rounded down to 16, so that 16 keys lie in one page).  Its rows are (token, head of the group), token-major, in slices.
 struct Keys {
     int first, n;  // token rows
     int start, len, base, units;
 };
 
+template <int D>
 __device__ __forceinline__ Keys keys_of(const AttnParams &p, int b, int32_t *status)
 {
     Keys k;
@@ -83,7 +86,7 @@ __device__ __forceinline__ Keys keys_of(const AttnParams &p, int b, int32_t *sta
     const int p0 = k.len - k.n;
     k.start = p.window ? max(0, p0 - p.window + 1) : 0;
     k.base = k.start & ~15;
-    k.units = k.n > 0 ? (k.len - k.base + kDecUnit - 1) / kDecUnit : 0;
+    k.units = k.n > 0 ? (k.len - k.base + dec_unit(D) - 1) / dec_unit(D) : 0;
     return k;
 }
 
@@ -105,7 +108,7 @@ struct Place {
     Keys k;
 };
 
-template <int NT>
+template <int D, int NT>
 __device__ __forceinline__ void step(const AttnParams &p, Place &at)
 {
     if (++at.u < at.k.units) return;
@@ -115,7 +118,7 @@ __device__ __forceinline__ void step(const AttnParams &p, Place &at)
     if (++at.h < p.c.kv_heads) return;
     at.h = 0;
     while (++at.b < p.b.seqs) {
-        at.k = keys_of(p, at.b, nullptr);
+        at.k = keys_of<D>(p, at.b, nullptr);
         if (at.k.units) {
             at.slices = slices_of<NT>(p, at.k);
             return;
@@ -150,8 +153,9 @@ __device__ __forceinline__ void store_row(const AttnParams &p, int token, int he
 template <int D, int NT>
 struct DecShape {
     static constexpr int kRow = D * 2;                       // bytes of a key
-    static constexpr int kSlot = 2 * kDecKeys * kRow;        // a warp's keys and values of a unit
-    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kTiles = dec_tiles(D), kKeys = 16 * kTiles;
+    static constexpr int kSlot = 2 * kKeys * kRow;           // a warp's keys and values of a unit
+    static constexpr int kStages = 3;
     static constexpr int kRing = kSlot * kStages * kDecWarps;
     static constexpr int kPitch = D + 4;                     // floats of a row in the join: O, m, l
     static constexpr int kJoin = kDecWarps * 8 * kPitch * 4; // a piece's rows and queries lie over it
@@ -161,7 +165,7 @@ struct DecShape {
     static_assert(kRows0 + 8 * NT * (int)sizeof(Row) <= kJoin, "rows of a slice");
 };
 
-// NT: n-tiles of 8 rows of a slice.  The products are formed transposed, S^T = K Q^T and
+// NT: n-tiles of 8 rows of a slice, 1 to 4.  The products are formed transposed, S^T = K Q^T and
 // O^T += V^T P^T: the 16 keys of a warp fill the rows of the m16n8k16 instruction and the
 // slice's rows its 8 columns, half the instructions and accumulators of the other way.
 template <int D, bool BF16, int NT>
@@ -177,18 +181,30 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
     pdl_trigger();
     pdl_wait();
 
-    // all units, and the place of this CTA's first: a sequence per lane
+    // all units, and the place of this CTA's first
     int64_t total = 0, own = 0;
     int ctas;
     int64_t u0 = 0, u1 = 0;
     Place at;  // compute side
     at.b = -1;
-    if (p.b.seqs <= 32) {
-        own = lane < p.b.seqs ? units_of<NT>(p, keys_of(p, lane, p.status)) : 0;
+    const bool few = p.b.seqs <= 128;
+    const int each = p.b.seqs <= 32 ? 1 : 4;  // sequences a lane
+    int mine[4] = {0, 0, 0, 0}, sum4 = 0;
+    bool small = true;
+    if (few) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i >= each) break;
+            const int b = each * lane + i;
+            const int64_t n = b < p.b.seqs ? units_of<NT>(p, keys_of<D>(p, b, p.status)) : 0;
+            small &= n < 1 << 24;
+            mine[i] = (int)n;
+            sum4 += mine[i];
+        }
     }
-    if (p.b.seqs <= 32 && __all_sync(0xffffffffu, own < 1 << 26)) {
+    if (few && __all_sync(0xffffffffu, small)) {
         // 32 bits hold it all, and the divisions are by fixed numbers but one
-        int sum = (int)own;
+        int sum = sum4;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int o = __shfl_up_sync(0xffffffffu, sum, d);
@@ -203,17 +219,28 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             const int c = blockIdx.x, first = q * c + by_grid.div(rest * c), end = q * (c + 1) + by_grid.div(rest * (c + 1));
             u0 = first;
             u1 = end;
-            at.b = __ffs(__ballot_sync(0xffffffffu, sum > first)) - 1;
-            at.k = keys_of(p, at.b, nullptr);
+            const int l = __ffs(__ballot_sync(0xffffffffu, sum > first)) - 1;
+            int r = first - __shfl_sync(0xffffffffu, sum - sum4, l);
+            at.b = each * l;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                if (i + 1 >= each) break;
+                const int n = __shfl_sync(0xffffffffu, mine[i], l);
+                if (at.b == each * l + i && r >= n) {
+                    r -= n;
+                    ++at.b;
+                }
+            }
+            at.k = keys_of<D>(p, at.b, nullptr);
             at.slices = slices_of<NT>(p, at.k);
-            const int r = first - __shfl_sync(0xffffffffu, sum - (int)own, at.b), item = (int)((unsigned)r / (unsigned)at.k.units);
+            const int item = (int)((unsigned)r / (unsigned)at.k.units);
             at.u = r - item * at.k.units;
             at.h = at.slices == 1 ? item : (int)((unsigned)item / (unsigned)at.slices);
             at.sl = item - at.h * at.slices;
         }
     } else {
         for (int b0 = 0; b0 < p.b.seqs; b0 += 32) {
-            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, p.status)) : 0;
+            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of<D>(p, b0 + lane, p.status)) : 0;
             int64_t n = own;
 #pragma unroll
             for (int d = 16; d >= 1; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
@@ -225,7 +252,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         u1 = any ? muldiv64(total, blockIdx.x + 1, ctas) : 0;
         int64_t skipped = 0;
         for (int b0 = 0; any && at.b < 0 && b0 < p.b.seqs; b0 += 32) {
-            if (p.b.seqs > 32) own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of(p, b0 + lane, nullptr)) : 0;
+            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of<D>(p, b0 + lane, nullptr)) : 0;
             int64_t sum = own;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -240,7 +267,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             }
             const int l = __ffs(hit) - 1;
             at.b = b0 + l;
-            at.k = keys_of(p, at.b, nullptr);
+            at.k = keys_of<D>(p, at.b, nullptr);
             at.slices = slices_of<NT>(p, at.k);
             const int64_t r = u0 - __shfl_sync(0xffffffffu, sum - own, l), item = div64(r, at.k.units);
             at.u = (int)(r - item * at.k.units);
@@ -255,29 +282,35 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
     const int lc = lane % kChunks, lr = lane / kChunks;
     const uint64_t policy = policy_evict_first();
     Place ld = at;
-    int ld_left = left, page = -1;
+    int ld_left = left, page[Sh::kTiles];
     auto fetch_page = [&]() {
-        const int j = ld.k.base + ld.u * kDecUnit + warp * kDecKeys;
-        page = ld_left > 0 && j < ld.k.len ? seq_page(p.b, p.c, ld.b, p.c.page.div(j), p.status) : -1;
+#pragma unroll
+        for (int kt = 0; kt < Sh::kTiles; ++kt) {
+            const int j = ld.k.base + ld.u * dec_unit(D) + warp * Sh::kKeys + 16 * kt;
+            page[kt] = ld_left > 0 && j < ld.k.len ? seq_page(p.b, p.c, ld.b, p.c.page.div(j), p.status) : -1;
+        }
     };
     auto issue = [&](int slot) {
         if (ld_left > 0) {
-            const int j = ld.k.base + ld.u * kDecUnit + warp * kDecKeys;
-            int row;
-            p.c.page.div(j, row);
-            const int64_t off = (page < 0 ? 0 : page * p.c.page_stride) +
-                                ((int64_t)ld.h * p.c.page_size + row + lr) * D + lc * 8;
-            const uint32_t dst = ring + slot * Sh::kSlot;
 #pragma unroll
-            for (int i = 0; i < kDecKeys / kPer; ++i) {
-                const int r = lr + i * kPer;
-                const bool real = page >= 0 && j + r >= ld.k.start && j + r < ld.k.len;
-                const uint32_t d = dst + r * Sh::kRow + ((lc ^ (r & 7)) << 4);
-                copy16(d, p.c.k + (real ? off + i * kPer * D : 0), real, policy);
-                copy16(d + kDecKeys * Sh::kRow, p.c.v + (real ? off + i * kPer * D : 0), real, policy);
+            for (int kt = 0; kt < Sh::kTiles; ++kt) {
+                const int j = ld.k.base + ld.u * dec_unit(D) + warp * Sh::kKeys + 16 * kt;
+                int row;
+                p.c.page.div(j, row);
+                const int64_t off = (page[kt] < 0 ? 0 : page[kt] * p.c.page_stride) +
+                                    ((int64_t)ld.h * p.c.page_size + row + lr) * D + lc * 8;
+                const uint32_t dst = ring + slot * Sh::kSlot + 16 * kt * Sh::kRow;
+#pragma unroll
+                for (int i = 0; i < 16 / kPer; ++i) {
+                    const int r = lr + i * kPer;
+                    const bool real = page[kt] >= 0 && j + r >= ld.k.start && j + r < ld.k.len;
+                    const uint32_t d = dst + r * Sh::kRow + ((lc ^ (r & 7)) << 4);
+                    copy16(d, p.c.k + (real ? off + i * kPer * D : 0), real, policy);
+                    copy16(d + Sh::kKeys * Sh::kRow, p.c.v + (real ? off + i * kPer * D : 0), real, policy);
+                }
             }
             --ld_left;
-            step<NT>(p, ld);
+            step<D, NT>(p, ld);
             fetch_page();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -347,64 +380,77 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kStages - 2) : "memory");
             __syncwarp();  // every lane is done with the slot of the round before, which is filled next
             issue(slot == 0 ? Sh::kStages - 1 : slot - 1);
-            const uint32_t kk = ring + slot * Sh::kSlot, vv = kk + kDecKeys * Sh::kRow;
-            const int j0 = keys.base + u * kDecUnit + warp * kDecKeys;
+            const uint32_t kk = ring + slot * Sh::kSlot, vv = kk + Sh::kKeys * Sh::kRow;
+            const int j0 = keys.base + u * dec_unit(D) + warp * Sh::kKeys;
             if (j0 < keys.len) {
                 // S^T: rows are keys g, g + 8; columns the slice's rows 2 t4, 2 t4 + 1; few
-                // n-tiles take two accumulators each, so that the chain is half as long
-                constexpr int kChains = NT > 2 ? 1 : 2;
-                float s[NT][kChains][4];
+                // tiles take two accumulators each, so that the chain is half as long
+                constexpr int kChains = NT * Sh::kTiles > 2 ? 1 : 2;
+                float s[Sh::kTiles][NT][kChains][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) s[nt][0][c] = s[nt][kChains - 1][c] = 0.f;
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) s[kt][nt][0][c] = s[kt][nt][kChains - 1][c] = 0.f;
                 const int kr = lane & 15;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    uint32_t a[4];
-                    ldsm4(a, kk + kr * Sh::kRow + (((2 * ks + (lane >> 4)) ^ (kr & 7)) << 4));
+                    uint32_t a[Sh::kTiles][4];
+#pragma unroll
+                    for (int kt = 0; kt < Sh::kTiles; ++kt)
+                        ldsm4(a[kt], kk + (16 * kt + kr) * Sh::kRow + (((2 * ks + (lane >> 4)) ^ (kr & 7)) << 4));
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        if (Sh::kQShared) {
-                            const uint2 q = qs[(nt * (D / 16) + ks) * 32 + lane];
-                            mma16<BF16>(s[nt][0], a, q.x, q.y);
-                        } else {
-                            mma16<BF16>(s[nt][ks % kChains], a, qf[nt][ks][0], qf[nt][ks][1]);
-                        }
+                        uint2 q;
+                        if (Sh::kQShared) q = qs[(nt * (D / 16) + ks) * 32 + lane];
+                        else q = make_uint2(qf[Sh::kQShared ? 0 : nt][ks][0], qf[Sh::kQShared ? 0 : nt][ks][1]);
+#pragma unroll
+                        for (int kt = 0; kt < Sh::kTiles; ++kt) mma16<BF16>(s[kt][nt][ks % kChains], a[kt], q.x, q.y);
                     }
                 }
-                const bool masked = j0 < all_lo || j0 + kDecKeys > all_hi;
+                const bool masked = j0 < all_lo || j0 + Sh::kKeys > all_hi;
                 bool over = false;
-                float x[NT][4];
+                float x[Sh::kTiles][NT][4];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float v = (kChains == 2 ? s[nt][0][c] + s[nt][kChains - 1][c] : s[nt][0][c]) * p.scale;
-                        if (p.cap > 0.f) v = capped(v, p.cap);
-                        x[nt][c] = v;
-                    }
-                    if (masked || p.slopes) {
+                    for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const Row w = rows[8 * nt + 2 * t4 + (c & 1)];
-                            const int j = j0 + g + (c >> 1) * 8;
-                            x[nt][c] = fmaf(w.slope, (float)(j - w.pos), x[nt][c]);
-                            if (j < w.lo || j >= w.hi) x[nt][c] = -INFINITY;
+                            float v = (kChains == 2 ? s[kt][nt][0][c] + s[kt][nt][kChains - 1][c] : s[kt][nt][0][c]) * p.scale;
+                            if (p.cap > 0.f) v = capped(v, p.cap);
+                            x[kt][nt][c] = v;
+                        }
+                    if (masked || p.slopes) {
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const Row w = rows[8 * nt + 2 * t4 + c];
+#pragma unroll
+                            for (int kt = 0; kt < Sh::kTiles; ++kt)
+#pragma unroll
+                                for (int e = c; e < 4; e += 2) {
+                                    const int j = j0 + 16 * kt + g + (e >> 1) * 8;
+                                    x[kt][nt][e] = fmaf(w.slope, (float)(j - w.pos), x[kt][nt][e]);
+                                    if (j < w.lo || j >= w.hi) x[kt][nt][e] = -INFINITY;
+                                }
                         }
                     }
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) over |= x[nt][c] > m[nt][c & 1] + kLazy;
+                    for (int kt = 0; kt < Sh::kTiles; ++kt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) over |= x[kt][nt][c] > m[nt][c & 1] + kLazy;
                 }
                 if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            float top = fmaxf(x[nt][c], x[nt][c + 2]);
+                            float top = m[nt][c];
+#pragma unroll
+                            for (int kt = 0; kt < Sh::kTiles; ++kt) top = fmaxf(top, fmaxf(x[kt][nt][c], x[kt][nt][c + 2]));
 #pragma unroll
                             for (int d = 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                            top = fmaxf(top, m[nt][c]);
                             const float keep = top == m[nt][c] ? 1.f : ex2(m[nt][c] - top);
                             m[nt][c] = top;
                             l[nt][c] *= keep;
@@ -415,28 +461,32 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                             }
                         }
                 }
-                uint32_t pf[NT][2];
+                uint32_t pf[Sh::kTiles][NT][2];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float pr[4];
+                for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float ref = m[nt][c & 1];
-                        pr[c] = ex2(x[nt][c] - (ref == -INFINITY ? 0.f : ref));
-                        l[nt][c & 1] += pr[c];
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float pr[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float ref = m[nt][c & 1];
+                            pr[c] = ex2(x[kt][nt][c] - (ref == -INFINITY ? 0.f : ref));
+                            l[nt][c & 1] += pr[c];
+                        }
+                        // rounded to the cache's type for the second product; l keeps fp32
+                        pf[kt][nt][0] = transposed8x8(pack2<BF16>(pr[0], pr[1]));
+                        pf[kt][nt][1] = transposed8x8(pack2<BF16>(pr[2], pr[3]));
                     }
-                    // rounded to the cache's type for the second product; l keeps fp32
-                    pf[nt][0] = transposed8x8(pack2<BF16>(pr[0], pr[1]));
-                    pf[nt][1] = transposed8x8(pack2<BF16>(pr[2], pr[3]));
-                }
                 const int vr = (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
-                for (int mt = 0; mt < D / 16; ++mt) {
-                    uint32_t a[4];
-                    ldsm4t(a, vv + vr * Sh::kRow + (((2 * mt + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
+                for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma16<BF16>(o[nt][mt], a, pf[nt][0], pf[nt][1]);
-                }
+                    for (int mt = 0; mt < D / 16; ++mt) {
+                        uint32_t a[4];
+                        ldsm4t(a, vv + (16 * kt + vr) * Sh::kRow + (((2 * mt + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16<BF16>(o[nt][mt], a, pf[kt][nt][0], pf[kt][nt][1]);
+                    }
             }
             if (++slot == Sh::kStages) slot = 0;
         }
@@ -501,13 +551,13 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         }
         left -= n;
         at.u += n - 1;
-        step<NT>(p, at);
+        step<D, NT>(p, at);
     }
     if (!open_tail && tid == 0) open[blockIdx.x].pieces = 0;
 
     // sequences without keys
     for (int b = blockIdx.x; b < p.b.seqs; b += gridDim.x) {
-        const Keys k = keys_of(p, b, nullptr);
+        const Keys k = keys_of<D>(p, b, nullptr);
         if (k.len > 0) continue;
         for (int t = k.first; t < k.first + k.n; ++t) {
             for (int i = tid; i < p.q_heads * D / 8; i += kDecThreads)
@@ -596,7 +646,7 @@ static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t s
     // not time: an atomic and two dependent reads by one CTA against a CTA per row: 777 keys 7.8 us
     // with the second launch, 9.9 without, 16 ragged sequences 26.9 and 29.5, 8000 keys of one key
     // head 12.5 and 32.1.)
-    if (e != cudaSuccess || (int64_t)p.b.table_width * p.c.page_size <= kDecUnit) return e;
+    if (e != cudaSuccess || (int64_t)p.b.table_width * p.c.page_size <= dec_unit(D)) return e;
     profile_begin(kKAttnJoin, st);
     e = launch_k(join_kernel<D, BF16>, dim3(ctas, 8 * NT), dim3(128), 0, st, p, (const OpenItem *)open, (const float *)part, NT);
     profile_end(kKAttnJoin, st);
@@ -606,8 +656,10 @@ static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t s
 template <int D, bool BF16>
 static cudaError_t launch_decode_n(const AttnParams &p, int rows, int ctas, cudaStream_t st)
 {
-    return rows <= 8 ? launch_decode_t<D, BF16, 1>(p, ctas, st) : rows <= 16 ? launch_decode_t<D, BF16, 2>(p, ctas, st)
-                                                                            : launch_decode_t<D, BF16, kDecMaxTiles>(p, ctas, st);
+    return rows <= 8    ? launch_decode_t<D, BF16, 1>(p, ctas, st)
+           : rows <= 16 ? launch_decode_t<D, BF16, 2>(p, ctas, st)
+           : rows <= 24 ? launch_decode_t<D, BF16, 3>(p, ctas, st)
+                        : launch_decode_t<D, BF16, kDecMaxTiles>(p, ctas, st);
 }
 
 // rows: what most sequences have, (token, head of the group) each; the smallest slice that
