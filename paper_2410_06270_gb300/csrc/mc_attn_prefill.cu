@@ -286,42 +286,6 @@ __device__ __forceinline__ void pf_ld16(uint32_t taddr, uint32_t *r)
         : "memory");
 }
 
-__device__ __forceinline__ uint64_t pair2(float lo, float hi)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-
-__device__ __forceinline__ void unpair2(uint64_t v, float &lo, float &hi)
-{
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-
-// Two fp32 operations for one issue slot (the pipe takes as long as for two: what is saved
-// is issue, which the softmax warps run short of; one by one a unit's softmax takes 1610
-// cycles instead of 1340).
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // Instruction descriptor: fp16 or bf16 operands, fp32 accumulator, M = 128; b_mn: the B
 // operand's N dimension is the contiguous one (values: [key][d]).
 __host__ __device__ constexpr uint32_t pf_idesc(bool bf16, int N, bool b_mn)
