@@ -402,6 +402,17 @@ def _bad(msg):
     raise MCError(ERR_INVALID_ARG, msg)
 
 
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 class KVCache:
     """A paged key-value cache over the caller's tensors k and v, both [pages, kv_heads,
     page_size, head_dim] in bf16 or fp16.  Pages may be strided (one layer of a larger
@@ -422,6 +433,7 @@ class KVCache:
         stride = k.stride(0) if pages > 1 else max(k.stride(0), heads * size * dim)
         self._c = _KvCacheC(k.data_ptr(), v.data_ptr(), stride, pages, size, heads, dim, codes[k.dtype])
         self._ref = ctypes.addressof(self._c)
+        self.index = k.get_device()
 
 
 class KVBatch:
@@ -445,26 +457,54 @@ class KVBatch:
         self.tokens = self.seqs if tokens is None else int(tokens)
         self._c = _KvBatchC(lens.data_ptr(), table.data_ptr(), _ptr(cu_q), self.seqs, self.tokens, table.shape[1])
         self._ref = ctypes.addressof(self._c)
+        self.index = lens.get_device()
 
 
-def _rows(name, t, cache, batch, heads=None):
-    """Token stride of t [tokens, heads, head_dim] (heads contiguous)."""
-    sh, st = t.shape, t.stride()
-    if len(sh) != 3 or sh[0] != batch.tokens or sh[2] != cache.head_dim or (heads is not None and sh[1] != heads):
-        _bad("%s must be [tokens, heads, head_dim], got %s" % (name, tuple(sh)))
-    if t.dtype != cache.dtype or t.device != cache.device or batch.device != cache.device:
-        _bad("%s, the batch and the cache must share a device, %s and the cache a dtype" % (name, name))
-    if st[2] != 1 or (sh[1] > 1 and st[1] != sh[2]):
-        _bad("%s: the heads of a token must be contiguous" % name)
-    return st[0] if sh[0] > 1 else max(st[0], sh[1] * sh[2])
+def _rows(name, t, cache, batch, heads=0):
+    """(heads, token stride) of t [tokens, heads, head_dim] (heads contiguous; 0: any number)."""
+    sh = t.shape
+    if len(sh) == 3:
+        n, h, d = sh
+        s0, s1, s2 = t.stride()
+        if (n == batch.tokens and d == cache.head_dim and (h == heads or not heads) and t.dtype is cache.dtype and
+                t.get_device() == cache.index == batch.index and s2 == 1 and (s1 == d or h == 1)):
+            return h, s0 if n > 1 else max(s0, h * d)
+    _bad("%s must be [tokens = %d, heads%s, head_dim = %d] of %s on the device of the cache and of the batch, the heads of "
+         "a token contiguous; got %s, strides %s, of %s on %s" % (name, batch.tokens, " = %d" % heads if heads else "",
+                                                                cache.head_dim, cache.dtype, tuple(sh), t.stride(), t.dtype,
+                                                                t.device))
 
 
-def _side(name, t, cache, dtype, shape):
-    """Pointer of a contiguous side input, or None."""
+_fast_module = None
+
+
+def _fast():
+    """The extension that marshals plain calls (None answers, for the rest: the code below)."""
+    global _fast_module
+    if _fast_module is None:
+        import importlib.machinery
+        import importlib.util
+        lib, torch = load(), _torch()
+        path = os.path.join(_HERE, "_build", "_mcbind.so")
+        if not os.path.exists(path):
+            raise ImportError("_mcbind.so not built: run `python paper_2410_06270_gb300/build.py`")
+        spec = importlib.util.spec_from_loader("_mcbind", importlib.machinery.ExtensionFileLoader("_mcbind", path))
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        at = [ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in ("mc_kv_append", "mc_attn_decode", "mc_attn_prefill")]
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        m.setup(*at, torch.empty, raw, getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device, torch.float32,
+                torch.int32, torch.uint8)
+        _fast_module = m
+    return _fast_module
+
+
+def _side(name, t, cache, dtype, n):
+    """Pointer of a contiguous side input of n elements, or None."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != cache.device:
-        _bad("%s must be a contiguous %s tensor %s on the cache's device" % (name, dtype, shape))
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != cache.index:
+        _bad("%s must be a contiguous %s tensor of %d elements on the cache's device" % (name, dtype, n))
     return t.data_ptr()
 
 
@@ -485,47 +525,67 @@ def kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope=None, interleaved: b
     rot_dim]: rot_dim/2 cosines, then sines; None: not), k and v written to their pages.
     Returns the queries [tokens, q_heads, head_dim].  q, k, v may be slices of one
     projection's output."""
-    import torch
-    heads = q.shape[1] if q.dim() == 3 else -1
-    qs = _rows("q", q, cache, batch)
-    ks = _rows("k", k, cache, batch, cache.kv_heads)
-    vs = _rows("v", v, cache, batch, cache.kv_heads)
+    r = (_fast_module or _fast()).kv_append(cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace)
+    if r is not None:
+        return _check(r) if r.__class__ is int else r
+    heads, qs = _rows("q", q, cache, batch)
+    _, ks = _rows("k", k, cache, batch, cache.kv_heads)
+    _, vs = _rows("v", v, cache, batch, cache.kv_heads)
     if q_out is None:
-        q_out = torch.empty((batch.tokens, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+        q_out = _torch().empty((batch.tokens, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
     elif not q_out.is_contiguous():
         _bad("q_out must be contiguous")
     else:
         _rows("q_out", q_out, cache, batch, heads)
-    rows = rot = 0
+    rows, rot, table = 0, 0, None
     if rope is not None:
-        if rope.dim() != 2 or rope.dtype != torch.float32 or not rope.is_contiguous() or rope.device != cache.device:
+        if rope.dim() != 2 or rope.dtype is not _torch().float32 or not rope.is_contiguous() or rope.get_device() != cache.index:
             _bad("rope must be a contiguous fp32 [positions, rot_dim] on the cache's device")
         rows, rot = rope.shape
-    dim = (cache.head_dim,)
-    _check(load().mc_kv_append(cache._ref, batch._ref, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, heads,
-                               _side("q_norm", q_norm, cache, cache.dtype, dim),
-                               _side("k_norm", k_norm, cache, cache.dtype, dim), eps, _ptr(rope), rows, rot,
-                               1 if interleaved else 0, q_out.data_ptr(), _ptr(workspace), _stream()))
+        table = rope.data_ptr()
+    if q_norm is not None:
+        q_norm = _side("q_norm", q_norm, cache, cache.dtype, cache.head_dim)
+    if k_norm is not None:
+        k_norm = _side("k_norm", k_norm, cache, cache.dtype, cache.head_dim)
+    if workspace is not None:
+        workspace = _status(workspace, cache)
+    rc = load().mc_kv_append(cache._ref, batch._ref, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, heads, q_norm,
+                             k_norm, eps, table, rows, rot, 1 if interleaved else 0, q_out.data_ptr(), workspace, _stream())
+    if rc:
+        _check(rc)
     return q_out
 
 
-def _attention(fn, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace):
-    import torch
-    qs = _rows("q", q, cache, batch)
-    heads = q.shape[1]
+def _status(workspace, cache):
+    if workspace.get_device() != cache.index or not workspace.is_contiguous():
+        _bad("the workspace must be contiguous on the cache's device")
+    return workspace.data_ptr()
+
+
+def _attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace):
+    r = (_fast_module or _fast()).attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace)
+    if r is not None:
+        return _check(r) if r.__class__ is int else r
+    fn = load().mc_attn_prefill if prefill else load().mc_attn_decode
+    heads, qs = _rows("q", q, cache, batch)
+    empty, dev = _torch().empty, cache.device
     if out is None:
-        out = torch.empty((batch.tokens, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
-    os_ = _rows("out", out, cache, batch, heads)
+        out, os_ = empty((batch.tokens, heads, cache.head_dim), dtype=cache.dtype, device=dev), heads * cache.head_dim
+    else:
+        os_ = _rows("out", out, cache, batch, heads)[1]
     if workspace is None:
         workspace = attn_workspace(cache, heads)
-    elif workspace.device != cache.device:
-        _bad("the workspace must be on the cache's device")
-    lse = torch.empty((batch.tokens, heads), dtype=torch.float32, device=cache.device) if with_lse else None
-    opts = _AttnOptsC(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
-                      _side("slopes", slopes, cache, torch.float32, (heads,)),
-                      _side("prefix", prefix, cache, torch.int32, (batch.seqs,)))
-    _check(fn(cache._ref, batch._ref, q.data_ptr(), qs, heads, ctypes.addressof(opts), out.data_ptr(), os_, _ptr(lse),
-              workspace.data_ptr(), workspace.numel(), _stream()))
+    ws = _status(workspace, cache)
+    lse = empty((batch.tokens, heads), dtype=_torch().float32, device=dev) if with_lse else None
+    if slopes is not None:
+        slopes = _side("slopes", slopes, cache, _torch().float32, heads)
+    if prefix is not None:
+        prefix = _side("prefix", prefix, cache, _torch().int32, batch.seqs)
+    opts = _AttnOptsC(cache.head_dim ** -0.5 if scale is None else scale, softcap, window, slopes, prefix)
+    rc = fn(cache._ref, batch._ref, q.data_ptr(), qs, heads, ctypes.addressof(opts), out.data_ptr(), os_,
+            lse.data_ptr() if with_lse else None, ws, workspace.numel() * workspace.element_size(), _stream())
+    if rc:
+        _check(rc)
     return (out, lse) if with_lse else out
 
 
@@ -535,7 +595,7 @@ def attn_decode(cache: KVCache, batch: KVBatch, q, scale=None, softcap: float = 
     that already holds it.  scale: head_dim ** -0.5 by default; softcap > 0: scores
     softcap * tanh(x / softcap); window > 0: the last `window` keys only; slopes fp32
     [heads]: bias slope * (j - p).  Returns out (and lse fp32 [seqs, heads])."""
-    return _attention(load().mc_attn_decode, cache, batch, q, scale, softcap, window, slopes, None, out, with_lse,
+    return _attention(False, cache, batch, q, scale, softcap, window, slopes, None, out, with_lse,
                       workspace)
 
 
@@ -544,7 +604,7 @@ def attn_prefill(cache: KVCache, batch: KVBatch, q, scale=None, softcap: float =
     """Causal attention of the batch's new tokens, q [tokens, heads, head_dim], over the
     cache that already holds them; options as attn_decode's, and prefix int32 [seqs]:
     leading keys that every query of the sequence sees.  Returns out (and lse)."""
-    return _attention(load().mc_attn_prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse,
+    return _attention(True, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse,
                       workspace)
 
 

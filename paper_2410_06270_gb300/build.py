@@ -3,7 +3,8 @@
 Every translation unit is compiled in parallel to an object file under
 ``paper_2410_06270_gb300/_build/`` and linked into ``_build/libmc.so``.  Objects
 are rebuilt when their source or any header is newer.  No cmake, no torch
-extension machinery: the library has a plain C ABI.
+extension machinery: the library has a plain C ABI.  Beside it, the marshalling of
+the calls that a decode step makes is a small CPython extension.
 """
 from __future__ import annotations
 
@@ -13,12 +14,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libmc.so")
+BIND = os.path.join(BUILD, "_mcbind.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -71,7 +74,19 @@ def build(verbose: bool = False, force: bool = False, ptxas_verbose: bool = Fals
         tmp = LIB + ".tmp%d" % os.getpid()
         subprocess.check_call([nvcc, "-shared"] + ARCH + ["-o", tmp] + objs + ["-lcudart"])
         os.replace(tmp, LIB)
+    _build_binding()
     return LIB
+
+
+def _build_binding() -> None:
+    """The CPython extension that marshals the calls of a decode step (host code, gcc)."""
+    src = os.path.join(HERE, "bind", "mc_bind.c")
+    if os.path.exists(BIND) and os.path.getmtime(BIND) >= max(os.path.getmtime(src), *[os.path.getmtime(h) for h in _headers()]):
+        return
+    tmp = BIND + ".tmp%d" % os.getpid()
+    subprocess.check_call(["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", INCLUDE, src,
+                           "-o", tmp])
+    os.replace(tmp, BIND)
 
 
 if __name__ == "__main__":
