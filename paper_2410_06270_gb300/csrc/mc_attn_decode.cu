@@ -6,7 +6,7 @@
 // the design is about keeping loads in flight on every SM whatever the lengths are.
 //
 // Work is cut into units of 64 (heads of 64: 128) keys of one (sequence, key head); the units of the whole
-// batch, in order, are dealt to the CTAs as equal contiguous runs, which each CTA finds from
+// batch, in order, are dealt to the CTAs as contiguous runs of equal cost, which each CTA finds from
 // the lengths by itself (no host knowledge of them, so a captured graph serves any).  A run
 // that ends inside an item leaves a partial result (m, l, o in fp32); join_kernel adds the
 // pieces of an item in their order.  At most two partials per CTA, whatever the batch.
@@ -26,6 +26,8 @@ constexpr int dec_tiles(int D) { return D == 64 ? 2 : 1; }
 constexpr int dec_unit(int D) { return 16 * dec_tiles(D) * kDecWarps; }
 constexpr int kDecCtasPerSm = 2;
 constexpr int kDecMaxTiles = 4;                // n-tiles of the largest slice
+constexpr int kDecItemCost = 2;  // what an item costs on top of its units, in units (up to 128 sequences; 64 of up
+                                // to 500 keys 23.8 us at 0, 18.4 at 1, 18.1 at 2, 18.4 at 3)
 constexpr float kLazy = 8.f;  // the maximum moves only when a score passes it by 2^8: the
                               // weights stay below 2^8, far inside fp16 and bf16
 
@@ -181,62 +183,73 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
     pdl_trigger();
     pdl_wait();
 
-    // all units, and the place of this CTA's first
+    // the batch's cost, and where this CTA's run of it starts and ends
     int64_t total = 0, own = 0;
-    int ctas;
+    int ctas, left = 0;
     int64_t u0 = 0, u1 = 0;
     Place at;  // compute side
     at.b = -1;
     const bool few = p.b.seqs <= 128;
     const int each = p.b.seqs <= 32 ? 1 : 4;  // sequences a lane
-    int mine[4] = {0, 0, 0, 0}, sum4 = 0;
+    int cost[4] = {0, 0, 0, 0}, units[4] = {0, 0, 0, 0}, cost4 = 0, units4 = 0;
     bool small = true;
     if (few) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (i >= each) break;
             const int b = each * lane + i;
-            const int64_t n = b < p.b.seqs ? units_of<NT>(p, keys_of<D>(p, b, p.status)) : 0;
-            small &= n < 1 << 24;
-            mine[i] = (int)n;
-            sum4 += mine[i];
+            if (b >= p.b.seqs) break;
+            const Keys k = keys_of<D>(p, b, p.status);
+            const int64_t n = units_of<NT>(p, k);
+            small &= n < 1 << 22;
+            units[i] = (int)n;
+            cost[i] = n ? units[i] + kDecItemCost * slices_of<NT>(p, k) * p.c.kv_heads : 0;
+            units4 += units[i];
+            cost4 += cost[i];
         }
     }
     if (few && __all_sync(0xffffffffu, small)) {
         // 32 bits hold it all, and the divisions are by fixed numbers but one
-        int sum = sum4;
+        int upto = cost4, units_upto = units4;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, sum, d);
-            if (lane >= d) sum += o;
+            const int o = __shfl_up_sync(0xffffffffu, upto, d), v = __shfl_up_sync(0xffffffffu, units_upto, d);
+            if (lane >= d) upto += o, units_upto += v;
         }
-        const int all = __shfl_sync(0xffffffffu, sum, 31);
+        const int all = __shfl_sync(0xffffffffu, upto, 31);
         total = all;
         ctas = min(all, (int)gridDim.x);
+        // place of a cost in the batch; returns the units before it
+        auto find = [&](int pos, Place &x) {
+            const int l = __ffs(__ballot_sync(0xffffffffu, upto > pos)) - 1;
+            int r = pos - __shfl_sync(0xffffffffu, upto - cost4, l), before = __shfl_sync(0xffffffffu, units_upto - units4, l);
+            x.b = each * l;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                if (i + 1 >= each) break;
+                const int n = __shfl_sync(0xffffffffu, cost[i], l), v = __shfl_sync(0xffffffffu, units[i], l);
+                if (x.b == each * l + i && r >= n) {
+                    r -= n;
+                    before += v;
+                    ++x.b;
+                }
+            }
+            x.k = keys_of<D>(p, x.b, nullptr);
+            x.slices = slices_of<NT>(p, x.k);
+            const int per = x.k.units + kDecItemCost, item = (int)((unsigned)r / (unsigned)per);
+            x.u = max(0, r - item * per - kDecItemCost);
+            x.h = x.slices == 1 ? item : (int)((unsigned)item / (unsigned)x.slices);
+            x.sl = item - x.h * x.slices;
+            return before + item * x.k.units + x.u;
+        };
         if ((int)blockIdx.x < ctas) {
             int rest = 0, q = 1;
             if (ctas == (int)gridDim.x) q = by_grid.div(all, rest);
             const int c = blockIdx.x, first = q * c + by_grid.div(rest * c), end = q * (c + 1) + by_grid.div(rest * (c + 1));
-            u0 = first;
             u1 = end;
-            const int l = __ffs(__ballot_sync(0xffffffffu, sum > first)) - 1;
-            int r = first - __shfl_sync(0xffffffffu, sum - sum4, l);
-            at.b = each * l;
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                if (i + 1 >= each) break;
-                const int n = __shfl_sync(0xffffffffu, mine[i], l);
-                if (at.b == each * l + i && r >= n) {
-                    r -= n;
-                    ++at.b;
-                }
-            }
-            at.k = keys_of<D>(p, at.b, nullptr);
-            at.slices = slices_of<NT>(p, at.k);
-            const int item = (int)((unsigned)r / (unsigned)at.k.units);
-            at.u = r - item * at.k.units;
-            at.h = at.slices == 1 ? item : (int)((unsigned)item / (unsigned)at.slices);
-            at.sl = item - at.h * at.slices;
+            Place past;
+            const int until = end < all ? find(end, past) : __shfl_sync(0xffffffffu, units_upto, 31);
+            left = until - find(first, at);
         }
     } else {
         for (int b0 = 0; b0 < p.b.seqs; b0 += 32) {
@@ -273,10 +286,9 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             at.u = (int)(r - item * at.k.units);
             at.h = (int)div64(item, at.slices);
             at.sl = (int)(item - (int64_t)at.h * at.slices);
+            left = (int)(u1 - u0);
         }
     }
-    int left = at.b < 0 ? 0 : (int)(u1 - u0);
-
     // ---- loads: this warp's 16 keys and values of a unit into ring slot i % kStages
     constexpr int kChunks = D / 8, kPer = 32 / kChunks;  // 16-byte chunks of a row; rows per warp copy
     const int lc = lane % kChunks, lr = lane / kChunks;
@@ -544,7 +556,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         if (from_first && !to_last) {
             open_tail = true;
             if (tid == 0) {
-                const int64_t end = u1 - left + at.k.units;  // one past the item's last unit
+                const int64_t end = u1 - n + at.k.units;  // the item's end: the run ends n units into it
                 const int64_t last = div64(end * ctas + total - 1, total);  // one past the CTA that holds it
                 open[blockIdx.x] = {(int32_t)(last - blockIdx.x), at.b, at.h, at.sl};
             }
