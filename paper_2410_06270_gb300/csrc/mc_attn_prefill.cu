@@ -19,9 +19,9 @@
 // This splits a long cache over the SMs when there are few rows, and balances the causal
 // triangle, by the same rule.
 //
-// Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 issues the MMAs,
-// 9 copies keys and values (TMA, a box per page and 64 columns), 10 the queries (TMA where a
-// tile is whole tokens of the group's heads, else with 11 by cp.async).
+// Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 and 9 issue a tile's MMAs,
+// 10 copies keys and values (TMA, a box per page and 64 columns), 11 the queries (TMA where a
+// tile is whole tokens of the group's heads, else cp.async).
 // Tensor memory: S (and P) of tile t at column 128 t, O at 256 + 128 t.
 #include <math.h>
 
@@ -38,7 +38,7 @@
 namespace mc {
 
 constexpr int kPfRows = 256, kPfTile = 128, kPfKeys = 128;
-constexpr int kPfThreads = 384, kPfMma = 8, kPfKv = 9, kPfQ0 = 10, kPfQWarps = 2;
+constexpr int kPfThreads = 384, kPfMma = 8, kPfKv = 10;  // MMA: two warps; after kPfKv the queries
 constexpr int kPfMaxStages = 8;
 constexpr float kPfLazy = 8.f;
 
@@ -467,17 +467,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     if (tid == 0) {
         for (int i = 0; i < Sh::kStages; ++i) {
             mbar_init(&sh->kfull[i], 1);
-            mbar_init(&sh->kempty[i], 1);
+            mbar_init(&sh->kempty[i], 2);
         }
         mbar_init(&sh->vpatch, 1);
         for (int t = 0; t < 2; ++t) {
-            mbar_init(&sh->qfull[t], pp.q_boxes ? 1 : 32 * kPfQWarps);
+            mbar_init(&sh->qfull[t], pp.q_boxes ? 1 : 32);
             mbar_init(&sh->qempty[t], 1);
             mbar_init(&sh->sfull[t], 1);
             mbar_init(&sh->pfull[t], 4);
             mbar_init(&sh->ofull[t], 1);
         }
-        mbar_init(&sh->drain, 1);
+        mbar_init(&sh->drain, 2);
         sh->abort = 0;
         fence_mbar_init();
     }
@@ -622,9 +622,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1)))
                     if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
             pdl_trigger();
-        } else if (warp == kPfQ0 || !pp.q_boxes) {
+        } else {
             // queries, a tile as soon as the last item's has been read
-            constexpr int kChunks = D / 8, kPer = 32 / kChunks, kQStep = kPfQWarps * kPer;
+            constexpr int kChunks = D / 8, kPer = 32 / kChunks, kQStep = kPer;
             const int lc = lane % kChunks, lr = lane / kChunks;
             const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
             const int step_hg = kQStep % p.group;
@@ -649,7 +649,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         continue;
                     }
                     // one row per kChunks lanes, zeros past the last
-                    int r = t * kPfTile + (warp - kPfQ0) * kPer + lr;
+                    int r = t * kPfTile + lr;
                     int hg;
                     const int tok = p.by_group.div(rows0 + r, hg);
                     const uint16_t *src = p.q + (at.s.first + tok) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         const uint32_t q0 = pf_desc_k(smem_u32(smem + Sh::kHdr)), k0 = pf_desc_k(smem_u32(smem + Sh::kRing));
         const uint32_t v0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
         constexpr uint32_t kStep = Sh::kTileBytes >> 4;
-        int uses[2] = {0, 0}, quses[2] = {0, 0};
+        int uses = 0, quses = 0;
         bool ok = true;
         auto qk = [&](int t, int slot) {  // S_t = Q_t K^T
             const uint32_t a = q0 + t * kStep, b = k0 + slot * kStep;
@@ -706,23 +706,32 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         };
         auto full = [&](const Slot &x) { return warp_wait(&sh->kfull[x.i], x.phase, pp, sh); };
         auto tiles_of = [&](const PfPlace &a) { return a.s.n * p.group - a.mt * kPfRows > kPfTile ? 2 : 1; };
-        // Unit j's PV of a tile is followed by unit j + 1's QK of it, the next item's first one
+        // Unit j's PV of the tile is followed by unit j + 1's QK of it, the next item's first one
         // after the last: the next queries and the other tile's softmax hide the change of item.
+        // A warp for each tile: their waits do not add up, and either's MMAs fill the pipe.
+        const int t = warp - kPfMma;
         Slot k = {0, 0};  // of the last keys that QK was issued for
         int n = pf_units(run, at), tiles = n > 0 ? tiles_of(at) : 0;
-        auto issue_qk = [&](int t, const Slot &x, bool last_tile, bool last_unit) {
+        // a ring slot that this warp has no MMA for (the item has one tile) is given back at once
+        auto pass = [&](const Slot &x) {
+            if (lane == 0) mbar_arrive(&sh->kempty[x.i]);
+        };
+        auto first_qk = [&](const Slot &x, bool last_unit) {
+            if (!warp_wait(&sh->qfull[t], quses++ & 1, pp, sh)) return false;
             tc_fence_after();
             if (elect_one()) {
                 qk(t, x.i);
                 umma_commit(&sh->sfull[t]);
-                if (last_tile) umma_commit(&sh->kempty[x.i]);
+                umma_commit(&sh->kempty[x.i]);
                 if (last_unit) umma_commit(&sh->qempty[t]);
             }
             __syncwarp();
+            return true;
         };
-        if (n > 0) ok = full(k);
-        for (int t = 0; ok && t < tiles; ++t)
-            if ((ok = warp_wait(&sh->qfull[t], quses[t]++ & 1, pp, sh))) issue_qk(t, k, t == tiles - 1, n == 1);
+        if (n > 0 && (ok = full(k))) {
+            if (t < tiles) ok = first_qk(k, n == 1);
+            else pass(k);
+        }
         while (ok && n > 0) {
             PfPlace nx = at;
             int next_n = 0, next_tiles = 0;
@@ -731,24 +740,25 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 next_n = pf_units(run, nx);
                 if (next_n > 0) next_tiles = tiles_of(nx);
             }
-            // inside the item: unit j's PV and unit j + 1's QK of a tile are issued together
+            // inside the item: unit j's PV and unit j + 1's QK are issued together
             for (int j = 0; ok && j + 1 < n; ++j) {
                 const Slot v = k.next(), k2 = v.next();
                 if (!(ok = full(v) && full(k2))) break;
-                for (int t = 0; t < tiles; ++t) {
-                    if (!(ok = warp_wait(&sh->pfull[t], uses[t]++ & 1, pp, sh))) break;
+                if (t < tiles) {
+                    if (!(ok = warp_wait(&sh->pfull[t], uses++ & 1, pp, sh))) break;
                     tc_fence_after();
                     if (elect_one()) {
                         pv(t, v.i, j == 0);
+                        umma_commit(&sh->kempty[v.i]);
                         qk(t, k2.i);
                         umma_commit(&sh->sfull[t]);
-                        if (t == tiles - 1) {
-                            umma_commit(&sh->kempty[v.i]);
-                            umma_commit(&sh->kempty[k2.i]);
-                        }
+                        umma_commit(&sh->kempty[k2.i]);
                         if (j + 2 == n) umma_commit(&sh->qempty[t]);
                     }
                     __syncwarp();
+                } else {
+                    pass(v);
+                    pass(k2);
                 }
                 k = k2;
             }
@@ -757,22 +767,22 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             const Slot v = k.next();
             if (!(ok = full(v))) break;
             k = v.next();
-            for (int t = 0; t < max(tiles, next_tiles); ++t) {
-                if (t < tiles) {
-                    if (!(ok = warp_wait(&sh->pfull[t], uses[t]++ & 1, pp, sh))) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        pv(t, v.i, n == 1);
-                        if (t == tiles - 1) umma_commit(&sh->kempty[v.i]);
-                        umma_commit(&sh->ofull[t]);
-                    }
-                    __syncwarp();
+            if (t < tiles) {
+                if (!(ok = warp_wait(&sh->pfull[t], uses++ & 1, pp, sh))) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    pv(t, v.i, n == 1);
+                    umma_commit(&sh->kempty[v.i]);
+                    umma_commit(&sh->ofull[t]);
                 }
-                if (t < next_tiles) {
-                    if (t == 0 && !(ok = full(k))) break;
-                    if (!(ok = warp_wait(&sh->qfull[t], quses[t]++ & 1, pp, sh))) break;
-                    issue_qk(t, k, t == next_tiles - 1, next_n == 1);
-                }
+                __syncwarp();
+            } else {
+                pass(v);
+            }
+            if (next_n > 0) {
+                if (!(ok = full(k))) break;
+                if (t < next_tiles) ok = first_qk(k, next_n == 1);
+                else pass(k);
             }
             at = nx;
             n = next_n;
