@@ -243,6 +243,19 @@ def test_prefill_of_one_token_each_is_decode(mc):
     assert torch.allclose(dl, pl, rtol=1e-4, atol=1e-4)
 
 
+@pytest.mark.parametrize("dim,dtype,cap,spread", [(128, "bf16", 2.0, 1.0), (64, "fp16", 0.5, 3.0), (128, "fp16", 40.0, 1.5), (64, "bf16", 8.0, 2.0)])
+def test_caps_far_below_and_around_the_scores(mc, dim, dtype, cap, spread):
+    """Scores from a fraction of the cap to many times it: both of the cap's forms, in every kernel."""
+    for lens, new in (([200, 515], [1, 1]), ([200, 515], [7, 3]), ([260, 300], [260, 130])):
+        B = ref.Batch(lens, new, 2, 32, dim, dtype, 31)
+        q = spread * B.randn(B.tokens, 8, dim)
+        q[0] *= 0.01
+        want = ref.attention(B, q, dim ** -0.5, cap)
+        cache, batch = B.device(mc)
+        out, lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=cap, with_lse=True)
+        ref.assert_attention(out, lse, want, dtype, 520, 5.0)
+
+
 # ----------------------------------------------------------- streams, status --
 
 def test_on_another_stream_and_in_a_graph(mc):
