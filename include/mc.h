@@ -365,7 +365,8 @@ typedef struct {
  * head h reads key head h / (q_heads / kv_heads).
  *   out [token][q_heads][head_dim] (token stride out_stride) = softmax over the visible keys . v
  *   lse fp32 [tokens][q_heads] (may be NULL): log of the sum of exponentials
- * A query that sees no key gets a zero row and lse = -inf.  Scores, statistics and sums
+ * A query that sees no key gets a zero row and lse = -inf.  Keys that a query does not see do
+ * not reach its row, whatever they hold, infinities and NaN included.  Scores, statistics and sums
  * are fp32; the probabilities are rounded to the cache's dtype for their product with v.
  * mc_attn_decode takes one new token per sequence (cu_q NULL), mc_attn_prefill any number. */
 int mc_attn_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,

@@ -253,6 +253,56 @@ __device__ __forceinline__ float capped(float x, float top) { return fmaf(rcp(1.
 
 int launch_append(AppendParams p, int head_dim, bool bf16, cudaStream_t st);
 
+// One row by the definition, by a warp, key by key: what the kernels fall back to for a row
+// whose sum came out infinite or NaN.  They multiply hidden keys' values by weights of 0, which
+// an infinite or NaN value survives; here a hidden key is not touched.  (Slow, and meant to be:
+// finite caches never come here.)
+template <int D, bool BF16>
+__device__ __noinline__ void exact_row(const AttnParams &p, int b, int pos, int len, int prefix, int token, int head, int lane)
+{
+    constexpr int kPer = D / 64;  // 32-bit words a lane holds of a row
+    float2 q[kPer], o[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        q[e] = unpack2<BF16>(*reinterpret_cast<const uint32_t *>(p.q + token * p.q_stride + head * D + 2 * (lane * kPer + e)));
+        o[e] = make_float2(0.f, 0.f);
+    }
+    const int h = p.by_group.div(head), end = pos < 0 ? 0 : min(len, max(pos + 1, prefix));
+    const float slope = p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+    for (int j = p.window ? max(0, pos - p.window + 1) : 0; j < end; ++j) {
+        int row;
+        const int i = p.c.page.div(j, row), page = seq_page(p.b, p.c, b, i, p.status);
+        const int64_t at = page * p.c.page_stride + ((int64_t)h * p.c.page_size + row) * D;
+        float x = 0.f;
+        float2 v[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int64_t w = at + 2 * (lane * kPer + e);
+            const float2 k = unpack2<BF16>(page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(p.c.k + w));
+            v[e] = unpack2<BF16>(page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(p.c.v + w));
+            x = fmaf(q[e].x, k.x, fmaf(q[e].y, k.y, x));
+        }
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        x *= p.scale;
+        if (p.cap > 0.f) x = capped(x, p.cap);
+        x = fmaf(slope, (float)(j - pos), x);
+        const float top = fmaxf(m, x), keep = top == m ? 1.f : ex2(m - top), pr = ex2(x - top);
+        m = top;
+        l = fmaf(l, keep, pr);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = make_float2(fmaf(o[e].x, keep, pr * v[e].x), fmaf(o[e].y, keep, pr * v[e].y));
+    }
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        *reinterpret_cast<uint32_t *>(p.out + token * p.out_stride + head * D + 2 * (lane * kPer + e)) =
+            l == 0.f ? 0u : pack2<BF16>(o[e].x * inv, o[e].y * inv);
+    if (p.lse && lane == 0) p.lse[(int64_t)token * p.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
 constexpr int kAttnMaxSms = 160;  // SMs that the workspace has room for (the GB300's 152)
 // SMs of the current device, asked for once per device.
 cudaError_t sm_count(int *out);

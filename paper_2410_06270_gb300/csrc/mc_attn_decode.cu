@@ -152,6 +152,12 @@ __device__ __forceinline__ void store_row(const AttnParams &p, int token, int he
     if (p.lse && d == 0) p.lse[(int64_t)token * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
+__device__ __forceinline__ bool finite4(const float4 &a)
+{
+    const float z = fmaf(a.x, 0.f, fmaf(a.y, 0.f, fmaf(a.z, 0.f, a.w * 0.f)));
+    return z == z;
+}
+
 template <int D, int NT>
 struct DecShape {
     static constexpr int kRow = D * 2;                       // bytes of a key
@@ -179,6 +185,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
     float *jo = reinterpret_cast<float *>(smem + Sh::kRing);
     uint2 *qs = reinterpret_cast<uint2 *>(smem + Sh::kRing);  // [n-tile][k-step][lane]
     Row *rows = reinterpret_cast<Row *>(smem + Sh::kRing + Sh::kRows0);
+    int *marks = reinterpret_cast<int *>(smem + Sh::kRing);
     const uint32_t ring = smem_u32(smem) + warp * Sh::kSlot * Sh::kStages;
     pdl_trigger();
     pdl_wait();
@@ -505,6 +512,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 
         // ---- the four warps' parts, an n-tile at a time
         const bool whole = from_first && to_last;
+        unsigned odd = 0;  // rows that came out infinite or NaN
         float *mine = part + (2 * blockIdx.x + (from_first ? 1 : 0)) * dec_part_floats(D, NT);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -546,13 +554,27 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                     int hg;
                     const int tok = p.by_group.div(r0 + r, hg);
                     store_row<BF16>(p, keys.first + tok, h0 + hg, D, d, acc, top, sum);
+                    // (one token's row hides no key of its units: what it sums is what it sees)
+                    if (keys.n > 1 && !finite4(acc)) odd |= 1u << r;
                 } else {
                     *reinterpret_cast<float4 *>(mine + r * D + d) = acc;
                     if (d == 0) *reinterpret_cast<float2 *>(mine + 8 * NT * D + 2 * r) = make_float2(top, sum);
                 }
             }
         }
-        __syncthreads();  // the join buffers are free again
+        if (__syncthreads_or(odd)) {  // the join buffers are free again
+            if (tid < 8 * NT) marks[tid] = 0;
+            __syncthreads();
+            for (unsigned x = odd; x; x &= x - 1) marks[__ffs(x) - 1] = 1;
+            __syncthreads();
+            for (int r = warp; r < nrows; r += kDecWarps) {
+                if (!marks[r]) continue;
+                int hg;
+                const int tok = p.by_group.div(r0 + r, hg);
+                exact_row<D, BF16>(p, at.b, p0 + tok, keys.len, prefix, keys.first + tok, h0 + hg, lane);
+            }
+            __syncthreads();
+        }
         if (from_first && !to_last) {
             open_tail = true;
             if (tid == 0) {
@@ -594,8 +616,8 @@ __global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const Ope
     if (it.pieces == 0) return;
     const int r = blockIdx.y, tid = threadIdx.x;
     int first, hg;
-    const int rows = seq_rows(p.b, it.b, first, nullptr) * p.group, f = it.sl * 8 * nt + r;
-    if (f >= rows) return;
+    const int n = seq_rows(p.b, it.b, first, nullptr), f = it.sl * 8 * nt + r;
+    if (f >= n * p.group) return;
     const int tok = p.by_group.div(f, hg);
     const size_t stride = dec_part_floats(D, nt);
     auto piece = [&](int i) { return part + (2 * ((size_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * stride; };
@@ -621,16 +643,23 @@ __global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const Ope
     acc_s[tid] = acc;
     if (col == 0) sums[grp] = sum;
     __syncthreads();
-    if (grp) return;
-    sum = 0.f;
-    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    bool odd = false;
+    if (grp == 0) {
+        sum = 0.f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-        const float4 v = acc_s[i * kCols + col];
-        sum += sums[i];
-        acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
+        for (int i = 0; i < kGroups; ++i) {
+            const float4 v = acc_s[i * kCols + col];
+            sum += sums[i];
+            acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
+        }
+        store_row<BF16>(p, first + tok, it.h * p.group + hg, D, 4 * col, acc, top, sum);
+        odd = n > 1 && !finite4(acc);
     }
-    store_row<BF16>(p, first + tok, it.h * p.group + hg, D, 4 * col, acc, top, sum);
+    if (__syncthreads_or(odd) && tid < 32) {
+        const int len = seq_len(p.b, p.c, it.b, nullptr);
+        exact_row<D, BF16>(p, it.b, len - n + tok, len, p.prefix ? __ldg(p.prefix + it.b) : 0, first + tok, it.h * p.group + hg, tid);
+    }
 }
 
 constexpr int kDecMaxCtas = kDecCtasPerSm * kAttnMaxSms;

@@ -128,17 +128,18 @@ __device__ __forceinline__ PfSeq pf_seq(const AttnParams &p, int b, int32_t *sta
 // Keys [base, end) that rows of item mt see, base rounded down to a unit; at least
 // one unit (of zeros, all masked), so that rows without keys take the same way.
 struct PfKeys {
-    int base, end, units, p_lo;
+    int base, end, units, first;  // first: the first key that is seen
 };
 
 __device__ __forceinline__ PfKeys pf_keys(const AttnParams &p, const PfSeq &s, int mt)
 {
     PfKeys k;
     const int last = min((mt + 1) * kPfRows, s.n * p.group) - 1;
-    k.p_lo = s.len - s.n + p.by_group.div(mt * kPfRows);
+    const int p_lo = s.len - s.n + p.by_group.div(mt * kPfRows);
     const int p_hi = s.len - s.n + p.by_group.div(last);
     k.end = p_hi < 0 ? 0 : min(s.len, max(p_hi + 1, s.prefix));
-    k.base = p.window ? max(0, k.p_lo - p.window + 1) & ~(kPfKeys - 1) : 0;
+    k.first = p.window ? max(0, p_lo - p.window + 1) : 0;
+    k.base = k.first & ~(kPfKeys - 1);
     k.units = max(1, (k.end - k.base + kPfKeys - 1) / kPfKeys);
     return k;
 }
@@ -564,13 +565,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         const uint32_t smem0 = smem_u32(smem);
         if (warp == kPfKv) {
             // keys and values: lane i copies the i-th box (of a page) of a tile.  A page that is
-            // not there, and rows past the last key's page, are read beyond the map: zeros.
+            // not there, and boxes before the first key or past the last, are read beyond the map:
+            // zeros.
             const int boxes = kPfKeys / pp.box_rows;
             int it = 0, patches = 0, n;
             bool ok = !(pp.debug & kDebugNoProducer);
             auto pages = [&](int u) {
                 const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
-                return lane < boxes && j < at.k.end ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j)) : -1;
+                return lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j)) : -1;
             };
             while (ok && (n = pf_units(run, at)) > 0) {
                 int page = pages(at.u);
@@ -580,7 +582,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                     int row;
                     p.c.page.div(j, row);
                     if ((unsigned)page >= (unsigned)p.c.num_pages) {
-                        if (lane < boxes && j < at.k.end) set_status(p.status, MC_ERR_RANGE);
+                        if (lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first) set_status(p.status, MC_ERR_RANGE);
                         page = p.c.num_pages;
                     }
                     for (int kv = 0; kv < 2; ++kv, ++it) {
@@ -849,6 +851,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 float *mine = pp.part + (2 * blockIdx.x + (from_first ? 1 : 0)) * pf_part_floats(D);
                 const bool whole = from_first && to_last;
                 if (wt * 32 < rows) {
+                    float odd = 0.f;  // NaN once an element of the row is infinite or NaN
 #pragma unroll
                     for (int d = 0; d < D; d += 32) {
                         uint32_t o[32];
@@ -859,6 +862,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
                                 v[i] = l == 0.f ? 0u : pack2<BF16>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) odd = fmaf(__uint_as_float(o[i]), 0.f, odd);
                             // a lane's row is 2 D bytes from its neighbour's: whole 32-byte sectors
 #pragma unroll
                             for (int i = 0; i < 16; i += 8) {
@@ -882,6 +887,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         p.lse[(int64_t)(at.s.first + tok) * p.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
                     if (live && !whole)
                         reinterpret_cast<float2 *>(mine + kPfRows * D)[t * kPfTile + row] = make_float2(m, l);
+                    for (unsigned which = __ballot_sync(0xffffffffu, odd != odd); which; which &= which - 1) {
+                        const int r = __ffs(which) - 1;
+                        const int tr = __shfl_sync(0xffffffffu, tok, r), hr = __shfl_sync(0xffffffffu, head, r);
+                        exact_row<D, BF16>(p, at.b, off + tr, at.s.len, at.s.prefix, at.s.first + tr, hr, lane);
+                    }
                 }
                 tc_fence_before();
             }
@@ -916,6 +926,7 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
 {
     constexpr int kQuads = D / 4 / 16;  // column quads of a thread: threadIdx.x / 16, + 16, ...
     __shared__ float2 ml[kAttnMaxSms][kPfJoinRows];
+    __shared__ int odd[kPfJoinRows];
     const AttnParams &p = pp.a;
     pdl_trigger();
     pdl_wait();
@@ -927,34 +938,50 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
     const PfSeq s = pf_seq(p, it.b, nullptr);
     const int f = it.mt * kPfRows + row;
     __syncthreads();
-    if (f >= s.n * p.group) return;
     int hg;
     const int tok = p.by_group.div(f, hg), head = it.h * p.group + hg;
-    float top = -INFINITY;
-    for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, ml[i][r].x);
-    float4 acc[kQuads];
+    float strange = 0.f;
+    if (f < s.n * p.group) {
+        float top = -INFINITY;
+        for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, ml[i][r].x);
+        float4 acc[kQuads];
 #pragma unroll
-    for (int k = 0; k < kQuads; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
+        for (int k = 0; k < kQuads; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
 #pragma unroll 4
-    for (int i = 0; i < it.pieces; ++i) {
-        const float *q = piece(i);
-        const float w = ml[i][r].x == -INFINITY ? 0.f : ex2(ml[i][r].x - top);
-        sum = fmaf(w, ml[i][r].y, sum);
+        for (int i = 0; i < it.pieces; ++i) {
+            const float *q = piece(i);
+            const float w = ml[i][r].x == -INFINITY ? 0.f : ex2(ml[i][r].x - top);
+            sum = fmaf(w, ml[i][r].y, sum);
+#pragma unroll
+            for (int k = 0; k < kQuads; ++k) {
+                const float4 v = reinterpret_cast<const float4 *>(q)[(size_t)(c0 + 16 * k) * kPfRows + row];
+                acc[k] = make_float4(fmaf(w, v.x, acc[k].x), fmaf(w, v.y, acc[k].y), fmaf(w, v.z, acc[k].z), fmaf(w, v.w, acc[k].w));
+            }
+        }
+        const float inv = 1.f / sum;
+        uint16_t *out = p.out + (s.first + tok) * p.out_stride + head * D;
 #pragma unroll
         for (int k = 0; k < kQuads; ++k) {
-            const float4 v = reinterpret_cast<const float4 *>(q)[(size_t)(c0 + 16 * k) * kPfRows + row];
-            acc[k] = make_float4(fmaf(w, v.x, acc[k].x), fmaf(w, v.y, acc[k].y), fmaf(w, v.z, acc[k].z), fmaf(w, v.w, acc[k].w));
+            *reinterpret_cast<uint2 *>(out + 4 * (c0 + 16 * k)) =
+                sum == 0.f ? make_uint2(0, 0)
+                           : make_uint2(pack2<BF16>(acc[k].x * inv, acc[k].y * inv), pack2<BF16>(acc[k].z * inv, acc[k].w * inv));
+            strange = fmaf(acc[k].x, 0.f, fmaf(acc[k].y, 0.f, fmaf(acc[k].z, 0.f, fmaf(acc[k].w, 0.f, strange))));
         }
+        if (p.lse && c0 == 0)
+            p.lse[(int64_t)(s.first + tok) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
-    const float inv = 1.f / sum;
-    uint16_t *out = p.out + (s.first + tok) * p.out_stride + head * D;
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k)
-        *reinterpret_cast<uint2 *>(out + 4 * (c0 + 16 * k)) =
-            sum == 0.f ? make_uint2(0, 0)
-                       : make_uint2(pack2<BF16>(acc[k].x * inv, acc[k].y * inv), pack2<BF16>(acc[k].z * inv, acc[k].w * inv));
-    if (p.lse && c0 == 0) p.lse[(int64_t)(s.first + tok) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    if (!__syncthreads_or(strange != strange)) return;
+    if (threadIdx.x < kPfJoinRows) odd[threadIdx.x] = 0;
+    __syncthreads();
+    if (strange != strange) odd[r] = 1;
+    __syncthreads();
+    for (int x = threadIdx.x >> 5; x < kPfJoinRows; x += 8) {
+        if (!odd[x]) continue;
+        int g2;
+        const int t2 = p.by_group.div(it.mt * kPfRows + blockIdx.y * kPfJoinRows + x, g2);
+        exact_row<D, BF16>(p, it.b, s.len - s.n + t2, s.len, s.prefix, s.first + t2, it.h * p.group + g2, threadIdx.x & 31);
+    }
 }
 
 size_t prefill_part_bytes(int head_dim)

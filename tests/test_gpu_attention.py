@@ -256,6 +256,42 @@ def test_caps_far_below_and_around_the_scores(mc, dim, dtype, cap, spread):
         ref.assert_attention(out, lse, want, dtype, 520, 5.0)
 
 
+@pytest.mark.parametrize("dim,dtype,lens,new,heads,kv,window", [
+    (128, "bf16", [40, 300], [6, 3], 4, 2, 0),         # few rows: decode kernel
+    (64, "fp16", [9000], [5], 2, 1, 100),              # the same, over pages that a window has left behind
+    (64, "bf16", [9000], [5], 2, 1, 0),                # the same, split and joined
+    (128, "bf16", [300, 130], [200, 130], 4, 2, 0),    # many rows
+    (64, "fp16", [300, 700], [300, 64], 3, 1, 40),
+    (128, "fp16", [5000], [100], 2, 1, 0),             # many rows, split and joined
+])
+def test_hidden_infinities_and_nan_stay_hidden(mc, dim, dtype, lens, new, heads, kv, window):
+    """NaN and infinities in keys and values that some queries see and others do not: rows that
+    do not see them are as if they were zero, rows that do are what the definition makes of them."""
+    B = ref.Batch(lens, new, kv, 16, dim, dtype, 41)
+    q = B.randn(B.tokens, heads, dim)
+    planted = []
+    for b, (n, length) in enumerate(zip(new, lens)):
+        for at, what, col in ((length - 1, float("nan"), 3), (length - 2, float("inf"), 7)):
+            B.v[B.table[b, at // 16], :, at % 16, col] = what
+            planted.append((b, at, col, what))
+        if window:  # a key that the window has left behind (the batch that starts at 0: seen by its first queries)
+            B.v[B.table[b, 0], :, 0, :] = float("nan")
+            B.k[B.table[b, 0], :, 0, :] = float("nan")
+    want = ref.attention(B, q, dim ** -0.5, window=window)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, heads)
+    got, lse = mc.attn_prefill(cache, batch, q.cuda(), window=window, with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    got = got.double().cpu()
+    odd = ~torch.isfinite(want[0])
+    assert odd.any() and torch.equal(torch.isnan(got), torch.isnan(want[0]))
+    assert torch.equal(got[odd & ~torch.isnan(got)], want[0][odd & ~torch.isnan(got)])
+    h = ref.HALF_ULP[dtype]
+    tol = (2 * h + 1e-4) * torch.nan_to_num(want[2], posinf=0) + 1e-30 + (2.0 ** -24 + max(lens) * 2.0 ** -25 * 5 if dtype == "fp16" else 0)
+    assert ((got - want[0]).abs() <= tol)[~odd].all()
+    assert torch.allclose(lse.double().cpu(), want[1], rtol=1e-4, atol=1e-4, equal_nan=True)
+
+
 # ----------------------------------------------------------- streams, status --
 
 def test_on_another_stream_and_in_a_graph(mc):
@@ -282,6 +318,24 @@ def test_on_another_stream_and_in_a_graph(mc):
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(res, want)
+
+
+def test_pages_behind_the_window_may_be_gone(mc):
+    """Their table entries are not read and their rows not looked at."""
+    for new, heads, cap in ((1, 4, 0.0), (4, 4, 0.0), (1, 32, 0.0), (150, 4, 0.0), (150, 4, 20.0)):
+        B = ref.Batch([700, 333], [new, new], 2, 16, 64, "bf16", 51)
+        q = B.randn(B.tokens, heads, 64)
+        want = ref.attention(B, q, 0.125, cap, 100)
+        for b, length in enumerate(B.lens):
+            gone = max(0, length - new - 100 + 1) // 16
+            B.v[B.table[b, :gone].long()] = float("nan")
+            B.k[B.table[b, :gone].long()] = float("nan")
+            B.table[b, :gone] = -1
+        cache, batch = B.device(mc)
+        ws = mc.attn_workspace(cache, heads)
+        out, lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=cap, window=100, with_lse=True, workspace=ws)
+        mc.check_status(ws)
+        ref.assert_attention(out, lse, want, "bf16", 700, 5.0)
 
 
 def test_bad_pages_lengths_and_positions_are_reported(mc):
