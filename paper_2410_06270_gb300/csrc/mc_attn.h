@@ -246,10 +246,25 @@ __device__ __forceinline__ float rcp(float x)
     return r;
 }
 
-// top * tanh(x / 2 log2 e), as top - 2 top / (1 + 2^x): off by a few units of fp32 of the
-// cap (tanh.approx, at 2^-11, would move a score of 20 by 0.01, a probability by 1 %).  2^x
-// may overflow to infinity: the quotient is then 0.
-__device__ __forceinline__ float capped(float x, float top) { return fmaf(rcp(1.f + ex2(x)), -2.f * top, top); }
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// top * tanh(x / 2 log2 e), as top - 2 top / (1 + 2^x): off by a few units of fp32 of the cap
+// (tanh.approx, at 2^-11, would move a score of 20 by 0.01, a probability by 1 %).  x stops at
+// 60, where tanh is 1.
+__device__ __forceinline__ float capped(float x, float top) { return fmaf(rcp(1.f + ex2(min_nan(x, 60.f))), -2.f * top, top); }
+// Two scores, one reciprocal for both (that of the denominators' product).  A NaN in either
+// makes both NaN.
+__device__ __forceinline__ void capped2(float &x, float &y, float top)
+{
+    const float a = 1.f + ex2(min_nan(x, 60.f)), b = 1.f + ex2(min_nan(y, 60.f)), r = -2.f * top * rcp(a * b);
+    x = fmaf(r, b, top);
+    y = fmaf(r, a, top);
+}
 
 int launch_append(AppendParams p, int head_dim, bool bf16, cudaStream_t st);
 

@@ -365,33 +365,34 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 
 // row sees, where `masked`.
 template <bool BF16, int MODE>
 __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, uint32_t o_tmem, int D, bool masked, int lo,
-                                           int hi, float c, float cap, float slope, float at0, bool fresh, float &m, float &l)
+                                           int hi, float c, float cap, bool biased, float slope, float at0, bool fresh, float &m, float &l)
 {
-    if (MODE != kPfPlain) {
+    if (MODE == kPfCap) {
+#pragma unroll
+        for (int i = 0; i < 128; i += 2) {
+            float a, b;
+            unpair2(mul2(pair2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), pair2(c, c)), a, b);
+            capped2(a, b, cap);
+            s[i] = __float_as_uint(a);
+            s[i + 1] = __float_as_uint(b);
+        }
+        c = 1.f;
+    }
+    if (MODE == kPfBias || (MODE == kPfCap && biased)) {
         // the bias is slope * (at0 + i): the distance counts up exactly, two keys at a time;
         // without a cap it is brought to the scores' units, so that c applies to both
         uint64_t at = pair2(at0, at0 + 1.f);
         const uint64_t two = pair2(2.f, 2.f);
         const float sl = MODE == kPfBias ? slope / c : slope;
-        const uint64_t sl2 = pair2(sl, sl), c2 = pair2(c, c), top2 = pair2(cap, cap), down2 = pair2(-2.f * cap, -2.f * cap);
+        const uint64_t sl2 = pair2(sl, sl);
 #pragma unroll
         for (int i = 0; i < 128; i += 2) {
-            uint64_t x = pair2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
             float a, b;
-            if (MODE == kPfCap) {
-                unpair2(mul2(x, c2), a, b);
-                const uint64_t y = add2(pair2(ex2(a), ex2(b)), pair2(1.f, 1.f));  // capped()
-                unpair2(y, a, b);
-                x = fma2(pair2(rcp(a), rcp(b)), down2, fma2(sl2, at, top2));
-            } else {
-                x = fma2(sl2, at, x);
-            }
+            unpair2(fma2(sl2, at, pair2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]))), a, b);
             at = add2(at, two);
-            unpair2(x, a, b);
             s[i] = __float_as_uint(a);
             s[i + 1] = __float_as_uint(b);
         }
-        if (MODE == kPfCap) c = 1.f;
     }
     if (masked) {
 #pragma unroll
@@ -589,8 +590,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         const int slot = it % Sh::kStages;
                         if (it >= Sh::kStages && !(ok = warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh))) break;
                         // values past the sequence's end may be NaN, and a weight of 0 would not
-                        // hide that: their rows are zeroed before the tile is given on
-                        const bool patch = kv && j0 + kPfKeys > at.s.len;
+                        // hide that (nor would a capped key's neighbour): their rows are zeroed
+                        // before the tile is given on
+                        const bool patch = (kv || MODE == kPfCap) && j0 + kPfKeys > at.s.len;
                         uint64_t *bar = patch ? &sh->vpatch : &sh->kfull[slot];
                         if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
                         __syncwarp();
@@ -836,7 +838,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 #pragma unroll
                         for (int q = 1; q < 4; ++q) pf_tie(s + 32 * q);
                         pf_softmax<BF16, MODE>(s, s_tmem, o_tmem, D, j0 < all_lo || j0 + kPfKeys > all_hi, lo - j0, hi - j0, p.scale,
-                                                p.cap, slope, (float)(j0 - pos), u == at.u, m, l);
+                                                p.cap, p.slopes != nullptr, slope, (float)(j0 - pos), u == at.u, m, l);
                         tmem_st_wait();
                     }
                     tc_fence_before();
