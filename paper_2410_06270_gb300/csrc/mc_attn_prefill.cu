@@ -50,6 +50,7 @@ struct PfShared {
     volatile int abort;
     int b[2], h[2], mt[2], u[2];                         // where this CTA's run starts and ends
     int off;                                             // the end's cost offset in its item
+    int run;                                             // cost of a run
     int64_t total;                                       // cost of the batch
     int sums[2][32];
 };
@@ -195,6 +196,27 @@ __device__ __forceinline__ PfRun pf_run(const AttnParams &p, const volatile PfSh
     }
     return {sh->b[1], sh->h[1], sh->mt[1], sh->u[1]};
 }
+
+// The order in which a run takes an item's units.  Runs of one key head start at different
+// places of a long cache; if each went straight on, a unit would be read for one row tile now
+// and for the next ones a large part of the call later, when L2 has lost it.  An item longer
+// than a run's cost R is started at the unit that is `spent` modulo R, spent the cost since the
+// run's start, and taken round: all runs are then at the same units modulo R at the same time.
+// 509 tokens over 30000 keys of 8 heads, 8 row tiles a head: 190 -> 167 us, 1024 over 60000 758 ->
+// 653.  Where the sequence's cache stays in L2 it goes straight on: 300 tokens over 120000 keys of
+// one head (61 MB) 190 us, taken round 200.
+constexpr int64_t kPfL2 = 64 << 20;
+struct PfOrder {
+    int first, n, shift;
+    __device__ __forceinline__ PfOrder(const AttnParams &p, int D, const PfPlace &at, int n_, int run, int spent)
+        : first(at.u), n(n_), shift(0)
+    {
+        if (at.k.units <= run || (int64_t)at.s.len * p.c.kv_heads * D * 4 <= kPfL2) return;
+        const int ahead = (spent - at.u) % run, to = ahead < 0 ? ahead + run : ahead;
+        if (to < n) shift = to;
+    }
+    __device__ __forceinline__ int unit(int i) const { return first + (i + shift < n ? i + shift : i + shift - n); }
+};
 
 // Units of the item at hand that belong to the run; 0: the run is over.
 __device__ __forceinline__ int pf_units(const PfRun &r, const PfPlace &at)
@@ -546,6 +568,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             if (warp) {
                 sh->total = total;
                 sh->off = off;
+                sh->run = max(1, (int)div64(total, max(ctas, (int64_t)1)));
             }
         }
     }
@@ -575,10 +598,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
                 return lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j)) : -1;
             };
+            int spent = 0;
             while (ok && (n = pf_units(run, at)) > 0) {
-                int page = pages(at.u);
-                for (int u = at.u; ok && u < at.u + n; ++u) {
-                    const int next = u + 1 < at.u + n ? pages(u + 1) : -1;  // used a unit later
+                const PfOrder order(p, D, at, n, sh->run, spent);
+                int page = pages(order.unit(0));
+                for (int i = 0; ok && i < n; ++i) {
+                    const int u = order.unit(i), next = i + 1 < n ? pages(order.unit(i + 1)) : -1;  // used a unit later
                     const int j0 = at.k.base + u * kPfKeys, j = j0 + lane * pp.box_rows;
                     int row;
                     p.c.page.div(j, row);
@@ -618,6 +643,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                     page = next;
                 }
                 if (at.u + n < at.k.units) break;
+                spent += n + kPfItemCost;
                 pf_next_item(p, at);
             }
             // the last copies land before the block's shared memory is given back, on an abort too
@@ -807,7 +833,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
         const uint32_t lanes = (uint32_t)(wt * 32) << 16;
         const uint32_t s_tmem = lanes + 128 * t, o_tmem = lanes + 256 + 128 * t;
-        int su = 0, ou = 0, n;
+        int su = 0, ou = 0, spent = 0, n;
         bool ok = true, tail = false;
         while (ok && (n = pf_units(run, at)) > 0) {
             const int rows0 = at.mt * kPfRows + t * kPfTile, rows = min(kPfTile, at.s.n * p.group - rows0);
@@ -825,12 +851,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 const int all_lo = p.window ? p_last - p.window + 1 : 0;
                 const float slope = MODE != kPfPlain && p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
                 float m = -INFINITY, l = 0.f;
-                for (int u = at.u; u < at.u + n; ++u) {
+                const PfOrder order(p, D, at, n, sh->run, spent);
+                for (int i = 0; i < n; ++i) {
                     if (!(ok = warp_wait(&sh->sfull[t], su & 1, pp, sh))) break;
                     ++su;
                     tc_fence_after();
                     if (wt * 32 < rows) {
-                        const int j0 = at.k.base + u * kPfKeys;
+                        const int j0 = at.k.base + order.unit(i) * kPfKeys;
                         uint32_t s[128];
 #pragma unroll
                         for (int q = 0; q < 4; ++q) pf_ld32(s_tmem + 32 * q, s + 32 * q);
@@ -838,7 +865,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 #pragma unroll
                         for (int q = 1; q < 4; ++q) pf_tie(s + 32 * q);
                         pf_softmax<BF16, MODE>(s, s_tmem, o_tmem, D, j0 < all_lo || j0 + kPfKeys > all_hi, lo - j0, hi - j0, p.scale,
-                                                p.cap, p.slopes != nullptr, slope, (float)(j0 - pos), u == at.u, m, l);
+                                                p.cap, p.slopes != nullptr, slope, (float)(j0 - pos), i == 0, m, l);
                         tmem_st_wait();
                     }
                     tc_fence_before();
@@ -907,6 +934,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 }
             }
             if (at.u + n < at.k.units) break;
+            spent += n + kPfItemCost;
             pf_next_item(p, at);
         }
         if (!tail && tid == 0) pp.open[blockIdx.x].pieces = 0;

@@ -128,7 +128,8 @@ def test_decode_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap,
     ref.assert_attention(out, lse, want, dtype, max(EDGES), 5.0)
 
 
-@pytest.mark.parametrize("seqs,length,kv,heads", [(1, 5000, 1, 8), (1, 20011, 2, 8), (3, 2049, 8, 32), (300, 40, 1, 2), (1, 1, 1, 1)])
+@pytest.mark.parametrize("seqs,length,kv,heads", [(1, 5000, 1, 8), (1, 20011, 2, 8), (3, 2049, 8, 32), (300, 40, 1, 2), (1, 1, 1, 1),
+                                                   (70, 900, 2, 8), (128, 129, 1, 16)])
 def test_decode_splits_and_joins(mc, seqs, length, kv, heads):
     lens = [max(1, length - 37 * b) if seqs < 100 else (b * 7) % length for b in range(seqs)]
     B = ref.Batch(lens, [1] * seqs, kv, 32, 128, "bf16", 8)
@@ -230,6 +231,45 @@ def test_prefill_splits_and_joins(mc, new, length, kv, heads, dim):
     ref.assert_attention(out, lse, want, "bf16", length, 5.0)
     again, _ = mc.attn_prefill(cache, batch, q.cuda(), with_lse=True)
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("softcap,window", [(0.0, 0), (20.0, 60000)])
+def test_prefill_of_a_chunk_over_a_cache_beyond_l2(mc, softcap, window):
+    """A cache of 80 MB, read by several row tiles a head: the units are taken in another order."""
+    B = ref.Batch([80000], [200], 2, 256, 128, "bf16", 17)
+    q = B.randn(200, 8, 128)
+    cache, batch = B.device(mc)
+    out, lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=softcap, window=window, with_lse=True)
+    some = [0, 1, 63, 64, 130, 199]  # rows of every tile
+    C = ref.Batch([80000], [200], 2, 256, 128, "bf16", 17)
+    C.new, C.cu, want = [1], [0, 1], []
+    for i in some:
+        C.lens = [80000 - 200 + i + 1]
+        want.append(ref.attention(C, q[i:i + 1], 128 ** -0.5, softcap, window))
+    want = tuple(torch.cat(x) for x in zip(*want))
+    ref.assert_attention(out[some], lse[some], want, "bf16", 80000, 5.0)
+
+
+@pytest.mark.parametrize("seqs,heads,kv", [(45, 16, 1), (70, 40, 1)])
+def test_prefill_of_many_sequences(mc, seqs, heads, kv):
+    """More sequences than a warp has lanes, some without tokens, some without keys."""
+    new = [(5 * b) % 23 for b in range(seqs)]
+    lens = [0 if b % 11 == 4 else new[b] + (37 * b) % 300 for b in range(seqs)]
+    B = ref.Batch(lens, new, kv, 16, 64, "bf16", 61, pad_tokens=1)
+    q = B.randn(B.tokens, heads, 64)
+    want = ref.attention(B, q, 0.125)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, heads)
+    out, lse = mc.attn_prefill(cache, batch, q.cuda(), with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    ref.assert_attention(out, lse, want, "bf16", 400, 5.0, rows=slice(0, B.cu[-1]))
+    # and the append of as many, then the same attention over what it wrote
+    x = B.randn(3, B.tokens, kv, 64)
+    full = ref.append(B, q, x[0], x[1])
+    mc.kv_append(cache, batch, q.cuda(), x[0].cuda(), x[1].cuda(), workspace=ws)
+    mc.check_status(ws)
+    assert torch.equal(torch.nan_to_num(cache.k.double().cpu()), torch.nan_to_num(full[1]))
+    assert torch.equal(torch.nan_to_num(cache.v.double().cpu()), torch.nan_to_num(full[2]))
 
 
 def test_prefill_of_one_token_each_is_decode(mc):
