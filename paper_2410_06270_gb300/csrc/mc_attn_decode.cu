@@ -5,11 +5,21 @@
 // for a group of query heads, 4 head_dim bytes for 4 head_dim group flops: bound by HBM, so
 // the design is about keeping loads in flight on every SM whatever the lengths are.
 //
-// Work is cut into units of 64 (heads of 64: 128) keys of one (sequence, key head); the units of the whole
-// batch, in order, are dealt to the CTAs as contiguous runs of equal cost, which each CTA finds from
-// the lengths by itself (no host knowledge of them, so a captured graph serves any).  A run
-// that ends inside an item leaves a partial result (m, l, o in fp32); join_kernel adds the
-// pieces of an item in their order.  At most two partials per CTA, whatever the batch.
+// Work is cut into units of 64 (heads of 64: 128) keys of one (sequence, key head); the units of
+// the whole batch, in order, are dealt to the CTAs as contiguous runs of equal cost, which each
+// CTA finds from the lengths by itself (no host knowledge of them, so a captured graph serves
+// any).  A run that ends inside an item leaves a partial result (m, l, o in fp32); join_kernel
+// adds the pieces of an item in their order.  At most two partials per CTA, whatever the batch.
+// Each warp streams its own 16 or 32 keys of a unit through a ring of its own (three stages of 8
+// KB, two CTAs an SM: 128 KB in flight), so the main loop has no block barrier.
+//
+// More rows than a group's heads (a few new tokens per sequence, with causal, window and prefix
+// masks row by row) are further columns of the same products, up to 32.
+//
+// Measured: 64 sequences of 8192 keys, 32 heads on 8 of 128, 311 us, 6.9 TB/s of keys and values
+// (1.02 of the measured copy rate); one of 131071 keys 83 us, 6.4 TB/s; DRAM bytes 537.1 MB for 536.9
+// (ncu, 16 x 8192).  Short ones are bound by latency: 777 keys 7.4 us, of which the schedule 1, the
+// first keys 1.5, the join and its launch 3.
 #include <math.h>
 
 #include "mc_attn.h"

@@ -19,6 +19,14 @@
 // This splits a long cache over the SMs when there are few rows, and balances the causal
 // triangle, by the same rule.
 //
+// What bounds it: a unit's 32 MMAs are 2048 cycles of the tensor pipe; it takes 2830, as QK^T with
+// both operands in shared memory runs at 78 cycles an MMA (8 KB each, all that shared memory
+// gives in 64), PV with P in tensor memory at 65, and the change of tiles costs the rest; the
+// softmax's 575 instructions a warp (1160 cycles) run beside it.  A prompt of 8192 tokens, 32 heads
+// on 8 of 128: 376 us, 1.46 PFLOP/s of the visible pairs, 0.77 of cuBLAS's burst rate and 0.86 of its
+// sustained one (at the power cap; 358 us in a short burst).  Capped scores take twice the time
+// (2^x and a reciprocal each: 223 us at 4096 tokens, 115 without).
+//
 // Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 and 9 issue a tile's MMAs,
 // 10 copies keys and values (TMA, a box per page and 64 columns), 11 the queries (TMA where a
 // tile is whole tokens of the group's heads, else cp.async).
@@ -581,250 +589,250 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         sh->abort = 1;
     }
     if (warp >= kPfMma) {
-      pf_give_regs();  // one instruction for the warpgroup
-      if (warp >= kPfKv) {
-        // -------------------------------------------------------------- copies --
-        PfPlace at;
-        const PfRun run = pf_run(p, sh, at);
-        const uint32_t smem0 = smem_u32(smem);
-        if (warp == kPfKv) {
-            // keys and values: lane i copies the i-th box (of a page) of a tile.  A page that is
-            // not there, and boxes before the first key or past the last, are read beyond the map:
-            // zeros.
-            const int boxes = kPfKeys / pp.box_rows;
-            int it = 0, patches = 0, n;
-            bool ok = !(pp.debug & kDebugNoProducer);
-            auto pages = [&](int u) {
-                const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
-                return lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j)) : -1;
-            };
-            int spent = 0;
-            while (ok && (n = pf_units(run, at)) > 0) {
-                const PfOrder order(p, D, at, n, sh->run, spent);
-                int page = pages(order.unit(0));
-                for (int i = 0; ok && i < n; ++i) {
-                    const int u = order.unit(i), next = i + 1 < n ? pages(order.unit(i + 1)) : -1;  // used a unit later
-                    const int j0 = at.k.base + u * kPfKeys, j = j0 + lane * pp.box_rows;
-                    int row;
-                    p.c.page.div(j, row);
-                    if ((unsigned)page >= (unsigned)p.c.num_pages) {
-                        if (lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first) set_status(p.status, MC_ERR_RANGE);
-                        page = p.c.num_pages;
-                    }
-                    for (int kv = 0; kv < 2; ++kv, ++it) {
-                        const int slot = it % Sh::kStages;
-                        if (it >= Sh::kStages && !(ok = warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh))) break;
-                        // values past the sequence's end may be NaN, and a weight of 0 would not
-                        // hide that (nor would a capped key's neighbour): their rows are zeroed
-                        // before the tile is given on
-                        const bool patch = (kv || MODE == kPfCap) && j0 + kPfKeys > at.s.len;
-                        uint64_t *bar = patch ? &sh->vpatch : &sh->kfull[slot];
-                        if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
-                        __syncwarp();
-                        if (lane < boxes) {
-                            const uint32_t dst = smem0 + Sh::kRing + slot * Sh::kTileBytes + lane * pp.box_rows * 128;
-#pragma unroll
-                            for (int h = 0; h < D / 64; ++h)
-                                pf_tma(dst + h * Sh::kHalf, kv ? &vmap : &kmap, 64 * h, row, at.h, page, bar);
+        pf_give_regs();  // one instruction for the warpgroup
+        if (warp >= kPfKv) {
+            // -------------------------------------------------------------- copies --
+            PfPlace at;
+            const PfRun run = pf_run(p, sh, at);
+            const uint32_t smem0 = smem_u32(smem);
+            if (warp == kPfKv) {
+                // keys and values: lane i copies the i-th box (of a page) of a tile.  A page that is
+                // not there, and boxes before the first key or past the last, are read beyond the map:
+                // zeros.
+                const int boxes = kPfKeys / pp.box_rows;
+                int it = 0, patches = 0, n;
+                bool ok = !(pp.debug & kDebugNoProducer);
+                auto pages = [&](int u) {
+                    const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
+                    return lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j)) : -1;
+                };
+                int spent = 0;
+                while (ok && (n = pf_units(run, at)) > 0) {
+                    const PfOrder order(p, D, at, n, sh->run, spent);
+                    int page = pages(order.unit(0));
+                    for (int i = 0; ok && i < n; ++i) {
+                        const int u = order.unit(i), next = i + 1 < n ? pages(order.unit(i + 1)) : -1;  // used a unit later
+                        const int j0 = at.k.base + u * kPfKeys, j = j0 + lane * pp.box_rows;
+                        int row;
+                        p.c.page.div(j, row);
+                        if ((unsigned)page >= (unsigned)p.c.num_pages) {
+                            if (lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first) set_status(p.status, MC_ERR_RANGE);
+                            page = p.c.num_pages;
                         }
-                        if (patch) {
-                            if (!(ok = warp_wait(&sh->vpatch, patches++ & 1, pp, sh))) break;
-                            const int from = max(0, at.s.len - j0);
-                            for (int i = from * 8 + lane; i < kPfKeys * 8; i += 32)
+                        for (int kv = 0; kv < 2; ++kv, ++it) {
+                            const int slot = it % Sh::kStages;
+                            if (it >= Sh::kStages && !(ok = warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh))) break;
+                            // values past the sequence's end may be NaN, and a weight of 0 would not
+                            // hide that (nor would a capped key's neighbour): their rows are zeroed
+                            // before the tile is given on
+                            const bool patch = (kv || MODE == kPfCap) && j0 + kPfKeys > at.s.len;
+                            uint64_t *bar = patch ? &sh->vpatch : &sh->kfull[slot];
+                            if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
+                            __syncwarp();
+                            if (lane < boxes) {
+                                const uint32_t dst = smem0 + Sh::kRing + slot * Sh::kTileBytes + lane * pp.box_rows * 128;
 #pragma unroll
                                 for (int h = 0; h < D / 64; ++h)
-                                    *reinterpret_cast<uint4 *>(smem + Sh::kRing + slot * Sh::kTileBytes + h * Sh::kHalf + i * 16) =
-                                        make_uint4(0, 0, 0, 0);
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&sh->kfull[slot]);
-                        }
-                    }
-                    page = next;
-                }
-                if (at.u + n < at.k.units) break;
-                spent += n + kPfItemCost;
-                pf_next_item(p, at);
-            }
-            // the last copies land before the block's shared memory is given back, on an abort too
-            const uint64_t t0 = globaltimer_ns();
-            for (int i = max(0, it - Sh::kStages); i < it; ++i)
-                while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1)))
-                    if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
-            pdl_trigger();
-        } else {
-            // queries, a tile as soon as the last item's has been read
-            constexpr int kChunks = D / 8, kPer = 32 / kChunks, kQStep = kPer;
-            const int lc = lane % kChunks, lr = lane / kChunks;
-            const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
-            const int step_hg = kQStep % p.group;
-            const int64_t q_step = kQStep / p.group * p.q_stride + step_hg * D, q_wrap = p.q_stride - p.group * D;
-            int uses[2] = {0, 0}, n;
-            bool ok = !(pp.debug & kDebugNoProducer);
-            while (ok && (n = pf_units(run, at)) > 0) {
-                const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
-                for (int t = 0; t < 2 && t * kPfTile < rows; ++t) {
-                    if (uses[t] && !(ok = warp_wait(&sh->qempty[t], (uses[t] + 1) & 1, pp, sh))) break;
-                    ++uses[t];
-                    const uint32_t tile = smem0 + Sh::kHdr + t * Sh::kTileBytes;
-                    if (pp.q_boxes) {
-                        // rows past the sequence's last are other tokens', or zeros: not stored
-                        if (lane == 0) {
-                            mbar_arrive_expect_tx(&sh->qfull[t], Sh::kTileBytes);
+                                    pf_tma(dst + h * Sh::kHalf, kv ? &vmap : &kmap, 64 * h, row, at.h, page, bar);
+                            }
+                            if (patch) {
+                                if (!(ok = warp_wait(&sh->vpatch, patches++ & 1, pp, sh))) break;
+                                const int from = max(0, at.s.len - j0);
+                                for (int i = from * 8 + lane; i < kPfKeys * 8; i += 32)
 #pragma unroll
-                            for (int h = 0; h < D / 64; ++h)
-                                pf_tma3(tile + h * Sh::kHalf, &qmap, 64 * h, at.h * p.group,
-                                        at.s.first + p.by_group.div(rows0 + t * kPfTile), &sh->qfull[t]);
+                                    for (int h = 0; h < D / 64; ++h)
+                                        *reinterpret_cast<uint4 *>(smem + Sh::kRing + slot * Sh::kTileBytes + h * Sh::kHalf + i * 16) =
+                                            make_uint4(0, 0, 0, 0);
+                                fence_proxy_async_smem();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(&sh->kfull[slot]);
+                            }
                         }
-                        continue;
+                        page = next;
                     }
-                    // one row per kChunks lanes, zeros past the last
-                    int r = t * kPfTile + lr;
-                    int hg;
-                    const int tok = p.by_group.div(rows0 + r, hg);
-                    const uint16_t *src = p.q + (at.s.first + tok) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
-                    for (; r < (t + 1) * kPfTile; r += kQStep) {
-                        const bool real = r < rows;
-                        pf_copy16z((tile + col + (r & 127) * 128) ^ ((r & 7) << 4), real ? src : p.q, real);
-                        src += q_step;
-                        if ((hg += step_hg) >= p.group) {
-                            hg -= p.group;
-                            src += q_wrap;
-                        }
-                    }
-                    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-                    fence_proxy_async_smem();
-                    mbar_arrive(&sh->qfull[t]);
+                    if (at.u + n < at.k.units) break;
+                    spent += n + kPfItemCost;
+                    pf_next_item(p, at);
                 }
-                if (!ok || at.u + n < at.k.units) break;
-                pf_next_item(p, at);
-            }
-            if (pp.q_boxes) {  // the last copies land before the block's shared memory is given back
+                // the last copies land before the block's shared memory is given back, on an abort too
                 const uint64_t t0 = globaltimer_ns();
-                for (int t = 0; t < 2; ++t)
-                    while (uses[t] && !__all_sync(0xffffffffu, mbar_try_wait(&sh->qfull[t], (uses[t] + 1) & 1)))
+                for (int i = max(0, it - Sh::kStages); i < it; ++i)
+                    while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1)))
                         if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
-            }
-        }
-      } else {
-        // ---------------------------------------------------------------- MMAs --
-        PfPlace at;
-        const PfRun run = pf_run(p, sh, at);
-        constexpr uint32_t kIdS = pf_idesc(BF16, kPfKeys, false), kIdO = pf_idesc(BF16, D, true);
-        const uint32_t q0 = pf_desc_k(smem_u32(smem + Sh::kHdr)), k0 = pf_desc_k(smem_u32(smem + Sh::kRing));
-        const uint32_t v0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
-        constexpr uint32_t kStep = Sh::kTileBytes >> 4;
-        int uses = 0, quses = 0;
-        bool ok = true;
-        auto qk = [&](int t, int slot) {  // S_t = Q_t K^T
-            const uint32_t a = q0 + t * kStep, b = k0 + slot * kStep;
+                pdl_trigger();
+            } else {
+                // queries, a tile as soon as the last item's has been read
+                constexpr int kChunks = D / 8, kPer = 32 / kChunks, kQStep = kPer;
+                const int lc = lane % kChunks, lr = lane / kChunks;
+                const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
+                const int step_hg = kQStep % p.group;
+                const int64_t q_step = kQStep / p.group * p.q_stride + step_hg * D, q_wrap = p.q_stride - p.group * D;
+                int uses[2] = {0, 0}, n;
+                bool ok = !(pp.debug & kDebugNoProducer);
+                while (ok && (n = pf_units(run, at)) > 0) {
+                    const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
+                    for (int t = 0; t < 2 && t * kPfTile < rows; ++t) {
+                        if (uses[t] && !(ok = warp_wait(&sh->qempty[t], (uses[t] + 1) & 1, pp, sh))) break;
+                        ++uses[t];
+                        const uint32_t tile = smem0 + Sh::kHdr + t * Sh::kTileBytes;
+                        if (pp.q_boxes) {
+                            // rows past the sequence's last are other tokens', or zeros: not stored
+                            if (lane == 0) {
+                                mbar_arrive_expect_tx(&sh->qfull[t], Sh::kTileBytes);
 #pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                const uint32_t o = (s >> 2) * (Sh::kHalf >> 4) + (s & 3) * 2;
-                pf_mma_ss(128 * t, a + o, b + o, kIdS, s > 0);
+                                for (int h = 0; h < D / 64; ++h)
+                                    pf_tma3(tile + h * Sh::kHalf, &qmap, 64 * h, at.h * p.group,
+                                            at.s.first + p.by_group.div(rows0 + t * kPfTile), &sh->qfull[t]);
+                            }
+                            continue;
+                        }
+                        // one row per kChunks lanes, zeros past the last
+                        int r = t * kPfTile + lr;
+                        int hg;
+                        const int tok = p.by_group.div(rows0 + r, hg);
+                        const uint16_t *src = p.q + (at.s.first + tok) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
+                        for (; r < (t + 1) * kPfTile; r += kQStep) {
+                            const bool real = r < rows;
+                            pf_copy16z((tile + col + (r & 127) * 128) ^ ((r & 7) << 4), real ? src : p.q, real);
+                            src += q_step;
+                            if ((hg += step_hg) >= p.group) {
+                                hg -= p.group;
+                                src += q_wrap;
+                            }
+                        }
+                        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+                        fence_proxy_async_smem();
+                        mbar_arrive(&sh->qfull[t]);
+                    }
+                    if (!ok || at.u + n < at.k.units) break;
+                    pf_next_item(p, at);
+                }
+                if (pp.q_boxes) {  // the last copies land before the block's shared memory is given back
+                    const uint64_t t0 = globaltimer_ns();
+                    for (int t = 0; t < 2; ++t)
+                        while (uses[t] && !__all_sync(0xffffffffu, mbar_try_wait(&sh->qfull[t], (uses[t] + 1) & 1)))
+                            if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
+                }
             }
-        };
-        auto pv = [&](int t, int slot, bool first) {  // O_t (+)= P_t V
-            const uint32_t b = v0 + slot * kStep;
+        } else {
+            // ---------------------------------------------------------------- MMAs --
+            PfPlace at;
+            const PfRun run = pf_run(p, sh, at);
+            constexpr uint32_t kIdS = pf_idesc(BF16, kPfKeys, false), kIdO = pf_idesc(BF16, D, true);
+            const uint32_t q0 = pf_desc_k(smem_u32(smem + Sh::kHdr)), k0 = pf_desc_k(smem_u32(smem + Sh::kRing));
+            const uint32_t v0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
+            constexpr uint32_t kStep = Sh::kTileBytes >> 4;
+            int uses = 0, quses = 0;
+            bool ok = true;
+            auto qk = [&](int t, int slot) {  // S_t = Q_t K^T
+                const uint32_t a = q0 + t * kStep, b = k0 + slot * kStep;
 #pragma unroll
-            for (int s = 0; s < kPfKeys / 16; ++s) pf_mma_ts(256 + 128 * t, 128 * t + 8 * s, b + s * (2048 >> 4), kIdO, !first || s > 0);
-        };
-        struct Slot {
-            int i;
-            uint32_t phase;
-            __device__ Slot next() const { return i + 1 == Sh::kStages ? Slot{0, phase ^ 1u} : Slot{i + 1, phase}; }
-        };
-        auto full = [&](const Slot &x) { return warp_wait(&sh->kfull[x.i], x.phase, pp, sh); };
-        auto tiles_of = [&](const PfPlace &a) { return a.s.n * p.group - a.mt * kPfRows > kPfTile ? 2 : 1; };
-        // Unit j's PV of the tile is followed by unit j + 1's QK of it, the next item's first one
-        // after the last: the next queries and the other tile's softmax hide the change of item.
-        // A warp for each tile: their waits do not add up, and either's MMAs fill the pipe.
-        const int t = warp - kPfMma;
-        Slot k = {0, 0};  // of the last keys that QK was issued for
-        int n = pf_units(run, at), tiles = n > 0 ? tiles_of(at) : 0;
-        // a ring slot that this warp has no MMA for (the item has one tile) is given back at once
-        auto pass = [&](const Slot &x) {
-            if (lane == 0) mbar_arrive(&sh->kempty[x.i]);
-        };
-        auto first_qk = [&](const Slot &x, bool last_unit) {
-            if (!warp_wait(&sh->qfull[t], quses++ & 1, pp, sh)) return false;
-            tc_fence_after();
-            if (elect_one()) {
-                qk(t, x.i);
-                umma_commit(&sh->sfull[t]);
-                umma_commit(&sh->kempty[x.i]);
-                if (last_unit) umma_commit(&sh->qempty[t]);
+                for (int s = 0; s < D / 16; ++s) {
+                    const uint32_t o = (s >> 2) * (Sh::kHalf >> 4) + (s & 3) * 2;
+                    pf_mma_ss(128 * t, a + o, b + o, kIdS, s > 0);
+                }
+            };
+            auto pv = [&](int t, int slot, bool first) {  // O_t (+)= P_t V
+                const uint32_t b = v0 + slot * kStep;
+#pragma unroll
+                for (int s = 0; s < kPfKeys / 16; ++s) pf_mma_ts(256 + 128 * t, 128 * t + 8 * s, b + s * (2048 >> 4), kIdO, !first || s > 0);
+            };
+            struct Slot {
+                int i;
+                uint32_t phase;
+                __device__ Slot next() const { return i + 1 == Sh::kStages ? Slot{0, phase ^ 1u} : Slot{i + 1, phase}; }
+            };
+            auto full = [&](const Slot &x) { return warp_wait(&sh->kfull[x.i], x.phase, pp, sh); };
+            auto tiles_of = [&](const PfPlace &a) { return a.s.n * p.group - a.mt * kPfRows > kPfTile ? 2 : 1; };
+            // Unit j's PV of the tile is followed by unit j + 1's QK of it, the next item's first one
+            // after the last: the next queries and the other tile's softmax hide the change of item.
+            // A warp for each tile: their waits do not add up, and either's MMAs fill the pipe.
+            const int t = warp - kPfMma;
+            Slot k = {0, 0};  // of the last keys that QK was issued for
+            int n = pf_units(run, at), tiles = n > 0 ? tiles_of(at) : 0;
+            // a ring slot that this warp has no MMA for (the item has one tile) is given back at once
+            auto pass = [&](const Slot &x) {
+                if (lane == 0) mbar_arrive(&sh->kempty[x.i]);
+            };
+            auto first_qk = [&](const Slot &x, bool last_unit) {
+                if (!warp_wait(&sh->qfull[t], quses++ & 1, pp, sh)) return false;
+                tc_fence_after();
+                if (elect_one()) {
+                    qk(t, x.i);
+                    umma_commit(&sh->sfull[t]);
+                    umma_commit(&sh->kempty[x.i]);
+                    if (last_unit) umma_commit(&sh->qempty[t]);
+                }
+                __syncwarp();
+                return true;
+            };
+            if (n > 0 && (ok = full(k))) {
+                if (t < tiles) ok = first_qk(k, n == 1);
+                else pass(k);
             }
-            __syncwarp();
-            return true;
-        };
-        if (n > 0 && (ok = full(k))) {
-            if (t < tiles) ok = first_qk(k, n == 1);
-            else pass(k);
-        }
-        while (ok && n > 0) {
-            PfPlace nx = at;
-            int next_n = 0, next_tiles = 0;
-            if (at.u + n == at.k.units) {
-                pf_next_item(p, nx);
-                next_n = pf_units(run, nx);
-                if (next_n > 0) next_tiles = tiles_of(nx);
-            }
-            // inside the item: unit j's PV and unit j + 1's QK are issued together
-            for (int j = 0; ok && j + 1 < n; ++j) {
-                const Slot v = k.next(), k2 = v.next();
-                if (!(ok = full(v) && full(k2))) break;
+            while (ok && n > 0) {
+                PfPlace nx = at;
+                int next_n = 0, next_tiles = 0;
+                if (at.u + n == at.k.units) {
+                    pf_next_item(p, nx);
+                    next_n = pf_units(run, nx);
+                    if (next_n > 0) next_tiles = tiles_of(nx);
+                }
+                // inside the item: unit j's PV and unit j + 1's QK are issued together
+                for (int j = 0; ok && j + 1 < n; ++j) {
+                    const Slot v = k.next(), k2 = v.next();
+                    if (!(ok = full(v) && full(k2))) break;
+                    if (t < tiles) {
+                        if (!(ok = warp_wait(&sh->pfull[t], uses++ & 1, pp, sh))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            pv(t, v.i, j == 0);
+                            umma_commit(&sh->kempty[v.i]);
+                            qk(t, k2.i);
+                            umma_commit(&sh->sfull[t]);
+                            umma_commit(&sh->kempty[k2.i]);
+                            if (j + 2 == n) umma_commit(&sh->qempty[t]);
+                        }
+                        __syncwarp();
+                    } else {
+                        pass(v);
+                        pass(k2);
+                    }
+                    k = k2;
+                }
+                if (!ok) break;
+                // its last unit's PV, and the next item's first QK
+                const Slot v = k.next();
+                if (!(ok = full(v))) break;
+                k = v.next();
                 if (t < tiles) {
                     if (!(ok = warp_wait(&sh->pfull[t], uses++ & 1, pp, sh))) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        pv(t, v.i, j == 0);
+                        pv(t, v.i, n == 1);
                         umma_commit(&sh->kempty[v.i]);
-                        qk(t, k2.i);
-                        umma_commit(&sh->sfull[t]);
-                        umma_commit(&sh->kempty[k2.i]);
-                        if (j + 2 == n) umma_commit(&sh->qempty[t]);
+                        umma_commit(&sh->ofull[t]);
                     }
                     __syncwarp();
                 } else {
                     pass(v);
-                    pass(k2);
                 }
-                k = k2;
-            }
-            if (!ok) break;
-            // its last unit's PV, and the next item's first QK
-            const Slot v = k.next();
-            if (!(ok = full(v))) break;
-            k = v.next();
-            if (t < tiles) {
-                if (!(ok = warp_wait(&sh->pfull[t], uses++ & 1, pp, sh))) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    pv(t, v.i, n == 1);
-                    umma_commit(&sh->kempty[v.i]);
-                    umma_commit(&sh->ofull[t]);
+                if (next_n > 0) {
+                    if (!(ok = full(k))) break;
+                    if (t < next_tiles) ok = first_qk(k, next_n == 1);
+                    else pass(k);
                 }
-                __syncwarp();
-            } else {
-                pass(v);
+                at = nx;
+                n = next_n;
+                tiles = next_tiles;
             }
-            if (next_n > 0) {
-                if (!(ok = full(k))) break;
-                if (t < next_tiles) ok = first_qk(k, next_n == 1);
-                else pass(k);
-            }
-            at = nx;
-            n = next_n;
-            tiles = next_tiles;
+            // the tensor pipe is idle before shared and tensor memory are given back
+            if (elect_one()) umma_commit(&sh->drain);
+            __syncwarp();
+            const uint64_t t0 = globaltimer_ns();
+            while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->drain, 0)))
+                if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
         }
-        // the tensor pipe is idle before shared and tensor memory are given back
-        if (elect_one()) umma_commit(&sh->drain);
-        __syncwarp();
-        const uint64_t t0 = globaltimer_ns();
-        while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->drain, 0)))
-            if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
-      }
     } else {
         // -------------------------------------------------- softmax and epilogue --
         pf_take_regs();
