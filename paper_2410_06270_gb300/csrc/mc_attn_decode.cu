@@ -83,7 +83,8 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real,
 }
 
 // A sequence's new tokens and the keys [start, len) that any of them sees, as units of
-// keys from `base` on (start rounded down to 16, so that 16 keys lie in one page).  Its rows are (token, head of the group), token-major, in slices.
+// keys from `base` on (start rounded down to 16, so that 16 keys lie in one page).  Its rows
+// are (token, head of the group), token-major, in slices.
 struct Keys {
     int first, n;  // token rows
     int start, len, base, units;
@@ -187,7 +188,8 @@ struct DecShape {
 // O^T += V^T P^T: the 16 keys of a warp fill the rows of the m16n8k16 instruction and the
 // slice's rows its 8 columns, half the instructions and accumulators of the other way.
 template <int D, bool BF16, int NT>
-__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(const AttnParams p, FastDiv by_grid, OpenItem *open, float *part)
+__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(const AttnParams p, FastDiv by_grid, OpenItem *open,
+                                                                             float *part)
 {
     using Sh = DecShape<D, NT>;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -446,12 +448,28 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 #pragma unroll
                     for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            float v = (kChains == 2 ? s[kt][nt][0][c] + s[kt][nt][kChains - 1][c] : s[kt][nt][0][c]) * p.scale;
-                            if (p.cap > 0.f) v = capped(v, p.cap);
-                            x[kt][nt][c] = v;
+                        for (int c = 0; c < 4; ++c)
+                            x[kt][nt][c] = (kChains == 2 ? s[kt][nt][0][c] + s[kt][nt][kChains - 1][c] : s[kt][nt][0][c]) * p.scale;
+                    if (p.cap > 0.f) {
+#pragma unroll
+                        for (int kt = 0; kt < Sh::kTiles; ++kt) {  // two keys of a row share a reciprocal
+                            capped2(x[kt][nt][0], x[kt][nt][2], p.cap);
+                            capped2(x[kt][nt][1], x[kt][nt][3], p.cap);
                         }
-                    if (masked || p.slopes) {
+                    }
+                    if (p.slopes) {
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const Row w = rows[8 * nt + 2 * t4 + c];
+                            const float first = (float)(j0 + g - w.pos);
+#pragma unroll
+                            for (int kt = 0; kt < Sh::kTiles; ++kt)
+#pragma unroll
+                                for (int e = c; e < 4; e += 2)
+                                    x[kt][nt][e] = fmaf(w.slope, first + (float)(16 * kt + (e >> 1) * 8), x[kt][nt][e]);
+                        }
+                    }
+                    if (masked) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const Row w = rows[8 * nt + 2 * t4 + c];
@@ -460,7 +478,6 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 #pragma unroll
                                 for (int e = c; e < 4; e += 2) {
                                     const int j = j0 + 16 * kt + g + (e >> 1) * 8;
-                                    x[kt][nt][e] = fmaf(w.slope, (float)(j - w.pos), x[kt][nt][e]);
                                     if (j < w.lo || j >= w.hi) x[kt][nt][e] = -INFINITY;
                                 }
                         }

@@ -273,8 +273,10 @@ __device__ __forceinline__ int64_t pf_sums(const AttnParams &p, int *sums, int b
 
 // ------------------------------------------------------------ device pieces --
 
-#define PF_R8(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3]), "=r"(a[i + 4]), "=r"(a[i + 5]), "=r"(a[i + 6]), "=r"(a[i + 7])
-#define PF_P8(a, i) "+r"(a[i]), "+r"(a[i + 1]), "+r"(a[i + 2]), "+r"(a[i + 3]), "+r"(a[i + 4]), "+r"(a[i + 5]), "+r"(a[i + 6]), "+r"(a[i + 7])
+#define PF_R8(a, i) \
+    "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3]), "=r"(a[i + 4]), "=r"(a[i + 5]), "=r"(a[i + 6]), "=r"(a[i + 7])
+#define PF_P8(a, i) \
+    "+r"(a[i]), "+r"(a[i + 1]), "+r"(a[i + 2]), "+r"(a[i + 3]), "+r"(a[i + 4]), "+r"(a[i + 5]), "+r"(a[i + 6]), "+r"(a[i + 7])
 #define PF_I8(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3]), "r"(a[i + 4]), "r"(a[i + 5]), "r"(a[i + 6]), "r"(a[i + 7])
 
 // 32 columns of the warp's 32 lanes; the values may be used after pf_ld_wait of them.
@@ -604,7 +606,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 bool ok = !(pp.debug & kDebugNoProducer);
                 auto pages = [&](int u) {
                     const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
-                    return lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first ? __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j)) : -1;
+                    if (lane >= boxes || j >= at.k.end || j + pp.box_rows <= at.k.first) return -1;
+                    return __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j));
                 };
                 int spent = 0;
                 while (ok && (n = pf_units(run, at)) > 0) {

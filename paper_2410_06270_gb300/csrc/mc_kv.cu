@@ -12,7 +12,10 @@ constexpr int kAppendPasses = 4;  // rows a half or quarter warp takes, loads fi
 constexpr int kAppendThreads = 128;
 
 // Warps that a token's heads of one kind take.
-__host__ __device__ constexpr int append_warps(int heads, int D) { return (heads * D / 256 + kAppendPasses - 1 + (heads * D % 256 != 0)) / kAppendPasses; }
+__host__ __device__ constexpr int append_warps(int heads, int D)
+{
+    return (heads * D / 256 + kAppendPasses - 1 + (heads * D % 256 != 0)) / kAppendPasses;
+}
 
 __device__ __forceinline__ uint64_t swapped(uint64_t v)
 {
