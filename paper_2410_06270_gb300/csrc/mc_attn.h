@@ -168,7 +168,7 @@ __device__ __forceinline__ TokenPlace token_place(const BatchView &bv, const KvV
         const int first = __shfl_sync(0xffffffffu, cu, s), end = __shfl_sync(0xffffffffu, cu, s + 1 < 32 ? s + 1 : 31);
         const int len = __shfl_sync(0xffffffffu, mine, s);
         if (s >= bv.seqs) return {-1, -1};
-        if (first < 0 || first > t || end > bv.tokens) {
+        if (first < 0 || first > t || end <= t || end > bv.tokens) {
             set_status(status, MC_ERR_RANGE);
             return {s, -1};
         }

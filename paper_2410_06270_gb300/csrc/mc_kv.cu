@@ -45,7 +45,15 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
     const int64_t warp = (int64_t)blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
     int w;  // of the token's warps
     const int t = p.per_token.div((int)warp, w);
-    if (t >= p.b.tokens) return;
+    if (t >= p.b.tokens) {
+        // the warp after the last token's looks over cu_q, of which a token meets one sequence's part
+        if (p.b.cu_q && t == p.b.tokens && w == 0)
+            for (int i = lane; i < p.b.seqs; i += 32) {
+                int first;
+                seq_rows(p.b, i, first, p.status);
+            }
+        return;
+    }
     const bool is_q = w < wq, is_v = w >= wq + wk;
     const int heads = is_q ? p.q_heads : p.c.kv_heads;
     const int h0 = (is_q ? w : is_v ? w - wq - wk : w - wq) * kRows * kAppendPasses + lane / kLanes;
@@ -176,7 +184,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
 int launch_append(AppendParams p, int head_dim, bool bf16, cudaStream_t st)
 {
     const int per = append_warps(p.q_heads, head_dim) + 2 * append_warps(p.c.kv_heads, head_dim);
-    const int64_t ctas = ((int64_t)p.b.tokens * per + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
+    const int64_t ctas = ((int64_t)p.b.tokens * per + (p.b.cu_q ? 1 : 0) + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
     if (ctas > 0x7fffffff / (kAppendThreads / 32))
         return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d heads in one call", p.b.tokens, p.q_heads + 2 * p.c.kv_heads);
     p.per_token = FastDiv(per);

@@ -414,6 +414,27 @@ def test_bad_pages_lengths_and_positions_are_reported(mc):
     mc.check_status(ws)
 
 
+@pytest.mark.parametrize("many", [False, True])
+def test_a_descending_cu_q_stays_within_the_tables(mc, many):
+    """A token that no sequence's rows hold is appended nowhere: not past its sequence's
+    length either, which the row after the last one's page list would be read for."""
+    seqs = 40 if many else 3
+    B = ref.Batch([32] * seqs, [1] * seqs, 2, 16, 64, "fp16", 24)
+    table = torch.cat([B.table, B.table[:1]])  # (what lies behind the last row here names a page)
+    table[seqs] = min(set(range(len(B.k))) - {int(i) for i in B.table.flatten()})
+    cu = torch.tensor([0, 9, 1, 2] + [2] * (seqs - 3), dtype=torch.int32).cuda()
+    B.k.zero_(), B.v.zero_()
+    cache, _ = B.device(mc)
+    batch = mc.KVBatch(torch.tensor(B.lens, dtype=torch.int32).cuda(), table.cuda()[:seqs], cu, 9)
+    q, k, v = (B.randn(9, n, 64).cuda() for n in (4, 2, 2))
+    ws = mc.attn_workspace(cache, 4)
+    mc.kv_append(cache, batch, q, k, v, workspace=ws)
+    with pytest.raises(mc.MCError):
+        mc.check_status(ws)
+    written = {int(i) for i in (cache.k.flatten(1) != 0).any(1).nonzero().flatten()}
+    assert written <= {int(i) for i in B.table.flatten()}
+
+
 def test_prefill_waits_expire_and_the_context_lives(mc):
     """With the copies switched off every wait of the kernel reaches its bound."""
     B = ref.Batch([300], [300], 1, 16, 64, "bf16", 23)
