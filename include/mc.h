@@ -368,7 +368,9 @@ typedef struct {
  * A query that sees no key gets a zero row and lse = -inf.  Keys that a query does not see do
  * not reach its row, whatever they hold, infinities and NaN included.  Scores, statistics and sums
  * are fp32; the probabilities are rounded to the cache's dtype for their product with v.
- * mc_attn_decode takes one new token per sequence (cu_q NULL), mc_attn_prefill any number. */
+ * mc_attn_decode takes one new token per sequence (cu_q NULL), mc_attn_prefill any number.
+ * out must not overlap q.  MC_ERR_UNSUPPORTED: more work in one call than the schedule counts, with
+ * every sequence as long as its table row, tokens * group / 256 * keys / 128 from 2^31 on a sequence. */
 int mc_attn_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
                    const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
                    size_t ws_bytes, void *stream);

@@ -62,7 +62,8 @@ static int check_counts(const mc_kv_batch *b)
 {
     if (!b) return set_error(MC_ERR_INVALID_ARG, "NULL batch");
     if (b->seqs < 0 || b->tokens < 0) return set_error(MC_ERR_INVALID_ARG, "seqs %d, tokens %d", b->seqs, b->tokens);
-    if (b->tokens > kMaxLen) return set_error(MC_ERR_UNSUPPORTED, "%d tokens in one call", b->tokens);
+    if (b->tokens > kMaxLen || b->seqs > kMaxLen)
+        return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d sequences in one call", b->tokens, b->seqs);
     return MC_OK;
 }
 
@@ -83,6 +84,16 @@ static KvView view(const mc_kv_cache *c)
 static BatchView view(const mc_kv_batch *b)
 {
     return {b->lens, b->table, b->cu_q, b->seqs, b->tokens, b->table_width};
+}
+
+// The schedules count a sequence's work in 32 bits, and a CTA's share of the batch's; what it could
+// be at most, every sequence as long as its table row, must fit (8192 tokens of a group of 8 over
+// 2^20 keys are 2^21 of the 2^31).
+static bool countable(const mc_kv_cache *c, const mc_kv_batch *b, int group)
+{
+    const int64_t room = (int64_t)b->table_width * c->page_size, most = room < kMaxLen ? room : kMaxLen;
+    const double rows = (double)b->tokens * group;
+    return (rows / 256 + 1) * (most / 128 + 3) < 0x7fffffff && (rows / 8 + b->seqs) * c->kv_heads * (most / 64 + 3) < 0x1p38;
 }
 
 constexpr int kFewRows = 16, kFewRowsCap = 32;
@@ -108,6 +119,9 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     if (!workspace || !aligned(workspace, 256)) return set_error(MC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const size_t need = mc_attn_workspace_size(cache, q_heads);
     if (ws_bytes < need) return set_error(MC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", ws_bytes, need);
+    if (!countable(cache, batch, q_heads / cache->kv_heads))
+        return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d sequences, tables of %d pages of %d keys, in one call", batch->tokens,
+                         batch->seqs, batch->table_width, cache->page_size);
     AttnParams p = {};
     p.c = view(cache);
     p.b = view(batch);
@@ -131,7 +145,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     // device's, so the mean decides.  8 sequences of 4000 keys, decode / tensor-memory kernel:
     // 20 rows 38 / 34 us, 32 rows 44 / 34; with a cap, whose cost follows the rows, 38 / 49 and
     // 45 / 49; one sequence of 2000 keys, 16 rows, 12 / 17.
-    const int64_t rows = (int64_t)((batch->tokens + batch->seqs - 1) / batch->seqs) * p.group;
+    const int64_t rows = ((int64_t)batch->tokens + batch->seqs - 1) / batch->seqs * p.group;
     const bool bf16 = cache->dtype == MC_BF16;
     if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, (int)rows, (cudaStream_t)stream);
     return launch_prefill(p, cache->head_dim, bf16, (cudaStream_t)stream);

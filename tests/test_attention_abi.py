@@ -119,3 +119,18 @@ def test_bad_options_and_pointers(mc):
                 {"rot": -16}, {"rot": 16}, {"rot": 16, "rope": fake}, {"rot": 16, "rope": odd, "rows": 9}, {"out": None},
                 {"out": odd}, {"ws": 0x100001}):
         assert append(**bad) == mc.ERR_INVALID_ARG, bad
+
+
+@pytest.mark.parametrize("seqs,tokens,width,heads", [
+    (1, 1 << 20, 1 << 20, 4096),          # 2^24 row tiles over 2^17 units
+    (1 << 24, 1 << 24, 1 << 22, 4),       # long tables of many sequences
+    (1, (1 << 30) + 1, 1, 2),
+    ((1 << 30) + 1, 1, 1, 2)])
+def test_more_work_than_the_schedule_counts(mc, seqs, tokens, width, heads):
+    cache, batch = _cpu(mc)
+    fake, need = 0x100000, mc.load().mc_attn_workspace_size(cache._ref, heads)
+    batch._c.seqs, batch._c.tokens, batch._c.table_width, batch._c.cu_q = seqs, tokens, width, fake
+    opts = mc._AttnOptsC(0.1, 0.0, 0, None, None)
+    assert mc.load().mc_attn_prefill(cache._ref, batch._ref, fake, heads * 64, heads, ctypes.addressof(opts), fake, heads * 64,
+                                     None, fake, need, None) == mc.ERR_UNSUPPORTED
+    assert mc.last_error()
