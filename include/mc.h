@@ -348,7 +348,7 @@ int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void 
                  const void *k_norm, float eps, const float *rope, int rope_rows, int rot_dim, int interleaved,
                  void *q_out, void *workspace, void *stream);
 
-/* What a query's scores go through (scale > 0).  With x = scale * (q . k_j):
+/* What a query's scores go through (scale, and softcap if not 0, within 1e-18 .. 1e18).  With x = scale * (q . k_j):
  *   softcap > 0   x <- softcap * tanh(x / softcap)
  *   slopes        (fp32 [q_heads], NULL: none) x <- x + slopes[head] * (j - p)
  * and the query at position p sees key j of its sequence iff

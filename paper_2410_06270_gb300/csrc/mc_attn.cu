@@ -106,7 +106,9 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     int rc = check_cache(cache, q_heads);
     if (rc || (rc = check_counts(batch))) return rc;
     if (!o) return set_error(MC_ERR_INVALID_ARG, "NULL options");
-    if (!(o->scale > 0.f) || !isfinite(o->scale) || !(o->softcap >= 0.f) || !isfinite(o->softcap) || o->window < 0)
+    // (the scale, its product with log2 e and its quotient by the cap, stay in fp32's range)
+    if (!(o->scale >= 1e-18f) || !(o->scale <= 1e18f) || !(o->softcap == 0.f || (o->softcap >= 1e-18f && o->softcap <= 1e18f)) ||
+        o->window < 0)
         return set_error(MC_ERR_INVALID_ARG, "scale %g, softcap %g, window %d", o->scale, o->softcap, o->window);
     if (decode && batch->cu_q) return set_error(MC_ERR_INVALID_ARG, "one token per sequence: cu_q must be NULL");
     if (decode && o->prefix) return set_error(MC_ERR_INVALID_ARG, "a prefix is mc_attn_prefill's");

@@ -75,6 +75,15 @@ def test_binding_refuses_what_c_cannot_see(mc):
     assert _code(mc, mc.attn_prefill, cache, batch, q, prefix=torch.zeros(3), workspace=ws) == -1
 
 
+@pytest.mark.parametrize("scale,cap", [(0.0, 0.0), (-1.0, 0.0), (1e-30, 0.0), (1e30, 0.0), (1.0, 1e-30), (1.0, 1e30), (1e30, 1e-30)])
+def test_scales_and_caps_out_of_range(mc, scale, cap):
+    cache, batch = _cpu(mc)
+    opts, fake = mc._AttnOptsC(scale, cap, 0, None, None), 0x100000
+    need = mc.load().mc_attn_workspace_size(cache._ref, 4)
+    for fn in (mc.load().mc_attn_decode, mc.load().mc_attn_prefill):
+        assert fn(cache._ref, batch._ref, fake, 256, 4, ctypes.addressof(opts), fake, 256, None, fake, need, None) == mc.ERR_INVALID_ARG
+
+
 def test_bad_options_and_pointers(mc):
     cache, batch = _cpu(mc)
     lib, need = mc.load(), mc.load().mc_attn_workspace_size(cache._ref, 4)
