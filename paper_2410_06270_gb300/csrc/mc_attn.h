@@ -304,7 +304,7 @@ __device__ __noinline__ void exact_row(const AttnParams &p, int b, int pos, int 
         x *= p.scale;
         if (p.cap > 0.f) x = capped(x, p.cap);
         x = fmaf(slope, (float)(j - pos), x);
-        const float top = fmaxf(m, x), keep = top == m ? 1.f : ex2(m - top), pr = ex2(x - top);
+        const float top = fmaxf(m, x), keep = top == m ? 1.f : ex2(m - top), pr = x == -INFINITY ? 0.f : ex2(x - top);
         m = top;
         l = fmaf(l, keep, pr);
 #pragma unroll

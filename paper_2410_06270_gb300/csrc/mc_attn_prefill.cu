@@ -927,6 +927,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         p.lse[(int64_t)(at.s.first + tok) * p.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
                     if (live && !whole)
                         reinterpret_cast<float2 *>(mine + kPfRows * D)[t * kPfTile + row] = make_float2(m, l);
+                    __syncwarp();  // (a row's stores above come before another lane's below)
                     for (unsigned which = __ballot_sync(0xffffffffu, odd != odd); which; which &= which - 1) {
                         const int r = __ffs(which) - 1;
                         const int tr = __shfl_sync(0xffffffffu, tok, r), hr = __shfl_sync(0xffffffffu, head, r);

@@ -332,6 +332,25 @@ def test_hidden_infinities_and_nan_stay_hidden(mc, dim, dtype, lens, new, heads,
     assert torch.allclose(lse.double().cpu(), want[1], rtol=1e-4, atol=1e-4, equal_nan=True)
 
 
+@pytest.mark.parametrize("dim,dtype,length,new,heads,window", [(128, "bf16", 300, 3, 2, 0), (64, "fp16", 9000, 5, 2, 0), (128, "fp16", 300, 100, 4, 0),
+                                                               (64, "bf16", 6000, 100, 2, 5950)])
+def test_a_visible_score_of_minus_infinity_weighs_nothing(mc, dim, dtype, length, new, heads, window):
+    """The first keys that a row sees score -inf, and a key that all but the last row do not see
+    has an infinite value."""
+    B = ref.Batch([length], [new], 1, 16, dim, dtype, 43)
+    first = max(0, length - new - window + 1) if window else 0
+    for j in range(first, first + 2):
+        B.k[B.table[0, j // 16], 0, j % 16, 0] = -float("inf")
+    B.v[B.table[0, (length - 1) // 16], 0, (length - 1) % 16, 5] = float("inf")
+    q = B.randn(new, heads, dim)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.25
+    want = ref.attention(B, q, dim ** -0.5, window=window)
+    cache, batch = B.device(mc)
+    got, lse = mc.attn_prefill(cache, batch, q.cuda(), window=window, with_lse=True)
+    rows = torch.arange(new - 1)
+    ref.assert_attention(got, lse, want, dtype, length, 5.0, rows=rows)
+
+
 # ----------------------------------------------------------- streams, status --
 
 def test_on_another_stream_and_in_a_graph(mc):
