@@ -557,8 +557,8 @@ def kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope=None, interleaved: b
 
 
 def _status(workspace, cache):
-    if workspace.get_device() != cache.index or not workspace.is_contiguous():
-        _bad("the workspace must be contiguous on the cache's device")
+    if workspace.get_device() != cache.index or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < 256:
+        _bad("the workspace must be contiguous on the cache's device, with its status word's 256 bytes")
     return workspace.data_ptr()
 
 

@@ -173,7 +173,7 @@ static PyObject *kv_append(PyObject *self, PyObject *const *a, Py_ssize_t na)
     if (!side(&c, a[5], t_float32, 2, rope_n, &rope)) return leave(&c);
     if (!side(&c, a[7], c.dtype, 1, n, &qn) || (qn && n[0] != D)) return leave(&c);
     if (!side(&c, a[8], c.dtype, 1, n, &kn) || (kn && n[0] != D)) return leave(&c);
-    if (!side(&c, a[11], t_uint8, 1, n, &ws)) return leave(&c);
+    if (!side(&c, a[11], t_uint8, 1, n, &ws) || (a[11] != Py_None && n[0] < 256)) return leave(&c);
     const double eps = PyFloat_AsDouble(a[9]);
     const int inter = PyObject_IsTrue(a[6]);
     const int64_t st = stream_of(&c);

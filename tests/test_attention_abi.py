@@ -71,6 +71,7 @@ def test_binding_refuses_what_c_cannot_see(mc):
     assert _code(mc, mc.kv_append, cache, batch, q, kv, kv, q_norm=torch.ones(32, dtype=torch.bfloat16)) == -1
     assert _code(mc, mc.kv_append, cache, batch, q, kv, kv, k_norm=torch.ones(64)) == -1
     assert _code(mc, mc.kv_append, cache, batch, q, kv, kv, rope=torch.zeros(10, 64, dtype=torch.float64)) == -1
+    assert _code(mc, mc.kv_append, cache, batch, q, kv, kv, workspace=torch.zeros(2, dtype=torch.uint8)) == -1
     assert _code(mc, mc.attn_decode, cache, batch, q, slopes=torch.zeros(3), workspace=ws) == -1
     assert _code(mc, mc.attn_prefill, cache, batch, q, prefix=torch.zeros(3), workspace=ws) == -1
 
