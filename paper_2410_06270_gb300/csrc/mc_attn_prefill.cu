@@ -16,16 +16,17 @@
 // Units of the whole batch, in order, are dealt to the CTAs (one per SM) as equal
 // contiguous runs, found on the device from the lengths; a run that ends inside an item
 // leaves (m, l, O) in fp32 and prefill_join_kernel adds an item's pieces in their order.
-// This splits a long cache over the SMs when there are few rows, and balances the causal
-// triangle, by the same rule.
+// This splits a long cache over the SMs when there are few rows, and balances short causal
+// triangles, by the same rule.  Batches with many items deal them whole, largest first, from a
+// common count (which CTA takes an item does not change its result).
 //
 // What bounds it: a unit's 32 MMAs are 2048 cycles of the tensor pipe; it takes 2830, as QK^T with
 // both operands in shared memory runs at 78 cycles an MMA (8 KB each, all that shared memory
 // gives in 64), PV with P in tensor memory at 65, and the change of tiles costs the rest; the
 // softmax's 575 instructions a warp (1160 cycles) run beside it.  A prompt of 8192 tokens, 32 heads
-// on 8 of 128: 376 us, 1.46 PFLOP/s of the visible pairs, 0.77 of cuBLAS's burst rate and 0.86 of its
-// sustained one (at the power cap; 358 us in a short burst).  Capped scores take twice the time
-// (2^x and a reciprocal each: 223 us at 4096 tokens, 115 without).
+// on 8 of 128: 358 us, 1.54 PFLOP/s of the visible pairs, 0.79 of cuBLAS's burst rate and 0.91 of its
+// sustained one (at the power cap).  Capped scores take twice the time (2^x and a reciprocal each:
+// 217 us at 4096 tokens, 105 without).
 //
 // Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 and 9 issue a tile's MMAs,
 // 10 copies keys and values (TMA, a box per page and 64 columns), 11 the queries (TMA where a
@@ -49,6 +50,28 @@ constexpr int kPfRows = 256, kPfTile = 128, kPfKeys = 128;
 constexpr int kPfThreads = 384, kPfMma = 8, kPfKv = 10;  // MMA: two warps; after kPfKv the queries
 constexpr int kPfMaxStages = 8;
 constexpr float kPfLazy = 8.f;
+constexpr int kPfAhead = 8;   // items that a block's roles may be apart (the copies lead the softmax by 4 at most)
+constexpr int kPfCount = 32;  // the queue's count: a word of the 256 bytes behind the status word
+// Items come from a queue where there are at least kPfQueueItems a block, none costs more than a
+// block's mean, and the last ones given out (a sequence's first row tile) at most 1 / kPfQueueFirst of it.
+constexpr int kPfQueueItems = 2, kPfQueueFirst = 4;
+
+struct PfSeq {
+    int first, n, len, prefix;  // first token row, new tokens, length, prefix
+};
+
+// Keys [base, end) that an item's rows see, base rounded down to a unit; at least one unit (of
+// zeros, all masked), so that rows without keys take the same way.
+struct PfKeys {
+    int base, end, units, first;  // first: the first key that is seen
+};
+
+// Row tile mt of key head h of sequence b; of its units, n from u on.
+struct PfItem {
+    int b, h, mt, u, n;
+    PfSeq s;
+    PfKeys k;
+};
 
 struct PfShared {
     uint64_t kfull[kPfMaxStages], kempty[kPfMaxStages];  // ring of keys / values
@@ -60,7 +83,12 @@ struct PfShared {
     int off;                                             // the end's cost offset in its item
     int run;                                             // cost of a run
     int64_t total;                                       // cost of the batch
-    int sums[2][32];
+    int queued;                                          // items come from the common queue, not as a run
+    uint64_t ifull[kPfAhead], iempty[kPfAhead];
+    union {
+        int sums[2][32];                                 // before the roles part
+        PfItem item[kPfAhead];                           // the block's items, in turn; n = 0: no more
+    };
 };
 
 template <int D>
@@ -85,6 +113,7 @@ struct PfParams {
     int debug;
     int q_boxes;   // a tile's queries are boxes of whole groups of heads (the group divides 128)
     int out32;     // rows of the output start at multiples of 32 bytes
+    int may_queue;  // the batch may have the items for a queue
     int box_rows;  // rows of a copied box: the largest power of two that divides a page, at most a unit
 };
 
@@ -121,10 +150,6 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, const 
 
 // ------------------------------------------------------------------ items --
 
-struct PfSeq {
-    int first, n, len, prefix;  // first token row, new tokens, length, prefix
-};
-
 __device__ __forceinline__ PfSeq pf_seq(const AttnParams &p, int b, int32_t *status)
 {
     PfSeq s;
@@ -133,12 +158,6 @@ __device__ __forceinline__ PfSeq pf_seq(const AttnParams &p, int b, int32_t *sta
     s.prefix = p.prefix ? __ldg(p.prefix + b) : 0;
     return s;
 }
-
-// Keys [base, end) that rows of item mt see, base rounded down to a unit; at least
-// one unit (of zeros, all masked), so that rows without keys take the same way.
-struct PfKeys {
-    int base, end, units, first;  // first: the first key that is seen
-};
 
 __device__ __forceinline__ PfKeys pf_keys(const AttnParams &p, const PfSeq &s, int mt)
 {
@@ -158,15 +177,19 @@ __device__ __forceinline__ int pf_tiles(const AttnParams &p, const PfSeq &s)
     return (s.n * p.group + kPfRows - 1) / kPfRows;
 }
 
-struct PfPlace {
+// The next item of a block's run, which ends before unit `u` of item (b, h, mt).
+struct PfRun {
     int b, h, mt, u;
-    PfSeq s;
-    PfKeys k;
 };
-
-__device__ __forceinline__ void pf_next_item(const AttnParams &p, PfPlace &at)
+__device__ __forceinline__ int pf_units(const PfRun &r, const PfItem &at)  // 0: the run is over
 {
-    at.u = 0;
+    return (at.b == r.b && at.h == r.h && at.mt == r.mt ? r.u : at.k.units) - at.u;
+}
+__device__ __forceinline__ void pf_next(const AttnParams &p, const PfRun &run, PfItem &at)
+{
+    const bool over = at.u + at.n < at.k.units;
+    at.u = at.n = 0;
+    if (over) return;
     if (++at.mt >= pf_tiles(p, at.s)) {
         at.mt = 0;
         if (++at.h >= p.c.kv_heads) {
@@ -178,32 +201,23 @@ __device__ __forceinline__ void pf_next_item(const AttnParams &p, PfPlace &at)
         }
     }
     at.k = pf_keys(p, at.s, at.mt);
+    at.n = pf_units(run, at);
 }
+
+// The block's turn-th item.  The role that copies keys finds the items, one ahead; the others read
+// them, where they need a field (held in registers through a unit's softmax, they would be spilled).
+__device__ __forceinline__ const volatile PfItem *pf_item(const PfParams &pp, PfShared *sh, int turn)
+{
+    const volatile PfItem *it = &sh->item[turn % kPfAhead];
+    return warp_wait(&sh->ifull[turn % kPfAhead], (turn / kPfAhead) & 1, pp, sh) && it->n > 0 ? it : nullptr;
+}
+__device__ __forceinline__ int pf_rows(const AttnParams &p, const volatile PfItem *it) { return it->s.n * p.group - it->mt * kPfRows; }
 
 // What an item costs on top of its units, in units: the change of queries, the first
 // unit's softmax with no other work beside it, the epilogue.  Runs are equal in cost
 // (equal in units alone, a CTA with the 29 short items at a causal prompt's start took a
 // third longer than the mean: 8192 tokens 489 us against 364).
 constexpr int kPfItemCost = 2;
-
-// The end of this CTA's run, read by each role for itself (state held from before the
-// roles part would be spilled for all of them by the softmax's need of registers).
-struct PfRun {
-    int b, h, mt, u;
-};
-
-__device__ __forceinline__ PfRun pf_run(const AttnParams &p, const volatile PfShared *sh, PfPlace &at)
-{
-    at.b = sh->b[0];
-    at.h = sh->h[0];
-    at.mt = sh->mt[0];
-    at.u = sh->u[0];
-    if (at.b >= 0) {
-        at.s = pf_seq(p, at.b, nullptr);
-        at.k = pf_keys(p, at.s, at.mt);
-    }
-    return {sh->b[1], sh->h[1], sh->mt[1], sh->u[1]};
-}
 
 // The order in which a run takes an item's units.  Runs of one key head start at different
 // places of a long cache; if each went straight on, a unit would be read for one row tile now
@@ -216,8 +230,8 @@ __device__ __forceinline__ PfRun pf_run(const AttnParams &p, const volatile PfSh
 constexpr int64_t kPfL2 = 64 << 20;
 struct PfOrder {
     int first, n, shift;
-    __device__ __forceinline__ PfOrder(const AttnParams &p, int D, const PfPlace &at, int n_, int run, int spent)
-        : first(at.u), n(n_), shift(0)
+    __device__ __forceinline__ PfOrder(const AttnParams &p, int D, const volatile PfItem &at, int run, int spent)
+        : first(at.u), n(at.n), shift(0)
     {
         if (at.k.units <= run || (int64_t)at.s.len * p.c.kv_heads * D * 4 <= kPfL2) return;
         const int ahead = (spent - at.u) % run, to = ahead < 0 ? ahead + run : ahead;
@@ -226,19 +240,21 @@ struct PfOrder {
     __device__ __forceinline__ int unit(int i) const { return first + (i + shift < n ? i + shift : i + shift - n); }
 };
 
-// Units of the item at hand that belong to the run; 0: the run is over.
-__device__ __forceinline__ int pf_units(const PfRun &r, const PfPlace &at)
-{
-    return (at.b == r.b && at.h == r.h && at.mt == r.mt ? r.u : at.k.units) - at.u;
-}
-
 // Costs of 32 sequences from b0 on (per key head) into sums, by one warp: the
-// sequences' items are laid end to end and taken 32 at a time.  Returns their total.
-__device__ __forceinline__ int64_t pf_sums(const AttnParams &p, int *sums, int b0, int lane, int32_t *status)
+// sequences' items are laid end to end and taken 32 at a time.  Returns their total, and in mix
+// (if it is not NULL) what the choice of schedule asks for, of the lane's sequence.
+struct PfMix {
+    int items, most, first;  // items of a key head, cost of the largest and of the first one
+};
+__device__ __forceinline__ int64_t pf_sums(const AttnParams &p, int *sums, int b0, int lane, int32_t *status, PfMix *mix)
 {
     PfSeq s = {0, 0, 0, 0};
     if (b0 + lane < p.b.seqs) s = pf_seq(p, b0 + lane, status);
     const int tiles = pf_tiles(p, s);
+    if (mix && tiles) {
+        const int first = pf_keys(p, s, 0).units + kPfItemCost, last = pf_keys(p, s, tiles - 1).units + kPfItemCost;
+        *mix = {tiles, max(first, last), first};
+    }
     int upto = tiles;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -504,6 +520,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             mbar_init(&sh->kempty[i], 2);
         }
         mbar_init(&sh->vpatch, 1);
+        for (int i = 0; i < kPfAhead; ++i) {
+            mbar_init(&sh->ifull[i], 1);
+            mbar_init(&sh->iempty[i], 8);
+        }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&sh->qfull[t], pp.q_boxes ? 1 : 32);
             mbar_init(&sh->qempty[t], 1);
@@ -521,15 +541,26 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         // where the run starts (warp 0) and ends (warp 1)
         int *sums = sh->sums[warp];
         int64_t total = 0;
-        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) total += pf_sums(p, sums, b0, lane, p.status);
+        PfMix mix = {0, 0, 0};
+        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) total += pf_sums(p, sums, b0, lane, p.status, pp.may_queue ? &mix : nullptr);
         total *= p.c.kv_heads;
         const int64_t ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
+        // Long prompts have items enough to be dealt one by one, largest first: no pieces to join, and
+        // SMs that are slower than others (units of the same work take up to a tenth longer on some) get
+        // fewer.  Runs / queue: 3000 tokens, 2.5 items a block, 84 / 73 us, 4096 124 / 105, 8192 378 / 358, four
+        // prompts of 2000 142 / 122, six ragged ones on top of a cache 247 / 237.
+        bool queued = false;
+        if (pp.may_queue) {
+            const int64_t items = (int64_t)__reduce_add_sync(0xffffffffu, mix.items) * p.c.kv_heads;
+            const int most = __reduce_max_sync(0xffffffffu, mix.most), first = __reduce_max_sync(0xffffffffu, mix.first);
+            queued = items >= kPfQueueItems * ctas && most * ctas <= total && kPfQueueFirst * first * ctas <= total;
+        }
         int fb = -1, fh = 0, fmt = 0, fu = 0, off = 0;
-        if ((int64_t)blockIdx.x < ctas) {
+        if (!queued && (int64_t)blockIdx.x < ctas) {
             int64_t r = muldiv64(total, blockIdx.x + warp, (int)ctas);  // cost before the place
             if (r == total) fb = p.b.seqs;
             for (int b0 = 0; b0 < p.b.seqs && fb < 0; b0 += 32) {
-                if (p.b.seqs > 32) pf_sums(p, sums, b0, lane, nullptr);
+                if (p.b.seqs > 32) pf_sums(p, sums, b0, lane, nullptr, nullptr);
                 const int64_t own = (int64_t)sums[lane] * p.c.kv_heads;
                 int64_t upto = own;
 #pragma unroll
@@ -576,6 +607,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             sh->mt[warp] = fmt;
             sh->u[warp] = fu;
             if (warp) {
+                sh->queued = queued;
                 sh->total = total;
                 sh->off = off;
                 sh->run = max(1, (int)div64(total, max(ctas, (int64_t)1)));
@@ -594,25 +626,80 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         pf_give_regs();  // one instruction for the warpgroup
         if (warp >= kPfKv) {
             // -------------------------------------------------------------- copies --
-            PfPlace at;
-            const PfRun run = pf_run(p, sh, at);
             const uint32_t smem0 = smem_u32(smem);
             if (warp == kPfKv) {
                 // keys and values: lane i copies the i-th box (of a page) of a tile.  A page that is
                 // not there, and boxes before the first key or past the last, are read beyond the map:
                 // zeros.
                 const int boxes = kPfKeys / pp.box_rows;
-                int it = 0, patches = 0, n;
+                int it = 0, patches = 0;
                 bool ok = !(pp.debug & kDebugNoProducer);
+                // The block's items.  Where they come from the queue: by falling row tile, then sequence and
+                // key head; the first is that of the block's number, the next ones those that a common
+                // count (zero between calls) gives it.
+                const bool queued = sh->queued;
+                const PfRun run = {sh->b[1], sh->h[1], sh->mt[1], sh->u[1]};
+                int level = 0, above = 0, tiles = 0;  // row tile at hand, items of higher ones; lane: its sequence's
+                auto queue_item = [&](int which, PfItem &x) {
+                    unsigned have;
+                    while ((have = __ballot_sync(0xffffffffu, tiles > level)), which - above >= __popc(have) * p.c.kv_heads && level >= 0) {
+                        above += __popc(have) * p.c.kv_heads;
+                        --level;
+                    }
+                    x.u = x.n = 0;
+                    if (level < 0 || which < 0) return;  // (below 0: the workspace was not zeroed)
+                    x.h = which - above;
+                    for (; x.h >= p.c.kv_heads; x.h -= p.c.kv_heads) have &= have - 1;
+                    const int b = __ffs(have) - 1;
+                    x.mt = level;
+                    if (b != x.b) x.s = pf_seq(p, b, nullptr);
+                    x.b = b;
+                    x.k = pf_keys(p, x.s, x.mt);
+                    x.n = x.k.units;
+                };
+                // The place is free once the softmax warps are done with the item before it; the roles
+                // between are ahead of them, or behind the copies by less than the places there are.
+                auto give = [&](const PfItem &x, int turn) {
+                    const int e = turn % kPfAhead;
+                    if (turn >= kPfAhead && !warp_wait(&sh->iempty[e], (turn / kPfAhead + 1) & 1, pp, sh)) return false;
+                    if (lane == 0) {
+                        sh->item[e] = x;
+                        mbar_arrive(&sh->ifull[e]);
+                    }
+                    __syncwarp();
+                    return true;
+                };
+                PfItem at = {};
                 auto pages = [&](int u) {
                     const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
                     if (lane >= boxes || j >= at.k.end || j + pp.box_rows <= at.k.first) return -1;
                     return __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j));
                 };
+                at.b = -1;
+                if (queued) {
+                    if (lane < p.b.seqs) tiles = pf_tiles(p, pf_seq(p, lane, nullptr));
+                    level = __reduce_max_sync(0xffffffffu, tiles) - 1;
+                    queue_item(blockIdx.x, at);
+                } else {
+                    at.b = sh->b[0];
+                    at.h = sh->h[0];
+                    at.mt = sh->mt[0];
+                    at.u = sh->u[0];
+                    at.n = 0;
+                    if (at.b >= 0) {
+                        at.s = pf_seq(p, at.b, nullptr);
+                        at.k = pf_keys(p, at.s, at.mt);
+                        at.n = pf_units(run, at);
+                    }
+                }
+                give(at, 0);
                 int spent = 0;
-                while (ok && (n = pf_units(run, at)) > 0) {
-                    const PfOrder order(p, D, at, n, sh->run, spent);
-                    int page = pages(order.unit(0));
+                for (int turn = 0; ok && at.n > 0; ++turn) {
+                    const int n = at.n;
+                    const PfOrder order(p, D, at, sh->run, spent);
+                    int page = pages(order.unit(0)), count = 0;
+                    PfItem next_item = at;
+                    if (queued && lane == 0) count = atomicAdd(p.status + kPfCount, 1);
                     for (int i = 0; ok && i < n; ++i) {
                         const int u = order.unit(i), next = i + 1 < n ? pages(order.unit(i + 1)) : -1;  // used a unit later
                         const int j0 = at.k.base + u * kPfKeys, j = j0 + lane * pp.box_rows;
@@ -652,10 +739,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                             }
                         }
                         page = next;
+                        if (i == 0) {  // early enough for the others, late enough not to hold the copies up
+                            if (queued) queue_item((int)gridDim.x + __shfl_sync(0xffffffffu, count, 0), next_item);
+                            else pf_next(p, run, next_item);
+                            ok = give(next_item, turn + 1) && ok;
+                        }
                     }
-                    if (at.u + n < at.k.units) break;
                     spent += n + kPfItemCost;
-                    pf_next_item(p, at);
+                    at = next_item;
                 }
                 // the last copies land before the block's shared memory is given back, on an abort too
                 const uint64_t t0 = globaltimer_ns();
@@ -670,10 +761,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 const uint32_t col = (uint32_t)(lc >> 3) * Sh::kHalf + ((lc & 7) << 4);  // 16-byte chunk, unswizzled
                 const int step_hg = kQStep % p.group;
                 const int64_t q_step = kQStep / p.group * p.q_stride + step_hg * D, q_wrap = p.q_stride - p.group * D;
-                int uses[2] = {0, 0}, n;
+                int uses[2] = {0, 0};
                 bool ok = !(pp.debug & kDebugNoProducer);
-                while (ok && (n = pf_units(run, at)) > 0) {
-                    const int rows0 = at.mt * kPfRows, rows = min(kPfRows, at.s.n * p.group - rows0);
+                const volatile PfItem *it;
+                for (int turn = 0; ok && (it = pf_item(pp, sh, turn)); ++turn) {
+                    const int first = it->s.first, head0 = it->h * p.group, rows0 = it->mt * kPfRows, rows = min(kPfRows, pf_rows(p, it));
                     for (int t = 0; t < 2 && t * kPfTile < rows; ++t) {
                         if (uses[t] && !(ok = warp_wait(&sh->qempty[t], (uses[t] + 1) & 1, pp, sh))) break;
                         ++uses[t];
@@ -684,8 +776,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                                 mbar_arrive_expect_tx(&sh->qfull[t], Sh::kTileBytes);
 #pragma unroll
                                 for (int h = 0; h < D / 64; ++h)
-                                    pf_tma3(tile + h * Sh::kHalf, &qmap, 64 * h, at.h * p.group,
-                                            at.s.first + p.by_group.div(rows0 + t * kPfTile), &sh->qfull[t]);
+                                    pf_tma3(tile + h * Sh::kHalf, &qmap, 64 * h, head0,
+                                            first + p.by_group.div(rows0 + t * kPfTile), &sh->qfull[t]);
                             }
                             continue;
                         }
@@ -693,7 +785,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         int r = t * kPfTile + lr;
                         int hg;
                         const int tok = p.by_group.div(rows0 + r, hg);
-                        const uint16_t *src = p.q + (at.s.first + tok) * p.q_stride + (at.h * p.group + hg) * D + lc * 8;
+                        const uint16_t *src = p.q + (first + tok) * p.q_stride + (head0 + hg) * D + lc * 8;
                         for (; r < (t + 1) * kPfTile; r += kQStep) {
                             const bool real = r < rows;
                             pf_copy16z((tile + col + (r & 127) * 128) ^ ((r & 7) << 4), real ? src : p.q, real);
@@ -707,8 +799,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         fence_proxy_async_smem();
                         mbar_arrive(&sh->qfull[t]);
                     }
-                    if (!ok || at.u + n < at.k.units) break;
-                    pf_next_item(p, at);
+                    if (!ok) break;
                 }
                 if (pp.q_boxes) {  // the last copies land before the block's shared memory is given back
                     const uint64_t t0 = globaltimer_ns();
@@ -719,8 +810,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             }
         } else {
             // ---------------------------------------------------------------- MMAs --
-            PfPlace at;
-            const PfRun run = pf_run(p, sh, at);
+            const volatile PfItem *at = pf_item(pp, sh, 0);
             constexpr uint32_t kIdS = pf_idesc(BF16, kPfKeys, false), kIdO = pf_idesc(BF16, D, true);
             const uint32_t q0 = pf_desc_k(smem_u32(smem + Sh::kHdr)), k0 = pf_desc_k(smem_u32(smem + Sh::kRing));
             const uint32_t v0 = pf_desc_mn(smem_u32(smem + Sh::kRing), Sh::kHalf);
@@ -746,13 +836,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 __device__ Slot next() const { return i + 1 == Sh::kStages ? Slot{0, phase ^ 1u} : Slot{i + 1, phase}; }
             };
             auto full = [&](const Slot &x) { return warp_wait(&sh->kfull[x.i], x.phase, pp, sh); };
-            auto tiles_of = [&](const PfPlace &a) { return a.s.n * p.group - a.mt * kPfRows > kPfTile ? 2 : 1; };
+            auto tiles_of = [&](const volatile PfItem *a) { return !a ? 0 : pf_rows(p, a) > kPfTile ? 2 : 1; };
             // Unit j's PV of the tile is followed by unit j + 1's QK of it, the next item's first one
             // after the last: the next queries and the other tile's softmax hide the change of item.
             // A warp for each tile: their waits do not add up, and either's MMAs fill the pipe.
             const int t = warp - kPfMma;
             Slot k = {0, 0};  // of the last keys that QK was issued for
-            int n = pf_units(run, at), tiles = n > 0 ? tiles_of(at) : 0;
+            int n = at ? at->n : 0, tiles = tiles_of(at), turn = 0;
             // a ring slot that this warp has no MMA for (the item has one tile) is given back at once
             auto pass = [&](const Slot &x) {
                 if (lane == 0) mbar_arrive(&sh->kempty[x.i]);
@@ -774,13 +864,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 else pass(k);
             }
             while (ok && n > 0) {
-                PfPlace nx = at;
-                int next_n = 0, next_tiles = 0;
-                if (at.u + n == at.k.units) {
-                    pf_next_item(p, nx);
-                    next_n = pf_units(run, nx);
-                    if (next_n > 0) next_tiles = tiles_of(nx);
-                }
+                const volatile PfItem *next = pf_item(pp, sh, ++turn);
+                const int next_n = next ? next->n : 0, next_tiles = tiles_of(next);
                 // inside the item: unit j's PV and unit j + 1's QK are issued together
                 for (int j = 0; ok && j + 1 < n; ++j) {
                     const Slot v = k.next(), k2 = v.next();
@@ -825,7 +910,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                     if (t < next_tiles) ok = first_qk(k, next_n == 1);
                     else pass(k);
                 }
-                at = nx;
                 n = next_n;
                 tiles = next_tiles;
             }
@@ -839,36 +923,39 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     } else {
         // -------------------------------------------------- softmax and epilogue --
         pf_take_regs();
-        PfPlace at;
-        const PfRun run = pf_run(p, sh, at);
         const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
         const uint32_t lanes = (uint32_t)(wt * 32) << 16;
         const uint32_t s_tmem = lanes + 128 * t, o_tmem = lanes + 256 + 128 * t;
-        int su = 0, ou = 0, spent = 0, n;
+        int su = 0, ou = 0, spent = 0;
         bool ok = true, tail = false;
-        while (ok && (n = pf_units(run, at)) > 0) {
-            const int rows0 = at.mt * kPfRows + t * kPfTile, rows = min(kPfTile, at.s.n * p.group - rows0);
-            const bool from_first = at.u == 0, to_last = at.u + n == at.k.units;
-            if (rows > 0) {
-                const bool live = row < rows;
+        const volatile PfItem *it;
+        for (int turn = 0; ok && (it = pf_item(pp, sh, turn)); ++turn) {
+            const int n = it->n, rows = min(kPfTile, pf_rows(p, it) - t * kPfTile);
+            auto place = [&](int &tok, int &head) {  // of this thread's row (the last one where it has none)
                 int hg;
-                const int tok = p.by_group.div(rows0 + min(row, rows - 1), hg), head = at.h * p.group + hg;
-                const int off = at.s.len - at.s.n, pos = off + tok;
+                tok = p.by_group.div(it->mt * kPfRows + t * kPfTile + min(row, rows - 1), hg);
+                head = it->h * p.group + hg;
+            };
+            if (rows > 0) {
+                int tok, head;
+                place(tok, head);
+                const int len = it->s.len, off = len - it->s.n, pos = off + tok, prefix = it->s.prefix;
                 const int lo = p.window ? max(0, pos - p.window + 1) : 0;
-                const int hi = pos < 0 ? 0 : min(at.s.len, max(pos + 1, at.s.prefix));
+                const int hi = pos < 0 ? 0 : min(len, max(pos + 1, prefix));
                 // what the tile's first and last rows see decides whether a unit needs the mask
+                const int rows0 = it->mt * kPfRows + t * kPfTile, base = it->k.base;
                 const int p_first = off + p.by_group.div(rows0), p_last = off + p.by_group.div(rows0 + rows - 1);
-                const int all_hi = p_first < 0 ? 0 : min(at.s.len, max(p_first + 1, at.s.prefix));
+                const int all_hi = p_first < 0 ? 0 : min(len, max(p_first + 1, prefix));
                 const int all_lo = p.window ? p_last - p.window + 1 : 0;
                 const float slope = MODE != kPfPlain && p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
                 float m = -INFINITY, l = 0.f;
-                const PfOrder order(p, D, at, n, sh->run, spent);
+                const PfOrder order(p, D, *it, sh->run, spent);
                 for (int i = 0; i < n; ++i) {
                     if (!(ok = warp_wait(&sh->sfull[t], su & 1, pp, sh))) break;
                     ++su;
                     tc_fence_after();
                     if (wt * 32 < rows) {
-                        const int j0 = at.k.base + order.unit(i) * kPfKeys;
+                        const int j0 = base + order.unit(i) * kPfKeys;
                         uint32_t s[128];
 #pragma unroll
                         for (int q = 0; q < 4; ++q) pf_ld32(s_tmem + 32 * q, s + 32 * q);
@@ -883,13 +970,15 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh->pfull[t]);
                 }
+                place(tok, head);
+                const bool live = row < rows, from_first = it->u == 0, whole = from_first && n == it->k.units;
+                const int first = it->s.first;
                 if (!ok || !(ok = warp_wait(&sh->ofull[t], ou & 1, pp, sh))) break;
                 ++ou;
                 tc_fence_after();
                 const float inv = 1.f / l;
-                uint16_t *out = p.out + (at.s.first + tok) * p.out_stride + head * D;
+                uint16_t *out = p.out + (first + tok) * p.out_stride + head * D;
                 float *mine = pp.part + (2 * blockIdx.x + (from_first ? 1 : 0)) * pf_part_floats(D);
-                const bool whole = from_first && to_last;
                 if (wt * 32 < rows) {
                     float odd = 0.f;  // NaN once an element of the row is infinite or NaN
 #pragma unroll
@@ -924,30 +1013,30 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         __syncwarp();
                     }
                     if (live && whole && p.lse)
-                        p.lse[(int64_t)(at.s.first + tok) * p.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+                        p.lse[(int64_t)(first + tok) * p.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
                     if (live && !whole)
                         reinterpret_cast<float2 *>(mine + kPfRows * D)[t * kPfTile + row] = make_float2(m, l);
                     __syncwarp();  // (a row's stores above come before another lane's below)
                     for (unsigned which = __ballot_sync(0xffffffffu, odd != odd); which; which &= which - 1) {
                         const int r = __ffs(which) - 1;
                         const int tr = __shfl_sync(0xffffffffu, tok, r), hr = __shfl_sync(0xffffffffu, head, r);
-                        exact_row<D, BF16>(p, at.b, off + tr, at.s.len, at.s.prefix, at.s.first + tr, hr, lane);
+                        exact_row<D, BF16>(p, it->b, it->s.len - it->s.n + tr, it->s.len, it->s.prefix, first + tr, hr, lane);
                     }
                 }
                 tc_fence_before();
             }
-            if (from_first && !to_last) {
+            if (it->u == 0 && n < it->k.units) {
                 tail = true;
                 if (tid == 0) {
                     // the pieces lie in the CTAs whose runs start before the item's end
                     const int64_t total = sh->total, ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
-                    const int64_t end = muldiv64(total, blockIdx.x + 1, (int)ctas) - sh->off + kPfItemCost + at.k.units;
-                    pp.open[blockIdx.x] = {(int32_t)(div64(end * ctas + total - 1, total) - blockIdx.x), at.b, at.h, at.mt};
+                    const int64_t end = muldiv64(total, blockIdx.x + 1, (int)ctas) - sh->off + kPfItemCost + it->k.units;
+                    pp.open[blockIdx.x] = {(int32_t)(div64(end * ctas + total - 1, total) - blockIdx.x), it->b, it->h, it->mt};
                 }
             }
-            if (at.u + n < at.k.units) break;
             spent += n + kPfItemCost;
-            pf_next_item(p, at);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->iempty[turn % kPfAhead]);
         }
         if (!tail && tid == 0) pp.open[blockIdx.x].pieces = 0;
     }
@@ -972,6 +1061,7 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
     const AttnParams &p = pp.a;
     pdl_trigger();
     pdl_wait();
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.status[kPfCount] = 0;
     const PfOpen it = pp.open[blockIdx.x];
     if (it.pieces == 0) return;
     const int r = threadIdx.x % kPfJoinRows, c0 = threadIdx.x / kPfJoinRows, row = blockIdx.y * kPfJoinRows + r;
@@ -1118,6 +1208,8 @@ int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st
     cudaError_t e = sm_count(&nsm);
     if (e == cudaSuccess) {
         const int ctas = nsm < kAttnMaxSms ? nsm : kAttnMaxSms;
+        const int64_t items = ((int64_t)a.b.tokens * a.group / kPfRows + a.b.seqs) * a.c.kv_heads;  // at most
+        p.may_queue = a.b.seqs <= 32 && items >= kPfQueueItems * ctas && items < 1 << 30;
         e = head_dim == 64 ? (bf16 ? launch_prefill_m<64, true>(p, mode, ctas, st) : launch_prefill_m<64, false>(p, mode, ctas, st))
                            : (bf16 ? launch_prefill_m<128, true>(p, mode, ctas, st) : launch_prefill_m<128, false>(p, mode, ctas, st));
     }

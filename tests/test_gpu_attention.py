@@ -272,6 +272,39 @@ def test_prefill_of_many_sequences(mc, seqs, heads, kv):
     assert torch.equal(torch.nan_to_num(cache.v.double().cpu()), torch.nan_to_num(full[2]))
 
 
+@pytest.mark.parametrize("lens,new,heads,kv,dim,dtype,window,cap", [
+    ([4096], [4096], 32, 8, 128, "bf16", 0, 0.0),
+    ([3001, 40, 0, 2500, 3700, 1], [3001, 9, 0, 2300, 3600, 1], 12, 4, 64, "fp16", 0, 20.0),  # items of five sequences
+    ([5000] + [700] * 31, [5000] + [300] * 31, 16, 4, 64, "bf16", 900, 0.0),                 # as many as a queue takes
+    ([4000] + [100] * 32, [4000] + [100] * 32, 16, 4, 64, "bf16", 0, 0.0),                   # one more: runs
+])
+def test_prefill_of_long_prompts(mc, lens, new, heads, kv, dim, dtype, window, cap):
+    """Batches of many items, a part of the rows against the definition; twice over, bit for bit."""
+    B = ref.Batch(lens, new, kv, 64, dim, dtype, 61, pad_tokens=2)
+    q = B.randn(B.tokens, heads, dim)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, heads)
+    slopes = -torch.linspace(0.1, 0.01, heads) if cap else None
+    kw = dict(softcap=cap, window=window, slopes=None if slopes is None else slopes.cuda(), workspace=ws)
+    got, lse = mc.attn_prefill(cache, batch, q.cuda(), with_lse=True, **kw)
+    again = torch.full_like(got, 3.0)
+    mc.attn_prefill(cache, batch, q.cuda(), out=again, **kw)
+    mc.check_status(ws)
+    assert torch.equal(got[:B.cu[-1]], again[:B.cu[-1]])
+    g = torch.Generator().manual_seed(62)
+    for b, (n, length) in enumerate(zip(new, lens)):
+        if not n or (4 < b < len(lens) - 2):
+            continue
+        toks = sorted({0, n - 1, n // 2} | {int(i) for i in torch.randint(0, n, (6,), generator=g)})
+        for i in toks:  # one new token at the end of a shorter sequence, the same cache
+            p = length - n + i
+            one = ref.Batch.__new__(ref.Batch)
+            one.__dict__.update(B.__dict__, lens=[p + 1], new=[1], cu=[0, 1], table=B.table[b:b + 1], tokens=1)
+            t = B.cu[b] + i
+            want = ref.attention(one, q[t:t + 1], dim ** -0.5, cap, window, slopes)
+            ref.assert_attention(got[t:t + 1], lse[t:t + 1], want, dtype, length, 5.0)
+
+
 def test_prefill_of_one_token_each_is_decode(mc):
     """The same rows through both entry points, each within its bound of the other's sums."""
     B = ref.Batch(EDGES, [1] * len(EDGES), 2, 16, 128, "bf16", 15)
