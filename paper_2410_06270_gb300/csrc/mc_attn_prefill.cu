@@ -113,7 +113,6 @@ struct PfParams {
     int debug;
     int q_boxes;   // a tile's queries are boxes of whole groups of heads (the group divides 128)
     int out32;     // rows of the output start at multiples of 32 bytes
-    int may_queue;  // the batch may have the items for a queue
     int box_rows;  // rows of a copied box: the largest power of two that divides a page, at most a unit
 };
 
@@ -503,7 +502,8 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 
 // ------------------------------------------------------------------ kernel --
 
-template <int D, bool BF16, int MODE>
+// QUEUE: the batch may have the items for a queue (the host's bound), so the kernel looks at them.
+template <int D, bool BF16, int MODE, bool QUEUE>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams pp, const __grid_constant__ CUtensorMap kmap,
                                                                    const __grid_constant__ CUtensorMap vmap,
                                                                    const __grid_constant__ CUtensorMap qmap)
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         int *sums = sh->sums[warp];
         int64_t total = 0;
         PfMix mix = {0, 0, 0};
-        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) total += pf_sums(p, sums, b0, lane, p.status, pp.may_queue ? &mix : nullptr);
+        for (int b0 = 0; b0 < p.b.seqs; b0 += 32) total += pf_sums(p, sums, b0, lane, p.status, QUEUE ? &mix : nullptr);
         total *= p.c.kv_heads;
         const int64_t ctas = total < (int64_t)gridDim.x ? total : gridDim.x;
         // Long prompts have items enough to be dealt one by one, largest first: no pieces to join, and
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         // fewer.  Runs / queue: 3000 tokens, 2.5 items a block, 84 / 73 us, 4096 124 / 105, 8192 378 / 358, four
         // prompts of 2000 142 / 122, six ragged ones on top of a cache 247 / 237.
         bool queued = false;
-        if (pp.may_queue) {
+        if (QUEUE) {
             const int64_t items = (int64_t)__reduce_add_sync(0xffffffffu, mix.items) * p.c.kv_heads;
             const int most = __reduce_max_sync(0xffffffffu, mix.most), first = __reduce_max_sync(0xffffffffu, mix.first);
             queued = items >= kPfQueueItems * ctas && most * ctas <= total && kPfQueueFirst * first * ctas <= total;
@@ -637,7 +637,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 // The block's items.  Where they come from the queue: by falling row tile, then sequence and
                 // key head; the first is that of the block's number, the next ones those that a common
                 // count (zero between calls) gives it.
-                const bool queued = sh->queued;
+                const bool queued = QUEUE && sh->queued;
                 const PfRun run = {sh->b[1], sh->h[1], sh->mt[1], sh->u[1]};
                 int level = 0, above = 0, tiles = 0;  // row tile at hand, items of higher ones; lane: its sequence's
                 auto queue_item = [&](int which, PfItem &x) {
@@ -1141,7 +1141,7 @@ static bool pf_map(CUtensorMap *m, const void *base, bool bf16, int rank, const 
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool BF16, int MODE>
+template <int D, bool BF16, int MODE, bool QUEUE>
 static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st)
 {
     const KvView &c = p.a.c;
@@ -1159,7 +1159,7 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
         qmap = kmap;  // not used
     }
     using Sh = PfShape<D>;
-    auto k = prefill_kernel<D, BF16, MODE>;
+    auto k = prefill_kernel<D, BF16, MODE, QUEUE>;
     static std::atomic<bool> known{false};  // (the same build on every device)
     cudaError_t e = cudaSuccess;
     if (!known.load(std::memory_order_relaxed)) {
@@ -1182,12 +1182,22 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
     return e;
 }
 
+template <int D, bool BF16, int MODE>
+static cudaError_t launch_prefill_q(const PfParams &p, int ctas, cudaStream_t st)
+{
+    // What the lengths decide is the kernel's; where there cannot be items enough, or sequences are
+    // more than the queue takes, one without the queue's code does (9 ragged prompts 32.7 -> 32.2 us).
+    const int64_t items = ((int64_t)p.a.b.tokens * p.a.group / kPfRows + p.a.b.seqs) * p.a.c.kv_heads;  // at most
+    return p.a.b.seqs <= 32 && items >= kPfQueueItems * ctas && items < 1 << 30 ? launch_prefill_t<D, BF16, MODE, true>(p, ctas, st)
+                                                                                : launch_prefill_t<D, BF16, MODE, false>(p, ctas, st);
+}
+
 template <int D, bool BF16>
 static cudaError_t launch_prefill_m(const PfParams &p, int mode, int ctas, cudaStream_t st)
 {
-    return mode == kPfCap    ? launch_prefill_t<D, BF16, kPfCap>(p, ctas, st)
-           : mode == kPfBias ? launch_prefill_t<D, BF16, kPfBias>(p, ctas, st)
-                             : launch_prefill_t<D, BF16, kPfPlain>(p, ctas, st);
+    return mode == kPfCap    ? launch_prefill_q<D, BF16, kPfCap>(p, ctas, st)
+           : mode == kPfBias ? launch_prefill_q<D, BF16, kPfBias>(p, ctas, st)
+                             : launch_prefill_q<D, BF16, kPfPlain>(p, ctas, st);
 }
 
 int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st)
@@ -1208,8 +1218,6 @@ int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st
     cudaError_t e = sm_count(&nsm);
     if (e == cudaSuccess) {
         const int ctas = nsm < kAttnMaxSms ? nsm : kAttnMaxSms;
-        const int64_t items = ((int64_t)a.b.tokens * a.group / kPfRows + a.b.seqs) * a.c.kv_heads;  // at most
-        p.may_queue = a.b.seqs <= 32 && items >= kPfQueueItems * ctas && items < 1 << 30;
         e = head_dim == 64 ? (bf16 ? launch_prefill_m<64, true>(p, mode, ctas, st) : launch_prefill_m<64, false>(p, mode, ctas, st))
                            : (bf16 ? launch_prefill_m<128, true>(p, mode, ctas, st) : launch_prefill_m<128, false>(p, mode, ctas, st));
     }
