@@ -325,8 +325,8 @@ typedef struct {
 } mc_kv_batch;
 
 /* Workspace bytes of the three calls below for a cache and a head count, whatever the
- * batch.  Zeroed once by the caller; the status word comes first.  Calls that share one
- * must not overlap in time. */
+ * batch.  Zeroed once by the caller, then left as the calls leave it; the status word comes
+ * first.  Calls that share one must not overlap in time. */
 size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads);
 
 /* New tokens into the cache, in one pass over their queries, keys and values:
