@@ -18,7 +18,7 @@
 //
 // Measured: 64 sequences of 8192 keys, 32 heads on 8 of 128, 311 us, 6.9 TB/s of keys and values
 // (1.02 of the measured copy rate); one of 131071 keys 83 us, 6.4 TB/s; DRAM bytes 537.1 MB for 536.9
-// (ncu, 16 x 8192).  Short ones are bound by latency: 777 keys 7.4 us, of which the schedule 1, the
+// (ncu, 16 x 8192).  Short ones are bound by latency: 777 keys 7.2 us, of which the schedule 1, the
 // first keys 1.5, the join and its launch 3.
 #include <math.h>
 
@@ -395,7 +395,10 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         }
         if (tid < 8 * NT) rows[tid] = row_of(min(tid, nrows - 1));
         // keys that every row of the slice sees: below the first row's end, from the last's start on
-        const int all_hi = row_of(0).hi, all_lo = row_of(nrows - 1).lo;
+        const Row first_row = row_of(0), last_row = row_of(nrows - 1);
+        const int all_hi = first_row.hi, all_lo = last_row.lo;
+        // (at most 64 keys for all rows: their scores' errors are not left to average out)
+        const bool few_capped = p.cap > 0.f && last_row.hi - first_row.lo <= 64;
         __syncthreads();
         float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -450,7 +453,12 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
                             x[kt][nt][c] = (kChains == 2 ? s[kt][nt][0][c] + s[kt][nt][kChains - 1][c] : s[kt][nt][0][c]) * p.scale;
-                    if (p.cap > 0.f) {
+                    if (few_capped) {
+#pragma unroll
+                        for (int kt = 0; kt < Sh::kTiles; ++kt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) x[kt][nt][c] = capped_exact(x[kt][nt][c], p.cap);
+                    } else if (p.cap > 0.f) {
 #pragma unroll
                         for (int kt = 0; kt < Sh::kTiles; ++kt) {  // two keys of a row share a reciprocal
                             capped2(x[kt][nt][0], x[kt][nt][2], p.cap);

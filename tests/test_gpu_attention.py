@@ -316,6 +316,20 @@ def test_prefill_of_one_token_each_is_decode(mc):
     assert torch.allclose(dl, pl, rtol=1e-4, atol=1e-4)
 
 
+@pytest.mark.parametrize("dim,dtype,cap,lens,new,window", [(128, "bf16", 50.0, [900, 2, 1, 3000], [1] * 4, 2), (64, "fp16", 50.0, [1, 2, 3, 5, 8, 64], [1] * 6, 0),
+                                                           (128, "bf16", 30.0, [4, 3, 70], [4, 2, 3], 3)])
+def test_caps_over_few_keys(mc, dim, dtype, cap, lens, new, window):
+    """With few keys the errors of their scores do not average out: lse to 8 roundings of fp32 (2^-24) of itself or
+    of the largest uncapped term, scores of a few units (products of 128 terms: 16 roundings of those)."""
+    B = ref.Batch(lens, new, 2, 16, dim, dtype, 71)
+    q = B.randn(B.tokens, 6, dim)
+    want = ref.attention(B, q, dim ** -0.5, cap, window)
+    cache, batch = B.device(mc)
+    out, lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=cap, window=window, with_lse=True)
+    ref.assert_attention(out, lse, want, dtype, 3000, 5.0)
+    assert ((lse.double().cpu() - want[1]).abs() <= 24 * 2.0 ** -24 * (1 + want[1].abs())).all()
+
+
 @pytest.mark.parametrize("dim,dtype,cap,spread", [(128, "bf16", 2.0, 1.0), (64, "fp16", 0.5, 3.0), (128, "fp16", 40.0, 1.5), (64, "bf16", 8.0, 2.0)])
 def test_caps_far_below_and_around_the_scores(mc, dim, dtype, cap, spread):
     """Scores from a fraction of the cap to many times it: both of the cap's forms, in every kernel."""
