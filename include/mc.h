@@ -315,7 +315,8 @@ typedef struct {
  * appended and sees no key.  Rows from cu_q[seqs] on are padding: nothing of theirs is
  * read or written.  table[b * table_width + i], i < ceil(lens[b] / page_size), are b's
  * pages; other entries are not read.  A page outside [0, num_pages) (its rows are not
- * written, and read as zeros), a length beyond table_width pages (cut to them), a cu_q that
+ * written, and read as zeros), a length beyond table_width pages (cut to them by the attentions;
+ * the append keeps the positions that it gives and writes no token past the pages), a cu_q that
  * descends or passes tokens (that sequence has no tokens) and a position outside the rope
  * table (as none) are recorded as MC_ERR_RANGE in the workspace's status word
  * (mc_check_status). */

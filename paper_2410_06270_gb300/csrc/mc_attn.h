@@ -82,14 +82,20 @@ struct AppendParams {
     int32_t *status;
 };
 
+// Keys that a row of the page table has pages for.
+__device__ __forceinline__ int seq_room(const BatchView &bv, const KvView &c)
+{
+    const int64_t room = (int64_t)bv.table_width * c.page_size;
+    return (int)(room < kMaxLen ? room : kMaxLen);
+}
+
 // Length of sequence b, cut to what its table row can hold.
 __device__ __forceinline__ int seq_len(const BatchView &bv, const KvView &c, int b, int32_t *status)
 {
-    const int len = __ldg(bv.lens + b);
-    const int64_t room = (int64_t)bv.table_width * c.page_size, cap = room < kMaxLen ? room : kMaxLen;
-    if (len > cap) {
+    const int len = __ldg(bv.lens + b), room = seq_room(bv, c);
+    if (len > room) {
         set_status(status, MC_ERR_RANGE);
-        return (int)cap;
+        return room;
     }
     return len < 0 ? 0 : len;
 }
@@ -158,12 +164,20 @@ __device__ __forceinline__ int token_seq(const BatchView &bv, int t, int lane)
 }
 
 // Where token row t is.  Up to 31 sequences every lane reads one boundary and one length, so
-// that all comes with one memory round trip; more are searched.
+// that all comes with one memory round trip; more are searched.  Positions follow from lengths
+// that are not cut: a token that its table row has no page for has no position, and the ones
+// before it keep theirs.
+__device__ __forceinline__ int placed(const BatchView &bv, const KvView &c, int pos, int32_t *status)
+{
+    if (pos < seq_room(bv, c)) return pos;
+    set_status(status, MC_ERR_RANGE);
+    return -1;
+}
 __device__ __forceinline__ TokenPlace token_place(const BatchView &bv, const KvView &c, int t, int lane, int32_t *status)
 {
     if (bv.cu_q && bv.seqs < 32) {
         const int cu = lane <= bv.seqs ? __ldg(bv.cu_q + lane) : 0x7fffffff;
-        const int mine = lane < bv.seqs ? seq_len(bv, c, lane, status) : 0;
+        const int mine = lane < bv.seqs ? max(0, __ldg(bv.lens + lane)) : 0;
         const int s = __popc(__ballot_sync(0xffffffffu, lane > 0 && lane <= bv.seqs && cu <= t));
         const int first = __shfl_sync(0xffffffffu, cu, s), end = __shfl_sync(0xffffffffu, cu, s + 1 < 32 ? s + 1 : 31);
         const int len = __shfl_sync(0xffffffffu, mine, s);
@@ -172,13 +186,13 @@ __device__ __forceinline__ TokenPlace token_place(const BatchView &bv, const KvV
             set_status(status, MC_ERR_RANGE);
             return {s, -1};
         }
-        return {s, len - (end - first) + (t - first)};
+        return {s, placed(bv, c, len - (end - first) + (t - first), status)};
     }
     const int s = token_seq(bv, t, lane);
     if (s < 0) return {-1, -1};
     int first;
-    const int n = seq_rows(bv, s, first, status), len = seq_len(bv, c, s, status);
-    return {s, t >= first && t - first < n ? len - n + (t - first) : -1};
+    const int n = seq_rows(bv, s, first, status), len = max(0, __ldg(bv.lens + s));
+    return {s, t >= first && t - first < n ? placed(bv, c, len - n + (t - first), status) : -1};
 }
 
 template <bool BF16>

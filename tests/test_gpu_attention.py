@@ -501,6 +501,34 @@ def test_a_descending_cu_q_stays_within_the_tables(mc, many):
     assert written <= {int(i) for i in B.table.flatten()}
 
 
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("new,over", [([1, 1], 1), ([1, 1], 40), ([5, 3], 2), ([5, 3], 30)])
+def test_an_overlong_length_moves_no_token(mc, new, over, many):
+    """A length past the page table's rows: the tokens that its pages hold go where that length
+    puts them, the others nowhere, and no row of another token is touched."""
+    fill = 40 if many else 0  # (idle slots: more sequences than a warp looks at at once)
+    B = ref.Batch([64, 40] + [0] * fill, new + [0 if sum(new) > 2 else 1] * fill, 2, 16, 64, "bf16", 26)
+    cache, _ = B.device(mc)
+    ragged = sum(new) > 2
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32).cuda()  # noqa: E731
+    batch = mc.KVBatch(i32([64 + over, 40] + [0] * fill), B.table.cuda(), i32(B.cu) if ragged else None, B.tokens if ragged else None)
+    q, k, v = (B.randn(B.tokens, n, 64) for n in (4, 2, 2))
+    ws = mc.attn_workspace(cache, 4)
+    got = mc.kv_append(cache, batch, q.cuda(), k.cuda(), v.cuda(), workspace=ws)
+    with pytest.raises(mc.MCError) as e:
+        mc.check_status(ws)
+    assert e.value.code == mc.ERR_RANGE
+    want_k, want_v, want_q = B.k.clone(), B.v.clone(), torch.zeros_like(q)
+    for b, (n, length) in enumerate(zip(B.new, [64 + over, 40] + [0] * fill)):
+        for i in range(n):
+            pos, t = length - n + i, B.cu[b] + i
+            if 0 <= pos < 64:
+                page, row = int(B.table[b, pos // 16]), pos % 16
+                want_k[page, :, row], want_v[page, :, row], want_q[t] = k[t], v[t], q[t]
+    for a, w in ((cache.k, want_k), (cache.v, want_v), (got, want_q)):
+        assert torch.equal(a.cpu().view(torch.int16), w.view(torch.int16))
+
+
 def test_prefill_waits_expire_and_the_context_lives(mc):
     """With the copies switched off every wait of the kernel reaches its bound."""
     B = ref.Batch([300], [300], 1, 16, 64, "bf16", 23)
