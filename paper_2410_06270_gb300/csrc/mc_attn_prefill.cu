@@ -79,6 +79,7 @@ struct PfShared {
     uint64_t drain, vpatch;
     uint32_t tmem_base;
     volatile int abort;
+    int odd;                                             // a finished row came out infinite or NaN
     int b[2], h[2], mt[2], u[2];                         // where this CTA's run starts and ends
     int off;                                             // the end's cost offset in its item
     int run;                                             // cost of a run
@@ -108,6 +109,7 @@ struct PfOpen;
 struct PfParams {
     AttnParams a;
     PfOpen *open;
+    int32_t *odd;  // of each CTA: whether a row that it finished came out infinite or NaN
     float *part;
     uint64_t timeout_ns;
     int debug;
@@ -532,7 +534,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
             mbar_init(&sh->ofull[t], 1);
         }
         mbar_init(&sh->drain, 2);
-        sh->abort = 0;
+        sh->abort = sh->odd = 0;
         fence_mbar_init();
     }
     if (warp == kPfMma) tmem_alloc(&sh->tmem_base, 512);
@@ -1016,12 +1018,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         p.lse[(int64_t)(first + tok) * p.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
                     if (live && !whole)
                         reinterpret_cast<float2 *>(mine + kPfRows * D)[t * kPfTile + row] = make_float2(m, l);
-                    __syncwarp();  // (a row's stores above come before another lane's below)
-                    for (unsigned which = __ballot_sync(0xffffffffu, odd != odd); which; which &= which - 1) {
-                        const int r = __ffs(which) - 1;
-                        const int tr = __shfl_sync(0xffffffffu, tok, r), hr = __shfl_sync(0xffffffffu, head, r);
-                        exact_row<D, BF16>(p, it->b, it->s.len - it->s.n + tr, it->s.len, it->s.prefix, first + tr, hr, lane);
-                    }
+                    // (redone by the join launch: here the other roles would wait for a row's keys, one by
+                    // one, for longer than their waits last)
+                    if (odd != odd) sh->odd = 1;
                 }
                 tc_fence_before();
             }
@@ -1043,6 +1042,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 
     tc_fence_before();
     __syncthreads();
+    if (tid == 0) pp.odd[blockIdx.x] = sh->odd;
     if (warp == kPfMma) {
         tc_fence_after();
         tmem_dealloc(sh->tmem_base, 512);
@@ -1053,17 +1053,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 // in flight at once.
 constexpr int kPfJoinRows = 16;
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
+__device__ __forceinline__ void pf_join(const PfParams &pp, const PfOpen &it)
 {
     constexpr int kQuads = D / 4 / 16;  // column quads of a thread: threadIdx.x / 16, + 16, ...
     __shared__ float2 ml[kAttnMaxSms][kPfJoinRows];
     __shared__ int odd[kPfJoinRows];
     const AttnParams &p = pp.a;
-    pdl_trigger();
-    pdl_wait();
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.status[kPfCount] = 0;
-    const PfOpen it = pp.open[blockIdx.x];
-    if (it.pieces == 0) return;
     const int r = threadIdx.x % kPfJoinRows, c0 = threadIdx.x / kPfJoinRows, row = blockIdx.y * kPfJoinRows + r;
     auto piece = [&](int i) { return pp.part + (2 * ((size_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * pf_part_floats(D); };
     for (int i = c0; i < it.pieces; i += 16) ml[i][r] = reinterpret_cast<const float2 *>(piece(i) + kPfRows * D)[row];
@@ -1116,9 +1111,60 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const PfParams pp)
     }
 }
 
+// Rows of whole items that came out infinite or NaN, redone by the definition: the launch's blocks
+// take the items' rows, kPfRedoRows at a time, in turn.  An open item's rows are its join's.
+constexpr int kPfRedoRows = 32;
+template <int D, bool BF16>
+__device__ __noinline__ void pf_redo(const PfParams &pp)
+{
+    const AttnParams &p = pp.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int grid = gridDim.x * gridDim.y;
+    int turn = blockIdx.y * gridDim.x + blockIdx.x;  // this block's next slice, counted from the sequence's first
+    for (int b = 0; b < p.b.seqs; ++b) {
+        const PfSeq s = pf_seq(p, b, nullptr);
+        const int tiles = pf_tiles(p, s), slices = tiles * p.c.kv_heads * (kPfRows / kPfRedoRows);
+        for (; turn < slices; turn += grid) {
+            const int item = turn / (kPfRows / kPfRedoRows), h = item / tiles, mt = item - h * tiles;
+            const int r0 = mt * kPfRows + turn % (kPfRows / kPfRedoRows) * kPfRedoRows, rows = min(kPfRedoRows, s.n * p.group - r0);
+            const PfOpen o = threadIdx.x < gridDim.x ? pp.open[threadIdx.x] : PfOpen{0, 0, 0, 0};
+            if (__syncthreads_or(o.pieces && o.b == b && o.h == h && o.mt == mt)) continue;
+            for (int r = warp; r < rows; r += 8) {
+                int hg;
+                const int tok = p.by_group.div(r0 + r, hg), head = h * p.group + hg;
+                const uint16_t *out = p.out + (s.first + tok) * p.out_stride + head * D;
+                float odd = 0.f;
+#pragma unroll
+                for (int d = 2 * lane; d < D; d += 64) {
+                    const float2 v = unpack2<BF16>(*reinterpret_cast<const uint32_t *>(out + d));
+                    odd = fmaf(v.x, 0.f, fmaf(v.y, 0.f, odd));
+                }
+                if (__any_sync(0xffffffffu, odd != odd))
+                    exact_row<D, BF16>(p, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
+            }
+        }
+        turn -= slices;
+    }
+}
+
+// (most blocks have nothing to add: with the 62 registers that heads of 64 take unbounded, four
+// blocks an SM, the launch is 0.6 us longer)
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256, D == 64 ? 5 : 4) prefill_join_kernel(const PfParams pp)
+{
+    pdl_trigger();
+    pdl_wait();
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) pp.a.status[kPfCount] = 0;
+    const PfOpen it = pp.open[blockIdx.x];
+    const bool redo = __syncthreads_or(threadIdx.x < gridDim.x && pp.odd[threadIdx.x]);
+    if (it.pieces) pf_join<D, BF16>(pp, it);
+    if (redo) pf_redo<D, BF16>(pp);
+}
+static_assert(kAttnMaxSms <= 256, "a thread per CTA of the first launch");
+
 size_t prefill_part_bytes(int head_dim)
 {
-    return kAttnMaxSms * (sizeof(PfOpen) + 2 * 4 * pf_part_floats(head_dim));
+    return kAttnMaxSms * (sizeof(PfOpen) + sizeof(int32_t) + 2 * 4 * pf_part_floats(head_dim));
 }
 
 // A tensor map of 16-bit elements in boxes of 64 columns, with the 128-byte swizzle.
@@ -1207,7 +1253,8 @@ int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st
     PfParams p;
     p.a = a;
     p.open = reinterpret_cast<PfOpen *>(a.part);
-    p.part = reinterpret_cast<float *>(a.part + kAttnMaxSms * sizeof(PfOpen));
+    p.odd = reinterpret_cast<int32_t *>(p.open + kAttnMaxSms);
+    p.part = reinterpret_cast<float *>(p.odd + kAttnMaxSms);
     p.timeout_ns = wait_bound_ns();
     p.debug = debug_flags();
     p.q_boxes = kPfTile % a.group == 0 && a.q_stride < (int64_t)1 << 38;

@@ -529,6 +529,36 @@ def test_an_overlong_length_moves_no_token(mc, new, over, many):
         assert torch.equal(a.cpu().view(torch.int16), w.view(torch.int16))
 
 
+@pytest.mark.parametrize("seqs,new,length,kv,heads", [(90, 64, 2000, 2, 8), (2, 3000, 3000, 8, 16)])  # runs, and a queue
+def test_rows_redone_do_not_hold_the_others_up(mc, seqs, new, length, kv, heads):
+    """A value that only a sequence's last token sees is infinite: the rows that share its units are
+    redone, which takes far longer than a wait of the pipeline may last, here 3 ms.  Against the same
+    batch with a zero there: each side is within 2 * 2^-8 + 1e-4 of the mean |v|, which is below 5, and
+    lse within 1e-4."""
+    B = ref.Batch([length] * seqs, [new] * seqs, kv, 64, 64, "bf16", 81)
+    q = B.randn(B.tokens, heads, 64).cuda()
+    ws = None
+    got = []
+    for what in (0.0, float("inf")):
+        for b in range(0, seqs, 2):
+            B.v[B.table[b, (length - 1) // 64], :, (length - 1) % 64, 9] = what
+        cache, batch = B.device(mc)
+        ws = mc.attn_workspace(cache, heads) if ws is None else ws
+        mc.set_debug(0, 3_000_000)
+        try:
+            out, lse = mc.attn_prefill(cache, batch, q, out=torch.full_like(q, 100.0), with_lse=True, workspace=ws)
+            mc.check_status(ws)
+        finally:
+            mc.set_debug(0, 1_000_000_000)
+        got.append((out.float().view(seqs, new, heads, 64), lse.view(seqs, new, heads)))
+    (want, want_lse), (out, lse) = got
+    assert torch.isposinf(out[0::2, -1, :, 9]).all()
+    out[0::2, -1, :, 9] = want[0::2, -1, :, 9] = 0
+    assert torch.isfinite(out).all()
+    assert ((out - want).abs() <= 2 * (2 * 2.0 ** -8 + 1e-4) * 5).all()
+    assert torch.allclose(lse, want_lse, rtol=2e-4, atol=2e-4)
+
+
 def test_prefill_waits_expire_and_the_context_lives(mc):
     """With the copies switched off every wait of the kernel reaches its bound."""
     B = ref.Batch([300], [300], 1, 16, 64, "bf16", 23)
