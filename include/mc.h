@@ -367,7 +367,8 @@ typedef struct {
  *   out [token][q_heads][head_dim] (token stride out_stride) = softmax over the visible keys . v
  *   lse fp32 [tokens][q_heads] (may be NULL): log of the sum of exponentials
  * A query that sees no key gets a zero row and lse = -inf.  Keys that a query does not see do
- * not reach its row, whatever they hold, infinities and NaN included.  Scores, statistics and sums
+ * not reach its row, whatever they hold, infinities and NaN included; one that it sees does (a
+ * weight that rounds to zero times an infinite value is NaN).  Scores, statistics and sums
  * are fp32; the probabilities are rounded to the cache's dtype for their product with v.
  * mc_attn_decode takes one new token per sequence (cu_q NULL), mc_attn_prefill any number.
  * out must not overlap q.  MC_ERR_UNSUPPORTED: more work in one call than the schedule counts, with

@@ -292,10 +292,36 @@ __device__ __forceinline__ void capped2(float &x, float &y, float top)
 
 int launch_append(AppendParams p, int head_dim, bool bf16, cudaStream_t st);
 
+// Whether a key or value in the rows [from, to) of head h of sequence b is infinite or NaN.
+// `warps` warps look, 16 rows at a time each, this one as number `warp`; the answer is the warp's.
+template <int D, bool BF16>
+__device__ __noinline__ bool odd_keys(const AttnParams &p, int b, int h, int from, int to, int warp, int warps, int lane)
+{
+    constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;  // infinities and NaN have the exponent's bits all set
+    bool odd = false;
+    for (int j = (from & ~15) + 16 * warp; j < to; j += 16 * warps) {
+        int row;
+        const int i = p.c.page.div(j, row), page = seq_page(p.b, p.c, b, i, nullptr);
+        if (page < 0) continue;
+        const int64_t at = page * p.c.page_stride + ((int64_t)h * p.c.page_size + row) * D;
+#pragma unroll 2
+        for (int c = lane; c < 2 * D; c += 32) {  // 16-byte chunks of the 16 rows
+            const int r = j + c / (D / 8);
+            if (r < from || r >= to) continue;
+            const uint4 k = *reinterpret_cast<const uint4 *>(p.c.k + at + 8 * c), v = *reinterpret_cast<const uint4 *>(p.c.v + at + 8 * c);
+            const uint32_t w[8] = {k.x, k.y, k.z, k.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) odd |= (w[e] & kExp) == kExp || (w[e] >> 16 & kExp) == kExp;
+        }
+    }
+    return __any_sync(0xffffffffu, odd);
+}
+
 // One row by the definition, by a warp, key by key: what the kernels fall back to for a row
-// whose sum came out infinite or NaN.  They multiply hidden keys' values by weights of 0, which
-// an infinite or NaN value survives; here a hidden key is not touched.  (Slow, and meant to be:
-// finite caches never come here.)
+// whose sum came out infinite or NaN and which hides a key that is.  They multiply hidden keys'
+// values by weights of 0, which an infinite or NaN value survives; here a hidden key is not
+// touched.  Where the keys that it hides are finite, the row is what those that it sees make it,
+// and stays.  (Slow, and meant to be: finite caches never come here.)
 template <int D, bool BF16>
 __device__ __noinline__ void exact_row(const AttnParams &p, int b, int pos, int len, int prefix, int token, int head, int lane)
 {

@@ -151,6 +151,18 @@ struct Row {
     float slope;
 };
 
+// Token tok of sequence b's, head `head`: a row that came out infinite or NaN, redone if a key of the
+// sequence's units that it hides is.
+template <int D, bool BF16>
+__device__ __noinline__ void redo_row(const AttnParams &p, int b, int tok, int head, int lane)
+{
+    const Keys k = keys_of<D>(p, b, nullptr);
+    const int h = p.by_group.div(head), pos = k.len - k.n + tok, prefix = p.prefix ? __ldg(p.prefix + b) : 0;
+    const int lo = p.window ? max(0, pos - p.window + 1) : 0, hi = pos < 0 ? 0 : max(pos + 1, prefix);
+    if (odd_keys<D, BF16>(p, b, h, k.start, min(lo, k.len), 0, 1, lane) || odd_keys<D, BF16>(p, b, h, max(hi, k.start), k.len, 0, 1, lane))
+        exact_row<D, BF16>(p, b, pos, k.len, prefix, k.first + tok, head, lane);
+}
+
 __host__ __device__ constexpr size_t dec_part_floats(int D, int nt) { return (size_t)8 * nt * (D + 2); }
 
 // Four elements of a finished row, and its lse with the first; a row without keys is zero.
@@ -606,7 +618,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                 if (!marks[r]) continue;
                 int hg;
                 const int tok = p.by_group.div(r0 + r, hg);
-                exact_row<D, BF16>(p, at.b, p0 + tok, keys.len, prefix, keys.first + tok, h0 + hg, lane);
+                redo_row<D, BF16>(p, at.b, tok, h0 + hg, lane);
             }
             __syncthreads();
         }
@@ -640,7 +652,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 // One CTA per (CTA of the pass before, row of a slice): adds the pieces of that CTA's open
 // item in their order.
 template <int D, bool BF16>
-__global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const OpenItem *open, const float *part, int nt)
+__global__ void __launch_bounds__(128, 12) join_kernel(const AttnParams p, const OpenItem *open, const float *part, int nt)
 {
     constexpr int kCols = D / 4, kGroups = 128 / kCols;
     __shared__ float red[4], sums[kGroups];
@@ -691,10 +703,7 @@ __global__ void __launch_bounds__(128) join_kernel(const AttnParams p, const Ope
         store_row<BF16>(p, first + tok, it.h * p.group + hg, D, 4 * col, acc, top, sum);
         odd = n > 1 && !finite4(acc);
     }
-    if (__syncthreads_or(odd) && tid < 32) {
-        const int len = seq_len(p.b, p.c, it.b, nullptr);
-        exact_row<D, BF16>(p, it.b, len - n + tok, len, p.prefix ? __ldg(p.prefix + it.b) : 0, first + tok, it.h * p.group + hg, tid);
-    }
+    if (__syncthreads_or(odd) && tid < 32) redo_row<D, BF16>(p, it.b, tok, it.h * p.group + hg, tid);
 }
 
 constexpr int kDecMaxCtas = kDecCtasPerSm * kAttnMaxSms;

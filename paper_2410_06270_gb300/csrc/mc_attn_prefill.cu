@@ -1049,9 +1049,34 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
     }
 }
 
+// Whether a key that was copied for an item, and that one of its tokens t0 .. t1 hides, is infinite or
+// NaN: by `warps` warps, the answer the warp's.
+template <int D, bool BF16>
+__device__ __forceinline__ bool pf_hides_odd(const PfParams &pp, int b, int h, int mt, const PfSeq &s, int t0, int t1, int warp, int warps,
+                                             int lane)
+{
+    const AttnParams &p = pp.a;
+    const PfKeys k = pf_keys(p, s, mt);
+    const int from = k.first & -pp.box_rows, to = min(s.len, (k.end + pp.box_rows - 1) & -pp.box_rows);  // whole boxes
+    const int p0 = s.len - s.n + t0, p1 = s.len - s.n + t1;
+    const int lo = p.window ? max(0, p1 - p.window + 1) : 0, hi = p0 < 0 ? 0 : max(p0 + 1, s.prefix);
+    return odd_keys<D, BF16>(p, b, h, from, min(lo, to), warp, warps, lane) ||
+           odd_keys<D, BF16>(p, b, h, max(hi, from), to, warp, warps, lane);
+}
+
+constexpr int kPfJoinRows = 16;  // rows of an open item that a block of the join launch adds
+
+// A row that came out infinite or NaN, redone if it hides a key that is.
+template <int D, bool BF16>
+__device__ __noinline__ void pf_redo_row(const PfParams &pp, int b, int mt, int tok, int head, int lane)
+{
+    const PfSeq s = pf_seq(pp.a, b, nullptr);
+    if (pf_hides_odd<D, BF16>(pp, b, pp.a.by_group.div(head), mt, s, tok, tok, 0, 1, lane))
+        exact_row<D, BF16>(pp.a, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
+}
+
 // 16 rows of a CTA's open item: adds its pieces in their order, the loads of four pieces
 // in flight at once.
-constexpr int kPfJoinRows = 16;
 template <int D, bool BF16>
 __device__ __forceinline__ void pf_join(const PfParams &pp, const PfOpen &it)
 {
@@ -1107,12 +1132,13 @@ __device__ __forceinline__ void pf_join(const PfParams &pp, const PfOpen &it)
         if (!odd[x]) continue;
         int g2;
         const int t2 = p.by_group.div(it.mt * kPfRows + blockIdx.y * kPfJoinRows + x, g2);
-        exact_row<D, BF16>(p, it.b, s.len - s.n + t2, s.len, s.prefix, s.first + t2, it.h * p.group + g2, threadIdx.x & 31);
+        pf_redo_row<D, BF16>(pp, it.b, it.mt, t2, it.h * p.group + g2, threadIdx.x & 31);
     }
 }
 
-// Rows of whole items that came out infinite or NaN, redone by the definition: the launch's blocks
-// take the items' rows, kPfRedoRows at a time, in turn.  An open item's rows are its join's.
+// Rows of whole items that came out infinite or NaN and hide a key that is, redone by the definition: the
+// launch's blocks take the items' rows, kPfRedoRows at a time, in turn.  An open item's rows are its join's.
+// A prompt of 4096 tokens, every row of which sees a NaN, takes 135 us instead of 112 (115 ms with every row redone).
 constexpr int kPfRedoRows = 32;
 template <int D, bool BF16>
 __device__ __noinline__ void pf_redo(const PfParams &pp)
@@ -1128,7 +1154,9 @@ __device__ __noinline__ void pf_redo(const PfParams &pp)
             const int item = turn / (kPfRows / kPfRedoRows), h = item / tiles, mt = item - h * tiles;
             const int r0 = mt * kPfRows + turn % (kPfRows / kPfRedoRows) * kPfRedoRows, rows = min(kPfRedoRows, s.n * p.group - r0);
             const PfOpen o = threadIdx.x < gridDim.x ? pp.open[threadIdx.x] : PfOpen{0, 0, 0, 0};
-            if (__syncthreads_or(o.pieces && o.b == b && o.h == h && o.mt == mt)) continue;
+            if (__syncthreads_or(o.pieces && o.b == b && o.h == h && o.mt == mt) || rows <= 0) continue;
+            if (!__syncthreads_or(pf_hides_odd<D, BF16>(pp, b, h, mt, s, p.by_group.div(r0), p.by_group.div(r0 + rows - 1), warp, 8, lane)))
+                continue;
             for (int r = warp; r < rows; r += 8) {
                 int hg;
                 const int tok = p.by_group.div(r0 + r, hg), head = h * p.group + hg;
@@ -1156,9 +1184,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 5 : 4) prefill_join_kernel(cons
     pdl_wait();
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) pp.a.status[kPfCount] = 0;
     const PfOpen it = pp.open[blockIdx.x];
-    const bool redo = __syncthreads_or(threadIdx.x < gridDim.x && pp.odd[threadIdx.x]);
+    const bool odd = __builtin_expect(__syncthreads_or(threadIdx.x < gridDim.x && pp.odd[threadIdx.x]), 0);
     if (it.pieces) pf_join<D, BF16>(pp, it);
-    if (redo) pf_redo<D, BF16>(pp);
+    if (odd) pf_redo<D, BF16>(pp);
 }
 static_assert(kAttnMaxSms <= 256, "a thread per CTA of the first launch");
 

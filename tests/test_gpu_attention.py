@@ -559,6 +559,39 @@ def test_rows_redone_do_not_hold_the_others_up(mc, seqs, new, length, kv, heads)
     assert torch.allclose(lse, want_lse, rtol=2e-4, atol=2e-4)
 
 
+@pytest.mark.parametrize("seqs,new,length,heads,kv", [(1, 4096, 4096, 16, 4),   # whole items
+                                                      (1, 300, 9000, 8, 2),     # split and joined
+                                                      (16, 4, 4000, 16, 4)])    # few rows a sequence
+def test_a_visible_nan_costs_little(mc, seqs, new, length, heads, kv):
+    """A NaN that every row sees: their results are NaN there as they come, none is redone key by
+    key.  (Ten times a finite call's time; redone, it is a hundred times and more.)"""
+    B = ref.Batch([length] * seqs, [new] * seqs, kv, 64, 128, "bf16", 83)
+    q = B.randn(B.tokens, heads, 128).cuda()
+    ws, took, got = None, [], []
+    for what in (0.0, float("nan")):
+        for b in range(seqs):
+            B.v[B.table[b, 0], :, 0, 3] = what
+        cache, batch = B.device(mc)
+        ws = mc.attn_workspace(cache, heads) if ws is None else ws
+        out = torch.full_like(q, 100.0)
+        call = lambda: mc.attn_prefill(cache, batch, q, out=out, workspace=ws)  # noqa: E731
+        for _ in range(3):
+            call()
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
+        for _ in range(10):
+            call()
+        end.record()
+        mc.check_status(ws)
+        torch.cuda.synchronize()
+        took.append(start.elapsed_time(end) / 10)
+        got.append(out)
+    assert torch.isnan(got[1][..., 3]).all()
+    got[1][..., 3] = got[0][..., 3]
+    assert torch.equal(got[0], got[1])
+    assert took[1] <= 10 * took[0], took
+
+
 def test_prefill_waits_expire_and_the_context_lives(mc):
     """With the copies switched off every wait of the kernel reaches its bound."""
     B = ref.Batch([300], [300], 1, 16, 64, "bf16", 23)
