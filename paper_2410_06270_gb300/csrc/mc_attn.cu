@@ -106,7 +106,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     int rc = check_cache(cache, q_heads);
     if (rc || (rc = check_counts(batch))) return rc;
     if (!o) return set_error(MC_ERR_INVALID_ARG, "NULL options");
-    // (the scale, its product with log2 e and its quotient by the cap, stay in fp32's range)
+    // (the scale, its product with log2 e and its quotient by the cap stay in fp32's range)
     if (!(o->scale >= 1e-18f) || !(o->scale <= 1e18f) || !(o->softcap == 0.f || (o->softcap >= 1e-18f && o->softcap <= 1e18f)) ||
         o->window < 0)
         return set_error(MC_ERR_INVALID_ARG, "scale %g, softcap %g, window %d", o->scale, o->softcap, o->window);
@@ -133,7 +133,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     p.group = q_heads / cache->kv_heads;
     p.by_group = FastDiv(p.group);
     p.cap = o->softcap * kLog2e;
-    p.scale = o->softcap > 0.f ? o->scale / o->softcap * (2.f * kLog2e) : o->scale * kLog2e;
+    p.scale = o->softcap > 0.f ? o->scale / o->softcap : o->scale * kLog2e;
     p.window = o->window >= kMaxLen ? 0 : o->window;  // no length passes kMaxLen
     p.slopes = o->slopes;
     p.prefix = o->prefix;

@@ -9,6 +9,7 @@ namespace mc {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kTanhOne = 8.5f;  // from here on tanh is 1
 constexpr int kMaxLen = 1 << 30;  // keys of a sequence, so that positions and windows stay in 32 bits
 
 // Division of 0 .. 2^31 - 1 by a number fixed for the call: the high product is the quotient
@@ -55,7 +56,7 @@ struct AttnParams {
     int64_t q_stride;
     int q_heads, group;  // group = q_heads / kv_heads
     FastDiv by_group;
-    float scale;         // q . k in units of log 2; with a cap: in the units of capped()
+    float scale;         // q . k in units of log 2; with a cap: of the cap
     float cap;           // the cap in units of log 2; 0: none
     int window;          // 0: none
     const float *slopes;
@@ -260,34 +261,57 @@ __device__ __forceinline__ float rcp(float x)
     return r;
 }
 
-__device__ __forceinline__ float min_nan(float a, float b)
+// y within [-kTanhOne, kTanhOne]; NaN stays.
+__device__ __forceinline__ float clamped(float y)
 {
     float r;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    asm("{\n\t.reg .f32 t;\n\tmin.NaN.f32 t, %1, %2;\n\tmax.NaN.f32 %0, t, %3;\n\t}" : "=f"(r) : "f"(y), "f"(kTanhOne), "f"(-kTanhOne));
     return r;
 }
 
-// top * tanh(x / 2 log2 e), as top - 2 top / (1 + 2^x): off by a few units of fp32 of the cap
-// (tanh.approx, at 2^-11, would move a score of 20 by 0.01, a probability by 1 %).  x stops at
-// 60, where tanh is 1.
-__device__ __forceinline__ float capped(float x, float top) { return fmaf(rcp(1.f + ex2(min_nan(x, 60.f))), -2.f * top, top); }
-// The same to fp32's relative precision: below tanh's 3/4, where the difference above cancels, y times a
-// polynomial in y^2 (a least-squares fit on Chebyshev nodes, off by 1.6e-7).  For rows that see few
-// keys, where the errors above, some 2^-24 of the cap, do not average out: two keys under a cap of
-// 50, lse off by 6e-6.
-__device__ __forceinline__ float capped_exact(float x, float top)
+// top * tanh(y), as top * y P(y^2) / Q(y^2) with polynomials of degree 4 that start at 1 (a fit of
+// tanh(y) / y on Chebyshev nodes over |y| <= 8.5, its relative error evened out by reweighting:
+// 1.3e-8; beyond, tanh is 1 to fp32), for two scores with one reciprocal, that of the denominators'
+// product (at most 1.6e5).  In fp32 off by 4.3e-7 of the result at most and 9e-8 in the mean, however
+// large the cap: formed from 2^x, as 1 - 2 / (1 + 2^x), it is off by 2^-23 of the cap, a score of 1.5
+// under a cap of 10^6 by 0.2.  (tanh.approx, at 2^-11, would move a score of 20 by 0.01.)
+// A NaN in either makes both NaN.
+__device__ __forceinline__ uint64_t capped2(uint64_t y2, float top)
 {
-    const float y = 0.5f * kLn2 * x, u = y * y;
-    const float t = fmaf(fmaf(fmaf(fmaf(fmaf(-4.723952e-3f, u, 1.9593786e-2f), u, -5.334982e-2f), u, 0.13325515f), u, -0.33332968f), u, 1.f);
-    return fabsf(y) < 0.75f ? top * y * t : capped(x, top);
+    constexpr float P[4] = {0.134158394f, 3.53705402e-3f, 2.12989525e-5f, 1.43323659e-8f};
+    constexpr float Q[4] = {0.467491656f, 2.60343995e-2f, 3.35373107e-4f, 8.17163198e-7f};
+    float a, b;
+    unpair2(y2, a, b);
+    const uint64_t y = pair2(clamped(a), clamped(b)), u = mul2(y, y), one = pair2(1.f, 1.f);
+    uint64_t n = pair2(P[3], P[3]), d = pair2(Q[3], Q[3]);
+#pragma unroll
+    for (int i = 2; i >= 0; --i) {
+        n = fma2(n, u, pair2(P[i], P[i]));
+        d = fma2(d, u, pair2(Q[i], Q[i]));
+    }
+    n = mul2(fma2(n, u, one), y);
+    d = fma2(d, u, one);
+    unpair2(d, a, b);
+    const float r = top * rcp(a * b);
+    return mul2(n, mul2(pair2(b, a), pair2(r, r)));
 }
-// Two scores, one reciprocal for both (that of the denominators' product).  A NaN in either
-// makes both NaN.
-__device__ __forceinline__ void capped2(float &x, float &y, float top)
+// The same for |y| <= 3/4, as top * y R(y^2) with a polynomial of degree 5 (fitted the same way, 3.3e-8;
+// in fp32 1.3e-7 at most).
+constexpr float kTanhNear = 0.75f;
+__device__ __forceinline__ uint64_t capped2_near(uint64_t y, float top)
 {
-    const float a = 1.f + ex2(min_nan(x, 60.f)), b = 1.f + ex2(min_nan(y, 60.f)), r = -2.f * top * rcp(a * b);
-    x = fmaf(r, b, top);
-    y = fmaf(r, a, top);
+    constexpr float R[5] = {-0.333330684f, 0.133265212f, -5.33902597e-2f, 1.96649155e-2f, -4.76949155e-3f};
+    const uint64_t u = mul2(y, y);
+    uint64_t r = pair2(R[4], R[4]);
+#pragma unroll
+    for (int i = 3; i >= 0; --i) r = fma2(r, u, pair2(R[i], R[i]));
+    return mul2(mul2(fma2(r, u, pair2(1.f, 1.f)), y), pair2(top, top));
+}
+__device__ __forceinline__ float capped(float y, float top)
+{
+    float a, b;
+    unpair2(capped2(pair2(y, y), top), a, b);
+    return a;
 }
 
 int launch_append(AppendParams p, int head_dim, bool bf16, cudaStream_t st);
@@ -352,7 +376,7 @@ __device__ __noinline__ void exact_row(const AttnParams &p, int b, int pos, int 
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
         x *= p.scale;
-        if (p.cap > 0.f) x = capped_exact(x, p.cap);
+        if (p.cap > 0.f) x = capped(x, p.cap);
         x = fmaf(slope, (float)(j - pos), x);
         const float top = fmaxf(m, x), keep = top == m ? 1.f : ex2(m - top), pr = x == -INFINITY ? 0.f : ex2(x - top);
         m = top;

@@ -407,10 +407,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         }
         if (tid < 8 * NT) rows[tid] = row_of(min(tid, nrows - 1));
         // keys that every row of the slice sees: below the first row's end, from the last's start on
-        const Row first_row = row_of(0), last_row = row_of(nrows - 1);
-        const int all_hi = first_row.hi, all_lo = last_row.lo;
-        // (at most 64 keys for all rows: their scores' errors are not left to average out)
-        const bool few_capped = p.cap > 0.f && last_row.hi - first_row.lo <= 64;
+        const int all_hi = row_of(0).hi, all_lo = row_of(nrows - 1).lo;
         __syncthreads();
         float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -465,17 +462,12 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
                             x[kt][nt][c] = (kChains == 2 ? s[kt][nt][0][c] + s[kt][nt][kChains - 1][c] : s[kt][nt][0][c]) * p.scale;
-                    if (few_capped) {
+                    if (p.cap > 0.f) {
 #pragma unroll
                         for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) x[kt][nt][c] = capped_exact(x[kt][nt][c], p.cap);
-                    } else if (p.cap > 0.f) {
-#pragma unroll
-                        for (int kt = 0; kt < Sh::kTiles; ++kt) {  // two keys of a row share a reciprocal
-                            capped2(x[kt][nt][0], x[kt][nt][2], p.cap);
-                            capped2(x[kt][nt][1], x[kt][nt][3], p.cap);
-                        }
+                            for (int c = 0; c < 2; ++c)  // two keys of a row share a reciprocal
+                                unpair2(capped2(pair2(x[kt][nt][c], x[kt][nt][c + 2]), p.cap), x[kt][nt][c], x[kt][nt][c + 2]);
                     }
                     if (p.slopes) {
 #pragma unroll

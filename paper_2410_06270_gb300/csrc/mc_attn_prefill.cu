@@ -25,8 +25,8 @@
 // gives in 64), PV with P in tensor memory at 65, and the change of tiles costs the rest; the
 // softmax's 575 instructions a warp (1160 cycles) run beside it.  A prompt of 8192 tokens, 32 heads
 // on 8 of 128: 358 us, 1.54 PFLOP/s of the visible pairs, 0.79 of cuBLAS's burst rate and 0.91 of its
-// sustained one (at the power cap).  Capped scores take twice the time (2^x and a reciprocal each:
-// 217 us at 4096 tokens, 105 without).
+// sustained one (at the power cap).  Capped scores take 1.7 times the time (a polynomial each: 174 us at
+// 4096 tokens, 104 without; 289 with the form for scores beyond 3/4 of the cap alone).
 //
 // Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 and 9 issue a tile's MMAs,
 // 10 copies keys and values (TMA, a box per page and 64 columns), 11 the queries (TMA where a
@@ -417,14 +417,25 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
                                            int hi, float c, float cap, bool biased, float slope, float at0, bool fresh, float &m, float &l)
 {
     if (MODE == kPfCap) {
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 128; i += 2) {
-            float a, b;
-            unpair2(mul2(pair2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), pair2(c, c)), a, b);
-            capped2(a, b, cap);
-            s[i] = __float_as_uint(a);
-            s[i + 1] = __float_as_uint(b);
-        }
+        for (int i = 0; i < 128; i += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] = fmaxf(t[k], fmaxf(fabsf(__uint_as_float(s[i + k])), fabsf(__uint_as_float(s[i + k + 4]))));
+        const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * c;
+        auto cap_all = [&](auto form) {
+#pragma unroll
+            for (int i = 0; i < 128; i += 2) {
+                float a, b;
+                unpair2(form(mul2(pair2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), pair2(c, c)), cap), a, b);
+                s[i] = __float_as_uint(a);
+                s[i + 1] = __float_as_uint(b);
+            }
+        };
+        // (rows of scores below 3/4 of the cap, the common ones, without the clamps and the reciprocal)
+        if (most <= kTanhNear) cap_all([](uint64_t y, float top) { return capped2_near(y, top); });
+        else cap_all([](uint64_t y, float top) { return capped2(y, top); });
+        __syncwarp();
         c = 1.f;
     }
     if (MODE == kPfBias || (MODE == kPfCap && biased)) {

@@ -343,6 +343,24 @@ def test_caps_far_below_and_around_the_scores(mc, dim, dtype, cap, spread):
         ref.assert_attention(out, lse, want, dtype, 520, 5.0)
 
 
+@pytest.mark.parametrize("cap", [50.0, 1e3, 1e5, 1e8, 1e18])
+@pytest.mark.parametrize("dim,dtype,lens,new", [(128, "bf16", [500, 2, 131], [1, 1, 1]), (64, "fp16", [300, 90], [4, 2]),  # few rows a sequence
+                                                (128, "fp16", [150, 400], [150, 60]), (64, "bf16", [140, 300], [140, 80])])
+def test_caps_far_above_the_scores(mc, dim, dtype, cap, lens, new):
+    """A cap far above the scores leaves them as they are, whatever its size, in either kernel and
+    for rows of few keys and of many.  Bound on lse: its sums and products as in the caps over few
+    keys, 24 roundings of fp32, and 8 more for the cap of each score (its form's error)."""
+    B = ref.Batch(lens, new, 2, 16, dim, dtype, 91)
+    q = B.randn(B.tokens, 12, dim)
+    want = ref.attention(B, q, dim ** -0.5, cap)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, 12)
+    out, lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=cap, with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    ref.assert_attention(out, lse, want, dtype, 500, 5.0)
+    assert ((lse.double().cpu() - want[1]).abs() <= 32 * 2.0 ** -24 * (1 + want[1].abs())).all()
+
+
 @pytest.mark.parametrize("dim,dtype,lens,new,heads,kv,window", [
     (128, "bf16", [40, 300], [6, 3], 4, 2, 0),         # few rows: decode kernel
     (64, "fp16", [9000], [5], 2, 1, 100),              # the same, over pages that a window has left behind
