@@ -314,6 +314,12 @@ __device__ __forceinline__ float capped(float y, float top)
     return a;
 }
 
+// Weights are 2^(x - m).  When a score passes m by more than kLazy, m moves to kBelow under the row's
+// maximum, so that a row's largest weight lies in 2^7 .. 2^15, inside fp16: a weight keeps its 11 bits
+// down to 2^-21 of the largest one, and 2^-32 of it is what rounds to zero.  (With the largest at 1,
+// 8192 keys 17 below one other counted 41 % too much: their weights, 4e-8, are subnormal.)
+constexpr float kBelow = 7.f, kLazy = 15.f;
+
 int launch_append(AppendParams p, int head_dim, bool bf16, cudaStream_t st);
 
 // Whether a key or value in the rows [from, to) of head h of sequence b is infinite or NaN.

@@ -1,9 +1,10 @@
 // mc_attn_decode.cu -- attention of one new token per sequence over the paged cache.
 //
 // o = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m), one pass over the keys with a running
-// maximum m and sum l (scores carried in units of log 2).  Every key and value is read once
-// for a group of query heads, 4 head_dim bytes for 4 head_dim group flops: bound by HBM, so
-// the design is about keeping loads in flight on every SM whatever the lengths are.
+// reference m (the maximum, less a constant) and sum l (scores carried in units of log 2).  Every
+// key and value is read once for a group of query heads, 4 head_dim bytes for 4 head_dim group
+// flops: bound by HBM, so the design is about keeping loads in flight on every SM whatever the
+// lengths are.
 //
 // Work is cut into units of 64 (heads of 64: 128) keys of one (sequence, key head); the units of
 // the whole batch, in order, are dealt to the CTAs as contiguous runs of equal cost, which each
@@ -38,8 +39,6 @@ constexpr int kDecCtasPerSm = 2;
 constexpr int kDecMaxTiles = 4;                // n-tiles of the largest slice
 constexpr int kDecItemCost = 2;  // what an item costs on top of its units, in units (up to 128 sequences; 64 of up
                                 // to 500 keys 23.8 us at 0, 18.4 at 1, 18.1 at 2, 18.4 at 3)
-constexpr float kLazy = 8.f;  // the maximum moves only when a score passes it by 2^8: the
-                              // weights stay below 2^8, far inside fp16 and bf16
 
 template <bool BF16>
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -504,11 +503,12 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            float top = m[nt][c];
+                            float top = -INFINITY;
 #pragma unroll
                             for (int kt = 0; kt < Sh::kTiles; ++kt) top = fmaxf(top, fmaxf(x[kt][nt][c], x[kt][nt][c + 2]));
 #pragma unroll
                             for (int d = 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                            top = fmaxf(m[nt][c], top - kBelow);
                             const float keep = top == m[nt][c] ? 1.f : ex2(m[nt][c] - top);
                             m[nt][c] = top;
                             l[nt][c] *= keep;

@@ -10,8 +10,8 @@
 //   O (+)= P V           tcgen05.mma with P (rounded to the cache's type) in tensor memory
 //                        over S's columns, V as stored, key-major
 // The two tiles alternate: the tensor pipe works for one while the other's softmax runs.
-// The maximum moves only when a row's scores pass it by 2^8 (the weights then stay below
-// 2^8), so O is rescaled in the first few units of a row and hardly after.
+// The reference m moves only when a row's scores pass the maximum that it was taken from by 2^8 (the
+// weights stay below 2^15), so O is rescaled in the first few units of a row and hardly after.
 //
 // Units of the whole batch, in order, are dealt to the CTAs (one per SM) as equal
 // contiguous runs, found on the device from the lengths; a run that ends inside an item
@@ -26,7 +26,7 @@
 // softmax's 575 instructions a warp (1160 cycles) run beside it.  A prompt of 8192 tokens, 32 heads
 // on 8 of 128: 358 us, 1.54 PFLOP/s of the visible pairs, 0.79 of cuBLAS's burst rate and 0.91 of its
 // sustained one (at the power cap).  Capped scores take 1.7 times the time (a polynomial each: 174 us at
-// 4096 tokens, 104 without; 289 with the form for scores beyond 3/4 of the cap alone).
+// 4096 tokens, 104 without), rows with scores beyond 3/4 of the cap 2.8 times (293).
 //
 // Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 and 9 issue a tile's MMAs,
 // 10 copies keys and values (TMA, a box per page and 64 columns), 11 the queries (TMA where a
@@ -49,7 +49,6 @@ namespace mc {
 constexpr int kPfRows = 256, kPfTile = 128, kPfKeys = 128;
 constexpr int kPfThreads = 384, kPfMma = 8, kPfKv = 10;  // MMA: two warps; after kPfKv the queries
 constexpr int kPfMaxStages = 8;
-constexpr float kPfLazy = 8.f;
 constexpr int kPfAhead = 8;   // items that a block's roles may be apart (the copies lead the softmax by 4 at most)
 constexpr int kPfCount = 32;  // the queue's count: a word of the 256 bytes behind the status word
 // Items come from a queue where there are at least kPfQueueItems a block, none costs more than a
@@ -474,8 +473,8 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
     }
     float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
     top *= c;
-    if (__any_sync(0xffffffffu, top > m + kPfLazy)) {
-        const float next = top > m + kPfLazy ? top : m;
+    if (__any_sync(0xffffffffu, top > m + kLazy)) {
+        const float next = top > m + kLazy ? top - kBelow : m;
         const float keep = next == m ? 1.f : ex2(m - next);
         m = next;
         l *= keep;

@@ -155,6 +155,35 @@ def test_decode_large_scores(mc):
         assert ((lse.double().cpu() - want[1]).abs() <= 1e-5 * want[1].abs() + 1e-4).all()
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("below", [9.0, 14.0, 17.0, 17.40625])  # (fp16 and, but for the last, bf16 hold them)
+@pytest.mark.parametrize("new,group", [(1, 1), (32, 8)])  # each kernel
+def test_small_weights_keep_their_sum(mc, dtype, below, new, group):
+    """8191 equal keys far below one: each weighs little, in fp16 less than the type's normal numbers,
+    together they weigh what they should.  A weight of the largest one's 2^-21 or more is rounded to
+    half an ulp, a smaller one to 2^-25 of 2^7."""
+    if dtype == "bf16" and below == 17.40625:
+        below = 17.375
+    seqs, kv, length, dim = 40, 8, 8192, 64
+    k, v = (torch.zeros(length // 128, kv, 128, dim, dtype=ref.DT[dtype], device="cuda") for _ in range(2))
+    v[:] = torch.linspace(1, 64, dim, device="cuda").to(v.dtype)
+    k[0, :, 0, 0], v[0, :, 0] = below, 0.0
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    table = torch.arange(length // 128, dtype=torch.int32, device="cuda").repeat(seqs, 1)  # (one cache for all)
+    cache = mc.KVCache(k, v)
+    batch = mc.KVBatch(i32([length] * seqs), table, i32([new * b for b in range(seqs + 1)]), new * seqs)
+    q = torch.zeros(new * seqs, kv * group, dim, dtype=ref.DT[dtype], device="cuda")
+    q[..., 0] = 1.0
+    out, lse = mc.attn_prefill(cache, batch, q, scale=1.0, with_lse=True)
+    others = torch.arange(length - new, length, dtype=torch.float64)  # keys after the first one, of each new token
+    w = others * np.exp(-below)
+    want = (w / (1 + w))[:, None] * v[0, 0, 1].double().cpu()
+    h = ref.HALF_ULP[dtype]
+    tol = (2 * h + 1e-4) * want + (2.0 ** -24 + length * 2.0 ** -32 * 64 if dtype == "fp16" else 0)
+    assert ((out.view(seqs, new, kv * group, dim).double().cpu() - want[:, None]).abs() <= tol[:, None]).all()
+    assert ((lse.view(seqs, new, kv * group).double().cpu() - (below + torch.log1p(w))[:, None]).abs() <= 1e-4).all()
+
+
 # --------------------------------------------------------------- prefill --
 
 PREFILL = [
