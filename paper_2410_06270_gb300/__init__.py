@@ -499,6 +499,15 @@ def _fast():
     return _fast_module
 
 
+def _on_current(cache):
+    """The kernels run on the current device's stream, so the tensors have to be there."""
+    if cache.index < 0:
+        _bad("the cache is in host memory (%s)" % cache.device)
+    here = _torch().cuda.current_device()
+    if cache.index != here:
+        _bad("the cache is on %s, the current device is cuda:%d" % (cache.device, here))
+
+
 def _side(name, t, cache, dtype, n):
     """Pointer of a contiguous side input of n elements, or None."""
     if t is None:
@@ -549,6 +558,7 @@ def kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope=None, interleaved: b
         k_norm = _side("k_norm", k_norm, cache, cache.dtype, cache.head_dim)
     if workspace is not None:
         workspace = _status(workspace, cache)
+    _on_current(cache)
     rc = load().mc_kv_append(cache._ref, batch._ref, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, heads, q_norm,
                              k_norm, eps, table, rows, rot, 1 if interleaved else 0, q_out.data_ptr(), workspace, _stream())
     if rc:
@@ -581,6 +591,7 @@ def _attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix,
         slopes = _side("slopes", slopes, cache, _torch().float32, heads)
     if prefix is not None:
         prefix = _side("prefix", prefix, cache, _torch().int32, batch.seqs)
+    _on_current(cache)
     opts = _AttnOptsC(cache.head_dim ** -0.5 if scale is None else scale, softcap, window, slopes, prefix)
     rc = fn(cache._ref, batch._ref, q.data_ptr(), qs, heads, ctypes.addressof(opts), out.data_ptr(), os_,
             lse.data_ptr() if with_lse else None, ws, workspace.numel() * workspace.element_size(), _stream())

@@ -76,6 +76,37 @@ def test_binding_refuses_what_c_cannot_see(mc):
     assert _code(mc, mc.attn_prefill, cache, batch, q, prefix=torch.zeros(3), workspace=ws) == -1
 
 
+def _aligned(n):
+    t = torch.zeros(n + 256, dtype=torch.uint8)
+    return t[-t.data_ptr() % 256:][:n]
+
+
+def test_host_tensors_and_other_devices_are_refused(mc, monkeypatch):
+    """Before anything is launched: the answer is an argument error, not a launch's."""
+    cache, batch = _cpu(mc)
+    q, kv = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    ws = _aligned(mc.load().mc_attn_workspace_size(cache._ref, 4))
+    assert _code(mc, mc.kv_append, cache, batch, q, kv, kv) == mc.ERR_INVALID_ARG
+    assert _code(mc, mc.kv_append, cache, batch, q, kv, kv, q_out=torch.empty_like(q), workspace=ws) == mc.ERR_INVALID_ARG
+    for fn in (mc.attn_decode, mc.attn_prefill):
+        assert _code(mc, fn, cache, batch, q, workspace=ws) == mc.ERR_INVALID_ARG
+
+    class Elsewhere:  # a torch whose current device is not the tensors'
+        class cuda:
+            current_device = staticmethod(lambda: 0)
+
+        def __getattr__(self, name):
+            return getattr(torch, name)
+
+    monkeypatch.setattr(mc, "_torch", lambda: Elsewhere())
+    for where, refused in ((1, True), (0, False)):
+        cache.index = where
+        if refused:
+            assert _code(mc, mc._on_current, cache) == mc.ERR_INVALID_ARG
+        else:
+            mc._on_current(cache)
+
+
 @pytest.mark.parametrize("scale,cap", [(0.0, 0.0), (-1.0, 0.0), (1e-30, 0.0), (1e30, 0.0), (1.0, 1e-30), (1.0, 1e30), (1e30, 1e-30)])
 def test_scales_and_caps_out_of_range(mc, scale, cap):
     cache, batch = _cpu(mc)
