@@ -9,6 +9,7 @@ stream.  If the library has not been built, importing this package raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import numpy as np
@@ -499,6 +500,11 @@ def _fast():
     return _fast_module
 
 
+def _opts(scale, softcap, window, slopes, prefix):
+    """The C options; a window beyond 32 bits is any length's (ctypes would take its low bits)."""
+    return _AttnOptsC(scale, softcap, max(-1, min(operator.index(window), 0x7fffffff)), slopes, prefix)
+
+
 def _on_current(cache):
     """The kernels run on the current device's stream, so the tensors have to be there."""
     if cache.index < 0:
@@ -592,7 +598,7 @@ def _attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix,
     if prefix is not None:
         prefix = _side("prefix", prefix, cache, _torch().int32, batch.seqs)
     _on_current(cache)
-    opts = _AttnOptsC(cache.head_dim ** -0.5 if scale is None else scale, softcap, window, slopes, prefix)
+    opts = _opts(cache.head_dim ** -0.5 if scale is None else scale, softcap, window, slopes, prefix)
     rc = fn(cache._ref, batch._ref, q.data_ptr(), qs, heads, ctypes.addressof(opts), out.data_ptr(), os_,
             lse.data_ptr() if with_lse else None, ws, workspace.numel() * workspace.element_size(), _stream())
     if rc:

@@ -107,6 +107,31 @@ def test_host_tensors_and_other_devices_are_refused(mc, monkeypatch):
             mc._on_current(cache)
 
 
+@pytest.mark.parametrize("window,c_window", [(0, 0), (5, 5), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 32, 2 ** 31 - 1),
+                                             (2 ** 32 + 5, 2 ** 31 - 1), (-1, -1), (-2 ** 32, -1), (-2 ** 32 + 7, -1)])
+def test_a_window_beyond_32_bits_is_no_shorter_one(mc, monkeypatch, window, c_window):
+    """It reaches the C call (a stand-in for it here) as the longest window, and a negative one as
+    one that is refused."""
+    seen = []
+    cache, batch = _cpu(mc)
+    q, ws = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(1 << 10, dtype=torch.uint8)
+
+    class Lib:
+        def mc_attn_decode(self, *a):
+            seen.append(mc._AttnOptsC.from_address(a[5]).window)
+            return mc.OK
+
+        mc_attn_prefill = mc_attn_decode
+
+    monkeypatch.setattr(mc, "_fast_module", type("NotPlain", (), {"attention": staticmethod(lambda *a: None)}))
+    monkeypatch.setattr(mc, "load", Lib)
+    monkeypatch.setattr(mc, "_stream", lambda: 0)
+    monkeypatch.setattr(mc, "_on_current", lambda cache: None)
+    for fn in (mc.attn_decode, mc.attn_prefill):
+        fn(cache, batch, q, window=window, workspace=ws)
+    assert seen == [c_window] * 2
+
+
 @pytest.mark.parametrize("scale,cap", [(0.0, 0.0), (-1.0, 0.0), (1e-30, 0.0), (1e30, 0.0), (1.0, 1e-30), (1.0, 1e30), (1e30, 1e-30)])
 def test_scales_and_caps_out_of_range(mc, scale, cap):
     cache, batch = _cpu(mc)
