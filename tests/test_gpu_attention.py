@@ -445,6 +445,122 @@ def test_a_visible_score_of_minus_infinity_weighs_nothing(mc, dim, dtype, length
     ref.assert_attention(got, lse, want, dtype, length, 5.0, rows=rows)
 
 
+# ------------------------------------------- both kernels, by the mean of rows --
+# A sequence's new tokens times its group are its rows; with a mean of up to 16 (32 under a cap) the
+# batch takes the kernel for few rows, beyond that the tensor-memory one.
+
+@pytest.mark.parametrize("heads,kv,dim,dtype,cap", [(8, 2, 128, "bf16", 0.0), (6, 2, 64, "fp16", 0.0), (8, 2, 128, "bf16", 30.0)])
+def test_one_token_each_through_either_kernel(mc, heads, kv, dim, dtype, cap):
+    """The same single tokens alone and beside a prompt that takes the batch over the limit."""
+    B = ref.Batch(EDGES + [900], [1] * len(EDGES) + [900], kv, 16, dim, dtype, 101)
+    n = len(EDGES)
+    q = B.randn(B.tokens, heads, dim)
+    want = ref.attention(B, q, dim ** -0.5, cap)
+    cache, batch = B.device(mc)
+    mixed, mixed_lse = mc.attn_prefill(cache, batch, q.cuda(), softcap=cap, with_lse=True)
+    assert (n + 900) * (heads // kv) / (n + 1) > 32
+    ref.assert_attention(mixed, mixed_lse, want, dtype, 900, 5.0)
+    one = mc.KVBatch(batch._keep[0][:n].contiguous(), batch._keep[1][:n].contiguous())
+    for call in (mc.attn_decode, mc.attn_prefill):
+        alone, lse = call(cache, one, q[:n].cuda(), softcap=cap, with_lse=True)
+        ref.assert_attention(alone, lse, tuple(w[:n] for w in want), dtype, 900, 5.0)
+
+
+@pytest.mark.parametrize("dtype,window,prefix", [("bf16", 0, False), ("fp16", 90, False), ("bf16", 0, True)])
+def test_a_long_prompt_through_the_kernel_for_few_rows(mc, dtype, window, prefix):
+    """Many slots with a token or none bring the mean down: the prompt's rows are many slices."""
+    lens, new = [650] + [0, 40, 7] * 20, [600] + [0, 1, 1] * 20
+    B = ref.Batch(lens, new, 1, 32, 64, dtype, 103, pad_tokens=1)
+    assert B.tokens / len(lens) <= 16
+    q = B.randn(B.tokens, 1, 64)
+    pre = [300] + [0] * 60 if prefix else None
+    want = ref.attention(B, q, 0.125, window=window, prefix=pre)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, 1)
+    out, lse = mc.attn_prefill(cache, batch, q.cuda(), window=window, with_lse=True, workspace=ws,
+                               prefix=None if pre is None else torch.tensor(pre, dtype=torch.int32).cuda())
+    mc.check_status(ws)
+    ref.assert_attention(out, lse, want, dtype, 650, 5.0, rows=slice(0, B.cu[-1]))
+
+
+@pytest.mark.parametrize("new", [[2, 3, 1], [200, 131, 60]])  # few rows, many rows
+@pytest.mark.parametrize("heads,kv,dim,dtype", [(4, 1, 128, "bf16"), (3, 1, 64, "fp16"), (10, 2, 128, "fp16"), (14, 2, 64, "bf16"),
+                                                (24, 1, 128, "bf16"), (17, 1, 64, "bf16")])
+def test_queries_and_outputs_with_a_token_stride(mc, new, heads, kv, dim, dtype):
+    """Queries as a slice of the projection's output, for groups that divide a tile and others; outputs
+    whose rows start at multiples of 16 bytes but not of 32."""
+    B = ref.Batch([260, 400, 61], new, kv, 16, dim, dtype, 107, pad_tokens=1)
+    wide = B.randn(B.tokens, (heads + 2 * kv) * dim + 8)
+    q = wide[:, 8:8 + heads * dim].unflatten(1, (heads, dim))
+    want = ref.attention(B, q, dim ** -0.5)
+    cache, batch = B.device(mc)
+    ws = mc.attn_workspace(cache, heads)
+    dev = wide.cuda()[:, 8:8 + heads * dim].unflatten(1, (heads, dim))
+    buf = torch.full((B.tokens, heads * dim + 8), 3.0, dtype=ref.DT[dtype], device="cuda")
+    out = buf[:, :heads * dim].unflatten(1, (heads, dim))
+    got, lse = mc.attn_prefill(cache, batch, dev, out=out, with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    assert (buf[:, heads * dim:] == 3).all() and (buf[B.cu[-1]:] == 3).all()
+    ref.assert_attention(got, lse, want, dtype, 400, 5.0, rows=slice(0, B.cu[-1]))
+
+
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("new", [[2, 1, 3], [50, 70, 130]])  # few rows, many rows
+def test_pages_lengths_and_boundaries_that_are_not_sound(mc, new, cap):
+    """In either kernel: a page outside the pool reads as zeros, a length is cut to the table's rows, a
+    sequence whose boundaries are not sound has no tokens; each is recorded, and the other sequences
+    are right."""
+    lens, heads, kv, dim = [96, 160, 144], 8, 2, 64
+    ok = ref.Batch(lens, new, kv, 16, dim, "bf16", 109)
+    q = ok.randn(ok.tokens, heads, dim)
+    cache, batch = ok.device(mc)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32).cuda()  # noqa: E731
+
+    def attend(b):
+        ws = mc.attn_workspace(cache, heads)
+        out = torch.full((ok.tokens, heads, dim), 3.0, dtype=torch.bfloat16, device="cuda")
+        _, lse = mc.attn_prefill(cache, b, q.cuda(), softcap=cap, out=out, with_lse=True, workspace=ws)
+        return out, lse, ws
+
+    def reported(ws):
+        with pytest.raises(mc.MCError) as e:
+            mc.check_status(ws)
+        assert e.value.code == mc.ERR_RANGE
+
+    want = ref.attention(ok, q, dim ** -0.5, cap)
+    good, good_lse, ws = attend(batch)
+    mc.check_status(ws)
+    ref.assert_attention(good, good_lse, want, "bf16", 160, 5.0)
+
+    for page in (ok.k.shape[0], -1, 2 ** 31 - 1, -2 ** 31):  # of sequence 1's keys 32 .. 47
+        table = ok.table.clone()
+        table[1, 2] = page
+        out, lse, ws = attend(mc.KVBatch(batch._keep[0], table.cuda(), batch._keep[2], ok.tokens))
+        reported(ws)
+        zero = ref.Batch(lens, new, kv, 16, dim, "bf16", 109)
+        zero.k[zero.table[1, 2].long()] = 0
+        zero.v[zero.table[1, 2].long()] = 0
+        ref.assert_attention(out, lse, ref.attention(zero, q, dim ** -0.5, cap), "bf16", 160, 5.0)
+        others = [t for t in range(ok.tokens) if not ok.cu[1] <= t < ok.cu[2]]
+        assert torch.equal(out[others], good[others])
+
+    for length in (161, 1 << 20, 2 ** 31 - 1):
+        out, lse, ws = attend(mc.KVBatch(i32([96, length, 144]), batch._keep[1], batch._keep[2], ok.tokens))
+        reported(ws)
+        ref.assert_attention(out, lse, want, "bf16", 160, 5.0)  # (the table has pages for 160 rows)
+
+    # (in the first, sequence 2 claims every row, those of sequence 0 too: none is anybody's alone)
+    for cu, sound in (([0, ok.cu[1], 0, ok.cu[3]], []), ([0, ok.cu[1], ok.tokens + 1, ok.tokens + 1], [0]),
+                      ([-1, ok.cu[1], ok.cu[2], ok.cu[3]], [1, 2]), ([0, ok.cu[1], ok.cu[2], ok.cu[2] - 1], [0, 1])):
+        out, lse, ws = attend(mc.KVBatch(batch._keep[0], batch._keep[1], i32(cu), ok.tokens))
+        reported(ws)
+        for b in sound:
+            t = slice(ok.cu[b], ok.cu[b + 1])
+            ref.assert_attention(out[t], lse[t], tuple(w[t] for w in want), "bf16", 160, 5.0)
+        if sound == [1, 2]:
+            assert (out[:ok.cu[1]] == 3).all()
+
+
 # ----------------------------------------------------------- streams, status --
 
 def test_on_another_stream_and_in_a_graph(mc):
