@@ -313,7 +313,7 @@ typedef struct {
  * lens[b] is its length WITH them: new token i has position p = lens[b] - n_b + i.
  * A token with p < 0 (an idle slot has lens[b] = 0) has no position: it is not
  * appended and sees no key.  Rows from cu_q[seqs] on are padding: nothing of theirs is
- * read or written.  table[b * table_width + i], i < ceil(lens[b] / page_size), are b's
+ * written, and what they hold does not matter.  table[b * table_width + i], i < ceil(lens[b] / page_size), are b's
  * pages; other entries are not read.  A page outside [0, num_pages) (its rows are not
  * written, and read as zeros), a length beyond table_width pages (cut to them by the attentions;
  * the append keeps the positions that it gives and writes no token past the pages), a cu_q that

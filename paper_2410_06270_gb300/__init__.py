@@ -525,7 +525,8 @@ def _side(name, t, cache, dtype, n):
 
 def attn_workspace(cache: KVCache, q_heads: int):
     """Zeroed workspace of attn_decode / attn_prefill (and the status word of kv_append)
-    for a cache and a number of query heads, whatever the batch."""
+    for a cache and a number of query heads, whatever the batch.  Calls without one cannot be
+    asked what the device found (check_status)."""
     import torch
     n = load().mc_attn_workspace_size(cache._ref, int(q_heads))
     if n == 0:

@@ -145,8 +145,8 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     // Few rows (tokens x heads of a group) a sequence take the decode kernel, whose time grows
     // with them, more the tensor-memory one, whose rows come 128 at a time; the counts are the
     // device's, so the mean decides.  8 sequences of 4000 keys, decode / tensor-memory kernel:
-    // 20 rows 38 / 34 us, 32 rows 44 / 34; with a cap, whose cost follows the rows, 38 / 49 and
-    // 45 / 49; one sequence of 2000 keys, 16 rows, 12 / 17.
+    // 16 rows 30 / 36 us, 20 rows 37 / 36, 32 rows 42 / 36; with a cap, whose cost follows the rows,
+    // 36 / 51 at 20 and 44 / 51 at 32; one sequence of 2000 keys, 16 rows, 12 / 14.
     const int64_t rows = ((int64_t)batch->tokens + batch->seqs - 1) / batch->seqs * p.group;
     const bool bf16 = cache->dtype == MC_BF16;
     if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, (int)rows, (cudaStream_t)stream);

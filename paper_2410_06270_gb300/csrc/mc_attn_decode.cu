@@ -17,10 +17,11 @@
 // More rows than a group's heads (a few new tokens per sequence, with causal, window and prefix
 // masks row by row) are further columns of the same products, up to 32.
 //
-// Measured: 64 sequences of 8192 keys, 32 heads on 8 of 128, 311 us, 6.9 TB/s of keys and values
-// (1.02 of the measured copy rate); one of 131071 keys 83 us, 6.4 TB/s; DRAM bytes 537.1 MB for 536.9
-// (ncu, 16 x 8192).  Short ones are bound by latency: 777 keys 7.2 us, of which the schedule 1, the
-// first keys 1.5, the join and its launch 3.
+// Measured: 64 sequences of 8192 keys, 32 heads on 8 of 128, 310 to 318 us by the box, 6.8 to 6.9 TB/s
+// of keys and values (1.00 to 1.02 of the measured copy rate); one of 131071 keys 83 us, 6.5 TB/s; DRAM
+// bytes 537.1 MB for 536.9 (ncu, 16 x 8192).  Short ones are bound by latency: 777 keys 7.4 us, of which
+// the schedule 1, the first keys 1.5, the join and its launch 3; so are caps over more than 8 rows (33
+// sequences of a window of 1024 keys, 12 heads a key head: 17 us, special functions 4 % active).
 #include <math.h>
 
 #include "mc_attn.h"

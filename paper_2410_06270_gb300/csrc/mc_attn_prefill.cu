@@ -24,8 +24,8 @@
 // both operands in shared memory runs at 78 cycles an MMA (8 KB each, all that shared memory
 // gives in 64), PV with P in tensor memory at 65, and the change of tiles costs the rest; the
 // softmax's 575 instructions a warp (1160 cycles) run beside it.  A prompt of 8192 tokens, 32 heads
-// on 8 of 128: 358 us, 1.54 PFLOP/s of the visible pairs, 0.79 of cuBLAS's burst rate and 0.91 of its
-// sustained one (at the power cap).  Capped scores take 1.7 times the time (a polynomial each: 174 us at
+// on 8 of 128: 357 us, 1.54 PFLOP/s of the visible pairs, 0.81 of cuBLAS's burst rate and 0.90 of its
+// sustained one (at the power cap).  Capped scores take 1.7 times the time (a polynomial each: 175 us at
 // 4096 tokens, 104 without), rows with scores beyond 3/4 of the cap 2.8 times (293).
 //
 // Warps: 0-3 and 4-7 the softmax of tile 0 and 1 (also the epilogue), 8 and 9 issue a tile's MMAs,

@@ -32,8 +32,8 @@ __device__ __forceinline__ uint64_t swapped(uint64_t v)
 // between lanes but the norm's sum.  With the weights g folded in, the two elements of a pair are
 //   a' = (a (g_a c) - b (g_b s)) / rms,  b' = (b (g_b c) + a (g_a s)) / rms
 // two at a time (f32x2).  Issue-bound before that (850 instructions a warp, rows of all kinds
-// alike): 8192 tokens of 48 heads of 128, norms and rotation, 48 us; now 41 us, 5.0 TB/s (issue
-// 71 % active, ALU 58 %).  Eight passes a warp (84 registers) take 48 us, ten blocks an SM (48) 41.
+// alike): 8192 tokens of 48 heads of 128, norms and rotation, 48 us; now 37 us, 5.6 TB/s (issue
+// 77 % active, ALU 61 %).  Eight passes a warp (84 registers) took 48 us where four took 41.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams p)
 {
