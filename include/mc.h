@@ -380,6 +380,93 @@ int mc_attn_prefill(const mc_kv_cache *cache, const mc_kv_batch *batch, const vo
                     const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
                     size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------ *
+ * The same cache held in 4 bits: a quarter of the bytes (and a sixteenth for scales), with the
+ * append that fills it and the attention that reads it.  Batches, options, workspace and every rule
+ * above hold; a cache is described by mc_kv_cache too, where
+ *   page_stride is in BYTES (a multiple of 16, >= kv_heads * mc_kv4_block_size);
+ *   dtype is that of the queries and outputs, and of the numbers that the cache stands for.
+ *
+ * A row of a head is stored in groups of 64 elements.  With x the elements rounded to dtype, lo the
+ * smallest of them and 0, hi the largest of them and 0, a group is the grid s (c - z):
+ *   s  the smallest number of 4 significant bits with 15 s >= hi - lo, but at least 2^-100 (bf16)
+ *      or 2^-20 (fp16)   (hi / 16 - lo / 16, rounded to fp32, is the difference that is meant)
+ *   z  floor(-lo / s + 1/2), 0 .. 15
+ *   c  floor(x / s + 1/2) + z, at most 15, and none that stands for more than dtype's largest number
+ * |x - s (c - z)| <= s (s / 2 where neither end is cut).  s (c - z) has at most 8 significant bits: it
+ * is a number of dtype, and what the attention multiplies is exactly that.  A group with an infinite or
+ * NaN element is stored with a NaN scale and stands for 64 NaNs.
+ *
+ * Bytes of (page, head), from page * page_stride + head * mc_kv4_block_size on:
+ *   codes  row r's head_dim / 2 bytes from r * head_dim / 2 on, as 32-bit words of 8 elements each: word
+ *          i * groups + g holds elements 64 g + 8 i .. + 7; of these, 2 j at bits 4 j .. 4 j + 3 and 2 j + 1 at
+ *          bits 16 + 4 j .. 19 + 4 j
+ *   words  behind the codes of all rows, 16 bits for (row, group): bits 4 .. 14 the upper bits of the scale as
+ *          fp32 (8 of exponent, 3 of mantissa), bits 0 .. 3 z
+ * ------------------------------------------------------------------------ */
+/* Bytes of (page, head): page_size * 17 * head_dim / 32; 0 for sizes that are refused. */
+size_t mc_kv4_block_size(int page_size, int head_dim);
+
+/* Workspace bytes of the attn4 calls (as mc_attn_workspace_size). */
+size_t mc_attn4_workspace_size(const mc_kv_cache *cache, int q_heads);
+
+/* As mc_kv_append; a key's or value's row is rounded to dtype, then stored on its groups' grids. */
+int mc_kv4_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
+                  int64_t k_stride, const void *v, int64_t v_stride, int q_heads, const void *q_norm,
+                  const void *k_norm, float eps, const float *rope, int rope_rows, int rot_dim, int interleaved,
+                  void *q_out, void *workspace, void *stream);
+
+/* What the cache stands for in the rows of the batch's new tokens: k and v [tokens][kv_heads][head_dim] in
+ * dtype, contiguous, 16-byte aligned (either may be NULL).  A token without a position, or on a page outside the
+ * cache, reads as zeros. */
+int mc_kv4_read(const mc_kv_cache *cache, const mc_kv_batch *batch, void *k, void *v, void *workspace, void *stream);
+
+/* As mc_attn_decode and mc_attn_prefill. */
+int mc_attn4_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                    const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                    size_t ws_bytes, void *stream);
+int mc_attn4_prefill(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                     const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                     size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------ *
+ * The pages of a server's requests, dealt out on the device: what a step needs before the appends and
+ * the attentions, from the lengths alone.  One call takes the finished sequences' pages back, gives the
+ * growing ones theirs, and says where every new token goes.
+ *
+ * Pool: free pages stand in a ring, entries state[0] .. state[1] - 1 (modulo num_pages): state[0] counts the
+ * pages ever taken, state[1] those ever returned (num_pages at the start, when all are free).
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    int32_t *ring;        /* device [num_pages] */
+    const int64_t *state; /* device [2], 8-byte aligned */
+    int32_t num_pages, page_size;
+} mc_kv_pool;
+
+/* Workspace bytes of mc_kv_plan for up to `seqs` sequences: status word first, zeroed once by the caller. */
+size_t mc_kv_plan_workspace_size(int seqs);
+
+/* Sequence b is lens[b] tokens long (a negative length counts as 0) and holds the pages of its row of
+ * table [seqs][table_width].  In the order of the sequences:
+ *   done[b] != 0 (done: uint8 [seqs], may be NULL): its pages go to the ring, its length is 0 from there on
+ *   it gets add[b] new tokens, and the pages for them from the ring (those returned in this call are not
+ *   given out in it), entered into its table row, if add[b] >= 0, the row is wide enough, the free pages
+ *   suffice for it and all such sequences before it, and `tokens` rows do for its tokens and theirs; else it
+ *   gets none and stays as it is, and MC_ERR_RANGE is recorded in the workspace's status word
+ * Outputs (device):
+ *   lens_out int32 [seqs]       lengths with the new tokens (may be lens)
+ *   cu_q     int32 [seqs + 1]   rows of each sequence's new tokens in the step's token arrays
+ *   positions int32 [tokens], slots int64 [tokens] (either may be NULL): position of each new token and its slot,
+ *            page * page_size + position % page_size; -1 for rows from cu_q[seqs] on, and as the slot of a token
+ *            whose page is outside the pool (MC_ERR_RANGE)
+ *   state_out int64 [2]         the counts after the call (may be pool->state)
+ * lens_out, table and cu_q are what mc_kv_batch takes.  A page that would not fit in the ring is not returned
+ * (MC_ERR_RANGE).  Without committing (state_out and lens_out apart from the inputs) the same call may be
+ * made again: it writes the same entries. */
+int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, const uint8_t *done, int seqs, int tokens,
+               int32_t *table, int table_width, int32_t *lens_out, int32_t *cu_q, int32_t *positions, int64_t *slots,
+               int64_t *state_out, void *workspace, size_t ws_bytes, void *stream);
+
 /* Test hook: choose the expert path of mc_moe_forward: 0 = automatic (the GEMV
  * below 240 kept-or-not pairs, 2T < 240, else the GEMM), 1 = the mma.sync
  * grouped GEMV with work chunks of 16 pairs (decode), 2 = the tcgen05 grouped
@@ -424,7 +511,8 @@ int mc_check_status(void *workspace, void *stream);
  * synchronises on the recorded events, writes the summed milliseconds and launch
  * counts of kernel ids 0 .. n-1 (names from mc_profile_name: route, permute,
  * gemv_w13, gemv_w2, combine, frag_x, gemm_w13, gemm_w2, rmsnorm, importance,
- * x_img, kv_append, attn_decode, attn_prefill, attn_join) and
+ * x_img, kv_append, attn_decode, attn_prefill, attn_join, kv_read, kv_plan,
+ * residual_norm) and
  * clears the records.  Inside stream capture the events become event nodes of
  * the graph: every replay records them again, and each mc_profile_read reports
  * the latest replay and keeps those records until mc_profile_clear. */
@@ -445,6 +533,30 @@ int mc_rmsnorm(const void *x, const void *gamma, int T, int H, float eps, void *
 
 /* out = a + b elementwise over n bf16 values (residual add; may alias a). */
 int mc_add(const void *a, const void *b, size_t n, void *out, void *stream);
+
+/* What lies between a block of a layer and the next one, in one pass over a token's row: the norm behind the
+ * block, its gate and scale, the residual sum and the norm before the next block.
+ *   u = y / sqrt(mean(y^2) + eps) * post_norm       (post_norm [H], NULL: u = y)
+ *   h_out = residual_scale * h + scale * gate * u   rounded once to dtype   (gate NULL: none)
+ *   x = h_out / sqrt(mean(h_out^2) + eps) * pre_norm    (pre_norm [H], NULL: none; of h_out as rounded)
+ * y, h, h_out, x: [T][H] in dtype (MC_BF16 or MC_FP16), rows y_stride, h_stride, h_out_stride, x_stride elements
+ * apart; gate element (t, i) at gate[t * gate_row + i * gate_col], gate_col 0 or 1 (a row, a column, or all of
+ * [T][H]).  Arithmetic in fp32.  h_out may be h or y, x may be y; no other overlaps.  H up to 65536; any 2-byte alignment
+ * (16-byte aligned rows with H a multiple of 8 take wide accesses).
+ * With bf16, scales of 1 and neither gate nor post_norm, the results are those of mc_add and mc_rmsnorm. */
+typedef struct {
+    int32_t T, H, dtype;
+    const void *y, *h;
+    int64_t y_stride, h_stride;
+    const void *post_norm, *pre_norm;
+    const void *gate;
+    int64_t gate_row;
+    int32_t gate_col;
+    float scale, residual_scale, eps;
+    void *h_out, *x;
+    int64_t h_out_stride, x_stride;
+} mc_residual_norm_args;
+int mc_residual_norm(const mc_residual_norm_args *args, void *stream);
 
 #ifdef __cplusplus
 }

@@ -83,6 +83,15 @@ def load():
         "mc_kv_append": (I, [P, P, P, L, P, L, P, L, I, P, P, F32, P, I, I, I, P, P, P]),
         "mc_attn_decode": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
         "mc_attn_prefill": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
+        "mc_kv4_block_size": (Z, [I, I]),
+        "mc_attn4_workspace_size": (Z, [P, I]),
+        "mc_kv4_append": (I, [P, P, P, L, P, L, P, L, I, P, P, F32, P, I, I, I, P, P, P]),
+        "mc_kv4_read": (I, [P, P, P, P, P, P]),
+        "mc_attn4_decode": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
+        "mc_attn4_prefill": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
+        "mc_kv_plan_workspace_size": (Z, [I]),
+        "mc_kv_plan": (I, [P, P, P, P, I, I, P, I, P, P, P, P, P, P, Z, P]),
+        "mc_residual_norm": (I, [P, P]),
         "mc_profile_enable": (I, [I]),
         "mc_profile_select": (ctypes.c_uint, [ctypes.c_uint]),
         "mc_profile_read": (I, [P, P, I]),
@@ -437,6 +446,40 @@ class KVCache:
         self.index = k.get_device()
 
 
+class KVCache4:
+    """A paged key-value cache in 4 bits over the caller's tensors k and v, both uint8 [pages,
+    kv_heads, kv4_block_size(page_size, head_dim)] (what a block holds is the library's; mc.h
+    describes it).  Pages may be strided; the rest is contiguous.  dtype (bf16 or fp16): that of the
+    queries and outputs."""
+
+    def __init__(self, k, v, page_size: int, head_dim: int, dtype=None):
+        import torch
+        codes = {torch.bfloat16: 0, torch.float16: 1}
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in codes:
+            raise MCError(ERR_UNSUPPORTED, "cache of %s" % dtype)
+        block = kv4_block_size(page_size, head_dim)
+        if k.dim() != 3 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+            _bad("k and v must be alike: uint8 [pages, kv_heads, block]")
+        pages, heads, size = k.shape
+        if k.dtype != torch.uint8 or size != block or k.stride(2) != 1 or (heads > 1 and k.stride(1) != block):
+            _bad("k and v must be uint8 [pages, kv_heads, %d], the blocks of a page contiguous" % block)
+        self.k, self.v, self.dtype, self.device = k, v, dtype, k.device
+        self.kv_heads, self.page_size, self.head_dim = heads, int(page_size), int(head_dim)
+        stride = k.stride(0) if pages > 1 else max(k.stride(0), heads * block) + 15 & -16
+        self._c = _KvCacheC(k.data_ptr(), v.data_ptr(), stride, pages, self.page_size, heads, self.head_dim, codes[dtype])
+        self._ref = ctypes.addressof(self._c)
+        self.index = k.get_device()
+
+
+def kv4_block_size(page_size: int, head_dim: int) -> int:
+    """Bytes that a KVCache4 takes for the keys (or values) of one head in one page."""
+    n = load().mc_kv4_block_size(int(page_size), int(head_dim))
+    if n == 0:
+        raise MCError(ERR_INVALID_ARG, last_error())
+    return n
+
+
 class KVBatch:
     """The tokens of one call: lens int32 [seqs] (lengths WITH the new tokens), table int32
     [seqs, width] (pages), cu_q int32 [seqs + 1] (rows of each sequence's new tokens; None:
@@ -492,7 +535,8 @@ def _fast():
         spec = importlib.util.spec_from_loader("_mcbind", importlib.machinery.ExtensionFileLoader("_mcbind", path))
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)
-        at = [ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in ("mc_kv_append", "mc_attn_decode", "mc_attn_prefill")]
+        at = [ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in ("mc_kv_append", "mc_attn_decode", "mc_attn_prefill",
+                                                                            "mc_kv4_append", "mc_attn4_decode", "mc_attn4_prefill")]
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
         m.setup(*at, torch.empty, raw, getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device, torch.float32,
                 torch.int32, torch.uint8)
@@ -505,13 +549,13 @@ def _opts(scale, softcap, window, slopes, prefix):
     return _AttnOptsC(scale, softcap, max(-1, min(operator.index(window), 0x7fffffff)), slopes, prefix)
 
 
-def _on_current(cache):
+def _on_current(cache, what="cache"):
     """The kernels run on the current device's stream, so the tensors have to be there."""
     if cache.index < 0:
-        _bad("the cache is in host memory (%s)" % cache.device)
+        _bad("the %s is in host memory (%s)" % (what, cache.device))
     here = _torch().cuda.current_device()
     if cache.index != here:
-        _bad("the cache is on %s, the current device is cuda:%d" % (cache.device, here))
+        _bad("the %s is on %s, the current device is cuda:%d" % (what, cache.device, here))
 
 
 def _side(name, t, cache, dtype, n):
@@ -527,21 +571,31 @@ def attn_workspace(cache: KVCache, q_heads: int):
     """Zeroed workspace of attn_decode / attn_prefill (and the status word of kv_append)
     for a cache and a number of query heads, whatever the batch.  Calls without one cannot be
     asked what the device found (check_status)."""
+    _kind(cache, False)
+    return _attn_workspace(cache, load().mc_attn_workspace_size(cache._ref, int(q_heads)))
+
+
+def _attn_workspace(cache, n):
     import torch
-    n = load().mc_attn_workspace_size(cache._ref, int(q_heads))
     if n == 0:
         raise MCError(ERR_INVALID_ARG, last_error())
     return torch.zeros(n, dtype=torch.uint8, device=cache.device)
 
 
-def kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope=None, interleaved: bool = False, q_norm=None, k_norm=None,
-              eps: float = 1e-6, q_out=None, workspace=None):
-    """New tokens into the cache, in one pass: q and k [tokens, heads, head_dim] normed per
-    head (q_norm / k_norm [head_dim], None: not) and rotated (rope fp32 [positions,
-    rot_dim]: rot_dim/2 cosines, then sines; None: not), k and v written to their pages.
-    Returns the queries [tokens, q_heads, head_dim].  q, k, v may be slices of one
-    projection's output."""
-    r = (_fast_module or _fast()).kv_append(cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace)
+def attn4_workspace(cache: KVCache4, q_heads: int):
+    """attn_workspace for the calls on a KVCache4."""
+    _kind(cache, True)
+    return _attn_workspace(cache, load().mc_attn4_workspace_size(cache._ref, int(q_heads)))
+
+
+def _kind(cache, bits4):
+    if (cache.__class__ is KVCache4) != bool(bits4):
+        _bad("a %s where a %s is taken" % (type(cache).__name__, "KVCache4" if bits4 else "KVCache"))
+
+
+def _append(bits4, cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace):
+    _kind(cache, bits4)
+    r = (_fast_module or _fast()).append(bits4, cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace)
     if r is not None:
         return _check(r) if r.__class__ is int else r
     heads, qs = _rows("q", q, cache, batch)
@@ -566,24 +620,36 @@ def kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope=None, interleaved: b
     if workspace is not None:
         workspace = _status(workspace, cache)
     _on_current(cache)
-    rc = load().mc_kv_append(cache._ref, batch._ref, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, heads, q_norm,
+    fn = load().mc_kv4_append if bits4 else load().mc_kv_append
+    rc = fn(cache._ref, batch._ref, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, heads, q_norm,
                              k_norm, eps, table, rows, rot, 1 if interleaved else 0, q_out.data_ptr(), workspace, _stream())
     if rc:
         _check(rc)
     return q_out
 
 
-def _status(workspace, cache):
+def kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope=None, interleaved: bool = False, q_norm=None, k_norm=None,
+              eps: float = 1e-6, q_out=None, workspace=None):
+    """New tokens into the cache, in one pass: q and k [tokens, heads, head_dim] normed per
+    head (q_norm / k_norm [head_dim], None: not) and rotated (rope fp32 [positions,
+    rot_dim]: rot_dim/2 cosines, then sines; None: not), k and v written to their pages.
+    Returns the queries [tokens, q_heads, head_dim].  q, k, v may be slices of one
+    projection's output."""
+    return _append(False, cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace)
+
+
+def _status(workspace, cache, what="cache"):
     if workspace.get_device() != cache.index or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < 256:
-        _bad("the workspace must be contiguous on the cache's device, with its status word's 256 bytes")
+        _bad("the workspace must be contiguous on the %s's device, with its status word's 256 bytes" % what)
     return workspace.data_ptr()
 
 
-def _attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace):
-    r = (_fast_module or _fast()).attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace)
+def _attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace, bits4=False):
+    _kind(cache, bits4)
+    r = (_fast_module or _fast()).attention(prefill + 2 * bits4, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace)
     if r is not None:
         return _check(r) if r.__class__ is int else r
-    fn = load().mc_attn_prefill if prefill else load().mc_attn_decode
+    fn = getattr(load(), "mc_attn%s_%s" % ("4" if bits4 else "", "prefill" if prefill else "decode"))
     heads, qs = _rows("q", q, cache, batch)
     empty, dev = _torch().empty, cache.device
     if out is None:
@@ -591,7 +657,7 @@ def _attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix,
     else:
         os_ = _rows("out", out, cache, batch, heads)[1]
     if workspace is None:
-        workspace = attn_workspace(cache, heads)
+        workspace = (attn4_workspace if bits4 else attn_workspace)(cache, heads)
     ws = _status(workspace, cache)
     lse = empty((batch.tokens, heads), dtype=_torch().float32, device=dev) if with_lse else None
     if slopes is not None:
@@ -626,9 +692,195 @@ def attn_prefill(cache: KVCache, batch: KVBatch, q, scale=None, softcap: float =
                       workspace)
 
 
+# ------------------------------------------------------- the 4-bit cache --
+
+def kv4_append(cache: KVCache4, batch: KVBatch, q, k, v, rope=None, interleaved: bool = False, q_norm=None, k_norm=None,
+               eps: float = 1e-6, q_out=None, workspace=None):
+    """kv_append to a cache in 4 bits: keys and values are rounded to the cache's dtype, then stored in
+    groups of 64 elements as s (c - z), codes and zero point of 4 bits.  Returns the queries."""
+    return _append(True, cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace)
+
+
+def kv4_read(cache: KVCache4, batch: KVBatch, k=None, v=None, workspace=None):
+    """What the cache stands for in the rows of the batch's new tokens: (k, v), each [tokens,
+    kv_heads, head_dim] in the cache's dtype."""
+    _kind(cache, True)
+    torch = _torch()
+    if batch.index != cache.index:
+        _bad("the batch is on %s, the cache on %s" % (batch.device, cache.device))
+    ws = None if workspace is None else _status(workspace, cache)
+    _on_current(cache)
+    both = []
+    for name, t in (("k", k), ("v", v)):
+        if t is None:
+            t = torch.empty((batch.tokens, cache.kv_heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+        elif not t.is_contiguous():
+            _bad("%s must be contiguous" % name)
+        else:
+            _rows(name, t, cache, batch, cache.kv_heads)
+        both.append(t)
+    _check(load().mc_kv4_read(cache._ref, batch._ref, both[0].data_ptr(), both[1].data_ptr(), ws, _stream()))
+    return both[0], both[1]
+
+
+def attn4_decode(cache: KVCache4, batch: KVBatch, q, scale=None, softcap: float = 0.0, window: int = 0, slopes=None,
+                 out=None, with_lse: bool = False, workspace=None):
+    """attn_decode over a cache in 4 bits (workspace: attn4_workspace's)."""
+    return _attention(False, cache, batch, q, scale, softcap, window, slopes, None, out, with_lse, workspace, True)
+
+
+def attn4_prefill(cache: KVCache4, batch: KVBatch, q, scale=None, softcap: float = 0.0, window: int = 0, slopes=None,
+                  prefix=None, out=None, with_lse: bool = False, workspace=None):
+    """attn_prefill over a cache in 4 bits (workspace: attn4_workspace's)."""
+    return _attention(True, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace, True)
+
+
+# ------------------------------------------------------------ block tables --
+
+class _KvPoolC(ctypes.Structure):
+    _fields_ = [("ring", ctypes.c_void_p), ("state", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class KVPool:
+    """The free pages of a cache: a ring of them, int32 [num_pages], and two counts, int64 [2]: pages ever
+    taken, pages ever returned (at first all are free: 0 and num_pages)."""
+
+    def __init__(self, num_pages: int, page_size: int, device="cuda", ring=None, state=None):
+        import torch
+        if ring is None:
+            ring = torch.arange(num_pages, dtype=torch.int32, device=device)
+        if state is None:
+            state = torch.tensor([0, num_pages], dtype=torch.int64, device=ring.device)
+        if ring.dtype != torch.int32 or tuple(ring.shape) != (num_pages,) or not ring.is_contiguous():
+            _bad("ring must be a contiguous int32 [num_pages = %d]" % num_pages)
+        if state.dtype != torch.int64 or tuple(state.shape) != (2,) or not state.is_contiguous() or state.device != ring.device:
+            _bad("state must be a contiguous int64 [2] on the ring's device")
+        self.ring, self.state, self.device, self.index = ring, state, ring.device, ring.get_device()
+        self.num_pages, self.page_size = int(num_pages), int(page_size)
+        self._c = _KvPoolC(ring.data_ptr(), state.data_ptr(), self.num_pages, self.page_size)
+        self._ref = ctypes.addressof(self._c)
+
+
+class KVPlan:
+    """A step's lengths (with the new tokens), row boundaries, positions and slots (None where not asked for),
+    and the pool's counts after it; batch: the KVBatch of the appends and the attentions."""
+
+    def __init__(self, lens, cu_q, positions, slots, state, table, tokens):
+        self.lens, self.cu_q, self.positions, self.slots, self.state, self._table, self._tokens = lens, cu_q, positions, slots, state, table, tokens
+        self._batch = None
+
+    @property
+    def batch(self):
+        if self._batch is None:
+            self._batch = KVBatch(self.lens, self._table, self.cu_q, self._tokens)
+        return self._batch
+
+
+def kv_plan_workspace(seqs: int, device="cuda"):
+    """Zeroed workspace of kv_plan for up to `seqs` sequences (its status word: check_status)."""
+    import torch
+    n = load().mc_kv_plan_workspace_size(int(seqs))
+    if n == 0:
+        raise MCError(ERR_INVALID_ARG, last_error())
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=None, positions: bool = True, slots: bool = True,
+            commit: bool = True, workspace=None):
+    """The pages and slots of a step's new tokens, from the lengths of its sequences: add[b] new tokens of
+    sequence b, after lens[b] that it has (int32 [seqs], on the GPU).  Sequences with done[b] != 0 (uint8 [seqs])
+    give their pages back first and start at length 0.  New pages come from the pool and are entered into
+    table (int32 [seqs, width]).  A sequence that cannot have its pages, or rows among the `tokens` of the step's
+    token arrays (by default: one for each sequence), gets no tokens, and check_status(workspace) raises ERR_RANGE.
+    lens_out: may be lens; without it lens stays as it is.  commit=False leaves the pool's counts as they are: what
+    the step would be.  Returns a KVPlan."""
+    torch = _torch()
+    if table.dim() != 2 or lens.dim() != 1 or table.shape[0] != lens.shape[0]:
+        _bad("lens [seqs] and table [seqs, width]")
+    seqs = lens.shape[0]
+    dev = pool.device
+    for name, t, dt, shape in (("table", table, torch.int32, table.shape), ("lens", lens, torch.int32, (seqs,)), ("add", add, torch.int32, (seqs,)),
+                               ("done", done, torch.uint8, (seqs,)), ("lens_out", lens_out, torch.int32, (seqs,))):
+        if t is not None and (t.dtype is not dt or t.shape != shape or not t.is_contiguous() or t.get_device() != pool.index):
+            _bad("%s must be a contiguous %s %s on the pool's device" % (name, dt, list(shape)))
+    _on_current(pool, "pool")
+    tokens = seqs if tokens is None else int(tokens)
+    if workspace is None:
+        workspace = kv_plan_workspace(seqs, dev)
+    ws = _status(workspace, pool, "pool")
+    empty = torch.empty
+    if lens_out is None:
+        lens_out = empty(seqs, dtype=torch.int32, device=dev)
+    cu_q = empty(seqs + 1, dtype=torch.int32, device=dev)
+    pos = empty(tokens, dtype=torch.int32, device=dev) if positions else None
+    slot = empty(tokens, dtype=torch.int64, device=dev) if slots else None
+    state = pool.state if commit else empty(2, dtype=torch.int64, device=dev)
+    rc = load().mc_kv_plan(pool._ref, lens.data_ptr(), add.data_ptr(), None if done is None else done.data_ptr(), seqs, tokens,
+                           table.data_ptr(), table.shape[1], lens_out.data_ptr(), cu_q.data_ptr(), pos.data_ptr() if positions else None,
+                           slot.data_ptr() if slots else None, state.data_ptr(), ws, workspace.numel() * workspace.element_size(), _stream())
+    if rc:
+        _check(rc)
+    return KVPlan(lens_out, cu_q, pos, slot, state, table, tokens)
+
+
+# -------------------------------------------------------- between the blocks --
+
+class _ResidualC(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("H", ctypes.c_int32), ("dtype", ctypes.c_int32), ("y", ctypes.c_void_p), ("h", ctypes.c_void_p),
+                ("y_stride", ctypes.c_int64), ("h_stride", ctypes.c_int64), ("post_norm", ctypes.c_void_p), ("pre_norm", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_row", ctypes.c_int64), ("gate_col", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float), ("h_out", ctypes.c_void_p), ("x", ctypes.c_void_p),
+                ("h_out_stride", ctypes.c_int64), ("x_stride", ctypes.c_int64)]
+
+
+def residual_norm(y, h, pre_norm=None, post_norm=None, gate=None, scale: float = 1.0, residual_scale: float = 1.0, eps: float = 1e-5,
+                  h_out=None, x=None):
+    """What lies between a block's output y and the next block, for the residual h, both [T, H] in bf16 or fp16:
+        u = rmsnorm(y) * post_norm            (post_norm [H]; None: u = y)
+        h_out = residual_scale * h + scale * gate * u       (gate [1 or T, 1 or H]; None: 1)
+        x = rmsnorm(h_out) * pre_norm         (pre_norm [H]; None: no x)
+    Rows may be strided.  h_out may be h or y, x may be y.  Returns (h_out, x)."""
+    torch = _torch()
+    codes = {torch.bfloat16: 0, torch.float16: 1}
+    if y.dtype not in codes:
+        raise MCError(ERR_UNSUPPORTED, "rows of %s" % y.dtype)
+    if y.dim() != 2 or y.shape[1] < 1:
+        _bad("y must be [T, H]")
+    T, H = y.shape
+    here = y.get_device()
+    if here < 0 or here != torch.cuda.current_device():
+        _bad("y is on %s, not on the current device" % y.device)
+    for name, t, shape in (("h", h, (T, H)), ("h_out", h_out, (T, H)), ("x", x, (T, H)), ("pre_norm", pre_norm, (H,)), ("post_norm", post_norm, (H,))):
+        if t is not None and (t.shape != shape or t.dtype is not y.dtype or t.get_device() != here or (H > 1 and t.stride(-1) != 1)):
+            _bad("%s must be %s of %s on y's device, the columns contiguous" % (name, list(shape), y.dtype))
+    if H > 1 and y.stride(1) != 1:
+        _bad("the columns of y must be contiguous")
+    row = col = 0
+    if gate is not None:
+        if gate.dim() != 2 or gate.shape[0] not in (1, T) or gate.shape[1] not in (1, H) or gate.dtype is not y.dtype or gate.get_device() != here:
+            _bad("gate must be [1 or %d, 1 or %d] of %s on y's device" % (T, H, y.dtype))
+        row = gate.stride(0) if gate.shape[0] > 1 else 0
+        col = gate.stride(1) if gate.shape[1] > 1 else 0
+        if col not in (0, 1):
+            _bad("the columns of the gate must be contiguous")
+    if h_out is None:
+        h_out = torch.empty((T, H), dtype=y.dtype, device=y.device)
+    if pre_norm is None:
+        x = None
+    elif x is None:
+        x = torch.empty((T, H), dtype=y.dtype, device=y.device)
+    step = lambda t: t.stride(0) if T > 1 else H  # noqa: E731  (a single row's stride means nothing)
+    a = _ResidualC(T, H, codes[y.dtype], y.data_ptr(), h.data_ptr(), step(y), step(h), _ptr(post_norm), _ptr(pre_norm), _ptr(gate), row, col,
+                   scale, residual_scale, eps, h_out.data_ptr(), _ptr(x), step(h_out), step(x) if x is not None else H)
+    rc = load().mc_residual_norm(ctypes.addressof(a), _stream())
+    if rc:
+        _check(rc)
+    return h_out, x
+
+
 # -------------------------------------------------------------- profiling --
 
-N_KERNELS = 15
+N_KERNELS = 18
 
 
 def token_importance(t, attn, protect_frac: float = 0.02, importance=None, mask=None, with_mask: bool = True,

@@ -1,6 +1,6 @@
 /*
  * mc_bind.c -- argument marshalling of the calls that a decode step makes many times a
- * second (kv_append, attn_decode, attn_prefill), as a CPython extension: what the binding
+ * second (kv_append, attn_decode, attn_prefill and their 4-bit forms), as a CPython extension: what the binding
  * does in Python with ctypes costs 6 to 8 us a call, several times such a call's kernels.
  *
  * It takes the plain cases only.  Whatever is not as it should be (a shape, a stride, a type,
@@ -18,8 +18,8 @@ typedef int (*append_fn)(const mc_kv_cache *, const mc_kv_batch *, const void *,
 typedef int (*attn_fn)(const mc_kv_cache *, const mc_kv_batch *, const void *, int64_t, int, const mc_attn_opts *, void *, int64_t,
                        float *, void *, size_t, void *);
 
-static append_fn c_append;
-static attn_fn c_attn[2]; /* decode, prefill */
+static append_fn c_append[2]; /* to the 16-bit cache, to the 4-bit one */
+static attn_fn c_attn[4];     /* decode, prefill; over the 4-bit cache */
 static PyObject *t_empty, *t_stream, *t_device, *t_float32, *t_int32, *t_uint8;
 static PyObject *n_shape, *n_stride, *n_dtype, *n_device, *n_get_device, *n_data_ptr, *n_is_contiguous, *n_ref, *n_index,
     *kw_empty;
@@ -159,12 +159,13 @@ static PyObject *leave(Call *c)
     Py_RETURN_NONE;
 }
 
-/* kv_append(cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace) */
-static PyObject *kv_append(PyObject *self, PyObject *const *a, Py_ssize_t na)
+/* append(bits4, cache, batch, q, k, v, rope, interleaved, q_norm, k_norm, eps, q_out, workspace) */
+static PyObject *append(PyObject *self, PyObject *const *a, Py_ssize_t na)
 {
     (void)self;
     Call c = {0};
-    if (na != 12 || !begin(&c, a[0], a[1])) return leave(&c);
+    const int bits4 = na == 13 ? PyObject_IsTrue(*a++) : -1;
+    if (bits4 < 0 || !begin(&c, a[0], a[1])) return leave(&c);
     int heads = 0, kh;
     int64_t qs, ks, vs, os, n[2], rope_n[2] = {0, 0};
     const void *rope, *qn, *kn, *ws = NULL;
@@ -191,7 +192,7 @@ static PyObject *kv_append(PyObject *self, PyObject *const *a, Py_ssize_t na)
     void *o = ptr_of(out);
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = c_append(c.cache, c.batch, q, qs, k, ks, v, vs, heads, qn, kn, (float)eps, (const float *)rope, (int)rope_n[0], (int)rope_n[1],
+    rc = c_append[bits4](c.cache, c.batch, q, qs, k, ks, v, vs, heads, qn, kn, (float)eps, (const float *)rope, (int)rope_n[0], (int)rope_n[1],
                   inter, o, (void *)ws, (void *)(intptr_t)st);
     Py_END_ALLOW_THREADS
     end(&c);
@@ -202,7 +203,7 @@ static PyObject *kv_append(PyObject *self, PyObject *const *a, Py_ssize_t na)
     return out;
 }
 
-/* attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace) */
+/* attention(which, cache, batch, q, scale, softcap, window, slopes, prefix, out, with_lse, workspace) */
 static PyObject *attention(PyObject *self, PyObject *const *a, Py_ssize_t na)
 {
     (void)self;
@@ -222,9 +223,10 @@ static PyObject *attention(PyObject *self, PyObject *const *a, Py_ssize_t na)
     o.window = (int32_t)window;
     o.slopes = (const float *)slopes;
     o.prefix = (const int32_t *)prefix;
-    const int kind = PyObject_IsTrue(a[0]), with_lse = PyObject_IsTrue(a[10]);
+    const long kind = PyLong_AsLong(a[0]);
+    const int with_lse = PyObject_IsTrue(a[10]);
     const int64_t st = stream_of(&c);
-    if (st < 0 || kind < 0 || with_lse < 0 || window != o.window || PyErr_Occurred()) return leave(&c);
+    if (st < 0 || kind < 0 || kind > 3 || with_lse < 0 || window != o.window || PyErr_Occurred()) return leave(&c);
     PyObject *out = a[9], *lse = NULL;
     if (out == Py_None) {
         out = empty3(&c, c.batch->tokens, heads, c.cache->head_dim, c.dtype);
@@ -259,16 +261,18 @@ static PyObject *attention(PyObject *self, PyObject *const *a, Py_ssize_t na)
     return both;
 }
 
-/* setup(append, decode, prefill, empty, raw_stream, current_device, float32, int32, uint8) */
+/* setup(append, decode, prefill, append4, decode4, prefill4, empty, raw_stream, current_device, float32, int32, uint8) */
 static PyObject *setup(PyObject *self, PyObject *args)
 {
     (void)self;
-    unsigned long long fa, fd, fp;
+    unsigned long long f[6];
     PyObject *o[6];
-    if (!PyArg_ParseTuple(args, "KKKOOOOOO", &fa, &fd, &fp, &o[0], &o[1], &o[2], &o[3], &o[4], &o[5])) return NULL;
-    c_append = (append_fn)(uintptr_t)fa;
-    c_attn[0] = (attn_fn)(uintptr_t)fd;
-    c_attn[1] = (attn_fn)(uintptr_t)fp;
+    if (!PyArg_ParseTuple(args, "KKKKKKOOOOOO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &o[0], &o[1], &o[2], &o[3], &o[4], &o[5])) return NULL;
+    for (int i = 0; i < 2; ++i) {
+        c_append[i] = (append_fn)(uintptr_t)f[3 * i];
+        c_attn[2 * i] = (attn_fn)(uintptr_t)f[3 * i + 1];
+        c_attn[2 * i + 1] = (attn_fn)(uintptr_t)f[3 * i + 2];
+    }
     PyObject **to[6] = {&t_empty, &t_stream, &t_device, &t_float32, &t_int32, &t_uint8};
     for (int i = 0; i < 6; ++i) {
         Py_INCREF(o[i]);
@@ -278,7 +282,7 @@ static PyObject *setup(PyObject *self, PyObject *args)
 }
 
 static PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, "entry points and torch's parts"},
-                                {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, ""},
+                                {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, ""},
                                 {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, ""},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mcbind", NULL, -1, methods, NULL, NULL, NULL, NULL};

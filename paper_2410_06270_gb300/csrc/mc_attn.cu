@@ -7,6 +7,7 @@
 
 #include "mc_attn.h"
 #include "mc_host.h"
+#include "mc_kv4.cuh"
 #include "mc_profile.h"
 
 namespace mc {
@@ -27,7 +28,8 @@ cudaError_t sm_count(int *out)
     return cudaSuccess;
 }
 
-static int check_cache(const mc_kv_cache *c, int q_heads)
+// q4: the cache is the 4-bit one (page_stride in bytes)
+static int check_cache(const mc_kv_cache *c, int q_heads, bool q4)
 {
     if (!c) return set_error(MC_ERR_INVALID_ARG, "NULL cache");
     if (c->dtype != MC_BF16 && c->dtype != MC_FP16) return set_error(MC_ERR_UNSUPPORTED, "cache dtype %d", c->dtype);
@@ -38,8 +40,8 @@ static int check_cache(const mc_kv_cache *c, int q_heads)
     if (c->page_size < 16 || c->page_size > 32768 || c->page_size % 16)
         return set_error(MC_ERR_INVALID_ARG, "page_size %d (a multiple of 16, at most 32768)", c->page_size);
     if (c->num_pages < 1) return set_error(MC_ERR_INVALID_ARG, "num_pages %d", c->num_pages);
-    if (c->page_stride % 8 || c->page_stride < (int64_t)c->kv_heads * c->page_size * c->head_dim ||
-        c->page_stride >= (int64_t)1 << 38)
+    const int64_t page = (int64_t)c->kv_heads * c->page_size * (q4 ? kv4_row_bytes(c->head_dim) : c->head_dim);
+    if (c->page_stride % (q4 ? 16 : 8) || c->page_stride < page || c->page_stride >= (int64_t)1 << 38)
         return set_error(MC_ERR_INVALID_ARG, "page_stride %lld", (long long)c->page_stride);
     return MC_OK;
 }
@@ -96,14 +98,16 @@ static bool countable(const mc_kv_cache *c, const mc_kv_batch *b, int group)
     return (rows / 256 + 1) * (most / 128 + 3) < 0x7fffffff && (rows / 8 + b->seqs) * c->kv_heads * (most / 64 + 3) < 0x1p38;
 }
 
+static size_t workspace_size(int head_dim) { return 256 + std::max(decode_part_bytes(head_dim), prefill_part_bytes(head_dim)); }
+
 constexpr int kFewRows = 16, kFewRowsCap = 32;
 
 static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
                      const mc_attn_opts *o, void *out, int64_t out_stride, float *lse, void *workspace, size_t ws_bytes,
-                     bool decode, void *stream)
+                     bool decode, bool q4, void *stream)
 {
     clear_error();
-    int rc = check_cache(cache, q_heads);
+    int rc = check_cache(cache, q_heads, q4);
     if (rc || (rc = check_counts(batch))) return rc;
     if (!o) return set_error(MC_ERR_INVALID_ARG, "NULL options");
     // (the scale, its product with log2 e and its quotient by the cap stay in fp32's range)
@@ -119,7 +123,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     if (!aligned(lse, 4) || !aligned(o->slopes, 4) || !aligned(o->prefix, 4))
         return set_error(MC_ERR_INVALID_ARG, "misaligned lse, slopes or prefix");
     if (!workspace || !aligned(workspace, 256)) return set_error(MC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-    const size_t need = mc_attn_workspace_size(cache, q_heads);
+    const size_t need = workspace_size(cache->head_dim);
     if (ws_bytes < need) return set_error(MC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", ws_bytes, need);
     if (!countable(cache, batch, q_heads / cache->kv_heads))
         return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d sequences, tables of %d pages of %d keys, in one call", batch->tokens,
@@ -149,30 +153,18 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     // 36 / 51 at 20 and 44 / 51 at 32; one sequence of 2000 keys, 16 rows, 12 / 14.
     const int64_t rows = ((int64_t)batch->tokens + batch->seqs - 1) / batch->seqs * p.group;
     const bool bf16 = cache->dtype == MC_BF16;
+    if (q4) return launch_rows4(p, cache->head_dim, bf16, (cudaStream_t)stream);
     if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, (int)rows, (cudaStream_t)stream);
     return launch_prefill(p, cache->head_dim, bf16, (cudaStream_t)stream);
 }
 
-}  // namespace mc
-
-using namespace mc;
-
-extern "C" {
-
-size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads)
+static int append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
+                  int64_t k_stride, const void *v, int64_t v_stride, int q_heads, const void *q_norm, const void *k_norm,
+                  float eps, const float *rope, int rope_rows, int rot_dim, int interleaved, void *q_out, void *workspace,
+                  bool q4, void *stream)
 {
     clear_error();
-    if (check_cache(cache, q_heads)) return 0;
-    return 256 + std::max(decode_part_bytes(cache->head_dim), prefill_part_bytes(cache->head_dim));
-}
-
-int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
-                 int64_t k_stride, const void *v, int64_t v_stride, int q_heads, const void *q_norm,
-                 const void *k_norm, float eps, const float *rope, int rope_rows, int rot_dim, int interleaved,
-                 void *q_out, void *workspace, void *stream)
-{
-    clear_error();
-    int rc = check_cache(cache, q_heads);
+    int rc = check_cache(cache, q_heads, q4);
     if (rc || (rc = check_counts(batch))) return rc;
     const int D = cache->head_dim;
     if (rot_dim < 0 || rot_dim > D || rot_dim % 16)
@@ -207,21 +199,91 @@ int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void 
     p.interleaved = interleaved != 0;
     p.q_out = (uint16_t *)q_out;
     p.status = (int32_t *)workspace;
-    return launch_append(p, D, cache->dtype == MC_BF16, (cudaStream_t)stream);
+    return launch_append(p, D, cache->dtype == MC_BF16, q4, (cudaStream_t)stream);
+}
+
+}  // namespace mc
+
+using namespace mc;
+
+extern "C" {
+
+size_t mc_attn_workspace_size(const mc_kv_cache *cache, int q_heads)
+{
+    clear_error();
+    return check_cache(cache, q_heads, false) ? 0 : workspace_size(cache->head_dim);
+}
+
+size_t mc_attn4_workspace_size(const mc_kv_cache *cache, int q_heads)
+{
+    clear_error();
+    return check_cache(cache, q_heads, true) ? 0 : workspace_size(cache->head_dim);
+}
+
+size_t mc_kv4_block_size(int page_size, int head_dim)
+{
+    clear_error();
+    const mc_kv_cache c = {nullptr, nullptr, (int64_t)1 << 37, 1, page_size, 1, head_dim, MC_BF16};
+    return check_cache(&c, 1, true) ? 0 : (size_t)page_size * kv4_row_bytes(head_dim);
+}
+
+int mc_kv_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
+                 int64_t k_stride, const void *v, int64_t v_stride, int q_heads, const void *q_norm,
+                 const void *k_norm, float eps, const float *rope, int rope_rows, int rot_dim, int interleaved,
+                 void *q_out, void *workspace, void *stream)
+{
+    return append(cache, batch, q, q_stride, k, k_stride, v, v_stride, q_heads, q_norm, k_norm, eps, rope, rope_rows, rot_dim,
+                  interleaved, q_out, workspace, false, stream);
+}
+
+int mc_kv4_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
+                  int64_t k_stride, const void *v, int64_t v_stride, int q_heads, const void *q_norm,
+                  const void *k_norm, float eps, const float *rope, int rope_rows, int rot_dim, int interleaved,
+                  void *q_out, void *workspace, void *stream)
+{
+    return append(cache, batch, q, q_stride, k, k_stride, v, v_stride, q_heads, q_norm, k_norm, eps, rope, rope_rows, rot_dim,
+                  interleaved, q_out, workspace, true, stream);
+}
+
+int mc_kv4_read(const mc_kv_cache *cache, const mc_kv_batch *batch, void *k, void *v, void *workspace, void *stream)
+{
+    clear_error();
+    int rc = check_cache(cache, cache ? cache->kv_heads : 1, true);
+    if (rc || (rc = check_counts(batch))) return rc;
+    if (batch->tokens == 0 || batch->seqs == 0 || (!k && !v)) return MC_OK;
+    if ((rc = check_batch(cache, batch))) return rc;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(workspace, 4))
+        return set_error(MC_ERR_INVALID_ARG, "k and v must be 16-byte aligned, the workspace 4");
+    ReadParams p = {view(cache), view(batch), (uint16_t *)k, (uint16_t *)v, (int32_t *)workspace};
+    return launch_read4(p, cache->head_dim, cache->dtype == MC_BF16, (cudaStream_t)stream);
 }
 
 int mc_attn_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
                    const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
                    size_t ws_bytes, void *stream)
 {
-    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, true, stream);
+    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, true, false, stream);
 }
 
 int mc_attn_prefill(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
                     const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
                     size_t ws_bytes, void *stream)
 {
-    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, false, stream);
+    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, false, false, stream);
+}
+
+int mc_attn4_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                   const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                   size_t ws_bytes, void *stream)
+{
+    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, true, true, stream);
+}
+
+int mc_attn4_prefill(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
+                    const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
+                    size_t ws_bytes, void *stream)
+{
+    return attention(cache, batch, q, q_stride, q_heads, opts, out, out_stride, lse, workspace, ws_bytes, false, true, stream);
 }
 
 }  // extern "C"

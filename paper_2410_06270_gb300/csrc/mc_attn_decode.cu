@@ -24,7 +24,7 @@
 // sequences of a window of 1024 keys, 12 heads a key head: 17 us, special functions 4 % active).
 #include <math.h>
 
-#include "mc_attn.h"
+#include "mc_attn_row.cuh"
 #include "mc_host.h"
 #include "mc_profile.h"
 
@@ -159,8 +159,8 @@ __device__ __noinline__ void redo_row(const AttnParams &p, int b, int tok, int h
     const Keys k = keys_of<D>(p, b, nullptr);
     const int h = p.by_group.div(head), pos = k.len - k.n + tok, prefix = p.prefix ? __ldg(p.prefix + b) : 0;
     const int lo = p.window ? max(0, pos - p.window + 1) : 0, hi = pos < 0 ? 0 : max(pos + 1, prefix);
-    if (odd_keys<D, BF16>(p, b, h, k.start, min(lo, k.len), 0, 1, lane) || odd_keys<D, BF16>(p, b, h, max(hi, k.start), k.len, 0, 1, lane))
-        exact_row<D, BF16>(p, b, pos, k.len, prefix, k.first + tok, head, lane);
+    if (odd_keys<D, BF16, false>(p, b, h, k.start, min(lo, k.len), 0, 1, lane) || odd_keys<D, BF16, false>(p, b, h, max(hi, k.start), k.len, 0, 1, lane))
+        exact_row<D, BF16, false>(p, b, pos, k.len, prefix, k.first + tok, head, lane);
 }
 
 __host__ __device__ constexpr size_t dec_part_floats(int D, int nt) { return (size_t)8 * nt * (D + 2); }

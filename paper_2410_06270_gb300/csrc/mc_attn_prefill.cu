@@ -39,7 +39,7 @@
 
 #include <cuda.h>
 
-#include "mc_attn.h"
+#include "mc_attn_row.cuh"
 #include "mc_host.h"
 #include "mc_profile.h"
 #include "mc_umma.cuh"
@@ -1070,8 +1070,8 @@ __device__ __forceinline__ bool pf_hides_odd(const PfParams &pp, int b, int h, i
     const int from = k.first & -pp.box_rows, to = min(s.len, (k.end + pp.box_rows - 1) & -pp.box_rows);  // whole boxes
     const int p0 = s.len - s.n + t0, p1 = s.len - s.n + t1;
     const int lo = p.window ? max(0, p1 - p.window + 1) : 0, hi = p0 < 0 ? 0 : max(p0 + 1, s.prefix);
-    return odd_keys<D, BF16>(p, b, h, from, min(lo, to), warp, warps, lane) ||
-           odd_keys<D, BF16>(p, b, h, max(hi, from), to, warp, warps, lane);
+    return odd_keys<D, BF16, false>(p, b, h, from, min(lo, to), warp, warps, lane) ||
+           odd_keys<D, BF16, false>(p, b, h, max(hi, from), to, warp, warps, lane);
 }
 
 constexpr int kPfJoinRows = 16;  // rows of an open item that a block of the join launch adds
@@ -1082,7 +1082,7 @@ __device__ __noinline__ void pf_redo_row(const PfParams &pp, int b, int mt, int 
 {
     const PfSeq s = pf_seq(pp.a, b, nullptr);
     if (pf_hides_odd<D, BF16>(pp, b, pp.a.by_group.div(head), mt, s, tok, tok, 0, 1, lane))
-        exact_row<D, BF16>(pp.a, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
+        exact_row<D, BF16, false>(pp.a, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
 }
 
 // 16 rows of a CTA's open item: adds its pieces in their order, the loads of four pieces
@@ -1178,7 +1178,7 @@ __device__ __noinline__ void pf_redo(const PfParams &pp)
                     odd = fmaf(v.x, 0.f, fmaf(v.y, 0.f, odd));
                 }
                 if (__any_sync(0xffffffffu, odd != odd))
-                    exact_row<D, BF16>(p, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
+                    exact_row<D, BF16, false>(p, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
             }
         }
         turn -= slices;

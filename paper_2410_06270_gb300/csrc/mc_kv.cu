@@ -1,9 +1,10 @@
-// mc_kv.cu -- mc_kv_append: new tokens into the paged key-value cache, with the per-head
-// norms and the position rotation on the way.
+// mc_kv.cu -- mc_kv_append and mc_kv4_append: new tokens into the paged key-value cache, in 16 or in 4 bits,
+// with the per-head norms and the position rotation on the way; mc_kv4_read: the 4-bit cache's rows as they stand.
 #include <math.h>
 
 #include "mc_attn.h"
 #include "mc_host.h"
+#include "mc_kv4.cuh"
 #include "mc_profile.h"
 
 namespace mc {
@@ -34,10 +35,15 @@ __device__ __forceinline__ uint64_t swapped(uint64_t v)
 // two at a time (f32x2).  Issue-bound before that (850 instructions a warp, rows of all kinds
 // alike): 8192 tokens of 48 heads of 128, norms and rotation, 48 us; now 37 us, 5.6 TB/s (issue
 // 77 % active, ALU 61 %).  Eight passes a warp (84 registers) took 48 us where four took 41.
-template <int D, bool BF16>
+//
+// Q4: a key's or value's row, rounded to the type, is brought into its own order where the rotation's runs are
+// not (through shared memory, a row of D elements by its D / 8 lanes), so that the 8 lanes of a group hold its 64
+// elements, 8 each; they find its ends by exchanging pairs and each writes a word of codes.
+template <int D, bool BF16, bool Q4>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams p)
 {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+    __shared__ __align__(16) uint16_t rows_s[Q4 ? kAppendThreads / 32 : 1][Q4 ? 256 : 8];
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, li = lane % kLanes;
@@ -84,7 +90,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
     const TokenPlace place = token_place(p.b, p.c, t, lane, p.status);
     if (place.seq < 0) return;  // padding
     int pos = place.pos;
-    int64_t at = -1;  // the row's element offset in the cache
+    int64_t at = -1;  // the row's element offset in the cache (Q4: of its page, in bytes)
+    int at_row = 0;
     float4 cs = make_float4(1.f, 1.f, 1.f, 1.f), sn = make_float4(0.f, 0.f, 0.f, 0.f);
     if (p.rot && pos >= p.rope_rows) {
         set_status(p.status, MC_ERR_RANGE);
@@ -99,17 +106,44 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
         if (!is_q) {
             int row;
             const int i = p.c.page.div(pos, row), page = seq_page(p.b, p.c, place.seq, i, p.status);
-            if (page >= 0) at = page * p.c.page_stride + (int64_t)row * D;
+            if (page >= 0) at = page * p.c.page_stride + (Q4 ? 0 : (int64_t)row * D);
+            at_row = row;
         }
     }
     if (!is_q && at < 0) return;
-    uint16_t *dst = is_q ? p.q_out + (int64_t)t * p.q_heads * D : (is_v ? p.c.v : p.c.k) + at;
+    uint16_t *dst = is_q ? p.q_out + (int64_t)t * p.q_heads * D : Q4 ? nullptr : (is_v ? p.c.v : p.c.k) + at;
     const int64_t head_stride = is_q ? D : (int64_t)p.c.page_size * D;
+    // a row of a key or value on its grids; the whole warp, with rows of heads past the last among them
+    auto store4 = [&](int h, const uint32_t (&v)[4]) {
+        uint32_t x[4] = {v[0], v[1], v[2], v[3]}, word;
+        if (rot && !p.interleaved) {
+            uint16_t *own = rows_s[threadIdx.x >> 5] + lane / kLanes * D;
+            *reinterpret_cast<uint2 *>(own + ea) = make_uint2(v[0], v[1]);
+            *reinterpret_cast<uint2 *>(own + eb) = make_uint2(v[2], v[3]);
+            __syncwarp();
+            const uint4 y = *reinterpret_cast<const uint4 *>(own + 8 * li);
+            x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
+            __syncwarp();
+        }
+        const uint32_t codes = kv4_quantise<BF16>(x, word);
+        if (h >= heads) return;
+        constexpr int kGroups = D / kKv4Group;
+        const int g = li / 8, i = li % 8;
+        uint8_t *block = reinterpret_cast<uint8_t *>(is_v ? p.c.v : p.c.k) + at + (int64_t)h * p.c.page_size * kv4_row_bytes(D);
+        *reinterpret_cast<uint32_t *>(block + at_row * kv4_code_bytes(D) + 4 * (i * kGroups + g)) = codes;
+        if (i == 0)
+            *reinterpret_cast<uint16_t *>(block + p.c.page_size * kv4_code_bytes(D) + at_row * kv4_word_bytes(D) + 2 * g) = (uint16_t)word;
+    };
 
     if ((!gain && !rot) || pos < 0) {  // copied, or zero
 #pragma unroll
         for (int i = 0; i < kAppendPasses; ++i) {
             const int h = h0 + i * kRows;
+            if (Q4 && !is_q) {
+                if (h - lane / kLanes >= heads) break;  // (for all lanes)
+                store4(h, {a[i].x, a[i].y, b[i].x, b[i].y});
+                continue;
+            }
             if (h >= heads) continue;
             *reinterpret_cast<uint2 *>(dst + h * head_stride + ea) = pos < 0 ? make_uint2(0, 0) : a[i];
             *reinterpret_cast<uint2 *>(dst + h * head_stride + eb) = pos < 0 ? make_uint2(0, 0) : b[i];
@@ -174,22 +208,79 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
             unpair2(z, lo, hi);
             out[e] = pack2<BF16>(lo, hi);
         }
-        if (h < heads) {
+        if (Q4 && !is_q) {
+            store4(h, out);
+        } else if (h < heads) {
             *reinterpret_cast<uint2 *>(dst + h * head_stride + ea) = make_uint2(out[0], out[1]);
             *reinterpret_cast<uint2 *>(dst + h * head_stride + eb) = make_uint2(out[2], out[3]);
         }
     }
 }
 
-int launch_append(AppendParams p, int head_dim, bool bf16, cudaStream_t st)
+// Rows of the batch's new tokens as they are stored: a warp takes a token's heads of one side (keys or values),
+// 256 elements at a time, a word of codes a lane.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kAppendThreads) read4_kernel(const ReadParams p)
+{
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes, kGroups = D / kKv4Group;
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, li = lane % kLanes, g = li / 8, i = li % 8;
+    const int64_t warp = (int64_t)blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
+    const int t = (int)(warp >> 1);
+    if (t >= p.b.tokens) return;
+    uint16_t *out = warp & 1 ? p.v : p.k;
+    if (!out) return;
+    const TokenPlace place = token_place(p.b, p.c, t, lane, p.status);
+    if (place.seq < 0) return;  // padding
+    int row = 0, page = -1;
+    if (place.pos >= 0) {
+        const int n = p.c.page.div(place.pos, row);
+        page = seq_page(p.b, p.c, place.seq, n, p.status);
+    }
+    out += (int64_t)t * p.c.kv_heads * D;
+    for (int h = lane / kLanes; h < p.c.kv_heads; h += kRows) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (page >= 0) {
+            const uint8_t *block = kv4_block<D>(p.c, warp & 1 ? p.c.v : p.c.k, page, h);
+            const uint32_t codes = *reinterpret_cast<const uint32_t *>(block + row * kv4_code_bytes(D) + 4 * (i * kGroups + g));
+            const uint32_t word = *reinterpret_cast<const uint16_t *>(block + p.c.page_size * kv4_code_bytes(D) + row * kv4_word_bytes(D) + 2 * g);
+            using P = Kv4Pairs<BF16>;
+            const uint32_t z = P::zeros(word), s = P::scales(word);
+            x = make_uint4(P::mul(P::sub(P::magic(codes, 0), z), s), P::mul(P::sub(P::magic(codes, 1), z), s),
+                           P::mul(P::sub(P::magic(codes, 2), z), s), P::mul(P::sub(P::magic(codes, 3), z), s));
+        }
+        *reinterpret_cast<uint4 *>(out + h * D + 8 * li) = x;
+    }
+}
+
+int launch_read4(const ReadParams &p, int head_dim, bool bf16, cudaStream_t st)
+{
+    const int64_t ctas = ((int64_t)p.b.tokens * 2 + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
+    auto k = head_dim == 64 ? (bf16 ? read4_kernel<64, true> : read4_kernel<64, false>)
+                            : (bf16 ? read4_kernel<128, true> : read4_kernel<128, false>);
+    profile_begin(kKRead, st);
+    cudaError_t e = launch_k(k, dim3((unsigned)ctas), dim3(kAppendThreads), 0, st, p);
+    profile_end(kKRead, st);
+    if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "read launch: %s", cudaGetErrorString(e));
+    return MC_OK;
+}
+
+template <bool Q4>
+static auto append_of(int head_dim, bool bf16)
+{
+    return head_dim == 64 ? (bf16 ? append_kernel<64, true, Q4> : append_kernel<64, false, Q4>)
+                          : (bf16 ? append_kernel<128, true, Q4> : append_kernel<128, false, Q4>);
+}
+
+int launch_append(AppendParams p, int head_dim, bool bf16, bool q4, cudaStream_t st)
 {
     const int per = append_warps(p.q_heads, head_dim) + 2 * append_warps(p.c.kv_heads, head_dim);
     const int64_t ctas = ((int64_t)p.b.tokens * per + (p.b.cu_q ? 1 : 0) + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
     if (ctas > 0x7fffffff / (kAppendThreads / 32))
         return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d heads in one call", p.b.tokens, p.q_heads + 2 * p.c.kv_heads);
     p.per_token = FastDiv(per);
-    auto k = head_dim == 64 ? (bf16 ? append_kernel<64, true> : append_kernel<64, false>)
-                            : (bf16 ? append_kernel<128, true> : append_kernel<128, false>);
+    auto k = q4 ? append_of<true>(head_dim, bf16) : append_of<false>(head_dim, bf16);
     profile_begin(kKAppend, st);
     cudaError_t e = launch_k(k, dim3((unsigned)ctas), dim3(kAppendThreads), 0, st, p);
     profile_end(kKAppend, st);

@@ -21,6 +21,9 @@ enum KernelId {
     kKAttnDecode,
     kKAttnPrefill,
     kKAttnJoin,   // partial results of items split over the cache's length
+    kKRead,       // rows of the 4-bit cache in 16 bits
+    kKPlan,       // pages and slots of a step
+    kKResidual,   // norms, gate and residual sum between blocks
     kKCount
 };
 

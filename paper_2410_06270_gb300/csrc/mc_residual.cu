@@ -1,0 +1,253 @@
+// mc_residual.cu -- mc_residual_norm: the norm behind a block, its gate and scale, the residual sum and
+// the norm before the next block, a token's row at a time.
+//
+//   u = y r(y) post,  h' = a h + b gate u,  x = h' r(h') pre,   r(v) = 1 / sqrt(mean(v^2) + eps)
+//
+// Bound by HBM: y, h (and a whole gate) read once, h' and x written once, 8 to 10 bytes an element for a dozen
+// flops.  A row stays in registers between the passes, all of its loads issued before the first use.
+// The sums take mc_rmsnorm's order (thread i of 256 over the 8-element chunks i, i + 256, ...; lanes by halves;
+// warps in turn), so x is bit for bit mc_rmsnorm of h_out, and short rows share a block, warps of 256 columns
+// each, with the same sums.
+#include <math.h>
+
+#include "mc_attn.h"
+#include "mc_host.h"
+#include "mc_profile.h"
+
+namespace mc {
+
+struct ResidualParams {
+    int T, H, rows, warps;  // rows a block, warps a row
+    const uint16_t *y, *h, *post, *pre, *gate;
+    int64_t y_stride, h_stride, gate_row, out_stride, x_stride;
+    int gate_col;
+    float scale, residual_scale, eps;
+    uint16_t *out, *x;
+};
+
+template <bool BF16>
+__device__ __forceinline__ float load1(const uint16_t *p)
+{
+    return BF16 ? __uint_as_float((uint32_t)*p << 16) : __half2float(*reinterpret_cast<const __half *>(p));
+}
+template <bool BF16>
+__device__ __forceinline__ uint16_t store1(float v)
+{
+    return (uint16_t)pack2<BF16>(v, 0.f);
+}
+
+// 1 / sqrt of a row's mean square, from each of its threads' part.
+__device__ __forceinline__ float row_rms(const ResidualParams &p, float ss, float *red, int w0)
+{
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+    if (p.warps == 1) return rsqrtf(ss / p.H + p.eps);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = ss;
+    __syncthreads();
+    float tot = 0.f;
+    for (int w = 0; w < p.warps; ++w) tot += red[w0 + w];
+    return rsqrtf(tot / p.H + p.eps);
+}
+
+__device__ __forceinline__ float value(const ResidualParams &p, float y, float h, float gate) { return fmaf(p.residual_scale, h, p.scale * (gate * y)); }
+
+// Rows of whole 16-byte chunks, PER of them a thread.
+template <int PER, bool BF16>
+__global__ void __launch_bounds__(256) residual_kernel(const ResidualParams p)
+{
+    __shared__ float red[2][16];  // (warps of no row read past the eighth)
+    pdl_trigger();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, sub = p.warps == 8 ? 0 : warp / p.warps, w0 = sub * p.warps;
+    const int first = threadIdx.x - 32 * w0, step = 32 * p.warps, n8 = p.H >> 3;
+    const int64_t t = (int64_t)blockIdx.x * p.rows + sub;
+    const bool real = sub < p.rows && t < p.T;
+    const bool gated = p.gate && p.gate_col;
+    uint4 y[PER], h[PER], gate[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int c = first + step * i;
+        const bool in = real && c < n8;
+        gate[i] = gated && in ? *reinterpret_cast<const uint4 *>(p.gate + t * p.gate_row + 8 * c) : make_uint4(0, 0, 0, 0);
+        y[i] = in ? *reinterpret_cast<const uint4 *>(p.y + t * p.y_stride + 8 * c) : make_uint4(0, 0, 0, 0);
+        h[i] = in ? *reinterpret_cast<const uint4 *>(p.h + t * p.h_stride + 8 * c) : make_uint4(0, 0, 0, 0);
+    }
+    const float whole = p.gate && !p.gate_col && real ? load1<BF16>(p.gate + t * p.gate_row) : 1.f;
+    float inv = 1.f;
+    if (p.post) {
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t w[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 f = unpack2<BF16>(w[k]);
+                ss = fmaf(f.x, f.x, ss);
+                ss = fmaf(f.y, f.y, ss);
+            }
+        }
+        inv = row_rms(p, ss, red[0], w0);
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int c = first + step * i;
+        if (!real || c >= n8) continue;
+        const uint4 post = p.post ? *reinterpret_cast<const uint4 *>(p.post + 8 * c) : make_uint4(0, 0, 0, 0);
+        const uint32_t w[4] = {y[i].x, y[i].y, y[i].z, y[i].w}, r[4] = {h[i].x, h[i].y, h[i].z, h[i].w};
+        const uint32_t pw[4] = {post.x, post.y, post.z, post.w}, g[4] = {gate[i].x, gate[i].y, gate[i].z, gate[i].w};
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float2 u = unpack2<BF16>(w[k]);
+            if (p.post) {
+                const float2 a = unpack2<BF16>(pw[k]);
+                u = make_float2(u.x * inv * a.x, u.y * inv * a.y);
+            }
+            const float2 b = gated ? unpack2<BF16>(g[k]) : make_float2(whole, whole);
+            const float2 res = unpack2<BF16>(r[k]);
+            o[k] = pack2<BF16>(value(p, u.x, res.x, b.x), value(p, u.y, res.y, b.y));
+            const float2 f = unpack2<BF16>(o[k]);
+            ss = fmaf(f.x, f.x, ss);
+            ss = fmaf(f.y, f.y, ss);
+        }
+        h[i] = make_uint4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<uint4 *>(p.out + t * p.out_stride + 8 * c) = h[i];
+    }
+    if (!p.pre) return;
+    inv = row_rms(p, ss, red[1], w0);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int c = first + step * i;
+        if (!real || c >= n8) continue;
+        const uint4 pre = *reinterpret_cast<const uint4 *>(p.pre + 8 * c);
+        const uint32_t w[4] = {h[i].x, h[i].y, h[i].z, h[i].w}, a[4] = {pre.x, pre.y, pre.z, pre.w};
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = unpack2<BF16>(w[k]), g = unpack2<BF16>(a[k]);
+            o[k] = pack2<BF16>(f.x * inv * g.x, f.y * inv * g.y);
+        }
+        *reinterpret_cast<uint4 *>(p.x + t * p.x_stride + 8 * c) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+// Any row: odd widths and alignments, element by element, a block a row.  h' is read back by the thread that
+// wrote it.
+template <bool BF16>
+__global__ void __launch_bounds__(256) residual_any_kernel(const ResidualParams p)
+{
+    __shared__ float red[2][16];
+    pdl_trigger();
+    pdl_wait();
+    const int64_t t = blockIdx.x;
+    const uint16_t *y = p.y + t * p.y_stride, *h = p.h + t * p.h_stride;
+    uint16_t *out = p.out + t * p.out_stride, *x = p.x + t * p.x_stride;
+    // column k of this thread: its 8-element chunks in turn, or every 256th
+    const bool chunks = p.H % 8 == 0;
+    const int count = chunks ? (p.H / 8 - (int)threadIdx.x + 255) / 256 * 8 : (p.H - (int)threadIdx.x + 255) / 256;
+    auto col = [&](int k) { return chunks ? 8 * ((int)threadIdx.x + 256 * (k >> 3)) + (k & 7) : (int)threadIdx.x + 256 * k; };
+    float inv = 1.f;
+    if (p.post) {
+        float ss = 0.f;
+#pragma unroll 8
+        for (int k = 0; k < count; ++k) {
+            const float v = load1<BF16>(y + col(k));
+            ss = fmaf(v, v, ss);
+        }
+        inv = row_rms(p, ss, red[0], 0);
+    }
+    float ss = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < count; ++k) {
+        const int c = col(k);
+        float u = load1<BF16>(y + c);
+        if (p.post) u = u * inv * load1<BF16>(p.post + c);
+        const float g = p.gate ? load1<BF16>(p.gate + t * p.gate_row + (p.gate_col ? c : 0)) : 1.f;
+        out[c] = store1<BF16>(value(p, u, load1<BF16>(h + c), g));
+        const float v = load1<BF16>(out + c);
+        ss = fmaf(v, v, ss);
+    }
+    if (!p.pre) return;
+    inv = row_rms(p, ss, red[1], 0);
+#pragma unroll 8
+    for (int k = 0; k < count; ++k) {
+        const int c = col(k);
+        x[c] = store1<BF16>(load1<BF16>(out + c) * inv * load1<BF16>(p.pre + c));
+    }
+}
+
+template <bool BF16>
+static cudaError_t launch_residual(ResidualParams p, bool wide, cudaStream_t st)
+{
+    p.rows = 1;
+    p.warps = 8;
+    if (!wide) return launch_k(residual_any_kernel<BF16>, dim3(p.T), dim3(256), 0, st, p);
+    if (p.H < 2048) {
+        p.warps = (p.H + 255) / 256;
+        p.rows = 8 / p.warps;
+    }
+    auto k = p.H <= 2048 ? residual_kernel<1, BF16> : p.H <= 4096 ? residual_kernel<2, BF16>
+             : p.H <= 8192 ? residual_kernel<4, BF16> : residual_kernel<8, BF16>;
+    return launch_k(k, dim3((unsigned)((p.T + p.rows - 1) / p.rows)), dim3(256), 0, st, p);
+}
+
+}  // namespace mc
+
+using namespace mc;
+
+extern "C" int mc_residual_norm(const mc_residual_norm_args *a, void *stream)
+{
+    clear_error();
+    if (!a) return set_error(MC_ERR_INVALID_ARG, "NULL arguments");
+    if (a->dtype != MC_BF16 && a->dtype != MC_FP16) return set_error(MC_ERR_UNSUPPORTED, "dtype %d", a->dtype);
+    if (a->T < 0 || a->H < 1 || !(a->eps >= 0.f) || !isfinite(a->eps)) return set_error(MC_ERR_INVALID_ARG, "T %d, H %d, eps %g", a->T, a->H, a->eps);
+    if (a->H > 65536) return set_error(MC_ERR_UNSUPPORTED, "H %d (at most 65536)", a->H);
+    if (!isfinite(a->scale) || !isfinite(a->residual_scale))
+        return set_error(MC_ERR_INVALID_ARG, "scale %g, residual_scale %g", a->scale, a->residual_scale);
+    if (a->T == 0) return MC_OK;
+    if (!a->y || !a->h || !a->h_out || (a->pre_norm && !a->x)) return set_error(MC_ERR_INVALID_ARG, "NULL pointer argument");
+    const void *ptrs[7] = {a->y, a->h, a->post_norm, a->pre_norm, a->gate, a->h_out, a->pre_norm ? a->x : nullptr};
+    bool wide = a->H % 8 == 0 && a->H <= 16384;
+    for (int i = 0; i < 7; ++i) {
+        if (!aligned(ptrs[i], 2)) return set_error(MC_ERR_INVALID_ARG, "misaligned pointer argument");
+        wide = wide && (aligned(ptrs[i], 16) || (i == 4 && a->gate_col == 0));
+    }
+    const int64_t strides[4] = {a->y_stride, a->h_stride, a->h_out_stride, a->pre_norm ? a->x_stride : a->H};
+    for (int64_t s : strides) {
+        if (s < a->H && a->T > 1) return set_error(MC_ERR_INVALID_ARG, "row stride %lld of %d columns", (long long)s, a->H);
+        wide = wide && (s % 8 == 0 || a->T == 1);
+    }
+    if (a->gate) {
+        if (a->gate_col != 0 && a->gate_col != 1) return set_error(MC_ERR_INVALID_ARG, "gate_col %d (0 or 1)", a->gate_col);
+        if (a->gate_row < 0) return set_error(MC_ERR_INVALID_ARG, "gate_row %lld", (long long)a->gate_row);
+        wide = wide && (a->gate_col == 0 || a->gate_row % 8 == 0 || a->T == 1);
+    }
+    if (a->x && a->pre_norm && a->x == a->h_out) return set_error(MC_ERR_INVALID_ARG, "x must not be h_out");
+    if (a->x && a->pre_norm && a->x == a->h) return set_error(MC_ERR_INVALID_ARG, "x must not be h");
+    ResidualParams p = {};
+    p.T = a->T;
+    p.H = a->H;
+    p.y = (const uint16_t *)a->y;
+    p.h = (const uint16_t *)a->h;
+    p.post = (const uint16_t *)a->post_norm;
+    p.pre = (const uint16_t *)a->pre_norm;
+    p.gate = (const uint16_t *)a->gate;
+    p.y_stride = a->y_stride;
+    p.h_stride = a->h_stride;
+    p.gate_row = a->gate_row;
+    p.gate_col = a->gate_col;
+    p.out_stride = a->h_out_stride;
+    p.x_stride = a->x_stride;
+    p.scale = a->scale;
+    p.residual_scale = a->residual_scale;
+    p.eps = a->eps;
+    p.out = (uint16_t *)a->h_out;
+    p.x = (uint16_t *)a->x;
+    cudaStream_t st = (cudaStream_t)stream;
+    profile_begin(kKResidual, st);
+    const cudaError_t e = a->dtype == MC_BF16 ? launch_residual<true>(p, wide, st) : launch_residual<false>(p, wide, st);
+    profile_end(kKResidual, st);
+    if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "residual launch: %s", cudaGetErrorString(e));
+    return MC_OK;
+}
