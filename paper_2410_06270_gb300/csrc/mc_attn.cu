@@ -153,8 +153,8 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     // 36 / 51 at 20 and 44 / 51 at 32; one sequence of 2000 keys, 16 rows, 12 / 14.
     const int64_t rows = ((int64_t)batch->tokens + batch->seqs - 1) / batch->seqs * p.group;
     const bool bf16 = cache->dtype == MC_BF16;
+    if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, q4, (int)rows, (cudaStream_t)stream);
     if (q4) return launch_rows4(p, cache->head_dim, bf16, (cudaStream_t)stream);
-    if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, (int)rows, (cudaStream_t)stream);
     return launch_prefill(p, cache->head_dim, bf16, (cudaStream_t)stream);
 }
 

@@ -34,9 +34,9 @@ constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 // Keys of a unit that one warp takes, in tiles of 16: heads of 64 take two tiles in one step,
 // whose chains of products and exponentials overlap (a step of 16 keys takes about as long
 // whatever the head, and 16 keys of 64 are half the bytes).
-constexpr int dec_tiles(int D) { return D == 64 ? 2 : 1; }
-constexpr int dec_unit(int D) { return 16 * dec_tiles(D) * kDecWarps; }
-constexpr int kDecCtasPerSm = 2;
+constexpr int dec_tiles(int D, bool q4) { return q4 || D == 64 ? 2 : 1; }
+constexpr int dec_unit(int D, bool q4) { return 16 * dec_tiles(D, q4) * kDecWarps; }
+constexpr int dec_ctas(bool q4, int nt) { return q4 && nt == 1 ? 3 : 2; }  // an SM
 constexpr int kDecMaxTiles = 4;                // n-tiles of the largest slice
 constexpr int kDecItemCost = 2;  // what an item costs on top of its units, in units (up to 128 sequences; 64 of up
                                 // to 500 keys 23.8 us at 0, 18.4 at 1, 18.1 at 2, 18.4 at 3)
@@ -72,6 +72,36 @@ __device__ __forceinline__ uint32_t transposed8x8(uint32_t a)
     return r;
 }
 
+// Words of codes from shared memory: a lane's of a key, D / 32 of them; of a value, one for each group; and the
+// groups' 16-bit words of row i of those at `addr`.
+template <int D>
+__device__ __forceinline__ void lds_row(uint32_t addr, uint32_t (&w)[D / 32])
+{
+    if constexpr (D == 128)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+    else
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr) : "memory");
+}
+template <int D>
+__device__ __forceinline__ void lds_pair(uint32_t addr, uint32_t (&w)[D / 64])
+{
+    if constexpr (D == 128) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr) : "memory");
+    else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(addr) : "memory");
+}
+template <int D>
+__device__ __forceinline__ uint32_t lds_word(uint32_t addr, int i)
+{
+    uint32_t w;
+    if constexpr (D == 128) {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(addr + 4 * i) : "memory");
+    } else {
+        uint16_t h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(addr + 2 * i) : "memory");
+        w = h;
+    }
+    return w;
+}
+
 // 16 bytes to shared memory, or 16 zeros where !real (the address is then not read).  The
 // cache is read once a step and leaves L2 first: lengths, tables and what other kernels keep
 // there stay.
@@ -90,7 +120,7 @@ struct Keys {
     int start, len, base, units;
 };
 
-template <int D>
+template <int U>
 __device__ __forceinline__ Keys keys_of(const AttnParams &p, int b, int32_t *status)
 {
     Keys k;
@@ -99,7 +129,7 @@ __device__ __forceinline__ Keys keys_of(const AttnParams &p, int b, int32_t *sta
     const int p0 = k.len - k.n;
     k.start = p.window ? max(0, p0 - p.window + 1) : 0;
     k.base = k.start & ~15;
-    k.units = k.n > 0 ? (k.len - k.base + dec_unit(D) - 1) / dec_unit(D) : 0;
+    k.units = k.n > 0 ? (k.len - k.base + U - 1) / U : 0;
     return k;
 }
 
@@ -121,7 +151,7 @@ struct Place {
     Keys k;
 };
 
-template <int D, int NT>
+template <int U, int NT>
 __device__ __forceinline__ void step(const AttnParams &p, Place &at)
 {
     if (++at.u < at.k.units) return;
@@ -131,7 +161,7 @@ __device__ __forceinline__ void step(const AttnParams &p, Place &at)
     if (++at.h < p.c.kv_heads) return;
     at.h = 0;
     while (++at.b < p.b.seqs) {
-        at.k = keys_of<D>(p, at.b, nullptr);
+        at.k = keys_of<U>(p, at.b, nullptr);
         if (at.k.units) {
             at.slices = slices_of<NT>(p, at.k);
             return;
@@ -153,14 +183,14 @@ struct Row {
 
 // Token tok of sequence b's, head `head`: a row that came out infinite or NaN, redone if a key of the
 // sequence's units that it hides is.
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 __device__ __noinline__ void redo_row(const AttnParams &p, int b, int tok, int head, int lane)
 {
-    const Keys k = keys_of<D>(p, b, nullptr);
+    const Keys k = keys_of<dec_unit(D, Q4)>(p, b, nullptr);
     const int h = p.by_group.div(head), pos = k.len - k.n + tok, prefix = p.prefix ? __ldg(p.prefix + b) : 0;
     const int lo = p.window ? max(0, pos - p.window + 1) : 0, hi = pos < 0 ? 0 : max(pos + 1, prefix);
-    if (odd_keys<D, BF16, false>(p, b, h, k.start, min(lo, k.len), 0, 1, lane) || odd_keys<D, BF16, false>(p, b, h, max(hi, k.start), k.len, 0, 1, lane))
-        exact_row<D, BF16, false>(p, b, pos, k.len, prefix, k.first + tok, head, lane);
+    if (odd_keys<D, BF16, Q4>(p, b, h, k.start, min(lo, k.len), 0, 1, lane) || odd_keys<D, BF16, Q4>(p, b, h, max(hi, k.start), k.len, 0, 1, lane))
+        exact_row<D, BF16, Q4>(p, b, pos, k.len, prefix, k.first + tok, head, lane);
 }
 
 __host__ __device__ constexpr size_t dec_part_floats(int D, int nt) { return (size_t)8 * nt * (D + 2); }
@@ -181,11 +211,12 @@ __device__ __forceinline__ bool finite4(const float4 &a)
     return z == z;
 }
 
-template <int D, int NT>
+template <int D, int NT, bool Q4>
 struct DecShape {
-    static constexpr int kRow = D * 2;                       // bytes of a key
-    static constexpr int kTiles = dec_tiles(D), kKeys = 16 * kTiles;
-    static constexpr int kSlot = 2 * kKeys * kRow;           // a warp's keys and values of a unit
+    static constexpr int kRow = Q4 ? kv4_code_bytes(D) : D * 2;  // bytes of a key (Q4: of its codes)
+    static constexpr int kTiles = dec_tiles(D, Q4), kKeys = 16 * kTiles;
+    static constexpr int kWords = Q4 ? 2 * kKeys * kRow : 0;     // where the groups' words lie in a slot
+    static constexpr int kSlot = 2 * kKeys * (kRow + (Q4 ? kv4_word_bytes(D) : 0));  // a warp's keys and values of a unit
     static constexpr int kStages = 3;
     static constexpr int kRing = kSlot * kStages * kDecWarps;
     static constexpr int kPitch = D + 4;                     // floats of a row in the join: O, m, l
@@ -199,17 +230,22 @@ struct DecShape {
 // NT: n-tiles of 8 rows of a slice, 1 to 4.  The products are formed transposed, S^T = K Q^T and
 // O^T += V^T P^T: the 16 keys of a warp fill the rows of the m16n8k16 instruction and the
 // slice's rows its 8 columns, half the instructions and accumulators of the other way.
-template <int D, bool BF16, int NT>
-__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(const AttnParams p, FastDiv by_grid, OpenItem *open,
+template <int D, bool BF16, int NT, bool Q4>
+__global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(const AttnParams p, FastDiv by_grid, OpenItem *open,
                                                                              float *part)
 {
-    using Sh = DecShape<D, NT>;
+    using Sh = DecShape<D, NT, Q4>;
+    constexpr int kUnit = dec_unit(D, Q4);
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     float *jo = reinterpret_cast<float *>(smem + Sh::kRing);
     uint2 *qs = reinterpret_cast<uint2 *>(smem + Sh::kRing);  // [n-tile][k-step][lane]
     Row *rows = reinterpret_cast<Row *>(smem + Sh::kRing + Sh::kRows0);
     int *marks = reinterpret_cast<int *>(smem + Sh::kRing);
+    using P4 = Kv4Pairs<BF16>;
+    // Key of a tile that the products' row g stands for (row g + 8: 8 more).  Q4: rows 2 t and 2 t + 1 are keys t and
+    // t + 4, so that the lanes of a load of values have neighbouring keys, in different banks.
+    const int own_key = Q4 ? (g >> 1) + 4 * (g & 1) : g;
     const uint32_t ring = smem_u32(smem) + warp * Sh::kSlot * Sh::kStages;
     pdl_trigger();
     pdl_wait();
@@ -230,7 +266,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             if (i >= each) break;
             const int b = each * lane + i;
             if (b >= p.b.seqs) break;
-            const Keys k = keys_of<D>(p, b, p.status);
+            const Keys k = keys_of<kUnit>(p, b, p.status);
             const int64_t n = units_of<NT>(p, k);
             small &= n < 1 << 22;
             units[i] = (int)n;
@@ -265,7 +301,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                     ++x.b;
                 }
             }
-            x.k = keys_of<D>(p, x.b, nullptr);
+            x.k = keys_of<kUnit>(p, x.b, nullptr);
             x.slices = slices_of<NT>(p, x.k);
             const int per = x.k.units + kDecItemCost, item = (int)((unsigned)r / (unsigned)per);
             x.u = max(0, r - item * per - kDecItemCost);
@@ -284,7 +320,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         }
     } else {
         for (int b0 = 0; b0 < p.b.seqs; b0 += 32) {
-            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of<D>(p, b0 + lane, p.status)) : 0;
+            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of<kUnit>(p, b0 + lane, p.status)) : 0;
             int64_t n = own;
 #pragma unroll
             for (int d = 16; d >= 1; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
@@ -296,7 +332,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         u1 = any ? muldiv64(total, blockIdx.x + 1, ctas) : 0;
         int64_t skipped = 0;
         for (int b0 = 0; any && at.b < 0 && b0 < p.b.seqs; b0 += 32) {
-            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of<D>(p, b0 + lane, nullptr)) : 0;
+            own = b0 + lane < p.b.seqs ? units_of<NT>(p, keys_of<kUnit>(p, b0 + lane, nullptr)) : 0;
             int64_t sum = own;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -311,7 +347,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             }
             const int l = __ffs(hit) - 1;
             at.b = b0 + l;
-            at.k = keys_of<D>(p, at.b, nullptr);
+            at.k = keys_of<kUnit>(p, at.b, nullptr);
             at.slices = slices_of<NT>(p, at.k);
             const int64_t r = u0 - __shfl_sync(0xffffffffu, sum - own, l), item = div64(r, at.k.units);
             at.u = (int)(r - item * at.k.units);
@@ -324,12 +360,13 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
     constexpr int kChunks = D / 8, kPer = 32 / kChunks;  // 16-byte chunks of a row; rows per warp copy
     const int lc = lane % kChunks, lr = lane / kChunks;
     const uint64_t policy = policy_evict_first();
+    const uint8_t *k4 = reinterpret_cast<const uint8_t *>(p.c.k), *v4 = reinterpret_cast<const uint8_t *>(p.c.v);
     Place ld = at;
     int ld_left = left, page[Sh::kTiles];
     auto fetch_page = [&]() {
 #pragma unroll
         for (int kt = 0; kt < Sh::kTiles; ++kt) {
-            const int j = ld.k.base + ld.u * dec_unit(D) + warp * Sh::kKeys + 16 * kt;
+            const int j = ld.k.base + ld.u * kUnit + warp * Sh::kKeys + 16 * kt;
             page[kt] = ld_left > 0 && j < ld.k.len ? seq_page(p.b, p.c, ld.b, p.c.page.div(j), p.status) : -1;
         }
     };
@@ -337,9 +374,32 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         if (ld_left > 0) {
 #pragma unroll
             for (int kt = 0; kt < Sh::kTiles; ++kt) {
-                const int j = ld.k.base + ld.u * dec_unit(D) + warp * Sh::kKeys + 16 * kt;
+                const int j = ld.k.base + ld.u * kUnit + warp * Sh::kKeys + 16 * kt;
                 int row;
                 p.c.page.div(j, row);
+                if constexpr (Q4) {
+                    // codes of 16 keys, contiguous; see the fragments below for where a key's 16-byte chunks go
+                    constexpr int kRowChunks = Sh::kRow / 16;
+                    const bool real = page[kt] >= 0;
+                    const int64_t block = kv4_offset<D>(p.c, max(page[kt], 0), ld.h) + row * Sh::kRow;
+                    const uint32_t dst = ring + slot * Sh::kSlot + 16 * kt * Sh::kRow;
+#pragma unroll
+                    for (int i = 0; i < kRowChunks / 2; ++i) {
+                        const int c = lane + 32 * i, key = c / kRowChunks, ch = c % kRowChunks;
+                        const int place = (key & 8) | (key & 3) << 1 | (key >> 2 & 1);
+                        copy16(dst + place * Sh::kRow + 16 * ch, k4 + block + 16 * c, real, policy);
+                        copy16(dst + Sh::kKeys * Sh::kRow + key * Sh::kRow + 16 * (ch ^ (kRowChunks == 4 ? key & 2 : 0)), v4 + block + 16 * c, real, policy);
+                    }
+                    // the groups' words (zeros, that is scales of 0, where there is no page)
+                    constexpr int kWordChunks = kv4_word_bytes(D);  // of 16 keys
+                    if (lane < 2 * kWordChunks) {
+                        const int side = lane / kWordChunks, c = lane % kWordChunks;
+                        const int64_t words = block + (p.c.page_size - row) * Sh::kRow + row * kv4_word_bytes(D);
+                        copy16(ring + slot * Sh::kSlot + Sh::kWords + (side * Sh::kKeys + 16 * kt) * kv4_word_bytes(D) + 16 * c,
+                               (side ? v4 : k4) + words + 16 * c, real, policy);
+                    }
+                    continue;
+                }
                 const int64_t off = (page[kt] < 0 ? 0 : page[kt] * p.c.page_stride) +
                                     ((int64_t)ld.h * p.c.page_size + row + lr) * D + lc * 8;
                 const uint32_t dst = ring + slot * Sh::kSlot + 16 * kt * Sh::kRow;
@@ -353,7 +413,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                 }
             }
             --ld_left;
-            step<D, NT>(p, ld);
+            step<kUnit, NT>(p, ld);
             fetch_page();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -386,22 +446,25 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             return p.q + (keys.first + tok) * p.q_stride + (h0 + hg) * D;
         };
         auto pair = [&](const uint16_t *q, int d, int r) { return r < nrows ? *reinterpret_cast<const uint32_t *>(q + d) : 0u; };
+        // Where lane t's pairs of a k-step begin.  Q4: step 4 g + 2 w + i of word 2 t + w of group g, its elements 4 i to
+        // 4 i + 3 (the order of a product's terms is free, so each lane takes whole words).
+        auto column = [](int ks, int t) { return Q4 ? 64 * (ks >> 2) + 8 * (2 * t + (ks >> 1 & 1)) + 4 * (ks & 1) : 16 * ks + 2 * t; };
         uint32_t qf[Sh::kQShared ? 1 : NT][D / 16][2];
         if (Sh::kQShared) {
             for (int i = tid; i < NT * (D / 16) * 32; i += kDecThreads) {
                 const int l = i & 31, ks = (i >> 5) % (D / 16), nt = (i >> 5) / (D / 16);
-                const int r = 8 * nt + (l >> 2), d = 16 * ks + 2 * (l & 3);
+                const int r = 8 * nt + (l >> 2), d = column(ks, l & 3);
                 const uint16_t *q = query(r);
-                qs[i] = make_uint2(pair(q, d, r), pair(q, d + 8, r));
+                qs[i] = make_uint2(pair(q, d, r), pair(q, d + (Q4 ? 2 : 8), r));
             }
         } else {
 #pragma unroll
             for (int nt = 0; nt < (Sh::kQShared ? 1 : NT); ++nt) {
-                const uint16_t *q = query(8 * nt + g) + 2 * t4;
+                const uint16_t *q = query(8 * nt + g);
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    qf[nt][ks][0] = pair(q, 16 * ks, 8 * nt + g);
-                    qf[nt][ks][1] = pair(q, 16 * ks + 8, 8 * nt + g);
+                    qf[nt][ks][0] = pair(q, column(ks, t4), 8 * nt + g);
+                    qf[nt][ks][1] = pair(q, column(ks, t4) + (Q4 ? 2 : 8), 8 * nt + g);
                 }
             }
         }
@@ -424,11 +487,12 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             __syncwarp();  // every lane is done with the slot of the round before, which is filled next
             issue(slot == 0 ? Sh::kStages - 1 : slot - 1);
             const uint32_t kk = ring + slot * Sh::kSlot, vv = kk + Sh::kKeys * Sh::kRow;
-            const int j0 = keys.base + u * dec_unit(D) + warp * Sh::kKeys;
+            const int j0 = keys.base + u * kUnit + warp * Sh::kKeys;
             if (j0 < keys.len) {
                 // S^T: rows are keys g, g + 8; columns the slice's rows 2 t4, 2 t4 + 1; few
                 // tiles take two accumulators each, so that the chain is half as long
-                constexpr int kChains = NT * Sh::kTiles > 2 ? 1 : 2;
+                // (Q4: an accumulator for each group, whose scale comes after)
+                constexpr int kChains = Q4 ? D / kKv4Group : NT * Sh::kTiles > 2 ? 1 : 2;
                 float s[Sh::kTiles][NT][kChains][4];
 #pragma unroll
                 for (int kt = 0; kt < Sh::kTiles; ++kt)
@@ -437,19 +501,57 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 #pragma unroll
                         for (int c = 0; c < 4; ++c) s[kt][nt][0][c] = s[kt][nt][kChains - 1][c] = 0.f;
                 const int kr = lane & 15;
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    uint32_t a[Sh::kTiles][4];
+                auto q_of = [&](int nt, int ks) {
+                    return Sh::kQShared ? qs[(nt * (D / 16) + ks) * 32 + lane]
+                                        : make_uint2(qf[Sh::kQShared ? 0 : nt][ks][0], qf[Sh::kQShared ? 0 : nt][ks][1]);
+                };
+                uint32_t k_words[Sh::kTiles][2], v_words[Sh::kTiles][2];  // Q4: of the lane's keys, rows g and g + 8
+                if constexpr (Q4) {
+                    const bool edge = j0 < keys.start || j0 + Sh::kKeys > keys.len;
 #pragma unroll
                     for (int kt = 0; kt < Sh::kTiles; ++kt)
-                        ldsm4(a[kt], kk + (16 * kt + kr) * Sh::kRow + (((2 * ks + (lane >> 4)) ^ (kr & 7)) << 4));
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        uint2 q;
-                        if (Sh::kQShared) q = qs[(nt * (D / 16) + ks) * 32 + lane];
-                        else q = make_uint2(qf[Sh::kQShared ? 0 : nt][ks][0], qf[Sh::kQShared ? 0 : nt][ks][1]);
+                        for (int i = 0; i < 2; ++i) {
+                            const int key = 16 * kt + 8 * i + own_key;
+                            k_words[kt][i] = lds_word<D>(kk + Sh::kWords, key);
+                            v_words[kt][i] = lds_word<D>(kk + Sh::kWords, Sh::kKeys + key);
+                            // a row that no token was written to has any scale
+                            if (edge && (j0 + key < keys.start || j0 + key >= keys.len)) k_words[kt][i] = v_words[kt][i] = 0;
+                        }
 #pragma unroll
-                        for (int kt = 0; kt < Sh::kTiles; ++kt) mma16<BF16>(s[kt][nt][ks % kChains], a[kt], q.x, q.y);
+                    for (int kt = 0; kt < Sh::kTiles; ++kt) {
+                        uint32_t w[2][D / 32];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) lds_row<D>(kk + (16 * kt + 8 * i + g) * Sh::kRow + t4 * (D / 8), w[i]);
+#pragma unroll
+                        for (int grp = 0; grp < kChains; ++grp) {
+                            const uint32_t z0 = P4::zeros(k_words[kt][0] >> (16 * grp)), z1 = P4::zeros(k_words[kt][1] >> (16 * grp));
+#pragma unroll
+                            for (int ks = 0; ks < 4; ++ks) {
+                                const int x = (ks >> 1) * kChains + grp, j = 2 * (ks & 1);
+                                const uint32_t a[4] = {P4::sub(P4::magic(w[0][x], j), z0), P4::sub(P4::magic(w[1][x], j), z1),
+                                                       P4::sub(P4::magic(w[0][x], j + 1), z0), P4::sub(P4::magic(w[1][x], j + 1), z1)};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    const uint2 q = q_of(nt, 4 * grp + ks);
+                                    mma16<BF16>(s[kt][nt][grp], a, q.x, q.y);
+                                }
+                            }
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        uint32_t a[Sh::kTiles][4];
+#pragma unroll
+                        for (int kt = 0; kt < Sh::kTiles; ++kt)
+                            ldsm4(a[kt], kk + (16 * kt + kr) * Sh::kRow + (((2 * ks + (lane >> 4)) ^ (kr & 7)) << 4));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint2 q = q_of(nt, ks);
+#pragma unroll
+                            for (int kt = 0; kt < Sh::kTiles; ++kt) mma16<BF16>(s[kt][nt][ks % kChains], a[kt], q.x, q.y);
+                        }
                     }
                 }
                 const bool masked = j0 < all_lo || j0 + Sh::kKeys > all_hi;
@@ -460,8 +562,16 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 #pragma unroll
                     for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            x[kt][nt][c] = (kChains == 2 ? s[kt][nt][0][c] + s[kt][nt][kChains - 1][c] : s[kt][nt][0][c]) * p.scale;
+                        for (int c = 0; c < 4; ++c) {
+                            float sum = s[kt][nt][0][c];
+                            if constexpr (Q4) {
+                                sum *= kv4_scale(k_words[kt][c >> 1]);
+                                if (kChains == 2) sum = fmaf(s[kt][nt][kChains - 1][c], kv4_scale(k_words[kt][c >> 1] >> 16), sum);
+                            } else if (kChains == 2) {
+                                sum += s[kt][nt][kChains - 1][c];
+                            }
+                            x[kt][nt][c] = sum * p.scale;
+                        }
                     if (p.cap > 0.f) {
 #pragma unroll
                         for (int kt = 0; kt < Sh::kTiles; ++kt)
@@ -473,7 +583,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const Row w = rows[8 * nt + 2 * t4 + c];
-                            const float first = (float)(j0 + g - w.pos);
+                            const float first = (float)(j0 + own_key - w.pos);
 #pragma unroll
                             for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
@@ -489,7 +599,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                             for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
                                 for (int e = c; e < 4; e += 2) {
-                                    const int j = j0 + 16 * kt + g + (e >> 1) * 8;
+                                    const int j = j0 + 16 * kt + own_key + (e >> 1) * 8;
                                     if (j < w.lo || j >= w.hi) x[kt][nt][e] = -INFINITY;
                                 }
                         }
@@ -520,7 +630,10 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                             }
                         }
                 }
-                uint32_t pf[Sh::kTiles][NT][2];
+                // (Q4 in bf16: a weight for each group, its scale in it; in fp16 a product with the scale
+                // could leave the type's range, and the values take it)
+                constexpr int kWeights = Q4 && BF16 ? D / kKv4Group : 1;
+                uint32_t pf[Sh::kTiles][NT][kWeights][2];
 #pragma unroll
                 for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
@@ -533,19 +646,65 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                             l[nt][c & 1] += pr[c];
                         }
                         // rounded to the cache's type for the second product; l keeps fp32
-                        pf[kt][nt][0] = transposed8x8(pack2<BF16>(pr[0], pr[1]));
-                        pf[kt][nt][1] = transposed8x8(pack2<BF16>(pr[2], pr[3]));
+#pragma unroll
+                        for (int w = 0; w < kWeights; ++w)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const float f = Q4 && BF16 ? kv4_scale(v_words[kt][i] >> (16 * w)) : 1.f;
+                                pf[kt][nt][w][i] = transposed8x8(pack2<BF16>(Q4 && BF16 ? pr[2 * i] * f : pr[2 * i], Q4 && BF16 ? pr[2 * i + 1] * f : pr[2 * i + 1]));
+                            }
                     }
-                const int vr = (lane & 7) + ((lane >> 4) << 3);
+                if constexpr (Q4) {
 #pragma unroll
-                for (int kt = 0; kt < Sh::kTiles; ++kt)
+                    for (int kt = 0; kt < Sh::kTiles; ++kt) {
+                        // the lane's keys are t, t + 4, t + 8, t + 12 of the tile (the products' rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9), its
+                        // dimensions word g of each group, which two keys' words give in pairs
+                        uint32_t w[4][D / 64], words[4];
 #pragma unroll
-                    for (int mt = 0; mt < D / 16; ++mt) {
-                        uint32_t a[4];
-                        ldsm4t(a, vv + (16 * kt + vr) * Sh::kRow + (((2 * mt + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = 16 * kt + t4 + 4 * i;
+                            lds_pair<D>(vv + key * Sh::kRow + (D == 128 ? ((g >> 1) ^ (t4 & 2)) * 16 + (g & 1) * 8 : g * 4), w[i]);
+                            words[i] = lds_word<D>(kk + Sh::kWords, Sh::kKeys + key);
+                            if (!BF16 && (j0 + key < keys.start || j0 + key >= keys.len)) words[i] = 0;
+                        }
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16<BF16>(o[nt][mt], a, pf[kt][nt][0], pf[kt][nt][1]);
+                        for (int grp = 0; grp < D / kKv4Group; ++grp) {
+                            const uint32_t half = grp ? 0x7632 : 0x5410;
+                            const uint32_t w01 = __byte_perm(words[0], words[1], half), w23 = __byte_perm(words[2], words[3], half);
+                            const uint32_t z01 = lop_and_or(w01, 0x000f000fu, P4::kMagic), z23 = lop_and_or(w23, 0x000f000fu, P4::kMagic);
+                            uint32_t s01 = 0, s23 = 0;
+                            if (!BF16) {
+                                s01 = pack2<BF16>(kv4_scale(w01), kv4_scale(w01 >> 16));
+                                s23 = pack2<BF16>(kv4_scale(w23), kv4_scale(w23 >> 16));
+                            }
+                            const uint32_t lo01 = __byte_perm(w[0][grp], w[1][grp], 0x5410), hi01 = __byte_perm(w[0][grp], w[1][grp], 0x7632);
+                            const uint32_t lo23 = __byte_perm(w[2][grp], w[3][grp], 0x5410), hi23 = __byte_perm(w[2][grp], w[3][grp], 0x7632);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t a[4] = {P4::sub(P4::magic(lo01, j), z01), P4::sub(P4::magic(hi01, j), z01),
+                                                 P4::sub(P4::magic(lo23, j), z23), P4::sub(P4::magic(hi23, j), z23)};
+                                if (!BF16) {
+                                    a[0] = P4::mul(a[0], s01), a[1] = P4::mul(a[1], s01);
+                                    a[2] = P4::mul(a[2], s23), a[3] = P4::mul(a[3], s23);
+                                }
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+                                    mma16<BF16>(o[nt][4 * grp + j], a, pf[kt][nt][kWeights == 2 ? grp : 0][0], pf[kt][nt][kWeights == 2 ? grp : 0][1]);
+                            }
+                        }
                     }
+                } else {
+                    const int vr = (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                    for (int kt = 0; kt < Sh::kTiles; ++kt)
+#pragma unroll
+                        for (int mt = 0; mt < D / 16; ++mt) {
+                            uint32_t a[4];
+                            ldsm4t(a, vv + (16 * kt + vr) * Sh::kRow + (((2 * mt + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma16<BF16>(o[nt][mt], a, pf[kt][nt][0][0], pf[kt][nt][0][1]);
+                        }
+                }
             }
             if (++slot == Sh::kStages) slot = 0;
         }
@@ -569,7 +728,8 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
             for (int mt = 0; mt < D / 16; ++mt)
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    jo[(warp * 8 + 2 * t4 + (c & 1)) * Sh::kPitch + 16 * mt + g + (c >> 1) * 8] = o[nt][mt][c];
+                    jo[(warp * 8 + 2 * t4 + (c & 1)) * Sh::kPitch + (Q4 ? 64 * (mt / 4) + 8 * g + 2 * (mt % 4) + (c >> 1) : 16 * mt + g + (c >> 1) * 8)] =
+                        o[nt][mt][c];
             __syncthreads();
             for (int i = tid; i < 8 * (D / 4); i += kDecThreads) {
                 const int h = i / (D / 4), d = (i % (D / 4)) * 4, r = 8 * nt + h;
@@ -611,7 +771,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
                 if (!marks[r]) continue;
                 int hg;
                 const int tok = p.by_group.div(r0 + r, hg);
-                redo_row<D, BF16>(p, at.b, tok, h0 + hg, lane);
+                redo_row<D, BF16, Q4>(p, at.b, tok, h0 + hg, lane);
             }
             __syncthreads();
         }
@@ -625,13 +785,13 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
         }
         left -= n;
         at.u += n - 1;
-        step<D, NT>(p, at);
+        step<kUnit, NT>(p, at);
     }
     if (!open_tail && tid == 0) open[blockIdx.x].pieces = 0;
 
     // sequences without keys
     for (int b = blockIdx.x; b < p.b.seqs; b += gridDim.x) {
-        const Keys k = keys_of<D>(p, b, nullptr);
+        const Keys k = keys_of<kUnit>(p, b, nullptr);
         if (k.len > 0) continue;
         for (int t = k.first; t < k.first + k.n; ++t) {
             for (int i = tid; i < p.q_heads * D / 8; i += kDecThreads)
@@ -644,7 +804,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_kernel(cons
 
 // One CTA per (CTA of the pass before, row of a slice): adds the pieces of that CTA's open
 // item in their order.
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 __global__ void __launch_bounds__(128, 12) join_kernel(const AttnParams p, const OpenItem *open, const float *part, int nt)
 {
     constexpr int kCols = D / 4, kGroups = 128 / kCols;
@@ -696,23 +856,26 @@ __global__ void __launch_bounds__(128, 12) join_kernel(const AttnParams p, const
         store_row<BF16>(p, first + tok, it.h * p.group + hg, D, 4 * col, acc, top, sum);
         odd = n > 1 && !finite4(acc);
     }
-    if (__syncthreads_or(odd) && tid < 32) redo_row<D, BF16>(p, it.b, tok, it.h * p.group + hg, tid);
+    if (__syncthreads_or(odd) && tid < 32) redo_row<D, BF16, Q4>(p, it.b, tok, it.h * p.group + hg, tid);
 }
 
-constexpr int kDecMaxCtas = kDecCtasPerSm * kAttnMaxSms;
+constexpr int kDecMaxCtas = 4 * kAttnMaxSms;
 
 size_t decode_part_bytes(int head_dim)
 {
-    return kDecMaxCtas * (sizeof(OpenItem) + 2 * 4 * dec_part_floats(head_dim, kDecMaxTiles));
+    return kDecMaxCtas * sizeof(OpenItem) + 2 * kAttnMaxSms * 2 * 4 * dec_part_floats(head_dim, kDecMaxTiles);
 }
 
-template <int D, bool BF16, int NT>
-static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t st)
+template <int D, bool BF16, int NT, bool Q4>
+static cudaError_t launch_decode_t(const AttnParams &p, int sms, cudaStream_t st)
 {
-    using Sh = DecShape<D, NT>;
+    using Sh = DecShape<D, NT, Q4>;
+    // (more blocks have smaller parts: the workspace holds those of two an SM with the largest slices)
+    static_assert(dec_ctas(Q4, NT) <= 4 && dec_ctas(Q4, NT) * NT <= 2 * kDecMaxTiles, "parts");
+    const int ctas = dec_ctas(Q4, NT) * sms;
     OpenItem *open = reinterpret_cast<OpenItem *>(p.part);
     float *part = reinterpret_cast<float *>(p.part + kDecMaxCtas * sizeof(OpenItem));
-    auto k = decode_kernel<D, BF16, NT>;
+    auto k = decode_kernel<D, BF16, NT, Q4>;
     static SmemAttr attr;
     cudaError_t e = attr.set((const void *)k, Sh::kSmem);
     if (e != cudaSuccess) return e;
@@ -724,32 +887,38 @@ static cudaError_t launch_decode_t(const AttnParams &p, int ctas, cudaStream_t s
     // not time: an atomic and two dependent reads by one CTA against a CTA per row: 777 keys 7.8 us
     // with the second launch, 9.9 without, 16 ragged sequences 26.9 and 29.5, 8000 keys of one key
     // head 12.5 and 32.1.)
-    if (e != cudaSuccess || (int64_t)p.b.table_width * p.c.page_size <= dec_unit(D)) return e;
+    if (e != cudaSuccess || (int64_t)p.b.table_width * p.c.page_size <= dec_unit(D, Q4)) return e;
     profile_begin(kKAttnJoin, st);
-    e = launch_k(join_kernel<D, BF16>, dim3(ctas, 8 * NT), dim3(128), 0, st, p, (const OpenItem *)open, (const float *)part, NT);
+    e = launch_k(join_kernel<D, BF16, Q4>, dim3(ctas, 8 * NT), dim3(128), 0, st, p, (const OpenItem *)open, (const float *)part, NT);
     profile_end(kKAttnJoin, st);
     return e;
 }
 
-template <int D, bool BF16>
-static cudaError_t launch_decode_n(const AttnParams &p, int rows, int ctas, cudaStream_t st)
+template <int D, bool BF16, bool Q4>
+static cudaError_t launch_decode_n(const AttnParams &p, int rows, int sms, cudaStream_t st)
 {
-    return rows <= 8    ? launch_decode_t<D, BF16, 1>(p, ctas, st)
-           : rows <= 16 ? launch_decode_t<D, BF16, 2>(p, ctas, st)
-           : rows <= 24 ? launch_decode_t<D, BF16, 3>(p, ctas, st)
-                        : launch_decode_t<D, BF16, kDecMaxTiles>(p, ctas, st);
+    return rows <= 8    ? launch_decode_t<D, BF16, 1, Q4>(p, sms, st)
+           : rows <= 16 ? launch_decode_t<D, BF16, 2, Q4>(p, sms, st)
+           : rows <= 24 ? launch_decode_t<D, BF16, 3, Q4>(p, sms, st)
+                        : launch_decode_t<D, BF16, kDecMaxTiles, Q4>(p, sms, st);
+}
+
+template <bool Q4>
+static cudaError_t launch_decode_d(const AttnParams &p, int head_dim, bool bf16, int rows, int sms, cudaStream_t st)
+{
+    return head_dim == 64 ? (bf16 ? launch_decode_n<64, true, Q4>(p, rows, sms, st) : launch_decode_n<64, false, Q4>(p, rows, sms, st))
+                          : (bf16 ? launch_decode_n<128, true, Q4>(p, rows, sms, st) : launch_decode_n<128, false, Q4>(p, rows, sms, st));
 }
 
 // rows: what most sequences have, (token, head of the group) each; the smallest slice that
 // holds them is taken, and sequences with more take several.
-int launch_decode(const AttnParams &p, int head_dim, bool bf16, int rows, cudaStream_t st)
+int launch_decode(const AttnParams &p, int head_dim, bool bf16, bool q4, int rows, cudaStream_t st)
 {
     int nsm = 0;
     cudaError_t e = sm_count(&nsm);
     if (e == cudaSuccess) {
-        const int ctas = kDecCtasPerSm * (nsm < kAttnMaxSms ? nsm : kAttnMaxSms);
-        e = head_dim == 64 ? (bf16 ? launch_decode_n<64, true>(p, rows, ctas, st) : launch_decode_n<64, false>(p, rows, ctas, st))
-                           : (bf16 ? launch_decode_n<128, true>(p, rows, ctas, st) : launch_decode_n<128, false>(p, rows, ctas, st));
+        const int sms = nsm < kAttnMaxSms ? nsm : kAttnMaxSms;
+        e = q4 ? launch_decode_d<true>(p, head_dim, bf16, rows, sms, st) : launch_decode_d<false>(p, head_dim, bf16, rows, sms, st);
     }
     if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "decode launch: %s", cudaGetErrorString(e));
     return MC_OK;

@@ -13,9 +13,14 @@ __host__ __device__ constexpr int kv4_row_bytes(int D) { return kv4_code_bytes(D
 // Address of (page, head): a block of codes [page_size][D / 2] and, behind them, words [page_size][D / 64].
 // (KvView's k and v are bytes here, page_stride counts them.)
 template <int D>
+__device__ __forceinline__ int64_t kv4_offset(const KvView &c, int page, int h)
+{
+    return page * c.page_stride + (int64_t)h * (c.page_size * kv4_row_bytes(D));
+}
+template <int D>
 __device__ __forceinline__ const uint8_t *kv4_block(const KvView &c, const uint16_t *side, int page, int h)
 {
-    return reinterpret_cast<const uint8_t *>(side) + page * c.page_stride + (int64_t)h * c.page_size * kv4_row_bytes(D);
+    return reinterpret_cast<const uint8_t *>(side) + kv4_offset<D>(c, page, h);
 }
 
 __device__ __forceinline__ float kv4_scale(uint32_t word) { return __uint_as_float((word & 0xfff0u) << 16); }

@@ -250,6 +250,36 @@ def test_groups_far_apart_in_scale(mc):
         ref.assert_attention(pre, pl, want, dtype, 300, 600.0)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("below", [9.0, 14.0, 17.0])
+@pytest.mark.parametrize("new,group", [(1, 1)])
+def test_small_weights_keep_their_sum(mc, dtype, below, new, group):
+    """8191 equal keys far below one: each weighs little, together they weigh what they should."""
+    seqs, kv, length, dim, page = 40, 8, 8192, 64, 128
+    T = ref.DT[dtype]
+    pages = length // page
+    k, v = (torch.zeros(pages, kv, page, dim, dtype=T) for _ in range(2))
+    v[:] = (torch.arange(dim) % 16).to(T)  # on the grid of step 1
+    k[0, :, 0, 0], v[0, :, 0] = below, 0.0
+    B = ref.Batch.__new__(ref.Batch)
+    B.__dict__.update(k=k, v=v, kv=kv, page=page, dim=dim, dtype=dtype, lens=[length] * seqs, new=[new] * seqs, table=torch.arange(pages, dtype=torch.int32).repeat(seqs, 1),
+                      cu=[new * b for b in range(seqs + 1)], tokens=new * seqs)
+    blocks = ref4.fast_blocks(B)
+    assert torch.equal(B.v[0, 0, 1], v[0, 0, 1])
+    below = float(B.k[0, 0, 0, 0])
+    cache, batch = blocks.device(mc)
+    q = torch.zeros(new * seqs, kv * group, dim, dtype=T, device="cuda")
+    q[..., 0] = 1.0
+    out, lse = mc.attn4_prefill(cache, batch, q, scale=1.0, with_lse=True)
+    others = torch.arange(length - new, length, dtype=torch.float64)  # keys after the first one, of each new token
+    w = others * np.exp(-below)
+    want = (w / (1 + w))[:, None] * v[0, 0, 1].double()
+    h = ref.HALF_ULP[dtype]
+    tol = (2 * h + 1e-4) * want + (2.0 ** -24 + length * 2.0 ** -32 * 64 if dtype == "fp16" else 0) + 1e-30
+    assert ((out.view(seqs, new, kv * group, dim).double().cpu() - want[:, None]).abs() <= tol[:, None]).all()
+    assert ((lse.view(seqs, new, kv * group).double().cpu() - (below + torch.log1p(w))[:, None]).abs() <= 1e-4).all()
+
+
 # --------------------------------------------------------------- prefill --
 
 PREFILL = [
