@@ -154,8 +154,7 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     const int64_t rows = ((int64_t)batch->tokens + batch->seqs - 1) / batch->seqs * p.group;
     const bool bf16 = cache->dtype == MC_BF16;
     if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, q4, (int)rows, (cudaStream_t)stream);
-    if (q4) return launch_rows4(p, cache->head_dim, bf16, (cudaStream_t)stream);
-    return launch_prefill(p, cache->head_dim, bf16, (cudaStream_t)stream);
+    return launch_prefill(p, cache->head_dim, bf16, q4, (cudaStream_t)stream);
 }
 
 static int append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,

@@ -350,8 +350,7 @@ struct SmemAttr {
 };
 size_t decode_part_bytes(int head_dim);
 int launch_decode(const AttnParams &p, int head_dim, bool bf16, bool q4, int rows, cudaStream_t st);
-int launch_rows4(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
 size_t prefill_part_bytes(int head_dim);
-int launch_prefill(const AttnParams &p, int head_dim, bool bf16, cudaStream_t st);
+int launch_prefill(const AttnParams &p, int head_dim, bool bf16, bool q4, cudaStream_t st);
 
 }  // namespace mc

@@ -47,7 +47,8 @@
 namespace mc {
 
 constexpr int kPfRows = 256, kPfTile = 128, kPfKeys = 128;
-constexpr int kPfThreads = 384, kPfMma = 8, kPfKv = 10;  // MMA: two warps; after kPfKv the queries
+constexpr int kPfMma = 8, kPfKv = 10, kPfUnpack = 12;  // MMA: two warps; after kPfKv the queries
+constexpr int pf_threads(bool q4) { return q4 ? 512 : 384; }
 constexpr int kPfMaxStages = 8;
 constexpr int kPfAhead = 8;   // items that a block's roles may be apart (the copies lead the softmax by 4 at most)
 constexpr int kPfCount = 32;  // the queue's count: a word of the 256 bytes behind the status word
@@ -230,10 +231,10 @@ constexpr int kPfItemCost = 2;
 constexpr int64_t kPfL2 = 64 << 20;
 struct PfOrder {
     int first, n, shift;
-    __device__ __forceinline__ PfOrder(const AttnParams &p, int D, const volatile PfItem &at, int run, int spent)
+    __device__ __forceinline__ PfOrder(const AttnParams &p, int key_bytes, const volatile PfItem &at, int run, int spent)
         : first(at.u), n(at.n), shift(0)
     {
-        if (at.k.units <= run || (int64_t)at.s.len * p.c.kv_heads * D * 4 <= kPfL2) return;
+        if (at.k.units <= run || (int64_t)at.s.len * p.c.kv_heads * key_bytes <= kPfL2) return;
         const int ahead = (spent - at.u) % run, to = ahead < 0 ? ahead + run : ahead;
         if (to < n) shift = to;
     }
@@ -393,12 +394,16 @@ __device__ __forceinline__ void pf_copy16z(uint32_t dst, const void *src, bool r
 }
 
 // Registers: the softmax threads hold a row of 128 scores, the others little.  The shares
-// (2 warpgroups of kPfSoftRegs and one of kPfRestRegs) are within what the block has at
-// launch, kPfRegs a thread (checked before the launch: a larger share would wait for ever).
-constexpr int kPfRegs = 168, kPfSoftRegs = 208, kPfRestRegs = 80;
-static_assert(2 * kPfSoftRegs + kPfRestRegs <= 3 * kPfRegs, "register shares");
-__device__ __forceinline__ void pf_take_regs() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfSoftRegs)); }
-__device__ __forceinline__ void pf_give_regs() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfRestRegs)); }
+// (2 warpgroups of kSoft and the others of kRest) are within what the block has at
+// launch, kAll a thread (checked before the launch: a larger share would wait for ever).
+// Q4 has a warpgroup more.
+template <bool Q4>
+struct PfRegs {
+    static constexpr int kAll = Q4 ? 128 : 168, kSoft = Q4 ? 192 : 208, kRest = Q4 ? 64 : 80;
+    static_assert(2 * kSoft + (Q4 ? 2 : 1) * kRest <= (Q4 ? 4 : 3) * kAll, "register shares");
+    static __device__ __forceinline__ void take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoft)); }
+    static __device__ __forceinline__ void give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRest)); }
+};
 
 // ---------------------------------------------------------------- softmax --
 
@@ -515,12 +520,57 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 // ------------------------------------------------------------------ kernel --
 
 // QUEUE: the batch may have the items for a queue (the host's bound), so the kernel looks at them.
-template <int D, bool BF16, int MODE, bool QUEUE>
-__global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams pp, const __grid_constant__ CUtensorMap kmap,
+// A key's row of the 4-bit cache, as loaded, and into a tile: its groups' 64 columns in 8 chunks of 16 bytes, swizzled.
+template <int D>
+struct PfRaw {
+    uint4 w[D / 32];
+    uint32_t word;
+
+    // (zeros, that is a scale of 0, where there is no such key)
+    __device__ __forceinline__ void load(const KvView &c, const uint16_t *side, int page, int h, int row)
+    {
+        if (page < 0) {
+            word = 0;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) w[i] = make_uint4(0, 0, 0, 0);
+            return;
+        }
+        const uint8_t *block = kv4_block<D>(c, side, page, h);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(block + row * kv4_code_bytes(D)) + i);
+        const uint8_t *words = block + c.page_size * kv4_code_bytes(D) + row * kv4_word_bytes(D);
+        word = D == 128 ? __ldg(reinterpret_cast<const uint32_t *>(words)) : __ldg(reinterpret_cast<const uint16_t *>(words));
+    }
+
+    template <bool BF16>
+    __device__ __forceinline__ void store(uint32_t tile, int half, int r) const
+    {
+        using P = Kv4Pairs<BF16>;
+        constexpr int kGroups = D / kKv4Group;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const uint32_t z = P::zeros(word >> (16 * g)), sc = P::scales(word >> (16 * g));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int x = i * kGroups + g;
+                const uint32_t v = x % 4 == 0 ? w[x / 4].x : x % 4 == 1 ? w[x / 4].y : x % 4 == 2 ? w[x / 4].z : w[x / 4].w;
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + g * half + r * 128 + ((i ^ (r & 7)) << 4)),
+                             "r"(P::mul(P::sub(P::magic(v, 0), z), sc)), "r"(P::mul(P::sub(P::magic(v, 1), z), sc)),
+                             "r"(P::mul(P::sub(P::magic(v, 2), z), sc)), "r"(P::mul(P::sub(P::magic(v, 3), z), sc))
+                             : "memory");
+            }
+        }
+    }
+};
+
+template <int D, bool BF16, int MODE, bool QUEUE, bool Q4>
+__global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfParams pp, const __grid_constant__ CUtensorMap kmap,
                                                                    const __grid_constant__ CUtensorMap vmap,
                                                                    const __grid_constant__ CUtensorMap qmap)
 {
     using Sh = PfShape<D>;
+    using Regs = PfRegs<Q4>;
+    constexpr int kKeyBytes = Q4 ? 2 * kv4_row_bytes(D) : 4 * D;
     extern __shared__ __align__(1024) uint8_t smem[];
     PfShared *sh = reinterpret_cast<PfShared *>(smem);
     const AttnParams &p = pp.a;
@@ -528,7 +578,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 
     if (tid == 0) {
         for (int i = 0; i < Sh::kStages; ++i) {
-            mbar_init(&sh->kfull[i], 1);
+            mbar_init(&sh->kfull[i], Q4 ? 4 : 1);
             mbar_init(&sh->kempty[i], 2);
         }
         mbar_init(&sh->vpatch, 1);
@@ -635,8 +685,90 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         sh->abort = 1;
     }
     if (warp >= kPfMma) {
-        pf_give_regs();  // one instruction for the warpgroup
-        if (warp >= kPfKv) {
+        Regs::give();  // one instruction for the warpgroup
+        if (Q4 && warp >= kPfUnpack) {
+            // ------------------------------------------------- keys and values in 4 bits --
+            // A thread a key: its row is loaded a tile ahead, while the tile before is written out, as exact numbers
+            // of the type, to where a copy would have put them.
+            const int r = tid - 32 * kPfUnpack;
+            const uint32_t ring = smem_u32(smem) + Sh::kRing;
+            int it = 0;
+            bool ok = !(pp.debug & kDebugNoProducer);
+            const volatile PfItem *item = ok ? pf_item(pp, sh, 0) : nullptr;
+            int b = 0, h = 0, base = 0, from = 0, to = 0, page = -1, row = 0, spent = 0;
+            // the page of this thread's key of unit u (as the table has it)
+            auto look = [&](int u) {
+                const int j = base + u * kPfKeys + r;
+                if (j < from || j >= to) return -1;
+                const int pg = __ldg(p.b.table + (int64_t)b * p.b.table_width + p.c.page.div(j, row));
+                return pg;
+            };
+            auto checked = [&](int u, int pg) {
+                if ((unsigned)pg < (unsigned)p.c.num_pages) return pg;
+                const int j = base + u * kPfKeys + r;
+                if (j >= from && j < to) set_status(p.status, MC_ERR_RANGE);
+                return -1;
+            };
+            auto enter = [&]() {
+                b = item->b;
+                h = item->h;
+                base = item->k.base;
+                from = item->k.first;
+                to = min(item->k.end, item->s.len);
+            };
+            // tile number `it`, when its slot is free
+            auto put = [&](const PfRaw<D> &x) {
+                const int slot = it % Sh::kStages;
+                if (it >= Sh::kStages && !(ok = warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh))) return;
+                x.template store<BF16>(ring + slot * Sh::kTileBytes, Sh::kHalf, r);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh->kfull[slot]);
+                ++it;
+            };
+            PfRaw<D> k, v;
+            int n = 0, u = 0;
+            PfOrder order(p, kKeyBytes, sh->item[0], sh->run, 0);
+            if (item) {
+                enter();
+                n = item->n;
+                u = order.unit(0);
+                page = checked(u, look(u));
+                k.load(p.c, p.c.k, page, h, row);
+            }
+            for (int turn = 0; ok && n > 0;) {
+                for (int i = 0; ok && i < n; ++i) {
+                    v.load(p.c, p.c.v, page, h, row);
+                    int next = -1, next_h = h;
+                    if (i + 1 < n) {
+                        u = order.unit(i + 1);
+                        next = look(u);
+                    }
+                    put(k);
+                    if (!ok) break;
+                    if (i + 1 == n) {
+                        spent += n + kPfItemCost;
+                        item = pf_item(pp, sh, ++turn);
+                        n = 0;
+                        if (item) {
+                            enter();
+                            next_h = h;
+                            order = PfOrder(p, kKeyBytes, *item, sh->run, spent);
+                            n = item->n;
+                            u = order.unit(0);
+                            next = look(u);
+                        }
+                        page = n ? checked(u, next) : -1;
+                        k.load(p.c, p.c.k, page, next_h, row);
+                        put(v);
+                        break;
+                    }
+                    page = checked(u, next);
+                    k.load(p.c, p.c.k, page, h, row);
+                    put(v);
+                }
+            }
+        } else if (warp >= kPfKv) {
             // -------------------------------------------------------------- copies --
             const uint32_t smem0 = smem_u32(smem);
             if (warp == kPfKv) {
@@ -684,7 +816,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 PfItem at = {};
                 auto pages = [&](int u) {
                     const int j = at.k.base + u * kPfKeys + lane * pp.box_rows;
-                    if (lane >= boxes || j >= at.k.end || j + pp.box_rows <= at.k.first) return -1;
+                    if (Q4 || lane >= boxes || j >= at.k.end || j + pp.box_rows <= at.k.first) return -1;
                     return __ldg(p.b.table + (int64_t)at.b * p.b.table_width + p.c.page.div(j));
                 };
                 at.b = -1;
@@ -708,7 +840,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 int spent = 0;
                 for (int turn = 0; ok && at.n > 0; ++turn) {
                     const int n = at.n;
-                    const PfOrder order(p, D, at, sh->run, spent);
+                    const PfOrder order(p, kKeyBytes, at, sh->run, spent);
                     int page = pages(order.unit(0)), count = 0;
                     PfItem next_item = at;
                     if (queued && lane == 0) count = atomicAdd(p.status + kPfCount, 1);
@@ -717,13 +849,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                         const int j0 = at.k.base + u * kPfKeys, j = j0 + lane * pp.box_rows;
                         int row;
                         p.c.page.div(j, row);
-                        if ((unsigned)page >= (unsigned)p.c.num_pages) {
+                        if (!Q4 && (unsigned)page >= (unsigned)p.c.num_pages) {
                             if (lane < boxes && j < at.k.end && j + pp.box_rows > at.k.first) set_status(p.status, MC_ERR_RANGE);
                             page = p.c.num_pages;
                         }
                         for (int kv = 0; kv < 2; ++kv, ++it) {
                             const int slot = it % Sh::kStages;
                             if (it >= Sh::kStages && !(ok = warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh))) break;
+                            if (Q4) continue;  // (others fill it; this role keeps to their pace)
                             // values past the sequence's end may be NaN, and a weight of 0 would not
                             // hide that (nor would a capped key's neighbour): their rows are zeroed
                             // before the tile is given on
@@ -762,7 +895,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 }
                 // the last copies land before the block's shared memory is given back, on an abort too
                 const uint64_t t0 = globaltimer_ns();
-                for (int i = max(0, it - Sh::kStages); i < it; ++i)
+                for (int i = Q4 ? it : max(0, it - Sh::kStages); i < it; ++i)
                     while (!__all_sync(0xffffffffu, mbar_try_wait(&sh->kfull[i % Sh::kStages], (i / Sh::kStages) & 1)))
                         if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > pp.timeout_ns)) break;
                 pdl_trigger();
@@ -934,7 +1067,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
         }
     } else {
         // -------------------------------------------------- softmax and epilogue --
-        pf_take_regs();
+        Regs::take();
         const int t = warp >> 2, wt = warp & 3, row = wt * 32 + lane;
         const uint32_t lanes = (uint32_t)(wt * 32) << 16;
         const uint32_t s_tmem = lanes + 128 * t, o_tmem = lanes + 256 + 128 * t;
@@ -961,7 +1094,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
                 const int all_lo = p.window ? p_last - p.window + 1 : 0;
                 const float slope = MODE != kPfPlain && p.slopes ? __ldg(p.slopes + head) * kLog2e : 0.f;
                 float m = -INFINITY, l = 0.f;
-                const PfOrder order(p, D, *it, sh->run, spent);
+                const PfOrder order(p, kKeyBytes, *it, sh->run, spent);
                 for (int i = 0; i < n; ++i) {
                     if (!(ok = warp_wait(&sh->sfull[t], su & 1, pp, sh))) break;
                     ++su;
@@ -1061,7 +1194,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const PfParams p
 
 // Whether a key that was copied for an item, and that one of its tokens t0 .. t1 hides, is infinite or
 // NaN: by `warps` warps, the answer the warp's.
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 __device__ __forceinline__ bool pf_hides_odd(const PfParams &pp, int b, int h, int mt, const PfSeq &s, int t0, int t1, int warp, int warps,
                                              int lane)
 {
@@ -1070,24 +1203,24 @@ __device__ __forceinline__ bool pf_hides_odd(const PfParams &pp, int b, int h, i
     const int from = k.first & -pp.box_rows, to = min(s.len, (k.end + pp.box_rows - 1) & -pp.box_rows);  // whole boxes
     const int p0 = s.len - s.n + t0, p1 = s.len - s.n + t1;
     const int lo = p.window ? max(0, p1 - p.window + 1) : 0, hi = p0 < 0 ? 0 : max(p0 + 1, s.prefix);
-    return odd_keys<D, BF16, false>(p, b, h, from, min(lo, to), warp, warps, lane) ||
-           odd_keys<D, BF16, false>(p, b, h, max(hi, from), to, warp, warps, lane);
+    return odd_keys<D, BF16, Q4>(p, b, h, from, min(lo, to), warp, warps, lane) ||
+           odd_keys<D, BF16, Q4>(p, b, h, max(hi, from), to, warp, warps, lane);
 }
 
 constexpr int kPfJoinRows = 16;  // rows of an open item that a block of the join launch adds
 
 // A row that came out infinite or NaN, redone if it hides a key that is.
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 __device__ __noinline__ void pf_redo_row(const PfParams &pp, int b, int mt, int tok, int head, int lane)
 {
     const PfSeq s = pf_seq(pp.a, b, nullptr);
-    if (pf_hides_odd<D, BF16>(pp, b, pp.a.by_group.div(head), mt, s, tok, tok, 0, 1, lane))
-        exact_row<D, BF16, false>(pp.a, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
+    if (pf_hides_odd<D, BF16, Q4>(pp, b, pp.a.by_group.div(head), mt, s, tok, tok, 0, 1, lane))
+        exact_row<D, BF16, Q4>(pp.a, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
 }
 
 // 16 rows of a CTA's open item: adds its pieces in their order, the loads of four pieces
 // in flight at once.
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 __device__ __forceinline__ void pf_join(const PfParams &pp, const PfOpen &it)
 {
     constexpr int kQuads = D / 4 / 16;  // column quads of a thread: threadIdx.x / 16, + 16, ...
@@ -1142,7 +1275,7 @@ __device__ __forceinline__ void pf_join(const PfParams &pp, const PfOpen &it)
         if (!odd[x]) continue;
         int g2;
         const int t2 = p.by_group.div(it.mt * kPfRows + blockIdx.y * kPfJoinRows + x, g2);
-        pf_redo_row<D, BF16>(pp, it.b, it.mt, t2, it.h * p.group + g2, threadIdx.x & 31);
+        pf_redo_row<D, BF16, Q4>(pp, it.b, it.mt, t2, it.h * p.group + g2, threadIdx.x & 31);
     }
 }
 
@@ -1150,7 +1283,7 @@ __device__ __forceinline__ void pf_join(const PfParams &pp, const PfOpen &it)
 // launch's blocks take the items' rows, kPfRedoRows at a time, in turn.  An open item's rows are its join's.
 // A prompt of 4096 tokens, every row of which sees a NaN, takes 135 us instead of 112 (115 ms with every row redone).
 constexpr int kPfRedoRows = 32;
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 __device__ __noinline__ void pf_redo(const PfParams &pp)
 {
     const AttnParams &p = pp.a;
@@ -1165,7 +1298,7 @@ __device__ __noinline__ void pf_redo(const PfParams &pp)
             const int r0 = mt * kPfRows + turn % (kPfRows / kPfRedoRows) * kPfRedoRows, rows = min(kPfRedoRows, s.n * p.group - r0);
             const PfOpen o = threadIdx.x < gridDim.x ? pp.open[threadIdx.x] : PfOpen{0, 0, 0, 0};
             if (__syncthreads_or(o.pieces && o.b == b && o.h == h && o.mt == mt) || rows <= 0) continue;
-            if (!__syncthreads_or(pf_hides_odd<D, BF16>(pp, b, h, mt, s, p.by_group.div(r0), p.by_group.div(r0 + rows - 1), warp, 8, lane)))
+            if (!__syncthreads_or(pf_hides_odd<D, BF16, Q4>(pp, b, h, mt, s, p.by_group.div(r0), p.by_group.div(r0 + rows - 1), warp, 8, lane)))
                 continue;
             for (int r = warp; r < rows; r += 8) {
                 int hg;
@@ -1178,7 +1311,7 @@ __device__ __noinline__ void pf_redo(const PfParams &pp)
                     odd = fmaf(v.x, 0.f, fmaf(v.y, 0.f, odd));
                 }
                 if (__any_sync(0xffffffffu, odd != odd))
-                    exact_row<D, BF16, false>(p, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
+                    exact_row<D, BF16, Q4>(p, b, s.len - s.n + tok, s.len, s.prefix, s.first + tok, head, lane);
             }
         }
         turn -= slices;
@@ -1187,7 +1320,7 @@ __device__ __noinline__ void pf_redo(const PfParams &pp)
 
 // (most blocks have nothing to add: with the 62 registers that heads of 64 take unbounded, four
 // blocks an SM, the launch is 0.6 us longer)
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 __global__ void __launch_bounds__(256, D == 64 ? 5 : 4) prefill_join_kernel(const PfParams pp)
 {
     pdl_trigger();
@@ -1195,8 +1328,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 5 : 4) prefill_join_kernel(cons
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) pp.a.status[kPfCount] = 0;
     const PfOpen it = pp.open[blockIdx.x];
     const bool odd = __builtin_expect(__syncthreads_or(threadIdx.x < gridDim.x && pp.odd[threadIdx.x]), 0);
-    if (it.pieces) pf_join<D, BF16>(pp, it);
-    if (odd) pf_redo<D, BF16>(pp);
+    if (it.pieces) pf_join<D, BF16, Q4>(pp, it);
+    if (odd) pf_redo<D, BF16, Q4>(pp);
 }
 static_assert(kAttnMaxSms <= 256, "a thread per CTA of the first launch");
 
@@ -1225,15 +1358,15 @@ static bool pf_map(CUtensorMap *m, const void *base, bool bf16, int rank, const 
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool BF16, int MODE, bool QUEUE>
+template <int D, bool BF16, int MODE, bool QUEUE, bool Q4>
 static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st)
 {
     const KvView &c = p.a.c;
-    CUtensorMap kmap, vmap, qmap;
+    CUtensorMap kmap = {}, vmap = {}, qmap;
     const cuuint64_t dims[4] = {D, (cuuint64_t)c.page_size, (cuuint64_t)c.kv_heads, (cuuint64_t)c.num_pages};
     const cuuint64_t strides[3] = {D * 2, (cuuint64_t)c.page_size * D * 2, (cuuint64_t)c.page_stride * 2};
     const cuuint32_t box[4] = {64, (cuuint32_t)p.box_rows, 1, 1};
-    if (!pf_map(&kmap, c.k, BF16, 4, dims, strides, box) || !pf_map(&vmap, c.v, BF16, 4, dims, strides, box)) return cudaErrorInvalidValue;
+    if (!Q4 && (!pf_map(&kmap, c.k, BF16, 4, dims, strides, box) || !pf_map(&vmap, c.v, BF16, 4, dims, strides, box))) return cudaErrorInvalidValue;
     if (p.q_boxes) {
         const cuuint64_t qdims[3] = {D, (cuuint64_t)p.a.q_heads, (cuuint64_t)p.a.b.tokens};
         const cuuint64_t qstrides[2] = {D * 2, (cuuint64_t)p.a.q_stride * 2};
@@ -1243,48 +1376,55 @@ static cudaError_t launch_prefill_t(const PfParams &p, int ctas, cudaStream_t st
         qmap = kmap;  // not used
     }
     using Sh = PfShape<D>;
-    auto k = prefill_kernel<D, BF16, MODE, QUEUE>;
+    auto k = prefill_kernel<D, BF16, MODE, QUEUE, Q4>;
     static std::atomic<bool> known{false};  // (the same build on every device)
     cudaError_t e = cudaSuccess;
     if (!known.load(std::memory_order_relaxed)) {
         cudaFuncAttributes at;
         e = cudaFuncGetAttributes(&at, k);
         if (e != cudaSuccess) return e;
-        if (at.numRegs < kPfRegs) return cudaErrorInvalidConfiguration;
+        if (at.numRegs < PfRegs<Q4>::kAll) return cudaErrorInvalidConfiguration;
         known.store(true, std::memory_order_relaxed);
     }
     static SmemAttr attr;
     e = attr.set((const void *)k, Sh::kSmem);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnPrefill, st);
-    e = launch_k(k, dim3(ctas), dim3(kPfThreads), Sh::kSmem, st, p, kmap, vmap, qmap);
+    e = launch_k(k, dim3(ctas), dim3(pf_threads(Q4)), Sh::kSmem, st, p, kmap, vmap, qmap);
     profile_end(kKAttnPrefill, st);
     if (e != cudaSuccess) return e;
     profile_begin(kKAttnJoin, st);
-    e = launch_k(prefill_join_kernel<D, BF16>, dim3(ctas, kPfRows / kPfJoinRows), dim3(256), 0, st, p);
+    e = launch_k(prefill_join_kernel<D, BF16, Q4>, dim3(ctas, kPfRows / kPfJoinRows), dim3(256), 0, st, p);
     profile_end(kKAttnJoin, st);
     return e;
 }
 
-template <int D, bool BF16, int MODE>
+template <int D, bool BF16, int MODE, bool Q4>
 static cudaError_t launch_prefill_q(const PfParams &p, int ctas, cudaStream_t st)
 {
     // What the lengths decide is the kernel's; where there cannot be items enough, or sequences are
     // more than the queue takes, one without the queue's code does (9 ragged prompts 32.7 -> 32.2 us).
     const int64_t items = ((int64_t)p.a.b.tokens * p.a.group / kPfRows + p.a.b.seqs) * p.a.c.kv_heads;  // at most
-    return p.a.b.seqs <= 32 && items >= kPfQueueItems * ctas && items < 1 << 30 ? launch_prefill_t<D, BF16, MODE, true>(p, ctas, st)
-                                                                                : launch_prefill_t<D, BF16, MODE, false>(p, ctas, st);
+    return p.a.b.seqs <= 32 && items >= kPfQueueItems * ctas && items < 1 << 30 ? launch_prefill_t<D, BF16, MODE, true, Q4>(p, ctas, st)
+                                                                                : launch_prefill_t<D, BF16, MODE, false, Q4>(p, ctas, st);
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool Q4>
 static cudaError_t launch_prefill_m(const PfParams &p, int mode, int ctas, cudaStream_t st)
 {
-    return mode == kPfCap    ? launch_prefill_q<D, BF16, kPfCap>(p, ctas, st)
-           : mode == kPfBias ? launch_prefill_q<D, BF16, kPfBias>(p, ctas, st)
-                             : launch_prefill_q<D, BF16, kPfPlain>(p, ctas, st);
+    return mode == kPfCap    ? launch_prefill_q<D, BF16, kPfCap, Q4>(p, ctas, st)
+           : mode == kPfBias ? launch_prefill_q<D, BF16, kPfBias, Q4>(p, ctas, st)
+                             : launch_prefill_q<D, BF16, kPfPlain, Q4>(p, ctas, st);
 }
 
-int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st)
+template <bool Q4>
+static cudaError_t launch_prefill_d(const PfParams &p, int head_dim, bool bf16, int mode, int ctas, cudaStream_t st)
+{
+    return head_dim == 64 ? (bf16 ? launch_prefill_m<64, true, Q4>(p, mode, ctas, st) : launch_prefill_m<64, false, Q4>(p, mode, ctas, st))
+                          : (bf16 ? launch_prefill_m<128, true, Q4>(p, mode, ctas, st) : launch_prefill_m<128, false, Q4>(p, mode, ctas, st));
+}
+
+int launch_prefill(const AttnParams &a, int head_dim, bool bf16, bool q4, cudaStream_t st)
 {
     if ((int64_t)a.b.tokens * a.group > 0x7fffffff - kPfRows)
         return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d heads a group in one call", a.b.tokens, a.group);
@@ -1297,14 +1437,13 @@ int launch_prefill(const AttnParams &a, int head_dim, bool bf16, cudaStream_t st
     p.debug = debug_flags();
     p.q_boxes = kPfTile % a.group == 0 && a.q_stride < (int64_t)1 << 38;
     p.out32 = (uintptr_t)a.out % 32 == 0 && a.out_stride % 16 == 0;
-    p.box_rows = std::min(a.c.page_size & -a.c.page_size, kPfKeys);
+    p.box_rows = q4 ? 1 : std::min(a.c.page_size & -a.c.page_size, kPfKeys);  // (the 4-bit cache's keys come one by one)
     const int mode = a.cap > 0.f ? kPfCap : a.slopes ? kPfBias : kPfPlain;
     int nsm = 0;
     cudaError_t e = sm_count(&nsm);
     if (e == cudaSuccess) {
         const int ctas = nsm < kAttnMaxSms ? nsm : kAttnMaxSms;
-        e = head_dim == 64 ? (bf16 ? launch_prefill_m<64, true>(p, mode, ctas, st) : launch_prefill_m<64, false>(p, mode, ctas, st))
-                           : (bf16 ? launch_prefill_m<128, true>(p, mode, ctas, st) : launch_prefill_m<128, false>(p, mode, ctas, st));
+        e = q4 ? launch_prefill_d<true>(p, head_dim, bf16, mode, ctas, st) : launch_prefill_d<false>(p, head_dim, bf16, mode, ctas, st);
     }
     if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "prefill launch: %s", cudaGetErrorString(e));
     return MC_OK;

@@ -252,7 +252,7 @@ def test_groups_far_apart_in_scale(mc):
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("below", [9.0, 14.0, 17.0])
-@pytest.mark.parametrize("new,group", [(1, 1)])
+@pytest.mark.parametrize("new,group", [(1, 1), (32, 8)])  # each kernel
 def test_small_weights_keep_their_sum(mc, dtype, below, new, group):
     """8191 equal keys far below one: each weighs little, together they weigh what they should."""
     seqs, kv, length, dim, page = 40, 8, 8192, 64, 128
@@ -537,6 +537,40 @@ def test_pages_behind_the_window_may_be_gone(mc):
         ref.assert_attention(out, lse, want, "bf16", 700, 5.0)
 
 
+@pytest.mark.parametrize("seqs,new,length,heads,kv", [(1, 4096, 4096, 16, 4),   # whole items
+                                                      (1, 300, 9000, 8, 2),     # split and joined
+                                                      (16, 4, 4000, 16, 4)])    # few rows a sequence
+def test_a_visible_nan_costs_little(mc, seqs, new, length, heads, kv):
+    """A NaN that every row sees: none is redone key by key."""
+    B = ref.Batch([length] * seqs, [new] * seqs, kv, 64, 128, "bf16", 83)
+    q = B.randn(B.tokens, heads, 128).cuda()
+    k0, v0 = B.k.clone(), B.v.clone()
+    took, got = [], []
+    for what in (None, float("nan")):
+        B.k, B.v = k0.clone(), v0.clone()
+        if what is not None:
+            for b in range(seqs):
+                B.v[B.table[b, 0], :, 0, 3] = what
+        cache, batch = ref4.fast_blocks(B).device(mc)
+        ws = mc.attn4_workspace(cache, heads)
+        out = torch.full_like(q, 100.0)
+        call = lambda: mc.attn4_prefill(cache, batch, q, out=out, workspace=ws)  # noqa: E731
+        for _ in range(3):
+            call()
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
+        for _ in range(10):
+            call()
+        end.record()
+        mc.check_status(ws)
+        torch.cuda.synchronize()
+        took.append(start.elapsed_time(end) / 10)
+        got.append(out)
+    assert torch.isnan(got[1][..., :64]).all()
+    assert torch.equal(got[0][..., 64:], got[1][..., 64:])
+    assert took[1] <= 10 * took[0], took
+
+
 # ----------------------------------------------------------- streams, status --
 
 def test_on_another_stream_and_in_graphs_that_share_a_workspace(mc):
@@ -589,3 +623,23 @@ def test_an_append_without_a_page_or_position_is_reported(mc):
     _reported(mc, ws)
     mc.kv4_append(cache, mc.KVBatch(_i32([200, 64]), B.table.cuda()), q, k, v, workspace=ws)  # a length past the pages
     _reported(mc, ws)
+
+
+def test_prefill_waits_expire_and_the_context_lives(mc):
+    """With the copies switched off every wait of the kernel reaches its bound."""
+    B = ref.Batch([300], [300], 1, 16, 64, "bf16", 23)
+    cache, batch = ref4.fast_blocks(B).device(mc)
+    q = B.randn(300, 4, 64).cuda()
+    ws = mc.attn4_workspace(cache, 4)
+    want = mc.attn4_prefill(cache, batch, q, workspace=ws)
+    mc.check_status(ws)
+    mc.set_debug(1, 20_000_000)
+    try:
+        mc.attn4_prefill(cache, batch, q, workspace=ws)
+        with pytest.raises(mc.MCError) as e:
+            mc.check_status(ws)
+        assert e.value.code == mc.ERR_TIMEOUT
+    finally:
+        mc.set_debug(0, 1_000_000_000)
+    assert torch.equal(mc.attn4_prefill(cache, batch, q, workspace=ws), want)
+    mc.check_status(ws)
