@@ -35,9 +35,10 @@ constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 // Keys of a unit that one warp takes, in tiles of 16: heads of 64 take two tiles in one step,
 // whose chains of products and exponentials overlap (a step of 16 keys takes about as long
 // whatever the head, and 16 keys of 64 are half the bytes).
-constexpr int dec_tiles(int D, bool q4) { return q4 || D == 64 ? 2 : 1; }
-constexpr int dec_unit(int D, bool q4) { return 16 * dec_tiles(D, q4) * kDecWarps; }
-constexpr int dec_ctas(bool q4, int nt) { return q4 && nt == 1 ? 3 : 2; }  // an SM
+constexpr int dec_tiles(int D, bool q4, int nt) { return q4 ? (nt == 1 ? 4 : nt == 4 ? 1 : 2) : D == 64 ? 2 : 1; }
+constexpr int dec_unit(int D, bool q4, int nt) { return 16 * dec_tiles(D, q4, nt) * kDecWarps; }
+constexpr int dec_ctas(int D, bool q4, int nt) { return q4 && D == 64 && nt == 1 ? 3 : 2; }  // an SM
+constexpr int dec_stages(bool q4, int nt) { return q4 && nt == 1 ? 2 : 3; }
 constexpr int kDecMaxTiles = 4;                // n-tiles of the largest slice
 constexpr int kDecItemCost = 2;  // what an item costs on top of its units, in units (up to 128 sequences; 64 of up
                                 // to 500 keys 23.8 us at 0, 18.4 at 1, 18.1 at 2, 18.4 at 3)
@@ -54,6 +55,14 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
         mma16816(d, a[0], a[1], a[2], a[3], b0, b1);
 }
 
+// D = A * B in fp16.
+__device__ __forceinline__ void mma16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -66,11 +75,21 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
+// 1024 + 16 z of a group, twice, in fp16.
+__device__ __forceinline__ uint32_t sixteenth_zeros(uint32_t word) { return (word & 15u) * 0x100010u + 0x64006400u; }
+
 __device__ __forceinline__ uint32_t transposed8x8(uint32_t a)
 {
     uint32_t r;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
     return r;
+}
+
+// The same without a hint: what the hint takes (two moves to uniform registers a copy) is a tenth of the time of a step
+// of the 4-bit cache.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 
 // Words of codes from shared memory: a lane's of a key, D / 32 of them; of a value, one for each group; and the
@@ -187,7 +206,7 @@ struct Row {
 template <int D, bool BF16, bool Q4>
 __device__ __noinline__ void redo_row(const AttnParams &p, int b, int tok, int head, int lane)
 {
-    const Keys k = keys_of<dec_unit(D, Q4)>(p, b, nullptr);
+    const Keys k = keys_of<dec_unit(D, Q4, 1)>(p, b, nullptr);
     const int h = p.by_group.div(head), pos = k.len - k.n + tok, prefix = p.prefix ? __ldg(p.prefix + b) : 0;
     const int lo = p.window ? max(0, pos - p.window + 1) : 0, hi = pos < 0 ? 0 : max(pos + 1, prefix);
     if (odd_keys<D, BF16, Q4>(p, b, h, k.start, min(lo, k.len), 0, 1, lane) || odd_keys<D, BF16, Q4>(p, b, h, max(hi, k.start), k.len, 0, 1, lane))
@@ -215,28 +234,29 @@ __device__ __forceinline__ bool finite4(const float4 &a)
 template <int D, int NT, bool Q4>
 struct DecShape {
     static constexpr int kRow = Q4 ? kv4_code_bytes(D) : D * 2;  // bytes of a key (Q4: of its codes)
-    static constexpr int kTiles = dec_tiles(D, Q4), kKeys = 16 * kTiles;
+    static constexpr int kTiles = dec_tiles(D, Q4, NT), kKeys = 16 * kTiles;
     static constexpr int kWords = Q4 ? 2 * kKeys * kRow : 0;     // where the groups' words lie in a slot
     static constexpr int kSlot = 2 * kKeys * (kRow + (Q4 ? kv4_word_bytes(D) : 0));  // a warp's keys and values of a unit
-    static constexpr int kStages = 3;
+    static constexpr int kStages = dec_stages(Q4, NT);
     static constexpr int kRing = kSlot * kStages * kDecWarps;
     static constexpr int kPitch = D + 4;                     // floats of a row in the join: O, m, l
     static constexpr int kJoin = kDecWarps * 8 * kPitch * 4; // a piece's rows and queries lie over it
     static constexpr bool kQShared = NT > 2;                 // the queries' fragments: shared memory or registers
     static constexpr int kRows0 = kQShared ? NT * (D / 16) * 256 : 0;
+    static constexpr int kTops = kRows0 + 8 * NT * (int)sizeof(Row);  // Q4: largest |q| of each row, as bits
     static constexpr int kSmem = kRing + kJoin;
-    static_assert(kRows0 + 8 * NT * (int)sizeof(Row) <= kJoin, "rows of a slice");
+    static_assert(kTops + 8 * NT * 4 <= kJoin, "rows of a slice");
 };
 
 // NT: n-tiles of 8 rows of a slice, 1 to 4.  The products are formed transposed, S^T = K Q^T and
 // O^T += V^T P^T: the 16 keys of a warp fill the rows of the m16n8k16 instruction and the
 // slice's rows its 8 columns, half the instructions and accumulators of the other way.
 template <int D, bool BF16, int NT, bool Q4>
-__global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(const AttnParams p, FastDiv by_grid, OpenItem *open,
+__global__ void __launch_bounds__(kDecThreads, dec_ctas(D, Q4, NT)) decode_kernel(const AttnParams p, FastDiv by_grid, OpenItem *open,
                                                                              float *part)
 {
     using Sh = DecShape<D, NT, Q4>;
-    constexpr int kUnit = dec_unit(D, Q4);
+    constexpr int kUnit = dec_unit(D, Q4, NT);
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     float *jo = reinterpret_cast<float *>(smem + Sh::kRing);
@@ -361,10 +381,23 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(c
     constexpr int kChunks = D / 8, kPer = 32 / kChunks;  // 16-byte chunks of a row; rows per warp copy
     const int lc = lane % kChunks, lr = lane / kChunks;
     const uint64_t policy = policy_evict_first();
-    const uint8_t *k4 = reinterpret_cast<const uint8_t *>(p.c.k), *v4 = reinterpret_cast<const uint8_t *>(p.c.v);
     Place ld = at;
-    int ld_left = left, page[Sh::kTiles];
+    int ld_left = left, page[Q4 ? 1 : Sh::kTiles], page_row = 0;
+    // Q4: a tile is copied by its share of the lanes, so that each has one page to find and one address to form: every
+    // kShare-th 16-byte chunk of the tile's codes, and one of its groups' words.  A key goes where the loads below
+    // meet no bank twice: keys in the order of the products' rows (0, 4, 1, 5, ...), values in their own with
+    // neighbouring pairs' halves exchanged.
+    constexpr int kShare = 32 / Sh::kTiles, kRowChunks = Q4 ? Sh::kRow / 16 : 1, kWordChunks = Q4 ? kv4_word_bytes(D) : 1;
+    static_assert(!Q4 || kShare >= 2 * kWordChunks, "a lane for each chunk of words");
+    constexpr int kKeyStep = kShare / kRowChunks;
+    const int own_tile = lane / kShare, mine16 = lane % kShare, first_key = mine16 / kRowChunks, chunk = mine16 % kRowChunks;
+    auto place = [](int key) { return (key & 8) | (key & 3) << 1 | (key >> 2 & 1); };
     auto fetch_page = [&]() {
+        if constexpr (Q4) {
+            const int j = ld.k.base + ld.u * kUnit + warp * Sh::kKeys + 16 * own_tile;
+            page[0] = ld_left > 0 && j < ld.k.len ? seq_page(p.b, p.c, ld.b, p.c.page.div(j, page_row), p.status) : -1;
+            return;
+        }
 #pragma unroll
         for (int kt = 0; kt < Sh::kTiles; ++kt) {
             const int j = ld.k.base + ld.u * kUnit + warp * Sh::kKeys + 16 * kt;
@@ -372,35 +405,37 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(c
         }
     };
     auto issue = [&](int slot) {
+        if constexpr (Q4) {
+            if (ld_left > 0) {
+                const bool real = page[0] >= 0;  // (zeros, that is scales of 0, where there is no page)
+                const int64_t block = kv4_offset<D>(p.c, max(page[0], 0), ld.h);
+                const uint8_t *k = reinterpret_cast<const uint8_t *>(p.c.k) + block, *v = reinterpret_cast<const uint8_t *>(p.c.v) + block;
+                const int at = page_row * Sh::kRow + 16 * mine16;
+                const uint32_t to = ring + slot * Sh::kSlot + 16 * own_tile * Sh::kRow;
+                const uint32_t kt = to + place(first_key) * Sh::kRow + 16 * chunk, vt = to + (Sh::kKeys + first_key) * Sh::kRow;
+#pragma unroll
+                for (int i = 0; i < 16 / kKeyStep; ++i) {
+                    copy16(kt + place(kKeyStep * i) * Sh::kRow, k + at + 16 * kShare * i, real);
+                    copy16(vt + kKeyStep * i * Sh::kRow + 16 * (D == 128 ? chunk ^ ((first_key + kKeyStep * i) & 2) : chunk), v + at + 16 * kShare * i, real);
+                }
+                if (mine16 < 2 * kWordChunks) {
+                    const int side = mine16 / kWordChunks, c = mine16 % kWordChunks;
+                    copy16(ring + slot * Sh::kSlot + Sh::kWords + (side * Sh::kKeys + 16 * own_tile) * kv4_word_bytes(D) + 16 * c,
+                           (side ? v : k) + p.c.page_size * Sh::kRow + page_row * kv4_word_bytes(D) + 16 * c, real);
+                }
+                --ld_left;
+                step<kUnit, NT>(p, ld);
+                fetch_page();
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            return;
+        }
         if (ld_left > 0) {
 #pragma unroll
             for (int kt = 0; kt < Sh::kTiles; ++kt) {
                 const int j = ld.k.base + ld.u * kUnit + warp * Sh::kKeys + 16 * kt;
                 int row;
                 p.c.page.div(j, row);
-                if constexpr (Q4) {
-                    // codes of 16 keys, contiguous; see the fragments below for where a key's 16-byte chunks go
-                    constexpr int kRowChunks = Sh::kRow / 16;
-                    const bool real = page[kt] >= 0;
-                    const int64_t block = kv4_offset<D>(p.c, max(page[kt], 0), ld.h) + row * Sh::kRow;
-                    const uint32_t dst = ring + slot * Sh::kSlot + 16 * kt * Sh::kRow;
-#pragma unroll
-                    for (int i = 0; i < kRowChunks / 2; ++i) {
-                        const int c = lane + 32 * i, key = c / kRowChunks, ch = c % kRowChunks;
-                        const int place = (key & 8) | (key & 3) << 1 | (key >> 2 & 1);
-                        copy16(dst + place * Sh::kRow + 16 * ch, k4 + block + 16 * c, real, policy);
-                        copy16(dst + Sh::kKeys * Sh::kRow + key * Sh::kRow + 16 * (ch ^ (kRowChunks == 4 ? key & 2 : 0)), v4 + block + 16 * c, real, policy);
-                    }
-                    // the groups' words (zeros, that is scales of 0, where there is no page)
-                    constexpr int kWordChunks = kv4_word_bytes(D);  // of 16 keys
-                    if (lane < 2 * kWordChunks) {
-                        const int side = lane / kWordChunks, c = lane % kWordChunks;
-                        const int64_t words = block + (p.c.page_size - row) * Sh::kRow + row * kv4_word_bytes(D);
-                        copy16(ring + slot * Sh::kSlot + Sh::kWords + (side * Sh::kKeys + 16 * kt) * kv4_word_bytes(D) + 16 * c,
-                               (side ? v4 : k4) + words + 16 * c, real, policy);
-                    }
-                    continue;
-                }
                 const int64_t off = (page[kt] < 0 ? 0 : page[kt] * p.c.page_stride) +
                                     ((int64_t)ld.h * p.c.page_size + row + lr) * D + lc * 8;
                 const uint32_t dst = ring + slot * Sh::kSlot + 16 * kt * Sh::kRow;
@@ -449,23 +484,90 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(c
         auto pair = [&](const uint16_t *q, int d, int r) { return r < nrows ? *reinterpret_cast<const uint32_t *>(q + d) : 0u; };
         // Where lane t's pairs of a k-step begin.  Q4: step 4 g + 2 w + i of word 2 t + w of group g, its elements 4 i to
         // 4 i + 3 (the order of a product's terms is free, so each lane takes whole words).
-        auto column = [](int ks, int t) { return Q4 ? 64 * (ks >> 2) + 8 * (2 * t + (ks >> 1 & 1)) + 4 * (ks & 1) : 16 * ks + 2 * t; };
+        auto column = [](int ks, int t) { return 64 * (ks >> 2) + 8 * (2 * t + (ks >> 1 & 1)) + 4 * (ks & 1); };
+        // Q4: fp16 whatever the type (a code is one LOP3 in it where bf16 needs a shift as well), each row times a power of
+        // two that brings its largest element into 2^7 .. 2^8: exact, but for elements 2^-17 of that one and
+        // less (off by 2^-28 of it).  The second pair of a word's four stands at 16 times its value, so
+        // its queries are a sixteenth.
         uint32_t qf[Sh::kQShared ? 1 : NT][D / 16][2];
-        if (Sh::kQShared) {
+        float rs[Q4 ? NT : 1][2];  // a score's factor: the scale and the row's power of two
+        if constexpr (Q4) {
+            uint32_t *tops = reinterpret_cast<uint32_t *>(smem + Sh::kRing + Sh::kTops);
+            constexpr int kMine = Sh::kQShared ? NT * (D / 16) / kDecWarps : NT * (D / 16);
+            uint2 mine[kMine];
+            if (Sh::kQShared) {
+                if (tid < 8 * NT) tops[tid] = 0;
+                __syncthreads();
+            }
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int x = Sh::kQShared ? warp + kDecWarps * i : i, ks = x % (D / 16), r = 8 * (x / (D / 16)) + g;
+                const uint16_t *q = query(r);
+                mine[i] = make_uint2(pair(q, column(ks, t4), r), pair(q, column(ks, t4) + 2, r));
+            }
+            auto size = [](uint32_t w) {  // the larger magnitude of a pair's finite elements, as bits
+                const float2 f = unpack2<BF16>(w);
+                const float a = fabsf(f.x), b = fabsf(f.y);
+                return max(__float_as_uint(a) < 0x7f800000u ? __float_as_uint(a) : 0u, __float_as_uint(b) < 0x7f800000u ? __float_as_uint(b) : 0u);
+            };
+            uint32_t top[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) top[nt] = 0;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const uint32_t w = max(size(mine[i].x), size(mine[i].y));
+                if (Sh::kQShared) atomicMax(tops + 8 * ((warp + kDecWarps * i) / (D / 16)) + g, w);
+                else top[i / (D / 16)] = max(top[i / (D / 16)], w);
+            }
+            if (Sh::kQShared) {
+                __syncthreads();
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) top[nt] = tops[8 * nt + g];
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    top[nt] = max(top[nt], __shfl_xor_sync(0xffffffffu, top[nt], 1));
+                    top[nt] = max(top[nt], __shfl_xor_sync(0xffffffffu, top[nt], 2));
+                }
+            }
+            float up[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                // 2^(7 - e) for a largest element in 2^e .. 2^(e + 1); both powers stay in fp32's normal range
+                const int e = min(max((int)(top[nt] >> 23) - 127, -110), 127), k = 7 - e;
+                up[nt] = __uint_as_float((uint32_t)(127 + k) << 23);
+                const float down = __uint_as_float((uint32_t)(127 - k) << 23);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) rs[nt][c] = __shfl_sync(0xffffffffu, down, 8 * t4 + 4 * c) * p.scale;
+            }
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int x = Sh::kQShared ? warp + kDecWarps * i : i;
+                const float f = up[Sh::kQShared ? x / (D / 16) : i / (D / 16)];
+                const float2 a = unpack2<BF16>(mine[i].x), b = unpack2<BF16>(mine[i].y);
+                const uint2 h = make_uint2(pack2<false>(a.x * f, a.y * f), pack2<false>(b.x * f * 0.0625f, b.y * f * 0.0625f));
+                if (Sh::kQShared) {
+                    qs[x * 32 + lane] = h;
+                } else {
+                    qf[Sh::kQShared ? 0 : i / (D / 16)][i % (D / 16)][0] = h.x;
+                    qf[Sh::kQShared ? 0 : i / (D / 16)][i % (D / 16)][1] = h.y;
+                }
+            }
+        } else if (Sh::kQShared) {
             for (int i = tid; i < NT * (D / 16) * 32; i += kDecThreads) {
                 const int l = i & 31, ks = (i >> 5) % (D / 16), nt = (i >> 5) / (D / 16);
-                const int r = 8 * nt + (l >> 2), d = column(ks, l & 3);
+                const int r = 8 * nt + (l >> 2), d = 16 * ks + 2 * (l & 3);
                 const uint16_t *q = query(r);
-                qs[i] = make_uint2(pair(q, d, r), pair(q, d + (Q4 ? 2 : 8), r));
+                qs[i] = make_uint2(pair(q, d, r), pair(q, d + 8, r));
             }
         } else {
 #pragma unroll
             for (int nt = 0; nt < (Sh::kQShared ? 1 : NT); ++nt) {
-                const uint16_t *q = query(8 * nt + g);
+                const uint16_t *q = query(8 * nt + g) + 2 * t4;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    qf[nt][ks][0] = pair(q, column(ks, t4), 8 * nt + g);
-                    qf[nt][ks][1] = pair(q, column(ks, t4) + (Q4 ? 2 : 8), 8 * nt + g);
+                    qf[nt][ks][0] = pair(q, 16 * ks, 8 * nt + g);
+                    qf[nt][ks][1] = pair(q, 16 * ks + 8, 8 * nt + g);
                 }
             }
         }
@@ -494,13 +596,7 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(c
                 // tiles take two accumulators each, so that the chain is half as long
                 // (Q4: an accumulator for each group, whose scale comes after)
                 constexpr int kChains = Q4 ? D / kKv4Group : NT * Sh::kTiles > 2 ? 1 : 2;
-                float s[Sh::kTiles][NT][kChains][4];
-#pragma unroll
-                for (int kt = 0; kt < Sh::kTiles; ++kt)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) s[kt][nt][0][c] = s[kt][nt][kChains - 1][c] = 0.f;
+                float s[Q4 ? 1 : Sh::kTiles][NT][kChains][4], x[Sh::kTiles][NT][4];
                 const int kr = lane & 15;
                 auto q_of = [&](int nt, int ks) {
                     return Sh::kQShared ? qs[(nt * (D / 16) + ks) * 32 + lane]
@@ -516,9 +612,16 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(c
                             const int key = 16 * kt + 8 * i + own_key;
                             k_words[kt][i] = lds_word<D>(kk + Sh::kWords, key);
                             v_words[kt][i] = lds_word<D>(kk + Sh::kWords, Sh::kKeys + key);
-                            // a row that no token was written to has any scale
-                            if (edge && (j0 + key < keys.start || j0 + key >= keys.len)) k_words[kt][i] = v_words[kt][i] = 0;
                         }
+                    if (edge) {  // a row that no token was written to has any scale
+#pragma unroll
+                        for (int kt = 0; kt < Sh::kTiles; ++kt)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int j = j0 + 16 * kt + 8 * i + own_key;
+                                if (j < keys.start || j >= keys.len) k_words[kt][i] = v_words[kt][i] = 0;
+                            }
+                    }
 #pragma unroll
                     for (int kt = 0; kt < Sh::kTiles; ++kt) {
                         uint32_t w[2][D / 32];
@@ -526,21 +629,42 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(c
                         for (int i = 0; i < 2; ++i) lds_row<D>(kk + (16 * kt + 8 * i + g) * Sh::kRow + t4 * (D / 8), w[i]);
 #pragma unroll
                         for (int grp = 0; grp < kChains; ++grp) {
-                            const uint32_t z0 = P4::zeros(k_words[kt][0] >> (16 * grp)), z1 = P4::zeros(k_words[kt][1] >> (16 * grp));
+                            const uint32_t z[2] = {Kv4Pairs<false>::zeros(k_words[kt][0] >> (16 * grp)), Kv4Pairs<false>::zeros(k_words[kt][1] >> (16 * grp))};
+                            const uint32_t z16[2] = {sixteenth_zeros(k_words[kt][0] >> (16 * grp)), sixteenth_zeros(k_words[kt][1] >> (16 * grp))};
 #pragma unroll
                             for (int ks = 0; ks < 4; ++ks) {
-                                const int x = (ks >> 1) * kChains + grp, j = 2 * (ks & 1);
-                                const uint32_t a[4] = {P4::sub(P4::magic(w[0][x], j), z0), P4::sub(P4::magic(w[1][x], j), z1),
-                                                       P4::sub(P4::magic(w[0][x], j + 1), z0), P4::sub(P4::magic(w[1][x], j + 1), z1)};
+                                const int x = (ks >> 1) * kChains + grp;
+                                uint32_t a[4];
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const uint32_t y = ks & 1 ? w[i][x] >> 8 : w[i][x];
+                                    a[i] = Kv4Pairs<false>::sub(lop_and_or(y, 0x000f000fu, Kv4Pairs<false>::kMagic), z[i]);
+                                    a[2 + i] = Kv4Pairs<false>::sub(lop_and_or(y, 0x00f000f0u, Kv4Pairs<false>::kMagic), z16[i]);
+                                }
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
                                     const uint2 q = q_of(nt, 4 * grp + ks);
-                                    mma16<BF16>(s[kt][nt][grp], a, q.x, q.y);
+                                    if (ks == 0) mma16_first(s[0][nt][grp], a, q.x, q.y);
+                                    else mma16<false>(s[0][nt][grp], a, q.x, q.y);
                                 }
                             }
                         }
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                float sum = s[0][nt][0][c] * kv4_scale(k_words[kt][c >> 1]);
+                                if (kChains == 2) sum = fmaf(s[0][nt][kChains - 1][c], kv4_scale(k_words[kt][c >> 1] >> 16), sum);
+                                x[kt][nt][c] = sum * rs[nt][c & 1];
+                            }
                     }
                 } else {
+#pragma unroll
+                    for (int kt = 0; kt < Sh::kTiles; ++kt)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) s[kt][nt][0][c] = s[kt][nt][kChains - 1][c] = 0.f;
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks) {
                         uint32_t a[Sh::kTiles][4];
@@ -557,22 +681,15 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(Q4, NT)) decode_kernel(c
                 }
                 const bool masked = j0 < all_lo || j0 + Sh::kKeys > all_hi;
                 bool over = false;
-                float x[Sh::kTiles][NT][4];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
+                    if constexpr (!Q4) {
 #pragma unroll
-                    for (int kt = 0; kt < Sh::kTiles; ++kt)
+                        for (int kt = 0; kt < Sh::kTiles; ++kt)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            float sum = s[kt][nt][0][c];
-                            if constexpr (Q4) {
-                                sum *= kv4_scale(k_words[kt][c >> 1]);
-                                if (kChains == 2) sum = fmaf(s[kt][nt][kChains - 1][c], kv4_scale(k_words[kt][c >> 1] >> 16), sum);
-                            } else if (kChains == 2) {
-                                sum += s[kt][nt][kChains - 1][c];
-                            }
-                            x[kt][nt][c] = sum * p.scale;
-                        }
+                            for (int c = 0; c < 4; ++c)
+                                x[kt][nt][c] = (kChains == 2 ? s[kt][nt][0][c] + s[kt][nt][kChains - 1][c] : s[kt][nt][0][c]) * p.scale;
+                    }
                     if (p.cap > 0.f) {
 #pragma unroll
                         for (int kt = 0; kt < Sh::kTiles; ++kt)
@@ -867,8 +984,8 @@ static cudaError_t launch_decode_t(const AttnParams &p, int sms, cudaStream_t st
 {
     using Sh = DecShape<D, NT, Q4>;
     // (more blocks have smaller parts: the workspace holds those of two an SM with the largest slices)
-    static_assert(dec_ctas(Q4, NT) <= 4 && dec_ctas(Q4, NT) * NT <= 2 * kDecMaxTiles, "parts");
-    const int ctas = dec_ctas(Q4, NT) * sms;
+    static_assert(dec_ctas(D, Q4, NT) <= 4 && dec_ctas(D, Q4, NT) * NT <= 2 * kDecMaxTiles, "parts");
+    const int ctas = dec_ctas(D, Q4, NT) * sms;
     OpenItem *open = reinterpret_cast<OpenItem *>(p.part);
     float *part = reinterpret_cast<float *>(p.part + kDecMaxCtas * sizeof(OpenItem));
     auto k = decode_kernel<D, BF16, NT, Q4>;
@@ -883,7 +1000,7 @@ static cudaError_t launch_decode_t(const AttnParams &p, int sms, cudaStream_t st
     // not time: an atomic and two dependent reads by one CTA against a CTA per row: 777 keys 7.8 us
     // with the second launch, 9.9 without, 16 ragged sequences 26.9 and 29.5, 8000 keys of one key
     // head 12.5 and 32.1.)
-    if (e != cudaSuccess || (int64_t)p.b.table_width * p.c.page_size <= dec_unit(D, Q4)) return e;
+    if (e != cudaSuccess || (int64_t)p.b.table_width * p.c.page_size <= dec_unit(D, Q4, NT)) return e;
     profile_begin(kKAttnJoin, st);
     e = launch_k(join_kernel<D, BF16, Q4>, dim3(ctas, 8 * NT), dim3(128), 0, st, p, (const OpenItem *)open, (const float *)part, NT);
     profile_end(kKAttnJoin, st);

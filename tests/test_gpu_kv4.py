@@ -250,6 +250,27 @@ def test_groups_far_apart_in_scale(mc):
         ref.assert_attention(pre, pl, want, dtype, 300, 600.0)
 
 
+@pytest.mark.parametrize("dim,dtype", [(128, "bf16"), (64, "bf16"), (128, "fp16"), (64, "fp16")])
+@pytest.mark.parametrize("heads", [8, 40])  # queries in registers and in shared memory
+def test_queries_of_any_size(mc, dim, dtype, heads):
+    """Rows whose largest element is 2^-40 to 2^40 (fp16: 2^-12 to 2^12), some elements far below it, a row of zeros: the
+    scale makes up for it, and lse is off by 48 roundings of a score of ten at most."""
+    B = ref.Batch([300, 77, 5, 130], [1] * 4, 1, 16, dim, dtype, 14)
+    blocks = ref4.fast_blocks(B)
+    base = B.randn(4, heads, dim).float()
+    base[:, :, 3::7] *= 2.0 ** -9
+    base[1, 0] = 0
+    span = 40 if dtype == "bf16" else 12
+    for e in (-span, -10, 0, 11, span):
+        q = (base * 2.0 ** e).to(ref.DT[dtype])
+        scale = 0.1 * 2.0 ** -e
+        want = ref.attention(B, q, scale)
+        cache, batch = blocks.device(mc, cu=False)
+        out, lse = mc.attn4_decode(cache, batch, q.cuda(), scale=scale, with_lse=True)
+        ref.assert_attention(out, lse, want, dtype, 300, 5.0)
+        assert ((lse.double().cpu() - want[1]).abs() <= 48 * 2.0 ** -24 * 10).all()
+
+
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("below", [9.0, 14.0, 17.0])
 @pytest.mark.parametrize("new,group", [(1, 1), (32, 8)])  # each kernel
@@ -625,12 +646,13 @@ def test_an_append_without_a_page_or_position_is_reported(mc):
     _reported(mc, ws)
 
 
-def test_prefill_waits_expire_and_the_context_lives(mc):
-    """With the copies switched off every wait of the kernel reaches its bound."""
-    B = ref.Batch([300], [300], 1, 16, 64, "bf16", 23)
+@pytest.mark.parametrize("lens,new,heads", [([300], [300], 4), ([300, 40], [200, 40], 3)])
+def test_waits_expire_and_the_context_lives(mc, lens, new, heads):
+    """With the copies switched off every wait of the kernel for many rows reaches its bound."""
+    B = ref.Batch(lens, new, 1, 16, 64, "bf16", 23)
     cache, batch = ref4.fast_blocks(B).device(mc)
-    q = B.randn(300, 4, 64).cuda()
-    ws = mc.attn4_workspace(cache, 4)
+    q = B.randn(B.tokens, heads, 64).cuda()
+    ws = mc.attn4_workspace(cache, heads)
     want = mc.attn4_prefill(cache, batch, q, workspace=ws)
     mc.check_status(ws)
     mc.set_debug(1, 20_000_000)
