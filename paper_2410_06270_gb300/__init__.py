@@ -536,10 +536,11 @@ def _fast():
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)
         at = [ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in ("mc_kv_append", "mc_attn_decode", "mc_attn_prefill",
-                                                                            "mc_kv4_append", "mc_attn4_decode", "mc_attn4_prefill")]
+                                                                            "mc_kv4_append", "mc_attn4_decode", "mc_attn4_prefill", "mc_kv4_read",
+                                                                            "mc_kv_plan", "mc_residual_norm")]
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
         m.setup(*at, torch.empty, raw, getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device, torch.float32,
-                torch.int32, torch.uint8)
+                torch.int32, torch.uint8, torch.int64, torch.bfloat16, torch.float16)
         _fast_module = m
     return _fast_module
 
@@ -705,6 +706,9 @@ def kv4_read(cache: KVCache4, batch: KVBatch, k=None, v=None, workspace=None):
     """What the cache stands for in the rows of the batch's new tokens: (k, v), each [tokens,
     kv_heads, head_dim] in the cache's dtype."""
     _kind(cache, True)
+    r = (_fast_module or _fast()).kv4_read(cache, batch, k, v, workspace)
+    if r is not None:
+        return _check(r) if r.__class__ is int else r
     torch = _torch()
     if batch.index != cache.index:
         _bad("the batch is on %s, the cache on %s" % (batch.device, cache.device))
@@ -794,6 +798,9 @@ def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=Non
     token arrays (by default: one for each sequence), gets no tokens, and check_status(workspace) raises ERR_RANGE.
     lens_out: may be lens; without it lens stays as it is.  commit=False leaves the pool's counts as they are: what
     the step would be.  Returns a KVPlan."""
+    r = (_fast_module or _fast()).plan(pool, table, lens, add, done, tokens, lens_out, positions, slots, commit, workspace)
+    if r is not None:
+        return _check(r) if r.__class__ is int else KVPlan(*r[:5], table, r[5])
     torch = _torch()
     if table.dim() != 2 or lens.dim() != 1 or table.shape[0] != lens.shape[0]:
         _bad("lens [seqs] and table [seqs, width]")
@@ -840,6 +847,9 @@ def residual_norm(y, h, pre_norm=None, post_norm=None, gate=None, scale: float =
         h_out = residual_scale * h + scale * gate * u       (gate [1 or T, 1 or H]; None: 1)
         x = rmsnorm(h_out) * pre_norm         (pre_norm [H]; None: no x)
     Rows may be strided.  h_out may be h or y, x may be y.  Returns (h_out, x)."""
+    r = (_fast_module or _fast()).residual(y, h, pre_norm, post_norm, gate, scale, residual_scale, eps, h_out, x)
+    if r is not None:
+        return _check(r) if r.__class__ is int else r
     torch = _torch()
     codes = {torch.bfloat16: 0, torch.float16: 1}
     if y.dtype not in codes:

@@ -1,6 +1,6 @@
 /*
  * mc_bind.c -- argument marshalling of the calls that a decode step makes many times a
- * second (kv_append, attn_decode, attn_prefill and their 4-bit forms), as a CPython extension: what the binding
+ * second (kv_append, attn_decode, attn_prefill, their 4-bit forms, kv4_read, kv_plan, residual_norm), as a CPython extension: what the binding
  * does in Python with ctypes costs 6 to 8 us a call, several times such a call's kernels.
  *
  * It takes the plain cases only.  Whatever is not as it should be (a shape, a stride, a type,
@@ -20,8 +20,15 @@ typedef int (*attn_fn)(const mc_kv_cache *, const mc_kv_batch *, const void *, i
 
 static append_fn c_append[2]; /* to the 16-bit cache, to the 4-bit one */
 static attn_fn c_attn[4];     /* decode, prefill; over the 4-bit cache */
-static PyObject *t_empty, *t_stream, *t_device, *t_float32, *t_int32, *t_uint8;
-static PyObject *n_shape, *n_stride, *n_dtype, *n_device, *n_get_device, *n_data_ptr, *n_is_contiguous, *n_ref, *n_index,
+typedef int (*read_fn)(const mc_kv_cache *, const mc_kv_batch *, void *, void *, void *, void *);
+typedef int (*plan_fn)(const mc_kv_pool *, const int32_t *, const int32_t *, const uint8_t *, int, int, int32_t *, int, int32_t *, int32_t *,
+                       int32_t *, int64_t *, int64_t *, void *, size_t, void *);
+typedef int (*residual_fn)(const mc_residual_norm_args *, void *);
+static read_fn c_read;
+static plan_fn c_plan;
+static residual_fn c_residual;
+static PyObject *t_empty, *t_stream, *t_device, *t_float32, *t_int32, *t_uint8, *t_int64, *t_bf16, *t_fp16;
+static PyObject *n_state, *n_shape, *n_stride, *n_dtype, *n_device, *n_get_device, *n_data_ptr, *n_is_contiguous, *n_ref, *n_index,
     *kw_empty;
 
 /* a call without arguments, as an integer; -1 and an error set on failure */
@@ -261,20 +268,244 @@ static PyObject *attention(PyObject *self, PyObject *const *a, Py_ssize_t na)
     return both;
 }
 
-/* setup(append, decode, prefill, append4, decode4, prefill4, empty, raw_stream, current_device, float32, int32, uint8) */
+/* kv4_read(cache, batch, k, v, workspace) */
+static PyObject *kv4_read(PyObject *self, PyObject *const *a, Py_ssize_t na)
+{
+    (void)self;
+    Call c = {0};
+    if (na != 5 || !begin(&c, a[0], a[1]) || c.batch->tokens < 1) return leave(&c);
+    int64_t n[1];
+    const void *ws = NULL;
+    if (!side(&c, a[4], t_uint8, 1, n, &ws) || (a[4] != Py_None && n[0] < 256)) return leave(&c);
+    const int64_t st = stream_of(&c);
+    if (st < 0 || PyErr_Occurred()) return leave(&c);
+    PyObject *out[2] = {NULL, NULL};
+    for (int i = 0; i < 2; ++i) {
+        int got;
+        int64_t os;
+        if (a[2 + i] == Py_None) {
+            out[i] = empty3(&c, c.batch->tokens, c.cache->kv_heads, c.cache->head_dim, c.dtype);
+        } else if (rows(&c, a[2 + i], c.cache->kv_heads, &got, &os) && is_true(a[2 + i], n_is_contiguous)) {
+            out[i] = a[2 + i];
+            Py_INCREF(out[i]);
+        }
+        if (!out[i]) {
+            Py_XDECREF(out[0]);
+            return leave(&c);
+        }
+    }
+    void *k = ptr_of(out[0]), *v = ptr_of(out[1]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c_read(c.cache, c.batch, k, v, (void *)ws, (void *)(intptr_t)st);
+    Py_END_ALLOW_THREADS
+    end(&c);
+    PyObject *both = rc ? PyLong_FromLong(rc) : PyTuple_Pack(2, out[0], out[1]);
+    Py_DECREF(out[0]);
+    Py_DECREF(out[1]);
+    return both;
+}
+
+/* Sizes and strides of a tensor of `dims` dimensions and this type on device `index`; 0: not a plain case. */
+static int tensor(PyObject *t, PyObject *dtype, int64_t index, int dims, int64_t *n, int64_t *s)
+{
+    int ok = 0;
+    PyObject *sh = PyObject_GetAttr(t, n_shape), *st = NULL, *dt = NULL;
+    if (sh && PyTuple_Check(sh) && PyTuple_GET_SIZE(sh) == dims && (st = PyObject_CallMethodNoArgs(t, n_stride)) && PyTuple_Check(st) &&
+        (dt = PyObject_GetAttr(t, n_dtype)) && dt == dtype) {
+        for (int i = 0; i < dims; ++i) {
+            n[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, i));
+            s[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st, i));
+        }
+        ok = int_of(t, n_get_device) == index;
+    }
+    Py_XDECREF(sh);
+    Py_XDECREF(st);
+    Py_XDECREF(dt);
+    return ok && !PyErr_Occurred();
+}
+
+/* n contiguous elements */
+static int vec(PyObject *t, PyObject *dtype, int64_t index, int64_t n)
+{
+    int64_t got, s;
+    return tensor(t, dtype, index, 1, &got, &s) && got == n && (s == 1 || n < 2);
+}
+
+/* a new tensor of one or two (b > 0) dimensions */
+static PyObject *empty(int64_t a, int64_t b, PyObject *dtype, PyObject *device)
+{
+    PyObject *shape = b > 0 ? Py_BuildValue("(LL)", (long long)a, (long long)b) : Py_BuildValue("(L)", (long long)a);
+    if (!shape) return NULL;
+    PyObject *args[3] = {shape, dtype, device};
+    PyObject *r = PyObject_Vectorcall(t_empty, args, 1, kw_empty);
+    Py_DECREF(shape);
+    return r;
+}
+
+/* torch's current stream if device `index` is the current one; -1 otherwise (stream_of) */
+static int64_t stream_on(int64_t index)
+{
+    Call c = {0};
+    c.index = index;
+    return index < 0 ? -1 : stream_of(&c);
+}
+
+static PyObject *not_plain(PyObject **owned, int count)
+{
+    for (int i = 0; i < count; ++i) Py_XDECREF(owned[i]);
+    PyErr_Clear();
+    Py_RETURN_NONE;
+}
+
+/* plan(pool, table, lens, add, done, tokens, lens_out, positions, slots, commit, workspace):
+ * (lens_out, cu_q, positions, slots, state, tokens) */
+static PyObject *plan(PyObject *self, PyObject *const *a, Py_ssize_t na)
+{
+    (void)self;
+    enum { kLens, kCu, kPos, kSlots, kState, kDevice, kOwned };
+    PyObject *o[kOwned] = {0};
+    if (na != 11 || a[10] == Py_None) return not_plain(o, kOwned);
+    const mc_kv_pool *pool = (const mc_kv_pool *)(uintptr_t)attr_int(a[0], n_ref);
+    const int64_t index = attr_int(a[0], n_index);
+    int64_t n[2], s[2], wn, wst;
+    if (PyErr_Occurred() || !tensor(a[1], t_int32, index, 2, n, s)) return not_plain(o, kOwned);
+    const int64_t seqs = n[0], width = n[1];
+    if (seqs < 1 || seqs > 0x7fffffff || width < 1 || width > 0x7fffffff || (s[1] != 1 && width > 1) || (s[0] != width && seqs > 1)) return not_plain(o, kOwned);
+    if (!vec(a[2], t_int32, index, seqs) || !vec(a[3], t_int32, index, seqs)) return not_plain(o, kOwned);
+    if (a[4] != Py_None && !vec(a[4], t_uint8, index, seqs)) return not_plain(o, kOwned);
+    if (a[6] != Py_None && !vec(a[6], t_int32, index, seqs)) return not_plain(o, kOwned);
+    if (!tensor(a[10], t_uint8, index, 1, &wn, &wst) || wst != 1 || wn < 256) return not_plain(o, kOwned);
+    const int64_t tokens = a[5] == Py_None ? seqs : PyLong_AsLongLong(a[5]);
+    const int positions = PyObject_IsTrue(a[7]), slots = PyObject_IsTrue(a[8]), commit = PyObject_IsTrue(a[9]);
+    if (PyErr_Occurred() || tokens < 0 || tokens > 0x7fffffff) return not_plain(o, kOwned);
+    const int64_t st = stream_on(index);
+    if (st < 0) return not_plain(o, kOwned);
+    o[kDevice] = PyObject_GetAttr(a[0], n_device);
+    if (!o[kDevice]) return not_plain(o, kOwned);
+    if (a[6] != Py_None) {
+        o[kLens] = a[6];
+        Py_INCREF(a[6]);
+    } else {
+        o[kLens] = empty(seqs, 0, t_int32, o[kDevice]);
+    }
+    o[kCu] = empty(seqs + 1, 0, t_int32, o[kDevice]);
+    if (positions) o[kPos] = empty(tokens, 0, t_int32, o[kDevice]);
+    else o[kPos] = Py_None, Py_INCREF(Py_None);
+    if (slots) o[kSlots] = empty(tokens, 0, t_int64, o[kDevice]);
+    else o[kSlots] = Py_None, Py_INCREF(Py_None);
+    o[kState] = commit ? PyObject_GetAttr(a[0], n_state) : empty(2, 0, t_int64, o[kDevice]);
+    for (int i = 0; i < kOwned; ++i)
+        if (!o[i]) return not_plain(o, kOwned);
+    const void *table = ptr_of(a[1]), *lens = ptr_of(a[2]), *add = ptr_of(a[3]), *done = a[4] == Py_None ? NULL : ptr_of(a[4]), *ws = ptr_of(a[10]);
+    void *lo = ptr_of(o[kLens]), *cu = ptr_of(o[kCu]), *po = positions ? ptr_of(o[kPos]) : NULL, *sl = slots ? ptr_of(o[kSlots]) : NULL,
+         *so = ptr_of(o[kState]);
+    if (PyErr_Occurred()) return not_plain(o, kOwned);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c_plan(pool, lens, add, done, (int)seqs, (int)tokens, (int32_t *)table, (int)width, lo, cu, po, sl, so, (void *)ws, (size_t)wn,
+                (void *)(intptr_t)st);
+    Py_END_ALLOW_THREADS
+    PyObject *r = rc ? PyLong_FromLong(rc) : Py_BuildValue("(OOOOOL)", o[kLens], o[kCu], o[kPos], o[kSlots], o[kState], (long long)tokens);
+    for (int i = 0; i < kOwned; ++i) Py_DECREF(o[i]);
+    return r;
+}
+
+/* residual(y, h, pre_norm, post_norm, gate, scale, residual_scale, eps, h_out, x): (h_out, x) */
+static PyObject *residual(PyObject *self, PyObject *const *a, Py_ssize_t na)
+{
+    (void)self;
+    enum { kType, kDevice, kHOut, kX, kOwned };
+    PyObject *o[kOwned] = {0};
+    if (na != 10) return not_plain(o, kOwned);
+    mc_residual_norm_args r = {0};
+    int64_t n[2], s[2], gn[2], gs[2], hs[2];
+    o[kType] = PyObject_GetAttr(a[0], n_dtype);
+    if (!o[kType] || (o[kType] != t_bf16 && o[kType] != t_fp16)) return not_plain(o, kOwned);
+    const int64_t index = int_of(a[0], n_get_device);
+    if (!tensor(a[0], o[kType], index, 2, n, s) || n[0] < 1 || n[0] > 0x7fffffff || n[1] < 1 || n[1] > 65536) return not_plain(o, kOwned);
+    const int64_t T = n[0], H = n[1];
+    /* rows of [T, H]: their stride, or 0 */
+#define ROWS(t, stride) \
+    (tensor(t, o[kType], index, 2, gn, gs) && gn[0] == T && gn[1] == H && (gs[1] == 1 || H == 1) && ((stride) = T > 1 ? gs[0] : H, 1))
+    if (s[1] != 1 && H > 1) return not_plain(o, kOwned);
+    r.y_stride = T > 1 ? s[0] : H;
+    if (!ROWS(a[1], hs[0])) return not_plain(o, kOwned);
+    r.h_stride = hs[0];
+    for (int i = 2; i < 4; ++i)
+        if (a[i] != Py_None && !vec(a[i], o[kType], index, H)) return not_plain(o, kOwned);
+    if (a[4] != Py_None) {
+        if (!tensor(a[4], o[kType], index, 2, gn, gs) || (gn[0] != 1 && gn[0] != T) || (gn[1] != 1 && gn[1] != H)) return not_plain(o, kOwned);
+        r.gate_row = gn[0] > 1 ? gs[0] : 0;
+        r.gate_col = gn[1] > 1 ? (int32_t)gs[1] : 0;
+        if (gn[1] > 1 && gs[1] != 1) return not_plain(o, kOwned);
+        r.gate = ptr_of(a[4]);
+    }
+    r.scale = (float)PyFloat_AsDouble(a[5]);
+    r.residual_scale = (float)PyFloat_AsDouble(a[6]);
+    r.eps = (float)PyFloat_AsDouble(a[7]);
+    const int64_t st = stream_on(index);
+    if (st < 0 || PyErr_Occurred()) return not_plain(o, kOwned);
+    r.h_out_stride = r.x_stride = H;
+    if ((a[8] == Py_None || a[9] == Py_None) && !(o[kDevice] = PyObject_GetAttr(a[0], n_device))) return not_plain(o, kOwned);
+    if (a[8] == Py_None) {
+        o[kHOut] = empty(T, H, o[kType], o[kDevice]);
+    } else {
+        if (!ROWS(a[8], r.h_out_stride)) return not_plain(o, kOwned);
+        o[kHOut] = a[8];
+        Py_INCREF(a[8]);
+    }
+    if (a[2] == Py_None) {
+        o[kX] = Py_None;
+        Py_INCREF(Py_None);
+    } else if (a[9] == Py_None) {
+        o[kX] = empty(T, H, o[kType], o[kDevice]);
+    } else {
+        if (!ROWS(a[9], r.x_stride)) return not_plain(o, kOwned);
+        o[kX] = a[9];
+        Py_INCREF(a[9]);
+    }
+#undef ROWS
+    if (!o[kHOut] || !o[kX]) return not_plain(o, kOwned);
+    r.T = (int32_t)T;
+    r.H = (int32_t)H;
+    r.dtype = o[kType] == t_bf16 ? MC_BF16 : MC_FP16;
+    r.y = ptr_of(a[0]);
+    r.h = ptr_of(a[1]);
+    r.pre_norm = a[2] == Py_None ? NULL : ptr_of(a[2]);
+    r.post_norm = a[3] == Py_None ? NULL : ptr_of(a[3]);
+    r.h_out = ptr_of(o[kHOut]);
+    r.x = o[kX] == Py_None ? NULL : ptr_of(o[kX]);
+    if (PyErr_Occurred()) return not_plain(o, kOwned);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c_residual(&r, (void *)(intptr_t)st);
+    Py_END_ALLOW_THREADS
+    PyObject *both = rc ? PyLong_FromLong(rc) : PyTuple_Pack(2, o[kHOut], o[kX]);
+    for (int i = 0; i < kOwned; ++i) Py_XDECREF(o[i]);
+    return both;
+}
+
+/* setup(append, decode, prefill, append4, decode4, prefill4, read, plan, residual, empty, raw_stream, current_device, float32, int32, uint8, int64, bfloat16,
+ * float16) */
 static PyObject *setup(PyObject *self, PyObject *args)
 {
     (void)self;
-    unsigned long long f[6];
-    PyObject *o[6];
-    if (!PyArg_ParseTuple(args, "KKKKKKOOOOOO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &o[0], &o[1], &o[2], &o[3], &o[4], &o[5])) return NULL;
+    unsigned long long f[9];
+    PyObject *o[9];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOOOOO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &o[0], &o[1], &o[2], &o[3],
+                          &o[4], &o[5], &o[6], &o[7], &o[8]))
+        return NULL;
     for (int i = 0; i < 2; ++i) {
         c_append[i] = (append_fn)(uintptr_t)f[3 * i];
         c_attn[2 * i] = (attn_fn)(uintptr_t)f[3 * i + 1];
         c_attn[2 * i + 1] = (attn_fn)(uintptr_t)f[3 * i + 2];
     }
-    PyObject **to[6] = {&t_empty, &t_stream, &t_device, &t_float32, &t_int32, &t_uint8};
-    for (int i = 0; i < 6; ++i) {
+    c_read = (read_fn)(uintptr_t)f[6];
+    c_plan = (plan_fn)(uintptr_t)f[7];
+    c_residual = (residual_fn)(uintptr_t)f[8];
+    PyObject **to[9] = {&t_empty, &t_stream, &t_device, &t_float32, &t_int32, &t_uint8, &t_int64, &t_bf16, &t_fp16};
+    for (int i = 0; i < 9; ++i) {
         Py_INCREF(o[i]);
         Py_XSETREF(*to[i], o[i]);
     }
@@ -284,6 +515,9 @@ static PyObject *setup(PyObject *self, PyObject *args)
 static PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, "entry points and torch's parts"},
                                 {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, ""},
                                 {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, ""},
+                                {"kv4_read", (PyCFunction)(void (*)(void))kv4_read, METH_FASTCALL, ""},
+                                {"plan", (PyCFunction)(void (*)(void))plan, METH_FASTCALL, ""},
+                                {"residual", (PyCFunction)(void (*)(void))residual, METH_FASTCALL, ""},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mcbind", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -293,7 +527,7 @@ PyMODINIT_FUNC PyInit__mcbind(void)
         PyObject **to;
         const char *name;
     } names[] = {{&n_shape, "shape"}, {&n_stride, "stride"}, {&n_dtype, "dtype"}, {&n_device, "device"}, {&n_get_device, "get_device"},
-                 {&n_data_ptr, "data_ptr"}, {&n_is_contiguous, "is_contiguous"}, {&n_ref, "_ref"}, {&n_index, "index"}};
+                 {&n_data_ptr, "data_ptr"}, {&n_is_contiguous, "is_contiguous"}, {&n_ref, "_ref"}, {&n_index, "index"}, {&n_state, "state"}};
     for (size_t i = 0; i < sizeof names / sizeof names[0]; ++i)
         if (!(*names[i].to = PyUnicode_InternFromString(names[i].name))) return NULL;
     if (!(kw_empty = Py_BuildValue("(ss)", "dtype", "device"))) return NULL;
