@@ -407,8 +407,10 @@ int mc_attn_prefill(const mc_kv_cache *cache, const mc_kv_batch *batch, const vo
 /* Bytes of (page, head): page_size * 17 * head_dim / 32; 0 for sizes that are refused. */
 size_t mc_kv4_block_size(int page_size, int head_dim);
 
-/* Workspace bytes of the attn4 calls (as mc_attn_workspace_size). */
-size_t mc_attn4_workspace_size(const mc_kv_cache *cache, int q_heads);
+/* Workspace bytes of the attn4 calls (as mc_attn_workspace_size), the status word first.  With `prompts`, 256 MiB
+ * more, in which a call unpacks the keys of long prompts once, where the pages that its tables have room for fit
+ * there in 16 bits.  A call takes either size, and has the same results up to the order of its sums. */
+size_t mc_attn4_workspace_size(const mc_kv_cache *cache, int q_heads, int prompts);
 
 /* As mc_kv_append; a key's or value's row is rounded to dtype, then stored on its groups' grids. */
 int mc_kv4_append(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, const void *k,
@@ -512,7 +514,7 @@ int mc_check_status(void *workspace, void *stream);
  * counts of kernel ids 0 .. n-1 (names from mc_profile_name: route, permute,
  * gemv_w13, gemv_w2, combine, frag_x, gemm_w13, gemm_w2, rmsnorm, importance,
  * x_img, kv_append, attn_decode, attn_prefill, attn_join, kv_read, kv_plan,
- * residual_norm) and
+ * kv_unpack, residual_norm) and
  * clears the records.  Inside stream capture the events become event nodes of
  * the graph: every replay records them again, and each mc_profile_read reports
  * the latest replay and keeps those records until mc_profile_clear. */

@@ -84,7 +84,7 @@ def load():
         "mc_attn_decode": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
         "mc_attn_prefill": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
         "mc_kv4_block_size": (Z, [I, I]),
-        "mc_attn4_workspace_size": (Z, [P, I]),
+        "mc_attn4_workspace_size": (Z, [P, I, I]),
         "mc_kv4_append": (I, [P, P, P, L, P, L, P, L, I, P, P, F32, P, I, I, I, P, P, P]),
         "mc_kv4_read": (I, [P, P, P, P, P, P]),
         "mc_attn4_decode": (I, [P, P, P, L, I, P, P, L, P, P, Z, P]),
@@ -583,10 +583,11 @@ def _attn_workspace(cache, n):
     return torch.zeros(n, dtype=torch.uint8, device=cache.device)
 
 
-def attn4_workspace(cache: KVCache4, q_heads: int):
-    """attn_workspace for the calls on a KVCache4."""
+def attn4_workspace(cache: KVCache4, q_heads: int, prompts: bool = True):
+    """attn_workspace for the calls on a KVCache4.  prompts: with the 256 MiB in which attn4_prefill
+    unpacks the keys of long prompts (without them, as without a workspace, it takes longer)."""
     _kind(cache, True)
-    return _attn_workspace(cache, load().mc_attn4_workspace_size(cache._ref, int(q_heads)))
+    return _attn_workspace(cache, load().mc_attn4_workspace_size(cache._ref, int(q_heads), 1 if prompts else 0))
 
 
 def _kind(cache, bits4):
@@ -658,7 +659,7 @@ def _attention(prefill, cache, batch, q, scale, softcap, window, slopes, prefix,
     else:
         os_ = _rows("out", out, cache, batch, heads)[1]
     if workspace is None:
-        workspace = (attn4_workspace if bits4 else attn_workspace)(cache, heads)
+        workspace = attn4_workspace(cache, heads, prompts=False) if bits4 else attn_workspace(cache, heads)
     ws = _status(workspace, cache)
     lse = empty((batch.tokens, heads), dtype=_torch().float32, device=dev) if with_lse else None
     if slopes is not None:
@@ -890,7 +891,7 @@ def residual_norm(y, h, pre_norm=None, post_norm=None, gate=None, scale: float =
 
 # -------------------------------------------------------------- profiling --
 
-N_KERNELS = 18
+N_KERNELS = 19
 
 
 def token_importance(t, attn, protect_frac: float = 0.02, importance=None, mask=None, with_mask: bool = True,

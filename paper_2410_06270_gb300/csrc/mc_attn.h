@@ -90,6 +90,14 @@ struct ReadParams {
     int32_t *status;
 };
 
+struct Unpack4Params {
+    KvView c;
+    BatchView b;
+    int window;
+    uint16_t *k, *v;  // pages of [kv_heads][page_size][head_dim]
+    int32_t *table, *status;
+};
+
 // Keys that a row of the page table has pages for.
 __device__ __forceinline__ int seq_room(const BatchView &bv, const KvView &c)
 {
@@ -328,6 +336,7 @@ __device__ __forceinline__ float capped(float y, float top)
 constexpr float kBelow = 7.f, kLazy = 15.f;
 
 int launch_append(AppendParams p, int head_dim, bool bf16, bool q4, cudaStream_t st);
+int launch_unpack4(const Unpack4Params &p, int head_dim, bool bf16, cudaStream_t st);
 int launch_read4(const ReadParams &p, int head_dim, bool bf16, cudaStream_t st);
 
 constexpr int kAttnMaxSms = 160;  // SMs that the workspace has room for (the GB300's 152)

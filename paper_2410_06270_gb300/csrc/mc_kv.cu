@@ -266,6 +266,70 @@ int launch_read4(const ReadParams &p, int head_dim, bool bf16, cudaStream_t st)
     return MC_OK;
 }
 
+// The keys that a batch's new tokens see, as 16-bit pages of sequence after sequence (page i of sequence b at
+// b * table_width + i, which is also what the table written here says): what attention of prompts reads, so that a key
+// is unpacked once and not for every 256 rows that see it.  A block takes 64 keys of a head, a thread
+// a 16-byte chunk of codes of a key and of a value.  Bound by the writes, 4 D bytes a key (they stay in L2 for the
+// attention as far as they fit): 8192 keys of 8 heads of 128, 33 MB, 9 us.
+constexpr int kUnpackKeys = 64;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kUnpackKeys * D / 32) unpack4_kernel(const Unpack4Params p)
+{
+    constexpr int kChunks = D / 32, kGroups = D / kKv4Group;  // 16-byte chunks of a row's codes
+    pdl_trigger();
+    pdl_wait();
+    const int b = blockIdx.z, h = blockIdx.y, row = threadIdx.x / kChunks, ch = threadIdx.x % kChunks;
+    const int j = blockIdx.x * kUnpackKeys + row;
+    if (h == 0)
+        for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < p.b.table_width; i += gridDim.x * blockDim.x)
+            p.table[(int64_t)b * p.b.table_width + i] = b * p.b.table_width + i;
+    int first;
+    const int n = seq_rows(p.b, b, first, p.status), len = seq_len(p.b, p.c, b, p.status);
+    const int seen = p.window ? max(0, len - n - p.window + 1) : 0;
+    if (n == 0 || j >= len || j < (seen & ~127)) return;
+    int r;
+    const int i = p.c.page.div(j, r), page = j < seen ? -1 : seq_page(p.b, p.c, b, i, p.status);
+    const int64_t to = (((int64_t)b * p.b.table_width + i) * p.c.kv_heads + h) * p.c.page_size * D + (int64_t)r * D;
+    uint4 codes[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    uint32_t words[2] = {0, 0};  // (no such page, or behind the window: zeros)
+    if (page >= 0) {
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const uint8_t *block = kv4_block<D>(p.c, side ? p.c.v : p.c.k, page, h);
+            codes[side] = __ldg(reinterpret_cast<const uint4 *>(block + r * kv4_code_bytes(D)) + ch);
+            const uint8_t *w = block + p.c.page_size * kv4_code_bytes(D) + r * kv4_word_bytes(D);
+            words[side] = D == 128 ? __ldg(reinterpret_cast<const uint32_t *>(w)) : __ldg(reinterpret_cast<const uint16_t *>(w));
+        }
+    }
+    using P = Kv4Pairs<BF16>;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        uint16_t *out = (side ? p.v : p.k) + to;
+        const uint32_t w[4] = {codes[side].x, codes[side].y, codes[side].z, codes[side].w};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int at = 4 * ch + x, g = at % kGroups;  // word at / kGroups of group g
+            const uint32_t z = P::zeros(words[side] >> (16 * g)), sc = P::scales(words[side] >> (16 * g));
+            *reinterpret_cast<uint4 *>(out + 64 * g + 8 * (at / kGroups)) =
+                make_uint4(P::mul(P::sub(P::magic(w[x], 0), z), sc), P::mul(P::sub(P::magic(w[x], 1), z), sc),
+                           P::mul(P::sub(P::magic(w[x], 2), z), sc), P::mul(P::sub(P::magic(w[x], 3), z), sc));
+        }
+    }
+}
+
+int launch_unpack4(const Unpack4Params &p, int head_dim, bool bf16, cudaStream_t st)
+{
+    const int64_t room = (int64_t)p.b.table_width * p.c.page_size;
+    const dim3 grid((unsigned)((room + kUnpackKeys - 1) / kUnpackKeys), p.c.kv_heads, p.b.seqs);
+    auto k = head_dim == 64 ? (bf16 ? unpack4_kernel<64, true> : unpack4_kernel<64, false>)
+                            : (bf16 ? unpack4_kernel<128, true> : unpack4_kernel<128, false>);
+    profile_begin(kKUnpack, st);
+    cudaError_t e = launch_k(k, grid, dim3(kUnpackKeys * head_dim / 32), 0, st, p);
+    profile_end(kKUnpack, st);
+    if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "unpack launch: %s", cudaGetErrorString(e));
+    return MC_OK;
+}
+
 template <bool Q4>
 static auto append_of(int head_dim, bool bf16)
 {

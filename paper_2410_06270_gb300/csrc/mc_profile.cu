@@ -21,7 +21,7 @@ std::vector<cudaEvent_t> g_pool;
 cudaEvent_t g_pending[kKCount];
 const char *g_names[kKCount] = {"route", "permute", "gemv_w13", "gemv_w2", "combine",
                                 "frag_x", "gemm_w13", "gemm_w2", "rmsnorm", "importance", "x_img", "kv_append", "attn_decode",
-                                "attn_prefill", "attn_join", "kv_read", "kv_plan", "residual_norm"};
+                                "attn_prefill", "attn_join", "kv_read", "kv_plan", "kv_unpack", "residual_norm"};
 
 // An event record on st; inside stream capture it becomes an event node of the
 // graph, so every replay of the graph records it again.

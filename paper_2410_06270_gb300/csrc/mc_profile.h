@@ -23,6 +23,7 @@ enum KernelId {
     kKAttnJoin,   // partial results of items split over the cache's length
     kKRead,       // rows of the 4-bit cache in 16 bits
     kKPlan,       // pages and slots of a step
+    kKUnpack,     // keys of the 4-bit cache in 16 bits for a call
     kKResidual,   // norms, gate and residual sum between blocks
     kKCount
 };

@@ -13,8 +13,9 @@ import kv4_ref as ref4  # noqa: E402
 pytestmark = pytest.mark.gpu
 
 
-@pytest.fixture(scope="module")
-def mc():
+@pytest.fixture(scope="module", params=["room for prompts", "no room"])
+def mc(request):
+    """Every test with a workspace in which long prompts' keys are unpacked, and with one without."""
     if not torch.cuda.is_available():
         pytest.skip("no CUDA device")
     from paper_2410_06270_gb300 import build
@@ -22,7 +23,11 @@ def mc():
     import paper_2410_06270_gb300 as m
     m.load()
     m.set_debug(0, 1_000_000_000)
-    return m
+    patch = pytest.MonkeyPatch()
+    whole = m.attn4_workspace
+    patch.setattr(m, "attn4_workspace", lambda cache, heads, prompts=request.param == "room for prompts": whole(cache, heads, prompts))
+    yield m
+    patch.undo()
 
 
 EDGES = [0, 1, 2, 15, 16, 17, 31, 63, 64, 65, 100, 127, 128, 129, 255, 257, 700]
@@ -340,6 +345,60 @@ def test_prefill_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap
     ref.assert_attention(got, lse, want, dtype, 1025, 5.0, rows=slice(0, n))
 
 
+@pytest.mark.parametrize("heads,kv,dim,dtype,page,softcap,window,bias,prefix,nan", [
+    (32, 2, 128, "bf16", 16, 0.0, 0, False, False, False),
+    (24, 1, 64, "fp16", 48, 0.0, 0, False, True, False),
+    (20, 1, 128, "fp16", 64, 30.0, 0, True, False, False),
+    (40, 2, 64, "bf16", 32, 0.0, 50, False, False, True),
+    (17, 1, 128, "bf16", 128, 50.0, 129, True, True, False),
+    (32, 2, 128, "bf16", 16, 0.0, 0, False, False, True),
+    (20, 1, 64, "fp16", 16, 20.0, 100, False, False, False),
+])
+def test_prompts_of_many_rows(mc, heads, kv, dim, dtype, page, softcap, window, bias, prefix, nan):
+    """More than 1024 rows a sequence, which is where a workspace with room for prompts has their keys unpacked
+    first: strided queries and outputs, more new tokens than the length, sequences without tokens or keys, hidden groups of
+    NaN, pages that a window has left behind; and again over what the call before left in the workspace."""
+    lens, new, pre = [0, 3, 130, 300, 511, 9, 700, 64], [2, 3, 130, 1, 129, 12, 400, 0], [0, 1, 64, 70, 299, 4, 650, 64]
+    B = ref.Batch(lens, new, kv, page, dim, dtype, 6, pad_tokens=2)
+    assert -(-B.tokens // len(lens)) * (heads // kv) > 1024
+    if nan:
+        for b, length in enumerate(lens):
+            if new[b] > 1 and length:
+                B.v[B.table[b, (length - 1) // page], :, (length - 1) % page, 3] = float("nan")
+    blocks = ref4.fast_blocks(B)
+    wide = 1.5 * B.randn(B.tokens, heads * dim + 8)
+    q = wide[:, 8:].unflatten(1, (heads, dim))
+    sl = _slopes(heads) if bias else None
+    pre = pre if prefix else None
+    want = ref.attention(B, q, dim ** -0.5, softcap, window, sl, pre)
+    if window:
+        for b, (n, length) in enumerate(zip(new, lens)):
+            gone = max(0, length - n - window + 1) // page
+            for p in blocks.pools:
+                p[B.table[b, :gone].long()] = 0xff
+            B.table[b, :gone] = -1
+    cache, batch = blocks.device(mc, interleave=True)
+    ws = mc.attn4_workspace(cache, heads)
+    ws[256 + (1 << 20):] = 0xff  # (what a call leaves there is any bits)
+    dev = wide.cuda()[:, 8:].unflatten(1, (heads, dim))
+    for _ in range(2):
+        buf = torch.full((B.tokens, heads * dim + 8), 3.0, dtype=ref.DT[dtype], device="cuda")
+        got, lse = mc.attn4_prefill(cache, batch, dev, softcap=softcap, window=window, slopes=None if sl is None else sl.cuda(),
+                                    prefix=None if pre is None else _i32(pre), out=buf[:, :heads * dim].unflatten(1, (heads, dim)),
+                                    with_lse=True, workspace=ws)
+        mc.check_status(ws)
+        n = B.cu[-1]
+        assert (buf[:, heads * dim:] == 3).all() and (buf[n:] == 3).all()
+        if nan:
+            assert torch.equal(torch.isnan(got[:n].cpu()), torch.isnan(want[0][:n]))
+            seen = torch.isnan(want[0][:n]).flatten(1).any(1).nonzero().flatten().tolist()
+            assert seen
+            rows = [t for t in range(n) if t not in seen]
+        else:
+            rows = slice(0, n)
+        ref.assert_attention(got, lse, want, dtype, 700, 5.0, rows=rows)
+
+
 @pytest.mark.parametrize("new,length,kv,heads,dim", [(1, 4000, 1, 4, 128), (5, 9000, 1, 5, 128), (40, 6000, 2, 4, 64), (700, 700, 1, 1, 128),
                                                      (515, 2100, 2, 6, 128), (1, 1, 1, 1, 64)])
 def test_prefill_splits_and_joins(mc, new, length, kv, heads, dim):
@@ -493,11 +552,11 @@ def test_queries_and_outputs_with_a_token_stride(mc, new, heads, kv, dim, dtype)
 
 
 @pytest.mark.parametrize("cap", [0.0, 20.0])
-@pytest.mark.parametrize("new", [[1, 1, 1], [2, 1, 3], [50, 70, 130]])  # one, few and many rows
-def test_pages_lengths_and_boundaries_that_are_not_sound(mc, new, cap):
+@pytest.mark.parametrize("new,heads", [([1, 1, 1], 8), ([2, 1, 3], 8), ([50, 70, 130], 8), ([50, 70, 130], 40)])  # one, few and many rows
+def test_pages_lengths_and_boundaries_that_are_not_sound(mc, new, heads, cap):
     """A page outside the pool reads as zeros, a length is cut to the table's rows, a sequence whose
     boundaries are not sound has no tokens; each is recorded, and the other sequences are right."""
-    lens, heads, kv, dim = [96, 160, 144], 8, 2, 64
+    lens, kv, dim = [96, 160, 144], 2, 64
     ok = ref.Batch(lens, new, kv, 16, dim, "bf16", 109)
     blocks = ref4.fast_blocks(ok)
     q = ok.randn(ok.tokens, heads, dim)

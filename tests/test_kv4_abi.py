@@ -42,7 +42,7 @@ def test_bad_caches(mc, field, value, code):
     cache, batch = _cpu(mc)
     setattr(cache._c, field, value)
     lib, fake = mc.load(), 0x100000  # never dereferenced: every call below is refused
-    assert lib.mc_attn4_workspace_size(cache._ref, 4) == 0 and mc.last_error()
+    assert lib.mc_attn4_workspace_size(cache._ref, 4, 1) == 0 and mc.last_error()
     opts = mc._AttnOptsC(0.1, 0.0, 0, None, None)
     for fn in (lib.mc_attn4_decode, lib.mc_attn4_prefill):
         assert fn(cache._ref, batch._ref, fake, 256, 4, ctypes.addressof(opts), fake, 256, None, fake, 1 << 30, None) == code
@@ -84,7 +84,7 @@ def test_host_tensors_are_refused(mc):
     """Before anything is launched: the answer is an argument error, not a launch's."""
     cache, batch = _cpu(mc)
     q, kv = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 64, dtype=torch.bfloat16)
-    ws = torch.zeros(mc.load().mc_attn4_workspace_size(cache._ref, 4) + 256, dtype=torch.uint8)
+    ws = torch.zeros(mc.load().mc_attn4_workspace_size(cache._ref, 4, 0) + 256, dtype=torch.uint8)
     ws = ws[-ws.data_ptr() % 256:]
     for call in (lambda: mc.kv4_append(cache, batch, q, kv, kv), lambda: mc.kv4_read(cache, batch),
                  lambda: mc.attn4_decode(cache, batch, q, workspace=ws), lambda: mc.attn4_prefill(cache, batch, q, workspace=ws)):
@@ -98,8 +98,8 @@ def test_host_tensors_are_refused(mc):
 def test_bad_pointers(mc):
     cache, batch = _cpu(mc)
     lib, fake, odd = mc.load(), 0x100000, 0x100008
-    need = lib.mc_attn4_workspace_size(cache._ref, 4)
-    assert need > 0
+    need = lib.mc_attn4_workspace_size(cache._ref, 4, 0)
+    assert 0 < need == lib.mc_attn4_workspace_size(cache._ref, 4, 1) - (256 << 20)
 
     def attn(fn, q=fake, qs=256, heads=4, out=fake, os=256, lse=None, ws=fake, nbytes=need, scale=0.1, cap=0.0, window=0, prefix=None):
         opts = mc._AttnOptsC(scale, cap, window, None, prefix)
