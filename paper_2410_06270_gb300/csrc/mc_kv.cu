@@ -113,8 +113,14 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
     if (!is_q && at < 0) return;
     uint16_t *dst = is_q ? p.q_out + (int64_t)t * p.q_heads * D : Q4 ? nullptr : (is_v ? p.c.v : p.c.k) + at;
     const int64_t head_stride = is_q ? D : (int64_t)p.c.page_size * D;
+    constexpr int kGroups = D / kKv4Group;
+    const int block_bytes = p.c.page_size * kv4_row_bytes(D);
+    uint8_t *const block = Q4 && !is_q ? reinterpret_cast<uint8_t *>(is_v ? p.c.v : p.c.k) + at + (int64_t)h0 * block_bytes : nullptr;
+    uint8_t *const codes_at = block + at_row * kv4_code_bytes(D) + 4 * (li % 8 * kGroups + li / 8);
+    uint8_t *const words_at = block + p.c.page_size * kv4_code_bytes(D) + at_row * kv4_word_bytes(D) + 2 * (li / 8);
+    const bool grids = Q4 && !is_q;
     // a row of a key or value on its grids; the whole warp, with rows of heads past the last among them
-    auto store4 = [&](int h, const uint32_t (&v)[4]) {
+    auto store4 = [&](int i, const uint32_t (&v)[4]) {
         uint32_t x[4] = {v[0], v[1], v[2], v[3]}, word;
         if (rot && !p.interleaved) {
             uint16_t *own = rows_s[threadIdx.x >> 5] + lane / kLanes * D;
@@ -126,27 +132,21 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
             __syncwarp();
         }
         const uint32_t codes = kv4_quantise<BF16>(x, word);
-        if (h >= heads) return;
-        constexpr int kGroups = D / kKv4Group;
-        const int g = li / 8, i = li % 8;
-        uint8_t *block = reinterpret_cast<uint8_t *>(is_v ? p.c.v : p.c.k) + at + (int64_t)h * p.c.page_size * kv4_row_bytes(D);
-        *reinterpret_cast<uint32_t *>(block + at_row * kv4_code_bytes(D) + 4 * (i * kGroups + g)) = codes;
-        if (i == 0)
-            *reinterpret_cast<uint16_t *>(block + p.c.page_size * kv4_code_bytes(D) + at_row * kv4_word_bytes(D) + 2 * g) = (uint16_t)word;
+        if (h0 + i * kRows >= heads) return;
+        const int64_t off = (int64_t)i * kRows * block_bytes;
+        *reinterpret_cast<uint32_t *>(codes_at + off) = codes;
+        if (li % 8 == 0) *reinterpret_cast<uint16_t *>(words_at + off) = (uint16_t)word;
     };
-
     if ((!gain && !rot) || pos < 0) {  // copied, or zero
 #pragma unroll
         for (int i = 0; i < kAppendPasses; ++i) {
             const int h = h0 + i * kRows;
-            if (Q4 && !is_q) {
-                if (h - lane / kLanes >= heads) break;  // (for all lanes)
-                store4(h, {a[i].x, a[i].y, b[i].x, b[i].y});
-                continue;
+            if (grids) {
+                if (h - lane / kLanes < heads) store4(i, {a[i].x, a[i].y, b[i].x, b[i].y});  // (for all lanes)
+            } else if (h < heads) {
+                *reinterpret_cast<uint2 *>(dst + h * head_stride + ea) = pos < 0 ? make_uint2(0, 0) : a[i];
+                *reinterpret_cast<uint2 *>(dst + h * head_stride + eb) = pos < 0 ? make_uint2(0, 0) : b[i];
             }
-            if (h >= heads) continue;
-            *reinterpret_cast<uint2 *>(dst + h * head_stride + ea) = pos < 0 ? make_uint2(0, 0) : a[i];
-            *reinterpret_cast<uint2 *>(dst + h * head_stride + eb) = pos < 0 ? make_uint2(0, 0) : b[i];
         }
         return;
     }
@@ -208,8 +208,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
             unpair2(z, lo, hi);
             out[e] = pack2<BF16>(lo, hi);
         }
-        if (Q4 && !is_q) {
-            store4(h, out);
+        if (grids) {
+            store4(i, out);
         } else if (h < heads) {
             *reinterpret_cast<uint2 *>(dst + h * head_stride + ea) = make_uint2(out[0], out[1]);
             *reinterpret_cast<uint2 *>(dst + h * head_stride + eb) = make_uint2(out[2], out[3]);

@@ -35,6 +35,15 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
     return r;
 }
 
+// Codes held to z - most .. z + most, where more steps than `most` pass the type's largest number.
+template <bool BF16>
+__device__ __noinline__ uint32_t kv4_held(uint32_t codes, int z, int most)
+{
+    uint32_t r = 0;
+    for (int i = 0; i < 32; i += 4) r |= (uint32_t)max(z - most, min(z + most, (int)(codes >> i & 15))) << i;
+    return r;
+}
+
 // A group's 64 elements, 8 in each of 8 neighbouring lanes (x: pairs of them, in order): returns the lane's
 // word of codes, and the group's scale and zero point in `word`.  All 8 lanes take part.
 //
@@ -58,26 +67,24 @@ __device__ __forceinline__ uint32_t kv4_quantise(const uint32_t (&x)[4], uint32_
     ends = max2<BF16>(ends, 0u);
     const float2 e = unpack2<BF16>(ends);  // hi, -lo
     const uint32_t span = __float_as_uint(fmaf(e.x, 0.0625f, e.y * 0.0625f));
-    if (span >= 0x7f800000u) {  // infinite or NaN
-        word = 0x7ff0u;
-        return 0u;
-    }
+    const bool odd = span >= 0x7f800000u;  // infinite or NaN
     const uint32_t m = (span & 0x7fffffu) | 0x800000u, n = (16u * m + (15u << 20) - 1) / (15u << 20);
     uint32_t bits = span & 0x7f800000u;
     bits += n <= 16 ? (n - 8) << 20 : (1u << 23) + (1u << 20);
     bits = max(bits, kLeast);
     const float s = __uint_as_float(bits), inv = rcp(s);
-    const float z = floorf(fmaf(e.y, inv, 0.5f + kTie)), most = floorf(kMost * inv);
-    word = (bits >> 16) | (uint32_t)z;
-    const float base = kShift + z, end = kShift + fminf(15.f, z + most), start = kShift + fmaxf(0.f, z - most);
+    const float zs = fmaf(e.y, inv, kTie) + kShift, z = zs - kShift;  // (not negative, at most 15)
+    word = odd ? 0x7ff0u : (bits >> 16) | (__float_as_uint(zs) & 15u);
+    const float base = kShift + z;
     uint32_t r = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {  // (no quotient rounds below -z)
         const float2 f = unpack2<BF16>(x[i]);
-        const float a = fminf(fmaxf(fmaf(f.x, inv, kTie) + base, start), end), b = fminf(fmaxf(fmaf(f.y, inv, kTie) + base, start), end);
+        const float a = fminf(fmaf(f.x, inv, kTie) + base, kShift + 15.f), b = fminf(fmaf(f.y, inv, kTie) + base, kShift + 15.f);
         r += __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410) << (4 * i);
     }
-    return r;
+    if (kMost * inv < 16.f && !odd) r = kv4_held<BF16>(r, (int)z, (int)(kMost * inv));
+    return odd ? 0u : r;
 }
 
 // Elements 2 i and 2 i + 1 of a row.

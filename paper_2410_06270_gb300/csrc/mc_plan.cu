@@ -1,10 +1,14 @@
 // mc_plan.cu -- mc_kv_plan: pages, positions and slots of a step's new tokens, from the lengths.
 //
-// Per sequence three running sums decide everything (pages that come back, pages asked for, rows), so one
-// block goes over the sequences, a thread each, 1024 at a time; the tokens, of which there may be hundreds of
+// Per sequence three running sums decide everything (pages that come back, pages asked for, rows), so a block
+// goes over the sequences, a thread each, 1024 at a time; the tokens, of which there may be hundreds of
 // thousands, then find their sequence in the boundaries and write 12 bytes each.  A step of few tokens is
-// one launch: the block that made the sums does the tokens too, with the sums still in shared memory.  More are a
-// second launch of as many blocks as they fill.
+// one launch of one block, with the sums still in shared memory.  Others are two: the first has several blocks, which
+// all make the sums and each copy a part of the returned pages (its results go to the workspace, since lens and the
+// counts may be overwritten by the call), the second as many as the tokens fill.
+// Bound by latency: 250 sequences of one token, 23 of them finished with 2000 pages, TODO1 us, of which the launch, three
+// round trips to memory (lengths; pages returned and taken; slots) and the sums; 1000 sequences, 40 of them with
+// prompts of 82000 tokens, 90 finished with 17000 pages, TODO2 us.
 #include "mc_attn.h"
 #include "mc_host.h"
 #include "mc_profile.h"
@@ -12,8 +16,11 @@
 namespace mc {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanFew = 4096;      // tokens that the first block does itself
+constexpr int kPlanFew = 4096;      // tokens that one block does by itself
+constexpr int kPlanEntries = 1 << 16;  // and table entries that it may have to give back pages of
+constexpr int kPlanBlocks = 32;     // of the first of two launches
 constexpr int kPlanPer = 4;         // tokens a thread of the second launch
+constexpr int kPlanStaged = 4096;   // sequences whose boundaries it takes to shared memory
 
 struct PlanParams {
     int32_t *ring;
@@ -24,36 +31,39 @@ struct PlanParams {
     const uint8_t *done;
     int32_t *table, *lens_out, *cu_q, *positions;
     int64_t *slots, *state_out;
-    int32_t *status, *base;  // base: where a sequence's new pages stand in the ring (workspace)
-    int alone;               // the tokens are the first block's too
+    int32_t *status;
+    // workspace of two launches: where a sequence's new pages stand in the ring, its new length, the counts
+    int32_t *base, *length;
+    int64_t *counts;
+    int alone;  // one launch
 };
 
 // What the tokens of a sequence need.
 struct PlanSeq {
-    int first, length, held, base;  // row of its first new token, tokens before, their pages, place in the ring
+    int first, length, held, base, last;  // row of its first new token, tokens before, their pages, place in the ring, last page
 };
 
-__device__ __forceinline__ int64_t ring_at(int64_t i, int pages)
+__device__ __forceinline__ int ring_at(int64_t i, int pages) { return (int)((uint64_t)i % (uint32_t)pages); }
+
+// The k-th place after `base` (both below the ring's size where the counts are sound).
+__device__ __forceinline__ int ring_next(const PlanParams &p, int base, int k)
 {
-    return (int64_t)((uint64_t)i % (uint32_t)pages);
+    const int64_t i = (int64_t)base + k;
+    if (i < p.num_pages) return (int)i;
+    return i < 2 * (int64_t)p.num_pages ? (int)(i - p.num_pages) : ring_at(i, p.num_pages);
 }
 
-// Token t, the i-th of a sequence's new ones: its page, slot and position; the first row of a page also
-// enters the page into the table (new pages begin with a new token, since the last held one is filled first).
+// Row t of sequence b: position, page and slot.  Tokens before the first new page lie in the last one held, which
+// they fill; the first row of a page enters it into the table.
 __device__ __forceinline__ void plan_token(const PlanParams &p, int t, int b, const PlanSeq &s)
 {
     const int pos = s.length + (t - s.first);
     int row;
     const int i = p.page.div(pos, row);
-    int32_t *at = p.table + (int64_t)b * p.table_width + i;
-    int page;
+    int page = s.last;
     if (i >= s.held) {
-        int64_t k = (int64_t)s.base + (i - s.held);
-        if (k >= p.num_pages) k = ring_at(k, p.num_pages);
-        page = p.ring[k];
-        if (row == 0) *at = page;
-    } else {
-        page = *at;
+        page = p.ring[ring_next(p, s.base, i - s.held)];
+        if (row == 0) p.table[(int64_t)b * p.table_width + i] = page;
     }
     if (p.positions) p.positions[t] = pos;
     const bool in = (unsigned)page < (unsigned)p.num_pages;
@@ -74,52 +84,57 @@ __device__ __forceinline__ int pages_of(const PlanParams &p, int tokens)
     return n + (rest > 0);
 }
 
-// Inclusive sums over the block; `upto` comes back with them, the total is returned.
+// Sums of numbers that are not negative stop at 2^31 - 1, which is beyond every limit they are held against.
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
+
+// Inclusive sums over the block in place; totals in `total`.
 template <int N>
-__device__ __forceinline__ void block_sums(int64_t (&upto)[N], int64_t (&total)[N], int64_t (*part)[32])
+__device__ __forceinline__ void block_sums(uint32_t (&upto)[N], uint32_t (&total)[N], uint32_t (*part)[32])
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1)
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int64_t o = __shfl_up_sync(0xffffffffu, upto[k], d);
-            if (lane >= d) upto[k] += o;
+            const uint32_t o = __shfl_up_sync(0xffffffffu, upto[k], d);
+            if (lane >= d) upto[k] = plus(upto[k], o);
         }
-    __syncthreads();  // (the sums before these have been read)
     if (lane == 31)
 #pragma unroll
         for (int k = 0; k < N; ++k) part[k][warp] = upto[k];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const int64_t mine = part[k][lane];
-        int64_t sum = mine;
+        uint32_t sum = part[k][lane];
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int64_t o = __shfl_up_sync(0xffffffffu, sum, d);
-            if (lane >= d) sum += o;
+            const uint32_t o = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum = plus(sum, o);
         }
         total[k] = __shfl_sync(0xffffffffu, sum, 31);
-        upto[k] += __shfl_sync(0xffffffffu, sum - mine, warp);
+        const uint32_t before = __shfl_sync(0xffffffffu, sum, warp ? warp - 1 : 0);
+        if (warp) upto[k] = plus(upto[k], before);
     }
 }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
 {
-    __shared__ int64_t part[3][32];
-    __shared__ PlanSeq seq[kPlanThreads + 1];
+    __shared__ uint32_t part[4][32];
+    __shared__ PlanSeq seq[kPlanThreads];
+    __shared__ uint32_t given[kPlanThreads];  // pages returned by the sequences before (of this thousand)
     const int tid = threadIdx.x, lane = tid & 31;
     pdl_trigger();
     pdl_wait();
-    const int64_t taken = p.state[0], returned = p.state[1], free = returned - taken;
+    const int64_t taken = p.state[0], returned = p.state[1];
+    const uint32_t free = (uint32_t)max((int64_t)0, min(returned - taken, (int64_t)kMaxLen));
     const int64_t room = (int64_t)p.table_width * p.page_size, most = room < kMaxLen ? room : kMaxLen;
-    int64_t back0 = 0, need0 = 0, want0 = 0, took = 0;  // sums of the sequences before
+    uint32_t back0 = 0, need0 = 0, want0 = 0, took = 0;  // sums of the sequences before
     int rows0 = 0;
+    const bool writes = blockIdx.x == 0;
     for (int b0 = 0; b0 < p.seqs; b0 += kPlanThreads) {
         const int b = b0 + tid;
         const bool real = b < p.seqs;
-        int old = 0, n = 0;
+        int old = 0, n = 0, last = -1;
         bool over = false;
         if (real) {
             old = max(p.lens[b], 0);
@@ -129,61 +144,68 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
         const int back = over ? min(pages_of(p, old), p.table_width) : 0;
         const int length = over ? 0 : old, held = pages_of(p, length);
         const bool fits = n >= 0 && (int64_t)length + n <= most;
-        const int need = fits ? pages_of(p, length + n) - held : 0;
-        int64_t upto[3] = {back, need, fits ? n : 0}, total[3];
+        if (p.alone && fits && n && held && held * (int64_t)p.page_size != length) last = p.table[(int64_t)b * p.table_width + held - 1];
+        const uint32_t need = fits ? pages_of(p, length + n) - held : 0;
+        uint32_t upto[3] = {(uint32_t)back, need, fits ? (uint32_t)n : 0u}, total[3];
         block_sums<3>(upto, total, part);
-        const int64_t before = back0 + upto[0] - back, asked = need0 + upto[1];
-        const bool served = fits && (need == 0 || asked <= free) && (n == 0 || want0 + upto[2] <= p.tokens);
-        if (real && !served) set_status(p.status, MC_ERR_RANGE);
+        const uint32_t asked = plus(need0, upto[1]);
+        const bool served = fits && (need == 0 || asked <= free) && (n == 0 || plus(want0, upto[2]) <= (uint32_t)p.tokens);
         const int got = served ? n : 0;
-        int64_t rows[1] = {got}, all[1];
-        block_sums<1>(rows, all, part);
-        const PlanSeq s = {rows0 + (int)rows[0] - got, length, held, (int)ring_at(taken + asked - need, p.num_pages)};
+        uint32_t rows[1] = {(uint32_t)got}, all[1];
+        block_sums<1>(rows, all, part + 3);
+        const int first = rows0 + (int)rows[0] - got;
+        const int64_t at = taken + (asked - need);
+        const int base = at >= 0 && at < p.num_pages ? (int)at : ring_at(at, p.num_pages);
         if (real) {
-            p.lens_out[b] = length + got;
-            p.cu_q[b + 1] = s.first + got;
-            if (b == 0) p.cu_q[0] = 0;
-            if (p.alone) seq[tid] = s;
-            else p.base[b] = s.base;
-            if (served && need > 0) took = asked;
-        }
-        // a finished sequence's pages, by the warp; none overwrites a page that is still to be given out
-        unsigned gone = __ballot_sync(0xffffffffu, back > 0);
-        while (gone) {
-            const int l = __ffs(gone) - 1;
-            gone &= gone - 1;
-            const int count = __shfl_sync(0xffffffffu, back, l);
-            const int64_t first = returned + __shfl_sync(0xffffffffu, before, l);
-            const int32_t *row = p.table + (int64_t)__shfl_sync(0xffffffffu, b, l) * p.table_width;
-            for (int k = lane; k < count; k += 128) {
-                int32_t page[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) page[i] = k + 32 * i < count ? row[k + 32 * i] : 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (k + 32 * i >= count) break;
-                    if (first + k + 32 * i - taken < p.num_pages) p.ring[ring_at(first + k + 32 * i, p.num_pages)] = page[i];
-                    else set_status(p.status, MC_ERR_RANGE);
-                    if ((unsigned)page[i] >= (unsigned)p.num_pages) set_status(p.status, MC_ERR_RANGE);
-                }
+            seq[tid] = {first, length, held, base, last};
+            if (served && need) took = asked;
+            if (writes) {
+                if (!served) set_status(p.status, MC_ERR_RANGE);
+                p.cu_q[b + 1] = first + got;
+                if (b == 0) p.cu_q[0] = 0;
+                (p.alone ? p.lens_out : p.length)[b] = length + got;
+                if (!p.alone) p.base[b] = base;
             }
         }
-        back0 += total[0];
-        need0 += total[1];
-        want0 += total[2];
+        if (total[0]) {
+            // finished sequences' pages, end to end; none overwrites a page that is still to be given out
+            given[tid] = upto[0] - back;
+            __syncthreads();
+            const int count = min(kPlanThreads, p.seqs - b0);
+            const int ring0 = ring_at(returned + back0, p.num_pages);
+            for (int64_t f = (int64_t)blockIdx.x * kPlanThreads + tid; f < total[0]; f += (int64_t)gridDim.x * kPlanThreads) {
+                int lo = 0, hi = count;  // the last sequence whose pages start at f or before it
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (given[mid] <= f) lo = mid;
+                    else hi = mid;
+                }
+                const int page = p.table[(int64_t)(b0 + lo) * p.table_width + (f - given[lo])];
+                if (returned + back0 + f - taken < p.num_pages) p.ring[ring_next(p, ring0, (int)f)] = page;
+                else set_status(p.status, MC_ERR_RANGE);
+                if ((unsigned)page >= (unsigned)p.num_pages) set_status(p.status, MC_ERR_RANGE);
+            }
+        }
+        back0 = plus(back0, total[0]);
+        need0 = plus(need0, total[1]);
+        want0 = plus(want0, total[2]);
         rows0 += (int)all[0];
+        if (b0 + kPlanThreads < p.seqs) __syncthreads();  // (the sums and places have been read)
     }
+    if (!writes) return;
     // the last sequence that took pages has the largest sum
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) took = max(took, __shfl_xor_sync(0xffffffffu, took, d));
+    took = __reduce_max_sync(0xffffffffu, took);
     __syncthreads();
     if (lane == 0) part[0][tid >> 5] = took;
     __syncthreads();
-    if (tid == 0) {
-        for (int i = 1; i < kPlanThreads / 32; ++i) took = max(took, part[0][i]);
-        const int64_t end = taken + p.num_pages, to = returned + back0;
-        p.state_out[0] = taken + took;
-        p.state_out[1] = to <= end ? to : max(returned, end);
+    if (tid < 32) {
+        took = __reduce_max_sync(0xffffffffu, part[0][lane]);
+        if (lane == 0) {
+            const int64_t end = taken + p.num_pages, to = returned + back0;
+            int64_t *out = p.alone ? p.state_out : p.counts;
+            out[0] = taken + took;
+            out[1] = to <= end ? to : max(returned, end);
+        }
     }
     if (!p.alone) return;
     for (int t = tid; t < p.tokens; t += kPlanThreads) {
@@ -201,13 +223,21 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
     }
 }
 
-// The tokens of a step, kPlanPer a thread in turn.
+// The tokens of a step, kPlanPer a thread in turn; and what the launch before left in the workspace, to its place.
 __global__ void __launch_bounds__(256) plan_tokens_kernel(const PlanParams p)
 {
+    __shared__ int staged[kPlanStaged + 1];
     pdl_trigger();
     pdl_wait();
-    const int rows = __ldg(p.cu_q + p.seqs);
-    const int t0 = blockIdx.x * (256 * kPlanPer) + threadIdx.x;
+    for (int b = blockIdx.x * 256 + threadIdx.x; b < p.seqs; b += gridDim.x * 256) p.lens_out[b] = p.length[b];
+    if (blockIdx.x == 0 && threadIdx.x < 2) p.state_out[threadIdx.x] = p.counts[threadIdx.x];
+    const bool all = p.seqs <= kPlanStaged;
+    if (all) {
+        for (int b = threadIdx.x; b <= p.seqs; b += 256) staged[b] = __ldg(p.cu_q + b);
+        __syncthreads();
+    }
+    auto start = [&](int b) { return all ? staged[b] : __ldg(p.cu_q + b); };
+    const int rows = start(p.seqs), t0 = blockIdx.x * (256 * kPlanPer) + threadIdx.x;
     int lo = 0;
 #pragma unroll
     for (int k = 0; k < kPlanPer; ++k) {
@@ -220,11 +250,13 @@ __global__ void __launch_bounds__(256) plan_tokens_kernel(const PlanParams p)
         int hi = p.seqs;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (__ldg(p.cu_q + mid) <= t) lo = mid;
+            if (start(mid) <= t) lo = mid;
             else hi = mid;
         }
-        const int first = __ldg(p.cu_q + lo), length = __ldg(p.lens_out + lo) - (__ldg(p.cu_q + lo + 1) - first);
-        plan_token(p, t, lo, {first, length, pages_of(p, length), __ldg(p.base + lo)});
+        const int first = start(lo), length = __ldg(p.length + lo) - (start(lo + 1) - first), held = pages_of(p, length);
+        int last = -1;
+        if (p.page.div(length + (t - first)) < held) last = p.table[(int64_t)lo * p.table_width + held - 1];
+        plan_token(p, t, lo, {first, length, held, __ldg(p.base + lo), last});
     }
 }
 
@@ -241,7 +273,7 @@ size_t mc_kv_plan_workspace_size(int seqs)
         set_error(MC_ERR_INVALID_ARG, "%d sequences", seqs);
         return 0;
     }
-    return 256 + (size_t)seqs * 4;
+    return 256 + (size_t)seqs * 8;
 }
 
 int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, const uint8_t *done, int seqs, int tokens,
@@ -253,7 +285,7 @@ int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, 
     if (pool->num_pages < 1 || pool->page_size < 1 || pool->page_size > 32768)
         return set_error(MC_ERR_INVALID_ARG, "%d pages of %d", pool->num_pages, pool->page_size);
     if (seqs < 0 || tokens < 0) return set_error(MC_ERR_INVALID_ARG, "seqs %d, tokens %d", seqs, tokens);
-    if (seqs > kMaxLen || tokens > kMaxLen) return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d sequences in one call", tokens, seqs);
+    if (seqs > kMaxLen || tokens > kMaxLen || pool->num_pages > kMaxLen) return set_error(MC_ERR_UNSUPPORTED, "%d tokens of %d sequences in one call, %d pages", tokens, seqs, pool->num_pages);
     if (seqs == 0 && tokens > 0) return set_error(MC_ERR_INVALID_ARG, "%d tokens of no sequence", tokens);
     if (seqs == 0) return MC_OK;
     if (table_width < 1) return set_error(MC_ERR_INVALID_ARG, "table_width %d", table_width);
@@ -285,12 +317,16 @@ int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, 
     p.state_out = state_out;
     p.status = (int32_t *)workspace;
     p.base = (int32_t *)((uint8_t *)workspace + 256);
-    p.alone = seqs <= kPlanThreads && tokens <= kPlanFew;
+    p.length = p.base + seqs;
+    p.counts = (int64_t *)((uint8_t *)workspace + 128);
+    p.alone = seqs <= kPlanThreads && tokens <= kPlanFew && (!done || (int64_t)seqs * table_width <= kPlanEntries);
     cudaStream_t st = (cudaStream_t)stream;
     profile_begin(kKPlan, st);
-    cudaError_t e = launch_k(plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
-    if (e == cudaSuccess && !p.alone && tokens)
-        e = launch_k(plan_tokens_kernel, dim3((unsigned)((tokens + 256 * kPlanPer - 1) / (256 * kPlanPer))), dim3(256), 0, st, p);
+    cudaError_t e = launch_k(plan_kernel, dim3(p.alone || !done ? 1 : kPlanBlocks), dim3(kPlanThreads), 0, st, p);
+    if (e == cudaSuccess && !p.alone) {
+        const int64_t per = 256 * kPlanPer, blocks = (tokens + per - 1) / per;
+        e = launch_k(plan_tokens_kernel, dim3((unsigned)(blocks ? blocks : 1)), dim3(256), 0, st, p);
+    }
     profile_end(kKPlan, st);
     if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "plan launch: %s", cudaGetErrorString(e));
     return MC_OK;
