@@ -154,9 +154,11 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     // device's, so the mean decides.  8 sequences of 4000 keys, decode / tensor-memory kernel:
     // 16 rows 30 / 36 us, 20 rows 37 / 36, 32 rows 42 / 36; with a cap, whose cost follows the rows,
     // 36 / 51 at 20 and 44 / 51 at 32; one sequence of 2000 keys, 16 rows, 12 / 14.
+    // Over the 4-bit cache up to 32 rows, with a cap or without: 64 sequences of 4000 keys, 20 rows, 131 / 280 us; 16 of
+    // them, 24 rows 44 / 73, 32 rows 62 / 74, 48 rows 103 / 77; one of 2000 keys, 32 rows, 20 / 17.
     const int64_t rows = ((int64_t)batch->tokens + batch->seqs - 1) / batch->seqs * p.group;
     const bool bf16 = cache->dtype == MC_BF16;
-    if (rows <= (p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, q4, (int)rows, (cudaStream_t)stream);
+    if (rows <= (q4 || p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, q4, (int)rows, (cudaStream_t)stream);
     if (q4) {
         // Prompts of many rows: their keys are unpacked once, where the workspace holds what the batch's tables reach,
         // not for every 256 rows.  Unpacked / in the kernel: 8192 tokens of a group of 4 343 / 524 us, 4096 116 / 162, 1024

@@ -400,10 +400,11 @@ __device__ __forceinline__ void pf_copy16z(uint32_t dst, const void *src, bool r
 // Q4 has a warpgroup more.
 template <bool Q4>
 struct PfRegs {
-    static constexpr int kAll = Q4 ? 128 : 168, kSoft = Q4 ? 192 : 208, kRest = Q4 ? 64 : 80;
-    static_assert(2 * kSoft + (Q4 ? 2 : 1) * kRest <= (Q4 ? 4 : 3) * kAll, "register shares");
+    static constexpr int kAll = Q4 ? 128 : 168, kSoft = Q4 ? 184 : 208, kRest = Q4 ? 48 : 80, kUnpack = 96;
+    static_assert(2 * kSoft + kRest + (Q4 ? kUnpack : 0) <= (Q4 ? 4 : 3) * kAll, "register shares");
     static __device__ __forceinline__ void take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoft)); }
     static __device__ __forceinline__ void give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRest)); }
+    static __device__ __forceinline__ void give_unpack() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kUnpack)); }
 };
 
 // ---------------------------------------------------------------- softmax --
@@ -521,45 +522,70 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 // ------------------------------------------------------------------ kernel --
 
 // QUEUE: the batch may have the items for a queue (the host's bound), so the kernel looks at them.
-// A key's row of the 4-bit cache, as loaded, and into a tile: its groups' 64 columns in 8 chunks of 16 bytes, swizzled.
+// A lane's part of 32 keys (a warp's) of the 4-bit cache: 16-byte chunks of codes, as they lie, kPer of them, 32 / kPer
+// keys apart; and into a tile, as exact numbers of the type, to where a copy would have put them (a group's 64 columns in
+// 8 chunks of 16 bytes, swizzled).  The keys lie in two runs of 16, each in one page.
 template <int D>
 struct PfRaw {
-    uint4 w[D / 32];
-    uint32_t word;
+    static constexpr int kPer = D / 32, kChunks = D / 32, kStep = 32 / kPer;
+    uint4 w[kPer];
+    uint32_t word[kPer];
 
-    // (zeros, that is a scale of 0, where there is no such key)
-    __device__ __forceinline__ void load(const KvView &c, const uint16_t *side, int page, int h, int row)
+    // page and row of each run (page < 0: zeros, that is scales of 0); keys outside [from, to), counted from the
+    // warp's first, are zeros too
+    __device__ __forceinline__ void load(const KvView &c, const uint16_t *side, const int (&page)[2], const int (&row)[2], int h, int from, int to, int lane)
     {
-        if (page < 0) {
-            word = 0;
+        const int block_bytes = c.page_size * kv4_row_bytes(D);
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) w[i] = make_uint4(0, 0, 0, 0);
-            return;
+        for (int run = 0; run < 2; ++run) {
+            const uint8_t *block = reinterpret_cast<const uint8_t *>(side) + (max(page[run], 0) * c.page_stride + (int64_t)h * block_bytes);
+            const uint8_t *codes = block + (row[run] + lane / kChunks) * kv4_code_bytes(D) + 16 * (lane % kChunks);
+            const uint8_t *words = block + c.page_size * kv4_code_bytes(D) + (row[run] + lane / kChunks) * kv4_word_bytes(D);
+#pragma unroll
+            for (int k = 0; k < kPer / 2; ++k) {
+                const int i = run * (kPer / 2) + k, key = lane / kChunks + kStep * i;
+                w[i] = make_uint4(0, 0, 0, 0);
+                word[i] = 0;
+                if (page[run] >= 0) {
+                    w[i] = __ldg(reinterpret_cast<const uint4 *>(codes + k * kStep * kv4_code_bytes(D)));
+                    if (key >= from && key < to)
+                        word[i] = D == 128 ? __ldg(reinterpret_cast<const uint32_t *>(words + k * kStep * kv4_word_bytes(D)))
+                                           : __ldg(reinterpret_cast<const uint16_t *>(words + k * kStep * kv4_word_bytes(D)));
+                }
+            }
         }
-        const uint8_t *block = kv4_block<D>(c, side, page, h);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(block + row * kv4_code_bytes(D)) + i);
-        const uint8_t *words = block + c.page_size * kv4_code_bytes(D) + row * kv4_word_bytes(D);
-        word = D == 128 ? __ldg(reinterpret_cast<const uint32_t *>(words)) : __ldg(reinterpret_cast<const uint16_t *>(words));
     }
 
+    // tile: of the warp's first key
     template <bool BF16>
-    __device__ __forceinline__ void store(uint32_t tile, int half, int r) const
+    __device__ __forceinline__ void store(uint8_t *tile, int half, int lane) const
     {
         using P = Kv4Pairs<BF16>;
         constexpr int kGroups = D / kKv4Group;
+        const int ch = lane % kChunks;
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            const uint32_t z = P::zeros(word >> (16 * g)), sc = P::scales(word >> (16 * g));
+        for (int i = 0; i < kPer; ++i) {
+            const int key = lane / kChunks + kStep * i;
+            uint32_t z[kGroups], sc[kGroups];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int x = i * kGroups + g;
-                const uint32_t v = x % 4 == 0 ? w[x / 4].x : x % 4 == 1 ? w[x / 4].y : x % 4 == 2 ? w[x / 4].z : w[x / 4].w;
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + g * half + r * 128 + ((i ^ (r & 7)) << 4)),
-                             "r"(P::mul(P::sub(P::magic(v, 0), z), sc)), "r"(P::mul(P::sub(P::magic(v, 1), z), sc)),
-                             "r"(P::mul(P::sub(P::magic(v, 2), z), sc)), "r"(P::mul(P::sub(P::magic(v, 3), z), sc))
-                             : "memory");
+            for (int g = 0; g < kGroups; ++g) {
+                z[g] = P::zeros(word[i] >> (16 * g));
+                sc[g] = P::scales(word[i] >> (16 * g));
             }
+            const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+            uint32_t y[4][4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[x][j] = P::magic(v[x], j);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[x][j] = P::mul(P::sub(y[x][j], z[x % kGroups]), sc[x % kGroups]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                *reinterpret_cast<uint4 *>(tile + (x % kGroups) * half + key * 128 + ((((4 * ch + x) / kGroups) ^ (key & 7)) << 4)) =
+                    make_uint4(y[x][0], y[x][1], y[x][2], y[x][3]);
         }
     }
 };
@@ -686,42 +712,51 @@ __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfPara
         sh->abort = 1;
     }
     if (warp >= kPfMma) {
-        Regs::give();  // one instruction for the warpgroup
         if (Q4 && warp >= kPfUnpack) {
+            Regs::give_unpack();
             // ------------------------------------------------- keys and values in 4 bits --
-            // A thread a key: its row is loaded a tile ahead, while the tile before is written out, as exact numbers
-            // of the type, to where a copy would have put them.
-            const int r = tid - 32 * kPfUnpack;
-            const uint32_t ring = smem_u32(smem) + Sh::kRing;
+            // A warp 32 keys of a tile: loaded a tile ahead, while the tile before is written out.
+            const int first_key = 32 * (warp - kPfUnpack);
             int it = 0;
             bool ok = !(pp.debug & kDebugNoProducer);
             const volatile PfItem *item = ok ? pf_item(pp, sh, 0) : nullptr;
-            int b = 0, h = 0, base = 0, from = 0, to = 0, page = -1, row = 0, spent = 0;
-            // the page of this thread's key of unit u (as the table has it)
+            int b = 0, h = 0, from = 0, to = 0, spent = 0;  // keys that the item's rows see, from its first unit's first on
+            int base = 0, page[2], row[2], next[2], next_row[2];
+            // the pages of the warp's two runs of unit u, as the table has them
             auto look = [&](int u) {
-                const int j = base + u * kPfKeys + r;
-                if (j < from || j >= to) return -1;
-                const int pg = __ldg(p.b.table + (int64_t)b * p.b.table_width + p.c.page.div(j, row));
-                return pg;
+#pragma unroll
+                for (int run = 0; run < 2; ++run) {
+                    const int j = u * kPfKeys + first_key + 16 * run;
+                    next[run] = -1;
+                    next_row[run] = 0;
+                    if (j < to && j + 16 > from)
+                        next[run] = __ldg(p.b.table + (int64_t)b * p.b.table_width + p.c.page.div(base + j, next_row[run]));
+                }
             };
-            auto checked = [&](int u, int pg) {
-                if ((unsigned)pg < (unsigned)p.c.num_pages) return pg;
-                const int j = base + u * kPfKeys + r;
-                if (j >= from && j < to) set_status(p.status, MC_ERR_RANGE);
-                return -1;
+            auto turn_to = [&](int u) {  // what look found
+#pragma unroll
+                for (int run = 0; run < 2; ++run) {
+                    const int j = u * kPfKeys + first_key + 16 * run;
+                    page[run] = next[run];
+                    row[run] = next_row[run];
+                    if ((unsigned)page[run] >= (unsigned)p.c.num_pages) {
+                        if (j < to && j + 16 > from) set_status(p.status, MC_ERR_RANGE);
+                        page[run] = -1;
+                    }
+                }
             };
             auto enter = [&]() {
                 b = item->b;
                 h = item->h;
                 base = item->k.base;
-                from = item->k.first;
-                to = min(item->k.end, item->s.len);
+                from = item->k.first - base;
+                to = min(item->k.end, item->s.len) - base;
             };
             // tile number `it`, when its slot is free
             auto put = [&](const PfRaw<D> &x) {
                 const int slot = it % Sh::kStages;
                 if (it >= Sh::kStages && !(ok = warp_wait(&sh->kempty[slot], (it / Sh::kStages + 1) & 1, pp, sh))) return;
-                x.template store<BF16>(ring + slot * Sh::kTileBytes, Sh::kHalf, r);
+                x.template store<BF16>(smem + Sh::kRing + slot * Sh::kTileBytes + first_key * 128, Sh::kHalf, lane);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh->kfull[slot]);
@@ -730,20 +765,24 @@ __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfPara
             PfRaw<D> k, v;
             int n = 0, u = 0;
             PfOrder order(p, kKeyBytes, sh->item[0], sh->run, 0);
+            auto load = [&](PfRaw<D> &x, const uint16_t *side) {
+                const int at = u * kPfKeys + first_key;
+                x.load(p.c, side, page, row, h, from - at, to - at, lane);
+            };
             if (item) {
                 enter();
                 n = item->n;
                 u = order.unit(0);
-                page = checked(u, look(u));
-                k.load(p.c, p.c.k, page, h, row);
+                look(u);
+                turn_to(u);
+                load(k, p.c.k);
             }
             for (int turn = 0; ok && n > 0;) {
                 for (int i = 0; ok && i < n; ++i) {
-                    v.load(p.c, p.c.v, page, h, row);
-                    int next = -1, next_h = h;
+                    load(v, p.c.v);
                     if (i + 1 < n) {
                         u = order.unit(i + 1);
-                        next = look(u);
+                        look(u);
                     }
                     put(k);
                     if (!ok) break;
@@ -753,23 +792,22 @@ __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfPara
                         n = 0;
                         if (item) {
                             enter();
-                            next_h = h;
                             order = PfOrder(p, kKeyBytes, *item, sh->run, spent);
                             n = item->n;
                             u = order.unit(0);
-                            next = look(u);
+                            look(u);
                         }
-                        page = n ? checked(u, next) : -1;
-                        k.load(p.c, p.c.k, page, next_h, row);
-                        put(v);
-                        break;
+                        i = -2;  // (the item is done)
                     }
-                    page = checked(u, next);
-                    k.load(p.c, p.c.k, page, h, row);
+                    if (n) {
+                        turn_to(u);
+                        load(k, p.c.k);
+                    }
                     put(v);
+                    if (i < 0) break;
                 }
             }
-        } else if (warp >= kPfKv) {
+        } else if (Regs::give(), warp >= kPfKv) {  // one instruction for the warpgroup
             // -------------------------------------------------------------- copies --
             const uint32_t smem0 = smem_u32(smem);
             if (warp == kPfKv) {
