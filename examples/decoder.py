@@ -1,12 +1,13 @@
 """A small Mixtral-style decoder served end to end with this library: prompts of several users
 prefilled in one ragged batch, then one token per user and step.
 
-    python examples/decoder.py [--layers 2] [--steps 16]
+    python examples/decoder.py [--layers 2] [--steps 16] [--bits4]
 
 Each layer is  h <- h + Wo attention(RMSNorm(h)),  h <- h + MoE(RMSNorm(h)):  kv_append norms and
 rotates the new queries and keys and writes keys and values to the paged cache, attn_prefill or
-attn_decode reads it, moe_forward is the compressed expert block.  The projections are plain
-torch matrix products, weights are random.
+attn_decode reads it, moe_forward is the compressed expert block, and residual_norm is what lies between the
+blocks.  kv_plan hands out the cache's pages as users grow, and takes them back.  With --bits4 the cache holds 4
+bits an element.  The projections are plain torch matrix products, weights are random.
 """
 from __future__ import annotations
 
@@ -27,7 +28,7 @@ HEADS, KV_HEADS, DIM, PAGE, VOCAB = 8, 2, 64, 16, 512
 class Layer:
     """Weights of one layer, and its slice of the cache."""
 
-    def __init__(self, seed, tokens, pages):
+    def __init__(self, seed, tokens, pages, bits4=False):
         g = torch.Generator(device="cuda").manual_seed(seed)
         L = synth.make_layer(tokens, 256, 512, 8, 64, [3, 2, 2, 1, 3, 2, 2, 3], seed)
         self.shape, self.bits, self.mu = mc.Shape(L.E, L.H, L.F, L.group), L.bits, 0.2
@@ -37,54 +38,65 @@ class Layer:
         w = lambda *s: (torch.randn(*s, generator=g, device="cuda") * s[0] ** -0.5).to(torch.bfloat16)  # noqa: E731
         self.qkv, self.out = w(L.H, (HEADS + 2 * KV_HEADS) * DIM), w(HEADS * DIM, L.H)
         self.norms = [torch.ones(n, dtype=torch.bfloat16, device="cuda") for n in (L.H, L.H, DIM, DIM)]
-        pool = torch.empty(pages, 2, KV_HEADS, PAGE, DIM, dtype=torch.bfloat16, device="cuda")  # keys, values of a page
-        self.cache = mc.KVCache(pool[:, 0], pool[:, 1])
+        if bits4:
+            pool = torch.empty(pages, 2, KV_HEADS, mc.kv4_block_size(PAGE, DIM), dtype=torch.uint8, device="cuda")
+            self.cache = mc.KVCache4(pool[:, 0], pool[:, 1], PAGE, DIM)
+        else:
+            pool = torch.empty(pages, 2, KV_HEADS, PAGE, DIM, dtype=torch.bfloat16, device="cuda")  # keys, values of a page
+            self.cache = mc.KVCache(pool[:, 0], pool[:, 1])
 
 
 class Decoder:
-    """Layers, the page table of every user, and the buffers that calls reuse."""
+    """Layers, the page table of every user, the free pages, and the buffers that calls reuse."""
 
-    def __init__(self, layers, users, max_len, seed=0, max_tokens=512):
+    def __init__(self, layers, users, max_len, seed=0, max_tokens=512, bits4=False):
         width = -(-max_len // PAGE)
-        self.layers = [Layer(seed + i, max_tokens, users * width) for i in range(layers)]
+        pages = (users + 1) * width  # (what a user gives back is free from the next step on)
+        self.layers = [Layer(seed + i, max_tokens, pages, bits4) for i in range(layers)]
+        self.append = mc.kv4_append if bits4 else mc.kv_append
+        self.attend = (mc.attn4_decode, mc.attn4_prefill) if bits4 else (mc.attn_decode, mc.attn_prefill)
         self.hidden = self.layers[0].shape.H
         g = torch.Generator(device="cuda").manual_seed(seed + 1000)
         self.embed, self.head = (torch.randn(VOCAB, self.hidden, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
         a = torch.arange(max_len, device="cuda", dtype=torch.float64)[:, None]
         a = a * 10000.0 ** (-torch.arange(0, DIM, 2, device="cuda", dtype=torch.float64) / DIM)
         self.rope = torch.cat([a.cos(), a.sin()], 1).float()
-        # a user's pages, in an order of their own (a server would hand them out as sequences grow)
-        self.table = torch.randperm(users * width, generator=torch.Generator().manual_seed(seed)).view(users, width).to(torch.int32).cuda()
+        # free pages, in an order of their own
+        ring = torch.randperm(pages, generator=torch.Generator().manual_seed(seed)).to(torch.int32).cuda()
+        self.pool = mc.KVPool(pages, PAGE, ring=ring)
+        self.table = torch.full((users, width), -1, dtype=torch.int32, device="cuda")
         self.lens = torch.zeros(users, dtype=torch.int32, device="cuda")
-        self.attn_ws = mc.attn_workspace(self.layers[0].cache, HEADS)
+        self.one = torch.ones(users, dtype=torch.int32, device="cuda")
+        self.attn_ws = (mc.attn4_workspace if bits4 else mc.attn_workspace)(self.layers[0].cache, HEADS)
+        self.plan_ws = mc.kv_plan_workspace(users)
         self.moe_ws = mc.alloc_workspace(self.layers[0].shape, max_tokens)
 
-    def forward(self, tokens, new=None):
-        """Hidden states after the last layer of `tokens`: new[b] of user b, in order (None: one each)."""
-        if new is None:
-            self.lens += 1
-            batch = mc.KVBatch(self.lens, self.table)
-        else:
-            new = torch.tensor(new, dtype=torch.int32)
-            self.lens += new.cuda()
-            cu = torch.cat([torch.zeros(1, dtype=torch.int32), new.cumsum(0, dtype=torch.int32)]).cuda()
-            batch = mc.KVBatch(self.lens, self.table, cu, tokens.shape[0])
+    def forward(self, tokens, new=None, over=None):
+        """Hidden states after the last layer of `tokens`: new[b] of user b, in order (None: one each).  Users with
+        over[b] are done: their pages go back, and what is new is another user's first text."""
+        add = self.one if new is None else torch.tensor(new, dtype=torch.int32).cuda()
+        over = None if over is None else torch.tensor(over, dtype=torch.uint8).cuda()
+        plan = mc.kv_plan(self.pool, self.table, self.lens, add, done=over, tokens=tokens.shape[0], lens_out=self.lens,
+                          positions=False, slots=False, workspace=self.plan_ws)
+        batch = mc.KVBatch(self.lens, self.table) if new is None else plan.batch
+        attend = self.attend[new is not None]
         h, T = self.embed[tokens], tokens.shape[0]
-        for w in self.layers:
-            x = (mc.rmsnorm(h, w.norms[0]) @ w.qkv).view(T, HEADS + 2 * KV_HEADS, DIM)
-            q = mc.kv_append(w.cache, batch, x[:, :HEADS], x[:, HEADS:HEADS + KV_HEADS], x[:, HEADS + KV_HEADS:], rope=self.rope,
-                             q_norm=w.norms[2], k_norm=w.norms[3], workspace=self.attn_ws)
-            attend = mc.attn_decode if new is None else mc.attn_prefill
+        x = mc.rmsnorm(h, self.layers[0].norms[0])
+        for i, w in enumerate(self.layers):
+            x = (x @ w.qkv).view(T, HEADS + 2 * KV_HEADS, DIM)
+            q = self.append(w.cache, batch, x[:, :HEADS], x[:, HEADS:HEADS + KV_HEADS], x[:, HEADS + KV_HEADS:], rope=self.rope,
+                            q_norm=w.norms[2], k_norm=w.norms[3], workspace=self.attn_ws)
             o = attend(w.cache, batch, q, workspace=self.attn_ws)
-            h = mc.add(h, o.view(T, -1) @ w.out)
-            y = mc.moe_forward(mc.rmsnorm(h, w.norms[1]), w.gate, w.shape, w.bits, w.experts, w.mu, workspace=self.moe_ws)
-            h = mc.add(h, y)
+            h, x = mc.residual_norm(o.view(T, -1) @ w.out, h, pre_norm=w.norms[1])
+            y = mc.moe_forward(x, w.gate, w.shape, w.bits, w.experts, w.mu, workspace=self.moe_ws)
+            h, x = mc.residual_norm(y, h, pre_norm=self.layers[i + 1].norms[0] if i + 1 < len(self.layers) else None)
         return h
 
     def logits(self, h):
         return (h @ self.head.T).float()
 
     def check(self):
+        mc.check_status(self.plan_ws)
         mc.check_status(self.attn_ws)
         mc.check_status(self.moe_ws)
 
@@ -93,9 +105,10 @@ def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--steps", type=int, default=16)
+    ap.add_argument("--bits4", action="store_true", help="the cache in 4 bits")
     a = ap.parse_args()
     prompts = [37, 5, 64, 1]
-    d = Decoder(a.layers, len(prompts), max(prompts) + a.steps)
+    d = Decoder(a.layers, len(prompts), max(prompts) + a.steps, bits4=a.bits4)
     tokens = torch.randint(VOCAB, (sum(prompts),), generator=torch.Generator().manual_seed(1)).cuda()
     h = d.forward(tokens, prompts)
     last = torch.tensor(prompts).cumsum(0).cuda() - 1
