@@ -22,6 +22,18 @@
 // bytes 537.1 MB for 536.9 (ncu, 16 x 8192).  Short ones are bound by latency: 777 keys 7.4 us, of which
 // the schedule 1, the first keys 1.5, the join and its launch 3; so are caps over more than 8 rows (33
 // sequences of a window of 1024 keys, 12 heads a key head: 17 us, special functions 4 % active).
+//
+// Q4, the cache in 4 bits (17 D / 16 bytes a key): the same schedule and products, the operands made from codes in
+// registers.  A code is a number of the type as it stands, (2^k + c) - (2^k + z): one LOP3 and half an instruction of
+// subtraction for two.  Q K^T is formed per group of 64 in fp16, whatever the type (LOP3 finds two of a half-word's four
+// codes in place there, bf16 one), and a group's scale multiplies its sum; in the product with V the scale is in the
+// weight (bf16: a weight for each group) or the value (fp16, whose range a weight times a scale could leave).
+// Bound by issue and the integer pipe, not by HBM: 660 instructions for 32 keys of 128 and 8 rows, 330 of them to
+// unpack, issue 49 % and ALU 51 % active.  64 sequences of 8192 keys, 32 heads on 8 of 128, 129 us, 4.4 TB/s (0.65 of
+// the measured copy rate; the 16-bit cache 310 us); one of 131071 keys 41 us (83); 777 keys 8.5 us.  Four tiles of 16 keys a
+// warp's step, two blocks an SM: 135 us where two tiles and three blocks took 145 (three blocks and four tiles, with
+// O joined a quarter at a time to make room, 128, but short ones longer: 777 keys 9.9 us for 8.6); keys, codes and
+// queries in bf16 161; copies by cp.async.bulk 163 (a lane's addresses go through uniform registers one by one).
 #pragma once
 #include <math.h>
 
@@ -34,7 +46,7 @@ namespace mc {
 constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 // Keys of a unit that one warp takes, in tiles of 16: heads of 64 take two tiles in one step,
 // whose chains of products and exponentials overlap (a step of 16 keys takes about as long
-// whatever the head, and 16 keys of 64 are half the bytes).
+// whatever the head, and 16 keys of 64 are half the bytes).  Q4: as many as the registers hold beside nt tiles of rows.
 constexpr int dec_tiles(int D, bool q4, int nt) { return q4 ? (nt == 1 ? 4 : nt == 4 ? 1 : 2) : D == 64 ? 2 : 1; }
 constexpr int dec_unit(int D, bool q4, int nt) { return 16 * dec_tiles(D, q4, nt) * kDecWarps; }
 constexpr int dec_ctas(int D, bool q4, int nt) { return q4 && D == 64 && nt == 1 ? 3 : 2; }  // an SM

@@ -32,6 +32,12 @@
 // 10 copies keys and values (TMA, a box per page and 64 columns), 11 the queries (TMA where a
 // tile is whole tokens of the group's heads, else cp.async).
 // Tensor memory: S (and P) of tile t at column 128 t, O at 256 + 128 t.
+//
+// Q4, the cache in 4 bits: warps 12-15 read the codes and write a tile as exact numbers of the type, which takes them
+// 2300 cycles a tile of 128 keys (1000 to convert, in 310 instructions a warp; the rest finding pages, loads and
+// waits), two tiles a unit: more than the products take, so prompts of many rows have their keys unpacked
+// before (mc_kv.cu) and come here as a 16-bit cache.  64 tokens over 30000 keys 51 us, 256 138.  What it hangs on is
+// registers: with 212 bytes spilled to a local memory that has no L1 left 64 tokens over 30000 keys took 76 us.
 #pragma once
 #include <math.h>
 

@@ -38,7 +38,8 @@ __device__ __forceinline__ uint64_t swapped(uint64_t v)
 //
 // Q4: a key's or value's row, rounded to the type, is brought into its own order where the rotation's runs are
 // not (through shared memory, a row of D elements by its D / 8 lanes), so that the 8 lanes of a group hold its 64
-// elements, 8 each; they find its ends by exchanging pairs and each writes a word of codes.
+// elements, 8 each; they find its ends by exchanging pairs and each writes a word of codes.  8192 tokens as above 47 us
+// (issue 68 % active, ALU 56 %: 120 instructions more for two rows of 128).
 template <int D, bool BF16, bool Q4>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams p)
 {
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
 }
 
 // Rows of the batch's new tokens as they are stored: a warp takes a token's heads of one side (keys or values),
-// 256 elements at a time, a word of codes a lane.
+// 256 elements at a time, a word of codes a lane.  Bound by the writes: 8192 tokens of 8 heads of 128, 42 MB in all, 9 us.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kAppendThreads) read4_kernel(const ReadParams p)
 {
@@ -239,6 +240,7 @@ __global__ void __launch_bounds__(kAppendThreads) read4_kernel(const ReadParams 
         page = seq_page(p.b, p.c, place.seq, n, p.status);
     }
     out += (int64_t)t * p.c.kv_heads * D;
+#pragma unroll 4
     for (int h = lane / kLanes; h < p.c.kv_heads; h += kRows) {
         uint4 x = make_uint4(0, 0, 0, 0);
         if (page >= 0) {
@@ -268,19 +270,19 @@ int launch_read4(const ReadParams &p, int head_dim, bool bf16, cudaStream_t st)
 
 // The keys that a batch's new tokens see, as 16-bit pages of sequence after sequence (page i of sequence b at
 // b * table_width + i, which is also what the table written here says): what attention of prompts reads, so that a key
-// is unpacked once and not for every 256 rows that see it.  A block takes 64 keys of a head, a thread
-// a 16-byte chunk of codes of a key and of a value.  Bound by the writes, 4 D bytes a key (they stay in L2 for the
+// is unpacked once and not for every 256 rows that see it.  A block takes 64 keys of four heads, a thread
+// a 16-byte chunk of codes of a key and of a value of each.  Bound by the writes, 4 D bytes a key (they stay in L2 for the
 // attention as far as they fit): 8192 keys of 8 heads of 128, 33 MB, 9 us.
-constexpr int kUnpackKeys = 64;
+constexpr int kUnpackKeys = 64, kUnpackHeads = 4;  // heads of a block
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kUnpackKeys * D / 32) unpack4_kernel(const Unpack4Params p)
 {
     constexpr int kChunks = D / 32, kGroups = D / kKv4Group;  // 16-byte chunks of a row's codes
     pdl_trigger();
     pdl_wait();
-    const int b = blockIdx.z, h = blockIdx.y, row = threadIdx.x / kChunks, ch = threadIdx.x % kChunks;
+    const int b = blockIdx.z, h0 = blockIdx.y * kUnpackHeads, row = threadIdx.x / kChunks, ch = threadIdx.x % kChunks;
     const int j = blockIdx.x * kUnpackKeys + row;
-    if (h == 0)
+    if (h0 == 0)
         for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < p.b.table_width; i += gridDim.x * blockDim.x)
             p.table[(int64_t)b * p.b.table_width + i] = b * p.b.table_width + i;
     int first;
@@ -289,30 +291,37 @@ __global__ void __launch_bounds__(kUnpackKeys * D / 32) unpack4_kernel(const Unp
     if (n == 0 || j >= len || j < (seen & ~127)) return;
     int r;
     const int i = p.c.page.div(j, r), page = j < seen ? -1 : seq_page(p.b, p.c, b, i, p.status);
-    const int64_t to = (((int64_t)b * p.b.table_width + i) * p.c.kv_heads + h) * p.c.page_size * D + (int64_t)r * D;
-    uint4 codes[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    uint32_t words[2] = {0, 0};  // (no such page, or behind the window: zeros)
-    if (page >= 0) {
-#pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            const uint8_t *block = kv4_block<D>(p.c, side ? p.c.v : p.c.k, page, h);
-            codes[side] = __ldg(reinterpret_cast<const uint4 *>(block + r * kv4_code_bytes(D)) + ch);
-            const uint8_t *w = block + p.c.page_size * kv4_code_bytes(D) + r * kv4_word_bytes(D);
-            words[side] = D == 128 ? __ldg(reinterpret_cast<const uint32_t *>(w)) : __ldg(reinterpret_cast<const uint16_t *>(w));
-        }
-    }
+    const int64_t plane = (int64_t)p.c.page_size * D;
+    const int64_t to = (((int64_t)b * p.b.table_width + i) * p.c.kv_heads + h0) * plane + (int64_t)r * D;
+    const int block_bytes = p.c.page_size * kv4_row_bytes(D);
     using P = Kv4Pairs<BF16>;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        uint16_t *out = (side ? p.v : p.k) + to;
-        const uint32_t w[4] = {codes[side].x, codes[side].y, codes[side].z, codes[side].w};
+        const uint8_t *block = kv4_block<D>(p.c, side ? p.c.v : p.c.k, max(page, 0), h0);
+        uint4 codes[kUnpackHeads];
+        uint32_t words[kUnpackHeads];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int at = 4 * ch + x, g = at % kGroups;  // word at / kGroups of group g
-            const uint32_t z = P::zeros(words[side] >> (16 * g)), sc = P::scales(words[side] >> (16 * g));
-            *reinterpret_cast<uint4 *>(out + 64 * g + 8 * (at / kGroups)) =
-                make_uint4(P::mul(P::sub(P::magic(w[x], 0), z), sc), P::mul(P::sub(P::magic(w[x], 1), z), sc),
-                           P::mul(P::sub(P::magic(w[x], 2), z), sc), P::mul(P::sub(P::magic(w[x], 3), z), sc));
+        for (int h = 0; h < kUnpackHeads; ++h) {  // all loads before the first use
+            codes[h] = make_uint4(0, 0, 0, 0);
+            words[h] = 0;  // (no such page, or behind the window: zeros)
+            if (page < 0 || h0 + h >= p.c.kv_heads) continue;
+            codes[h] = __ldg(reinterpret_cast<const uint4 *>(block + h * block_bytes + r * kv4_code_bytes(D)) + ch);
+            const uint8_t *w = block + h * block_bytes + p.c.page_size * kv4_code_bytes(D) + r * kv4_word_bytes(D);
+            words[h] = D == 128 ? __ldg(reinterpret_cast<const uint32_t *>(w)) : __ldg(reinterpret_cast<const uint16_t *>(w));
+        }
+#pragma unroll
+        for (int h = 0; h < kUnpackHeads; ++h) {
+            if (h0 + h >= p.c.kv_heads) break;
+            uint16_t *out = (side ? p.v : p.k) + to + h * plane;
+            const uint32_t w[4] = {codes[h].x, codes[h].y, codes[h].z, codes[h].w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int at = 4 * ch + x, g = at % kGroups;  // word at / kGroups of group g
+                const uint32_t z = P::zeros(words[h] >> (16 * g)), sc = P::scales(words[h] >> (16 * g));
+                *reinterpret_cast<uint4 *>(out + 64 * g + 8 * (at / kGroups)) =
+                    make_uint4(P::mul(P::sub(P::magic(w[x], 0), z), sc), P::mul(P::sub(P::magic(w[x], 1), z), sc),
+                               P::mul(P::sub(P::magic(w[x], 2), z), sc), P::mul(P::sub(P::magic(w[x], 3), z), sc));
+            }
         }
     }
 }
@@ -320,7 +329,7 @@ __global__ void __launch_bounds__(kUnpackKeys * D / 32) unpack4_kernel(const Unp
 int launch_unpack4(const Unpack4Params &p, int head_dim, bool bf16, cudaStream_t st)
 {
     const int64_t room = (int64_t)p.b.table_width * p.c.page_size;
-    const dim3 grid((unsigned)((room + kUnpackKeys - 1) / kUnpackKeys), p.c.kv_heads, p.b.seqs);
+    const dim3 grid((unsigned)((room + kUnpackKeys - 1) / kUnpackKeys), (p.c.kv_heads + kUnpackHeads - 1) / kUnpackHeads, p.b.seqs);
     auto k = head_dim == 64 ? (bf16 ? unpack4_kernel<64, true> : unpack4_kernel<64, false>)
                             : (bf16 ? unpack4_kernel<128, true> : unpack4_kernel<128, false>);
     profile_begin(kKUnpack, st);

@@ -35,6 +35,15 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
     return r;
 }
 
+template <bool BF16>
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    if (BF16) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 // Codes held to z - most .. z + most, where more steps than `most` pass the type's largest number.
 template <bool BF16>
 __device__ __noinline__ uint32_t kv4_held(uint32_t codes, int z, int most)
@@ -58,8 +67,7 @@ __device__ __forceinline__ uint32_t kv4_quantise(const uint32_t (&x)[4], uint32_
     constexpr float kMost = BF16 ? 0x1.fep127f : 65504.f;
     constexpr uint32_t kLeast = BF16 ? (127u - 100) << 23 : (127u - 20) << 23;
     uint32_t top = max2<BF16>(max2<BF16>(x[0], x[1]), max2<BF16>(x[2], x[3]));
-    const uint32_t n0 = x[0] ^ 0x80008000u, n1 = x[1] ^ 0x80008000u, n2 = x[2] ^ 0x80008000u, n3 = x[3] ^ 0x80008000u;
-    uint32_t low = max2<BF16>(max2<BF16>(n0, n1), max2<BF16>(n2, n3));
+    uint32_t low = min2<BF16>(min2<BF16>(x[0], x[1]), min2<BF16>(x[2], x[3])) ^ 0x80008000u;
     // (largest, largest of the negatives) in one register
     uint32_t ends = max2<BF16>(__byte_perm(top, low, 0x5410), __byte_perm(top, low, 0x7632));
 #pragma unroll
@@ -80,8 +88,9 @@ __device__ __forceinline__ uint32_t kv4_quantise(const uint32_t (&x)[4], uint32_
 #pragma unroll
     for (int i = 0; i < 4; ++i) {  // (no quotient rounds below -z)
         const float2 f = unpack2<BF16>(x[i]);
-        const float a = fminf(fmaf(f.x, inv, kTie) + base, kShift + 15.f), b = fminf(fmaf(f.y, inv, kTie) + base, kShift + 15.f);
-        r += __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410) << (4 * i);
+        float a, b;
+        unpair2(add2(fma2(pair2(f.x, f.y), pair2(inv, inv), pair2(kTie, kTie)), pair2(base, base)), a, b);
+        r += __byte_perm(__float_as_uint(fminf(a, kShift + 15.f)), __float_as_uint(fminf(b, kShift + 15.f)), 0x5410) << (4 * i);
     }
     if (kMost * inv < 16.f && !odd) r = kv4_held<BF16>(r, (int)z, (int)(kMost * inv));
     return odd ? 0u : r;
