@@ -1,7 +1,7 @@
 // mc_plan.cu -- mc_kv_plan: pages, positions and slots of a step's new tokens, from the lengths.
 //
 // Per sequence three running sums decide everything (pages that come back, pages asked for, rows), so a block
-// goes over the sequences, a thread each, 1024 at a time; the tokens, of which there may be hundreds of
+// goes over the sequences, 1024 or 4096 at a time; the tokens, of which there may be hundreds of
 // thousands, then find their sequence in the boundaries and write 12 bytes each.  A step of few tokens is
 // one launch of one block, with the sums still in shared memory.  Others are two: the first has several blocks, which
 // all make the sums and each copy a part of the returned pages (its results go to the workspace, since lens and the
@@ -87,11 +87,14 @@ __device__ __forceinline__ int pages_of(const PlanParams &p, int tokens)
 // Sums of numbers that are not negative stop at 2^31 - 1, which is beyond every limit they are held against.
 __device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
 
-// Inclusive sums over the block in place; totals in `total`.
+// Sums over the block's threads: of those before (before) and of all (total).
 template <int N>
-__device__ __forceinline__ void block_sums(uint32_t (&upto)[N], uint32_t (&total)[N], uint32_t (*part)[32])
+__device__ __forceinline__ void block_sums(const uint32_t (&own)[N], uint32_t (&before)[N], uint32_t (&total)[N], uint32_t (*part)[32])
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t upto[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) upto[k] = own[k];
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1)
 #pragma unroll
@@ -112,16 +115,19 @@ __device__ __forceinline__ void block_sums(uint32_t (&upto)[N], uint32_t (&total
             if (lane >= d) sum = plus(sum, o);
         }
         total[k] = __shfl_sync(0xffffffffu, sum, 31);
-        const uint32_t before = __shfl_sync(0xffffffffu, sum, warp ? warp - 1 : 0);
-        if (warp) upto[k] = plus(upto[k], before);
+        const uint32_t warps = __shfl_sync(0xffffffffu, sum, warp ? warp - 1 : 0), lanes = __shfl_up_sync(0xffffffffu, upto[k], 1);
+        before[k] = plus(warp ? warps : 0, lane ? lanes : 0);
     }
 }
 
+// ITEMS: sequences a thread (one launch: 1).
+template <int ITEMS>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
 {
+    constexpr int kAtOnce = kPlanThreads * ITEMS;
     __shared__ uint32_t part[4][32];
-    __shared__ PlanSeq seq[kPlanThreads];
-    __shared__ uint32_t given[kPlanThreads];  // pages returned by the sequences before (of this thousand)
+    __shared__ PlanSeq seq[ITEMS == 1 ? kPlanThreads : 1];
+    __shared__ uint32_t given[kAtOnce];  // pages returned by the sequences before (of these)
     const int tid = threadIdx.x, lane = tid & 31;
     pdl_trigger();
     pdl_wait();
@@ -131,47 +137,72 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
     uint32_t back0 = 0, need0 = 0, want0 = 0, took = 0;  // sums of the sequences before
     int rows0 = 0;
     const bool writes = blockIdx.x == 0;
-    for (int b0 = 0; b0 < p.seqs; b0 += kPlanThreads) {
-        const int b = b0 + tid;
-        const bool real = b < p.seqs;
-        int old = 0, n = 0, last = -1;
-        bool over = false;
-        if (real) {
-            old = max(p.lens[b], 0);
-            n = p.add[b];
-            over = p.done && p.done[b];
+    for (int b0 = 0; b0 < p.seqs; b0 += kAtOnce) {
+        const int b = b0 + tid * ITEMS;
+        int old[ITEMS], n[ITEMS], last = -1;
+        bool over[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const bool real = b + i < p.seqs;
+            old[i] = real ? max(p.lens[b + i], 0) : 0;
+            n[i] = real ? p.add[b + i] : 0;
+            over[i] = real && p.done && p.done[b + i];
         }
-        const int back = over ? min(pages_of(p, old), p.table_width) : 0;
-        const int length = over ? 0 : old, held = pages_of(p, length);
-        const bool fits = n >= 0 && (int64_t)length + n <= most;
-        if (p.alone && fits && n && held && held * (int64_t)p.page_size != length) last = p.table[(int64_t)b * p.table_width + held - 1];
-        const uint32_t need = fits ? pages_of(p, length + n) - held : 0;
-        uint32_t upto[3] = {(uint32_t)back, need, fits ? (uint32_t)n : 0u}, total[3];
-        block_sums<3>(upto, total, part);
-        const uint32_t asked = plus(need0, upto[1]);
-        const bool served = fits && (need == 0 || asked <= free) && (n == 0 || plus(want0, upto[2]) <= (uint32_t)p.tokens);
-        const int got = served ? n : 0;
-        uint32_t rows[1] = {(uint32_t)got}, all[1];
-        block_sums<1>(rows, all, part + 3);
-        const int first = rows0 + (int)rows[0] - got;
-        const int64_t at = taken + (asked - need);
-        const int base = at >= 0 && at < p.num_pages ? (int)at : ring_at(at, p.num_pages);
-        if (real) {
-            seq[tid] = {first, length, held, base, last};
-            if (served && need) took = asked;
-            if (writes) {
-                if (!served) set_status(p.status, MC_ERR_RANGE);
-                p.cu_q[b + 1] = first + got;
-                if (b == 0) p.cu_q[0] = 0;
-                (p.alone ? p.lens_out : p.length)[b] = length + got;
-                if (!p.alone) p.base[b] = base;
+        int length[ITEMS], held[ITEMS];
+        bool fits[ITEMS];
+        uint32_t back[ITEMS], need[ITEMS], upto[3] = {0, 0, 0}, total[3];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            back[i] = over[i] ? min(pages_of(p, old[i]), p.table_width) : 0;
+            length[i] = over[i] ? 0 : old[i];
+            held[i] = pages_of(p, length[i]);
+            fits[i] = n[i] >= 0 && (int64_t)length[i] + n[i] <= most;
+            need[i] = fits[i] ? pages_of(p, length[i] + n[i]) - held[i] : 0;
+            upto[0] = plus(upto[0], back[i]);
+            upto[1] = plus(upto[1], need[i]);
+            upto[2] = plus(upto[2], fits[i] ? n[i] : 0);
+        }
+        if (ITEMS == 1 && fits[0] && n[0] && held[0] && held[0] * (int64_t)p.page_size != length[0])
+            last = p.table[(int64_t)b * p.table_width + held[0] - 1];
+        uint32_t before[3];  // of the threads before, and then of the sequences before
+        block_sums<3>(upto, before, total, part);
+        uint32_t got[ITEMS], rows[1] = {0}, rows_before[1], all[1];
+        int base[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const bool real = b + i < p.seqs;
+            if (real) given[tid * ITEMS + i] = before[0];
+            const uint32_t asked = plus(plus(need0, before[1]), need[i]);
+            before[0] = plus(before[0], back[i]);
+            before[1] = plus(before[1], need[i]);
+            before[2] = plus(before[2], fits[i] ? n[i] : 0);
+            const bool served = fits[i] && (need[i] == 0 || asked <= free) && (n[i] == 0 || plus(want0, before[2]) <= (uint32_t)p.tokens);
+            got[i] = served ? n[i] : 0;
+            rows[0] += got[i];
+            const int64_t at = taken + (asked - need[i]);
+            base[i] = at >= 0 && at < p.num_pages ? (int)at : ring_at(at, p.num_pages);
+            if (served && need[i]) took = asked;
+            if (real && !served && writes) set_status(p.status, MC_ERR_RANGE);
+        }
+        block_sums<1>(rows, rows_before, all, part + 3);
+        int first = rows0 + (int)rows_before[0];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (b + i < p.seqs) {
+                if (ITEMS == 1) seq[tid] = {first, length[i], held[i], base[i], last};
+                if (writes) {
+                    p.cu_q[b + i + 1] = first + (int)got[i];
+                    if (b + i == 0) p.cu_q[0] = 0;
+                    (p.alone ? p.lens_out : p.length)[b + i] = length[i] + (int)got[i];
+                    if (!p.alone) p.base[b + i] = base[i];
+                }
             }
+            first += (int)got[i];
         }
         if (total[0]) {
             // finished sequences' pages, end to end; none overwrites a page that is still to be given out
-            given[tid] = upto[0] - back;
             __syncthreads();
-            const int count = min(kPlanThreads, p.seqs - b0);
+            const int count = min(kAtOnce, p.seqs - b0);
             const int ring0 = ring_at(returned + back0, p.num_pages);
             for (int64_t f = (int64_t)blockIdx.x * kPlanThreads + tid; f < total[0]; f += (int64_t)gridDim.x * kPlanThreads) {
                 int lo = 0, hi = count;  // the last sequence whose pages start at f or before it
@@ -190,7 +221,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
         need0 = plus(need0, total[1]);
         want0 = plus(want0, total[2]);
         rows0 += (int)all[0];
-        if (b0 + kPlanThreads < p.seqs) __syncthreads();  // (the sums and places have been read)
+        if (b0 + kAtOnce < p.seqs) __syncthreads();  // (the sums and places have been read)
     }
     if (!writes) return;
     // the last sequence that took pages has the largest sum
@@ -207,19 +238,21 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
             out[1] = to <= end ? to : max(returned, end);
         }
     }
-    if (!p.alone) return;
-    for (int t = tid; t < p.tokens; t += kPlanThreads) {
-        if (t >= rows0) {
-            plan_padding(p, t);
-            continue;
+    if constexpr (ITEMS == 1) {
+        if (!p.alone) return;
+        for (int t = tid; t < p.tokens; t += kPlanThreads) {
+            if (t >= rows0) {
+                plan_padding(p, t);
+                continue;
+            }
+            int lo = 0, hi = p.seqs;  // the last sequence that starts at t or before it
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (seq[mid].first <= t) lo = mid;
+                else hi = mid;
+            }
+            plan_token(p, t, lo, seq[lo]);
         }
-        int lo = 0, hi = p.seqs;  // the last sequence that starts at t or before it
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (seq[mid].first <= t) lo = mid;
-            else hi = mid;
-        }
-        plan_token(p, t, lo, seq[lo]);
     }
 }
 
@@ -322,7 +355,8 @@ int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, 
     p.alone = seqs <= kPlanThreads && tokens <= kPlanFew && (!done || (int64_t)seqs * table_width <= kPlanEntries);
     cudaStream_t st = (cudaStream_t)stream;
     profile_begin(kKPlan, st);
-    cudaError_t e = launch_k(plan_kernel, dim3(p.alone || !done ? 1 : kPlanBlocks), dim3(kPlanThreads), 0, st, p);
+    auto k = seqs <= kPlanThreads ? plan_kernel<1> : plan_kernel<4>;
+    cudaError_t e = launch_k(k, dim3(p.alone || !done ? 1 : kPlanBlocks), dim3(kPlanThreads), 0, st, p);
     if (e == cudaSuccess && !p.alone) {
         const int64_t per = 256 * kPlanPer, blocks = (tokens + per - 1) / per;
         e = launch_k(plan_tokens_kernel, dim3((unsigned)(blocks ? blocks : 1)), dim3(256), 0, st, p);

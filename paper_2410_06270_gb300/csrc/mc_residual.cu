@@ -24,7 +24,9 @@ struct ResidualParams {
     int gate_col;
     float scale, residual_scale, eps;
     uint16_t *out, *x;
+    int narrow;  // operands whose rows do not start at 16 bytes: bits y, h, post, pre, gate, out, x
 };
+enum { kY = 1, kH = 2, kPost = 4, kPre = 8, kGate = 16, kOut = 32, kX = 64 };
 
 template <bool BF16>
 __device__ __forceinline__ float load1(const uint16_t *p)
@@ -35,6 +37,30 @@ template <bool BF16>
 __device__ __forceinline__ uint16_t store1(float v)
 {
     return (uint16_t)pack2<BF16>(v, 0.f);
+}
+
+// Eight columns, by one access or (where the operand's rows are not aligned) one by one.
+template <bool ALIGNED>
+__device__ __forceinline__ uint4 load8(const ResidualParams &p, int which, const uint16_t *src)
+{
+    if (ALIGNED || !(p.narrow & which)) return *reinterpret_cast<const uint4 *>(src);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = src[2 * k] | (uint32_t)src[2 * k + 1] << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <bool ALIGNED>
+__device__ __forceinline__ void store8(const ResidualParams &p, int which, uint16_t *dst, const uint32_t (&w)[4])
+{
+    if (ALIGNED || !(p.narrow & which)) {
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        dst[2 * k] = (uint16_t)w[k];
+        dst[2 * k + 1] = (uint16_t)(w[k] >> 16);
+    }
 }
 
 // 1 / sqrt of a row's mean square, from each of its threads' part.
@@ -52,8 +78,8 @@ __device__ __forceinline__ float row_rms(const ResidualParams &p, float ss, floa
 
 __device__ __forceinline__ float value(const ResidualParams &p, float y, float h, float gate) { return fmaf(p.residual_scale, h, p.scale * (gate * y)); }
 
-// Rows of whole 16-byte chunks, PER of them a thread.
-template <int PER, bool BF16>
+// Rows of whole chunks of 8 columns, PER of them a thread.
+template <int PER, bool BF16, bool ALIGNED>
 __global__ void __launch_bounds__(256) residual_kernel(const ResidualParams p)
 {
     __shared__ float red[2][16];  // (warps of no row read past the eighth)
@@ -69,9 +95,9 @@ __global__ void __launch_bounds__(256) residual_kernel(const ResidualParams p)
     for (int i = 0; i < PER; ++i) {
         const int c = first + step * i;
         const bool in = real && c < n8;
-        gate[i] = gated && in ? *reinterpret_cast<const uint4 *>(p.gate + t * p.gate_row + 8 * c) : make_uint4(0, 0, 0, 0);
-        y[i] = in ? *reinterpret_cast<const uint4 *>(p.y + t * p.y_stride + 8 * c) : make_uint4(0, 0, 0, 0);
-        h[i] = in ? *reinterpret_cast<const uint4 *>(p.h + t * p.h_stride + 8 * c) : make_uint4(0, 0, 0, 0);
+        gate[i] = gated && in ? load8<ALIGNED>(p, kGate, p.gate + t * p.gate_row + 8 * c) : make_uint4(0, 0, 0, 0);
+        y[i] = in ? load8<ALIGNED>(p, kY, p.y + t * p.y_stride + 8 * c) : make_uint4(0, 0, 0, 0);
+        h[i] = in ? load8<ALIGNED>(p, kH, p.h + t * p.h_stride + 8 * c) : make_uint4(0, 0, 0, 0);
     }
     const float whole = p.gate && !p.gate_col && real ? load1<BF16>(p.gate + t * p.gate_row) : 1.f;
     float inv = 1.f;
@@ -94,7 +120,7 @@ __global__ void __launch_bounds__(256) residual_kernel(const ResidualParams p)
     for (int i = 0; i < PER; ++i) {
         const int c = first + step * i;
         if (!real || c >= n8) continue;
-        const uint4 post = p.post ? *reinterpret_cast<const uint4 *>(p.post + 8 * c) : make_uint4(0, 0, 0, 0);
+        const uint4 post = p.post ? load8<ALIGNED>(p, kPost, p.post + 8 * c) : make_uint4(0, 0, 0, 0);
         const uint32_t w[4] = {y[i].x, y[i].y, y[i].z, y[i].w}, r[4] = {h[i].x, h[i].y, h[i].z, h[i].w};
         const uint32_t pw[4] = {post.x, post.y, post.z, post.w}, g[4] = {gate[i].x, gate[i].y, gate[i].z, gate[i].w};
         uint32_t o[4];
@@ -113,7 +139,7 @@ __global__ void __launch_bounds__(256) residual_kernel(const ResidualParams p)
             ss = fmaf(f.y, f.y, ss);
         }
         h[i] = make_uint4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<uint4 *>(p.out + t * p.out_stride + 8 * c) = h[i];
+        store8<ALIGNED>(p, kOut, p.out + t * p.out_stride + 8 * c, o);
     }
     if (!p.pre) return;
     inv = row_rms(p, ss, red[1], w0);
@@ -121,7 +147,7 @@ __global__ void __launch_bounds__(256) residual_kernel(const ResidualParams p)
     for (int i = 0; i < PER; ++i) {
         const int c = first + step * i;
         if (!real || c >= n8) continue;
-        const uint4 pre = *reinterpret_cast<const uint4 *>(p.pre + 8 * c);
+        const uint4 pre = load8<ALIGNED>(p, kPre, p.pre + 8 * c);
         const uint32_t w[4] = {h[i].x, h[i].y, h[i].z, h[i].w}, a[4] = {pre.x, pre.y, pre.z, pre.w};
         uint32_t o[4];
 #pragma unroll
@@ -129,13 +155,71 @@ __global__ void __launch_bounds__(256) residual_kernel(const ResidualParams p)
             const float2 f = unpack2<BF16>(w[k]), g = unpack2<BF16>(a[k]);
             o[k] = pack2<BF16>(f.x * inv * g.x, f.y * inv * g.y);
         }
-        *reinterpret_cast<uint4 *>(p.x + t * p.x_stride + 8 * c) = make_uint4(o[0], o[1], o[2], o[3]);
+        store8<ALIGNED>(p, kX, p.x + t * p.x_stride + 8 * c, o);
     }
 }
 
-// Any row: odd widths and alignments, element by element, a block a row.  h' is read back by the thread that
-// wrote it.
-template <bool BF16>
+// A thread's k-th column, as mc_rmsnorm has them: its 8-element chunks in turn where the width is a multiple of 8, else
+// every 256th.
+template <bool CHUNKS>
+__device__ __forceinline__ int narrow_col(int first, int k)
+{
+    return CHUNKS ? 8 * (first + 256 * (k >> 3)) + (k & 7) : first + 256 * k;
+}
+
+// Rows that are not whole chunks, element by element, up to 256 PER columns; rows of up to 256 share a block, a warp for
+// each 32 columns.  Bound by the accesses of 2 bytes: 8000 rows of 999 32 us (of 1000 15).
+template <int PER, bool BF16>
+__global__ void __launch_bounds__(256) residual_narrow_kernel(const ResidualParams p)
+{
+    __shared__ float red[2][16];
+    pdl_trigger();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, sub = p.warps == 8 ? 0 : warp / p.warps, w0 = sub * p.warps, first = threadIdx.x - 32 * w0;
+    const int64_t t = (int64_t)blockIdx.x * p.rows + sub;
+    const int end = sub < p.rows && t < p.T ? p.H : 0;
+    const uint16_t *yr = p.y + t * p.y_stride, *hr = p.h + t * p.h_stride;
+    uint16_t y[PER], h[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = first + 256 * k;
+        y[k] = h[k] = 0;
+        if (c < end) y[k] = yr[c], h[k] = hr[c];
+    }
+    float inv = 1.f, ss = 0.f;
+    if (p.post) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const float v = load1<BF16>(y + k);
+            ss = fmaf(v, v, ss);
+        }
+        inv = row_rms(p, ss, red[0], w0);
+    }
+    uint16_t *out = p.out + t * p.out_stride, *x = p.x + t * p.x_stride;
+    ss = 0.f;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = first + 256 * k;
+        if (c >= end) continue;
+        float u = load1<BF16>(y + k);
+        if (p.post) u = u * inv * load1<BF16>(p.post + c);
+        const float g = p.gate ? load1<BF16>(p.gate + t * p.gate_row + (p.gate_col ? c : 0)) : 1.f;
+        h[k] = store1<BF16>(value(p, u, load1<BF16>(h + k), g));
+        out[c] = h[k];
+        const float v = load1<BF16>(h + k);
+        ss = fmaf(v, v, ss);
+    }
+    if (!p.pre) return;
+    inv = row_rms(p, ss, red[1], w0);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = first + 256 * k;
+        if (c < end) x[c] = store1<BF16>(load1<BF16>(h + k) * inv * load1<BF16>(p.pre + c));
+    }
+}
+
+// Wider rows, a block a row; h' is read back by the thread that wrote it.
+template <bool CHUNKS, bool BF16>
 __global__ void __launch_bounds__(256) residual_any_kernel(const ResidualParams p)
 {
     __shared__ float red[2][16];
@@ -144,16 +228,13 @@ __global__ void __launch_bounds__(256) residual_any_kernel(const ResidualParams 
     const int64_t t = blockIdx.x;
     const uint16_t *y = p.y + t * p.y_stride, *h = p.h + t * p.h_stride;
     uint16_t *out = p.out + t * p.out_stride, *x = p.x + t * p.x_stride;
-    // column k of this thread: its 8-element chunks in turn, or every 256th
-    const bool chunks = p.H % 8 == 0;
-    const int count = chunks ? (p.H / 8 - (int)threadIdx.x + 255) / 256 * 8 : (p.H - (int)threadIdx.x + 255) / 256;
-    auto col = [&](int k) { return chunks ? 8 * ((int)threadIdx.x + 256 * (k >> 3)) + (k & 7) : (int)threadIdx.x + 256 * k; };
+    const int tid = threadIdx.x, count = CHUNKS ? (p.H / 8 - tid + 255) / 256 * 8 : (p.H - tid + 255) / 256;
     float inv = 1.f;
     if (p.post) {
         float ss = 0.f;
 #pragma unroll 8
         for (int k = 0; k < count; ++k) {
-            const float v = load1<BF16>(y + col(k));
+            const float v = load1<BF16>(y + narrow_col<CHUNKS>(tid, k));
             ss = fmaf(v, v, ss);
         }
         inv = row_rms(p, ss, red[0], 0);
@@ -161,35 +242,52 @@ __global__ void __launch_bounds__(256) residual_any_kernel(const ResidualParams 
     float ss = 0.f;
 #pragma unroll 8
     for (int k = 0; k < count; ++k) {
-        const int c = col(k);
+        const int c = narrow_col<CHUNKS>(tid, k);
         float u = load1<BF16>(y + c);
         if (p.post) u = u * inv * load1<BF16>(p.post + c);
         const float g = p.gate ? load1<BF16>(p.gate + t * p.gate_row + (p.gate_col ? c : 0)) : 1.f;
-        out[c] = store1<BF16>(value(p, u, load1<BF16>(h + c), g));
-        const float v = load1<BF16>(out + c);
+        const uint16_t o = store1<BF16>(value(p, u, load1<BF16>(h + c), g));
+        out[c] = o;
+        const float v = load1<BF16>(&o);
         ss = fmaf(v, v, ss);
     }
     if (!p.pre) return;
     inv = row_rms(p, ss, red[1], 0);
 #pragma unroll 8
     for (int k = 0; k < count; ++k) {
-        const int c = col(k);
+        const int c = narrow_col<CHUNKS>(tid, k);
         x[c] = store1<BF16>(load1<BF16>(out + c) * inv * load1<BF16>(p.pre + c));
     }
 }
 
-template <bool BF16>
-static cudaError_t launch_residual(ResidualParams p, bool wide, cudaStream_t st)
+template <bool BF16, bool ALIGNED>
+static cudaError_t launch_chunks(ResidualParams p, cudaStream_t st)
 {
-    p.rows = 1;
-    p.warps = 8;
-    if (!wide) return launch_k(residual_any_kernel<BF16>, dim3(p.T), dim3(256), 0, st, p);
     if (p.H < 2048) {
         p.warps = (p.H + 255) / 256;
         p.rows = 8 / p.warps;
     }
-    auto k = p.H <= 2048 ? residual_kernel<1, BF16> : p.H <= 4096 ? residual_kernel<2, BF16>
-             : p.H <= 8192 ? residual_kernel<4, BF16> : residual_kernel<8, BF16>;
+    auto k = p.H <= 2048 ? residual_kernel<1, BF16, ALIGNED> : p.H <= 4096 ? residual_kernel<2, BF16, ALIGNED>
+             : p.H <= 8192 ? residual_kernel<4, BF16, ALIGNED> : residual_kernel<8, BF16, ALIGNED>;
+    return launch_k(k, dim3((unsigned)((p.T + p.rows - 1) / p.rows)), dim3(256), 0, st, p);
+}
+
+template <bool BF16>
+static cudaError_t launch_residual(ResidualParams p, cudaStream_t st)
+{
+    p.rows = 1;
+    p.warps = 8;
+    if (p.H % 8 == 0) {
+        if (p.H > 16384) return launch_k(residual_any_kernel<true, BF16>, dim3(p.T), dim3(256), 0, st, p);
+        return p.narrow ? launch_chunks<BF16, false>(p, st) : launch_chunks<BF16, true>(p, st);
+    }
+    if (p.H <= 256) {
+        p.warps = (p.H + 31) / 32;
+        p.rows = 8 / p.warps;
+    }
+    // Wider rows stay in registers only where they are few: 4096 rows of 4099 columns 95 us, read again 68; 16 of them 9.6 and 12.8.
+    auto k = p.H <= 256 ? residual_narrow_kernel<1, BF16> : p.H <= 2048 ? residual_narrow_kernel<8, BF16>
+             : p.H <= 8192 && p.T <= 304 ? residual_narrow_kernel<32, BF16> : residual_any_kernel<false, BF16>;
     return launch_k(k, dim3((unsigned)((p.T + p.rows - 1) / p.rows)), dim3(256), 0, st, p);
 }
 
@@ -209,21 +307,25 @@ extern "C" int mc_residual_norm(const mc_residual_norm_args *a, void *stream)
     if (a->T == 0) return MC_OK;
     if (!a->y || !a->h || !a->h_out || (a->pre_norm && !a->x)) return set_error(MC_ERR_INVALID_ARG, "NULL pointer argument");
     const void *ptrs[7] = {a->y, a->h, a->post_norm, a->pre_norm, a->gate, a->h_out, a->pre_norm ? a->x : nullptr};
-    bool wide = a->H % 8 == 0 && a->H <= 16384;
+    int narrow = 0;
     for (int i = 0; i < 7; ++i) {
         if (!aligned(ptrs[i], 2)) return set_error(MC_ERR_INVALID_ARG, "misaligned pointer argument");
-        wide = wide && (aligned(ptrs[i], 16) || (i == 4 && a->gate_col == 0));
+        if (!aligned(ptrs[i], 16)) narrow |= 1 << i;
     }
-    const int64_t strides[4] = {a->y_stride, a->h_stride, a->h_out_stride, a->pre_norm ? a->x_stride : a->H};
-    for (int64_t s : strides) {
-        if (s < a->H && a->T > 1) return set_error(MC_ERR_INVALID_ARG, "row stride %lld of %d columns", (long long)s, a->H);
-        wide = wide && (s % 8 == 0 || a->T == 1);
+    const struct {
+        int which;
+        int64_t stride;
+    } rows[4] = {{kY, a->y_stride}, {kH, a->h_stride}, {kOut, a->h_out_stride}, {kX, a->pre_norm ? a->x_stride : a->H}};
+    for (const auto &r : rows) {
+        if (r.stride < a->H && a->T > 1) return set_error(MC_ERR_INVALID_ARG, "row stride %lld of %d columns", (long long)r.stride, a->H);
+        if (r.stride % 8 && a->T > 1) narrow |= r.which;
     }
     if (a->gate) {
         if (a->gate_col != 0 && a->gate_col != 1) return set_error(MC_ERR_INVALID_ARG, "gate_col %d (0 or 1)", a->gate_col);
         if (a->gate_row < 0) return set_error(MC_ERR_INVALID_ARG, "gate_row %lld", (long long)a->gate_row);
-        wide = wide && (a->gate_col == 0 || a->gate_row % 8 == 0 || a->T == 1);
+        if (a->gate_row % 8 && a->T > 1) narrow |= kGate;
     }
+    if (!a->gate || a->gate_col == 0) narrow &= ~kGate;  // (a gate of one value a row is read as such)
     if (a->x && a->pre_norm && a->x == a->h_out) return set_error(MC_ERR_INVALID_ARG, "x must not be h_out");
     if (a->x && a->pre_norm && a->x == a->h) return set_error(MC_ERR_INVALID_ARG, "x must not be h");
     ResidualParams p = {};
@@ -245,9 +347,10 @@ extern "C" int mc_residual_norm(const mc_residual_norm_args *a, void *stream)
     p.eps = a->eps;
     p.out = (uint16_t *)a->h_out;
     p.x = (uint16_t *)a->x;
+    p.narrow = narrow;
     cudaStream_t st = (cudaStream_t)stream;
     profile_begin(kKResidual, st);
-    const cudaError_t e = a->dtype == MC_BF16 ? launch_residual<true>(p, wide, st) : launch_residual<false>(p, wide, st);
+    const cudaError_t e = a->dtype == MC_BF16 ? launch_residual<true>(p, st) : launch_residual<false>(p, st);
     profile_end(kKResidual, st);
     if (e != cudaSuccess) return set_error(MC_ERR_CUDA, "residual launch: %s", cudaGetErrorString(e));
     return MC_OK;

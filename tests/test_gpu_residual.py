@@ -41,7 +41,8 @@ def _check(y, h, got_h, got_x, pre, post, gate, scale, rs, eps):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("T,H", [(1, 1), (2, 7), (3, 64), (5, 99), (1, 256), (9, 264), (4, 1000), (7, 2048), (3, 2056), (2, 4096), (1, 8192),
-                                 (2, 16384), (2, 16392), (1, 65536), (3, 999), (33, 512)])
+                                 (2, 16384), (2, 16392), (1, 65536), (3, 999), (33, 512), (310, 4099),
+                                 (304, 2051), (3, 8191), (2, 8193)])
 @pytest.mark.parametrize("gate,post,pre", [("none", False, True), ("channel", True, True), ("token", True, False), ("element", False, True)])
 def test_matches_its_definition(mc, dtype, T, H, gate, post, pre):
     g = torch.Generator(device="cuda").manual_seed(T * H)
@@ -64,7 +65,8 @@ def test_matches_its_definition(mc, dtype, T, H, gate, post, pre):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("H,wide,off", [(64, 8, 8), (64, 8, 0), (64, 3, 1), (999, 1, 0), (4096, 64, 32), (4096, 1, 1), (512, 0, 4)])
+@pytest.mark.parametrize("H,wide,off", [(64, 8, 8), (64, 8, 0), (64, 3, 1), (999, 1, 0), (4096, 64, 32), (4096, 1, 1), (512, 0, 4), (8192, 3, 0),
+                                        (16384, 1, 3)])
 def test_strides_and_alignments(mc, dtype, H, wide, off):
     """Rows of wider tensors, aligned and not, each operand alike, and what lies beside them is left alone."""
     T = 6
@@ -86,6 +88,23 @@ def test_strides_and_alignments(mc, dtype, H, wide, off):
     a, b = mc.residual_norm(y.contiguous(), h.contiguous(), pre_norm=pre.clone(), post_norm=post.clone(), gate=gate.contiguous())
     if H % 8 == 0:
         assert torch.equal(a, h_out) and torch.equal(b, x)
+
+
+@pytest.mark.parametrize("which", range(7))
+def test_one_operand_off_its_alignment(mc, which):
+    """The others keep their wide accesses; the result is that of aligned copies, bit for bit."""
+    T, H = 5, 1000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    full = [torch.randn(T, H, generator=g, device="cuda").to(torch.bfloat16) for _ in range(3)] + [torch.randn(H, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    y, h, gate, post, pre = full
+    want = mc.residual_norm(y, h, pre_norm=pre, post_norm=post, gate=gate)
+    outs = [torch.empty_like(y), torch.empty_like(y)]
+    ops = full + outs
+    odd = torch.empty(ops[which].numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view(ops[which].shape)
+    ops[which] = odd.copy_(ops[which])
+    y, h, gate, post, pre, a, b = ops
+    got = mc.residual_norm(y, h, pre_norm=pre, post_norm=post, gate=gate, h_out=a, x=b)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 @pytest.mark.parametrize("T,H", [(5, 64), (3, 256), (4, 1000), (2, 4096), (3, 8192), (2, 16392), (3, 77)])
