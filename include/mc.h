@@ -462,7 +462,7 @@ size_t mc_kv_plan_workspace_size(int seqs);
  *            page * page_size + position % page_size; -1 for rows from cu_q[seqs] on, and as the slot of a token
  *            whose page is outside the pool (MC_ERR_RANGE)
  *   state_out int64 [2]         the counts after the call (may be pool->state)
- * lens_out, table and cu_q are what mc_kv_batch takes.  A page that would not fit in the ring is not returned
+ * (nothing for seqs == 0).  lens_out, table and cu_q are what mc_kv_batch takes.  A page that would not fit in the ring is not returned
  * (MC_ERR_RANGE).  Without committing (state_out and lens_out apart from the inputs) the same call may be
  * made again: it writes the same entries. */
 int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, const uint8_t *done, int seqs, int tokens,

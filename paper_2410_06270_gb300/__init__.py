@@ -816,13 +816,13 @@ def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=Non
     if workspace is None:
         workspace = kv_plan_workspace(seqs, dev)
     ws = _status(workspace, pool, "pool")
-    empty = torch.empty
+    empty = torch.empty if seqs else torch.zeros  # (of no sequence nothing is written)
     if lens_out is None:
         lens_out = empty(seqs, dtype=torch.int32, device=dev)
     cu_q = empty(seqs + 1, dtype=torch.int32, device=dev)
     pos = empty(tokens, dtype=torch.int32, device=dev) if positions else None
     slot = empty(tokens, dtype=torch.int64, device=dev) if slots else None
-    state = pool.state if commit else empty(2, dtype=torch.int64, device=dev)
+    state = pool.state if commit else pool.state.clone() if not seqs else empty(2, dtype=torch.int64, device=dev)
     rc = load().mc_kv_plan(pool._ref, lens.data_ptr(), add.data_ptr(), None if done is None else done.data_ptr(), seqs, tokens,
                            table.data_ptr(), table.shape[1], lens_out.data_ptr(), cu_q.data_ptr(), pos.data_ptr() if positions else None,
                            slot.data_ptr() if slots else None, state.data_ptr(), ws, workspace.numel() * workspace.element_size(), _stream())

@@ -164,11 +164,11 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
         // not for every 256 rows.  Unpacked / in the kernel: 8192 tokens of a group of 4 343 / 524 us, 4096 116 / 162, 1024
         // 40 / 41, 509 over 30000 keys 208 / 258; on the other side 256 over 30000 138 / 141, 8 x 256 over 1000
         // 69 / 70, 8 x 128 over 2000 77 / 68, 128 over 30000 106 / 84.
-        const int64_t pages = (int64_t)batch->seqs * batch->table_width;
+        const double reach = (double)batch->seqs * batch->table_width * cache->kv_heads * cache->page_size * cache->head_dim * 4;
+        const bool few = reach < (double)kUnpackBytes && batch->seqs <= 65535;  // (the sizes below are small numbers)
+        const int64_t pages = few ? (int64_t)batch->seqs * batch->table_width : 0;
         const int64_t side = pages * cache->kv_heads * cache->page_size * cache->head_dim * 2, table = (pages * 4 + 255) & ~(int64_t)255;
-        const double most = (double)batch->seqs * batch->table_width * cache->kv_heads * cache->page_size * cache->head_dim * 4;
-        if (rows > kUnpackRows && batch->seqs <= 65535 && cache->kv_heads <= 65535 && most < (double)kUnpackBytes &&
-            need + 2 * side + table <= (int64_t)ws_bytes) {
+        if (few && rows > kUnpackRows && (int64_t)need + 2 * side + table <= (int64_t)ws_bytes) {
             uint8_t *to = (uint8_t *)workspace + need;
             Unpack4Params u = {p.c, p.b, p.window, (uint16_t *)(to + table), (uint16_t *)(to + table + side), (int32_t *)to, p.status};
             if ((rc = launch_unpack4(u, cache->head_dim, bf16, (cudaStream_t)stream))) return rc;

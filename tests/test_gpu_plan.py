@@ -196,6 +196,32 @@ def test_a_preview_changes_nothing_but_may_be_repeated(mc):
     assert only.positions is None and only.slots is None
 
 
+def test_a_step_without_sequences(mc):
+    pool = mc.KVPool(4, 16)
+    none, table = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, 3, dtype=torch.int32, device="cuda")
+    p = mc.kv_plan(pool, table, none, none, commit=False)
+    assert p.cu_q.tolist() == [0] and p.state.tolist() == [0, 4] and p.lens.numel() == 0 == p.slots.numel()
+
+
+def test_another_stream_and_other_sizes_through_one_workspace(mc):
+    """Steps of one launch and of two in turn, on a stream of their own."""
+    a = Account(1500, 40, 9000, 16, 19)
+    d = Device(mc, a)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for add in ([1] * 1500, [3 + b % 5 for b in range(1500)], [1] * 1500):
+            want = a.step(add, None, sum(add))
+            plan = d.step(add, None, sum(add))
+            s.synchronize()
+            d.same(a, plan, want)
+    b = Account(5, 40, 300, 16, 23)
+    e = Device(mc, b)
+    e.ws = d.ws  # (one for up to 1500 sequences)
+    for add in ([600] * 5, [1] * 5):
+        e.same(b, e.step(add, None, sum(add)), b.step(add, None, sum(add)))
+
+
 def test_replayed_steps(mc):
     """A captured step, in place, replayed: each replay is the next step."""
     a = Account(20, 6, 200, 16, 13)
