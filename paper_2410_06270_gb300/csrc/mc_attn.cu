@@ -99,7 +99,8 @@ static bool countable(const mc_kv_cache *c, const mc_kv_batch *b, int group)
 }
 
 constexpr int64_t kUnpackBytes = (int64_t)256 << 20;  // of a workspace for the 4-bit cache: keys and values in 16 bits
-constexpr int kUnpackRows = 1024;  // (token, head of the group) of a sequence in the mean, more than
+constexpr int kUnpackRows = 1024;  // (token, head of the group) of a sequence in the mean
+constexpr int kUnpackUnits = 4096;  // of 256 rows and 128 keys, as far as the tables reach
 
 static size_t workspace_size(int head_dim) { return (256 + std::max(decode_part_bytes(head_dim), prefill_part_bytes(head_dim)) + 255) & ~(size_t)255; }
 
@@ -160,15 +161,17 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
     const bool bf16 = cache->dtype == MC_BF16;
     if (rows <= (q4 || p.cap > 0.f ? kFewRowsCap : kFewRows)) return launch_decode(p, cache->head_dim, bf16, q4, (int)rows, (cudaStream_t)stream);
     if (q4) {
-        // Prompts of many rows: their keys are unpacked once, where the workspace holds what the batch's tables reach,
-        // not for every 256 rows.  Unpacked / in the kernel: 8192 tokens of a group of 4 343 / 524 us, 4096 116 / 162, 1024
-        // 40 / 41, 509 over 30000 keys 208 / 258; on the other side 256 over 30000 138 / 141, 8 x 256 over 1000
-        // 69 / 70, 8 x 128 over 2000 77 / 68, 128 over 30000 106 / 84.
+        // Prompts of many rows, and enough of them: their keys are unpacked once, where the workspace holds what the
+        // batch's tables reach, not for every 256 rows.  Unpacked / in the kernel, us: 3000 tokens of a group of 4 on 8 heads
+        // (9000 units) 74 / 102, 509 over 30000 keys (15000) 194 / 250, 256 over 30000 (7500) 126 / 134, 8 x 300 over 4000
+        // (10200) 172 / 188, 2048 (4100) 67 / 67; 1024 (1000) 39 / 34, 8 x 256 over 1000 (2000) 71 / 61, 300 over 8000 (2500)
+        // 67 / 58; and 128 rows short of that, 128 over 30000 keys (3800) 106 / 84.
         const double reach = (double)batch->seqs * batch->table_width * cache->kv_heads * cache->page_size * cache->head_dim * 4;
         const bool few = reach < (double)kUnpackBytes && batch->seqs <= 65535;  // (the sizes below are small numbers)
         const int64_t pages = few ? (int64_t)batch->seqs * batch->table_width : 0;
         const int64_t side = pages * cache->kv_heads * cache->page_size * cache->head_dim * 2, table = (pages * 4 + 255) & ~(int64_t)255;
-        if (few && rows > kUnpackRows && (int64_t)need + 2 * side + table <= (int64_t)ws_bytes) {
+        const double units = (double)batch->tokens * p.group / 256 * cache->kv_heads * ((double)batch->table_width * cache->page_size / 128);
+        if (few && rows >= kUnpackRows && units >= kUnpackUnits && (int64_t)need + 2 * side + table <= (int64_t)ws_bytes) {
             uint8_t *to = (uint8_t *)workspace + need;
             Unpack4Params u = {p.c, p.b, p.window, (uint16_t *)(to + table), (uint16_t *)(to + table + side), (int32_t *)to, p.status};
             if ((rc = launch_unpack4(u, cache->head_dim, bf16, (cudaStream_t)stream))) return rc;

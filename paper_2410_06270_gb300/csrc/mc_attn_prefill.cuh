@@ -33,11 +33,12 @@
 // tile is whole tokens of the group's heads, else cp.async).
 // Tensor memory: S (and P) of tile t at column 128 t, O at 256 + 128 t.
 //
-// Q4, the cache in 4 bits: warps 12-15 read the codes and write a tile as exact numbers of the type, which takes them
-// 2300 cycles a tile of 128 keys (1000 to convert, in 310 instructions a warp; the rest finding pages, loads and
-// waits), two tiles a unit: more than the products take, so prompts of many rows have their keys unpacked
-// before (mc_kv.cu) and come here as a 16-bit cache.  64 tokens over 30000 keys 51 us, 256 138.  What it hangs on is
-// registers: with 212 bytes spilled to a local memory that has no L1 left 64 tokens over 30000 keys took 76 us.
+// Q4, the cache in 4 bits: warps 12-15 read the codes and write a tile as exact numbers of the type, in 310 instructions
+// a warp and about 2000 cycles a tile of 128 keys, two tiles a unit: more than the products take where those are back to
+// back.  Beside the 16-bit cache: 64 tokens over 30000 keys 51 / 48 us, 16 x 16 over 4000 71 / 60, 1000 tokens 33 / 29, 240
+// over 30000 134 / 96, 4096 tokens 155 / 104: the last have their keys unpacked before (mc_kv.cu) and come here as a 16-bit
+// cache.  It hangs on registers: with 212 bytes spilled to a local memory that has no L1 left 64 tokens over 30000
+// keys took 76 us.
 #pragma once
 #include <math.h>
 
@@ -406,7 +407,7 @@ __device__ __forceinline__ void pf_copy16z(uint32_t dst, const void *src, bool r
 // Q4 has a warpgroup more.
 template <bool Q4>
 struct PfRegs {
-    static constexpr int kAll = Q4 ? 128 : 168, kSoft = Q4 ? 184 : 208, kRest = Q4 ? 48 : 80, kUnpack = 96;
+    static constexpr int kAll = Q4 ? 128 : 168, kSoft = Q4 ? 192 : 208, kRest = Q4 ? 48 : 80, kUnpack = 80;
     static_assert(2 * kSoft + kRest + (Q4 ? kUnpack : 0) <= (Q4 ? 4 : 3) * kAll, "register shares");
     static __device__ __forceinline__ void take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoft)); }
     static __device__ __forceinline__ void give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRest)); }
@@ -528,38 +529,34 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 // ------------------------------------------------------------------ kernel --
 
 // QUEUE: the batch may have the items for a queue (the host's bound), so the kernel looks at them.
-// A lane's part of 32 keys (a warp's) of the 4-bit cache: 16-byte chunks of codes, as they lie, kPer of them, 32 / kPer
-// keys apart; and into a tile, as exact numbers of the type, to where a copy would have put them (a group's 64 columns in
-// 8 chunks of 16 bytes, swizzled).  The keys lie in two runs of 16, each in one page.
+// Where a warp's 32 keys of a unit lie in either side of the 4-bit cache: two runs of 16, each in one page.  Byte offsets of
+// the lane's first chunk of codes in each run (negative: no such page, zeros), and of the words of the lane's own key
+// (negative: zeros, as for keys that no row sees).
+struct PfPlace {
+    int64_t codes[2], words;
+};
+
+// A lane's part of them: 16-byte chunks of codes, as they lie, kPer of them, 32 / kPer keys apart, and its key's words; and
+// into a tile, as exact numbers of the type, to where a copy would have put them (a group's 64 columns in 8 chunks of 16
+// bytes, swizzled).
 template <int D>
 struct PfRaw {
     static constexpr int kPer = D / 32, kChunks = D / 32, kStep = 32 / kPer;
     uint4 w[kPer];
-    uint32_t word[kPer];
+    uint32_t words;
 
-    // page and row of each run (page < 0: zeros, that is scales of 0); keys outside [from, to), counted from the
-    // warp's first, are zeros too
-    __device__ __forceinline__ void load(const KvView &c, const uint16_t *side, const int (&page)[2], const int (&row)[2], int h, int from, int to, int lane)
+    __device__ __forceinline__ void load(const uint16_t *side, const PfPlace &at)
     {
-        const int block_bytes = c.page_size * kv4_row_bytes(D);
+        const uint8_t *base = reinterpret_cast<const uint8_t *>(side);
 #pragma unroll
-        for (int run = 0; run < 2; ++run) {
-            const uint8_t *block = reinterpret_cast<const uint8_t *>(side) + (max(page[run], 0) * c.page_stride + (int64_t)h * block_bytes);
-            const uint8_t *codes = block + (row[run] + lane / kChunks) * kv4_code_bytes(D) + 16 * (lane % kChunks);
-            const uint8_t *words = block + c.page_size * kv4_code_bytes(D) + (row[run] + lane / kChunks) * kv4_word_bytes(D);
-#pragma unroll
-            for (int k = 0; k < kPer / 2; ++k) {
-                const int i = run * (kPer / 2) + k, key = lane / kChunks + kStep * i;
-                w[i] = make_uint4(0, 0, 0, 0);
-                word[i] = 0;
-                if (page[run] >= 0) {
-                    w[i] = __ldg(reinterpret_cast<const uint4 *>(codes + k * kStep * kv4_code_bytes(D)));
-                    if (key >= from && key < to)
-                        word[i] = D == 128 ? __ldg(reinterpret_cast<const uint32_t *>(words + k * kStep * kv4_word_bytes(D)))
-                                           : __ldg(reinterpret_cast<const uint16_t *>(words + k * kStep * kv4_word_bytes(D)));
-                }
-            }
+        for (int i = 0; i < kPer; ++i) {
+            const int run = i / (kPer / 2), k = i % (kPer / 2);
+            w[i] = at.codes[run] < 0 ? make_uint4(0, 0, 0, 0)
+                                     : __ldg(reinterpret_cast<const uint4 *>(base + at.codes[run] + k * kStep * kv4_code_bytes(D)));
         }
+        words = at.words < 0 ? 0u
+                : D == 128   ? __ldg(reinterpret_cast<const uint32_t *>(base + at.words))
+                             : __ldg(reinterpret_cast<const uint16_t *>(base + at.words));
     }
 
     // tile: of the warp's first key
@@ -572,11 +569,12 @@ struct PfRaw {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int key = lane / kChunks + kStep * i;
+            const uint32_t word = __shfl_sync(0xffffffffu, words, key);
             uint32_t z[kGroups], sc[kGroups];
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
-                z[g] = P::zeros(word[i] >> (16 * g));
-                sc[g] = P::scales(word[i] >> (16 * g));
+                z[g] = P::zeros(word >> (16 * g));
+                sc[g] = P::scales(word >> (16 * g));
             }
             const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
             uint32_t y[4][4];
@@ -727,7 +725,9 @@ __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfPara
             bool ok = !(pp.debug & kDebugNoProducer);
             const volatile PfItem *item = ok ? pf_item(pp, sh, 0) : nullptr;
             int b = 0, h = 0, from = 0, to = 0, spent = 0;  // keys that the item's rows see, from its first unit's first on
-            int base = 0, page[2], row[2], next[2], next_row[2];
+            int base = 0, next[2], next_row[2];
+            const int block_bytes = p.c.page_size * kv4_row_bytes(D);
+            PfPlace at;
             // the pages of the warp's two runs of unit u, as the table has them
             auto look = [&](int u) {
 #pragma unroll
@@ -740,16 +740,23 @@ __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfPara
                 }
             };
             auto turn_to = [&](int u) {  // what look found
+                const int j0 = u * kPfKeys + first_key;
 #pragma unroll
                 for (int run = 0; run < 2; ++run) {
-                    const int j = u * kPfKeys + first_key + 16 * run;
-                    page[run] = next[run];
-                    row[run] = next_row[run];
-                    if ((unsigned)page[run] >= (unsigned)p.c.num_pages) {
+                    const int j = j0 + 16 * run;
+                    at.codes[run] = -1;
+                    if ((unsigned)next[run] >= (unsigned)p.c.num_pages) {
                         if (j < to && j + 16 > from) set_status(p.status, MC_ERR_RANGE);
-                        page[run] = -1;
+                    } else {
+                        at.codes[run] = next[run] * p.c.page_stride + (int64_t)h * block_bytes +
+                                        ((next_row[run] + lane / PfRaw<D>::kChunks) * kv4_code_bytes(D) + 16 * (lane % PfRaw<D>::kChunks));
                     }
                 }
+                const int run = lane >> 4, page = run ? next[1] : next[0], row = run ? next_row[1] : next_row[0];
+                at.words = (unsigned)page < (unsigned)p.c.num_pages && j0 + lane >= from && j0 + lane < to
+                               ? page * p.c.page_stride + (int64_t)h * block_bytes +
+                                     (p.c.page_size * kv4_code_bytes(D) + (row + (lane & 15)) * kv4_word_bytes(D))
+                               : -1;
             };
             auto enter = [&]() {
                 b = item->b;
@@ -771,21 +778,17 @@ __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfPara
             PfRaw<D> k, v;
             int n = 0, u = 0;
             PfOrder order(p, kKeyBytes, sh->item[0], sh->run, 0);
-            auto load = [&](PfRaw<D> &x, const uint16_t *side) {
-                const int at = u * kPfKeys + first_key;
-                x.load(p.c, side, page, row, h, from - at, to - at, lane);
-            };
             if (item) {
                 enter();
                 n = item->n;
                 u = order.unit(0);
                 look(u);
                 turn_to(u);
-                load(k, p.c.k);
+                k.load(p.c.k, at);
             }
             for (int turn = 0; ok && n > 0;) {
                 for (int i = 0; ok && i < n; ++i) {
-                    load(v, p.c.v);
+                    v.load(p.c.v, at);
                     if (i + 1 < n) {
                         u = order.unit(i + 1);
                         look(u);
@@ -807,7 +810,7 @@ __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfPara
                     }
                     if (n) {
                         turn_to(u);
-                        load(k, p.c.k);
+                        k.load(p.c.k, at);
                     }
                     put(v);
                     if (i < 0) break;

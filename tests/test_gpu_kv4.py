@@ -345,6 +345,41 @@ def test_prefill_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap
     ref.assert_attention(got, lse, want, dtype, 1025, 5.0, rows=slice(0, n))
 
 
+def _far(mc, blocks, **kw):
+    """(cache, batch) with tables of 12288 keys and more, their last entries no pages."""
+    cache, batch = blocks.device(mc, **kw)
+    B = blocks.B
+    table = torch.full((len(B.lens), -(-12288 // B.page)), -7, dtype=torch.int32)
+    table[:, :B.table.shape[1]] = B.table
+    assert B.cu[-1] * 1.0 * table.shape[1] * B.page / 256 / 128 > 4096 / 20
+    return cache, mc.KVBatch(batch._keep[0], table.cuda(), batch._keep[2], B.tokens)
+
+
+@pytest.mark.parametrize("page_of", [0, 17])
+def test_a_long_prompt_with_a_page_outside_the_pool(mc, page_of):
+    """It reads as zeros and is recorded, and what the workspace holds from before does not show."""
+    lens, new, heads, kv = [600, 300], [400, 300], 48, 2
+    ok = ref.Batch(lens, new, kv, 16, 64, "bf16", 111)
+    blocks = ref4.fast_blocks(ok)
+    q = ok.randn(ok.tokens, heads, 64)
+    cache, batch = _far(mc, blocks)
+    ws = mc.attn4_workspace(cache, heads)
+    got, lse = mc.attn4_prefill(cache, batch, q.cuda(), with_lse=True, workspace=ws)
+    mc.check_status(ws)
+    ref.assert_attention(got, lse, ref.attention(ok, q, 0.125), "bf16", 600, 5.0)
+    for bad in (ok.k.shape[0], -1, 2 ** 31 - 1, -2 ** 31):
+        table = batch._keep[1].clone()
+        table[0, page_of] = bad
+        out, out_lse = mc.attn4_prefill(cache, mc.KVBatch(batch._keep[0], table, batch._keep[2], ok.tokens), q.cuda(), with_lse=True, workspace=ws)
+        _reported(mc, ws)
+        assert torch.equal(out[400:], got[400:])
+    zero = ref.Batch(lens, new, kv, 16, 64, "bf16", 111)
+    ref4.fast_blocks(zero)
+    zero.k[zero.table[0, page_of].long()] = 0
+    zero.v[zero.table[0, page_of].long()] = 0
+    ref.assert_attention(out, out_lse, ref.attention(zero, q, 0.125), "bf16", 600, 5.0)
+
+
 @pytest.mark.parametrize("heads,kv,dim,dtype,page,softcap,window,bias,prefix,nan", [
     (32, 2, 128, "bf16", 16, 0.0, 0, False, False, False),
     (24, 1, 64, "fp16", 48, 0.0, 0, False, True, False),
@@ -355,12 +390,12 @@ def test_prefill_matches_its_definition(mc, heads, kv, dim, dtype, page, softcap
     (20, 1, 64, "fp16", 16, 20.0, 100, False, False, False),
 ])
 def test_prompts_of_many_rows(mc, heads, kv, dim, dtype, page, softcap, window, bias, prefix, nan):
-    """More than 1024 rows a sequence, which is where a workspace with room for prompts has their keys unpacked
-    first: strided queries and outputs, more new tokens than the length, sequences without tokens or keys, hidden groups of
+    """1024 rows a sequence and more, with tables that reach far, which is where a workspace with room for prompts has
+    their keys unpacked first: strided queries and outputs, more new tokens than the length, sequences without tokens or keys, hidden groups of
     NaN, pages that a window has left behind; and again over what the call before left in the workspace."""
     lens, new, pre = [0, 3, 130, 300, 511, 9, 700, 64], [2, 3, 130, 1, 129, 12, 400, 0], [0, 1, 64, 70, 299, 4, 650, 64]
     B = ref.Batch(lens, new, kv, page, dim, dtype, 6, pad_tokens=2)
-    assert -(-B.tokens // len(lens)) * (heads // kv) > 1024
+    assert -(-B.tokens // len(lens)) * (heads // kv) >= 1024
     if nan:
         for b, length in enumerate(lens):
             if new[b] > 1 and length:
@@ -377,7 +412,7 @@ def test_prompts_of_many_rows(mc, heads, kv, dim, dtype, page, softcap, window, 
             for p in blocks.pools:
                 p[B.table[b, :gone].long()] = 0xff
             B.table[b, :gone] = -1
-    cache, batch = blocks.device(mc, interleave=True)
+    cache, batch = _far(mc, blocks, interleave=True)
     ws = mc.attn4_workspace(cache, heads)
     ws[256 + (1 << 20):] = 0xff  # (what a call leaves there is any bits)
     dev = wide.cuda()[:, 8:].unflatten(1, (heads, dim))
