@@ -306,7 +306,7 @@ size_t mc_kv_plan_workspace_size(int seqs)
         set_error(MC_ERR_INVALID_ARG, "%d sequences", seqs);
         return 0;
     }
-    return 256 + (size_t)seqs * 8;
+    return 256 + 16 + (size_t)seqs * 8;
 }
 
 int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, const uint8_t *done, int seqs, int tokens,
@@ -349,9 +349,10 @@ int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, 
     p.slots = slots;
     p.state_out = state_out;
     p.status = (int32_t *)workspace;
-    p.base = (int32_t *)((uint8_t *)workspace + 256);
+    // (nothing but the status word in the first 256 bytes: the attentions keep a count there)
+    p.counts = (int64_t *)((uint8_t *)workspace + 256);
+    p.base = (int32_t *)(p.counts + 2);
     p.length = p.base + seqs;
-    p.counts = (int64_t *)((uint8_t *)workspace + 128);
     p.alone = seqs <= kPlanThreads && tokens <= kPlanFew && (!done || (int64_t)seqs * table_width <= kPlanEntries);
     cudaStream_t st = (cudaStream_t)stream;
     profile_begin(kKPlan, st);

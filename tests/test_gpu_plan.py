@@ -222,6 +222,30 @@ def test_another_stream_and_other_sizes_through_one_workspace(mc):
         e.same(b, e.step(add, None, sum(add)), b.step(add, None, sum(add)))
 
 
+def test_a_workspace_of_the_attentions_serves_the_plan_too(mc):
+    """Its status word, and a count that they keep between calls, stay what they are."""
+    g = torch.Generator().manual_seed(31)
+    pools = [torch.zeros(300, 2, mc.kv4_block_size(16, 64), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = mc.KVCache4(*pools, 16, 64)
+    ws = mc.attn4_workspace(cache, 32, prompts=False)
+    a = Account(1, 256, 300, 16, 29)
+    d = Device(mc, a)
+    d.ws = ws
+    outs = []
+    x = [torch.randn(4200, n, 64, generator=g).to(torch.bfloat16).cuda() for n in (32, 2, 2)]
+    for _ in range(3):  # a prompt of many items, which a common count deals, after a plan of two launches
+        a.lens[0], a.taken, a.returned = 0, 0, 300
+        d.lens.zero_(), d.pool.state.copy_(torch.tensor([0, 300]))
+        want = a.step([4000], None, 4200)
+        plan = d.step([4000], None, 4200)
+        d.same(a, plan, want)
+        batch = mc.KVBatch(plan.lens, d.table, plan.cu_q, 4200)
+        q = mc.kv4_append(cache, batch, *x, workspace=ws)
+        outs.append(mc.attn4_prefill(cache, batch, q, workspace=ws)[:4000].clone())
+        mc.check_status(ws)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
 def test_replayed_steps(mc):
     """A captured step, in place, replayed: each replay is the next step."""
     a = Account(20, 6, 200, 16, 13)
