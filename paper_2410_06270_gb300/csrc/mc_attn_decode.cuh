@@ -97,8 +97,8 @@ __device__ __forceinline__ uint32_t transposed8x8(uint32_t a)
     return r;
 }
 
-// The same without a hint: what the hint takes (two moves to uniform registers a copy) is a tenth of the time of a step
-// of the 4-bit cache.
+// The same without a hint, which costs instructions of its own: two a copy, 18 of a step's 790 over the 4-bit cache by the
+// profiler's counters.
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(D, Q4, NT)) decode_kerne
     constexpr int kShare = 32 / Sh::kTiles, kRowChunks = Q4 ? Sh::kRow / 16 : 1, kWordChunks = Q4 ? kv4_word_bytes(D) : 1;
     static_assert(!Q4 || kShare >= 2 * kWordChunks, "a lane for each chunk of words");
     constexpr int kKeyStep = kShare / kRowChunks;
-    const int own_tile = lane / kShare, mine16 = lane % kShare, first_key = mine16 / kRowChunks, chunk = mine16 % kRowChunks;
+    const int own_tile = lane / kShare, piece = lane % kShare, first_key = piece / kRowChunks, chunk = piece % kRowChunks;
     auto place = [](int key) { return (key & 8) | (key & 3) << 1 | (key >> 2 & 1); };
     auto fetch_page = [&]() {
         if constexpr (Q4) {
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(D, Q4, NT)) decode_kerne
                 const bool real = page[0] >= 0;  // (zeros, that is scales of 0, where there is no page)
                 const int64_t block = kv4_offset<D>(p.c, max(page[0], 0), ld.h);
                 const uint8_t *k = reinterpret_cast<const uint8_t *>(p.c.k) + block, *v = reinterpret_cast<const uint8_t *>(p.c.v) + block;
-                const int at = page_row * Sh::kRow + 16 * mine16;
+                const int at = page_row * Sh::kRow + 16 * piece;
                 const uint32_t to = ring + slot * Sh::kSlot + 16 * own_tile * Sh::kRow;
                 const uint32_t kt = to + place(first_key) * Sh::kRow + 16 * chunk, vt = to + (Sh::kKeys + first_key) * Sh::kRow;
 #pragma unroll
@@ -430,8 +430,8 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(D, Q4, NT)) decode_kerne
                     copy16(kt + place(kKeyStep * i) * Sh::kRow, k + at + 16 * kShare * i, real);
                     copy16(vt + kKeyStep * i * Sh::kRow + 16 * (D == 128 ? chunk ^ ((first_key + kKeyStep * i) & 2) : chunk), v + at + 16 * kShare * i, real);
                 }
-                if (mine16 < 2 * kWordChunks) {
-                    const int side = mine16 / kWordChunks, c = mine16 % kWordChunks;
+                if (piece < 2 * kWordChunks) {
+                    const int side = piece / kWordChunks, c = piece % kWordChunks;
                     copy16(ring + slot * Sh::kSlot + Sh::kWords + (side * Sh::kKeys + 16 * own_tile) * kv4_word_bytes(D) + 16 * c,
                            (side ? v : k) + p.c.page_size * Sh::kRow + page_row * kv4_word_bytes(D) + 16 * c, real);
                 }
