@@ -255,9 +255,14 @@ struct DecShape {
     static constexpr int kJoin = kDecWarps * 8 * kPitch * 4; // a piece's rows and queries lie over it
     static constexpr bool kQShared = NT > 2;                 // the queries' fragments: shared memory or registers
     static constexpr int kRows0 = kQShared ? NT * (D / 16) * 256 : 0;
-    static constexpr int kTops = kRows0 + 8 * NT * (int)sizeof(Row);  // Q4: largest |q| of each row, as bits
+    static constexpr int kGroups = Q4 ? D / kKv4Group : 1;
+    static constexpr int kTops = kRows0 + 8 * NT * (int)sizeof(Row);  // Q4: largest |q| of each row's groups, as bits
+    // The groups' factors lie beside the queries or in registers, whatever left a kernel the faster (16 sequences of 4000 keys,
+    // beside them / in registers: 24 rows 44.1 / 44.6 us, 32 rows 63.8 / 61.9).
+    static constexpr bool kFactorsShared = NT == 3;
+    static constexpr int kFactors = kTops + 8 * NT * kGroups * 4;
     static constexpr int kSmem = kRing + kJoin;
-    static_assert(kTops + 8 * NT * 4 <= kJoin, "rows of a slice");
+    static_assert(kFactors + 8 * NT * kGroups * 4 <= kJoin && kFactors % 8 == 0, "rows of a slice");
 };
 
 // NT: n-tiles of 8 rows of a slice, 1 to 4.  The products are formed transposed, S^T = K Q^T and
@@ -497,23 +502,30 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(D, Q4, NT)) decode_kerne
         // Where lane t's pairs of a k-step begin.  Q4: step 4 g + 2 w + i of word 2 t + w of group g, its elements 4 i to
         // 4 i + 3 (the order of a product's terms is free, so each lane takes whole words).
         auto column = [](int ks, int t) { return 64 * (ks >> 2) + 8 * (2 * t + (ks >> 1 & 1)) + 4 * (ks & 1); };
-        // Q4: fp16 whatever the type (a code is one LOP3 in it where bf16 needs a shift as well), each row times a power of
-        // two that brings its largest element into 2^7 .. 2^8: exact, but for elements 2^-17 of that one and
-        // less (off by 2^-28 of it).  The second pair of a word's four stands at 16 times its value, so
-        // its queries are a sixteenth.
+        // Q4: fp16 whatever the type (a code is one LOP3 in it where bf16 needs a shift as well), each group of a row
+        // times a power of two that brings its largest element into 2^7 .. 2^8: exact, but for elements 2^-17 of that one
+        // and less (off by 2^-28 of it).  One power for a row would do as well until keys of one group are large where
+        // the row is small.  The second pair of a word's four stands at 16 times its value, so its queries are a
+        // sixteenth.
         uint32_t qf[Sh::kQShared ? 1 : NT][D / 16][2];
-        float rs[Q4 ? NT : 1][2];  // a score's factor: the scale and the row's power of two
+        // the factor of a group's part of a score, the scale and its power of two, of rows 2 t and 2 t + 1
+        uint64_t rs[Q4 && !Sh::kFactorsShared ? NT : 1][Sh::kGroups];
+        float *factors = reinterpret_cast<float *>(smem + Sh::kRing + Sh::kFactors);  // [group][row]
         if constexpr (Q4) {
-            uint32_t *tops = reinterpret_cast<uint32_t *>(smem + Sh::kRing + Sh::kTops);
-            constexpr int kMine = Sh::kQShared ? NT * (D / 16) / kDecWarps : NT * (D / 16);
+            constexpr int kG = Sh::kGroups;
+            uint32_t *tops = reinterpret_cast<uint32_t *>(smem + Sh::kRing + Sh::kTops);  // [row][group]
+            constexpr int kSteps = D / 16, kMine = Sh::kQShared ? NT * kSteps / kDecWarps : NT * kSteps;
+            static_assert(kDecWarps == 4, "the four steps of a group, one a warp");
+            auto nt_of = [](int i) { return (Sh::kQShared ? kDecWarps * i : i) / kSteps; };
+            auto group_of = [](int i) { return (Sh::kQShared ? kDecWarps * i : i) % kSteps / 4; };
             uint2 mine[kMine];
             if (Sh::kQShared) {
-                if (tid < 8 * NT) tops[tid] = 0;
+                if (tid < 8 * NT * kG) tops[tid] = 0;
                 __syncthreads();
             }
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
-                const int x = Sh::kQShared ? warp + kDecWarps * i : i, ks = x % (D / 16), r = 8 * (x / (D / 16)) + g;
+                const int ks = Sh::kQShared ? 4 * group_of(i) + warp : i % kSteps, r = 8 * nt_of(i) + g;
                 const uint16_t *q = query(r);
                 mine[i] = make_uint2(pair(q, column(ks, t4), r), pair(q, column(ks, t4) + 2, r));
             }
@@ -522,47 +534,47 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(D, Q4, NT)) decode_kerne
                 const float a = fabsf(f.x), b = fabsf(f.y);
                 return max(__float_as_uint(a) < 0x7f800000u ? __float_as_uint(a) : 0u, __float_as_uint(b) < 0x7f800000u ? __float_as_uint(b) : 0u);
             };
-            uint32_t top[NT];
+            uint32_t top[NT][kG];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) top[nt] = 0;
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int grp = 0; grp < kG; ++grp) top[nt][grp] = 0;
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
                 const uint32_t w = max(size(mine[i].x), size(mine[i].y));
-                if (Sh::kQShared) atomicMax(tops + 8 * ((warp + kDecWarps * i) / (D / 16)) + g, w);
-                else top[i / (D / 16)] = max(top[i / (D / 16)], w);
+                if (Sh::kQShared) atomicMax(tops + (8 * nt_of(i) + g) * kG + group_of(i), w);
+                else top[nt_of(i)][group_of(i)] = max(top[nt_of(i)][group_of(i)], w);
             }
-            if (Sh::kQShared) {
-                __syncthreads();
+            if (Sh::kQShared) __syncthreads();
+            float up[NT][kG];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) top[nt] = tops[8 * nt + g];
-            } else {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    top[nt] = max(top[nt], __shfl_xor_sync(0xffffffffu, top[nt], 1));
-                    top[nt] = max(top[nt], __shfl_xor_sync(0xffffffffu, top[nt], 2));
+                for (int grp = 0; grp < kG; ++grp) {
+                    uint32_t &most = top[nt][grp];
+                    if (Sh::kQShared) {
+                        most = tops[(8 * nt + g) * kG + grp];
+                    } else {
+                        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                    }
+                    // 2^(7 - e) for a largest element in 2^e .. 2^(e + 1); both powers stay in fp32's normal range
+                    const int e = min(max((int)(most >> 23) - 127, -110), 127), k = 7 - e;
+                    up[nt][grp] = __uint_as_float((uint32_t)(127 + k) << 23);
+                    const float by = __uint_as_float((uint32_t)(127 - k) << 23) * p.scale;
+                    if (!Sh::kFactorsShared) rs[Sh::kFactorsShared ? 0 : nt][grp] = pair2(__shfl_sync(0xffffffffu, by, 8 * t4), __shfl_sync(0xffffffffu, by, 8 * t4 + 4));
+                    else if (warp == 0 && t4 == 0) factors[8 * (NT * grp + nt) + g] = by;
                 }
-            }
-            float up[NT];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                // 2^(7 - e) for a largest element in 2^e .. 2^(e + 1); both powers stay in fp32's normal range
-                const int e = min(max((int)(top[nt] >> 23) - 127, -110), 127), k = 7 - e;
-                up[nt] = __uint_as_float((uint32_t)(127 + k) << 23);
-                const float down = __uint_as_float((uint32_t)(127 - k) << 23);
-#pragma unroll
-                for (int c = 0; c < 2; ++c) rs[nt][c] = __shfl_sync(0xffffffffu, down, 8 * t4 + 4 * c) * p.scale;
-            }
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
-                const int x = Sh::kQShared ? warp + kDecWarps * i : i;
-                const float f = up[Sh::kQShared ? x / (D / 16) : i / (D / 16)];
+                const float f = up[nt_of(i)][group_of(i)];
                 const float2 a = unpack2<BF16>(mine[i].x), b = unpack2<BF16>(mine[i].y);
                 const uint2 h = make_uint2(pack2<false>(a.x * f, a.y * f), pack2<false>(b.x * f * 0.0625f, b.y * f * 0.0625f));
                 if (Sh::kQShared) {
-                    qs[x * 32 + lane] = h;
+                    qs[(warp + kDecWarps * i) * 32 + lane] = h;
                 } else {
-                    qf[Sh::kQShared ? 0 : i / (D / 16)][i % (D / 16)][0] = h.x;
-                    qf[Sh::kQShared ? 0 : i / (D / 16)][i % (D / 16)][1] = h.y;
+                    qf[Sh::kQShared ? 0 : nt_of(i)][i % kSteps][0] = h.x;
+                    qf[Sh::kQShared ? 0 : nt_of(i)][i % kSteps][1] = h.y;
                 }
             }
         } else if (Sh::kQShared) {
@@ -661,13 +673,21 @@ __global__ void __launch_bounds__(kDecThreads, dec_ctas(D, Q4, NT)) decode_kerne
                                 }
                             }
                         }
+                        // (the two factors first: queries near one end of the range meet keys near the other)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                float sum = s[0][nt][0][c] * kv4_scale(k_words[kt][c >> 1]);
-                                if (kChains == 2) sum = fmaf(s[0][nt][kChains - 1][c], kv4_scale(k_words[kt][c >> 1] >> 16), sum);
-                                x[kt][nt][c] = sum * rs[nt][c & 1];
+                            for (int i = 0; i < 2; ++i) {
+                                uint64_t sum = 0;
+#pragma unroll
+                                for (int grp = 0; grp < kChains; ++grp) {
+                                    const float f = kv4_scale(k_words[kt][i] >> (16 * grp));
+                                    const uint64_t by = mul2(Sh::kFactorsShared ? *reinterpret_cast<const uint64_t *>(factors + 8 * (NT * grp + nt) + 2 * t4)
+                                                                                : rs[Sh::kFactorsShared ? 0 : nt][grp], pair2(f, f));
+                                    const uint64_t part = pair2(s[0][nt][grp][2 * i], s[0][nt][grp][2 * i + 1]);
+                                    sum = grp == 0 ? mul2(part, by) : fma2(part, by, sum);
+                                }
+                                unpair2(sum, x[kt][nt][2 * i], x[kt][nt][2 * i + 1]);
                             }
                     }
                 } else {

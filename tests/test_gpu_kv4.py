@@ -276,6 +276,29 @@ def test_queries_of_any_size(mc, dim, dtype, heads):
         assert ((lse.double().cpu() - want[1]).abs() <= 48 * 2.0 ** -24 * 10).all()
 
 
+@pytest.mark.parametrize("heads,new", [(8, 1), (20, 1), (32, 1), (40, 1), (8, 3)])  # queries in registers, in shared memory, many rows, few tokens
+@pytest.mark.parametrize("dtype,queries,keys", [
+    ("bf16", (0, -30), (0, 30)), ("bf16", (-24, 3), (24, -3)), ("bf16", (0, -60), (-20, 40)), ("bf16", (50, -50), (-50, 50)),
+    ("bf16", (-100, -100), (118, 118)), ("bf16", (112, 112), (-94, -94)), ("bf16", (-100, 100), (118, -82)),
+    ("fp16", (0, -12), (0, 12)), ("fp16", (-10, 10), (12, -8))])
+def test_queries_and_keys_far_apart_in_scale(mc, heads, new, dtype, queries, keys):
+    """Groups of small queries against groups of large keys and the other way round, as powers of two for each group: what
+    they add to a score is of the same size.  Scores are those of 128 products of a few units (their sizes 30 at most in
+    sum after the scale), whose fp32 sums are off by 128 * 2^-24 * 30 in the worst case."""
+    B = ref.Batch([300, 77, 5, 130], [new] * 4, 1, 16, 128, dtype, 15)
+    size = lambda e: 2.0 ** torch.tensor(e, dtype=torch.float64).repeat_interleave(64)  # noqa: E731
+    B.k = (B.k.double() * size(keys)).to(B.k.dtype)
+    blocks = ref4.fast_blocks(B)
+    q = (B.randn(4 * new, heads, 128).double() * size(queries)).to(ref.DT[dtype])
+    scale = 0.1 * 2.0 ** -max(a + b for a, b in zip(queries, keys))
+    want = ref.attention(B, q, scale)
+    cache, batch = blocks.device(mc, cu=new > 1)
+    call = mc.attn4_prefill if new > 1 else mc.attn4_decode
+    out, lse = call(cache, batch, q.cuda(), scale=scale, with_lse=True)
+    ref.assert_attention(out, lse, want, dtype, 300, 5.0)
+    assert ((lse.double().cpu() - want[1]).abs() <= 128 * 2.0 ** -24 * 30).all()
+
+
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("below", [9.0, 14.0, 17.0])
 @pytest.mark.parametrize("new,group", [(1, 1), (32, 8)])  # each kernel
