@@ -464,10 +464,12 @@ size_t mc_kv_plan_workspace_size(int seqs);
  *   positions int32 [tokens], slots int64 [tokens] (either may be NULL): position of each new token and its slot,
  *            page * page_size + position % page_size; -1 for rows from cu_q[seqs] on, and as the slot of a token
  *            whose page is outside the pool (MC_ERR_RANGE)
- *   state_out int64 [2]         the counts after the call (may be pool->state)
+ *   state_out int64 [2]         the counts after the call (pool->state, or apart from it: a preview)
  * (nothing for seqs == 0).  lens_out, table and cu_q are what mc_kv_batch takes.  A page that would not fit in the ring is not returned
- * (MC_ERR_RANGE).  Without committing (state_out and lens_out apart from the inputs) the same call may be
- * made again: it writes the same entries. */
+ * (MC_ERR_RANGE).  The call commits where state_out is pool->state.  A preview (state_out and lens_out apart from the
+ * inputs) may be dropped, made again, or followed by the call that commits, with the same results: it enters new pages
+ * behind those in use, but none into the rows of sequences with done[b], whose pages the next call still reads there.
+ * Where such a sequence gets new tokens, its new pages are in a preview's slots alone. */
 int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, const uint8_t *done, int seqs, int tokens,
                int32_t *table, int table_width, int32_t *lens_out, int32_t *cu_q, int32_t *positions, int64_t *slots,
                int64_t *state_out, void *workspace, size_t ws_bytes, void *stream);

@@ -768,14 +768,17 @@ class KVPool:
 
 class KVPlan:
     """A step's lengths (with the new tokens), row boundaries, positions and slots (None where not asked for),
-    and the pool's counts after it; batch: the KVBatch of the appends and the attentions."""
+    and the pool's counts after it; batch: the KVBatch of the appends and the attentions (not of a preview with
+    finished sequences, whose rows of the table are the old ones)."""
 
-    def __init__(self, lens, cu_q, positions, slots, state, table, tokens):
+    def __init__(self, lens, cu_q, positions, slots, state, table, tokens, tabled=True):
         self.lens, self.cu_q, self.positions, self.slots, self.state, self._table, self._tokens = lens, cu_q, positions, slots, state, table, tokens
-        self._batch = None
+        self._batch, self._tabled = None, tabled
 
     @property
     def batch(self):
+        if not self._tabled:
+            _bad("a step with finished sequences that is not committed has no table: the rows of what takes their place are not written")
         if self._batch is None:
             self._batch = KVBatch(self.lens, self._table, self.cu_q, self._tokens)
         return self._batch
@@ -797,11 +800,12 @@ def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=Non
     give their pages back first and start at length 0.  New pages come from the pool and are entered into
     table (int32 [seqs, width]).  A sequence that cannot have its pages, or rows among the `tokens` of the step's
     token arrays (by default: one for each sequence), gets no tokens, and check_status(workspace) raises ERR_RANGE.
-    lens_out: may be lens; without it lens stays as it is.  commit=False leaves the pool's counts as they are: what
-    the step would be.  Returns a KVPlan."""
+    lens_out: may be lens; without it lens stays as it is.  commit=False leaves the pool's counts and the rows of finished
+    sequences as they are: what the step would be, which may be dropped, asked again, or committed by a call after it.
+    Returns a KVPlan."""
     r = (_fast_module or _fast()).plan(pool, table, lens, add, done, tokens, lens_out, positions, slots, commit, workspace)
     if r is not None:
-        return _check(r) if r.__class__ is int else KVPlan(*r[:5], table, r[5])
+        return _check(r) if r.__class__ is int else KVPlan(*r[:5], table, r[5], commit or done is None)
     torch = _torch()
     if table.dim() != 2 or lens.dim() != 1 or table.shape[0] != lens.shape[0]:
         _bad("lens [seqs] and table [seqs, width]")
@@ -828,7 +832,7 @@ def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=Non
                            slot.data_ptr() if slots else None, state.data_ptr(), ws, workspace.numel() * workspace.element_size(), _stream())
     if rc:
         _check(rc)
-    return KVPlan(lens_out, cu_q, pos, slot, state, table, tokens)
+    return KVPlan(lens_out, cu_q, pos, slot, state, table, tokens, commit or done is None)
 
 
 # -------------------------------------------------------- between the blocks --

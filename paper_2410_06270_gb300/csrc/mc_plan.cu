@@ -36,6 +36,7 @@ struct PlanParams {
     int32_t *base, *length;
     int64_t *counts;
     int alone;  // one launch
+    int preview;  // not committed: rows of finished sequences are left as they are, for the next call to read
 };
 
 // What the tokens of a sequence need.
@@ -54,7 +55,8 @@ __device__ __forceinline__ int ring_next(const PlanParams &p, int base, int k)
 }
 
 // Row t of sequence b: position, page and slot.  Tokens before the first new page lie in the last one held, which
-// they fill; the first row of a page enters it into the table.
+// they fill; the first row of a page enters it into the table (a finished sequence's row names the pages that it gives
+// back: only the call that commits writes over it).
 __device__ __forceinline__ void plan_token(const PlanParams &p, int t, int b, const PlanSeq &s)
 {
     const int pos = s.length + (t - s.first);
@@ -63,7 +65,7 @@ __device__ __forceinline__ void plan_token(const PlanParams &p, int t, int b, co
     int page = s.last;
     if (i >= s.held) {
         page = p.ring[ring_next(p, s.base, i - s.held)];
-        if (row == 0) p.table[(int64_t)b * p.table_width + i] = page;
+        if (row == 0 && !(p.preview && p.done[b])) p.table[(int64_t)b * p.table_width + i] = page;
     }
     if (p.positions) p.positions[t] = pos;
     const bool in = (unsigned)page < (unsigned)p.num_pages;
@@ -348,6 +350,7 @@ int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, 
     p.positions = positions;
     p.slots = slots;
     p.state_out = state_out;
+    p.preview = done && state_out != pool->state;
     p.status = (int32_t *)workspace;
     // (nothing but the status word in the first 256 bytes: the attentions keep a count there)
     p.counts = (int64_t *)((uint8_t *)workspace + 256);

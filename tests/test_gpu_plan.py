@@ -196,6 +196,58 @@ def test_a_preview_changes_nothing_but_may_be_repeated(mc):
     assert only.positions is None and only.slots is None
 
 
+REPLACED = [  # prompts of the first step, width, pages, page, new tokens of the second, done
+    ([40, 20], 4, 8, 16, [20, 1], [1, 0]),
+    ([40, 20, 7], 4, 16, 16, [64, 3, 0], [1, 0, 1]),          # longer and shorter than what was there
+    ([2100, 3000, 40], 200, 700, 16, [3000, 1, 1500], [1, 0, 1]),  # two launches
+    ([1 + b % 30 for b in range(1100)], 4, 5000, 16, [1 + b % 40 for b in range(1100)], [b % 3 == 0 for b in range(1100)])]
+
+
+@pytest.mark.parametrize("previews", [1, 2])
+@pytest.mark.parametrize("first,width,pages,page,add,done", REPLACED)
+def test_a_preview_of_replaced_sequences_may_be_repeated_and_committed(mc, first, width, pages, page, add, done, previews):
+    """A finished sequence whose place another takes in the same step: its pages are read from its row, which a call that
+    does not commit leaves as it is."""
+    a = Account(len(first), width, pages, page, 41)
+    d = Device(mc, a)
+    d.same(a, d.step(first, None, sum(first)), a.step(first, None, sum(first)))
+    t_add, t_done, tokens = d.t(add), d.t([int(x) for x in done], torch.uint8), sum(add) + 3
+    rows, old = d.t(done) != 0, d.table.clone()
+    seen = [mc.kv_plan(d.pool, d.table, d.lens, t_add, done=t_done, tokens=tokens, commit=False, workspace=d.ws) for _ in range(previews)]
+    assert torch.equal(d.table[rows], old[rows])
+    with pytest.raises(mc.MCError) as e:  # (its table would name the pages that go back)
+        seen[0].batch
+    assert e.value.code == mc.ERR_INVALID_ARG
+    want = a.step(add, done, tokens)
+    plan = d.step(add, [int(x) for x in done], tokens)
+    d.same(a, plan, want)
+    for p in seen:
+        for name in ("lens", "cu_q", "positions", "slots"):
+            assert torch.equal(getattr(p, name), getattr(plan, name))
+        assert p.state.tolist() == [a.taken, a.returned]
+    free = [a.ring[i % pages] for i in range(a.taken, a.returned)]
+    held = [p for b, n in enumerate(a.lens) for p in a.table[b][:a.pages(n)]]
+    assert sorted(free + held) == list(range(pages))
+    assert torch.equal(plan.batch._keep[1], d.table)
+
+
+def test_a_preview_that_is_dropped_leaves_the_sequence_whole(mc):
+    """Looked at as finished and replaced, then gone on with after all."""
+    a = Account(3, 8, 20, 16, 43)
+    d = Device(mc, a)
+    d.same(a, d.step([40, 20, 16], None, 76), a.step([40, 20, 16], None, 76))
+    mc.kv_plan(d.pool, d.table, d.lens, d.t([90, 1, 1]), done=d.t([1, 0, 1], torch.uint8), tokens=92, commit=False, workspace=d.ws)
+    assert d.fine()
+    cu, positions, slots, fine = a.step([9, 13, 1], None, 23)
+    plan = d.step([9, 13, 1], None, 23)
+    assert plan.cu_q.tolist() == cu and plan.positions.tolist() == positions and plan.slots.tolist() == slots and d.fine() == fine
+    assert plan.lens.tolist() == a.lens and d.pool.state.tolist() == [a.taken, a.returned]
+    for b, n in enumerate(a.lens):
+        assert d.table[b, :a.pages(n)].tolist() == a.table[b][:a.pages(n)]
+    ring = d.pool.ring.tolist()
+    assert [ring[i % 20] for i in range(a.taken, a.returned)] == [a.ring[i % 20] for i in range(a.taken, a.returned)]
+
+
 def test_a_step_without_sequences(mc):
     pool = mc.KVPool(4, 16)
     none, table = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, 3, dtype=torch.int32, device="cuda")
