@@ -4,10 +4,12 @@ prefilled in one ragged batch, then one token per user and step.
     python examples/decoder.py [--layers 2] [--steps 16] [--bits4]
 
 Each layer is  h <- h + Wo attention(RMSNorm(h)),  h <- h + MoE(RMSNorm(h)):  kv_append norms and
-rotates the new queries and keys and writes keys and values to the paged cache, attn_prefill or
-attn_decode reads it, moe_forward is the compressed expert block, and residual_norm is what lies between the
-blocks.  kv_plan hands out the cache's pages as users grow, and takes them back.  With --bits4 the cache holds 4
-bits an element.  The projections are plain torch matrix products, weights are random.
+rotates the new queries and keys and writes keys and values to the paged cache, attn_prefill reads it,
+moe_forward is the compressed expert block, and residual_norm is what lies between the
+blocks.  kv_plan hands out the cache's pages as users grow, and takes them back; its batch says which users have a row
+in the step, so one that it refuses (no page is left, or its table is full) is not in it.  (attn_decode, which takes a token
+of every user, could not leave one out; with a token or a few of each, attn_prefill runs the same kernel.)  With --bits4
+the cache holds 4 bits an element.  The projections are plain torch matrix products, weights are random.
 """
 from __future__ import annotations
 
@@ -54,7 +56,7 @@ class Decoder:
         pages = (users + 1) * width  # (what a user gives back is free from the next step on)
         self.layers = [Layer(seed + i, max_tokens, pages, bits4) for i in range(layers)]
         self.append = mc.kv4_append if bits4 else mc.kv_append
-        self.attend = (mc.attn4_decode, mc.attn4_prefill) if bits4 else (mc.attn_decode, mc.attn_prefill)
+        self.attend = mc.attn4_prefill if bits4 else mc.attn_prefill
         self.hidden = self.layers[0].shape.H
         g = torch.Generator(device="cuda").manual_seed(seed + 1000)
         self.embed, self.head = (torch.randn(VOCAB, self.hidden, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
@@ -73,24 +75,31 @@ class Decoder:
 
     def forward(self, tokens, new=None, over=None):
         """Hidden states after the last layer of `tokens`: new[b] of user b, in order (None: one each).  Users with
-        over[b] are done: their pages go back, and what is new is another user's first text."""
+        over[b] are done: their pages go back, and what is new is another user's first text.  A user that there are no
+        pages for stays as it is and may come again: its hidden states are zeros, and check() says so."""
         add = self.one if new is None else torch.tensor(new, dtype=torch.int32).cuda()
         over = None if over is None else torch.tensor(over, dtype=torch.uint8).cuda()
         plan = mc.kv_plan(self.pool, self.table, self.lens, add, done=over, tokens=tokens.shape[0], lens_out=self.lens,
                           positions=False, slots=False, workspace=self.plan_ws)
-        batch = mc.KVBatch(self.lens, self.table) if new is None else plan.batch
-        attend = self.attend[new is not None]
-        h, T = self.embed[tokens], tokens.shape[0]
+        # row t of the step holds the token `own[t]`: rows close up over the tokens of users that are refused, and as many
+        # behind the last user's are padding
+        T, first = tokens.shape[0], add.cumsum(0) - add
+        row = torch.arange(T, dtype=torch.int32, device="cuda")
+        user = (torch.searchsorted(plan.cu_q, row, right=True) - 1).clamp(max=add.shape[0] - 1)
+        own = (first[user] + row - plan.cu_q[user]).clamp(max=T - 1)
+        h = self.embed[tokens[own]]
         x = mc.rmsnorm(h, self.layers[0].norms[0])
         for i, w in enumerate(self.layers):
             x = (x @ w.qkv).view(T, HEADS + 2 * KV_HEADS, DIM)
-            q = self.append(w.cache, batch, x[:, :HEADS], x[:, HEADS:HEADS + KV_HEADS], x[:, HEADS + KV_HEADS:], rope=self.rope,
+            q = self.append(w.cache, plan.batch, x[:, :HEADS], x[:, HEADS:HEADS + KV_HEADS], x[:, HEADS + KV_HEADS:], rope=self.rope,
                             q_norm=w.norms[2], k_norm=w.norms[3], workspace=self.attn_ws)
-            o = attend(w.cache, batch, q, workspace=self.attn_ws)
+            o = self.attend(w.cache, plan.batch, q, out=torch.zeros_like(q), workspace=self.attn_ws)  # (padding has no attention)
             h, x = mc.residual_norm(o.view(T, -1) @ w.out, h, pre_norm=w.norms[1])
             y = mc.moe_forward(x, w.gate, w.shape, w.bits, w.experts, w.mu, workspace=self.moe_ws)
             h, x = mc.residual_norm(y, h, pre_norm=self.layers[i + 1].norms[0] if i + 1 < len(self.layers) else None)
-        return h
+        out = h.new_zeros(T + 1, self.hidden)
+        out[torch.where(row < plan.cu_q[-1], own, T)] = h
+        return out[:T]
 
     def logits(self, h):
         return (h @ self.head.T).float()

@@ -469,7 +469,10 @@ size_t mc_kv_plan_workspace_size(int seqs);
  * (MC_ERR_RANGE).  The call commits where state_out is pool->state.  A preview (state_out and lens_out apart from the
  * inputs) may be dropped, made again, or followed by the call that commits, with the same results: it enters new pages
  * behind those in use, but none into the rows of sequences with done[b], whose pages the next call still reads there.
- * Where such a sequence gets new tokens, its new pages are in a preview's slots alone. */
+ * Where such a sequence gets new tokens, its new pages are in a preview's slots alone.
+ * A refused sequence has no rows between its boundaries: the appends and mc_attn(4)_prefill, which runs mc_attn(4)_decode's
+ * kernel for few rows, take the step with cu_q.  With cu_q NULL every sequence has a token, at lens[b] - 1: a
+ * refused one's would lie over its last. */
 int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, const uint8_t *done, int seqs, int tokens,
                int32_t *table, int table_width, int32_t *lens_out, int32_t *cu_q, int32_t *positions, int64_t *slots,
                int64_t *state_out, void *workspace, size_t ws_bytes, void *stream);

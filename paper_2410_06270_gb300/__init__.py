@@ -800,6 +800,9 @@ def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=Non
     give their pages back first and start at length 0.  New pages come from the pool and are entered into
     table (int32 [seqs, width]).  A sequence that cannot have its pages, or rows among the `tokens` of the step's
     token arrays (by default: one for each sequence), gets no tokens, and check_status(workspace) raises ERR_RANGE.
+    The plan's batch says which tokens are in the step: rows close up over those of refused sequences.  A
+    KVBatch(lens, table), as attn_decode takes it, is one token of every sequence: appended by it, a refused sequence's would
+    overwrite its last one.  attn_prefill over the plan's batch runs the same kernel for few tokens a sequence.
     lens_out: may be lens; without it lens stays as it is.  commit=False leaves the pool's counts and the rows of finished
     sequences as they are: what the step would be, which may be dropped, asked again, or committed by a call after it.
     Returns a KVPlan."""

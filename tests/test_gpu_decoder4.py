@@ -88,3 +88,41 @@ def test_without_pages_a_step_is_refused_and_reported(decoder):
     with pytest.raises(mc.MCError) as e:
         d.check()
     assert e.value.code == mc.ERR_RANGE and d.lens.tolist() == [32, 29]
+
+
+def _bytes(d, rows):
+    """What the caches hold of a user: its pages of every layer, keys and values."""
+    return [side[rows].clone() for w in d.layers for side in (w.cache.k, w.cache.v)]
+
+
+@pytest.mark.parametrize("bits4", [False, True])
+@pytest.mark.parametrize("new", [None, [1, 1, 1], [3, 2, 4], [2, 5, 1]])
+def test_a_refused_user_keeps_its_cache_and_goes_on(decoder, bits4, new):
+    """The first is out of pages for a step: nothing of its cache changes, the others' rows are those of their own
+    tokens, and when there are pages again it goes on as one that was never refused."""
+    import paper_2410_06270_gb300 as mc
+    n = new or [1, 1, 1]
+    d, e = (decoder.Decoder(2, 3, 64, max_tokens=64, bits4=bits4) for _ in range(2))
+    texts = [_text(m, 60 + m, decoder) for m in (32, 18, 5)]
+    more = [_text(m, 80 + i, decoder) for i, m in enumerate(n)]
+    for x in (d, e):
+        x.forward(torch.cat(texts), [32, 18, 5])
+        x.check()
+    own = d.table[0, :2].long()
+    kept, counts = _bytes(d, own), d.pool.state.clone()
+    d.pool.state[1] = d.pool.state[0]  # no page is free
+    got = d.forward(torch.cat(more), new).split(n)
+    with pytest.raises(mc.MCError) as err:
+        d.check()
+    assert err.value.code == mc.ERR_RANGE and d.lens.tolist() == [32] + [18 + n[1], 5 + n[2]]
+    assert all(torch.equal(x, y) for x, y in zip(_bytes(d, own), kept))
+    want = e.forward(torch.cat(more[1:]), [0] + n[1:]).split(n[1:])
+    for x, y in zip(got[1:], want):
+        assert _rel(x, y) <= 5e-2
+    assert not got[0].any()
+    d.pool.state.copy_(counts)
+    last = [_text(1, 90 + i, decoder) for i in range(3)]
+    x = d.forward(torch.cat([more[0], last[1], last[2]]), [n[0], 1, 1])
+    y = e.forward(torch.cat([more[0], last[1], last[2]]), [n[0], 1, 1])
+    d.check(), e.check()
+    assert _rel(x, y) <= 5e-2
