@@ -551,7 +551,7 @@ int mc_add(const void *a, const void *b, size_t n, void *out, void *stream);
  *   x = h_out / sqrt(mean(h_out^2) + eps) * pre_norm    (pre_norm [H], NULL: none; of h_out as rounded)
  * y, h, h_out, x: [T][H] in dtype (MC_BF16 or MC_FP16), rows y_stride, h_stride, h_out_stride, x_stride elements
  * apart; gate element (t, i) at gate[t * gate_row + i * gate_col], gate_col 0 or 1 (a row, a column, or all of
- * [T][H]).  Arithmetic in fp32.  h_out may be h or y, x may be y; no other overlaps.  H up to 65536; any 2-byte alignment
+ * [T][H]).  Arithmetic in fp32.  h_out may be h or y, x may be y, with the same row stride; no other overlaps.  H up to 65536; any 2-byte alignment
  * (16-byte aligned rows with H a multiple of 8 take wide accesses).
  * With bf16, scales of 1 and neither gate nor post_norm, the results are those of mc_add and mc_rmsnorm. */
 typedef struct {

@@ -854,7 +854,7 @@ def residual_norm(y, h, pre_norm=None, post_norm=None, gate=None, scale: float =
         u = rmsnorm(y) * post_norm            (post_norm [H]; None: u = y)
         h_out = residual_scale * h + scale * gate * u       (gate [1 or T, 1 or H]; None: 1)
         x = rmsnorm(h_out) * pre_norm         (pre_norm [H]; None: no x)
-    Rows may be strided.  h_out may be h or y, x may be y.  Returns (h_out, x)."""
+    Rows may be strided.  h_out may be h or y, x may be y, each with the same strides.  Returns (h_out, x)."""
     r = (_fast_module or _fast()).residual(y, h, pre_norm, post_norm, gate, scale, residual_scale, eps, h_out, x)
     if r is not None:
         return _check(r) if r.__class__ is int else r

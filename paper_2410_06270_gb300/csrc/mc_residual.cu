@@ -328,6 +328,16 @@ extern "C" int mc_residual_norm(const mc_residual_norm_args *a, void *stream)
     if (!a->gate || a->gate_col == 0) narrow &= ~kGate;  // (a gate of one value a row is read as such)
     if (a->x && a->pre_norm && a->x == a->h_out) return set_error(MC_ERR_INVALID_ARG, "x must not be h_out");
     if (a->x && a->pre_norm && a->x == a->h) return set_error(MC_ERR_INVALID_ARG, "x must not be h");
+    // (in place, a row's block writes what it alone has read)
+    const struct {
+        const char *what;
+        const void *to, *from;
+        int64_t to_stride, from_stride;
+    } over[3] = {{"h_out over h", a->h_out, a->h, a->h_out_stride, a->h_stride}, {"h_out over y", a->h_out, a->y, a->h_out_stride, a->y_stride},
+                 {"x over y", a->pre_norm ? a->x : nullptr, a->y, a->x_stride, a->y_stride}};
+    for (const auto &o : over)
+        if (a->T > 1 && o.to == o.from && o.to_stride != o.from_stride)
+            return set_error(MC_ERR_INVALID_ARG, "%s with row strides %lld and %lld", o.what, (long long)o.to_stride, (long long)o.from_stride);
     ResidualParams p = {};
     p.T = a->T;
     p.H = a->H;

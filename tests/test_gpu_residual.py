@@ -159,3 +159,28 @@ def test_many_rows_a_stream_and_a_graph(mc):
     graph.replay()
     want = mc.residual_norm(y, h, pre_norm=one)
     assert torch.equal(res[0], want[0]) and torch.equal(res[1], want[1])
+
+
+@pytest.mark.parametrize("H", [64, 999, 4096, 20000])
+def test_in_place_over_strided_rows(mc, H):
+    """Over rows of a wider tensor with its stride, what comes out apart; over them with another stride, nothing."""
+    g = torch.Generator(device="cuda").manual_seed(H)
+    T = 40
+    y, h = (torch.randn(T, H + 24, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    pre, post = (torch.randn(H, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    kept = [t.clone() for t in (y, h)]
+    want = mc.residual_norm(y[:, :H], h[:, :H], pre_norm=pre, post_norm=post)
+    for over in ({"h_out": h[:, :H], "x": y[:, :H]}, {"h_out": y[:, :H]}):
+        y.copy_(kept[0]), h.copy_(kept[1])
+        got = mc.residual_norm(y[:, :H], h[:, :H], pre_norm=pre, post_norm=post, **over)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(y[:, H:], kept[0][:, H:]) and torch.equal(h[:, H:], kept[1][:, H:])
+    y.copy_(kept[0]), h.copy_(kept[1])
+    flat = [t.view(-1)[:T * H].view(T, H) for t in (y, h)]  # the same first element, rows nearer together
+    for over in ({"h_out": flat[1]}, {"h_out": flat[0]}, {"x": flat[0]}):
+        with pytest.raises(mc.MCError) as e:
+            mc.residual_norm(y[:, :H], h[:, :H], pre_norm=pre, post_norm=post, **over)
+        assert e.value.code == mc.ERR_INVALID_ARG
+    assert torch.equal(y, kept[0]) and torch.equal(h, kept[1])
+    one = mc.residual_norm(y[:1, :H], h[:1, :H], pre_norm=pre, post_norm=post, h_out=flat[1][:1], x=flat[0][:1])
+    assert all(torch.equal(a, b[:1]) for a, b in zip(one, want))

@@ -165,3 +165,16 @@ def test_residual_norms(mc):
     assert call(dtype=2) == mc.ERR_UNSUPPORTED and call(H=65537, ys=65537, hs=65537, os=65537, xs=65537) == mc.ERR_UNSUPPORTED
     assert mc.load().mc_residual_norm(None, None) == mc.ERR_INVALID_ARG
     assert call(T=0, y=None) == mc.OK
+
+
+def test_residual_rows_in_place_keep_their_stride(mc):
+    """Over another operand with another row stride, a row would lie over rows that other blocks still read."""
+    y, h, out, x = 0x100000, 0x110000, 0x120000, 0x130000
+
+    def call(T=3, y=y, h=h, out=out, x=x, ys=64, hs=64, os=64, xs=64, pre=y + 0x8000):
+        a = mc._ResidualC(T, 64, 0, y, h, ys, hs, None, pre, None, 0, 0, 1.0, 1.0, 1e-5, out, x, os, xs)
+        return mc.load().mc_residual_norm(ctypes.addressof(a), None)
+
+    for bad in ({"out": h, "os": 72}, {"out": h, "hs": 72}, {"out": y, "os": 128}, {"out": y, "ys": 65}, {"x": y, "xs": 65}, {"x": y, "ys": 128}):
+        assert call(**bad) == mc.ERR_INVALID_ARG, bad
+        assert "stride" in mc.last_error()
