@@ -591,7 +591,7 @@ def attn4_workspace(cache: KVCache4, q_heads: int, prompts: bool = True):
 
 
 def _kind(cache, bits4):
-    if (cache.__class__ is KVCache4) != bool(bits4):
+    if isinstance(cache, KVCache4) != bool(bits4):
         _bad("a %s where a %s is taken" % (type(cache).__name__, "KVCache4" if bits4 else "KVCache"))
 
 

@@ -80,6 +80,28 @@ def test_binding_refuses_what_c_cannot_see(mc):
     assert _code(mc, mc.attn_workspace, cache, 4) == -1
 
 
+def test_a_users_own_kind_of_cache_is_what_it_derives_from(mc):
+    """A class derived from KVCache4 holds bytes: the 16-bit calls, which would take its strides for elements, refuse it."""
+    class Four(mc.KVCache4):
+        pass
+
+    class Sixteen(mc.KVCache):
+        pass
+
+    k, v = (torch.zeros(4, 2, mc.kv4_block_size(16, 64), dtype=torch.uint8) for _ in range(2))
+    four, sixteen = Four(k, v, 16, 64), Sixteen(*(torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16) for _ in range(2)))
+    batch = _cpu(mc)[1]
+    q, kv = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    for call in (lambda: mc.kv_append(four, batch, q, kv, kv), lambda: mc.attn_decode(four, batch, q), lambda: mc.attn_prefill(four, batch, q),
+                 lambda: mc.attn_workspace(four, 4), lambda: mc.kv4_append(sixteen, batch, q, kv, kv), lambda: mc.attn4_decode(sixteen, batch, q),
+                 lambda: mc.attn4_prefill(sixteen, batch, q), lambda: mc.kv4_read(sixteen, batch), lambda: mc.attn4_workspace(sixteen, 4)):
+        with pytest.raises(mc.MCError, match="is taken") as e:
+            call()
+        assert e.value.code == mc.ERR_INVALID_ARG
+    assert mc.attn4_workspace(four, 4, prompts=False).numel() == mc.attn4_workspace(_cpu(mc)[0], 4, prompts=False).numel()
+    assert mc.attn_workspace(sixteen, 4).numel() > 0
+
+
 def test_host_tensors_are_refused(mc):
     """Before anything is launched: the answer is an argument error, not a launch's."""
     cache, batch = _cpu(mc)
