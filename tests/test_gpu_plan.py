@@ -131,6 +131,30 @@ def test_one_launch_and_two(mc, seqs, tokens):
         d.same(a, d.step(add, done, tokens), a.step(add, done, tokens))
 
 
+@pytest.mark.parametrize("short", [None, "pages", "rows"])
+@pytest.mark.parametrize("seqs", [4095, 4096, 4097, 8193, 9000])
+def test_more_sequences_than_a_block_takes_at_a_time(mc, seqs, short):
+    """Sums that go on from one round of 4096 sequences to the next: finished ones on both sides of its border, and pages
+    or rows that run short behind it (with fewer sequences: at the last ones)."""
+    rng = random.Random(seqs)
+    first = [rng.randint(0, 40) for _ in range(seqs)]
+    add = [rng.choice([0, 1, 17, 30]) for _ in range(seqs)]
+    done = [int(rng.random() < 0.2 or b in (0, 4095, 4096, 8191, 8192, seqs - 1)) for b in range(seqs)]
+    pages = lambda n: -(-n // 16)  # noqa: E731
+    from_ = 4096 + (seqs - 4096) // 2 if seqs > 5000 else seqs - 3  # whose claim is the last that is met
+    need = sum(pages((0 if o else n) + m) - (0 if o else pages(n)) for n, m, o in list(zip(first, add, done))[:from_])
+    held = sum(map(pages, first))
+    a = Account(seqs, 5, held + (need if short == "pages" else 3 * seqs), 16, 47, 5)
+    d = Device(mc, a)
+    d.same(a, d.step(first, None, sum(first)), a.step(first, None, sum(first)))
+    tokens = sum(add[:from_]) if short == "rows" else sum(add) + 9
+    plan, want = d.step(add, done, tokens), a.step(add, done, tokens)
+    assert want[3] == (short is None)
+    d.same(a, plan, want)
+    add = [b % 2 for b in range(seqs)]
+    d.same(a, d.step(add, None, seqs), a.step(add, None, seqs))
+
+
 def test_what_does_not_fit_is_refused_in_order(mc):
     # three pages free: the first takes two, the second wants two and gets none, the third needs none, the fourth
     # wants one more than are left after the second's claim
