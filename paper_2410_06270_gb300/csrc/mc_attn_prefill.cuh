@@ -528,7 +528,6 @@ __device__ __forceinline__ void pf_softmax(uint32_t (&s)[128], uint32_t s_tmem, 
 
 // ------------------------------------------------------------------ kernel --
 
-// QUEUE: the batch may have the items for a queue (the host's bound), so the kernel looks at them.
 // Where a warp's 32 keys of a unit lie in either side of the 4-bit cache: two runs of 16, each in one page.  Byte offsets of
 // the lane's first chunk of codes in each run (negative: no such page, zeros), and of the words of the lane's own key
 // (negative: zeros, as for keys that no row sees).
@@ -594,6 +593,7 @@ struct PfRaw {
     }
 };
 
+// QUEUE: the batch may have the items for a queue (the host's bound), so the kernel looks at them.
 template <int D, bool BF16, int MODE, bool QUEUE, bool Q4>
 __global__ void __launch_bounds__(pf_threads(Q4), 1) prefill_kernel(const PfParams pp, const __grid_constant__ CUtensorMap kmap,
                                                                    const __grid_constant__ CUtensorMap vmap,

@@ -36,12 +36,13 @@ struct PlanParams {
     int32_t *base, *length;
     int64_t *counts;
     int alone;  // one launch
-    int preview;  // not committed: rows of finished sequences are left as they are, for the next call to read
+    int preview;  // not committed: the table's rows of finished sequences stay as they are, for the next call to read
 };
 
 // What the tokens of a sequence need.
 struct PlanSeq {
     int first, length, held, base, last;  // row of its first new token, tokens before, their pages, place in the ring, last page
+    // (base: the complement of the place where the table's row is to stay as it is)
 };
 
 __device__ __forceinline__ int ring_at(int64_t i, int pages) { return (int)((uint64_t)i % (uint32_t)pages); }
@@ -64,8 +65,9 @@ __device__ __forceinline__ void plan_token(const PlanParams &p, int t, int b, co
     const int i = p.page.div(pos, row);
     int page = s.last;
     if (i >= s.held) {
-        page = p.ring[ring_next(p, s.base, i - s.held)];
-        if (row == 0 && !(p.preview && p.done[b])) p.table[(int64_t)b * p.table_width + i] = page;
+        const bool stays = s.base < 0;
+        page = p.ring[ring_next(p, stays ? ~s.base : s.base, i - s.held)];
+        if (row == 0 && !stays) p.table[(int64_t)b * p.table_width + i] = page;
     }
     if (p.positions) p.positions[t] = pos;
     const bool in = (unsigned)page < (unsigned)p.num_pages;
@@ -183,6 +185,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
             rows[0] += got[i];
             const int64_t at = taken + (asked - need[i]);
             base[i] = at >= 0 && at < p.num_pages ? (int)at : ring_at(at, p.num_pages);
+            if (p.preview && over[i]) base[i] = ~base[i];
             if (served && need[i]) took = asked;
             if (real && !served && writes) set_status(p.status, MC_ERR_RANGE);
         }
