@@ -426,7 +426,7 @@ int mc_kv4_read(const mc_kv_cache *cache, const mc_kv_batch *batch, void *k, voi
 /* As mc_attn_decode and mc_attn_prefill.  Where rows are few, each group of 64 elements of a query is multiplied as fp16
  * times a power of two: exact, but for elements 2^-17 (bf16: 2^-20) of the group's largest and less, which are off by
  * 2^-28 of it; times the largest key of a group, 15 s, that is 2^-23 of what half a step s of the grid makes of the
- * group's largest element. */
+ * group's largest element.  What is rounded for the product with v is the probability, in bf16 there times the scale of v's group. */
 int mc_attn4_decode(const mc_kv_cache *cache, const mc_kv_batch *batch, const void *q, int64_t q_stride, int q_heads,
                     const mc_attn_opts *opts, void *out, int64_t out_stride, float *lse, void *workspace,
                     size_t ws_bytes, void *stream);

@@ -165,7 +165,9 @@ static int attention(const mc_kv_cache *cache, const mc_kv_batch *batch, const v
         // batch's tables reach, not for every 256 rows.  Unpacked / in the kernel, us: 3000 tokens of a group of 4 on 8 heads
         // (9000 units) 74 / 102, 509 over 30000 keys (15000) 194 / 250, 256 over 30000 (7500) 126 / 134, 8 x 300 over 4000
         // (10200) 172 / 188, 2048 (4100) 67 / 67; 1024 (1000) 39 / 34, 8 x 256 over 1000 (2000) 71 / 61, 300 over 8000 (2500)
-        // 67 / 58; and 128 rows short of that, 128 over 30000 keys (3800) 106 / 84.
+        // 67 / 58; and 128 rows short of that, 128 over 30000 keys (3800) 106 / 84.  All with tables as wide as the texts: the
+        // host knows no lengths.  What wider ones cost: 8192 tokens, whose tables reach 8192 to 65500 keys 340 to 346, from
+        // 65536 on 544; 256 tokens over 300 keys in a table of 65000 25 where the kernel takes 19.
         const double reach = (double)batch->seqs * batch->table_width * cache->kv_heads * cache->page_size * cache->head_dim * 4;
         const bool few = reach < (double)kUnpackBytes && batch->seqs <= 65535;  // (the sizes below are small numbers)
         const int64_t pages = few ? (int64_t)batch->seqs * batch->table_width : 0;

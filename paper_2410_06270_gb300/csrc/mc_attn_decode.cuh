@@ -26,10 +26,10 @@
 // Q4, the cache in 4 bits (17 D / 16 bytes a key): the same schedule and products, the operands made from codes in
 // registers.  A code is a number of the type as it stands, (2^k + c) - (2^k + z): one LOP3 and half an instruction of
 // subtraction for two.  Q K^T is formed per group of 64 in fp16, whatever the type (LOP3 finds two of a half-word's four
-// codes in place there, bf16 one), and a group's scale multiplies its sum; in the product with V the scale is in the
+// codes in place there, bf16 one), and a group's scale, with the power of two of its queries, multiplies its sum; in the product with V the scale is in the
 // weight (bf16: a weight for each group) or the value (fp16, whose range a weight times a scale could leave).
-// Bound by issue and the integer pipe, not by HBM: 660 instructions for 32 keys of 128 and 8 rows, 330 of them to
-// unpack, issue 49 % and ALU 51 % active.  64 sequences of 8192 keys, 32 heads on 8 of 128, 129 us, 4.4 TB/s (0.65 of
+// Bound by the length of a warp's step, not by HBM: 650 instructions for 32 keys of 128 and 8 rows, 330 of them to
+// unpack, with the two warps a scheduler that the registers allow; no pipe is full (issue 48 %, ALU 51 % active).  64 sequences of 8192 keys, 32 heads on 8 of 128, 129 us, 4.4 TB/s (0.65 of
 // the measured copy rate; the 16-bit cache 310 us); one of 131071 keys 41 us (83); 777 keys 8.5 us.  Four tiles of 16 keys a
 // warp's step, two blocks an SM: 135 us where two tiles and three blocks took 145 (three blocks and four tiles, with
 // O joined a quarter at a time to make room, 128, but short ones longer: 777 keys 9.9 us for 8.6); keys, codes and

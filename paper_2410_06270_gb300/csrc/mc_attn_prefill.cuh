@@ -34,11 +34,11 @@
 // Tensor memory: S (and P) of tile t at column 128 t, O at 256 + 128 t.
 //
 // Q4, the cache in 4 bits: warps 12-15 read the codes and write a tile as exact numbers of the type, in 310 instructions
-// a warp and about 2000 cycles a tile of 128 keys, two tiles a unit: more than the products take where those are back to
-// back.  Beside the 16-bit cache: 64 tokens over 30000 keys 51 / 48 us, 16 x 16 over 4000 71 / 60, 1000 tokens 33 / 29, 240
+// a warp a tile of 128 keys, two tiles a unit; 240 tokens over 30000 keys take 2260 cycles a tile all in all, more than the
+// products where those are back to back (1400).  Beside the 16-bit cache: 64 tokens over 30000 keys 51 / 48 us, 16 x 16 over 4000 71 / 60, 1000 tokens 33 / 29, 240
 // over 30000 134 / 96, 4096 tokens 155 / 104: the last have their keys unpacked before (mc_kv.cu) and come here as a 16-bit
 // cache.  It hangs on registers: with 212 bytes spilled to a local memory that has no L1 left 64 tokens over 30000
-// keys took 76 us.
+// keys took 76 us.  None are spilled without a cap, but 8 bytes by fp16 heads of 128; 50 to 58 with one (the 16-bit kernel 66 to 114).
 #pragma once
 #include <math.h>
 
