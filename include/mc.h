@@ -466,10 +466,10 @@ size_t mc_kv_plan_workspace_size(int seqs);
  *            whose page is outside the pool (MC_ERR_RANGE)
  *   state_out int64 [2]         the counts after the call (pool->state, or apart from it: a preview)
  * (nothing for seqs == 0).  lens_out, table and cu_q are what mc_kv_batch takes.  A page that would not fit in the ring is not returned
- * (MC_ERR_RANGE).  The call commits where state_out is pool->state.  A preview (state_out and lens_out apart from the
- * inputs) may be dropped, made again, or followed by the call that commits, with the same results: it enters new pages
- * behind those in use, but none into the rows of sequences with done[b], whose pages the next call still reads there.
- * Where such a sequence gets new tokens, its new pages are in a preview's slots alone.
+ * (MC_ERR_RANGE).  A preview, a call with both state_out and lens_out apart from the inputs, may be dropped, made again, or
+ * followed by the call that commits, with the same results: it enters new pages behind those in use, but none into the
+ * rows of sequences with done[b], whose pages the next call still reads there.  Where such a sequence gets new tokens,
+ * its new pages are in a preview's slots alone (copying a preview's lengths and counts over the inputs is no commit then).
  * A refused sequence has no rows between its boundaries: the appends and mc_attn(4)_prefill, which runs mc_attn(4)_decode's
  * kernel for few rows, take the step with cu_q.  With cu_q NULL every sequence has a token, at lens[b] - 1: a
  * refused one's would lie over its last. */

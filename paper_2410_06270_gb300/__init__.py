@@ -803,12 +803,12 @@ def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=Non
     The plan's batch says which tokens are in the step: rows close up over those of refused sequences.  A
     KVBatch(lens, table), as attn_decode takes it, is one token of every sequence: appended by it, a refused sequence's would
     overwrite its last one.  attn_prefill over the plan's batch runs the same kernel for few tokens a sequence.
-    lens_out: may be lens; without it lens stays as it is.  commit=False leaves the pool's counts and the rows of finished
-    sequences as they are: what the step would be, which may be dropped, asked again, or committed by a call after it.
-    Returns a KVPlan."""
+    lens_out: may be lens; without it lens stays as it is.  commit=False leaves the pool's counts as they are, and without
+    lens in place the rows of finished sequences too: what the step would be, which may be dropped, asked again, or
+    committed by a call after it.  Returns a KVPlan."""
     r = (_fast_module or _fast()).plan(pool, table, lens, add, done, tokens, lens_out, positions, slots, commit, workspace)
     if r is not None:
-        return _check(r) if r.__class__ is int else KVPlan(*r[:5], table, r[5], commit or done is None)
+        return _check(r) if r.__class__ is int else KVPlan(*r[:5], table, r[5], commit or done is None or r[0].data_ptr() == lens.data_ptr())
     torch = _torch()
     if table.dim() != 2 or lens.dim() != 1 or table.shape[0] != lens.shape[0]:
         _bad("lens [seqs] and table [seqs, width]")
@@ -835,7 +835,7 @@ def kv_plan(pool: KVPool, table, lens, add, done=None, tokens=None, lens_out=Non
                            slot.data_ptr() if slots else None, state.data_ptr(), ws, workspace.numel() * workspace.element_size(), _stream())
     if rc:
         _check(rc)
-    return KVPlan(lens_out, cu_q, pos, slot, state, table, tokens, commit or done is None)
+    return KVPlan(lens_out, cu_q, pos, slot, state, table, tokens, commit or done is None or lens_out.data_ptr() == lens.data_ptr())
 
 
 # -------------------------------------------------------- between the blocks --

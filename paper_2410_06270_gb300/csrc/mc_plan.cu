@@ -354,7 +354,7 @@ int mc_kv_plan(const mc_kv_pool *pool, const int32_t *lens, const int32_t *add, 
     p.positions = positions;
     p.slots = slots;
     p.state_out = state_out;
-    p.preview = done && state_out != pool->state;
+    p.preview = done && state_out != pool->state && lens_out != lens;
     p.status = (int32_t *)workspace;
     // (nothing but the status word in the first 256 bytes: the attentions keep a count there)
     p.counts = (int64_t *)((uint8_t *)workspace + 256);

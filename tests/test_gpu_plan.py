@@ -255,6 +255,18 @@ def test_a_preview_of_replaced_sequences_may_be_repeated_and_committed(mc, first
     assert torch.equal(plan.batch._keep[1], d.table)
 
 
+def test_counts_apart_with_lengths_in_place_are_a_step(mc):
+    """A caller that keeps two sets of counts in turn and its lengths in place: rows of replaced sequences are entered."""
+    a = Account(2, 4, 8, 16, 45)
+    d = Device(mc, a)
+    d.same(a, d.step([40, 20], None, 60), a.step([40, 20], None, 60))
+    want = a.step([20, 1], [1, 0], 21)
+    plan = d.step([20, 1], [1, 0], 21, commit=False)
+    assert torch.equal(plan.batch._keep[1], d.table)
+    d.pool.state.copy_(plan.state)
+    d.same(a, plan, want)
+
+
 def test_a_preview_that_is_dropped_leaves_the_sequence_whole(mc):
     """Looked at as finished and replaced, then gone on with after all."""
     a = Account(3, 8, 20, 16, 43)
